@@ -192,6 +192,96 @@ hif4_status hif4_grouped_gemm_noalloc(const void* A_units, const void* B_units, 
 /* Size in bytes of the built-in scratch array (HIF4_NOALLOC_SCRATCH_BYTES).  Host-only.  */
 size_t hif4_grouped_gemm_noalloc_capacity(void);
 
+/* ---------------------------------------------------------------------------------------------
+ * What stands between two HiF4 linears of a transformer block.  The paper converts the inputs of every linear layer
+ * (Section IV); the calls below produce those inputs and consume the products without a round trip through FP32
+ * matrices: the norms before and after a block, the linear with its epilogue, the gated feed-forward, each with its
+ * backward pass.  Weights are codes and therefore constants here: the backward passes give the gradients of
+ * activations, biases, norm weights and gates, and pass straight through the conversion of the activations.
+ *
+ * All arithmetic outside Algorithm 1 and Eq. 3 is FP32; a result is rounded once, to the type it is stored in.
+ * Matrices that a call writes must not overlap what it reads, except where a parameter says so. */
+typedef enum { HIF4_NORM_NONE = 0, HIF4_NORM_RMS = 1, HIF4_NORM_LAYER = 2 } hif4_norm_kind;
+typedef enum {
+  HIF4_ACT_NONE = 0,
+  HIF4_ACT_RELU = 1,       /* max(z, 0)                                              */
+  HIF4_ACT_SILU = 2,       /* z / (1 + e^-z)                                         */
+  HIF4_ACT_GELU = 3,       /* z Phi(z), Phi the normal distribution function         */
+  HIF4_ACT_GELU_TANH = 4   /* z (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3))) / 2        */
+} hif4_activation;
+
+/* hif4_block_norm -- the norms around a block with its gate and residual, per row of `cols` elements:
+ *     h = res_scale * residual + gate[row / rows_per_gate] * post(x)
+ *     y = pre(h)
+ *   RMS   v * w / sqrt(mean(v^2) + eps)              LAYER   (v - mean v) * w / sqrt(mean((v - mean v)^2) + eps) + b
+ *   x is the output of the block that ends here, `post` the norm on it (NONE: x itself), `pre` the norm in front of
+ *   the next block.  y is taken from h before h is rounded.  */
+typedef struct {
+  int64_t rows, cols;            /* cols <= 32768                                                              */
+  hif4_dtype dt;                 /* type of x, residual, gate, h and y: BF16, FP16 or FP32                     */
+  hif4_dtype dt_w;               /* type of the weights and of the bias                                        */
+  const void* x;                 /* device, [rows, cols], row stride ld_x elements                             */
+  int64_t ld_x;
+  const void* residual;          /* device, [rows, cols], or NULL: no residual                                 */
+  int64_t ld_residual;
+  float res_scale;
+  const void* gate;              /* device, [ceil(rows / rows_per_gate), cols], or NULL: 1                     */
+  int64_t ld_gate;
+  int64_t rows_per_gate;         /* rows that share a row of gates, >= 1 when there is a gate                  */
+  hif4_norm_kind post;
+  const void* post_weight;       /* device, [cols], or NULL: 1                                                 */
+  hif4_norm_kind pre;            /* NONE: y must be NULL (only h is wanted)                                    */
+  const void* pre_weight;        /* device, [cols], or NULL: 1                                                 */
+  const void* pre_bias;          /* device, [cols], or NULL: 0 (LAYER only)                                    */
+  float eps;                     /* >= 0                                                                       */
+  void* h;                       /* device, [rows, cols], or NULL: not stored; may be x or residual itself     */
+  int64_t ld_h;
+  void* y;                       /* device, [rows, cols] of dt, or HiF4 units [rows, cols / 64] (4-byte aligned) */
+  int64_t ld_y;                  /* (elements; not used for units)                                             */
+  int y_units;                   /* 1: y is hif4_quantize of what y would be in dt; cols % 64 == 0             */
+  hif4_round mode;               /* rounding of that conversion                                                */
+} hif4_block_norm_args;
+hif4_status hif4_block_norm(const hif4_block_norm_args* args, void* stream);
+
+/* hif4_block_norm_backward -- gradients of hif4_block_norm from dy (of y), dh (of h, from the residual stream), the
+ * stored h and x.  With n the normalised row of h, rstd its factor, and dn = dy * w:
+ *     dt = dh + rstd * (dn - n mean(dn n) - [LAYER] mean(dn))
+ *     dresidual = res_scale dt,  dweight = sum dy n,  dbias = sum dy,  dgate = sum over the gate's rows of dt post(x)
+ *   and dx likewise through gate and post norm.  Statistics are taken again from h and x (nothing but them is kept
+ *   from the forward pass).  Gradients of weights are FP32 and overwritten; their sums run in an order that depends
+ *   only on the sizes.  Outputs that are NULL are not computed.  */
+typedef struct {
+  int64_t rows, cols;
+  hif4_dtype dt, dt_w;
+  const void* dy;                /* [rows, cols], or NULL: 0 (then pre does not matter)                        */
+  int64_t ld_dy;
+  const void* dh;                /* [rows, cols], or NULL: 0; at least one of dy and dh                        */
+  int64_t ld_dh;
+  const void* h;                 /* [rows, cols] as stored by the forward pass; not read when dy is NULL       */
+  int64_t ld_h;
+  const void* x;                 /* [rows, cols]; needed for post != NONE and for dgate                        */
+  int64_t ld_x;
+  float res_scale;
+  const void* gate;
+  int64_t ld_gate, rows_per_gate;
+  hif4_norm_kind post;
+  const void* post_weight;
+  hif4_norm_kind pre;
+  const void* pre_weight;
+  float eps;
+  void* dx;                      /* [rows, cols] of dt or NULL                                                 */
+  int64_t ld_dx;
+  void* dresidual;               /* [rows, cols] of dt or NULL; dx and dresidual may not be the same           */
+  int64_t ld_dresidual;
+  void* dgate;                   /* [ceil(rows / rows_per_gate), cols] of dt, contiguous, or NULL              */
+  float* dpre_weight;            /* [cols] or NULL                                                             */
+  float* dpre_bias;
+  float* dpost_weight;
+} hif4_block_norm_backward_args;
+hif4_status hif4_block_norm_backward_workspace(int64_t rows, int64_t cols, size_t* bytes);
+hif4_status hif4_block_norm_backward(const hif4_block_norm_backward_args* args, void* workspace, size_t workspace_bytes,
+                                     void* stream);
+
 /* hif4_mse_roundtrip -- the quantization-error experiment of Section III-A for one tensor: convert a BF16 tensor
  * to a 4-bit block format and back, write the image as FP32 and sum the squared error against the source.
  *   HIF4_FMT_HIF4       Algorithm 1 (round-half-to-even), then Eq. 2

@@ -19,6 +19,8 @@ UNIT_ELEMS, UNIT_BYTES = 64, 36
 HIF4_BF16, HIF4_FP32, HIF4_FP16 = 0, 1, 2
 HIF4_RNE, HIF4_RHA = 0, 1
 HIF4_FMT_HIF4, HIF4_FMT_MXFP4, HIF4_FMT_NVFP4, HIF4_FMT_NVFP4_PTS = 0, 1, 2, 3
+HIF4_NORM_NONE, HIF4_NORM_RMS, HIF4_NORM_LAYER = 0, 1, 2
+HIF4_ACT_NONE, HIF4_ACT_RELU, HIF4_ACT_SILU, HIF4_ACT_GELU, HIF4_ACT_GELU_TANH = 0, 1, 2, 3, 4
 HIF4_OK = 0
 
 EXPORTED_SYMBOLS = [
@@ -27,6 +29,7 @@ EXPORTED_SYMBOLS = [
     "hif4_debug_launch_count", "hif4_debug_set_gemm_path", "hif4_grouped_gemm_noalloc", "hif4_grouped_gemm_noalloc_capacity",
     "hif4_linear", "hif4_linear_workspace", "hif4_quantize_transposed", "hif4_debug_wait_timeout",
     "hif4_mse_workspace", "hif4_mse_roundtrip",
+    "hif4_block_norm", "hif4_block_norm_backward", "hif4_block_norm_backward_workspace",
 ]
 
 
@@ -34,6 +37,26 @@ class Hif4Error(RuntimeError):
     def __init__(self, call: str, code: int):
         self.code = code
         super().__init__(f"{call} failed: {status_string(code)} (status {code})")
+
+
+_I64, _VP, _CI, _CF = ctypes.c_int64, ctypes.c_void_p, ctypes.c_int, ctypes.c_float
+
+
+class _BlockNormArgs(ctypes.Structure):
+    _fields_ = [("rows", _I64), ("cols", _I64), ("dt", _CI), ("dt_w", _CI), ("x", _VP), ("ld_x", _I64),
+                ("residual", _VP), ("ld_residual", _I64), ("res_scale", _CF), ("gate", _VP), ("ld_gate", _I64),
+                ("rows_per_gate", _I64), ("post", _CI), ("post_weight", _VP), ("pre", _CI), ("pre_weight", _VP),
+                ("pre_bias", _VP), ("eps", _CF), ("h", _VP), ("ld_h", _I64), ("y", _VP), ("ld_y", _I64),
+                ("y_units", _CI), ("mode", _CI)]
+
+
+class _BlockNormBackwardArgs(ctypes.Structure):
+    _fields_ = [("rows", _I64), ("cols", _I64), ("dt", _CI), ("dt_w", _CI), ("dy", _VP), ("ld_dy", _I64),
+                ("dh", _VP), ("ld_dh", _I64), ("h", _VP), ("ld_h", _I64), ("x", _VP), ("ld_x", _I64),
+                ("res_scale", _CF), ("gate", _VP), ("ld_gate", _I64), ("rows_per_gate", _I64), ("post", _CI),
+                ("post_weight", _VP), ("pre", _CI), ("pre_weight", _VP), ("eps", _CF), ("dx", _VP), ("ld_dx", _I64),
+                ("dresidual", _VP), ("ld_dresidual", _I64), ("dgate", _VP), ("dpre_weight", _VP), ("dpre_bias", _VP),
+                ("dpost_weight", _VP)]
 
 
 def _load() -> ctypes.CDLL:
@@ -71,6 +94,12 @@ def _load() -> ctypes.CDLL:
     L.hif4_mse_workspace.argtypes = [i64, ci, ctypes.POINTER(sz)]
     L.hif4_mse_roundtrip.restype = ci
     L.hif4_mse_roundtrip.argtypes = [vp, i64, ci, vp, vp, vp, sz, vp]
+    L.hif4_block_norm.restype = ci
+    L.hif4_block_norm.argtypes = [ctypes.POINTER(_BlockNormArgs), vp]
+    L.hif4_block_norm_backward_workspace.restype = ci
+    L.hif4_block_norm_backward_workspace.argtypes = [i64, i64, ctypes.POINTER(sz)]
+    L.hif4_block_norm_backward.restype = ci
+    L.hif4_block_norm_backward.argtypes = [ctypes.POINTER(_BlockNormBackwardArgs), vp, sz, vp]
     L.hif4_last_device_status.restype = ci
     L.hif4_last_device_status.argtypes = [vp]
     L.hif4_status_string.restype = ctypes.c_char_p
@@ -317,6 +346,146 @@ def hif4_mse_roundtrip(src: torch.Tensor, fmt: int, want_image: bool = True, wor
     _check("hif4_mse_roundtrip", lib.hif4_mse_roundtrip(src.data_ptr(), n, fmt, image.data_ptr() if want_image else None,
                                                         err.data_ptr(), workspace.data_ptr(), workspace.numel(), _stream(stream)))
     return image, err
+
+
+# ---------------------------------------------------------------------------------------- between two linears of a block
+def _dtype_any(dt: torch.dtype) -> int:
+    code = _TYPE_CODES.get(dt)
+    if code is None:
+        raise TypeError(f"bfloat16, float16 or float32 expected, not {dt}")
+    return code
+
+
+_TYPE_CODES = {torch.bfloat16: HIF4_BF16, torch.float32: HIF4_FP32, torch.float16: HIF4_FP16}
+
+
+def _use(stream, *tensors) -> None:
+    """Memory that this call allocated on the current stream and uses on another one stays reserved until that is done."""
+    if stream is not None and stream != torch.cuda.current_stream():
+        for t in tensors:
+            if t is not None:
+                t.record_stream(stream)
+
+
+def _matrix(t: Optional[torch.Tensor], rows: int, cols: int, dtype: torch.dtype, what: str):
+    """(address, row stride) of a [rows, cols] operand with unit column stride; (None, 0) without one."""
+    if t is None:
+        return None, 0
+    if not t.is_cuda:
+        raise ValueError("the HiF4 library takes device tensors only (no CPU path exists)")
+    if t.dtype != dtype or t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols or (cols > 1 and t.stride(1) != 1):
+        raise ValueError(f"{what}: [{rows}, {cols}] of {dtype} with unit column stride expected, got "
+                         f"{tuple(t.shape)} of {t.dtype}, strides {t.stride()}")
+    ld = t.stride(0)
+    return t.data_ptr(), (ld if rows > 1 or ld >= cols else cols)
+
+
+def _vector(t: Optional[torch.Tensor], n: int, dtype: Optional[torch.dtype], what: str):
+    """Address of a contiguous [n] operand of `dtype`; None without one."""
+    if t is None:
+        return None
+    if not t.is_cuda:
+        raise ValueError("the HiF4 library takes device tensors only (no CPU path exists)")
+    if t.dim() != 1 or t.shape[0] != n or t.dtype != dtype or (n > 1 and t.stride(0) != 1):
+        raise ValueError(f"{what}: contiguous [{n}] of {dtype} expected, got {tuple(t.shape)} of {t.dtype}, strides {t.stride()}")
+    return t.data_ptr()
+
+
+def _gates(gate: Optional[torch.Tensor], rows: int, cols: int, rows_per_gate: int, dtype: torch.dtype):
+    if gate is None:
+        return None, 0
+    if rows_per_gate < 1:
+        raise ValueError("a gate needs rows_per_gate >= 1")
+    return _matrix(gate, -(-rows // rows_per_gate), cols, dtype, "gate")
+
+
+def hif4_block_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None, *,
+                    residual: Optional[torch.Tensor] = None, res_scale: float = 1.0, gate: Optional[torch.Tensor] = None,
+                    rows_per_gate: int = 0, post: int = HIF4_NORM_NONE, post_weight: Optional[torch.Tensor] = None,
+                    pre: int = HIF4_NORM_RMS, eps: float = 1e-5, units: bool = False, mode: int = HIF4_RNE,
+                    out_h: Optional[torch.Tensor] = None, out_y: Optional[torch.Tensor] = None, stream=None):
+    """h = res_scale * residual + gate[row // rows_per_gate] * post(x), y = pre(h): the norms behind and in front of a
+    block with its gate and residual, one pass.  Returns (h, y); y is None for pre = HIF4_NORM_NONE and HiF4 units
+    [rows, cols // 64, 36] with units=True.  h is x itself where nothing changes it and no out_h is given."""
+    if x.dim() != 2:
+        raise ValueError("x: a matrix expected")
+    rows, cols = x.shape
+    dtype = x.dtype
+    px, ldx = _matrix(x, rows, cols, dtype, "x")
+    pr, ldr = _matrix(residual, rows, cols, dtype, "residual")
+    pg, ldg = _gates(gate, rows, cols, rows_per_gate, dtype)
+    wt = next((w.dtype for w in (weight, bias, post_weight) if w is not None), dtype)
+    same = residual is None and gate is None and post == HIF4_NORM_NONE and out_h is None
+    h = None if same else out_h if out_h is not None else torch.empty((rows, cols), dtype=dtype, device=x.device)
+    y = out_y
+    if y is None and pre != HIF4_NORM_NONE:
+        y = (torch.empty((rows, cols // UNIT_ELEMS, UNIT_BYTES), dtype=torch.uint8, device=x.device) if units
+             else torch.empty((rows, cols), dtype=dtype, device=x.device))
+    ph, ldh = _matrix(h, rows, cols, dtype, "out_h")
+    if units and y is not None:
+        if not (y.is_cuda and y.dtype == torch.uint8 and tuple(y.shape) == (rows, cols // UNIT_ELEMS, UNIT_BYTES) and y.is_contiguous()):
+            raise ValueError(f"out_y: contiguous uint8 units [{rows}, {cols // UNIT_ELEMS}, {UNIT_BYTES}] expected")
+        py, ldy = y.data_ptr(), 0
+    else:
+        py, ldy = _matrix(y, rows, cols, dtype, "out_y")
+    if h is None and y is None:
+        return x, None
+    a = _BlockNormArgs(rows, cols, _dtype_any(dtype), _dtype_any(wt), px, ldx, pr, ldr, res_scale, pg, ldg, rows_per_gate, post,
+                       _vector(post_weight, cols, wt, "post_weight"), pre, _vector(weight, cols, wt, "weight"),
+                       _vector(bias, cols, wt, "bias"), eps, ph, ldh, py, ldy, 1 if units else 0, mode)
+    _check("hif4_block_norm", lib.hif4_block_norm(a, _stream(stream)))
+    _use(stream, h, y)
+    return (x if h is None else h), y
+
+
+def hif4_block_norm_backward_workspace(rows: int, cols: int) -> int:
+    n = ctypes.c_size_t(0)
+    _check("hif4_block_norm_backward_workspace", lib.hif4_block_norm_backward_workspace(rows, cols, ctypes.byref(n)))
+    return int(n.value)
+
+
+def hif4_block_norm_backward(dy: Optional[torch.Tensor], h: Optional[torch.Tensor], weight: Optional[torch.Tensor] = None, *,
+                             dh: Optional[torch.Tensor] = None, x: Optional[torch.Tensor] = None, bias: bool = False,
+                             res_scale: float = 1.0, gate: Optional[torch.Tensor] = None, rows_per_gate: int = 0,
+                             post: int = HIF4_NORM_NONE, post_weight: Optional[torch.Tensor] = None,
+                             pre: int = HIF4_NORM_RMS, eps: float = 1e-5, want_dresidual: bool = True,
+                             workspace: Optional[torch.Tensor] = None, stream=None) -> dict:
+    """Gradients of hif4_block_norm from those of its outputs (dy, dh) and the stored h (and x, where there is a post norm
+    or a gate): a dict of dx, dresidual, dgate, dweight, dbias (with bias=True) and dpost_weight; None where the
+    forward call had no such input."""
+    first = dy if dy is not None else dh
+    if first is None or first.dim() != 2:
+        raise ValueError("dy or dh: a matrix expected")
+    rows, cols = first.shape
+    dtype, dev = first.dtype, first.device
+    pdy, lddy = _matrix(dy, rows, cols, dtype, "dy")
+    pdh, lddh = _matrix(dh, rows, cols, dtype, "dh")
+    ph, ldh = _matrix(h, rows, cols, dtype, "h")
+    px, ldx = _matrix(x, rows, cols, dtype, "x")
+    pg, ldg = _gates(gate, rows, cols, rows_per_gate, dtype)
+    wt = next((w.dtype for w in (weight, post_weight) if w is not None), dtype)
+    pw, pwp = _vector(weight, cols, wt, "weight"), _vector(post_weight, cols, wt, "post_weight")
+    d = {"dx": torch.empty((rows, cols), dtype=dtype, device=dev),
+         "dresidual": torch.empty((rows, cols), dtype=dtype, device=dev) if want_dresidual else None,
+         "dgate": torch.empty((gate.shape[0], cols), dtype=dtype, device=dev) if gate is not None else None,
+         "dweight": torch.empty(cols, dtype=torch.float32, device=dev) if weight is not None and dy is not None else None,
+         "dbias": torch.empty(cols, dtype=torch.float32, device=dev) if bias and dy is not None else None,
+         "dpost_weight": torch.empty(cols, dtype=torch.float32, device=dev) if post_weight is not None else None}
+    need = hif4_block_norm_backward_workspace(rows, cols)
+    if workspace is None and need:
+        workspace = torch.empty(need, dtype=torch.uint8, device=dev)
+
+    def at(k):
+        return d[k].data_ptr() if d[k] is not None else None
+
+    a = _BlockNormBackwardArgs(rows, cols, _dtype_any(dtype), _dtype_any(wt), pdy, lddy, pdh, lddh, ph, ldh, px, ldx, res_scale,
+                               pg, ldg, rows_per_gate, post, pwp, pre, pw, eps, at("dx"), cols, at("dresidual"), cols,
+                               at("dgate"), at("dweight"), at("dbias"), at("dpost_weight"))
+    _check("hif4_block_norm_backward", lib.hif4_block_norm_backward(
+        a, workspace.data_ptr() if workspace is not None else None, workspace.numel() if workspace is not None else 0,
+        _stream(stream)))
+    _use(stream, workspace, *d.values())
+    return d
 
 
 def hif4_debug_wait_timeout(budget_ns: int, stream=None) -> None:
