@@ -282,6 +282,73 @@ hif4_status hif4_block_norm_backward_workspace(int64_t rows, int64_t cols, size_
 hif4_status hif4_block_norm_backward(const hif4_block_norm_backward_args* args, void* workspace, size_t workspace_bytes,
                                      void* stream);
 
+/* hif4_linear_act -- the linear layer with its epilogue:
+ *     Y = act(HiF4(X) * W^T + bias) + res_scale * residual
+ * hif4_gated_linear -- the gated feed-forward's first half, two projections of the same activations:
+ *     Y = act(HiF4(X) * W^T + bias) * (HiF4(X) * W_up^T + bias_up) + res_scale * residual
+ * The products are those of hif4_gemm; everything behind them is FP32 until Y is rounded to `dt`.  One token takes the
+ * weight-streaming form, a prompt the tensor-core form, as in hif4_linear.  */
+typedef struct {
+  int64_t M, N, K;               /* K % 64 == 0                                                                */
+  const void* X;                 /* device, [M, K] of dt_x, rows 16-byte aligned, or HiF4 units [M, K / 64]    */
+  int64_t ld_x;                  /* (elements; not used for units)                                             */
+  hif4_dtype dt_x;
+  int x_units;                   /* 1: X holds units already                                                   */
+  hif4_round mode;               /* rounding of the conversions to units                                       */
+  const void* W_units;           /* device, [N, K / 64] units                                                  */
+  const void* W_up_units;        /* the same; hif4_gated_linear only                                           */
+  hif4_dtype dt;                 /* type of bias, residual and Y: BF16, FP16 or FP32                           */
+  const void* bias;              /* device, [N], or NULL                                                       */
+  const void* bias_up;           /* device, [N], or NULL; hif4_gated_linear only                               */
+  hif4_activation act;
+  const void* residual;          /* device, [M, N], or NULL                                                    */
+  int64_t ld_residual;
+  float res_scale;
+  void* Y;                       /* device, [M, N] of dt (may be residual itself), or units [M, N / 64] (4-byte aligned) */
+  int64_t ld_y;
+  int y_units;                   /* 1: Y is hif4_quantize of what it would be in dt; N % 64 == 0               */
+} hif4_linear_act_args;
+/* Device scratch for these arguments (sizes, types and flags are read, no pointer is followed), 256-byte aligned.  */
+hif4_status hif4_linear_act_workspace(const hif4_linear_act_args* args, size_t* bytes);
+hif4_status hif4_linear_act(const hif4_linear_act_args* args, void* workspace, size_t workspace_bytes, void* stream);
+hif4_status hif4_gated_linear_workspace(const hif4_linear_act_args* args, size_t* bytes);
+hif4_status hif4_gated_linear(const hif4_linear_act_args* args, void* workspace, size_t workspace_bytes, void* stream);
+
+/* hif4_linear_act_backward, hif4_gated_linear_backward -- gradients with respect to the activations and the biases from
+ * dY, the weights being constants and the conversion of X passed straight through.  The products are taken again
+ * from X (nothing else is kept from the forward pass):
+ *     dZ = dY * act'(Z),  dX = dZ * W,  dbias = sum over the rows of dZ
+ *     dG = dY * U * act'(G),  dU = dY * act(G),  dX = dG * W + dU * W_up,  dbias = sum dG,  dbias_up = sum dU
+ * (the residual's gradient is res_scale * dY).  dZ, dG and dU enter the last product as sums of BF16 numbers: one for
+ * BF16 gradients, two for FP16 (which hold its 11 bits); sums of biases run over the unrounded values, in an order
+ * that depends only on the sizes.  FP32 gradients are refused (HIF4_ERR_DTYPE).  */
+typedef struct {
+  int64_t M, N, K;
+  const void* X;                 /* as in the forward pass; not read by hif4_linear_act_backward for act NONE   */
+  int64_t ld_x;
+  hif4_dtype dt_x;
+  int x_units;
+  hif4_round mode;
+  const void* W_units;
+  const void* W_up_units;
+  hif4_dtype dt;                 /* type of the biases, dY and dX: BF16 or FP16                                 */
+  const void* bias;
+  const void* bias_up;
+  hif4_activation act;
+  const void* dY;                /* device, [M, N]                                                             */
+  int64_t ld_dy;
+  void* dX;                      /* device, [M, K], or NULL                                                    */
+  int64_t ld_dx;
+  float* dbias;                  /* device, [N], or NULL; overwritten                                          */
+  float* dbias_up;
+} hif4_linear_act_backward_args;
+hif4_status hif4_linear_act_backward_workspace(const hif4_linear_act_backward_args* args, size_t* bytes);
+hif4_status hif4_linear_act_backward(const hif4_linear_act_backward_args* args, void* workspace, size_t workspace_bytes,
+                                     void* stream);
+hif4_status hif4_gated_linear_backward_workspace(const hif4_linear_act_backward_args* args, size_t* bytes);
+hif4_status hif4_gated_linear_backward(const hif4_linear_act_backward_args* args, void* workspace, size_t workspace_bytes,
+                                       void* stream);
+
 /* hif4_mse_roundtrip -- the quantization-error experiment of Section III-A for one tensor: convert a BF16 tensor
  * to a 4-bit block format and back, write the image as FP32 and sum the squared error against the source.
  *   HIF4_FMT_HIF4       Algorithm 1 (round-half-to-even), then Eq. 2

@@ -4,5 +4,6 @@ from .binding import (  # noqa: F401
     hif4_dequantize, hif4_gemm, hif4_gemm_workspace, hif4_grouped_gemm, hif4_grouped_gemm_noalloc, hif4_grouped_gemm_noalloc_capacity, hif4_grouped_gemm_workspace,
     hif4_last_device_status, hif4_linear, hif4_linear_workspace, hif4_packed_bytes, hif4_quantize, hif4_quantize_transposed, hif4_debug_set_gemm_path, hif4_debug_wait_timeout, launch_count, lib, status_string,
     HIF4_ACT_GELU, HIF4_ACT_GELU_TANH, HIF4_ACT_NONE, HIF4_ACT_RELU, HIF4_ACT_SILU, HIF4_NORM_LAYER, HIF4_NORM_NONE, HIF4_NORM_RMS,
-    hif4_block_norm, hif4_block_norm_backward, hif4_block_norm_backward_workspace,
+    hif4_block_norm, hif4_block_norm_backward, hif4_block_norm_backward_workspace, hif4_gated_linear, hif4_gated_linear_backward,
+    hif4_linear_act, hif4_linear_act_backward,
 )

@@ -7,6 +7,7 @@ not been built, importing this module raises.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from typing import Optional
 
@@ -30,6 +31,8 @@ EXPORTED_SYMBOLS = [
     "hif4_linear", "hif4_linear_workspace", "hif4_quantize_transposed", "hif4_debug_wait_timeout",
     "hif4_mse_workspace", "hif4_mse_roundtrip",
     "hif4_block_norm", "hif4_block_norm_backward", "hif4_block_norm_backward_workspace",
+    "hif4_linear_act", "hif4_linear_act_workspace", "hif4_linear_act_backward", "hif4_linear_act_backward_workspace",
+    "hif4_gated_linear", "hif4_gated_linear_workspace", "hif4_gated_linear_backward", "hif4_gated_linear_backward_workspace",
 ]
 
 
@@ -57,6 +60,19 @@ class _BlockNormBackwardArgs(ctypes.Structure):
                 ("post_weight", _VP), ("pre", _CI), ("pre_weight", _VP), ("eps", _CF), ("dx", _VP), ("ld_dx", _I64),
                 ("dresidual", _VP), ("ld_dresidual", _I64), ("dgate", _VP), ("dpre_weight", _VP), ("dpre_bias", _VP),
                 ("dpost_weight", _VP)]
+
+
+class _LinearActArgs(ctypes.Structure):
+    _fields_ = [("M", _I64), ("N", _I64), ("K", _I64), ("X", _VP), ("ld_x", _I64), ("dt_x", _CI), ("x_units", _CI),
+                ("mode", _CI), ("W_units", _VP), ("W_up_units", _VP), ("dt", _CI), ("bias", _VP), ("bias_up", _VP),
+                ("act", _CI), ("residual", _VP), ("ld_residual", _I64), ("res_scale", _CF), ("Y", _VP), ("ld_y", _I64),
+                ("y_units", _CI)]
+
+
+class _LinearActBackwardArgs(ctypes.Structure):
+    _fields_ = [("M", _I64), ("N", _I64), ("K", _I64), ("X", _VP), ("ld_x", _I64), ("dt_x", _CI), ("x_units", _CI),
+                ("mode", _CI), ("W_units", _VP), ("W_up_units", _VP), ("dt", _CI), ("bias", _VP), ("bias_up", _VP),
+                ("act", _CI), ("dY", _VP), ("ld_dy", _I64), ("dX", _VP), ("ld_dx", _I64), ("dbias", _VP), ("dbias_up", _VP)]
 
 
 def _load() -> ctypes.CDLL:
@@ -100,6 +116,12 @@ def _load() -> ctypes.CDLL:
     L.hif4_block_norm_backward_workspace.argtypes = [i64, i64, ctypes.POINTER(sz)]
     L.hif4_block_norm_backward.restype = ci
     L.hif4_block_norm_backward.argtypes = [ctypes.POINTER(_BlockNormBackwardArgs), vp, sz, vp]
+    for name in ("hif4_linear_act", "hif4_gated_linear"):
+        for suffix, args in (("", _LinearActArgs), ("_backward", _LinearActBackwardArgs)):
+            call, query = getattr(L, name + suffix), getattr(L, name + suffix + "_workspace")
+            call.restype = query.restype = ci
+            call.argtypes = [ctypes.POINTER(args), vp, sz, vp]
+            query.argtypes = [ctypes.POINTER(args), ctypes.POINTER(sz)]
     L.hif4_last_device_status.restype = ci
     L.hif4_last_device_status.argtypes = [vp]
     L.hif4_status_string.restype = ctypes.c_char_p
@@ -359,12 +381,16 @@ def _dtype_any(dt: torch.dtype) -> int:
 _TYPE_CODES = {torch.bfloat16: HIF4_BF16, torch.float32: HIF4_FP32, torch.float16: HIF4_FP16}
 
 
-def _use(stream, *tensors) -> None:
-    """Memory that this call allocated on the current stream and uses on another one stays reserved until that is done."""
-    if stream is not None and stream != torch.cuda.current_stream():
-        for t in tensors:
-            if t is not None:
-                t.record_stream(stream)
+def _on_stream(call):
+    """With stream=s the whole call runs under s, allocations included: memory that the caching allocator hands out on one
+    stream may still be written by that stream's pending work when another stream's kernel gets it."""
+    @functools.wraps(call)
+    def wrapped(*args, stream=None, **kw):
+        if stream is None:
+            return call(*args, **kw)
+        with torch.cuda.stream(stream):
+            return call(*args, **kw)
+    return wrapped
 
 
 def _matrix(t: Optional[torch.Tensor], rows: int, cols: int, dtype: torch.dtype, what: str):
@@ -399,11 +425,12 @@ def _gates(gate: Optional[torch.Tensor], rows: int, cols: int, rows_per_gate: in
     return _matrix(gate, -(-rows // rows_per_gate), cols, dtype, "gate")
 
 
+@_on_stream
 def hif4_block_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None, *,
                     residual: Optional[torch.Tensor] = None, res_scale: float = 1.0, gate: Optional[torch.Tensor] = None,
                     rows_per_gate: int = 0, post: int = HIF4_NORM_NONE, post_weight: Optional[torch.Tensor] = None,
                     pre: int = HIF4_NORM_RMS, eps: float = 1e-5, units: bool = False, mode: int = HIF4_RNE,
-                    out_h: Optional[torch.Tensor] = None, out_y: Optional[torch.Tensor] = None, stream=None):
+                    out_h: Optional[torch.Tensor] = None, out_y: Optional[torch.Tensor] = None):
     """h = res_scale * residual + gate[row // rows_per_gate] * post(x), y = pre(h): the norms behind and in front of a
     block with its gate and residual, one pass.  Returns (h, y); y is None for pre = HIF4_NORM_NONE and HiF4 units
     [rows, cols // 64, 36] with units=True.  h is x itself where nothing changes it and no out_h is given."""
@@ -433,8 +460,7 @@ def hif4_block_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias
     a = _BlockNormArgs(rows, cols, _dtype_any(dtype), _dtype_any(wt), px, ldx, pr, ldr, res_scale, pg, ldg, rows_per_gate, post,
                        _vector(post_weight, cols, wt, "post_weight"), pre, _vector(weight, cols, wt, "weight"),
                        _vector(bias, cols, wt, "bias"), eps, ph, ldh, py, ldy, 1 if units else 0, mode)
-    _check("hif4_block_norm", lib.hif4_block_norm(a, _stream(stream)))
-    _use(stream, h, y)
+    _check("hif4_block_norm", lib.hif4_block_norm(a, _stream(None)))
     return (x if h is None else h), y
 
 
@@ -444,12 +470,13 @@ def hif4_block_norm_backward_workspace(rows: int, cols: int) -> int:
     return int(n.value)
 
 
+@_on_stream
 def hif4_block_norm_backward(dy: Optional[torch.Tensor], h: Optional[torch.Tensor], weight: Optional[torch.Tensor] = None, *,
                              dh: Optional[torch.Tensor] = None, x: Optional[torch.Tensor] = None, bias: bool = False,
                              res_scale: float = 1.0, gate: Optional[torch.Tensor] = None, rows_per_gate: int = 0,
                              post: int = HIF4_NORM_NONE, post_weight: Optional[torch.Tensor] = None,
                              pre: int = HIF4_NORM_RMS, eps: float = 1e-5, want_dresidual: bool = True,
-                             workspace: Optional[torch.Tensor] = None, stream=None) -> dict:
+                             workspace: Optional[torch.Tensor] = None) -> dict:
     """Gradients of hif4_block_norm from those of its outputs (dy, dh) and the stored h (and x, where there is a post norm
     or a gate): a dict of dx, dresidual, dgate, dweight, dbias (with bias=True) and dpost_weight; None where the
     forward call had no such input."""
@@ -483,9 +510,134 @@ def hif4_block_norm_backward(dy: Optional[torch.Tensor], h: Optional[torch.Tenso
                                at("dgate"), at("dweight"), at("dbias"), at("dpost_weight"))
     _check("hif4_block_norm_backward", lib.hif4_block_norm_backward(
         a, workspace.data_ptr() if workspace is not None else None, workspace.numel() if workspace is not None else 0,
-        _stream(stream)))
-    _use(stream, workspace, *d.values())
+        _stream(None)))
     return d
+
+
+def _activations(x: torch.Tensor):
+    """(rows, K, address, row stride, type code, 1 for units) of activations [rows, K] or units [rows, K / 64, 36]."""
+    if not x.is_cuda:
+        raise ValueError("the HiF4 library takes device tensors only (no CPU path exists)")
+    if x.dtype == torch.uint8:
+        if x.dim() != 3 or x.shape[2] != UNIT_BYTES or not x.is_contiguous():
+            raise ValueError(f"x: contiguous units [rows, K / {UNIT_ELEMS}, {UNIT_BYTES}] expected, got {tuple(x.shape)}, strides {x.stride()}")
+        return x.shape[0], x.shape[1] * UNIT_ELEMS, x.data_ptr(), 0, HIF4_BF16, 1
+    if x.dim() != 2 or (x.shape[1] > 1 and x.stride(1) != 1):
+        raise ValueError(f"x: a matrix with unit column stride expected, got {tuple(x.shape)}, strides {x.stride()}")
+    rows, K = x.shape
+    ld = x.stride(0)
+    return rows, K, x.data_ptr(), (ld if rows > 1 or ld >= K else K), _dtype_any(x.dtype), 0
+
+
+def _weight(w: torch.Tensor, N: int, K: int, what: str) -> int:
+    if not w.is_cuda:
+        raise ValueError("the HiF4 library takes device tensors only (no CPU path exists)")
+    if w.dtype != torch.uint8 or w.dim() != 3 or w.shape[0] != N or w.shape[1] * UNIT_ELEMS != K or w.shape[2] != UNIT_BYTES or not w.is_contiguous():
+        raise ValueError(f"{what}: contiguous units [{N}, {K // UNIT_ELEMS}, {UNIT_BYTES}] expected, got {tuple(w.shape)} of {w.dtype}")
+    return w.data_ptr()
+
+
+def _run_with_workspace(name: str, args, workspace: Optional[torch.Tensor], device) -> Optional[torch.Tensor]:
+    need = ctypes.c_size_t(0)
+    _check(name + "_workspace", getattr(lib, name + "_workspace")(args, ctypes.byref(need)))
+    if workspace is None and need.value:
+        workspace = torch.empty(need.value, dtype=torch.uint8, device=device)
+    _check(name, getattr(lib, name)(args, workspace.data_ptr() if workspace is not None else None,
+                                    workspace.numel() if workspace is not None else 0, _stream(None)))
+    return workspace
+
+
+def _linear_act(name, x, w_units, w_up, bias, bias_up, residual, res_scale, act, dtype, units, mode, out, workspace):
+    M, K, px, ldx, dt_x, x_units = _activations(x)
+    N = w_units.shape[0]
+    if dtype is None:
+        dtype = out.dtype if out is not None and not units else x.dtype if not x_units else torch.bfloat16
+    pr, ldr = _matrix(residual, M, N, dtype, "residual")
+    if out is None:
+        out = (torch.empty((M, N // UNIT_ELEMS, UNIT_BYTES), dtype=torch.uint8, device=x.device) if units
+               else torch.empty((M, N), dtype=dtype, device=x.device))
+    if units:
+        if out.dtype != torch.uint8 or tuple(out.shape) != (M, N // UNIT_ELEMS, UNIT_BYTES) or not out.is_contiguous() or not out.is_cuda:
+            raise ValueError(f"out: contiguous uint8 units [{M}, {N // UNIT_ELEMS}, {UNIT_BYTES}] expected")
+        py, ldy = out.data_ptr(), 0
+    else:
+        py, ldy = _matrix(out, M, N, dtype, "out")
+    a = _LinearActArgs(M, N, K, px, ldx, dt_x, x_units, mode, _weight(w_units, N, K, "w_units"),
+                       None if w_up is None else _weight(w_up, N, K, "w_up_units"), _dtype_any(dtype),
+                       _vector(bias, N, dtype, "bias"), _vector(bias_up, N, dtype, "bias_up"), act, pr, ldr, res_scale, py, ldy,
+                       1 if units else 0)
+    workspace = _run_with_workspace(name, a, workspace, x.device)
+    return out
+
+
+@_on_stream
+def hif4_linear_act(x: torch.Tensor, w_units: torch.Tensor, bias: Optional[torch.Tensor] = None, *,
+                    residual: Optional[torch.Tensor] = None, res_scale: float = 1.0, act: int = HIF4_ACT_NONE,
+                    dtype: Optional[torch.dtype] = None, units: bool = False, mode: int = HIF4_RNE,
+                    out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """act(HiF4(x) @ W^T + bias) + res_scale * residual in `dtype` (that of x; BF16 where x is units), or its units.
+
+    x is [M, K] BF16 / FP16 / FP32 or units [M, K / 64, 36]; w_units [N, K / 64, 36]; bias [N] and residual [M, N] in `dtype`;
+    `out` may be the residual itself."""
+    return _linear_act("hif4_linear_act", x, w_units, None, bias, None, residual, res_scale, act, dtype, units, mode, out,
+                       workspace)
+
+
+@_on_stream
+def hif4_gated_linear(x: torch.Tensor, w_units: torch.Tensor, w_up_units: torch.Tensor, bias: Optional[torch.Tensor] = None,
+                      bias_up: Optional[torch.Tensor] = None, *, act: int = HIF4_ACT_SILU,
+                      residual: Optional[torch.Tensor] = None, res_scale: float = 1.0, dtype: Optional[torch.dtype] = None,
+                      units: bool = False, mode: int = HIF4_RNE, out: Optional[torch.Tensor] = None,
+                      workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """act(HiF4(x) @ W^T + bias) * (HiF4(x) @ W_up^T + bias_up) + res_scale * residual; arguments as in hif4_linear_act."""
+    return _linear_act("hif4_gated_linear", x, w_units, w_up_units, bias, bias_up, residual, res_scale, act, dtype, units, mode,
+                       out, workspace)
+
+
+def _linear_act_backward(name, dy, x, w_units, w_up, bias, bias_up, act, mode, want_dx, want_dbias, workspace):
+    if dy.dim() != 2:
+        raise ValueError("dy: a matrix expected")
+    M, N = dy.shape
+    dtype, dev = dy.dtype, dy.device
+    pdy, lddy = _matrix(dy, M, N, dtype, "dy")
+    K = w_units.shape[1] * UNIT_ELEMS
+    if x is not None:
+        rows, kx, px, ldx, dt_x, x_units = _activations(x)
+        if rows != M or kx != K:
+            raise ValueError(f"x: {M} rows of {K} activations expected, got {rows} of {kx}")
+    else:
+        px, ldx, dt_x, x_units = None, K, HIF4_BF16, 0
+    dx = torch.empty((M, K), dtype=dtype, device=dev) if want_dx else None
+    db = torch.empty(N, dtype=torch.float32, device=dev) if want_dbias else None
+    dbu = torch.empty(N, dtype=torch.float32, device=dev) if want_dbias and w_up is not None else None
+    a = _LinearActBackwardArgs(M, N, K, px, ldx, dt_x, x_units, mode, _weight(w_units, N, K, "w_units"),
+                               None if w_up is None else _weight(w_up, N, K, "w_up_units"), _dtype_any(dtype),
+                               _vector(bias, N, dtype, "bias"), _vector(bias_up, N, dtype, "bias_up"), act, pdy, lddy,
+                               None if dx is None else dx.data_ptr(), K, None if db is None else db.data_ptr(),
+                               None if dbu is None else dbu.data_ptr())
+    workspace = _run_with_workspace(name, a, workspace, dev)
+    return dx, db, dbu
+
+
+@_on_stream
+def hif4_linear_act_backward(dy: torch.Tensor, x: Optional[torch.Tensor], w_units: torch.Tensor,
+                             bias: Optional[torch.Tensor] = None, *, act: int = HIF4_ACT_NONE, mode: int = HIF4_RNE,
+                             want_dx: bool = True, want_dbias: bool = False, workspace: Optional[torch.Tensor] = None):
+    """(dx, dbias) of hif4_linear_act from dy (BF16 or FP16): dx in the type of dy, dbias FP32; None where not wanted.  The
+    residual's gradient is res_scale * dy.  x may be None for act = HIF4_ACT_NONE."""
+    dx, db, _ = _linear_act_backward("hif4_linear_act_backward", dy, x, w_units, None, bias, None, act, mode, want_dx, want_dbias,
+                                     workspace)
+    return dx, db
+
+
+@_on_stream
+def hif4_gated_linear_backward(dy: torch.Tensor, x: torch.Tensor, w_units: torch.Tensor, w_up_units: torch.Tensor,
+                               bias: Optional[torch.Tensor] = None, bias_up: Optional[torch.Tensor] = None, *,
+                               act: int = HIF4_ACT_SILU, mode: int = HIF4_RNE, want_dx: bool = True, want_dbias: bool = False,
+                               workspace: Optional[torch.Tensor] = None):
+    """(dx, dbias, dbias_up) of hif4_gated_linear from dy (BF16 or FP16); as hif4_linear_act_backward."""
+    return _linear_act_backward("hif4_gated_linear_backward", dy, x, w_units, w_up_units, bias, bias_up, act, mode, want_dx,
+                                want_dbias, workspace)
 
 
 def hif4_debug_wait_timeout(budget_ns: int, stream=None) -> None:
