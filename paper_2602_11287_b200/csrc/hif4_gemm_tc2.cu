@@ -29,23 +29,10 @@
 #include "hif4_quantize_device.cuh"
 #include "hif4_tc_common.cuh"
 #include "hif4_tc2_common.cuh"
+#include "hif4_tc2_dense.cuh"
 
 namespace hif4 {
 namespace {
-
-constexpr int kPairM = 256, kPairN = 256;             // output tile of a CTA pair
-constexpr int kRows = 128;                            // A rows and B rows per CTA
-constexpr int kRawHalfBytes = kRows * kRawRowBytes;   // 18432
-constexpr int kRawStageBytes = 2 * kRawHalfBytes;     // A rows then B rows
-constexpr int kDecHalfBytes = kRows * 128;            // 128 rows x 64 BF16
-constexpr int kDecStageBytes = 2 * kDecHalfBytes;
-constexpr int kRawStages = 2;
-constexpr int kDecStages = 4;                         // one per unit of a raw chunk
-constexpr int kTmemCols = 512;                        // two 256-column accumulators
-
-constexpr int kDecodeWarp0 = 6;
-constexpr int kDecodeThreads = 4 * kRows;             // 512: (A rows + B rows) x 2 unit pairs
-constexpr int kThreads = kDecodeWarp0 * 32 + kDecodeThreads;   // 704
 
 constexpr int kEpiCols = 16;                          // FP32 columns per staged slab (64-byte rows)
 constexpr int kEpiSlabBytes = 32 * kEpiCols * 4;      // 32 rows of one epilogue warp: 2048
@@ -90,101 +77,6 @@ struct Gemm2Params {
   const uint16_t* x;
   int64_t ld_x;
 };
-
-constexpr int kMaxSlices = 4;
-
-struct WorkItem {
-  int m0, n0;           // tile origin
-  int kc0, kc1;         // K = 256 chunks [kc0, kc1)
-  int tail;             // index among the tail tiles, -1 for a whole tile
-  int slice;            // K slice of a tail tile
-};
-// First and last chunk (exclusive) of a pair's run in the balanced rounds, in chunks of the sk_tiles tiles laid end to
-// end.  The runs go to the pairs in descending order (`run` = num_pairs - 1 - pair), so that the pair that waits
-// for its neighbour's part of a shared tile has the higher index: CTAs are handed out in index order, and a
-// grid that is only partly resident still cannot wait for a CTA that has not started.
-__device__ __forceinline__ int balanced_run(const Gemm2Params& p, int pair, int num_pairs, int64_t& c0, int64_t& c1) {
-  const int64_t total = static_cast<int64_t>(p.sk_tiles) * p.num_kc;
-  const int run = num_pairs - 1 - pair;
-  c0 = total * run / num_pairs;
-  c1 = total * (run + 1) / num_pairs;
-  return run;
-}
-__device__ __forceinline__ int num_work_items(const Gemm2Params& p, int pair, int num_pairs) {
-  if (p.sk_tiles > 0) {
-    int64_t c0, c1;
-    balanced_run(p, pair, num_pairs, c0, c1);
-    return p.full_rounds + static_cast<int>((c1 - 1) / p.num_kc - c0 / p.num_kc) + 1;
-  }
-  return p.full_rounds + (pair < p.tail_tiles * p.slices ? 1 : 0);
-}
-__device__ __forceinline__ WorkItem work_item(const Gemm2Params& p, int pair, int num_pairs, int i) {
-  WorkItem w;
-  int t;
-  if (i < p.full_rounds) {
-    t = i * num_pairs + pair;
-    w.kc0 = 0; w.kc1 = p.num_kc; w.tail = -1; w.slice = 0;
-  } else if (p.sk_tiles > 0) {
-    int64_t c0, c1;
-    const int run = balanced_run(p, pair, num_pairs, c0, c1);
-    const int64_t tr = c0 / p.num_kc + (i - p.full_rounds);
-    const int64_t first = tr * p.num_kc;
-    w.kc0 = c0 > first ? static_cast<int>(c0 - first) : 0;
-    w.kc1 = c1 < first + p.num_kc ? static_cast<int>(c1 - first) : p.num_kc;
-    t = p.sk_tile0 + static_cast<int>(tr);
-    if (w.kc0 > 0) { w.tail = run; w.slice = 0; }                        // end of a tile: computed first, stored
-    else if (w.kc1 < p.num_kc) { w.tail = run + 1; w.slice = 1; }        // beginning of a tile: computed last, added
-    else { w.tail = -1; w.slice = 0; }
-  } else {
-    w.tail = pair % p.tail_tiles;
-    w.slice = pair / p.tail_tiles;
-    t = p.full_rounds * num_pairs + w.tail;
-    w.kc0 = static_cast<int>(static_cast<int64_t>(w.slice) * p.num_kc / p.slices);
-    w.kc1 = static_cast<int>(static_cast<int64_t>(w.slice + 1) * p.num_kc / p.slices);
-  }
-  const int mt = t / p.n_tiles;
-  w.m0 = mt * kPairM;
-  w.n0 = (t - mt * p.n_tiles) * kPairN;
-  return w;
-}
-
-// Bounded wait until a word in global memory, written by another CTA after a __threadfence(), has reached
-// `want`.  Returns false when the budget ran out or another thread has already given up.
-__device__ __noinline__ bool wait_count(const unsigned int* counter, unsigned int want, volatile uint32_t* abort_flag) {
-  const uint64_t t0 = global_ns();
-  for (uint32_t it = 1;; ++it) {
-    unsigned int v;
-    asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(counter) : "memory");
-    if (v >= want) return true;
-    __nanosleep(128);
-    if ((it & 63u) == 0u) {
-      if (*abort_flag) return false;
-      if (global_ns() - t0 > kWaitBudgetNs) {
-        *abort_flag = 1u;
-        return false;
-      }
-    }
-  }
-}
-
-// Decodes the two units held in raw words W[0..8] and W[9..17] into decoded stages 2h and 2h+1.  Returns
-// false when a wait gave up.
-__device__ __forceinline__ bool decode_two_units(const uint32_t (&W)[18], const uint32_t (&chunk_addr)[8], uint32_t lut,
-                                                 const DecodeMul& mul, uint32_t dec_empty0, uint32_t dec_full0_leader,
-                                                 uint32_t parity_free, volatile uint32_t* abort_flag) {
-#pragma unroll
-  for (int u = 0; u < 2; ++u) {
-    // warp-uniform outcome, so that the warp barrier below is never reached by a part of the warp
-    if (!__all_sync(0xFFFFFFFFu, mbar_wait(dec_empty0 + 8 * u, parity_free, abort_flag))) return false;
-    decode_unit_balanced(W[9 * u], &W[9 * u + 1], chunk_addr, u * kDecStageBytes, lut, mul);
-    fence_proxy_async_smem();                  // generic-proxy writes -> visible to the tensor core
-    // One remote arrive per warp; the warp barrier orders the other lanes' writes and proxy fences
-    // before it.
-    __syncwarp();
-    if ((threadIdx.x & 31) == 0) mbar_arrive_cluster(dec_full0_leader + 8 * u);
-  }
-  return true;
-}
 
 template <bool kFusedA>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
@@ -245,7 +137,7 @@ gemm_tc2_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
       uint32_t n = 0;
       bool ok = true;
       for (int i = 0; i < n_items && ok; ++i) {
-        const WorkItem w = work_item(p, pair, num_pairs, i);
+        const WorkItem w = work_item<kPairN>(p, pair, num_pairs, i);
         for (int kc = w.kc0; kc < w.kc1; ++kc, ++n) {
           const uint32_t s = n & 1u, ph = (n >> 1) & 1u;
           if (!(ok = mbar_wait(raw_empty + 8 * s, ph ^ 1u, abort_flag, 128))) break;
@@ -263,7 +155,7 @@ gemm_tc2_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
       uint32_t n = 0, tcount = 0;
       bool ok = true;
       for (int it = 0; it < n_items && ok; ++it, ++tcount) {
-        const WorkItem w = work_item(p, pair, num_pairs, it);
+        const WorkItem w = work_item<kPairN>(p, pair, num_pairs, it);
         const uint32_t acc = tcount & 1u, aph = (tcount >> 1) & 1u;
         if (!(ok = mbar_wait_cluster(tmem_empty + 8 * acc, aph ^ 1u, abort_flag))) break;
         tc_fence_after();
@@ -301,7 +193,7 @@ gemm_tc2_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
       const uint32_t sw = (static_cast<uint32_t>(lane) >> 1) & 3u;
       uint32_t slabs = 0;
       for (int it = 0; it < n_items; ++it, ++tcount) {
-        const WorkItem w = work_item(p, pair, num_pairs, it);
+        const WorkItem w = work_item<kPairN>(p, pair, num_pairs, it);
         const uint32_t acc = tcount & 1u, aph = (tcount >> 1) & 1u;
         if (!__all_sync(0xFFFFFFFFu, mbar_wait(tmem_full + 8 * acc, aph, abort_flag, 256))) break;
         tc_fence_after();
@@ -352,7 +244,7 @@ gemm_tc2_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
     } else {
       const bool vec_ok = ((reinterpret_cast<uintptr_t>(p.C) & 15u) == 0) && (p.ldc % 4 == 0);
       for (int it = 0; it < n_items; ++it, ++tcount) {         // (tail tiles are never K-sliced on this path)
-        const WorkItem w = work_item(p, pair, num_pairs, it);
+        const WorkItem w = work_item<kPairN>(p, pair, num_pairs, it);
         const uint32_t acc = tcount & 1u, aph = (tcount >> 1) & 1u;
         if (!__all_sync(0xFFFFFFFFu, mbar_wait(tmem_full + 8 * acc, aph, abort_flag, 256))) break;
         tc_fence_after();
@@ -399,7 +291,7 @@ gemm_tc2_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
     uint32_t n = 0;
     bool ok = true;
     for (int i = 0; i < n_items && ok; ++i) {
-      const WorkItem w = work_item(p, pair, num_pairs, i);
+      const WorkItem w = work_item<kPairN>(p, pair, num_pairs, i);
       for (int kc = w.kc0; kc < w.kc1 && ok; ++kc, ++n) {
         const uint32_t s = n & 1u, ph = (n >> 1) & 1u;
         if (kFusedA && row < kRows) {
@@ -482,55 +374,6 @@ bool make_c_map(CUtensorMap* map, float* C, int64_t M, int64_t N, int64_t ldc) {
 }
 
 }  // namespace
-
-// Tile schedule of the dense pair kernel for this shape on this device (see Gemm2Params).
-struct Tc2Plan {
-  int pairs, full_rounds, tail_tiles, slices, sk_tiles, sk_tile0;
-  size_t flag_bytes, bytes;          // workspace: the slices' completion words
-};
-static Tc2Plan tc2_plan(int64_t M, int64_t N, int64_t K) {
-  Tc2Plan pl{};
-  const int64_t tiles = ceil_div64(M, kPairM) * ceil_div64(N, kPairN);
-  const int64_t max_pairs = sm_count() / 2;
-  pl.pairs = static_cast<int>(tiles < max_pairs ? tiles : max_pairs);
-  pl.slices = 1;
-  if (pl.pairs <= 0 || tiles > 0x7FFFFFFFll) return pl;
-  pl.full_rounds = static_cast<int>(tiles / pl.pairs);
-  pl.tail_tiles = static_cast<int>(tiles % pl.pairs);
-  if (tiles < max_pairs) {            // a single, partial round: all its tiles are "tail" tiles
-    pl.full_rounds = 0;
-    pl.tail_tiles = static_cast<int>(tiles);
-  }
-  if (pl.tail_tiles > 0) {
-    // Slice s starts its epilogue when slice s - 1 has finished its own, which adds about the time of
-    // 3.5 K = 256 chunks per extra slice (measured): take the slice count with the shortest critical path.
-    int64_t s_max = max_pairs / pl.tail_tiles;
-    if (s_max > kMaxSlices) s_max = kMaxSlices;
-    const int64_t chunks = K / 256;
-    int64_t best = 1, best_cost = 2 * chunks;
-    for (int64_t s = 2; s <= s_max; ++s) {
-      const int64_t cost = 2 * ceil_div64(chunks, s) + 7 * (s - 1);       // in half chunks
-      if (cost < best_cost) { best = s; best_cost = cost; }
-    }
-    pl.slices = static_cast<int>(best);
-  }
-  if (pl.full_rounds >= 1 && pl.tail_tiles > 0) {
-    // Several rounds and a partial one: the last whole round and the partial one are balanced chunk by chunk
-    // instead (every pair then works tail_tiles / pairs of a tile longer than the whole rounds take, which is never
-    // more than the K slices of the partial round alone would cost).
-    pl.full_rounds -= 1;
-    pl.sk_tile0 = pl.full_rounds * pl.pairs;
-    pl.sk_tiles = pl.pairs + pl.tail_tiles;
-    pl.tail_tiles = 0;
-    pl.slices = 2;
-    pl.flag_bytes = (static_cast<size_t>(pl.pairs + 1) * 2 * 8 * sizeof(unsigned int) + 255) / 256 * 256;
-    pl.bytes = pl.flag_bytes;
-  } else if (pl.slices > 1) {
-    pl.flag_bytes = (static_cast<size_t>(pl.tail_tiles) * pl.slices * 8 * sizeof(unsigned int) + 255) / 256 * 256;
-    pl.bytes = pl.flag_bytes;
-  }
-  return pl;
-}
 
 size_t gemm_tc2_workspace_bytes(int64_t M, int64_t N, int64_t K) {
   if (M <= 0 || N <= 0 || K <= 0 || K % 256 != 0) return 0;

@@ -2,59 +2,11 @@
 #include "hif4_activation.cuh"
 #include "hif4_common.cuh"
 #include "hif4_gemm_internal.cuh"
+#include "hif4_linear_internal.cuh"
 #include "hif4_vec8.cuh"
 
 namespace hif4 {
 namespace {
-
-struct EpilogueParams {
-  const float *z, *u;               // FP32 products [M, N]; u = nullptr: not gated
-  int64_t M, N;
-  const void *bias, *bias_up;
-  int act;
-  const void* residual;
-  int64_t ld_residual;
-  float res_scale;
-  void* y;
-  int64_t ld_y;
-  int units, rha;
-};
-
-template <typename T>
-__global__ void __launch_bounds__(256) epilogue_kernel(const EpilogueParams p) {
-  const int64_t groups = ceil_div64(p.N, 8);
-  const int64_t idx = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
-  const int64_t row = idx / groups, col0 = (idx - row * groups) * 8;
-  float v[8];
-#pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    v[j] = 0.0f;
-    const int64_t col = col0 + j;
-    if (row < p.M && col < p.N) {
-      float z = p.z[row * p.N + col];
-      if (p.bias) z += to_f32(static_cast<const T*>(p.bias)[col]);
-      float y = activate(z, p.act);
-      if (p.u) {
-        float u = p.u[row * p.N + col];
-        if (p.bias_up) u += to_f32(static_cast<const T*>(p.bias_up)[col]);
-        y *= u;
-      }
-      if (p.residual) y = fmaf(p.res_scale, to_f32(static_cast<const T*>(p.residual)[row * p.ld_residual + col]), y);
-      if (!p.units) static_cast<T*>(p.y)[row * p.ld_y + col] = from_f32<T>(y);
-      v[j] = y;
-    }
-  }
-  if (!p.units) return;
-  const Raw8<T> r = pack8<T>(v);
-  const int g = static_cast<int>(col0 >> 3) & 7;
-  uint32_t meta;
-  const uint32_t code = p.rha ? encode_unit_octet<true>(r, g, meta) : encode_unit_octet<false>(r, g, meta);
-  if (row < p.M) {
-    uint32_t* dst = static_cast<uint32_t*>(p.y) + (row * (p.N / 64) + col0 / 64) * kUnitWords;
-    dst[1 + g] = code;
-    if (g == 0) dst[0] = meta;
-  }
-}
 
 struct EpilogueGradParams {
   float *z, *u;                     // FP32 products [M, N], overwritten by their gradients
@@ -155,6 +107,24 @@ hif4_status plan(int64_t M, int64_t N, int64_t K, bool gated, Scratch& s) {
   return HIF4_OK;
 }
 
+// Forward workspace: packed activations, the pair kernel's shared tiles, and for FP32 units the rows before their
+// conversion (64 FP32 columns of a row do not fit a thread's registers or the kernel's staging buffer).
+struct ForwardScratch {
+  size_t x, pair, y, total;
+  bool rows_first;
+};
+hif4_status forward_plan(const hif4_linear_act_args* a, bool gated, ForwardScratch& s) {
+  s = ForwardScratch{};
+  if (a->M < 0 || a->N < 0 || a->K < 0 || a->K % kUnitElems != 0) return HIF4_ERR_SHAPE;
+  if (a->M == 0 || a->N == 0) return HIF4_OK;
+  if (!linear_tc2_supported(gated, a->M, a->N, a->K)) return HIF4_ERR_SHAPE;
+  s.rows_first = a->y_units && a->dt == HIF4_FP32;
+  s.pair = a->x_units ? 0 : pad256(hif4_packed_bytes(a->M, a->K));
+  s.y = s.pair + pad256(linear_tc2_workspace(gated, a->M, a->N, a->K));
+  s.total = s.y + (s.rows_first ? static_cast<size_t>(a->M) * a->N * 4 : 0);
+  return HIF4_OK;
+}
+
 // The products of X with W (and W_up) as FP32 matrices in the workspace.
 template <typename Args>
 hif4_status products(const Args* a, bool gated, uint8_t* ws, const Scratch& s, void* stream) {
@@ -195,28 +165,29 @@ hif4_status forward(const hif4_linear_act_args* a, bool gated, void* workspace, 
   if (!a->Y) return HIF4_ERR_NULL;
   const size_t e = esize(a->dt);
   if (!is_aligned(a->Y, a->y_units ? 4 : e) || !is_aligned(a->residual, e)) return HIF4_ERR_ALIGN;
-  Scratch s;
-  const hif4_status ps = plan(a->M, a->N, a->K, gated, s);
+  ForwardScratch s;
+  const hif4_status ps = forward_plan(a, gated, s);
   if (ps != HIF4_OK) return ps;
-  if (!workspace || workspace_bytes < s.total) return HIF4_ERR_WORKSPACE;
+  if (s.total > 0 && (!workspace || workspace_bytes < s.total)) return HIF4_ERR_WORKSPACE;
   if (!is_aligned(workspace, 256)) return HIF4_ERR_ALIGN;
   uint8_t* ws = static_cast<uint8_t*>(workspace);
-  const hif4_status pr = products(a, gated, ws, s, stream);
-  if (pr != HIF4_OK) return pr;
-  EpilogueParams p{};
-  p.z = reinterpret_cast<const float*>(ws + s.z);
-  p.u = gated ? reinterpret_cast<const float*>(ws + s.u) : nullptr;
-  p.M = a->M; p.N = a->N; p.bias = a->bias; p.bias_up = a->bias_up; p.act = a->act;
-  p.residual = a->residual; p.ld_residual = a->ld_residual; p.res_scale = a->res_scale;
-  p.y = a->Y; p.ld_y = a->ld_y; p.units = a->y_units; p.rha = a->mode == HIF4_RHA;
-  const int64_t blocks = ceil_div64(a->M * ceil_div64(a->N, 8), 256);
-  if (blocks > 0x7FFFFFFFll) return HIF4_ERR_SHAPE;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  if (a->dt == HIF4_BF16) epilogue_kernel<__nv_bfloat16><<<static_cast<unsigned>(blocks), 256, 0, st>>>(p);
-  else if (a->dt == HIF4_FP16) epilogue_kernel<__half><<<static_cast<unsigned>(blocks), 256, 0, st>>>(p);
-  else epilogue_kernel<float><<<static_cast<unsigned>(blocks), 256, 0, st>>>(p);
-  note_launch();
-  return launch_status();
+  LinearCall c{};
+  c.gated = gated;
+  c.M = a->M; c.N = a->N; c.K = a->K;
+  c.A = a->X; c.B = a->W_units; c.B2 = a->W_up_units;
+  if (!a->x_units) {
+    const hif4_status q = hif4_quantize(a->X, a->dt_x, a->M, a->K, a->ld_x, ws + s.x, a->mode, stream);
+    if (q != HIF4_OK) return q;
+    c.A = ws + s.x;
+  }
+  c.dt = a->dt; c.bias = a->bias; c.bias_up = gated ? a->bias_up : nullptr; c.act = a->act;
+  c.side = a->residual; c.ld_side = a->ld_residual; c.res_scale = a->res_scale;
+  c.y = a->Y; c.ld_y = a->ld_y; c.units = a->y_units ? 1 : 0; c.rha = a->mode == HIF4_RHA;
+  if (!s.rows_first) return launch_linear_tc2(c, ws + s.pair, st);
+  c.y = ws + s.y; c.ld_y = a->N; c.units = 0;
+  const hif4_status pr = launch_linear_tc2(c, ws + s.pair, st);
+  return pr != HIF4_OK ? pr : hif4_quantize(ws + s.y, a->dt, a->M, a->N, a->N, a->Y, a->mode, stream);
 }
 
 template <typename T>
@@ -284,8 +255,17 @@ hif4_status workspace_size(const Args* a, bool gated, size_t* bytes) {
 
 using namespace hif4;
 
-extern "C" hif4_status hif4_linear_act_workspace(const hif4_linear_act_args* args, size_t* bytes) { return workspace_size(args, false, bytes); }
-extern "C" hif4_status hif4_gated_linear_workspace(const hif4_linear_act_args* args, size_t* bytes) { return workspace_size(args, true, bytes); }
+namespace {
+hif4_status forward_workspace(const hif4_linear_act_args* a, bool gated, size_t* bytes) {
+  if (!a || !bytes) return HIF4_ERR_NULL;
+  ForwardScratch s;
+  const hif4_status st = forward_plan(a, gated, s);
+  if (st == HIF4_OK) *bytes = s.total;
+  return st;
+}
+}  // namespace
+extern "C" hif4_status hif4_linear_act_workspace(const hif4_linear_act_args* args, size_t* bytes) { return forward_workspace(args, false, bytes); }
+extern "C" hif4_status hif4_gated_linear_workspace(const hif4_linear_act_args* args, size_t* bytes) { return forward_workspace(args, true, bytes); }
 extern "C" hif4_status hif4_linear_act_backward_workspace(const hif4_linear_act_backward_args* args, size_t* bytes) {
   return workspace_size(args, false, bytes);
 }

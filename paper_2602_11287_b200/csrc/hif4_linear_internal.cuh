@@ -1,0 +1,62 @@
+// Internal launchers behind hif4_linear_act / hif4_gated_linear and their backward passes (arguments already validated).
+#pragma once
+#include <cuda_bf16.h>
+
+#include "hif4_common.cuh"
+#include "hif4_tc_common.cuh"
+
+namespace hif4 {
+
+// One product with what follows it.  Forward: side = residual, y.  Gradient: side = dY, dz and colsum.
+struct LinearCall {
+  bool gated, grad;
+  int64_t M, N, K;
+  const void *A, *B, *B2;           // units
+  int dt;                           // type of bias, side and y
+  const void *bias, *bias_up;
+  int act;
+  const void* side;
+  int64_t ld_side;
+  float res_scale;
+  void* y;
+  int64_t ld_y;
+  int units, rha;
+  __nv_bfloat16* dz;                // planes of [M, ld_dz]: the BF16 parts of dZ (dG, then those of dU), or NULL
+  int64_t ld_dz, dz_plane;
+  float* colsum;                    // [1 or 2][ceil(M / 32)][N], or NULL
+};
+
+namespace {
+struct LinearParams {
+  int64_t M, N;
+  int num_kc, n_tiles, full_rounds, tail_tiles, slices, sk_tiles, sk_tile0;      // schedule (hif4_tc2_dense.cuh)
+  unsigned int* flags;              // [shared tiles][slices][8]: "this epilogue warp's rows of this slice's sums are there"
+  float* partial;                   // [shared tiles][2 ranks][256 columns][128 rows]
+  unsigned int* error_word;
+  DecodeMul mul;
+  int tma;                          // 1: units come through TMA, 0: copied word by word
+  const uint8_t *A, *B, *B2;
+  int64_t pitch;                    // bytes of a row of units
+  int upr;                          // units of a row
+  const void *bias, *bias_up;
+  int act;
+  const void* side;
+  int64_t ld_side;
+  int side_vec;
+  float res_scale;
+  void* y;
+  int64_t ld_y;
+  int y_vec, tma_store, units, rha;
+  __nv_bfloat16* dz;
+  int64_t ld_dz, dz_plane;
+  float* colsum;
+  int64_t colsum_plane;
+};
+}  // namespace
+
+size_t linear_tc2_workspace(bool gated, int64_t M, int64_t N, int64_t K);
+bool linear_tc2_supported(bool gated, int64_t M, int64_t N, int64_t K);
+hif4_status launch_linear_tc2(const LinearCall& c, void* workspace, cudaStream_t st);
+hif4_status launch_linear_tc2_grad(const LinearCall& c, void* workspace, cudaStream_t st);
+
+}  // namespace hif4

@@ -1,0 +1,80 @@
+// Host side of the CTA-pair linear kernel: tensor maps, schedule, launch.
+#pragma once
+#include "hif4_linear_tc2.cuh"
+
+namespace hif4 {
+namespace {
+
+inline bool at16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+
+// View of Y for the TMA stores: boxes of 64 bytes x 32 rows, SWIZZLE_64B.
+template <typename T>
+bool make_y_map(CUtensorMap* map, void* y, int64_t M, int64_t N, int64_t ld) {
+  EncodeTiledFn fn = encode_tiled_fn();
+  if (!fn) return false;
+  const CUtensorMapDataType type = sizeof(T) == 4 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_UINT16;
+  const cuuint64_t dims[2] = {static_cast<cuuint64_t>(N), static_cast<cuuint64_t>(M)};
+  const cuuint64_t strides[1] = {static_cast<cuuint64_t>(ld) * sizeof(T)};
+  const cuuint32_t box[2] = {static_cast<cuuint32_t>(64 / sizeof(T)), 32};
+  const cuuint32_t estr[2] = {1, 1};
+  return fn(map, type, 2, y, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_64B,
+            CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+inline size_t partial_tiles(const Tc2Plan& pl) {
+  return pl.sk_tiles > 0 ? static_cast<size_t>(pl.pairs) + 1 : pl.slices > 1 ? static_cast<size_t>(pl.tail_tiles) : 0;
+}
+constexpr size_t kPartialTileBytes = static_cast<size_t>(kPairM) * kPairN * sizeof(float);
+
+template <bool kGated, bool kGrad, typename T>
+hif4_status launch_linear(const LinearCall& c, void* workspace, cudaStream_t st) {
+  constexpr int kTileN = kGated ? kPairN / 2 : kPairN;
+  static uint64_t smem_opt_in = 0;
+  if (!ensure_dynamic_smem(linear_tc2_kernel<kGated, kGrad, T>, kLinSmemBytes, smem_opt_in)) return HIF4_ERR_CUDA;
+  LinearParams p{};
+  p.M = c.M; p.N = c.N;
+  p.error_word = device_error_word();
+  if (!p.error_word) return HIF4_ERR_CUDA;
+  const int64_t upr = c.K / kUnitElems;
+  p.num_kc = c.K > 0 ? static_cast<int>(ceil_div64(upr, kRawUnits)) : 1;       // K = 0: one chunk of zeros
+  p.n_tiles = static_cast<int>(ceil_div64(c.N, kTileN));
+  const Tc2Plan pl = tc2_plan(c.M, c.N, c.K, kTileN);
+  p.full_rounds = pl.full_rounds; p.tail_tiles = pl.tail_tiles; p.slices = pl.slices;
+  p.sk_tiles = pl.sk_tiles; p.sk_tile0 = pl.sk_tile0;
+  p.mul = make_decode_mul();
+  // no operand byte is read for K = 0, but the copy loop wants an address
+  p.A = static_cast<const uint8_t*>(c.K > 0 ? c.A : p.error_word);
+  p.B = static_cast<const uint8_t*>(c.K > 0 ? c.B : p.error_word);
+  p.B2 = static_cast<const uint8_t*>(c.K > 0 ? c.B2 : p.error_word);
+  p.pitch = upr * kUnitBytes;
+  p.upr = static_cast<int>(upr);
+  CUtensorMap tmA{}, tmB{}, tmB2{}, tmY{};
+  p.tma = c.K > 0 && c.K % (kRawUnits * kUnitElems) == 0 && at16(c.A) && at16(c.B) && (!kGated || at16(c.B2));
+  if (p.tma) {
+    if (!make_unit_map(&tmA, c.A, c.M, upr, kRows) || !make_unit_map(&tmB, c.B, c.N, upr, kRows)) return HIF4_ERR_CUDA;
+    if (kGated && !make_unit_map(&tmB2, c.B2, c.N, upr, kRows)) return HIF4_ERR_CUDA;
+  }
+  p.bias = c.bias; p.bias_up = c.bias_up; p.act = c.act;
+  p.side = c.side; p.ld_side = c.ld_side; p.res_scale = c.res_scale;
+  p.side_vec = at16(c.side) && (c.M == 1 || c.ld_side * sizeof(T) % 16 == 0);
+  p.y = c.y; p.ld_y = c.ld_y; p.units = c.units; p.rha = c.rha;
+  if (!kGrad && !c.units) {
+    p.y_vec = at16(c.y) && (c.M == 1 || c.ld_y * sizeof(T) % 16 == 0);
+    // (a TMA store clips the innermost dimension in 16-byte pieces: other widths take the per-thread stores)
+    p.tma_store = p.y_vec && c.ld_y * sizeof(T) % 16 == 0 && c.N * sizeof(T) % 16 == 0 && make_y_map<T>(&tmY, c.y, c.M, c.N, c.ld_y);
+  }
+  p.dz = c.dz; p.ld_dz = c.ld_dz; p.dz_plane = c.dz_plane;
+  p.colsum = c.colsum; p.colsum_plane = ceil_div64(c.M, 32) * c.N;
+  if (p.slices > 1) {
+    p.flags = static_cast<unsigned int*>(workspace);
+    p.partial = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + pl.flag_bytes);
+    if (cudaMemsetAsync(p.flags, 0, pl.flag_bytes, st) != cudaSuccess) return HIF4_ERR_CUDA;
+  }
+  const int pairs = p.full_rounds == 0 && p.sk_tiles == 0 ? p.tail_tiles * p.slices : pl.pairs;      // a single round: one pair per slice
+  linear_tc2_kernel<kGated, kGrad, T><<<2 * pairs, kThreads, kLinSmemBytes, st>>>(tmA, tmB, tmB2, tmY, p);
+  note_launch();
+  return launch_status();
+}
+
+}  // namespace
+}  // namespace hif4
