@@ -59,4 +59,20 @@ bool linear_tc2_supported(bool gated, int64_t M, int64_t N, int64_t K);
 hif4_status launch_linear_tc2(const LinearCall& c, void* workspace, cudaStream_t st);
 hif4_status launch_linear_tc2_grad(const LinearCall& c, void* workspace, cudaStream_t st);
 
+// dX = sum over phases dZ W: `parts` BF16 planes of [M, ld_dz] per weight matrix (rows 16-byte aligned, plane after
+// plane), one or two weight matrices.
+struct InputGradCall {
+  int64_t M, N, K;
+  const void* dz;
+  int64_t ld_dz;
+  int parts;
+  const void *B, *B2;
+  int dt;                           // BF16 or FP16
+  void* dx;
+  int64_t ld_dx;
+};
+size_t input_grad_tc2_workspace(int64_t M, int64_t N, int64_t K, int phases);
+bool input_grad_tc2_supported(int64_t M, int64_t N, int64_t K, int phases);
+hif4_status launch_input_grad_tc2(const InputGradCall& c, void* workspace, cudaStream_t st);
+
 }  // namespace hif4
