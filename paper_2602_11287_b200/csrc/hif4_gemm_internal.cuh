@@ -30,6 +30,9 @@ hif4_status launch_gemm_tc2_fused_bf16(const void* X, int64_t ld_x, const void* 
 constexpr int64_t kGemvMaxM = 32;
 bool gemv_supported(const void* A, const void* B, int64_t M, int64_t N, int64_t K);
 size_t gemv_workspace_bytes(int64_t M, int64_t K);
+// Token rows per n-tile that the streaming kernel builds itself in shared memory (1, 2, 4 or 8), or 0: a launch of its own
+// prepares them.
+int gemv_resident_rows(int64_t M, int num_kc, bool from_bf16);
 hif4_status launch_gemv(const void* A, const void* B, float* C, int64_t M, int64_t N, int64_t K, int64_t ldc,
                         void* workspace, cudaStream_t st);
 // The same with the activations not yet quantized ([M, K] of `dt`, row stride ld_x elements, 16-byte aligned rows):

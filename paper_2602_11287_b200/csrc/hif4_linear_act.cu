@@ -1,5 +1,6 @@
 // hif4_linear_act, hif4_gated_linear and their backward passes: argument checks, then the products and what follows them.
 #include "hif4_common.cuh"
+#include "hif4_gemm_internal.cuh"
 #include "hif4_linear_internal.cuh"
 #include "hif4_vec8.cuh"
 
@@ -54,21 +55,31 @@ bool is_aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p
 size_t esize(int dt) { return dt == HIF4_FP32 ? 4 : 2; }
 bool is_type(int dt) { return dt == HIF4_BF16 || dt == HIF4_FP32 || dt == HIF4_FP16; }
 
-// Forward workspace: packed activations, the pair kernel's shared tiles, and for FP32 units the rows before their
-// conversion (64 FP32 columns of a row do not fit a thread's registers or the kernel's staging buffer).
+// Up to 32 tokens stream the weights (K % 256 == 0, 16-byte aligned units); more of them, or other weights, take the pair kernel.
+bool streams(const hif4_linear_act_args* a, bool gated) {
+  return gemv_supported(a->X, a->W_units, a->M, a->N, a->K) && (!gated || is_aligned(a->W_up_units, 16)) &&
+         (a->x_units || gemv_linear_supported(a->X, a->dt_x, a->ld_x, a->W_units, a->M, a->N, a->K));
+}
+
+// Forward workspace: packed activations, the pair kernel's shared tiles, and for units the rows before their conversion where
+// the kernel cannot convert them itself (the streaming kernel's blocks do not hold whole units; 64 FP32 columns of a
+// row do not fit the pair kernel's staging buffer).  The size does not depend on the addresses.
 struct ForwardScratch {
   size_t x, pair, y, total;
-  bool rows_first;
+  bool rows_first, stream;          // stream: the weight-streaming kernel (its tokens take the place of x and pair)
 };
 hif4_status forward_plan(const hif4_linear_act_args* a, bool gated, ForwardScratch& s) {
   s = ForwardScratch{};
   if (a->M < 0 || a->N < 0 || a->K < 0 || a->K % kUnitElems != 0) return HIF4_ERR_SHAPE;
   if (a->M == 0 || a->N == 0) return HIF4_OK;
   if (!linear_tc2_supported(gated, a->M, a->N, a->K)) return HIF4_ERR_SHAPE;
-  s.rows_first = a->y_units && a->dt == HIF4_FP32;
+  s.stream = streams(a, gated);
+  s.rows_first = a->y_units && (a->dt == HIF4_FP32 || s.stream);
   s.pair = a->x_units ? 0 : pad256(hif4_packed_bytes(a->M, a->K));
   s.y = s.pair + pad256(linear_tc2_workspace(gated, a->M, a->N, a->K));
-  s.total = s.y + (s.rows_first ? static_cast<size_t>(a->M) * a->N * 4 : 0);
+  const size_t tokens = pad256(gemv_workspace_bytes(a->M, a->K));
+  if (tokens > s.y) s.y = tokens;
+  s.total = s.y + (a->y_units ? pad256(static_cast<size_t>(a->M) * a->N * esize(a->dt)) : 0);
   return HIF4_OK;
 }
 
@@ -134,17 +145,22 @@ hif4_status forward(const hif4_linear_act_args* a, bool gated, void* workspace, 
   c.gated = gated;
   c.M = a->M; c.N = a->N; c.K = a->K;
   c.A = a->X; c.B = a->W_units; c.B2 = a->W_up_units;
-  if (!a->x_units) {
-    const hif4_status q = hif4_quantize(a->X, a->dt_x, a->M, a->K, a->ld_x, ws + s.x, a->mode, stream);
-    if (q != HIF4_OK) return q;
-    c.A = ws + s.x;
-  }
   c.dt = a->dt; c.bias = a->bias; c.bias_up = gated ? a->bias_up : nullptr; c.act = a->act;
   c.side = a->residual; c.ld_side = a->ld_residual; c.res_scale = a->res_scale;
   c.y = a->Y; c.ld_y = a->ld_y; c.units = a->y_units ? 1 : 0; c.rha = a->mode == HIF4_RHA;
-  if (!s.rows_first) return launch_linear_tc2(c, ws + s.pair, st);
-  c.y = ws + s.y; c.ld_y = a->N; c.units = 0;
-  const hif4_status pr = launch_linear_tc2(c, ws + s.pair, st);
+  if (s.rows_first) { c.y = ws + s.y; c.ld_y = a->N; c.units = 0; }
+  hif4_status pr;
+  if (s.stream) {
+    pr = launch_linear_gemv(c, a->x_units ? nullptr : a->X, a->dt_x, a->ld_x, ws, st);
+  } else {
+    if (!a->x_units) {
+      const hif4_status q = hif4_quantize(a->X, a->dt_x, a->M, a->K, a->ld_x, ws + s.x, a->mode, stream);
+      if (q != HIF4_OK) return q;
+      c.A = ws + s.x;
+    }
+    pr = launch_linear_tc2(c, ws + s.pair, st);
+  }
+  if (!s.rows_first) return pr;
   return pr != HIF4_OK ? pr : hif4_quantize(ws + s.y, a->dt, a->M, a->N, a->N, a->Y, a->mode, stream);
 }
 

@@ -54,6 +54,10 @@ struct LinearParams {
 };
 }  // namespace
 
+// Weight-streaming form for M <= kGemvMaxM tokens (same requirements and workspace as launch_gemv / launch_gemv_linear);
+// A holds units (x = nullptr), or x the activations, row stride ld_x.
+hif4_status launch_linear_gemv(const LinearCall& c, const void* x, int dt_x, int64_t ld_x, void* workspace, cudaStream_t st);
+
 size_t linear_tc2_workspace(bool gated, int64_t M, int64_t N, int64_t K);
 bool linear_tc2_supported(bool gated, int64_t M, int64_t N, int64_t K);
 hif4_status launch_linear_tc2(const LinearCall& c, void* workspace, cudaStream_t st);
