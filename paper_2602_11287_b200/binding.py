@@ -7,8 +7,8 @@ not been built, importing this module raises.
 from __future__ import annotations
 
 import ctypes
-import functools
 import os
+import struct
 from typing import Optional
 
 import torch
@@ -40,39 +40,6 @@ class Hif4Error(RuntimeError):
     def __init__(self, call: str, code: int):
         self.code = code
         super().__init__(f"{call} failed: {status_string(code)} (status {code})")
-
-
-_I64, _VP, _CI, _CF = ctypes.c_int64, ctypes.c_void_p, ctypes.c_int, ctypes.c_float
-
-
-class _BlockNormArgs(ctypes.Structure):
-    _fields_ = [("rows", _I64), ("cols", _I64), ("dt", _CI), ("dt_w", _CI), ("x", _VP), ("ld_x", _I64),
-                ("residual", _VP), ("ld_residual", _I64), ("res_scale", _CF), ("gate", _VP), ("ld_gate", _I64),
-                ("rows_per_gate", _I64), ("post", _CI), ("post_weight", _VP), ("pre", _CI), ("pre_weight", _VP),
-                ("pre_bias", _VP), ("eps", _CF), ("h", _VP), ("ld_h", _I64), ("y", _VP), ("ld_y", _I64),
-                ("y_units", _CI), ("mode", _CI)]
-
-
-class _BlockNormBackwardArgs(ctypes.Structure):
-    _fields_ = [("rows", _I64), ("cols", _I64), ("dt", _CI), ("dt_w", _CI), ("dy", _VP), ("ld_dy", _I64),
-                ("dh", _VP), ("ld_dh", _I64), ("h", _VP), ("ld_h", _I64), ("x", _VP), ("ld_x", _I64),
-                ("res_scale", _CF), ("gate", _VP), ("ld_gate", _I64), ("rows_per_gate", _I64), ("post", _CI),
-                ("post_weight", _VP), ("pre", _CI), ("pre_weight", _VP), ("eps", _CF), ("dx", _VP), ("ld_dx", _I64),
-                ("dresidual", _VP), ("ld_dresidual", _I64), ("dgate", _VP), ("dpre_weight", _VP), ("dpre_bias", _VP),
-                ("dpost_weight", _VP)]
-
-
-class _LinearActArgs(ctypes.Structure):
-    _fields_ = [("M", _I64), ("N", _I64), ("K", _I64), ("X", _VP), ("ld_x", _I64), ("dt_x", _CI), ("x_units", _CI),
-                ("mode", _CI), ("W_units", _VP), ("W_up_units", _VP), ("dt", _CI), ("bias", _VP), ("bias_up", _VP),
-                ("act", _CI), ("residual", _VP), ("ld_residual", _I64), ("res_scale", _CF), ("Y", _VP), ("ld_y", _I64),
-                ("y_units", _CI)]
-
-
-class _LinearActBackwardArgs(ctypes.Structure):
-    _fields_ = [("M", _I64), ("N", _I64), ("K", _I64), ("X", _VP), ("ld_x", _I64), ("dt_x", _CI), ("x_units", _CI),
-                ("mode", _CI), ("W_units", _VP), ("W_up_units", _VP), ("dt", _CI), ("bias", _VP), ("bias_up", _VP),
-                ("act", _CI), ("dY", _VP), ("ld_dy", _I64), ("dX", _VP), ("ld_dx", _I64), ("dbias", _VP), ("dbias_up", _VP)]
 
 
 def _load() -> ctypes.CDLL:
@@ -111,17 +78,17 @@ def _load() -> ctypes.CDLL:
     L.hif4_mse_roundtrip.restype = ci
     L.hif4_mse_roundtrip.argtypes = [vp, i64, ci, vp, vp, vp, sz, vp]
     L.hif4_block_norm.restype = ci
-    L.hif4_block_norm.argtypes = [ctypes.POINTER(_BlockNormArgs), vp]
+    L.hif4_block_norm.argtypes = [ctypes.c_char_p, vp]
     L.hif4_block_norm_backward_workspace.restype = ci
     L.hif4_block_norm_backward_workspace.argtypes = [i64, i64, ctypes.POINTER(sz)]
     L.hif4_block_norm_backward.restype = ci
-    L.hif4_block_norm_backward.argtypes = [ctypes.POINTER(_BlockNormBackwardArgs), vp, sz, vp]
+    L.hif4_block_norm_backward.argtypes = [ctypes.c_char_p, vp, sz, vp]
     for name in ("hif4_linear_act", "hif4_gated_linear"):
-        for suffix, args in (("", _LinearActArgs), ("_backward", _LinearActBackwardArgs)):
+        for suffix in ("", "_backward"):
             call, query = getattr(L, name + suffix), getattr(L, name + suffix + "_workspace")
             call.restype = query.restype = ci
-            call.argtypes = [ctypes.POINTER(args), vp, sz, vp]
-            query.argtypes = [ctypes.POINTER(args), ctypes.POINTER(sz)]
+            call.argtypes = [ctypes.c_char_p, vp, sz, vp]
+            query.argtypes = [ctypes.c_char_p, ctypes.POINTER(sz)]
     L.hif4_last_device_status.restype = ci
     L.hif4_last_device_status.argtypes = [vp]
     L.hif4_status_string.restype = ctypes.c_char_p
@@ -381,86 +348,115 @@ def _dtype_any(dt: torch.dtype) -> int:
 _TYPE_CODES = {torch.bfloat16: HIF4_BF16, torch.float32: HIF4_FP32, torch.float16: HIF4_FP16}
 
 
-def _on_stream(call):
-    """With stream=s the whole call runs under s, allocations included: memory that the caching allocator hands out on one
-    stream may still be written by that stream's pending work when another stream's kernel gets it."""
-    @functools.wraps(call)
-    def wrapped(*args, stream=None, **kw):
-        if stream is None:
-            return call(*args, **kw)
-        with torch.cuda.stream(stream):
-            return call(*args, **kw)
-    return wrapped
+def _under(stream, call, params: dict):
+    """`call` again with the same parameters and `stream` as the current stream, so that its allocations belong to it too:
+    memory that the caching allocator hands out on one stream may still be written by that stream's pending work when
+    another stream's kernel gets it."""
+    del params["stream"]
+    with torch.cuda.stream(stream):
+        return call(**params)
+
+
+# Arguments go over as one packed structure (a ctypes.Structure costs three times as much to fill): the formats follow the
+# fields of the argument types in include/hif4.h.
+ARGUMENT_FORMATS = {
+    "hif4_block_norm_args": "qqiiPqPqfPqqiPiPPfPqPqii0q",
+    "hif4_block_norm_backward_args": "qqiiPqPqPqPqfPqqiPiPfPqPqPPPP0q",
+    "hif4_linear_act_args": "qqqPqiiiPPiPPiPqfPqi0q",
+    "hif4_linear_act_backward_args": "qqqPqiiiPPiPPiPqPqPP0q",
+}
+_pack_block_norm, _pack_block_norm_backward, _pack_linear_act, _pack_linear_act_backward = (
+    struct.Struct(f).pack for f in ARGUMENT_FORMATS.values())
+
+_current_raw_stream = torch._C._cuda_getCurrentRawStream      # what torch.cuda.current_stream(...).cuda_stream returns, without the object
 
 
 def _matrix(t: Optional[torch.Tensor], rows: int, cols: int, dtype: torch.dtype, what: str):
-    """(address, row stride) of a [rows, cols] operand with unit column stride; (None, 0) without one."""
+    """(address, row stride) of a [rows, cols] operand with unit column stride; (0, 0) without one."""
     if t is None:
-        return None, 0
+        return 0, 0
+    if t.dtype is dtype and t.is_cuda and t.shape == (rows, cols):
+        ld, step = t.stride()
+        if step == 1 or cols <= 1:
+            return t.data_ptr(), (ld if rows > 1 or ld >= cols else cols)
     if not t.is_cuda:
         raise ValueError("the HiF4 library takes device tensors only (no CPU path exists)")
-    if t.dtype != dtype or t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols or (cols > 1 and t.stride(1) != 1):
-        raise ValueError(f"{what}: [{rows}, {cols}] of {dtype} with unit column stride expected, got "
-                         f"{tuple(t.shape)} of {t.dtype}, strides {t.stride()}")
-    ld = t.stride(0)
-    return t.data_ptr(), (ld if rows > 1 or ld >= cols else cols)
+    raise ValueError(f"{what}: [{rows}, {cols}] of {dtype} with unit column stride expected, got "
+                     f"{tuple(t.shape)} of {t.dtype}, strides {t.stride()}")
 
 
-def _vector(t: Optional[torch.Tensor], n: int, dtype: Optional[torch.dtype], what: str):
-    """Address of a contiguous [n] operand of `dtype`; None without one."""
+def _vector(t: Optional[torch.Tensor], n: int, dtype: Optional[torch.dtype], what: str) -> int:
+    """Address of a contiguous [n] operand of `dtype`; 0 without one."""
     if t is None:
-        return None
+        return 0
+    if t.dtype is dtype and t.is_cuda and t.shape == (n,) and (n <= 1 or t.stride(0) == 1):
+        return t.data_ptr()
     if not t.is_cuda:
         raise ValueError("the HiF4 library takes device tensors only (no CPU path exists)")
-    if t.dim() != 1 or t.shape[0] != n or t.dtype != dtype or (n > 1 and t.stride(0) != 1):
-        raise ValueError(f"{what}: contiguous [{n}] of {dtype} expected, got {tuple(t.shape)} of {t.dtype}, strides {t.stride()}")
-    return t.data_ptr()
+    raise ValueError(f"{what}: contiguous [{n}] of {dtype} expected, got {tuple(t.shape)} of {t.dtype}, strides {t.stride()}")
+
+
+def _units(t: torch.Tensor, rows: int, units: int, what: str) -> int:
+    """Address of contiguous units [rows, units, 36]."""
+    if t.dtype is torch.uint8 and t.is_cuda and t.shape == (rows, units, UNIT_BYTES) and t.is_contiguous():
+        return t.data_ptr()
+    if not t.is_cuda:
+        raise ValueError("the HiF4 library takes device tensors only (no CPU path exists)")
+    raise ValueError(f"{what}: contiguous uint8 units [{rows}, {units}, {UNIT_BYTES}] expected, got {tuple(t.shape)} of {t.dtype}")
+
+
+def _rows_like(rows: int, cols: int, dtype: torch.dtype, device) -> torch.Tensor:
+    return torch.empty_strided((rows, cols), (cols, 1), dtype=dtype, device=device)
+
+
+def _new_units(rows: int, units: int, device) -> torch.Tensor:
+    return torch.empty_strided((rows, units, UNIT_BYTES), (units * UNIT_BYTES, UNIT_BYTES, 1), dtype=torch.uint8, device=device)
 
 
 def _gates(gate: Optional[torch.Tensor], rows: int, cols: int, rows_per_gate: int, dtype: torch.dtype):
     if gate is None:
-        return None, 0
+        return 0, 0
     if rows_per_gate < 1:
         raise ValueError("a gate needs rows_per_gate >= 1")
     return _matrix(gate, -(-rows // rows_per_gate), cols, dtype, "gate")
 
 
-@_on_stream
 def hif4_block_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None, *,
                     residual: Optional[torch.Tensor] = None, res_scale: float = 1.0, gate: Optional[torch.Tensor] = None,
                     rows_per_gate: int = 0, post: int = HIF4_NORM_NONE, post_weight: Optional[torch.Tensor] = None,
                     pre: int = HIF4_NORM_RMS, eps: float = 1e-5, units: bool = False, mode: int = HIF4_RNE,
-                    out_h: Optional[torch.Tensor] = None, out_y: Optional[torch.Tensor] = None):
+                    out_h: Optional[torch.Tensor] = None, out_y: Optional[torch.Tensor] = None, stream=None):
     """h = res_scale * residual + gate[row // rows_per_gate] * post(x), y = pre(h): the norms behind and in front of a
     block with its gate and residual, one pass.  Returns (h, y); y is None for pre = HIF4_NORM_NONE and HiF4 units
     [rows, cols // 64, 36] with units=True.  h is x itself where nothing changes it and no out_h is given."""
+    if stream is not None:
+        return _under(stream, hif4_block_norm, locals())
     if x.dim() != 2:
         raise ValueError("x: a matrix expected")
     rows, cols = x.shape
-    dtype = x.dtype
+    dtype, dev = x.dtype, x.device
+    code = _dtype_any(dtype)
     px, ldx = _matrix(x, rows, cols, dtype, "x")
     pr, ldr = _matrix(residual, rows, cols, dtype, "residual")
     pg, ldg = _gates(gate, rows, cols, rows_per_gate, dtype)
-    wt = next((w.dtype for w in (weight, bias, post_weight) if w is not None), dtype)
-    same = residual is None and gate is None and post == HIF4_NORM_NONE and out_h is None
-    h = None if same else out_h if out_h is not None else torch.empty((rows, cols), dtype=dtype, device=x.device)
-    y = out_y
+    wt = dtype if weight is None and bias is None and post_weight is None else next(
+        w.dtype for w in (weight, bias, post_weight) if w is not None)
+    h, y = out_h, out_y
+    if h is None and not (residual is None and gate is None and post == HIF4_NORM_NONE):
+        h = _rows_like(rows, cols, dtype, dev)
     if y is None and pre != HIF4_NORM_NONE:
-        y = (torch.empty((rows, cols // UNIT_ELEMS, UNIT_BYTES), dtype=torch.uint8, device=x.device) if units
-             else torch.empty((rows, cols), dtype=dtype, device=x.device))
-    ph, ldh = _matrix(h, rows, cols, dtype, "out_h")
-    if units and y is not None:
-        if not (y.is_cuda and y.dtype == torch.uint8 and tuple(y.shape) == (rows, cols // UNIT_ELEMS, UNIT_BYTES) and y.is_contiguous()):
-            raise ValueError(f"out_y: contiguous uint8 units [{rows}, {cols // UNIT_ELEMS}, {UNIT_BYTES}] expected")
-        py, ldy = y.data_ptr(), 0
-    else:
-        py, ldy = _matrix(y, rows, cols, dtype, "out_y")
+        y = _new_units(rows, cols // UNIT_ELEMS, dev) if units else _rows_like(rows, cols, dtype, dev)
     if h is None and y is None:
         return x, None
-    a = _BlockNormArgs(rows, cols, _dtype_any(dtype), _dtype_any(wt), px, ldx, pr, ldr, res_scale, pg, ldg, rows_per_gate, post,
-                       _vector(post_weight, cols, wt, "post_weight"), pre, _vector(weight, cols, wt, "weight"),
-                       _vector(bias, cols, wt, "bias"), eps, ph, ldh, py, ldy, 1 if units else 0, mode)
-    _check("hif4_block_norm", lib.hif4_block_norm(a, _stream(None)))
+    ph, ldh = _matrix(h, rows, cols, dtype, "out_h")
+    if units and y is not None:
+        py, ldy = _units(y, rows, cols // UNIT_ELEMS, "out_y"), 0
+    else:
+        py, ldy = _matrix(y, rows, cols, dtype, "out_y")
+    a = _pack_block_norm(rows, cols, code, code if wt is dtype else _dtype_any(wt), px, ldx, pr, ldr, res_scale, pg, ldg, rows_per_gate,
+                         post, _vector(post_weight, cols, wt, "post_weight"), pre, _vector(weight, cols, wt, "weight"),
+                         _vector(bias, cols, wt, "bias"), eps, ph, ldh, py, ldy, 1 if units else 0, mode)
+    _check("hif4_block_norm", lib.hif4_block_norm(a, _current_raw_stream(dev.index)))
     return (x if h is None else h), y
 
 
@@ -470,16 +466,17 @@ def hif4_block_norm_backward_workspace(rows: int, cols: int) -> int:
     return int(n.value)
 
 
-@_on_stream
 def hif4_block_norm_backward(dy: Optional[torch.Tensor], h: Optional[torch.Tensor], weight: Optional[torch.Tensor] = None, *,
                              dh: Optional[torch.Tensor] = None, x: Optional[torch.Tensor] = None, bias: bool = False,
                              res_scale: float = 1.0, gate: Optional[torch.Tensor] = None, rows_per_gate: int = 0,
                              post: int = HIF4_NORM_NONE, post_weight: Optional[torch.Tensor] = None,
                              pre: int = HIF4_NORM_RMS, eps: float = 1e-5, want_dresidual: bool = True,
-                             workspace: Optional[torch.Tensor] = None) -> dict:
+                             workspace: Optional[torch.Tensor] = None, stream=None) -> dict:
     """Gradients of hif4_block_norm from those of its outputs (dy, dh) and the stored h (and x, where there is a post norm
     or a gate): a dict of dx, dresidual, dgate, dweight, dbias (with bias=True) and dpost_weight; None where the
     forward call had no such input."""
+    if stream is not None:
+        return _under(stream, hif4_block_norm_backward, locals())
     first = dy if dy is not None else dh
     if first is None or first.dim() != 2:
         raise ValueError("dy or dh: a matrix expected")
@@ -492,9 +489,9 @@ def hif4_block_norm_backward(dy: Optional[torch.Tensor], h: Optional[torch.Tenso
     pg, ldg = _gates(gate, rows, cols, rows_per_gate, dtype)
     wt = next((w.dtype for w in (weight, post_weight) if w is not None), dtype)
     pw, pwp = _vector(weight, cols, wt, "weight"), _vector(post_weight, cols, wt, "post_weight")
-    d = {"dx": torch.empty((rows, cols), dtype=dtype, device=dev),
-         "dresidual": torch.empty((rows, cols), dtype=dtype, device=dev) if want_dresidual else None,
-         "dgate": torch.empty((gate.shape[0], cols), dtype=dtype, device=dev) if gate is not None else None,
+    d = {"dx": _rows_like(rows, cols, dtype, dev),
+         "dresidual": _rows_like(rows, cols, dtype, dev) if want_dresidual else None,
+         "dgate": _rows_like(gate.shape[0], cols, dtype, dev) if gate is not None else None,
          "dweight": torch.empty(cols, dtype=torch.float32, device=dev) if weight is not None and dy is not None else None,
          "dbias": torch.empty(cols, dtype=torch.float32, device=dev) if bias and dy is not None else None,
          "dpost_weight": torch.empty(cols, dtype=torch.float32, device=dev) if post_weight is not None else None}
@@ -503,93 +500,95 @@ def hif4_block_norm_backward(dy: Optional[torch.Tensor], h: Optional[torch.Tenso
         workspace = torch.empty(need, dtype=torch.uint8, device=dev)
 
     def at(k):
-        return d[k].data_ptr() if d[k] is not None else None
+        return d[k].data_ptr() if d[k] is not None else 0
 
-    a = _BlockNormBackwardArgs(rows, cols, _dtype_any(dtype), _dtype_any(wt), pdy, lddy, pdh, lddh, ph, ldh, px, ldx, res_scale,
+    a = _pack_block_norm_backward(rows, cols, _dtype_any(dtype), _dtype_any(wt), pdy, lddy, pdh, lddh, ph, ldh, px, ldx, res_scale,
                                pg, ldg, rows_per_gate, post, pwp, pre, pw, eps, at("dx"), cols, at("dresidual"), cols,
                                at("dgate"), at("dweight"), at("dbias"), at("dpost_weight"))
     _check("hif4_block_norm_backward", lib.hif4_block_norm_backward(
         a, workspace.data_ptr() if workspace is not None else None, workspace.numel() if workspace is not None else 0,
-        _stream(None)))
+        _current_raw_stream(dev.index)))
     return d
 
 
 def _activations(x: torch.Tensor):
     """(rows, K, address, row stride, type code, 1 for units) of activations [rows, K] or units [rows, K / 64, 36]."""
-    if not x.is_cuda:
-        raise ValueError("the HiF4 library takes device tensors only (no CPU path exists)")
-    if x.dtype == torch.uint8:
-        if x.dim() != 3 or x.shape[2] != UNIT_BYTES or not x.is_contiguous():
-            raise ValueError(f"x: contiguous units [rows, K / {UNIT_ELEMS}, {UNIT_BYTES}] expected, got {tuple(x.shape)}, strides {x.stride()}")
-        return x.shape[0], x.shape[1] * UNIT_ELEMS, x.data_ptr(), 0, HIF4_BF16, 1
-    if x.dim() != 2 or (x.shape[1] > 1 and x.stride(1) != 1):
-        raise ValueError(f"x: a matrix with unit column stride expected, got {tuple(x.shape)}, strides {x.stride()}")
+    if x.dtype is torch.uint8:
+        if x.dim() != 3:
+            raise ValueError(f"x: units [rows, K / {UNIT_ELEMS}, {UNIT_BYTES}] expected, got {tuple(x.shape)}")
+        rows, n, _ = x.shape
+        return rows, n * UNIT_ELEMS, _units(x, rows, n, "x"), 0, HIF4_BF16, 1
+    if x.dim() != 2:
+        raise ValueError(f"x: a matrix expected, got {tuple(x.shape)}")
     rows, K = x.shape
-    ld = x.stride(0)
-    return rows, K, x.data_ptr(), (ld if rows > 1 or ld >= K else K), _dtype_any(x.dtype), 0
+    p, ld = _matrix(x, rows, K, x.dtype, "x")
+    return rows, K, p, ld, _dtype_any(x.dtype), 0
 
 
-def _weight(w: torch.Tensor, N: int, K: int, what: str) -> int:
-    if not w.is_cuda:
-        raise ValueError("the HiF4 library takes device tensors only (no CPU path exists)")
-    if w.dtype != torch.uint8 or w.dim() != 3 or w.shape[0] != N or w.shape[1] * UNIT_ELEMS != K or w.shape[2] != UNIT_BYTES or not w.is_contiguous():
-        raise ValueError(f"{what}: contiguous units [{N}, {K // UNIT_ELEMS}, {UNIT_BYTES}] expected, got {tuple(w.shape)} of {w.dtype}")
-    return w.data_ptr()
+_workspace_bytes: dict = {}       # what the *_workspace queries answered, by everything that the answer depends on
 
 
-def _run_with_workspace(name: str, args, workspace: Optional[torch.Tensor], device) -> Optional[torch.Tensor]:
-    need = ctypes.c_size_t(0)
-    _check(name + "_workspace", getattr(lib, name + "_workspace")(args, ctypes.byref(need)))
-    if workspace is None and need.value:
-        workspace = torch.empty(need.value, dtype=torch.uint8, device=device)
-    _check(name, getattr(lib, name)(args, workspace.data_ptr() if workspace is not None else None,
-                                    workspace.numel() if workspace is not None else 0, _stream(None)))
-    return workspace
+def _run_with_workspace(name: str, args: bytes, key: tuple, workspace: Optional[torch.Tensor], device) -> None:
+    key = (name, device.index, key)
+    need = _workspace_bytes.get(key)
+    if need is None:
+        n = ctypes.c_size_t(0)
+        _check(name + "_workspace", getattr(lib, name + "_workspace")(args, ctypes.byref(n)))
+        if len(_workspace_bytes) >= 4096:
+            _workspace_bytes.clear()
+        need = _workspace_bytes[key] = int(n.value)
+    if workspace is None and need:
+        workspace = torch.empty_strided((need,), (1,), dtype=torch.uint8, device=device)
+    if workspace is None:
+        code = getattr(lib, name)(args, None, 0, _current_raw_stream(device.index))
+    else:
+        code = getattr(lib, name)(args, workspace.data_ptr(), workspace.numel(), _current_raw_stream(device.index))
+    if code != HIF4_OK:
+        raise Hif4Error(name, code)
 
 
 def _linear_act(name, x, w_units, w_up, bias, bias_up, residual, res_scale, act, dtype, units, mode, out, workspace):
     M, K, px, ldx, dt_x, x_units = _activations(x)
-    N = w_units.shape[0]
+    N, dev = w_units.shape[0], x.device
     if dtype is None:
         dtype = out.dtype if out is not None and not units else x.dtype if not x_units else torch.bfloat16
     pr, ldr = _matrix(residual, M, N, dtype, "residual")
     if out is None:
-        out = (torch.empty((M, N // UNIT_ELEMS, UNIT_BYTES), dtype=torch.uint8, device=x.device) if units
-               else torch.empty((M, N), dtype=dtype, device=x.device))
+        out = _new_units(M, N // UNIT_ELEMS, dev) if units else _rows_like(M, N, dtype, dev)
     if units:
-        if out.dtype != torch.uint8 or tuple(out.shape) != (M, N // UNIT_ELEMS, UNIT_BYTES) or not out.is_contiguous() or not out.is_cuda:
-            raise ValueError(f"out: contiguous uint8 units [{M}, {N // UNIT_ELEMS}, {UNIT_BYTES}] expected")
-        py, ldy = out.data_ptr(), 0
+        py, ldy = _units(out, M, N // UNIT_ELEMS, "out"), 0
     else:
         py, ldy = _matrix(out, M, N, dtype, "out")
-    a = _LinearActArgs(M, N, K, px, ldx, dt_x, x_units, mode, _weight(w_units, N, K, "w_units"),
-                       None if w_up is None else _weight(w_up, N, K, "w_up_units"), _dtype_any(dtype),
-                       _vector(bias, N, dtype, "bias"), _vector(bias_up, N, dtype, "bias_up"), act, pr, ldr, res_scale, py, ldy,
-                       1 if units else 0)
-    workspace = _run_with_workspace(name, a, workspace, x.device)
+    dt, units = _dtype_any(dtype), 1 if units else 0
+    a = _pack_linear_act(M, N, K, px, ldx, dt_x, x_units, mode, _units(w_units, N, K // UNIT_ELEMS, "w_units"),
+                         0 if w_up is None else _units(w_up, N, K // UNIT_ELEMS, "w_up_units"), dt,
+                         _vector(bias, N, dtype, "bias"), _vector(bias_up, N, dtype, "bias_up"), act, pr, ldr, res_scale, py, ldy, units)
+    _run_with_workspace(name, a, (M, N, K, x_units, dt, units), workspace, dev)
     return out
 
 
-@_on_stream
 def hif4_linear_act(x: torch.Tensor, w_units: torch.Tensor, bias: Optional[torch.Tensor] = None, *,
                     residual: Optional[torch.Tensor] = None, res_scale: float = 1.0, act: int = HIF4_ACT_NONE,
                     dtype: Optional[torch.dtype] = None, units: bool = False, mode: int = HIF4_RNE,
-                    out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+                    out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """act(HiF4(x) @ W^T + bias) + res_scale * residual in `dtype` (that of x; BF16 where x is units), or its units.
 
     x is [M, K] BF16 / FP16 / FP32 or units [M, K / 64, 36]; w_units [N, K / 64, 36]; bias [N] and residual [M, N] in `dtype`;
     `out` may be the residual itself."""
+    if stream is not None:
+        return _under(stream, hif4_linear_act, locals())
     return _linear_act("hif4_linear_act", x, w_units, None, bias, None, residual, res_scale, act, dtype, units, mode, out,
                        workspace)
 
 
-@_on_stream
 def hif4_gated_linear(x: torch.Tensor, w_units: torch.Tensor, w_up_units: torch.Tensor, bias: Optional[torch.Tensor] = None,
                       bias_up: Optional[torch.Tensor] = None, *, act: int = HIF4_ACT_SILU,
                       residual: Optional[torch.Tensor] = None, res_scale: float = 1.0, dtype: Optional[torch.dtype] = None,
                       units: bool = False, mode: int = HIF4_RNE, out: Optional[torch.Tensor] = None,
-                      workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+                      workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """act(HiF4(x) @ W^T + bias) * (HiF4(x) @ W_up^T + bias_up) + res_scale * residual; arguments as in hif4_linear_act."""
+    if stream is not None:
+        return _under(stream, hif4_gated_linear, locals())
     return _linear_act("hif4_gated_linear", x, w_units, w_up_units, bias, bias_up, residual, res_scale, act, dtype, units, mode,
                        out, workspace)
 
@@ -601,41 +600,44 @@ def _linear_act_backward(name, dy, x, w_units, w_up, bias, bias_up, act, mode, w
     dtype, dev = dy.dtype, dy.device
     pdy, lddy = _matrix(dy, M, N, dtype, "dy")
     K = w_units.shape[1] * UNIT_ELEMS
+    px, ldx, dt_x, x_units = 0, K, HIF4_BF16, 0
     if x is not None:
         rows, kx, px, ldx, dt_x, x_units = _activations(x)
         if rows != M or kx != K:
             raise ValueError(f"x: {M} rows of {K} activations expected, got {rows} of {kx}")
-    else:
-        px, ldx, dt_x, x_units = None, K, HIF4_BF16, 0
-    dx = torch.empty((M, K), dtype=dtype, device=dev) if want_dx else None
+    dx = _rows_like(M, K, dtype, dev) if want_dx else None
     db = torch.empty(N, dtype=torch.float32, device=dev) if want_dbias else None
     dbu = torch.empty(N, dtype=torch.float32, device=dev) if want_dbias and w_up is not None else None
-    a = _LinearActBackwardArgs(M, N, K, px, ldx, dt_x, x_units, mode, _weight(w_units, N, K, "w_units"),
-                               None if w_up is None else _weight(w_up, N, K, "w_up_units"), _dtype_any(dtype),
-                               _vector(bias, N, dtype, "bias"), _vector(bias_up, N, dtype, "bias_up"), act, pdy, lddy,
-                               None if dx is None else dx.data_ptr(), K, None if db is None else db.data_ptr(),
-                               None if dbu is None else dbu.data_ptr())
-    workspace = _run_with_workspace(name, a, workspace, dev)
+    dt = _dtype_any(dtype)
+    a = _pack_linear_act_backward(M, N, K, px, ldx, dt_x, x_units, mode, _units(w_units, N, K // UNIT_ELEMS, "w_units"),
+                                  0 if w_up is None else _units(w_up, N, K // UNIT_ELEMS, "w_up_units"), dt,
+                                  _vector(bias, N, dtype, "bias"), _vector(bias_up, N, dtype, "bias_up"), act, pdy, lddy,
+                                  0 if dx is None else dx.data_ptr(), K, 0 if db is None else db.data_ptr(),
+                                  0 if dbu is None else dbu.data_ptr())
+    _run_with_workspace(name, a, (M, N, K, x_units, dt, act == HIF4_ACT_NONE), workspace, dev)
     return dx, db, dbu
 
 
-@_on_stream
 def hif4_linear_act_backward(dy: torch.Tensor, x: Optional[torch.Tensor], w_units: torch.Tensor,
                              bias: Optional[torch.Tensor] = None, *, act: int = HIF4_ACT_NONE, mode: int = HIF4_RNE,
-                             want_dx: bool = True, want_dbias: bool = False, workspace: Optional[torch.Tensor] = None):
+                             want_dx: bool = True, want_dbias: bool = False, workspace: Optional[torch.Tensor] = None,
+                             stream=None):
     """(dx, dbias) of hif4_linear_act from dy (BF16 or FP16): dx in the type of dy, dbias FP32; None where not wanted.  The
     residual's gradient is res_scale * dy.  x may be None for act = HIF4_ACT_NONE."""
+    if stream is not None:
+        return _under(stream, hif4_linear_act_backward, locals())
     dx, db, _ = _linear_act_backward("hif4_linear_act_backward", dy, x, w_units, None, bias, None, act, mode, want_dx, want_dbias,
                                      workspace)
     return dx, db
 
 
-@_on_stream
 def hif4_gated_linear_backward(dy: torch.Tensor, x: torch.Tensor, w_units: torch.Tensor, w_up_units: torch.Tensor,
                                bias: Optional[torch.Tensor] = None, bias_up: Optional[torch.Tensor] = None, *,
                                act: int = HIF4_ACT_SILU, mode: int = HIF4_RNE, want_dx: bool = True, want_dbias: bool = False,
-                               workspace: Optional[torch.Tensor] = None):
+                               workspace: Optional[torch.Tensor] = None, stream=None):
     """(dx, dbias, dbias_up) of hif4_gated_linear from dy (BF16 or FP16); as hif4_linear_act_backward."""
+    if stream is not None:
+        return _under(stream, hif4_gated_linear_backward, locals())
     return _linear_act_backward("hif4_gated_linear_backward", dy, x, w_units, w_up_units, bias, bias_up, act, mode, want_dx,
                                 want_dbias, workspace)
 
