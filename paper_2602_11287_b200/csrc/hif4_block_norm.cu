@@ -3,10 +3,12 @@
 // loads to its stores, the row statistics are block-wide FP32 sums, and the result can leave as HiF4 units without the
 // 16-bit matrix being written.  Bound by HBM traffic (forward 6.6 - 8 bytes an element in 16 bits, backward 12).
 //
+// Instructions are the next bound after the loads, so the arithmetic runs in packed FP32 pairs.
 // A thread owns groups of eight columns (16-byte accesses when the matrices allow them).  Blocks take contiguous runs
 // of rows and keep the next row's loads in flight while they reduce the current one; weights and gates are re-read
 // per row, from L1 after a block's first row.
 #include "hif4_common.cuh"
+#include "hif4_tc_common.cuh"
 #include "hif4_vec8.cuh"
 
 namespace hif4 {
@@ -26,6 +28,8 @@ struct NormParams {
   int64_t ld_h, ld_y;
   int units, rha;
   int strided;              // element-wise access: element j of a group is column base + j * blockDim.x
+  int stages;               // ring depth of the bulk form
+  unsigned int* error_word;
 };
 
 struct NormGradParams {
@@ -42,6 +46,79 @@ struct NormGradParams {
   float* partial;           // [5][grid][cols]: dpre_weight, dpre_bias, dpost_weight, first and last group of gates of each block
   int grid;
   int strided;
+  int stages;
+  unsigned int* error_word;
+};
+
+// How a block gets at its rows: element by element (any alignment), in 16-byte accesses, or (kBulk) through a ring of
+// shared-memory stages that one thread fills rows ahead with bulk copies, so that the loads in flight do not depend on
+// how many threads the registers let run.
+enum Access { kElements = 0, kVectors = 1, kBulk = 2 };
+
+__device__ __forceinline__ void bulk_row(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar)
+               : "memory");
+}
+
+// The ring of the bulk form: `kMats` matrices' rows per stage (absent ones take no room), one barrier per stage.  A
+// block barrier after the rows were read lets thread 0 refill the stage, so there is no second set of mbarriers.
+template <typename T, int kMats>
+struct RowRing {
+  const T* mat[kMats];
+  int64_t ld[kMats];
+  uint32_t base, row_bytes, stage_bytes, bars;
+  int stages, first;                       // `first`: stages filled so far wrap at `stages`
+  int64_t row1;
+  __device__ __forceinline__ void start(uint32_t smem, int n_stages, int cols, int64_t row0, int64_t end) {
+    row_bytes = static_cast<uint32_t>(cols) * sizeof(T);
+    uint32_t mats = 0;
+#pragma unroll
+    for (int m = 0; m < kMats; ++m) mats += mat[m] != nullptr;
+    stages = n_stages;
+    stage_bytes = mats * row_bytes;
+    bars = smem;
+    base = smem + 128;
+    row1 = end;
+    if (threadIdx.x == 0) {
+      for (int s = 0; s < stages; ++s) mbar_init(bars + 8 * s, 1);
+      asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    __syncthreads();
+    if (threadIdx.x == 0)
+      for (int s = 0; s < stages && row0 + s < row1; ++s) fill(s, row0 + s);
+  }
+  __device__ __forceinline__ void fill(int s, int64_t row) {
+    mbar_expect_tx(bars + 8 * s, stage_bytes);
+    uint32_t dst = base + s * stage_bytes;
+#pragma unroll
+    for (int m = 0; m < kMats; ++m)
+      if (mat[m]) { bulk_row(dst, mat[m] + row * ld[m], row_bytes, bars + 8 * s); dst += row_bytes; }
+  }
+  // Group at column `col` of matrix m in stage s (zeros past the row's end, zeros for an absent matrix).
+  __device__ __forceinline__ Raw8<T> read(int s, int m, int col, int cols) const {
+    Raw8<T> r;
+    zero8(r);
+    if (!mat[m] || col >= cols) return r;
+    uint32_t before = 0;
+#pragma unroll
+    for (int k = 0; k < kMats; ++k) before += k < m && mat[k] != nullptr;
+    const uint32_t at = base + s * stage_bytes + before * row_bytes + static_cast<uint32_t>(col) * sizeof(T);
+    r.a = lds128(at);
+    if constexpr (sizeof(T) == 4) r.b = lds128(at + 16);
+    return r;
+  }
+  // All threads have read stage s (of `row`): refill it.
+  __device__ __forceinline__ void release(int s, int64_t row) {
+    fence_proxy_async_smem();              // these reads before the async proxy writes the stage again
+    __syncthreads();
+    if (threadIdx.x == 0 && row + stages < row1) fill(s, row + stages);
+  }
+  // A wait gave up: report it, and let copies that are still in flight land before the shared memory is released.
+  __device__ __forceinline__ void give_up(unsigned int* error_word) const {
+    const uint64_t t0 = global_ns();
+    while (global_ns() - t0 < 2000000ull) {}
+    if (threadIdx.x == 0) atomicExch(error_word, 1u);
+  }
 };
 
 // Columns of a thread's group i: eight consecutive ones, or (element-wise access of rows that are not cut into groups
@@ -86,17 +163,41 @@ __device__ __forceinline__ void store_group(T* row, const Cols& c, int cols, con
     }
   }
 }
+// Column sums of a group to an FP32 row of the workspace (16-byte aligned where the columns come in groups).
+template <bool kVec>
+__device__ __forceinline__ void store_sums(float* row, const Cols& c, int cols, const Pairs& g) {
+  store_group<kVec>(row, c, cols, raw_of<float>(g));
+}
 // Weights of any type as FP32; `fill` where there is no weight vector.
 template <bool kVec>
-__device__ __forceinline__ void load_weights(const void* w, int dt_w, const Cols& c, int cols, float fill, float (&v)[8]) {
-  if (!w) {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = fill;
-    return;
+__device__ __forceinline__ Pairs load_weights(const void* w, int dt_w, const Cols& c, int cols, float fill) {
+  if (!w) return pairs_filled(fill);
+  if (dt_w == HIF4_BF16) return pairs_of(load_group<kVec>(static_cast<const __nv_bfloat16*>(w), c, cols));
+  if (dt_w == HIF4_FP16) return pairs_of(load_group<kVec>(static_cast<const __half*>(w), c, cols));
+  return pairs_of(load_group<kVec>(static_cast<const float*>(w), c, cols));
+}
+// The same from the block's copy in shared memory (bulk form: what the ring leaves of L1 does not hold the weights, and
+// every row would fetch them from L2 again).
+__device__ __forceinline__ Pairs load_weights_shared(bool present, uint32_t at, int dt_w, int col, int cols, float fill) {
+  if (!present || col >= cols) return pairs_filled(present ? 0.0f : fill);
+  if (dt_w == HIF4_FP32) {
+    Raw8<float> r;
+    r.a = lds128(at + col * 4u);
+    r.b = lds128(at + col * 4u + 16u);
+    return pairs_of(r);
   }
-  if (dt_w == HIF4_BF16) unpack8(load_group<kVec>(static_cast<const __nv_bfloat16*>(w), c, cols), v);
-  else if (dt_w == HIF4_FP16) unpack8(load_group<kVec>(static_cast<const __half*>(w), c, cols), v);
-  else unpack8(load_group<kVec>(static_cast<const float*>(w), c, cols), v);
+  const uint4 a = lds128(at + col * 2u);
+  if (dt_w == HIF4_BF16) return pairs_of(Raw8<__nv_bfloat16>{a});
+  return pairs_of(Raw8<__half>{a});
+}
+__device__ __forceinline__ uint32_t weight_bytes(int cols, int dt_w) { return static_cast<uint32_t>(cols) * (dt_w == HIF4_FP32 ? 4u : 2u); }
+// Copies a weight vector to shared memory, 16 bytes a thread (cols % 8 == 0, 16-byte aligned).
+__device__ __forceinline__ void stage_weights(const void* w, uint32_t at, uint32_t bytes) {
+  if (!w) return;
+  for (uint32_t i = threadIdx.x * 16u; i < bytes; i += blockDim.x * 16u) {
+    const uint4 v = *reinterpret_cast<const uint4*>(static_cast<const uint8_t*>(w) + i);
+    sts128(at + i, v.x, v.y, v.z, v.w);
+  }
 }
 
 // Sums of kN values over the block.  `slot` alternates between calls, so that one barrier per call is enough: a warp
@@ -123,39 +224,62 @@ __device__ __forceinline__ void block_sums(float (&v)[kN], float (*red)[4][32], 
   ++slot;
 }
 
-// Mean (LAYER only, else 0) and 1 / sqrt(mean of squares around it + eps) of a row held as v[kVpt][8].  Columns past
-// the row's end hold zeros; the LAYER form keeps them out of the centred sum.
+// What is taken from the elements of a group to centre them: the mean, but zero past the row's end, where the elements
+// are zeros and have to stay that.
+template <bool kVec>
+__device__ __forceinline__ Pairs centre(float mean, const Cols& c, int cols) {
+  if (kVec) return pairs_filled(c.base < cols ? mean : 0.0f);
+  Pairs m;
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    m.p[j] = make_float2(c.base + 2 * j * c.step < cols ? mean : 0.0f, c.base + (2 * j + 1) * c.step < cols ? mean : 0.0f);
+  return m;
+}
+template <bool kVec>
+__device__ __forceinline__ void subtract_mean(Pairs& g, float mean, const Cols& c, int cols) {
+  const Pairs m = centre<kVec>(-mean, c, cols);
+#pragma unroll
+  for (int j = 0; j < 4; ++j) g.p[j] = add2(g.p[j], m.p[j]);
+}
 template <int kVpt>
-__device__ __forceinline__ void row_stats(const float (&v)[kVpt][8], int kind, const NormParams& p, float (*red)[4][32],
-                                          uint32_t& slot, float& mean, float& rstd) {
-  mean = 0.0f;
+__device__ __forceinline__ float sum_of(const Pairs (&v)[kVpt]) {
+  float2 s = both(0.0f);
+#pragma unroll
+  for (int i = 0; i < kVpt; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) s = add2(s, v[i].p[j]);
+  return s.x + s.y;
+}
+template <int kVpt>
+__device__ __forceinline__ float dot_of(const Pairs (&a)[kVpt], const Pairs (&b)[kVpt]) {
+  float2 s = both(0.0f);
+#pragma unroll
+  for (int i = 0; i < kVpt; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) s = fma2(a[i].p[j], b[i].p[j], s);
+  return s.x + s.y;
+}
+// Centres a row held as v (LAYER only) and returns 1 / sqrt(mean of squares + eps).
+template <bool kVec, int kVpt>
+__device__ __forceinline__ float normalise(Pairs (&v)[kVpt], int kind, const NormParams& p, float inv_cols, float (*red)[4][32], uint32_t& slot) {
   if (kind == HIF4_NORM_LAYER) {
-    float s[1] = {0.0f};
-#pragma unroll
-    for (int i = 0; i < kVpt; ++i)
-#pragma unroll
-      for (int j = 0; j < 8; ++j) s[0] += v[i][j];
+    float s[1] = {sum_of(v)};
     block_sums(s, red, slot);
-    mean = s[0] / static_cast<float>(p.cols);
-  }
-  float s[1] = {0.0f};
 #pragma unroll
-  for (int i = 0; i < kVpt; ++i) {
-    const Cols c(i, p.strided);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const float d = c.base + j * c.step < p.cols ? v[i][j] - mean : 0.0f;
-      s[0] = fmaf(d, d, s[0]);
-    }
+    for (int i = 0; i < kVpt; ++i) subtract_mean<kVec>(v[i], s[0] * inv_cols, Cols(i, p.strided), p.cols);
   }
+  float s[1] = {dot_of(v, v)};
   block_sums(s, red, slot);
-  rstd = 1.0f / sqrtf(s[0] / static_cast<float>(p.cols) + p.eps);
+  return 1.0f / sqrtf(fmaf(s[0], inv_cols, p.eps));
 }
 
-template <typename T, int kVpt, bool kVec>
+template <typename T, int kVpt, int kAccess>
 __global__ void __launch_bounds__(kVpt == 4 ? 1024 : 512)
 block_norm_kernel(const NormParams p) {
+  constexpr bool kVec = kAccess != kElements;
   __shared__ float red[2][4][32];
+  __shared__ uint32_t abort_word;
+  extern __shared__ __align__(128) uint8_t ring_smem[];
   uint32_t slot = 0;
   const int64_t row0 = static_cast<int64_t>(blockIdx.x) * p.rows / gridDim.x;
   const int64_t row1 = (static_cast<int64_t>(blockIdx.x) + 1) * p.rows / gridDim.x;
@@ -171,56 +295,97 @@ block_norm_kernel(const NormParams p) {
       else zero8(rr[i]);
     }
   };
-  if (row0 < row1) fetch(row0);
+  const float inv_cols = 1.0f / static_cast<float>(p.cols);
+  RowRing<T, 2> ring{{x, res}, {p.ld_x, p.ld_residual}};
+  int stage = 0;
+  uint32_t phase = 0, sm_post = 0, sm_pre = 0, sm_bias = 0;
+  if (kAccess == kBulk) {
+    const uint32_t wb = weight_bytes(p.cols, p.dt_w);
+    sm_post = smem_u32(ring_smem);
+    sm_pre = sm_post + (p.post_weight ? wb : 0u);
+    sm_bias = sm_pre + (p.pre_weight ? wb : 0u);
+    const uint32_t ring_at = sm_bias + (p.pre_bias ? wb : 0u);
+    stage_weights(p.post_weight, sm_post, wb);
+    stage_weights(p.pre_weight, sm_pre, wb);
+    stage_weights(p.pre_bias, sm_bias, wb);
+    if (threadIdx.x == 0) abort_word = 0u;
+    ring.start(ring_at, p.stages, p.cols, row0, row1);
+  } else if (row0 < row1) {
+    fetch(row0);
+  }
+  // gates: one row of them serves rows_per_gate rows
+  Raw8<T> gr[kVpt];
+  int64_t gate_row = p.gate ? row0 / p.rows_per_gate : 0, gate_end = row0;
   for (int64_t row = row0; row < row1; ++row) {
-    float v[kVpt][8], r[kVpt][8];
+    if (p.gate && row == gate_end) {
+      if (row != row0) ++gate_row;
+      gate_end = (gate_row + 1) * p.rows_per_gate;
 #pragma unroll
-    for (int i = 0; i < kVpt; ++i) { unpack8(xr[i], v[i]); unpack8(rr[i], r[i]); }
-    if (row + 1 < row1) fetch(row + 1);
-    if (p.kind_post != HIF4_NORM_NONE) {
-      float mean, rstd;
-      row_stats<kVpt>(v, p.kind_post, p, red, slot, mean, rstd);
+      for (int i = 0; i < kVpt; ++i)
+        gr[i] = load_group<kVec>(static_cast<const T*>(p.gate) + gate_row * p.ld_gate, Cols(i, p.strided), p.cols);
+    }
+    if (kAccess == kBulk) {
+      if (__syncthreads_or(!mbar_wait(ring.bars + 8 * stage, phase, &abort_word))) { ring.give_up(p.error_word); return; }
 #pragma unroll
       for (int i = 0; i < kVpt; ++i) {
-        float w[8];
-        load_weights<kVec>(p.post_weight, p.dt_w, Cols(i, p.strided), p.cols, 1.0f, w);
+        const Cols c(i, 0);
+        xr[i] = ring.read(stage, 0, c.base, p.cols);
+        rr[i] = ring.read(stage, 1, c.base, p.cols);
+      }
+      ring.release(stage, row);
+      if (++stage == p.stages) { stage = 0; phase ^= 1u; }
+    }
+    Pairs v[kVpt], r[kVpt];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[i][j] = (v[i][j] - mean) * rstd * w[j];
+    for (int i = 0; i < kVpt; ++i) { v[i] = pairs_of(xr[i]); r[i] = pairs_of(rr[i]); }
+    if (kAccess != kBulk && row + 1 < row1) fetch(row + 1);
+    if (p.kind_post != HIF4_NORM_NONE) {
+      const float2 rstd = both(normalise<kVec>(v, p.kind_post, p, inv_cols, red, slot));
+#pragma unroll
+      for (int i = 0; i < kVpt; ++i) {
+        const Cols c(i, p.strided);
+        const Pairs w = kAccess == kBulk ? load_weights_shared(p.post_weight, sm_post, p.dt_w, c.base, p.cols, 1.0f)
+                                         : load_weights<kVec>(p.post_weight, p.dt_w, c, p.cols, 1.0f);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[i].p[j] = mul2(mul2(v[i].p[j], rstd), w.p[j]);
       }
     }
     if (p.gate) {
-      const T* gate = static_cast<const T*>(p.gate) + (row / p.rows_per_gate) * p.ld_gate;
 #pragma unroll
       for (int i = 0; i < kVpt; ++i) {
-        float g[8];
-        unpack8(load_group<kVec>(gate, Cols(i, p.strided), p.cols), g);
+        const Pairs g = pairs_of(gr[i]);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[i][j] *= g[j];
+        for (int j = 0; j < 4; ++j) v[i].p[j] = mul2(v[i].p[j], g.p[j]);
       }
     }
     if (res) {
 #pragma unroll
       for (int i = 0; i < kVpt; ++i)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[i][j] = fmaf(p.res_scale, r[i][j], v[i][j]);
+        for (int j = 0; j < 4; ++j) v[i].p[j] = fma2(both(p.res_scale), r[i].p[j], v[i].p[j]);
     }
     if (p.h) {
 #pragma unroll
       for (int i = 0; i < kVpt; ++i)
-        store_group<kVec>(static_cast<T*>(p.h) + row * p.ld_h, Cols(i, p.strided), p.cols, pack8<T>(v[i]));
+        store_group<kVec>(static_cast<T*>(p.h) + row * p.ld_h, Cols(i, p.strided), p.cols, raw_of<T>(v[i]));
     }
     if (!p.y) continue;
-    float mean, rstd;
-    row_stats<kVpt>(v, p.kind_pre, p, red, slot, mean, rstd);
+    const float2 rstd = both(normalise<kVec>(v, p.kind_pre, p, inv_cols, red, slot));
 #pragma unroll
     for (int i = 0; i < kVpt; ++i) {
       const Cols c(i, p.strided);
-      float w[8], b[8];
-      load_weights<kVec>(p.pre_weight, p.dt_w, c, p.cols, 1.0f, w);
-      load_weights<kVec>(p.pre_bias, p.dt_w, c, p.cols, 0.0f, b);
+      Pairs w;
+      if (kAccess == kBulk) w = load_weights_shared(p.pre_weight, sm_pre, p.dt_w, c.base, p.cols, 1.0f);
+      else w = load_weights<kVec>(p.pre_weight, p.dt_w, c, p.cols, 1.0f);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) v[i][j] = fmaf((v[i][j] - mean) * rstd, w[j], b[j]);
-      const Raw8<T> out = pack8<T>(v[i]);
+      for (int j = 0; j < 4; ++j) v[i].p[j] = mul2(mul2(v[i].p[j], rstd), w.p[j]);
+      if (p.pre_bias) {
+        if (kAccess == kBulk) w = load_weights_shared(true, sm_bias, p.dt_w, c.base, p.cols, 0.0f);
+        else w = load_weights<kVec>(p.pre_bias, p.dt_w, c, p.cols, 0.0f);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[i].p[j] = add2(v[i].p[j], w.p[j]);
+      }
+      const Raw8<T> out = raw_of<T>(v[i]);
       if (!p.units) {
         store_group<kVec>(static_cast<T*>(p.y) + row * p.ld_y, c, p.cols, out);
       } else {
@@ -244,126 +409,166 @@ block_norm_kernel(const NormParams p) {
 // of a block reach into a neighbour's run, and their parts go to `partial` as well.  norm_grad_finish_kernel adds the
 // parts in block order, so the result does not depend on scheduling.
 // kPath: the gradient also passes a gate or a post norm, i.e. x takes part.
-template <typename T, int kVpt, bool kVec, bool kPath>
+template <typename T, int kVpt, int kAccess, bool kPath>
 __global__ void __launch_bounds__(kVpt == 4 ? 1024 : 512)
 block_norm_backward_kernel(const NormGradParams p) {
+  constexpr bool kVec = kAccess != kElements;
   __shared__ float red[2][4][32];
+  __shared__ uint32_t abort_word;
+  extern __shared__ __align__(128) uint8_t ring_smem[];
   uint32_t slot = 0;
   const int64_t row0 = static_cast<int64_t>(blockIdx.x) * p.rows / gridDim.x;
   const int64_t row1 = (static_cast<int64_t>(blockIdx.x) + 1) * p.rows / gridDim.x;
   const float inv_cols = 1.0f / static_cast<float>(p.cols);
   const bool pre_layer = p.kind_pre == HIF4_NORM_LAYER, post_layer = p.kind_post == HIF4_NORM_LAYER;
   const bool post = kPath && p.kind_post != HIF4_NORM_NONE;
-  float dw[kVpt][8], db[kVpt][8], dwp[kPath ? kVpt : 1][8], dg[kPath ? kVpt : 1][8];
+  Pairs dw[kVpt], db[kVpt], dwp[kPath ? kVpt : 1], dg[kPath ? kVpt : 1];
 #pragma unroll
-  for (int i = 0; i < kVpt; ++i)
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      dw[i][j] = db[i][j] = 0.0f;
-      if (kPath) dwp[i][j] = dg[i][j] = 0.0f;
-    }
+  for (int i = 0; i < kVpt; ++i) {
+    dw[i] = db[i] = pairs_filled(0.0f);
+    if (kPath) dwp[i] = dg[i] = pairs_filled(0.0f);
+  }
   int64_t group = kPath && p.gate ? row0 / p.rows_per_gate : 0;
+  const T* m_dy = static_cast<const T*>(p.dy);
+  const T* m_dh = static_cast<const T*>(p.dh);
+  const T* m_h = p.dy ? static_cast<const T*>(p.h) : nullptr;
+  const T* m_x = kPath ? static_cast<const T*>(p.x) : nullptr;
+  RowRing<T, 4> ring{{m_h, m_dy, m_dh, m_x}, {p.ld_h, p.ld_dy, p.ld_dh, p.ld_x}};
+  int stage = 0;
+  uint32_t phase = 0, sm_pre = 0, sm_post = 0;
+  if (kAccess == kBulk) {
+    const uint32_t wb = weight_bytes(p.cols, p.dt_w);
+    sm_pre = smem_u32(ring_smem);
+    sm_post = sm_pre + (p.pre_weight ? wb : 0u);
+    const uint32_t ring_at = sm_post + (post && p.post_weight ? wb : 0u);
+    stage_weights(p.pre_weight, sm_pre, wb);
+    if (post) stage_weights(p.post_weight, sm_post, wb);
+    if (threadIdx.x == 0) abort_word = 0u;
+    ring.start(ring_at, p.stages, p.cols, row0, row1);
+  }
+  Raw8<T> gr[kPath ? kVpt : 1];
+  int64_t gate_row = group, gate_end = row0;
   for (int64_t row = row0; row < row1; ++row) {
-    float a[kVpt][8], t[kVpt][8], x[kPath ? kVpt : 1][8], dyv[kVpt][8];      // h, gradient of h, x, dy
-    float s1[2] = {0.0f, 0.0f};
+    if (kAccess == kBulk && __syncthreads_or(!mbar_wait(ring.bars + 8 * stage, phase, &abort_word))) { ring.give_up(p.error_word); return; }
+    if (kPath && p.gate && row == gate_end) {
+      if (row != row0) ++gate_row;
+      gate_end = (gate_row + 1) * p.rows_per_gate;
+#pragma unroll
+      for (int i = 0; i < kVpt; ++i)
+        gr[i] = load_group<kVec>(static_cast<const T*>(p.gate) + gate_row * p.ld_gate, Cols(i, p.strided), p.cols);
+    }
+    Pairs a[kVpt], t[kVpt], x[kPath ? kVpt : 1], dy[kVpt];      // h, gradient of h, x, dy
 #pragma unroll
     for (int i = 0; i < kVpt; ++i) {
       const Cols c(i, p.strided);
       Raw8<T> z;
       zero8(z);
-      unpack8(p.dy ? load_group<kVec>(static_cast<const T*>(p.h) + row * p.ld_h, c, p.cols) : z, a[i]);
-      unpack8(p.dy ? load_group<kVec>(static_cast<const T*>(p.dy) + row * p.ld_dy, c, p.cols) : z, dyv[i]);
-      unpack8(p.dh ? load_group<kVec>(static_cast<const T*>(p.dh) + row * p.ld_dh, c, p.cols) : z, t[i]);
-      if (kPath) unpack8(p.x ? load_group<kVec>(static_cast<const T*>(p.x) + row * p.ld_x, c, p.cols) : z, x[i]);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) { s1[0] += a[i][j]; if (kPath) s1[1] += x[i][j]; }
-    }
-    float mean = 0.0f, mean_x = 0.0f;
-    if (pre_layer || post_layer) {
-      block_sums(s1, red, slot);
-      if (pre_layer) mean = s1[0] * inv_cols;
-      if (post_layer) mean_x = s1[1] * inv_cols;
-    }
-    // sums over the row: (h - mean)^2, dn (h - mean), dn, (x - mean_x)^2; columns past the end hold zero gradients
-    float s2[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-    for (int i = 0; i < kVpt; ++i) {
-      const Cols c(i, p.strided);
-      float w[8];
-      load_weights<kVec>(p.pre_weight, p.dt_w, c, p.cols, 1.0f, w);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const bool in = c.base + j * c.step < p.cols;
-        a[i][j] = in ? a[i][j] - mean : 0.0f;
-        const float dn = dyv[i][j] * w[j];
-        s2[0] = fmaf(a[i][j], a[i][j], s2[0]);
-        s2[1] = fmaf(dn, a[i][j], s2[1]);
-        s2[2] += dn;
-        if (kPath) {
-          x[i][j] = in ? x[i][j] - mean_x : 0.0f;
-          s2[3] = fmaf(x[i][j], x[i][j], s2[3]);
-        }
+      if (kAccess == kBulk) {
+        a[i] = pairs_of(ring.read(stage, 0, c.base, p.cols));
+        dy[i] = pairs_of(ring.read(stage, 1, c.base, p.cols));
+        t[i] = pairs_of(ring.read(stage, 2, c.base, p.cols));
+        if (kPath) x[i] = pairs_of(ring.read(stage, 3, c.base, p.cols));
+      } else {
+        a[i] = pairs_of(m_h ? load_group<kVec>(m_h + row * p.ld_h, c, p.cols) : z);
+        dy[i] = pairs_of(m_dy ? load_group<kVec>(m_dy + row * p.ld_dy, c, p.cols) : z);
+        t[i] = pairs_of(m_dh ? load_group<kVec>(m_dh + row * p.ld_dh, c, p.cols) : z);
+        if (kPath) x[i] = pairs_of(m_x ? load_group<kVec>(m_x + row * p.ld_x, c, p.cols) : z);
       }
     }
-    block_sums(s2, red, slot);
-    const float rstd = 1.0f / sqrtf(s2[0] * inv_cols + p.eps);
-    const float m1 = s2[1] * rstd * inv_cols, m0 = pre_layer ? s2[2] * inv_cols : 0.0f;
-    const float rstd_x = post ? 1.0f / sqrtf(s2[3] * inv_cols + p.eps) : 1.0f;
-    const T* gate = kPath && p.gate ? static_cast<const T*>(p.gate) + (row / p.rows_per_gate) * p.ld_gate : nullptr;
-    float s3[2] = {0.0f, 0.0f};
+    if (kAccess == kBulk) {
+      ring.release(stage, row);
+      if (++stage == p.stages) { stage = 0; phase ^= 1u; }
+    }
+    if (pre_layer || post_layer) {
+      float s1[2] = {sum_of(a), 0.0f};
+      if constexpr (kPath) s1[1] = sum_of(x);
+      block_sums(s1, red, slot);
+#pragma unroll
+      for (int i = 0; i < kVpt; ++i) {
+        const Cols c(i, p.strided);
+        if (pre_layer) subtract_mean<kVec>(a[i], s1[0] * inv_cols, c, p.cols);
+        if (kPath && post_layer) subtract_mean<kVec>(x[i], s1[1] * inv_cols, c, p.cols);
+      }
+    }
+    // sums over the row: (h - mean)^2, dn (h - mean), dn, (x - mean_x)^2; columns past the end hold zero gradients
+    float s2[4] = {dot_of(a, a), 0.0f, 0.0f, 0.0f};
+    if constexpr (kPath) s2[3] = dot_of(x, x);
+    Pairs dn[kVpt];
 #pragma unroll
     for (int i = 0; i < kVpt; ++i) {
       const Cols c(i, p.strided);
-      float w[8], o[8];
-      if (p.dy) {
-        load_weights<kVec>(p.pre_weight, p.dt_w, c, p.cols, 1.0f, w);
+      const Pairs w = kAccess == kBulk ? load_weights_shared(p.pre_weight, sm_pre, p.dt_w, c.base, p.cols, 1.0f)
+                                       : load_weights<kVec>(p.pre_weight, p.dt_w, c, p.cols, 1.0f);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const float n = a[i][j] * rstd, d = dyv[i][j];
-          dw[i][j] = fmaf(d, n, dw[i][j]);
-          db[i][j] += d;
-          t[i][j] = fmaf(rstd, fmaf(-n, m1, d * w[j] - m0), t[i][j]);
+      for (int j = 0; j < 4; ++j) dn[i].p[j] = mul2(dy[i].p[j], w.p[j]);
+    }
+    s2[1] = dot_of(dn, a);
+    if (pre_layer) s2[2] = sum_of(dn);
+    block_sums(s2, red, slot);
+    const float rstd = 1.0f / sqrtf(fmaf(s2[0], inv_cols, p.eps));
+    const float m1 = -s2[1] * rstd * inv_cols, m0 = -s2[2] * inv_cols;
+    const float rstd_x = post ? 1.0f / sqrtf(fmaf(s2[3], inv_cols, p.eps)) : 1.0f;
+    float2 s3a = both(0.0f), s3b = both(0.0f);
+#pragma unroll
+    for (int i = 0; i < kVpt; ++i) {
+      const Cols c(i, p.strided);
+      if (p.dy) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float2 n = mul2(a[i].p[j], both(rstd));
+          dw[i].p[j] = fma2(dy[i].p[j], n, dw[i].p[j]);
+          float2 d = fma2(n, both(m1), dn[i].p[j]);
+          if (pre_layer) {
+            db[i].p[j] = add2(db[i].p[j], dy[i].p[j]);
+            d = add2(d, both(m0));
+          }
+          t[i].p[j] = fma2(both(rstd), d, t[i].p[j]);
         }
       }
       if (p.dresidual) {
+        Pairs o;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) o[j] = p.res_scale * t[i][j];
-        store_group<kVec>(static_cast<T*>(p.dresidual) + row * p.ld_dresidual, c, p.cols, pack8<T>(o));
+        for (int j = 0; j < 4; ++j) o.p[j] = mul2(both(p.res_scale), t[i].p[j]);
+        store_group<kVec>(static_cast<T*>(p.dresidual) + row * p.ld_dresidual, c, p.cols, raw_of<T>(o));
       }
       if (kPath) {
-        float g[8], wp[8];
-        if (gate) unpack8(load_group<kVec>(gate, c, p.cols), g);
-        else {
+        if (pre_layer) {                                 // the shift by mean(dn) reached the columns past the end
+          const Pairs in = centre<kVec>(1.0f, c, p.cols);
 #pragma unroll
-          for (int j = 0; j < 8; ++j) g[j] = 1.0f;
+          for (int j = 0; j < 4; ++j) t[i].p[j] = mul2(t[i].p[j], in.p[j]);
         }
-        load_weights<kVec>(post ? p.post_weight : nullptr, p.dt_w, c, p.cols, 1.0f, wp);
+        const Pairs g = p.gate ? pairs_of(gr[i]) : pairs_filled(1.0f);
+        Pairs wp = pairs_filled(1.0f);
+        if (post) {
+          wp = kAccess == kBulk ? load_weights_shared(p.post_weight, sm_post, p.dt_w, c.base, p.cols, 1.0f)
+                                : load_weights<kVec>(p.post_weight, p.dt_w, c, p.cols, 1.0f);
+        }
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const float xn = x[i][j] * rstd_x;                     // x itself without a post norm
-          const float dp = t[i][j] * g[j];
-          dg[i][j] = fmaf(t[i][j], xn * wp[j], dg[i][j]);
-          dwp[i][j] = fmaf(dp, xn, dwp[i][j]);
-          x[i][j] = xn;
-          const bool in = c.base + j * c.step < p.cols;
-          t[i][j] = in ? dp * wp[j] : 0.0f;
-          s3[0] = fmaf(t[i][j], xn, s3[0]);
-          s3[1] += t[i][j];
+        for (int j = 0; j < 4; ++j) {
+          const float2 xn = mul2(x[i].p[j], both(rstd_x));         // x itself without a post norm
+          const float2 dp = mul2(t[i].p[j], g.p[j]);
+          dg[i].p[j] = fma2(t[i].p[j], mul2(xn, wp.p[j]), dg[i].p[j]);
+          dwp[i].p[j] = fma2(dp, xn, dwp[i].p[j]);
+          x[i].p[j] = xn;
+          t[i].p[j] = mul2(dp, wp.p[j]);
+          s3a = fma2(t[i].p[j], xn, s3a);
+          s3b = add2(s3b, t[i].p[j]);
         }
       }
     }
     if (post && p.dx) {
+      float s3[2] = {s3a.x + s3a.y, s3b.x + s3b.y};
       block_sums(s3, red, slot);
-      const float q1 = s3[0] * inv_cols, q0 = post_layer ? s3[1] * inv_cols : 0.0f;
+      const float2 q1 = both(-s3[0] * inv_cols), q0 = both(post_layer ? -s3[1] * inv_cols : 0.0f);
 #pragma unroll
       for (int i = 0; i < kVpt; ++i)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) t[i][j] = rstd_x * (fmaf(-x[i][j], q1, t[i][j]) - q0);
+        for (int j = 0; j < 4; ++j) t[i].p[j] = mul2(both(rstd_x), add2(fma2(x[i].p[j], q1, t[i].p[j]), q0));
     }
     if (p.dx) {
 #pragma unroll
       for (int i = 0; i < kVpt; ++i)
-        store_group<kVec>(static_cast<T*>(p.dx) + row * p.ld_dx, Cols(i, p.strided), p.cols, pack8<T>(t[i]));
+        store_group<kVec>(static_cast<T*>(p.dx) + row * p.ld_dx, Cols(i, p.strided), p.cols, raw_of<T>(t[i]));
     }
     if (kPath && p.dgate) {
       const int64_t end = (group + 1) * p.rows_per_gate < p.rows ? (group + 1) * p.rows_per_gate : p.rows;
@@ -373,15 +578,12 @@ block_norm_backward_kernel(const NormGradParams p) {
         for (int i = 0; i < kVpt; ++i) {
           const Cols c(i, p.strided);
           if (starts_here && ends_here) {
-            store_group<kVec>(static_cast<T*>(p.dgate) + group * p.cols, c, p.cols, pack8<T>(dg[i]));
+            store_group<kVec>(static_cast<T*>(p.dgate) + group * p.cols, c, p.cols, raw_of<T>(dg[i]));
           } else {
             float* part = p.partial + (static_cast<int64_t>(starts_here ? 4 : 3) * gridDim.x + blockIdx.x) * p.cols;
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-              if (c.base + j * c.step < p.cols) part[c.base + j * c.step] = dg[i][j];
+            store_sums<kVec>(part, c, p.cols, dg[i]);
           }
-#pragma unroll
-          for (int j = 0; j < 8; ++j) dg[i][j] = 0.0f;
+          dg[i] = pairs_filled(0.0f);
         }
         ++group;
       }
@@ -392,80 +594,82 @@ block_norm_backward_kernel(const NormGradParams p) {
     const Cols c(i, p.strided);
     float* part = p.partial + static_cast<int64_t>(blockIdx.x) * p.cols;
     const int64_t plane = static_cast<int64_t>(gridDim.x) * p.cols;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const int e = c.base + j * c.step;
-      if (e >= p.cols) continue;
-      if (p.dpre_weight) part[e] = dw[i][j];
-      if (p.dpre_bias) part[plane + e] = db[i][j];
-      if (kPath && p.dpost_weight) part[2 * plane + e] = dwp[i][j];
-    }
+    if (p.dpre_weight) store_sums<kVec>(part, c, p.cols, dw[i]);
+    if (p.dpre_bias) store_sums<kVec>(part + plane, c, p.cols, db[i]);
+    if (kPath && p.dpost_weight) store_sums<kVec>(part + 2 * plane, c, p.cols, dwp[i]);
   }
 }
 
-// blockIdx.y 0..2: one of the weight gradients, summed over the blocks of the pass above.  blockIdx.y = 3 + b, b >= 1: the
-// group of gates that runs over the boundary between blocks b - 1 and b, if that is the first boundary it crosses.
-constexpr int kFinishCols = 32, kFinishWays = 32;
+// blockIdx.y 0..2: one of the weight gradients, summed over the blocks of the pass above.  From 3 on: the groups of gates
+// that run over a boundary between two blocks, found from the group or from the boundary, whichever there are fewer of.
+constexpr int kFinishCols = 32, kFinishWays = 16;
 template <typename T>
 __global__ void __launch_bounds__(kFinishCols * kFinishWays)
-norm_grad_finish_kernel(const NormGradParams p) {
+norm_grad_finish_kernel(const NormGradParams p, int by_group) {
   __shared__ float part[kFinishWays][kFinishCols + 1];
-  const int col = blockIdx.x * kFinishCols + (threadIdx.x & (kFinishCols - 1)), way = threadIdx.x / kFinishCols;
+  const int lane = threadIdx.x & (kFinishCols - 1), col = blockIdx.x * kFinishCols + lane, way = threadIdx.x / kFinishCols;
   const int64_t plane = static_cast<int64_t>(p.grid) * p.cols;
+  const float* src;                                      // parts first .. last of a plane, and one more in front
+  int first = 0, last = p.grid;
+  const float* front = nullptr;
+  int64_t group = 0;
   if (blockIdx.y < 3) {
-    float* out = blockIdx.y == 0 ? p.dpre_weight : blockIdx.y == 1 ? p.dpre_bias : p.dpost_weight;
-    if (!out) return;
-    float s = 0.0f;
-    if (col < p.cols)
-      for (int b = way; b < p.grid; b += kFinishWays) s += p.partial[blockIdx.y * plane + static_cast<int64_t>(b) * p.cols + col];
-    part[way][threadIdx.x & (kFinishCols - 1)] = s;
-    __syncthreads();
-    if (way == 0 && col < p.cols) {
-#pragma unroll
-      for (int w = 1; w < kFinishWays; ++w) s += part[w][threadIdx.x];
-      out[col] = s;
-    }
-    return;
+    if (!(blockIdx.y == 0 ? p.dpre_weight : blockIdx.y == 1 ? p.dpre_bias : p.dpost_weight)) return;
+    src = p.partial + blockIdx.y * plane;
+  } else {
+    const int k = static_cast<int>(blockIdx.y) - 3;
+    group = by_group ? k : static_cast<int64_t>(k + 1) * p.rows / p.grid / p.rows_per_gate;
+    const int64_t g0 = group * p.rows_per_gate, g1 = g0 + p.rows_per_gate < p.rows ? g0 + p.rows_per_gate : p.rows;
+    const int b0 = static_cast<int>(((g0 + 1) * p.grid - 1) / p.rows), b1 = static_cast<int>((g1 * p.grid - 1) / p.rows);   // blocks of its ends
+    if (b0 == b1 || (!by_group && b0 != k)) return;      // inside one block, or another boundary's
+    src = p.partial + 3 * plane;
+    front = p.partial + 4 * plane + static_cast<int64_t>(b0) * p.cols;
+    first = b0 + 1; last = b1 + 1;
   }
-  const int b = static_cast<int>(blockIdx.y) - 3 + 1;
-  const int64_t start = static_cast<int64_t>(b) * p.rows / p.grid;                       // first row of block b
-  const int64_t group = start / p.rows_per_gate, g0 = group * p.rows_per_gate;
-  if (g0 == start || g0 < static_cast<int64_t>(b - 1) * p.rows / p.grid) return;         // does not cross, or crossed before
-  const int64_t g1 = g0 + p.rows_per_gate < p.rows ? g0 + p.rows_per_gate : p.rows;
+  float s = 0.0f;
+  if (col < p.cols) {
+    if (front && way == 0) s = front[col];
+    for (int b = first + way; b < last; b += kFinishWays) s += src[static_cast<int64_t>(b) * p.cols + col];
+  }
+  part[way][lane] = s;
+  __syncthreads();
   if (way != 0 || col >= p.cols) return;
-  float s = p.partial[4 * plane + static_cast<int64_t>(b - 1) * p.cols + col];
-  for (int k = b; k < p.grid && static_cast<int64_t>(k) * p.rows / p.grid < g1; ++k)
-    s += p.partial[3 * plane + static_cast<int64_t>(k) * p.cols + col];
-  static_cast<T*>(p.dgate)[group * p.cols + col] = from_f32<T>(s);
+#pragma unroll
+  for (int w = 1; w < kFinishWays; ++w) s += part[w][lane];
+  if (front) static_cast<T*>(p.dgate)[group * p.cols + col] = from_f32<T>(s);
+  else (blockIdx.y == 0 ? p.dpre_weight : blockIdx.y == 1 ? p.dpre_bias : p.dpost_weight)[col] = s;
 }
 
 // ------------------------------------------------------------------------------------------------------- host side
-int device_sms() {
-  static int cache[64] = {};
-  int dev = 0, v = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess) return 148;
-  if (dev >= 0 && dev < 64 && cache[dev] > 0) return cache[dev];
-  if (cudaDeviceGetAttribute(&v, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || v <= 0) return 148;
-  if (dev >= 0 && dev < 64) cache[dev] = v;
-  return v;
-}
-
 // Groups of eight columns per thread: one up to 4096 columns, then two, then four (and up to 1024 threads).
 int groups_per_thread(int64_t cols) { return cols <= 4096 ? 1 : cols <= 8192 ? 2 : 4; }
 int threads_for(int64_t cols, int vpt) {
   const int64_t t = ceil_div64(ceil_div64(cols, 8), vpt);
   return static_cast<int>(ceil_div64(t, 32) * 32);
 }
-// Blocks that one SM holds: about 1024 threads keep enough loads in flight, and no block may be alone with its barriers.
-int grid_for(int64_t rows, int threads, int per_sm_threads) {
-  const int per_sm = per_sm_threads / threads < 1 ? 1 : per_sm_threads / threads > 16 ? 16 : per_sm_threads / threads;
-  const int64_t g = static_cast<int64_t>(device_sms()) * per_sm;
+// Blocks per SM and, for the bulk form, stages per block: as many blocks as the registers let run (the grid of the
+// backward pass must not depend on the device's state, so the count comes from the thread number alone), and the ring
+// shares what shared memory there is between them.
+constexpr int kRingBytes = 200 * 1024, kMaxRing = 8;
+int blocks_per_sm(int threads, int threads_per_sm) {
+  const int b = threads_per_sm / threads;
+  return b < 1 ? 1 : b > 16 ? 16 : b;
+}
+int grid_for(int64_t rows, int threads, int threads_per_sm) {
+  const int64_t g = static_cast<int64_t>(sm_count()) * blocks_per_sm(threads, threads_per_sm);
   return static_cast<int>(rows < g ? rows : g);
 }
 constexpr int kForwardThreadsPerSm = 1024, kBackwardThreadsPerSm = 512;
 
-bool aligned_to(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+// Stages of the ring beside `weights` bytes of weights, or 0: rows too short, too few of them per block, or too wide for two stages.
+int ring_stages(int64_t rows, int grid, int per_sm, size_t stage_bytes, size_t weights) {
+  if (stage_bytes < 4096 || rows < 2 * static_cast<int64_t>(grid) || weights + 2 * stage_bytes > kRingBytes / static_cast<size_t>(per_sm)) return 0;
+  const size_t n = (kRingBytes / per_sm - weights) / stage_bytes;
+  return n < 2 ? 0 : n > kMaxRing ? kMaxRing : static_cast<int>(n);
+}
+
 size_t type_size(int dt) { return dt == HIF4_FP32 ? 4 : 2; }
+bool aligned_to(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 bool known_type(int dt) { return dt == HIF4_BF16 || dt == HIF4_FP32 || dt == HIF4_FP16; }
 bool known_kind(int k) { return k == HIF4_NORM_NONE || k == HIF4_NORM_RMS || k == HIF4_NORM_LAYER; }
 
@@ -488,10 +692,22 @@ hif4_status check_operands(const Operand* o, int n, int64_t rows, int64_t cols, 
 }
 
 template <typename T, int kVpt>
-hif4_status launch_norm(const NormParams& p, bool vec, cudaStream_t st) {
+hif4_status launch_norm(NormParams p, bool vec, cudaStream_t st) {
   const int threads = threads_for(p.cols, kVpt), grid = grid_for(p.rows, threads, kForwardThreadsPerSm);
-  if (vec) block_norm_kernel<T, kVpt, true><<<grid, threads, 0, st>>>(p);
-  else block_norm_kernel<T, kVpt, false><<<grid, threads, 0, st>>>(p);
+  const size_t stage = static_cast<size_t>(p.cols) * sizeof(T) * (p.residual ? 2 : 1);
+  const size_t weights = static_cast<size_t>(p.cols) * type_size(p.dt_w) * ((p.post_weight ? 1 : 0) + (p.pre_weight ? 1 : 0) + (p.pre_bias ? 1 : 0));
+  p.stages = vec ? ring_stages(p.rows, grid, blocks_per_sm(threads, kForwardThreadsPerSm), stage, weights) : 0;
+  if (p.stages > 0) {
+    static uint64_t smem_opt_in = 0;
+    if (!ensure_dynamic_smem(block_norm_kernel<T, kVpt, kBulk>, kRingBytes + 128, smem_opt_in)) return HIF4_ERR_CUDA;
+    p.error_word = device_error_word();
+    if (!p.error_word) return HIF4_ERR_CUDA;
+    block_norm_kernel<T, kVpt, kBulk><<<grid, threads, 128 + weights + p.stages * stage, st>>>(p);
+  } else if (vec) {
+    block_norm_kernel<T, kVpt, kVectors><<<grid, threads, 0, st>>>(p);
+  } else {
+    block_norm_kernel<T, kVpt, kElements><<<grid, threads, 0, st>>>(p);
+  }
   note_launch();
   return launch_status();
 }
@@ -504,29 +720,46 @@ hif4_status launch_norm_t(const NormParams& p, bool vec, cudaStream_t st) {
   }
 }
 
-template <typename T, int kVpt>
-void launch_norm_grad(const NormGradParams& p, bool vec, bool path, int threads, cudaStream_t st) {
-  if (path) {
-    if (vec) block_norm_backward_kernel<T, kVpt, true, true><<<p.grid, threads, 0, st>>>(p);
-    else block_norm_backward_kernel<T, kVpt, false, true><<<p.grid, threads, 0, st>>>(p);
+template <typename T, int kVpt, bool kPath>
+hif4_status launch_norm_grad(NormGradParams p, bool vec, int threads, cudaStream_t st) {
+  const int mats = (p.dy ? 2 : 0) + (p.dh ? 1 : 0) + (kPath && p.x ? 1 : 0);
+  const size_t stage = static_cast<size_t>(p.cols) * sizeof(T) * mats;
+  const size_t weights = static_cast<size_t>(p.cols) * type_size(p.dt_w) * ((p.pre_weight ? 1 : 0) + (kPath && p.post_weight ? 1 : 0));
+  p.stages = vec ? ring_stages(p.rows, p.grid, blocks_per_sm(threads, kBackwardThreadsPerSm), stage, weights) : 0;
+  if (p.stages > 0) {
+    static uint64_t smem_opt_in = 0;
+    if (!ensure_dynamic_smem(block_norm_backward_kernel<T, kVpt, kBulk, kPath>, kRingBytes + 128, smem_opt_in)) return HIF4_ERR_CUDA;
+    p.error_word = device_error_word();
+    if (!p.error_word) return HIF4_ERR_CUDA;
+    block_norm_backward_kernel<T, kVpt, kBulk, kPath><<<p.grid, threads, 128 + weights + p.stages * stage, st>>>(p);
+  } else if (vec) {
+    block_norm_backward_kernel<T, kVpt, kVectors, kPath><<<p.grid, threads, 0, st>>>(p);
   } else {
-    if (vec) block_norm_backward_kernel<T, kVpt, true, false><<<p.grid, threads, 0, st>>>(p);
-    else block_norm_backward_kernel<T, kVpt, false, false><<<p.grid, threads, 0, st>>>(p);
+    block_norm_backward_kernel<T, kVpt, kElements, kPath><<<p.grid, threads, 0, st>>>(p);
   }
+  note_launch();
+  return launch_status();
+}
+template <typename T, int kVpt>
+hif4_status launch_norm_grad(const NormGradParams& p, bool vec, int threads, cudaStream_t st) {
+  if (p.kind_post != HIF4_NORM_NONE || p.gate) return launch_norm_grad<T, kVpt, true>(p, vec, threads, st);
+  return launch_norm_grad<T, kVpt, false>(p, vec, threads, st);
 }
 template <typename T>
-hif4_status launch_norm_grad_t(NormGradParams p, bool vec, cudaStream_t st) {
+hif4_status launch_norm_grad_t(const NormGradParams& p, bool vec, cudaStream_t st) {
   const int vpt = groups_per_thread(p.cols), threads = threads_for(p.cols, vpt);
-  const bool path = p.kind_post != HIF4_NORM_NONE || p.gate != nullptr;
-  if (vpt == 1) launch_norm_grad<T, 1>(p, vec, path, threads, st);
-  else if (vpt == 2) launch_norm_grad<T, 2>(p, vec, path, threads, st);
-  else launch_norm_grad<T, 4>(p, vec, path, threads, st);
-  note_launch();
-  if (cudaGetLastError() != cudaSuccess) return HIF4_ERR_CUDA;
-  const int planes = p.dgate ? 3 + p.grid - 1 : (p.dpre_weight || p.dpre_bias || p.dpost_weight) ? 3 : 0;
+  const hif4_status s = vpt == 1 ? launch_norm_grad<T, 1>(p, vec, threads, st)
+                        : vpt == 2 ? launch_norm_grad<T, 2>(p, vec, threads, st) : launch_norm_grad<T, 4>(p, vec, threads, st);
+  if (s != HIF4_OK) return s;
+  int planes = p.dpre_weight || p.dpre_bias || p.dpost_weight ? 3 : 0, by_group = 0;
+  if (p.dgate) {
+    const int64_t groups = ceil_div64(p.rows, p.rows_per_gate);
+    by_group = groups < p.grid - 1;
+    planes = 3 + (by_group ? static_cast<int>(groups) : p.grid - 1);
+  }
   if (planes == 0) return HIF4_OK;
   const dim3 grid(static_cast<unsigned>(ceil_div64(p.cols, kFinishCols)), static_cast<unsigned>(planes));
-  norm_grad_finish_kernel<T><<<grid, kFinishCols * kFinishWays, 0, st>>>(p);
+  norm_grad_finish_kernel<T><<<grid, kFinishCols * kFinishWays, 0, st>>>(p, by_group);
   note_launch();
   return launch_status();
 }
@@ -570,7 +803,7 @@ extern "C" hif4_status hif4_block_norm(const hif4_block_norm_args* a, void* stre
   p.h = a->h; p.y = a->y; p.ld_h = a->ld_h; p.ld_y = a->ld_y;
   p.units = a->y_units ? 1 : 0; p.rha = a->mode == HIF4_RHA;
   vec = vec && vec_w;
-  p.strided = vec || p.units ? 0 : 1;                    // units: eight consecutive columns per lane, whatever the access
+  p.strided = a->cols % 8 != 0;            // (a function of the width alone: rows and their units come from the same sums)
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   if (a->dt == HIF4_BF16) return launch_norm_t<__nv_bfloat16>(p, vec, st);
   if (a->dt == HIF4_FP16) return launch_norm_t<__half>(p, vec, st);
@@ -629,7 +862,7 @@ extern "C" hif4_status hif4_block_norm_backward(const hif4_block_norm_backward_a
   p.dpre_weight = a->dpre_weight; p.dpre_bias = a->dpre_bias; p.dpost_weight = a->dpost_weight;
   p.partial = static_cast<float*>(workspace);
   p.grid = backward_grid(a->rows, a->cols);
-  p.strided = vec ? 0 : 1;
+  p.strided = a->cols % 8 != 0;
   if (a->dt == HIF4_BF16) return launch_norm_grad_t<__nv_bfloat16>(p, vec, st);
   if (a->dt == HIF4_FP16) return launch_norm_grad_t<__half>(p, vec, st);
   return launch_norm_grad_t<float>(p, vec, st);

@@ -93,6 +93,53 @@ __device__ __forceinline__ void store8(float* p, const Raw8<float>& r) {
   *reinterpret_cast<uint4*>(p + 4) = r.b;
 }
 
+// Two FP32 operations in one instruction (sm_100 issues packed FP32 arithmetic at the rate of scalar instructions).
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 d;
+  asm("{\n\t.reg .b64 a, b, c, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmov.b64 c, {%6, %7};\n\t"
+      "fma.rn.f32x2 d, a, b, c;\n\tmov.b64 {%0, %1}, d;\n\t}"
+      : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+  return d;
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  float2 d;
+  asm("{\n\t.reg .b64 a, b, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmul.rn.f32x2 d, a, b;\n\tmov.b64 {%0, %1}, d;\n\t}"
+      : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  float2 d;
+  asm("{\n\t.reg .b64 a, b, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tadd.rn.f32x2 d, a, b;\n\tmov.b64 {%0, %1}, d;\n\t}"
+      : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
+}
+__device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
+
+// A group as four pairs.
+struct Pairs { float2 p[4]; };
+template <typename T>
+__device__ __forceinline__ Pairs pairs_of(const Raw8<T>& r) {
+  float v[8];
+  unpack8(r, v);
+  Pairs g;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) g.p[i] = make_float2(v[2 * i], v[2 * i + 1]);
+  return g;
+}
+template <typename T>
+__device__ __forceinline__ Raw8<T> raw_of(const Pairs& g) {
+  float v[8];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) { v[2 * i] = g.p[i].x; v[2 * i + 1] = g.p[i].y; }
+  return pack8<T>(v);
+}
+__device__ __forceinline__ Pairs pairs_filled(float v) {
+  Pairs g;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) g.p[i] = both(v);
+  return g;
+}
+
 // Eight consecutive lanes (lane & 7 = level-2 group g of the unit) hold one unit: Algorithm 1 in BF16 arithmetic for
 // BF16 groups, in FP32 arithmetic for FP16 and FP32 groups, i.e. the bits that hif4_quantize writes for a matrix of
 // that type.  Returns the lane's code word; `meta` is the unit's metadata word in all eight lanes.  All 32 lanes call.
