@@ -50,77 +50,6 @@ struct NormGradParams {
   unsigned int* error_word;
 };
 
-// How a block gets at its rows: element by element (any alignment), in 16-byte accesses, or (kBulk) through a ring of
-// shared-memory stages that one thread fills rows ahead with bulk copies, so that the loads in flight do not depend on
-// how many threads the registers let run.
-enum Access { kElements = 0, kVectors = 1, kBulk = 2 };
-
-__device__ __forceinline__ void bulk_row(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
-  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar)
-               : "memory");
-}
-
-// The ring of the bulk form: `kMats` matrices' rows per stage (absent ones take no room), one barrier per stage.  A
-// block barrier after the rows were read lets thread 0 refill the stage, so there is no second set of mbarriers.
-template <typename T, int kMats>
-struct RowRing {
-  const T* mat[kMats];
-  int64_t ld[kMats];
-  uint32_t base, row_bytes, stage_bytes, bars;
-  int stages, first;                       // `first`: stages filled so far wrap at `stages`
-  int64_t row1;
-  __device__ __forceinline__ void start(uint32_t smem, int n_stages, int cols, int64_t row0, int64_t end) {
-    row_bytes = static_cast<uint32_t>(cols) * sizeof(T);
-    uint32_t mats = 0;
-#pragma unroll
-    for (int m = 0; m < kMats; ++m) mats += mat[m] != nullptr;
-    stages = n_stages;
-    stage_bytes = mats * row_bytes;
-    bars = smem;
-    base = smem + 128;
-    row1 = end;
-    if (threadIdx.x == 0) {
-      for (int s = 0; s < stages; ++s) mbar_init(bars + 8 * s, 1);
-      asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-    }
-    __syncthreads();
-    if (threadIdx.x == 0)
-      for (int s = 0; s < stages && row0 + s < row1; ++s) fill(s, row0 + s);
-  }
-  __device__ __forceinline__ void fill(int s, int64_t row) {
-    mbar_expect_tx(bars + 8 * s, stage_bytes);
-    uint32_t dst = base + s * stage_bytes;
-#pragma unroll
-    for (int m = 0; m < kMats; ++m)
-      if (mat[m]) { bulk_row(dst, mat[m] + row * ld[m], row_bytes, bars + 8 * s); dst += row_bytes; }
-  }
-  // Group at column `col` of matrix m in stage s (zeros past the row's end, zeros for an absent matrix).
-  __device__ __forceinline__ Raw8<T> read(int s, int m, int col, int cols) const {
-    Raw8<T> r;
-    zero8(r);
-    if (!mat[m] || col >= cols) return r;
-    uint32_t before = 0;
-#pragma unroll
-    for (int k = 0; k < kMats; ++k) before += k < m && mat[k] != nullptr;
-    const uint32_t at = base + s * stage_bytes + before * row_bytes + static_cast<uint32_t>(col) * sizeof(T);
-    r.a = lds128(at);
-    if constexpr (sizeof(T) == 4) r.b = lds128(at + 16);
-    return r;
-  }
-  // All threads have read stage s (of `row`): refill it.
-  __device__ __forceinline__ void release(int s, int64_t row) {
-    fence_proxy_async_smem();              // these reads before the async proxy writes the stage again
-    __syncthreads();
-    if (threadIdx.x == 0 && row + stages < row1) fill(s, row + stages);
-  }
-  // A wait gave up: report it, and let copies that are still in flight land before the shared memory is released.
-  __device__ __forceinline__ void give_up(unsigned int* error_word) const {
-    const uint64_t t0 = global_ns();
-    while (global_ns() - t0 < 2000000ull) {}
-    if (threadIdx.x == 0) atomicExch(error_word, 1u);
-  }
-};
-
 // Columns of a thread's group i: eight consecutive ones, or (element-wise access of rows that are not cut into groups
 // of eight) one in every blockDim.x, so that the lanes of a warp still touch neighbouring elements.
 struct Cols {
@@ -176,53 +105,44 @@ __device__ __forceinline__ Pairs load_weights(const void* w, int dt_w, const Col
   if (dt_w == HIF4_FP16) return pairs_of(load_group<kVec>(static_cast<const __half*>(w), c, cols));
   return pairs_of(load_group<kVec>(static_cast<const float*>(w), c, cols));
 }
-// The same from the block's copy in shared memory (bulk form: what the ring leaves of L1 does not hold the weights, and
-// every row would fetch them from L2 again).
-__device__ __forceinline__ Pairs load_weights_shared(bool present, uint32_t at, int dt_w, int col, int cols, float fill) {
-  if (!present || col >= cols) return pairs_filled(present ? 0.0f : fill);
-  if (dt_w == HIF4_FP32) {
-    Raw8<float> r;
-    r.a = lds128(at + col * 4u);
-    r.b = lds128(at + col * 4u + 16u);
-    return pairs_of(r);
+// Sums of kN (1, 2 or 4) values over the block.  A lane halves the values it still carries at every exchange until it
+// holds one, so kN values cost 5 + log2 kN exchanges per level instead of 5 kN.  `slot` alternates between calls, so
+// that one barrier per call is enough: a warp can only be one call ahead of another, and then it writes the other half.
+template <int kN, bool kAlwaysSync = false>
+__device__ __forceinline__ void block_sums(float (&v)[kN], float (*red)[4][32], uint32_t& slot) {
+  constexpr int kLanes = 32 / kN;                        // lanes that carry one value
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+  if constexpr (kN == 4) {
+    const bool up = lane & 16;
+    const float s0 = up ? v[0] : v[2], s1 = up ? v[1] : v[3];
+    v[0] = (up ? v[2] : v[0]) + __shfl_xor_sync(0xFFFFFFFFu, s0, 16);
+    v[1] = (up ? v[3] : v[1]) + __shfl_xor_sync(0xFFFFFFFFu, s1, 16);
   }
-  const uint4 a = lds128(at + col * 2u);
-  if (dt_w == HIF4_BF16) return pairs_of(Raw8<__nv_bfloat16>{a});
-  return pairs_of(Raw8<__half>{a});
-}
-__device__ __forceinline__ uint32_t weight_bytes(int cols, int dt_w) { return static_cast<uint32_t>(cols) * (dt_w == HIF4_FP32 ? 4u : 2u); }
-// Copies a weight vector to shared memory, 16 bytes a thread (cols % 8 == 0, 16-byte aligned).
-__device__ __forceinline__ void stage_weights(const void* w, uint32_t at, uint32_t bytes) {
-  if (!w) return;
-  for (uint32_t i = threadIdx.x * 16u; i < bytes; i += blockDim.x * 16u) {
-    const uint4 v = *reinterpret_cast<const uint4*>(static_cast<const uint8_t*>(w) + i);
-    sts128(at + i, v.x, v.y, v.z, v.w);
+  if constexpr (kN >= 2) {
+    const bool up = lane & kLanes;
+    const float s0 = up ? v[0] : v[1];
+    v[0] = (up ? v[1] : v[0]) + __shfl_xor_sync(0xFFFFFFFFu, s0, kLanes);
   }
+#pragma unroll
+  for (int s = kLanes / 2; s > 0; s >>= 1) v[0] += __shfl_xor_sync(0xFFFFFFFFu, v[0], s);
+  float total = v[0];
+  if (kAlwaysSync || warps > 1) {
+    const int n = lane / kLanes, k = lane % kLanes;      // value and place of this lane
+    if (k == 0) red[slot & 1u][n][warp] = v[0];
+    __syncthreads();
+    total = 0.0f;
+    for (int w = k; w < warps; w += kLanes) total += red[slot & 1u][n][w];
+#pragma unroll
+    for (int s = kLanes / 2; s > 0; s >>= 1) total += __shfl_xor_sync(0xFFFFFFFFu, total, s);
+    ++slot;
+  }
+#pragma unroll
+  for (int n = 0; n < kN; ++n) v[n] = kN == 1 ? total : __shfl_sync(0xFFFFFFFFu, total, n * kLanes);
 }
 
-// Sums of kN values over the block.  `slot` alternates between calls, so that one barrier per call is enough: a warp
-// can only be one call ahead of another, and then it writes the other half.
+// ... with a block barrier even where one warp needs none.
 template <int kN>
-__device__ __forceinline__ void block_sums(float (&v)[kN], float (*red)[4][32], uint32_t& slot) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
-#pragma unroll
-  for (int n = 0; n < kN; ++n)
-#pragma unroll
-    for (int s = 16; s > 0; s >>= 1) v[n] += __shfl_xor_sync(0xFFFFFFFFu, v[n], s);
-  if (warps == 1) return;
-  if (lane == 0) {
-#pragma unroll
-    for (int n = 0; n < kN; ++n) red[slot & 1u][n][warp] = v[n];
-  }
-  __syncthreads();
-#pragma unroll
-  for (int n = 0; n < kN; ++n) {
-    v[n] = lane < warps ? red[slot & 1u][n][lane] : 0.0f;
-#pragma unroll
-    for (int s = 16; s > 0; s >>= 1) v[n] += __shfl_xor_sync(0xFFFFFFFFu, v[n], s);
-  }
-  ++slot;
-}
+__device__ __forceinline__ void block_sums_synced(float (&v)[kN], float (*red)[4][32], uint32_t& slot) { block_sums<kN, true>(v, red, slot); }
 
 // What is taken from the elements of a group to centre them: the mean, but zero past the row's end, where the elements
 // are zeros and have to stay that.
@@ -270,16 +190,13 @@ __device__ __forceinline__ float normalise(Pairs (&v)[kVpt], int kind, const Nor
   }
   float s[1] = {dot_of(v, v)};
   block_sums(s, red, slot);
-  return 1.0f / sqrtf(fmaf(s[0], inv_cols, p.eps));
+  return rsqrtf(fmaf(s[0], inv_cols, p.eps));
 }
 
-template <typename T, int kVpt, int kAccess>
-__global__ void __launch_bounds__(kVpt == 4 ? 1024 : 512)
+template <typename T, int kVpt, bool kVec>
+__global__ void __launch_bounds__(kVpt <= 2 ? 320 : 512)
 block_norm_kernel(const NormParams p) {
-  constexpr bool kVec = kAccess != kElements;
   __shared__ float red[2][4][32];
-  __shared__ uint32_t abort_word;
-  extern __shared__ __align__(128) uint8_t ring_smem[];
   uint32_t slot = 0;
   const int64_t row0 = static_cast<int64_t>(blockIdx.x) * p.rows / gridDim.x;
   const int64_t row1 = (static_cast<int64_t>(blockIdx.x) + 1) * p.rows / gridDim.x;
@@ -296,23 +213,7 @@ block_norm_kernel(const NormParams p) {
     }
   };
   const float inv_cols = 1.0f / static_cast<float>(p.cols);
-  RowRing<T, 2> ring{{x, res}, {p.ld_x, p.ld_residual}};
-  int stage = 0;
-  uint32_t phase = 0, sm_post = 0, sm_pre = 0, sm_bias = 0;
-  if (kAccess == kBulk) {
-    const uint32_t wb = weight_bytes(p.cols, p.dt_w);
-    sm_post = smem_u32(ring_smem);
-    sm_pre = sm_post + (p.post_weight ? wb : 0u);
-    sm_bias = sm_pre + (p.pre_weight ? wb : 0u);
-    const uint32_t ring_at = sm_bias + (p.pre_bias ? wb : 0u);
-    stage_weights(p.post_weight, sm_post, wb);
-    stage_weights(p.pre_weight, sm_pre, wb);
-    stage_weights(p.pre_bias, sm_bias, wb);
-    if (threadIdx.x == 0) abort_word = 0u;
-    ring.start(ring_at, p.stages, p.cols, row0, row1);
-  } else if (row0 < row1) {
-    fetch(row0);
-  }
+  if (row0 < row1) fetch(row0);
   // gates: one row of them serves rows_per_gate rows
   Raw8<T> gr[kVpt];
   int64_t gate_row = p.gate ? row0 / p.rows_per_gate : 0, gate_end = row0;
@@ -324,28 +225,16 @@ block_norm_kernel(const NormParams p) {
       for (int i = 0; i < kVpt; ++i)
         gr[i] = load_group<kVec>(static_cast<const T*>(p.gate) + gate_row * p.ld_gate, Cols(i, p.strided), p.cols);
     }
-    if (kAccess == kBulk) {
-      if (__syncthreads_or(!mbar_wait(ring.bars + 8 * stage, phase, &abort_word))) { ring.give_up(p.error_word); return; }
-#pragma unroll
-      for (int i = 0; i < kVpt; ++i) {
-        const Cols c(i, 0);
-        xr[i] = ring.read(stage, 0, c.base, p.cols);
-        rr[i] = ring.read(stage, 1, c.base, p.cols);
-      }
-      ring.release(stage, row);
-      if (++stage == p.stages) { stage = 0; phase ^= 1u; }
-    }
     Pairs v[kVpt], r[kVpt];
 #pragma unroll
     for (int i = 0; i < kVpt; ++i) { v[i] = pairs_of(xr[i]); r[i] = pairs_of(rr[i]); }
-    if (kAccess != kBulk && row + 1 < row1) fetch(row + 1);
+    if (row + 1 < row1) fetch(row + 1);
     if (p.kind_post != HIF4_NORM_NONE) {
       const float2 rstd = both(normalise<kVec>(v, p.kind_post, p, inv_cols, red, slot));
 #pragma unroll
       for (int i = 0; i < kVpt; ++i) {
         const Cols c(i, p.strided);
-        const Pairs w = kAccess == kBulk ? load_weights_shared(p.post_weight, sm_post, p.dt_w, c.base, p.cols, 1.0f)
-                                         : load_weights<kVec>(p.post_weight, p.dt_w, c, p.cols, 1.0f);
+        const Pairs w = load_weights<kVec>(p.post_weight, p.dt_w, c, p.cols, 1.0f);
 #pragma unroll
         for (int j = 0; j < 4; ++j) v[i].p[j] = mul2(mul2(v[i].p[j], rstd), w.p[j]);
       }
@@ -374,14 +263,11 @@ block_norm_kernel(const NormParams p) {
 #pragma unroll
     for (int i = 0; i < kVpt; ++i) {
       const Cols c(i, p.strided);
-      Pairs w;
-      if (kAccess == kBulk) w = load_weights_shared(p.pre_weight, sm_pre, p.dt_w, c.base, p.cols, 1.0f);
-      else w = load_weights<kVec>(p.pre_weight, p.dt_w, c, p.cols, 1.0f);
+      Pairs w = load_weights<kVec>(p.pre_weight, p.dt_w, c, p.cols, 1.0f);
 #pragma unroll
       for (int j = 0; j < 4; ++j) v[i].p[j] = mul2(mul2(v[i].p[j], rstd), w.p[j]);
       if (p.pre_bias) {
-        if (kAccess == kBulk) w = load_weights_shared(true, sm_bias, p.dt_w, c.base, p.cols, 0.0f);
-        else w = load_weights<kVec>(p.pre_bias, p.dt_w, c, p.cols, 0.0f);
+        w = load_weights<kVec>(p.pre_bias, p.dt_w, c, p.cols, 0.0f);
 #pragma unroll
         for (int j = 0; j < 4; ++j) v[i].p[j] = add2(v[i].p[j], w.p[j]);
       }
@@ -409,13 +295,10 @@ block_norm_kernel(const NormParams p) {
 // of a block reach into a neighbour's run, and their parts go to `partial` as well.  norm_grad_finish_kernel adds the
 // parts in block order, so the result does not depend on scheduling.
 // kPath: the gradient also passes a gate or a post norm, i.e. x takes part.
-template <typename T, int kVpt, int kAccess, bool kPath>
+template <typename T, int kVpt, bool kVec, bool kPath>
 __global__ void __launch_bounds__(kVpt == 4 ? 1024 : 512)
 block_norm_backward_kernel(const NormGradParams p) {
-  constexpr bool kVec = kAccess != kElements;
   __shared__ float red[2][4][32];
-  __shared__ uint32_t abort_word;
-  extern __shared__ __align__(128) uint8_t ring_smem[];
   uint32_t slot = 0;
   const int64_t row0 = static_cast<int64_t>(blockIdx.x) * p.rows / gridDim.x;
   const int64_t row1 = (static_cast<int64_t>(blockIdx.x) + 1) * p.rows / gridDim.x;
@@ -433,23 +316,9 @@ block_norm_backward_kernel(const NormGradParams p) {
   const T* m_dh = static_cast<const T*>(p.dh);
   const T* m_h = p.dy ? static_cast<const T*>(p.h) : nullptr;
   const T* m_x = kPath ? static_cast<const T*>(p.x) : nullptr;
-  RowRing<T, 4> ring{{m_h, m_dy, m_dh, m_x}, {p.ld_h, p.ld_dy, p.ld_dh, p.ld_x}};
-  int stage = 0;
-  uint32_t phase = 0, sm_pre = 0, sm_post = 0;
-  if (kAccess == kBulk) {
-    const uint32_t wb = weight_bytes(p.cols, p.dt_w);
-    sm_pre = smem_u32(ring_smem);
-    sm_post = sm_pre + (p.pre_weight ? wb : 0u);
-    const uint32_t ring_at = sm_post + (post && p.post_weight ? wb : 0u);
-    stage_weights(p.pre_weight, sm_pre, wb);
-    if (post) stage_weights(p.post_weight, sm_post, wb);
-    if (threadIdx.x == 0) abort_word = 0u;
-    ring.start(ring_at, p.stages, p.cols, row0, row1);
-  }
   Raw8<T> gr[kPath ? kVpt : 1];
   int64_t gate_row = group, gate_end = row0;
   for (int64_t row = row0; row < row1; ++row) {
-    if (kAccess == kBulk && __syncthreads_or(!mbar_wait(ring.bars + 8 * stage, phase, &abort_word))) { ring.give_up(p.error_word); return; }
     if (kPath && p.gate && row == gate_end) {
       if (row != row0) ++gate_row;
       gate_end = (gate_row + 1) * p.rows_per_gate;
@@ -463,21 +332,10 @@ block_norm_backward_kernel(const NormGradParams p) {
       const Cols c(i, p.strided);
       Raw8<T> z;
       zero8(z);
-      if (kAccess == kBulk) {
-        a[i] = pairs_of(ring.read(stage, 0, c.base, p.cols));
-        dy[i] = pairs_of(ring.read(stage, 1, c.base, p.cols));
-        t[i] = pairs_of(ring.read(stage, 2, c.base, p.cols));
-        if (kPath) x[i] = pairs_of(ring.read(stage, 3, c.base, p.cols));
-      } else {
-        a[i] = pairs_of(m_h ? load_group<kVec>(m_h + row * p.ld_h, c, p.cols) : z);
-        dy[i] = pairs_of(m_dy ? load_group<kVec>(m_dy + row * p.ld_dy, c, p.cols) : z);
-        t[i] = pairs_of(m_dh ? load_group<kVec>(m_dh + row * p.ld_dh, c, p.cols) : z);
-        if (kPath) x[i] = pairs_of(m_x ? load_group<kVec>(m_x + row * p.ld_x, c, p.cols) : z);
-      }
-    }
-    if (kAccess == kBulk) {
-      ring.release(stage, row);
-      if (++stage == p.stages) { stage = 0; phase ^= 1u; }
+      a[i] = pairs_of(m_h ? load_group<kVec>(m_h + row * p.ld_h, c, p.cols) : z);
+      dy[i] = pairs_of(m_dy ? load_group<kVec>(m_dy + row * p.ld_dy, c, p.cols) : z);
+      t[i] = pairs_of(m_dh ? load_group<kVec>(m_dh + row * p.ld_dh, c, p.cols) : z);
+      if (kPath) x[i] = pairs_of(m_x ? load_group<kVec>(m_x + row * p.ld_x, c, p.cols) : z);
     }
     if (pre_layer || post_layer) {
       float s1[2] = {sum_of(a), 0.0f};
@@ -490,24 +348,29 @@ block_norm_backward_kernel(const NormGradParams p) {
         if (kPath && post_layer) subtract_mean<kVec>(x[i], s1[1] * inv_cols, c, p.cols);
       }
     }
-    // sums over the row: (h - mean)^2, dn (h - mean), dn, (x - mean_x)^2; columns past the end hold zero gradients
+    // sums over the row: (h - mean)^2, dn (h - mean), (x - mean_x)^2, dn; columns past the end hold zero gradients
     float s2[4] = {dot_of(a, a), 0.0f, 0.0f, 0.0f};
-    if constexpr (kPath) s2[3] = dot_of(x, x);
+    if constexpr (kPath) s2[2] = dot_of(x, x);
     Pairs dn[kVpt];
 #pragma unroll
     for (int i = 0; i < kVpt; ++i) {
       const Cols c(i, p.strided);
-      const Pairs w = kAccess == kBulk ? load_weights_shared(p.pre_weight, sm_pre, p.dt_w, c.base, p.cols, 1.0f)
-                                       : load_weights<kVec>(p.pre_weight, p.dt_w, c, p.cols, 1.0f);
+      const Pairs w = load_weights<kVec>(p.pre_weight, p.dt_w, c, p.cols, 1.0f);
 #pragma unroll
       for (int j = 0; j < 4; ++j) dn[i].p[j] = mul2(dy[i].p[j], w.p[j]);
     }
     s2[1] = dot_of(dn, a);
-    if (pre_layer) s2[2] = sum_of(dn);
-    block_sums(s2, red, slot);
-    const float rstd = 1.0f / sqrtf(fmaf(s2[0], inv_cols, p.eps));
-    const float m1 = -s2[1] * rstd * inv_cols, m0 = -s2[2] * inv_cols;
-    const float rstd_x = post ? 1.0f / sqrtf(fmaf(s2[3], inv_cols, p.eps)) : 1.0f;
+    if (pre_layer) s2[3] = sum_of(dn);
+    if (kPath || pre_layer) {
+      block_sums(s2, red, slot);
+    } else {
+      float s[2] = {s2[0], s2[1]};
+      block_sums(s, red, slot);
+      s2[0] = s[0]; s2[1] = s[1];
+    }
+    const float rstd = rsqrtf(fmaf(s2[0], inv_cols, p.eps));
+    const float m1 = -s2[1] * rstd * inv_cols, m0 = -s2[3] * inv_cols;
+    const float rstd_x = post ? rsqrtf(fmaf(s2[2], inv_cols, p.eps)) : 1.0f;
     float2 s3a = both(0.0f), s3b = both(0.0f);
 #pragma unroll
     for (int i = 0; i < kVpt; ++i) {
@@ -540,8 +403,7 @@ block_norm_backward_kernel(const NormGradParams p) {
         const Pairs g = p.gate ? pairs_of(gr[i]) : pairs_filled(1.0f);
         Pairs wp = pairs_filled(1.0f);
         if (post) {
-          wp = kAccess == kBulk ? load_weights_shared(p.post_weight, sm_post, p.dt_w, c.base, p.cols, 1.0f)
-                                : load_weights<kVec>(p.post_weight, p.dt_w, c, p.cols, 1.0f);
+          wp = load_weights<kVec>(p.post_weight, p.dt_w, c, p.cols, 1.0f);
         }
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
@@ -600,6 +462,8 @@ block_norm_backward_kernel(const NormGradParams p) {
   }
 }
 
+#include "hif4_block_norm_bulk.cuh"
+
 // blockIdx.y 0..2: one of the weight gradients, summed over the blocks of the pass above.  From 3 on: the groups of gates
 // that run over a boundary between two blocks, found from the group or from the boundary, whichever there are fewer of.
 constexpr int kFinishCols = 32, kFinishWays = 16;
@@ -641,16 +505,19 @@ norm_grad_finish_kernel(const NormGradParams p, int by_group) {
 }
 
 // ------------------------------------------------------------------------------------------------------- host side
-// Groups of eight columns per thread: one up to 4096 columns, then two, then four (and up to 1024 threads).
-int groups_per_thread(int64_t cols) { return cols <= 4096 ? 1 : cols <= 8192 ? 2 : 4; }
+// Groups of eight columns per thread.  Forward: two while 320 threads reach the row's end (8192 x 5120, two blocks an SM:
+// 63 us; one group 78 us, four 68 us), more beyond.  Backward: the column sums take 32 registers a group, so one while
+// 512 threads reach (4000 x 4096: 81 us, two groups 87 us).
+int groups_forward(int64_t cols) { return cols <= 1024 ? 1 : cols <= 5120 ? 2 : cols <= 16384 ? 4 : 8; }
+int groups_backward(int64_t cols) { return cols <= 4096 ? 1 : cols <= 8192 ? 2 : 4; }
 int threads_for(int64_t cols, int vpt) {
   const int64_t t = ceil_div64(ceil_div64(cols, 8), vpt);
   return static_cast<int>(ceil_div64(t, 32) * 32);
 }
-// Blocks per SM and, for the bulk form, stages per block: as many blocks as the registers let run (the grid of the
-// backward pass must not depend on the device's state, so the count comes from the thread number alone), and the ring
-// shares what shared memory there is between them.
+// Shared memory that the rings of an SM's blocks share, and the most stages of one.
 constexpr int kRingBytes = 200 * 1024, kMaxRing = 8;
+// Blocks per SM from the thread count alone: the sums of the backward pass run block by block, and their order must depend
+// on nothing but the sizes.  The forward pass also asks how many blocks the registers admit (launch_norm).
 int blocks_per_sm(int threads, int threads_per_sm) {
   const int b = threads_per_sm / threads;
   return b < 1 ? 1 : b > 16 ? 16 : b;
@@ -659,7 +526,7 @@ int grid_for(int64_t rows, int threads, int threads_per_sm) {
   const int64_t g = static_cast<int64_t>(sm_count()) * blocks_per_sm(threads, threads_per_sm);
   return static_cast<int>(rows < g ? rows : g);
 }
-constexpr int kForwardThreadsPerSm = 1024, kBackwardThreadsPerSm = 512;
+constexpr int kForwardThreadsPerSm = 768, kBackwardThreadsPerSm = 512;
 
 // Stages of the ring beside `weights` bytes of weights, or 0: rows too short, too few of them per block, or too wide for two stages.
 int ring_stages(int64_t rows, int grid, int per_sm, size_t stage_bytes, size_t weights) {
@@ -670,6 +537,9 @@ int ring_stages(int64_t rows, int grid, int per_sm, size_t stage_bytes, size_t w
 
 size_t type_size(int dt) { return dt == HIF4_FP32 ? 4 : 2; }
 bool aligned_to(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+template <typename T> int type_of() { return HIF4_BF16; }
+template <> int type_of<__half>() { return HIF4_FP16; }
+template <> int type_of<float>() { return HIF4_FP32; }
 bool known_type(int dt) { return dt == HIF4_BF16 || dt == HIF4_FP32 || dt == HIF4_FP16; }
 bool known_kind(int k) { return k == HIF4_NORM_NONE || k == HIF4_NORM_RMS || k == HIF4_NORM_LAYER; }
 
@@ -691,52 +561,76 @@ hif4_status check_operands(const Operand* o, int n, int64_t rows, int64_t cols, 
   return HIF4_OK;
 }
 
+template <typename T, typename W, int kVpt>
+hif4_status launch_norm_bulk(const NormParams& p, int grid, int threads, size_t smem, cudaStream_t st) {
+  static uint64_t smem_opt_in = 0;
+  if (!ensure_dynamic_smem(block_norm_bulk_kernel<T, W, kVpt>, kRingBytes + 128, smem_opt_in)) return HIF4_ERR_CUDA;
+  block_norm_bulk_kernel<T, W, kVpt><<<grid, threads, smem, st>>>(p);
+  note_launch();
+  return launch_status();
+}
 template <typename T, int kVpt>
 hif4_status launch_norm(NormParams p, bool vec, cudaStream_t st) {
-  const int threads = threads_for(p.cols, kVpt), grid = grid_for(p.rows, threads, kForwardThreadsPerSm);
+  const int threads = threads_for(p.cols, kVpt);
+  const bool wide = p.dt_w == HIF4_FP32;
   const size_t stage = static_cast<size_t>(p.cols) * sizeof(T) * (p.residual ? 2 : 1);
-  const size_t weights = static_cast<size_t>(p.cols) * type_size(p.dt_w) * ((p.post_weight ? 1 : 0) + (p.pre_weight ? 1 : 0) + (p.pre_bias ? 1 : 0));
-  p.stages = vec ? ring_stages(p.rows, grid, blocks_per_sm(threads, kForwardThreadsPerSm), stage, weights) : 0;
-  if (p.stages > 0) {
-    static uint64_t smem_opt_in = 0;
-    if (!ensure_dynamic_smem(block_norm_kernel<T, kVpt, kBulk>, kRingBytes + 128, smem_opt_in)) return HIF4_ERR_CUDA;
-    p.error_word = device_error_word();
-    if (!p.error_word) return HIF4_ERR_CUDA;
-    block_norm_kernel<T, kVpt, kBulk><<<grid, threads, 128 + weights + p.stages * stage, st>>>(p);
-  } else if (vec) {
-    block_norm_kernel<T, kVpt, kVectors><<<grid, threads, 0, st>>>(p);
-  } else {
-    block_norm_kernel<T, kVpt, kElements><<<grid, threads, 0, st>>>(p);
+  const size_t weights = static_cast<size_t>(p.cols) * type_size(p.dt_w) * ((p.y ? 1 : 0) + (p.kind_post != HIF4_NORM_NONE ? 1 : 0) + (p.pre_bias ? 1 : 0));
+  if (vec && (wide || p.dt_w == type_of<T>())) {
+    // blocks that the registers let run side by side: a block that had to wait for another's end would double the time
+    int fits = 1;
+    const cudaError_t e = wide ? cudaOccupancyMaxActiveBlocksPerMultiprocessor(&fits, block_norm_bulk_kernel<T, float, kVpt>, threads, 0)
+                               : cudaOccupancyMaxActiveBlocksPerMultiprocessor(&fits, block_norm_bulk_kernel<T, T, kVpt>, threads, 0);
+    if (e != cudaSuccess) return HIF4_ERR_CUDA;
+    const int want = blocks_per_sm(threads, kForwardThreadsPerSm), per_sm = fits < 1 ? 1 : fits < want ? fits : want;
+    const int64_t all = static_cast<int64_t>(sm_count()) * per_sm;
+    const int grid = static_cast<int>(p.rows < all ? p.rows : all);
+    p.stages = ring_stages(p.rows, grid, per_sm, stage, weights);
+    if (p.stages > 0) {
+      p.error_word = device_error_word();
+      if (!p.error_word) return HIF4_ERR_CUDA;
+      const size_t smem = 128 + weights + p.stages * stage;
+      return wide ? launch_norm_bulk<T, float, kVpt>(p, grid, threads, smem, st) : launch_norm_bulk<T, T, kVpt>(p, grid, threads, smem, st);
+    }
   }
+  const int grid = grid_for(p.rows, threads, kForwardThreadsPerSm);
+  if (vec) block_norm_kernel<T, kVpt, true><<<grid, threads, 0, st>>>(p);
+  else block_norm_kernel<T, kVpt, false><<<grid, threads, 0, st>>>(p);
   note_launch();
   return launch_status();
 }
 template <typename T>
 hif4_status launch_norm_t(const NormParams& p, bool vec, cudaStream_t st) {
-  switch (groups_per_thread(p.cols)) {
+  switch (groups_forward(p.cols)) {
     case 1: return launch_norm<T, 1>(p, vec, st);
     case 2: return launch_norm<T, 2>(p, vec, st);
-    default: return launch_norm<T, 4>(p, vec, st);
+    case 4: return launch_norm<T, 4>(p, vec, st);
+    default: return launch_norm<T, 8>(p, vec, st);
   }
 }
 
+template <typename T, typename W, int kVpt, bool kPath>
+hif4_status launch_norm_grad_bulk(const NormGradParams& p, int threads, size_t smem, cudaStream_t st) {
+  static uint64_t smem_opt_in = 0;
+  if (!ensure_dynamic_smem(block_norm_backward_bulk_kernel<T, W, kVpt, kPath>, kRingBytes + 128, smem_opt_in)) return HIF4_ERR_CUDA;
+  block_norm_backward_bulk_kernel<T, W, kVpt, kPath><<<p.grid, threads, smem, st>>>(p);
+  note_launch();
+  return launch_status();
+}
 template <typename T, int kVpt, bool kPath>
 hif4_status launch_norm_grad(NormGradParams p, bool vec, int threads, cudaStream_t st) {
+  const bool wide = p.dt_w == HIF4_FP32;
   const int mats = (p.dy ? 2 : 0) + (p.dh ? 1 : 0) + (kPath && p.x ? 1 : 0);
   const size_t stage = static_cast<size_t>(p.cols) * sizeof(T) * mats;
-  const size_t weights = static_cast<size_t>(p.cols) * type_size(p.dt_w) * ((p.pre_weight ? 1 : 0) + (kPath && p.post_weight ? 1 : 0));
-  p.stages = vec ? ring_stages(p.rows, p.grid, blocks_per_sm(threads, kBackwardThreadsPerSm), stage, weights) : 0;
+  const size_t weights = static_cast<size_t>(p.cols) * type_size(p.dt_w) * ((p.dy ? 1 : 0) + (p.kind_post != HIF4_NORM_NONE ? 1 : 0));
+  p.stages = vec && (wide || p.dt_w == type_of<T>()) ? ring_stages(p.rows, p.grid, blocks_per_sm(threads, kBackwardThreadsPerSm), stage, weights) : 0;
   if (p.stages > 0) {
-    static uint64_t smem_opt_in = 0;
-    if (!ensure_dynamic_smem(block_norm_backward_kernel<T, kVpt, kBulk, kPath>, kRingBytes + 128, smem_opt_in)) return HIF4_ERR_CUDA;
     p.error_word = device_error_word();
     if (!p.error_word) return HIF4_ERR_CUDA;
-    block_norm_backward_kernel<T, kVpt, kBulk, kPath><<<p.grid, threads, 128 + weights + p.stages * stage, st>>>(p);
-  } else if (vec) {
-    block_norm_backward_kernel<T, kVpt, kVectors, kPath><<<p.grid, threads, 0, st>>>(p);
-  } else {
-    block_norm_backward_kernel<T, kVpt, kElements, kPath><<<p.grid, threads, 0, st>>>(p);
+    const size_t smem = 128 + weights + p.stages * stage;
+    return wide ? launch_norm_grad_bulk<T, float, kVpt, kPath>(p, threads, smem, st) : launch_norm_grad_bulk<T, T, kVpt, kPath>(p, threads, smem, st);
   }
+  if (vec) block_norm_backward_kernel<T, kVpt, true, kPath><<<p.grid, threads, 0, st>>>(p);
+  else block_norm_backward_kernel<T, kVpt, false, kPath><<<p.grid, threads, 0, st>>>(p);
   note_launch();
   return launch_status();
 }
@@ -747,8 +641,8 @@ hif4_status launch_norm_grad(const NormGradParams& p, bool vec, int threads, cud
 }
 template <typename T>
 hif4_status launch_norm_grad_t(const NormGradParams& p, bool vec, cudaStream_t st) {
-  const int vpt = groups_per_thread(p.cols), threads = threads_for(p.cols, vpt);
-  const hif4_status s = vpt == 1 ? launch_norm_grad<T, 1>(p, vec, threads, st)
+  const int vpt = groups_backward(p.cols), threads = threads_for(p.cols, vpt);
+  const hif4_status s = vpt == 1   ? launch_norm_grad<T, 1>(p, vec, threads, st)
                         : vpt == 2 ? launch_norm_grad<T, 2>(p, vec, threads, st) : launch_norm_grad<T, 4>(p, vec, threads, st);
   if (s != HIF4_OK) return s;
   int planes = p.dpre_weight || p.dpre_bias || p.dpost_weight ? 3 : 0, by_group = 0;
@@ -765,7 +659,7 @@ hif4_status launch_norm_grad_t(const NormGradParams& p, bool vec, cudaStream_t s
 }
 
 int backward_grid(int64_t rows, int64_t cols) {
-  return grid_for(rows, threads_for(cols, groups_per_thread(cols)), kBackwardThreadsPerSm);
+  return grid_for(rows, threads_for(cols, groups_backward(cols)), kBackwardThreadsPerSm);
 }
 
 }  // namespace
