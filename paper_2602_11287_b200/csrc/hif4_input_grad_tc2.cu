@@ -218,7 +218,7 @@ input_grad_tc2_kernel(const __grid_constant__ CUtensorMap tmZ, const __grid_cons
     // ---------------------------------------------------------------- epilogue
     const int q = warp & 3;
     const uint32_t tmem_empty_leader = mapa(tmem_empty, 0);
-    const uint32_t stage = out_base + static_cast<uint32_t>(q) * (2 * kSlabBytes);
+    const uint32_t stage = out_base + static_cast<uint32_t>(q) * (kStageBufs * kSlabBytes);
     uint32_t tcount = 0, slabs = 0;
     for (int it = 0; it < n_items; ++it, ++tcount) {
       const WorkItem w = work_item<kPairN>(p, pair, num_pairs, it);
@@ -229,7 +229,7 @@ input_grad_tc2_kernel(const __grid_constant__ CUtensorMap tmZ, const __grid_cons
       const bool adds = shared_tile && w.slice > 0, leaves = shared_tile && w.slice + 1 < p.slices;
       unsigned int* my_flag = shared_tile ? p.flags + (static_cast<size_t>(w.tail) * p.slices + w.slice) * 8 + rank * 4 + q : nullptr;
       if (adds && !__all_sync(0xFFFFFFFFu, wait_count(my_flag - 8, 1u, abort_flag))) break;
-      float* part = shared_tile ? p.partial + (static_cast<size_t>(w.tail) * 2 + rank) * (kRows * kPairN) + q * 32 + lane : nullptr;
+      float4* part = shared_tile ? partial_of(p.partial, w.tail, rank, q, lane) : nullptr;
       const int64_t row0 = static_cast<int64_t>(w.m0) + rank * kRows + q * 32, row = row0 + lane;
       const uint32_t t_row = tmem_base + (static_cast<uint32_t>(q * 32) << 16) + acc * kPairN;
 #pragma unroll 1
@@ -254,13 +254,9 @@ input_grad_tc2_kernel(const __grid_constant__ CUtensorMap tmZ, const __grid_cons
             if (lane == 0) mbar_arrive_cluster(tmem_empty_leader + 8 * acc);
           }
           if (!inside) continue;
-          if (adds) {
-#pragma unroll
-            for (int e = 0; e < 16; ++e) z[e] += __ldcg(part + (c + e) * kRows);
-          }
+          if (adds) add_partial16(z, part + c * 8);
           if (leaves) {
-#pragma unroll
-            for (int e = 0; e < 16; ++e) __stcg(part + (c + e) * kRows, z[e]);
+            leave_partial16(z, part + c * 8);
             continue;
           }
 #pragma unroll

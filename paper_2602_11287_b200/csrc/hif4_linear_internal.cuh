@@ -31,7 +31,7 @@ struct LinearParams {
   int64_t M, N;
   int num_kc, n_tiles, full_rounds, tail_tiles, slices, sk_tiles, sk_tile0;      // schedule (hif4_tc2_dense.cuh)
   unsigned int* flags;              // [shared tiles][slices][8]: "this epilogue warp's rows of this slice's sums are there"
-  float* partial;                   // [shared tiles][2 ranks][256 columns][128 rows]
+  float* partial;                   // [shared tiles][2 ranks][4 warps][16 x 16 columns][4][32 rows][4]
   unsigned int* error_word;
   DecodeMul mul;
   int tma;                          // 1: units come through TMA, 0: copied word by word
@@ -39,10 +39,9 @@ struct LinearParams {
   int64_t pitch;                    // bytes of a row of units
   int upr;                          // units of a row
   const void *bias, *bias_up;
-  int act;
   const void* side;
   int64_t ld_side;
-  int side_vec;
+  int side_vec, side_tma;
   float res_scale;
   void* y;
   int64_t ld_y;
@@ -61,7 +60,9 @@ hif4_status launch_linear_gemv(const LinearCall& c, const void* x, int dt_x, int
 size_t linear_tc2_workspace(bool gated, int64_t M, int64_t N, int64_t K);
 bool linear_tc2_supported(bool gated, int64_t M, int64_t N, int64_t K);
 hif4_status launch_linear_tc2(const LinearCall& c, void* workspace, cudaStream_t st);
+hif4_status launch_gated_tc2(const LinearCall& c, void* workspace, cudaStream_t st);
 hif4_status launch_linear_tc2_grad(const LinearCall& c, void* workspace, cudaStream_t st);
+hif4_status launch_gated_tc2_grad(const LinearCall& c, void* workspace, cudaStream_t st);
 
 // dX = sum over phases dZ W: `parts` BF16 planes of [M, ld_dz] per weight matrix (rows 16-byte aligned, plane after
 // plane), one or two weight matrices.

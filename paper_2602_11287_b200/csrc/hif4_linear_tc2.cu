@@ -1,4 +1,4 @@
-// Forward instances of the CTA-pair linear kernel.
+// Forward instances of the CTA-pair linear kernel, one projection; sizes of all of them.
 #include "hif4_linear_tc2_launch.cuh"
 
 namespace hif4 {
@@ -15,11 +15,7 @@ bool linear_tc2_supported(bool gated, int64_t M, int64_t N, int64_t K) {
 }
 
 hif4_status launch_linear_tc2(const LinearCall& c, void* workspace, cudaStream_t st) {
-  if (c.gated) {
-    if (c.dt == HIF4_BF16) return launch_linear<true, false, __nv_bfloat16>(c, workspace, st);
-    if (c.dt == HIF4_FP16) return launch_linear<true, false, __half>(c, workspace, st);
-    return launch_linear<true, false, float>(c, workspace, st);
-  }
+  if (c.gated) return launch_gated_tc2(c, workspace, st);
   if (c.dt == HIF4_BF16) return launch_linear<false, false, __nv_bfloat16>(c, workspace, st);
   if (c.dt == HIF4_FP16) return launch_linear<false, false, __half>(c, workspace, st);
   return launch_linear<false, false, float>(c, workspace, st);

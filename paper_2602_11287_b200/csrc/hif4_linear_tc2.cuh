@@ -27,7 +27,8 @@ namespace hif4 {
 namespace {
 
 constexpr int kSlabBytes = 32 * 64;                   // 32 rows of one epilogue warp x 64 bytes
-constexpr int kStageOutBytes = 4 * 2 * kSlabBytes;    // 4 warps x 2 buffers (or one buffer of 32 x 128 bytes for units)
+constexpr int kStageBufs = 3;
+constexpr int kStageOutBytes = 4 * kStageBufs * kSlabBytes;    // 4 warps x 3 buffers (units: two of them as one of 32 x 128 bytes)
 constexpr int kLinSmemBytes = 1024 /*alignment slack*/ + kDecStages * kDecStageBytes + kRawStages * kRawStageBytes + kStageOutBytes +
                               256 /*barriers*/ + 1024 /*spread table*/;
 constexpr uint32_t kLinInstrDesc = (1u << 4) | (1u << 7) | (1u << 10) | (static_cast<uint32_t>(kPairN >> 3) << 17) |
@@ -47,36 +48,42 @@ __device__ __forceinline__ void load16(const T* p, bool vec, int valid, float (&
     for (int e = 0; e < 16; ++e) v[e] = e < valid ? to_f32(p[e]) : 0.0f;
   }
 }
-__device__ __forceinline__ void activate16(float (&v)[16], int act) {
-  switch (act) {
-#define HIF4_ACT_CASE(kind) \
-  case kind:                \
-    _Pragma("unroll") for (int e = 0; e < 16; ++e) v[e] = activate(v[e], kind); \
-    break;
-    HIF4_ACT_CASE(HIF4_ACT_RELU)
-    HIF4_ACT_CASE(HIF4_ACT_SILU)
-    HIF4_ACT_CASE(HIF4_ACT_GELU)
-    HIF4_ACT_CASE(HIF4_ACT_GELU_TANH)
-#undef HIF4_ACT_CASE
-    default: break;
+// Partial sums of 16 columns of a row: four 16-byte words, each beside those of the warp's other rows.
+__device__ __forceinline__ void add_partial16(float (&v)[16], const float4* part) {
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const float4 f = __ldcg(part + k * 32);
+    v[4 * k] += f.x; v[4 * k + 1] += f.y; v[4 * k + 2] += f.z; v[4 * k + 3] += f.w;
   }
 }
-// a = act(z), z = act'(z)
-__device__ __forceinline__ void activate_slope16(float (&z)[16], float (&a)[16], int act) {
-  switch (act) {
-#define HIF4_ACT_CASE(kind) \
-  case kind:                \
-    _Pragma("unroll") for (int e = 0; e < 16; ++e) { float s; activate_slope(z[e], kind, a[e], s); z[e] = s; } \
-    break;
-    HIF4_ACT_CASE(HIF4_ACT_RELU)
-    HIF4_ACT_CASE(HIF4_ACT_SILU)
-    HIF4_ACT_CASE(HIF4_ACT_GELU)
-    HIF4_ACT_CASE(HIF4_ACT_GELU_TANH)
-#undef HIF4_ACT_CASE
-    default:
+__device__ __forceinline__ void leave_partial16(const float (&v)[16], float4* part) {
 #pragma unroll
-      for (int e = 0; e < 16; ++e) { a[e] = z[e]; z[e] = 1.0f; }
+  for (int k = 0; k < 4; ++k) __stcg(part + k * 32, make_float4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]));
+}
+// A warp's corner of a shared tile's sums: 256 columns x 32 rows, 16 columns (2 KB) after 16 columns.
+__device__ __forceinline__ float4* partial_of(float* partial, int tail, uint32_t rank, int q, int lane) {
+  return reinterpret_cast<float4*>(partial) + ((static_cast<size_t>(tail) * 2 + rank) * 4 + q) * (32 * kPairN / 4) + lane;
+}
+template <int kAct>
+__device__ __forceinline__ void activate16(float (&v)[16]) {
+#pragma unroll
+  for (int e = 0; e < 16; ++e) v[e] = activate(v[e], kAct);
+}
+// a = act(z), z = act'(z)
+template <int kAct>
+__device__ __forceinline__ void activate_slope16(float (&z)[16], float (&a)[16]) {
+#pragma unroll
+  for (int e = 0; e < 16; ++e) {
+    float s;
+    activate_slope(z[e], kAct, a[e], s);
+    z[e] = s;
   }
+}
+// Waits for a tcgen05.ld into r; the registers pass through, so that nothing reads them before.
+__device__ __forceinline__ void tc_wait_ld16(uint32_t (&r)[16]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]),
+                 "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15])::"memory");
 }
 // Sums of the 16 columns over the 32 rows of a warp (lane = row), halving the columns a lane still owns at every step:
 // lane l ends with column (l >> 1) & 15 ... of the order below, both lanes of a pair with the same sum.
@@ -122,11 +129,13 @@ __device__ __forceinline__ void store_parts(const float (&v)[16], __nv_bfloat16*
   }
 }
 
-// kGated: two projections.  kGrad: the gradient form.  T: type of bias, residual, Y and dY.
-template <bool kGated, bool kGrad, typename T>
+// kGated: two projections.  kGrad: the gradient form.  T: type of bias, residual, Y and dY.  kAct: the activation (one kernel
+// each: five activations side by side cost the epilogue spills and instruction-cache misses).
+template <bool kGated, bool kGrad, typename T, int kAct>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 linear_tc2_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
-                  const __grid_constant__ CUtensorMap tmB2, const __grid_constant__ CUtensorMap tmY, const LinearParams p) {
+                  const __grid_constant__ CUtensorMap tmB2, const __grid_constant__ CUtensorMap tmY,
+                  const __grid_constant__ CUtensorMap tmSide, const LinearParams p) {
   constexpr int kOutCols = kGated ? kPairN / 2 : kPairN;             // outputs per tile row
   constexpr int kSlabCols = 64 / sizeof(T);                          // outputs per staged 64-byte row
   extern __shared__ uint8_t smem_raw[];
@@ -136,7 +145,7 @@ linear_tc2_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
   const uint32_t out_base = raw_base + kRawStages * kRawStageBytes;
   const uint32_t bar_base = out_base + kStageOutBytes;
   const uint32_t raw_full = bar_base, raw_empty = bar_base + 16, dec_full = bar_base + 32, dec_empty = bar_base + 64,
-                 tmem_full = bar_base + 96, tmem_empty = bar_base + 112;
+                 tmem_full = bar_base + 96, tmem_empty = bar_base + 112, side_full = bar_base + 144;      // [4 warps][kStageBufs]
   uint8_t* gen_base = smem_raw + (smem_base - smem_u32(smem_raw));
   volatile uint32_t* tmem_ptr_smem = reinterpret_cast<volatile uint32_t*>(gen_base + (bar_base - smem_base) + 128);
   volatile uint32_t* abort_flag = tmem_ptr_smem + 1;
@@ -162,6 +171,7 @@ linear_tc2_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
       mbar_init(tmem_full + 8 * s, 1);
       mbar_init(tmem_empty + 8 * s, 8);               // 4 epilogue warps of each CTA (used on rank 0)
     }
+    for (int s = 0; s < 4 * kStageBufs; ++s) mbar_init(side_full + 8 * s, 1);
     *abort_flag = 0u;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -259,193 +269,231 @@ linear_tc2_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
     // ---------------------------------------------------------------- epilogue
     const int q = warp & 3;                      // TMEM lane quadrant this warp may read
     const uint32_t tmem_empty_leader = mapa(tmem_empty, 0);
-    const uint32_t stage = out_base + static_cast<uint32_t>(q) * (2 * kSlabBytes);
+    const uint32_t stage = out_base + static_cast<uint32_t>(q) * (kStageBufs * kSlabBytes);
+    const uint32_t my_side_full = side_full + static_cast<uint32_t>(q) * (8 * kStageBufs);
+    const uint32_t sw = (static_cast<uint32_t>(lane) >> 1) & 3u;          // SWIZZLE_64B: 16-byte chunk c of row r at c ^ ((r >> 1) & 3)
     const T* bias = static_cast<const T*>(p.bias);
     const T* bias2 = static_cast<const T*>(p.bias_up);
     const T* side = static_cast<const T*>(p.side);        // residual, or dY in the gradient form
     const bool bias_vec = (reinterpret_cast<uintptr_t>(bias) & 15u) == 0 && (reinterpret_cast<uintptr_t>(bias2) & 15u) == 0;
-    uint32_t tcount = 0, slabs = 0;
+    constexpr int kSlabParts = kSlabCols / 16;
+    uint32_t tcount = 0, buf = 0, buf_phase = 0;          // staging buffer in turn, parity of its side barrier
     for (int it = 0; it < n_items; ++it, ++tcount) {
       const WorkItem w = work_item<kOutCols>(p, pair, num_pairs, it);
       const uint32_t acc = tcount & 1u, aph = (tcount >> 1) & 1u;
-      if (!__all_sync(0xFFFFFFFFu, mbar_wait(tmem_full + 8 * acc, aph, abort_flag, 256))) break;
-      tc_fence_after();
-      const bool shared_tile = w.tail >= 0 && p.slices > 1;
-      const bool adds = shared_tile && w.slice > 0, leaves = shared_tile && w.slice + 1 < p.slices;
-      unsigned int* my_flag = shared_tile ? p.flags + (static_cast<size_t>(w.tail) * p.slices + w.slice) * 8 + rank * 4 + q : nullptr;
-      if (adds && !__all_sync(0xFFFFFFFFu, wait_count(my_flag - 8, 1u, abort_flag))) break;
-      // this thread's row of the partial sums, column after column
-      float* part = shared_tile ? p.partial + (static_cast<size_t>(w.tail) * 2 + rank) * (kRows * kPairN) + q * 32 + lane : nullptr;
       const int64_t row0 = static_cast<int64_t>(w.m0) + rank * kRows + q * 32, row = row0 + lane;
       const bool row_ok = row < p.M;
-      const uint32_t t_row = tmem_base + (static_cast<uint32_t>(q * 32) << 16) + acc * kPairN;
-#pragma unroll 1
-      for (int slab = 0; slab < kOutCols / kSlabCols; ++slab) {
-        const int64_t col0 = static_cast<int64_t>(w.n0) + slab * kSlabCols;
-        const bool inside = row0 < p.M && col0 < p.N;                    // same for the whole warp
-        uint32_t words[16];
-#pragma unroll
-        for (int h = 0; h < kSlabCols / 16; ++h) {
-          const int c = slab * kSlabCols + h * 16;                       // tile column
-          float z[16], u[16];
-          if (inside) {
-            uint32_t r[16];
-            tc_ld16(t_row + c, r);
-            if (kGated) {
-              uint32_t r2[16];
-              tc_ld16(t_row + kOutCols + c, r2);
-              tc_wait_ld();
-#pragma unroll
-              for (int e = 0; e < 16; ++e) u[e] = __uint_as_float(r2[e]);
-            } else {
-              tc_wait_ld();
-            }
-#pragma unroll
-            for (int e = 0; e < 16; ++e) z[e] = __uint_as_float(r[e]);
-          }
-          if (slab == kOutCols / kSlabCols - 1 && h == kSlabCols / 16 - 1) {   // accumulator fully read: hand it back before the rest
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive_cluster(tmem_empty_leader + 8 * acc);
-          }
-          if (!inside) continue;
-          if (adds) {
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-              z[e] += __ldcg(part + (c + e) * kRows);
-              if (kGated) u[e] += __ldcg(part + (kOutCols + c + e) * kRows);
-            }
-          }
-          if (leaves) {
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-              __stcg(part + (c + e) * kRows, z[e]);
-              if (kGated) __stcg(part + (kOutCols + c + e) * kRows, u[e]);
-            }
-            continue;
-          }
-          const int64_t col = col0 + h * 16;
-          const int valid = p.N - col < 16 ? static_cast<int>(p.N - col) : 16;      // may be <= 0 in the second half of a slab
-          if (bias) {
-            float b[16];
-            load16(bias + col, bias_vec && valid == 16, valid, b);
-#pragma unroll
-            for (int e = 0; e < 16; ++e) z[e] += b[e];
-          }
-          if (kGated && bias2) {
-            float b[16];
-            load16(bias2 + col, bias_vec && valid == 16, valid, b);
-#pragma unroll
-            for (int e = 0; e < 16; ++e) u[e] += b[e];
-          }
-          if (!kGrad) {
-            activate16(z, p.act);
-            if (kGated) {
-#pragma unroll
-              for (int e = 0; e < 16; ++e) z[e] *= u[e];
-            }
-            if (side && row_ok) {
-              float s[16];
-              load16(side + row * p.ld_side + col, p.side_vec && valid == 16, valid, s);
-#pragma unroll
-              for (int e = 0; e < 16; ++e) z[e] = fmaf(p.res_scale, s[e], z[e]);
-            }
-            if (sizeof(T) == 2) {
-#pragma unroll
-              for (int e = 0; e < 8; ++e) words[(8 * h + e) & 15] = pack2(z[2 * e], z[2 * e + 1], T16<T>());
-            } else {
-#pragma unroll
-              for (int e = 0; e < 16; ++e) words[e] = __float_as_uint(z[e]);
-            }
-          } else {
-            float d[16], a[16];
-            load16(side + (row_ok ? row : row0) * p.ld_side + col, p.side_vec && valid == 16, valid, d);
-            activate_slope16(z, a, p.act);
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-              const bool in = row_ok && e < valid;
-              z[e] = in ? d[e] * z[e] * (kGated ? u[e] : 1.0f) : 0.0f;
-              if (kGated) u[e] = in ? d[e] * a[e] : 0.0f;
-            }
-            constexpr int kParts = sizeof(T16<T>) == 2 && IsHalf<T>::value ? 2 : 1;
-            if (p.dz && row_ok) {
-              __nv_bfloat16* dst = p.dz + row * p.ld_dz + col;
-              store_parts<kParts>(z, dst, p.dz_plane, p.ld_dz - col);
-              if (kGated) store_parts<kParts>(u, dst + kParts * p.dz_plane, p.dz_plane, p.ld_dz - col);
-            }
-            if (p.colsum) {
-              const float sz = column_sum16(z, lane);
-              const int cl = column_of_lane(lane);
-              float* sums = p.colsum + (row0 >> 5) * p.N + col;
-              if ((lane & 1) == 0 && cl < valid) sums[cl] = sz;
-              if (kGated) {
-                const float su = column_sum16(u, lane);
-                if ((lane & 1) == 0 && cl < valid) sums[p.colsum_plane + cl] = su;
-              }
-            }
-          }
-        }
-        if (kGrad || !inside || leaves) continue;
-        if (p.units) {
-          // 64 columns of 32 rows as 128-byte rows, 16-byte chunk c of row r at c ^ (r & 7); then eight lanes per unit
-          if (sizeof(T) == 2) {
-            const uint32_t my = stage + static_cast<uint32_t>(lane) * 128u;
-#pragma unroll
-            for (int v = 0; v < 4; ++v)
-              sts128(my + (((static_cast<uint32_t>(slab & 1) * 4u + v) ^ (static_cast<uint32_t>(lane) & 7u)) << 4), words[4 * v], words[4 * v + 1],
-                     words[4 * v + 2], words[4 * v + 3]);
-            if (slab & 1) {
-              __syncwarp();
-#pragma unroll 1
-              for (int pass = 0; pass < 8; ++pass) {
-                const int r = pass * 4 + (lane >> 3), g = lane & 7;
-                Raw8<T16<T>> x;
-                x.a = lds128(stage + static_cast<uint32_t>(r) * 128u + ((static_cast<uint32_t>(g) ^ (static_cast<uint32_t>(r) & 7u)) << 4));
-                uint32_t meta;
-                const uint32_t code = p.rha ? encode_unit_octet<true>(x, g, meta) : encode_unit_octet<false>(x, g, meta);
-                if (row0 + r < p.M) {
-                  uint32_t* dst = static_cast<uint32_t*>(p.y) + ((row0 + r) * (p.N >> 6) + (col0 >> 6)) * kUnitWords;
-                  dst[1 + g] = code;
-                  if (g == 0) dst[0] = meta;
-                }
-              }
-              __syncwarp();
-            }
-          }
-        } else if (p.tma_store) {
-          const uint32_t buf = stage + (slabs & 1u) * kSlabBytes;
-          const uint32_t my = buf + static_cast<uint32_t>(lane) * 64u, sw = (static_cast<uint32_t>(lane) >> 1) & 3u;    // SWIZZLE_64B
-          if (lane == 0) bulk_wait_read<1>();        // the store that used this buffer two slabs ago has read it
-          __syncwarp();
-#pragma unroll
-          for (int v = 0; v < 4; ++v)
-            sts128(my + ((static_cast<uint32_t>(v) ^ sw) << 4), words[4 * v], words[4 * v + 1], words[4 * v + 2], words[4 * v + 3]);
-          fence_proxy_async_smem();                  // generic-proxy writes -> visible to the TMA store
-          __syncwarp();
-          if (lane == 0) {
-            tma_store_2d(&tmY, static_cast<int>(col0), static_cast<int>(row0), buf);
-            bulk_commit();
-          }
-          ++slabs;
-        } else if (row_ok) {
-          T* dst = static_cast<T*>(p.y) + row * p.ld_y + col0;
-          if (p.y_vec && col0 + kSlabCols <= p.N) {
-#pragma unroll
-            for (int v = 0; v < 4; ++v)
-              reinterpret_cast<uint4*>(dst)[v] = make_uint4(words[4 * v], words[4 * v + 1], words[4 * v + 2], words[4 * v + 3]);
-          } else {
-            const int64_t left = p.N - col0;
-#pragma unroll
-            for (int e = 0; e < kSlabCols; ++e) {
-              if (e >= left) continue;
-              if (sizeof(T) == 2) reinterpret_cast<uint16_t*>(dst)[e] = static_cast<uint16_t>(words[(e >> 1) & 15] >> (16 * (e & 1)));
-              else reinterpret_cast<uint32_t*>(dst)[e] = words[e & 15];
-            }
-          }
+      const bool shared_tile = w.tail >= 0 && p.slices > 1;
+      const bool adds = shared_tile && w.slice > 0, leaves = shared_tile && w.slice + 1 < p.slices;
+      // steps of 16 columns that hold outputs (a slab is done as a whole)
+      const int64_t cols_left = p.N - w.n0;
+      const int parts = row0 >= p.M ? 0 : cols_left >= kOutCols ? kOutCols / 16 : static_cast<int>((cols_left + kSlabCols - 1) / kSlabCols) * kSlabParts;
+      // Residual or dY through the staging buffers: two slabs are requested ahead, the first two while the product still runs.
+      const bool side_staged = p.side_tma && !leaves;
+      if (side_staged && lane == 0 && parts > 0) {
+        bulk_wait_read<1>();                             // the two buffers' last stores have read them
+        for (int s = 0; s < 2 && s * kSlabParts < parts; ++s) {
+          const uint32_t b = (buf + s) % kStageBufs;
+          mbar_expect_tx(my_side_full + 8 * b, kSlabBytes);
+          tma_load_2d(stage + b * kSlabBytes, &tmSide, w.n0 + s * kSlabCols, static_cast<int>(row0), my_side_full + 8 * b);
         }
       }
+      if (!__all_sync(0xFFFFFFFFu, mbar_wait(tmem_full + 8 * acc, aph, abort_flag, 256))) break;
+      tc_fence_after();
+      unsigned int* my_flag = shared_tile ? p.flags + (static_cast<size_t>(w.tail) * p.slices + w.slice) * 8 + rank * 4 + q : nullptr;
+      if (adds && !__all_sync(0xFFFFFFFFu, wait_count(my_flag - 8, 1u, abort_flag))) break;
+      float4* part_sums = shared_tile ? partial_of(p.partial, w.tail, rank, q, lane) : nullptr;
+      const uint32_t t_row = tmem_base + (static_cast<uint32_t>(q * 32) << 16) + acc * kPairN;
+      uint32_t r[16];
+      if (!kGated && parts > 0) tc_ld16(t_row, r);
+      bool ok = true;
+#pragma unroll 1
+      for (int part = 0; part < parts; ++part) {
+        const int c = part * 16, h = part & (kSlabParts - 1);          // tile column, step within the slab
+        const int64_t col = static_cast<int64_t>(w.n0) + c;
+        float z[16], u[16];
+        if (kGated) {
+          uint32_t r2[16];
+          tc_ld16(t_row + c, r);
+          tc_ld16(t_row + kOutCols + c, r2);
+          tc_wait_ld16(r);
+          tc_wait_ld16(r2);
+#pragma unroll
+          for (int e = 0; e < 16; ++e) { z[e] = __uint_as_float(r[e]); u[e] = __uint_as_float(r2[e]); }
+        } else {
+          tc_wait_ld16(r);
+#pragma unroll
+          for (int e = 0; e < 16; ++e) z[e] = __uint_as_float(r[e]);
+          if (part + 1 < parts) tc_ld16(t_row + c + 16, r);             // the next step's while this one is finished
+        }
+        if (adds) {                                  // (16 columns are 128 words of 16 bytes)
+          add_partial16(z, part_sums + c * 8);
+          if (kGated) add_partial16(u, part_sums + (kOutCols + c) * 8);
+        }
+        if (leaves) {
+          leave_partial16(z, part_sums + c * 8);
+          if (kGated) leave_partial16(u, part_sums + (kOutCols + c) * 8);
+          continue;
+        }
+        const int valid = p.N - col < 16 ? static_cast<int>(p.N - col) : 16;      // may be <= 0 in the second half of a slab
+        if (bias) {
+          float b[16];
+          load16(bias + col, bias_vec && valid == 16, valid, b);
+#pragma unroll
+          for (int e = 0; e < 16; ++e) z[e] += b[e];
+        }
+        if (kGated && bias2) {
+          float b[16];
+          load16(bias2 + col, bias_vec && valid == 16, valid, b);
+#pragma unroll
+          for (int e = 0; e < 16; ++e) u[e] += b[e];
+        }
+        // this thread's row of the slab in the staging buffer in turn
+        const uint32_t my = stage + buf * kSlabBytes + static_cast<uint32_t>(lane) * 64u;
+        constexpr int kChunks = sizeof(T);               // 16-byte chunks of 16 elements: 2 or 4
+        float s[16];
+        if (side_staged) {
+          if (h == 0) ok = __all_sync(0xFFFFFFFFu, mbar_wait(my_side_full + 8 * buf, buf_phase, abort_flag)) && ok;
+          Raw8<T> lo, hi;
+          if constexpr (sizeof(T) == 2) {
+            lo.a = lds128(my + (((2u * h) ^ sw) << 4));
+            hi.a = lds128(my + (((2u * h + 1u) ^ sw) << 4));
+          } else {
+            lo.a = lds128(my + ((0u ^ sw) << 4));
+            lo.b = lds128(my + ((1u ^ sw) << 4));
+            hi.a = lds128(my + ((2u ^ sw) << 4));
+            hi.b = lds128(my + ((3u ^ sw) << 4));
+          }
+          float a8[8], b8[8];
+          unpack8(lo, a8);
+          unpack8(hi, b8);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) { s[e] = a8[e]; s[8 + e] = b8[e]; }
+        } else if (side) {
+          load16(side + (row_ok ? row : row0) * p.ld_side + col, p.side_vec && valid == 16, valid, s);
+        }
+        if constexpr (!kGrad) {
+          activate16<kAct>(z);
+          if (kGated) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) z[e] *= u[e];
+          }
+          if (side) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) z[e] = fmaf(p.res_scale, s[e], z[e]);
+          }
+          uint4 out[kChunks];
+          {
+            Raw8<T> lo, hi;
+            const float a8[8] = {z[0], z[1], z[2], z[3], z[4], z[5], z[6], z[7]};
+            const float b8[8] = {z[8], z[9], z[10], z[11], z[12], z[13], z[14], z[15]};
+            lo = pack8<T>(a8);
+            hi = pack8<T>(b8);
+            if constexpr (sizeof(T) == 2) {
+              out[0] = lo.a; out[1] = hi.a;
+            } else {
+              out[0] = lo.a; out[1] = lo.b; out[2] = hi.a; out[3] = hi.b;
+            }
+          }
+          if (p.units) {
+            // 64 columns of 32 rows as 128-byte rows, 16-byte chunk c of row r at c ^ (r & 7); then eight lanes per unit
+            if constexpr (sizeof(T) == 2) {
+              const uint32_t mine = stage + static_cast<uint32_t>(lane) * 128u, c0 = static_cast<uint32_t>(part & 3) * 2u, r7 = static_cast<uint32_t>(lane) & 7u;
+              sts128(mine + ((c0 ^ r7) << 4), out[0].x, out[0].y, out[0].z, out[0].w);
+              sts128(mine + (((c0 + 1u) ^ r7) << 4), out[1].x, out[1].y, out[1].z, out[1].w);
+              if ((part & 3) == 3) {
+                __syncwarp();
+#pragma unroll 1
+                for (int pass = 0; pass < 8; ++pass) {
+                  const int rr = pass * 4 + (lane >> 3), g = lane & 7;
+                  Raw8<T> x;
+                  x.a = lds128(stage + static_cast<uint32_t>(rr) * 128u + ((static_cast<uint32_t>(g) ^ (static_cast<uint32_t>(rr) & 7u)) << 4));
+                  uint32_t meta;
+                  const uint32_t code = p.rha ? encode_unit_octet<true>(x, g, meta) : encode_unit_octet<false>(x, g, meta);
+                  if (row0 + rr < p.M) {
+                    uint32_t* dst = static_cast<uint32_t*>(p.y) + ((row0 + rr) * (p.N >> 6) + (col >> 6)) * kUnitWords;
+                    dst[1 + g] = code;
+                    if (g == 0) dst[0] = meta;
+                  }
+                }
+                __syncwarp();
+              }
+            }
+          } else if (p.tma_store) {
+            if (!side_staged && h == 0) {
+              if (lane == 0) bulk_wait_read<kStageBufs - 1>();        // the store that used this buffer has read it
+              __syncwarp();
+            }
+#pragma unroll
+            for (int v = 0; v < kChunks; ++v)
+              sts128(my + (((static_cast<uint32_t>(kChunks * h + v)) ^ sw) << 4), out[v].x, out[v].y, out[v].z, out[v].w);
+            if (h == kSlabParts - 1) {
+              fence_proxy_async_smem();                  // generic-proxy writes -> visible to the TMA store
+              __syncwarp();
+              if (lane == 0) {
+                tma_store_2d(&tmY, static_cast<int>(col) - 16 * h, static_cast<int>(row0), stage + buf * kSlabBytes);
+                bulk_commit();
+              }
+            }
+          } else if (row_ok) {
+            T* dst = static_cast<T*>(p.y) + row * p.ld_y + col;
+            if (p.y_vec && valid == 16) {
+#pragma unroll
+              for (int v = 0; v < kChunks; ++v) reinterpret_cast<uint4*>(dst)[v] = out[v];
+            } else {
+#pragma unroll
+              for (int e = 0; e < 16; ++e)
+                if (e < valid) dst[e] = from_f32<T>(z[e]);
+            }
+          }
+        } else {
+          float a[16];
+          activate_slope16<kAct>(z, a);
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const bool in = row_ok && e < valid;
+            z[e] = in ? s[e] * z[e] * (kGated ? u[e] : 1.0f) : 0.0f;
+            if (kGated) u[e] = in ? s[e] * a[e] : 0.0f;
+          }
+          constexpr int kParts = IsHalf<T>::value ? 2 : 1;
+          if (p.dz && row_ok) {
+            __nv_bfloat16* dst = p.dz + row * p.ld_dz + col;
+            store_parts<kParts>(z, dst, p.dz_plane, p.ld_dz - col);
+            if (kGated) store_parts<kParts>(u, dst + kParts * p.dz_plane, p.dz_plane, p.ld_dz - col);
+          }
+          if (p.colsum) {
+            const float sz = column_sum16(z, lane);
+            const int cl = column_of_lane(lane);
+            float* sums = p.colsum + (row0 >> 5) * p.N + col;
+            if ((lane & 1) == 0 && cl < valid) sums[cl] = sz;
+            if (kGated) {
+              const float su = column_sum16(u, lane);
+              if ((lane & 1) == 0 && cl < valid) sums[p.colsum_plane + cl] = su;
+            }
+          }
+        }
+        if (h == kSlabParts - 1 && (side_staged || (!kGrad && p.tma_store && !p.units))) {
+          // the slab is done: request the one after next into the buffer that was stored (read) a slab ago
+          if (side_staged && part + 2 * kSlabParts < parts) {
+            if (kGrad) {
+              fence_proxy_async_smem();
+              __syncwarp();                              // every lane has read the buffers that are asked for again
+            }
+            const uint32_t b = buf >= 1 ? buf - 1 : kStageBufs - 1;       // (buf + 2) mod 3
+            if (lane == 0) {
+              bulk_wait_read<1>();
+              mbar_expect_tx(my_side_full + 8 * b, kSlabBytes);
+              tma_load_2d(stage + b * kSlabBytes, &tmSide, static_cast<int>(col) - 16 * h + 2 * kSlabCols, static_cast<int>(row0), my_side_full + 8 * b);
+            }
+          }
+          if (++buf == kStageBufs) { buf = 0; buf_phase ^= 1u; }
+        }
+      }
+      tc_fence_before();                             // accumulator fully read: hand it back
+      __syncwarp();
+      if (lane == 0) mbar_arrive_cluster(tmem_empty_leader + 8 * acc);
+      if (!ok) break;
       if (leaves) {                                  // this warp's rows of the partial sums are there for the next slice
-        __syncwarp();
         if (lane == 0) {
           __threadfence();
           asm volatile("st.release.gpu.global.u32 [%0], %1;" ::"l"(my_flag), "r"(1u) : "memory");

@@ -26,11 +26,11 @@ inline size_t partial_tiles(const Tc2Plan& pl) {
 }
 constexpr size_t kPartialTileBytes = static_cast<size_t>(kPairM) * kPairN * sizeof(float);
 
-template <bool kGated, bool kGrad, typename T>
-hif4_status launch_linear(const LinearCall& c, void* workspace, cudaStream_t st) {
+template <bool kGated, bool kGrad, typename T, int kAct>
+hif4_status launch_linear_act(const LinearCall& c, void* workspace, cudaStream_t st) {
   constexpr int kTileN = kGated ? kPairN / 2 : kPairN;
   static uint64_t smem_opt_in = 0;
-  if (!ensure_dynamic_smem(linear_tc2_kernel<kGated, kGrad, T>, kLinSmemBytes, smem_opt_in)) return HIF4_ERR_CUDA;
+  if (!ensure_dynamic_smem(linear_tc2_kernel<kGated, kGrad, T, kAct>, kLinSmemBytes, smem_opt_in)) return HIF4_ERR_CUDA;
   LinearParams p{};
   p.M = c.M; p.N = c.N;
   p.error_word = device_error_word();
@@ -48,15 +48,17 @@ hif4_status launch_linear(const LinearCall& c, void* workspace, cudaStream_t st)
   p.B2 = static_cast<const uint8_t*>(c.K > 0 ? c.B2 : p.error_word);
   p.pitch = upr * kUnitBytes;
   p.upr = static_cast<int>(upr);
-  CUtensorMap tmA{}, tmB{}, tmB2{}, tmY{};
+  CUtensorMap tmA{}, tmB{}, tmB2{}, tmY{}, tmSide{};
   p.tma = c.K > 0 && c.K % (kRawUnits * kUnitElems) == 0 && at16(c.A) && at16(c.B) && (!kGated || at16(c.B2));
   if (p.tma) {
     if (!make_unit_map(&tmA, c.A, c.M, upr, kRows) || !make_unit_map(&tmB, c.B, c.N, upr, kRows)) return HIF4_ERR_CUDA;
     if (kGated && !make_unit_map(&tmB2, c.B2, c.N, upr, kRows)) return HIF4_ERR_CUDA;
   }
-  p.bias = c.bias; p.bias_up = c.bias_up; p.act = c.act;
+  p.bias = c.bias; p.bias_up = c.bias_up;
   p.side = c.side; p.ld_side = c.ld_side; p.res_scale = c.res_scale;
   p.side_vec = at16(c.side) && (c.M == 1 || c.ld_side * sizeof(T) % 16 == 0);
+  // through the staging buffers where they are not taken by units (a load clips columns past N element by element)
+  p.side_tma = c.side && p.side_vec && c.ld_side * sizeof(T) % 16 == 0 && !c.units && make_y_map<T>(&tmSide, const_cast<void*>(c.side), c.M, c.N, c.ld_side);
   p.y = c.y; p.ld_y = c.ld_y; p.units = c.units; p.rha = c.rha;
   if (!kGrad && !c.units) {
     p.y_vec = at16(c.y) && (c.M == 1 || c.ld_y * sizeof(T) % 16 == 0);
@@ -71,9 +73,22 @@ hif4_status launch_linear(const LinearCall& c, void* workspace, cudaStream_t st)
     if (cudaMemsetAsync(p.flags, 0, pl.flag_bytes, st) != cudaSuccess) return HIF4_ERR_CUDA;
   }
   const int pairs = p.full_rounds == 0 && p.sk_tiles == 0 ? p.tail_tiles * p.slices : pl.pairs;      // a single round: one pair per slice
-  linear_tc2_kernel<kGated, kGrad, T><<<2 * pairs, kThreads, kLinSmemBytes, st>>>(tmA, tmB, tmB2, tmY, p);
+  linear_tc2_kernel<kGated, kGrad, T, kAct><<<2 * pairs, kThreads, kLinSmemBytes, st>>>(tmA, tmB, tmB2, tmY, tmSide, p);
   note_launch();
   return launch_status();
+}
+
+template <bool kGated, bool kGrad, typename T>
+hif4_status launch_linear(const LinearCall& c, void* workspace, cudaStream_t st) {
+  switch (c.act) {
+    case HIF4_ACT_RELU: return launch_linear_act<kGated, kGrad, T, HIF4_ACT_RELU>(c, workspace, st);
+    case HIF4_ACT_SILU: return launch_linear_act<kGated, kGrad, T, HIF4_ACT_SILU>(c, workspace, st);
+    case HIF4_ACT_GELU: return launch_linear_act<kGated, kGrad, T, HIF4_ACT_GELU>(c, workspace, st);
+    case HIF4_ACT_GELU_TANH: return launch_linear_act<kGated, kGrad, T, HIF4_ACT_GELU_TANH>(c, workspace, st);
+    default: break;
+  }
+  if constexpr (kGrad && !kGated) return HIF4_ERR_UNSUPPORTED;          // dZ = dY needs no product
+  else return launch_linear_act<kGated, kGrad, T, HIF4_ACT_NONE>(c, workspace, st);
 }
 
 }  // namespace
