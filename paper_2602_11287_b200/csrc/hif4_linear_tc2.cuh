@@ -79,6 +79,48 @@ __device__ __forceinline__ void activate_slope16(float (&z)[16], float (&a)[16])
     z[e] = s;
   }
 }
+template <bool kValue> struct Flag { static constexpr bool value = kValue; };
+
+// z += 16 elements of a bias vector (16-byte aligned, inside the row).
+template <typename T>
+__device__ __forceinline__ void add16(float (&z)[16], const Raw8<T>& lo, const Raw8<T>& hi) {
+  float a[8], b[8];
+  unpack8(lo, a);
+  unpack8(hi, b);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) { z[e] += a[e]; z[8 + e] += b[e]; }
+}
+// 16 elements of a staged 64-byte row (32 or 16 elements; `h`: which half of a 16-bit row).
+template <typename T>
+__device__ __forceinline__ void read_staged16(float (&v)[16], uint32_t row_at, uint32_t sw, int h) {
+  Raw8<T> lo, hi;
+  if constexpr (sizeof(T) == 2) {
+    lo.a = lds128(row_at + (((2u * h) ^ sw) << 4));
+    hi.a = lds128(row_at + (((2u * h + 1u) ^ sw) << 4));
+  } else {
+    lo.a = lds128(row_at + ((0u ^ sw) << 4));
+    lo.b = lds128(row_at + ((1u ^ sw) << 4));
+    hi.a = lds128(row_at + ((2u ^ sw) << 4));
+    hi.b = lds128(row_at + ((3u ^ sw) << 4));
+  }
+  float a[8], b[8];
+  unpack8(lo, a);
+  unpack8(hi, b);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) { v[e] = a[e]; v[8 + e] = b[e]; }
+}
+// The same place written with 16 results, rounded to T.
+template <typename T>
+__device__ __forceinline__ void pack16(uint4 (&out)[sizeof(T)], const float (&z)[16]) {
+  const float a[8] = {z[0], z[1], z[2], z[3], z[4], z[5], z[6], z[7]};
+  const float b[8] = {z[8], z[9], z[10], z[11], z[12], z[13], z[14], z[15]};
+  const Raw8<T> lo = pack8<T>(a), hi = pack8<T>(b);
+  if constexpr (sizeof(T) == 2) {
+    out[0] = lo.a; out[1] = hi.a;
+  } else {
+    out[0] = lo.a; out[1] = lo.b; out[2] = hi.a; out[3] = hi.b;
+  }
+}
 // Waits for a tcgen05.ld into r; the registers pass through, so that nothing reads them before.
 __device__ __forceinline__ void tc_wait_ld16(uint32_t (&r)[16]) {
   asm volatile("tcgen05.wait::ld.sync.aligned;"
@@ -304,9 +346,169 @@ linear_tc2_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
       if (adds && !__all_sync(0xFFFFFFFFu, wait_count(my_flag - 8, 1u, abort_flag))) break;
       float4* part_sums = shared_tile ? partial_of(p.partial, w.tail, rank, q, lane) : nullptr;
       const uint32_t t_row = tmem_base + (static_cast<uint32_t>(q * 32) << 16) + acc * kPairN;
+      bool ok = true;
+      // Eight lanes convert one unit of a staged 32 x 64 block (16-bit types), four rows at a time; `col`: a column of the block.
+      auto convert_units = [&](int64_t col) {
+        if constexpr (sizeof(T) == 2) {
+          __syncwarp();
+          uint32_t* dst = static_cast<uint32_t*>(p.y) + ((row0 + (lane >> 3)) * (p.N >> 6) + (col >> 6)) * kUnitWords;
+          const int g = lane & 7;
+#pragma unroll 1
+          for (int rr = lane >> 3; rr < 32; rr += 4) {
+            Raw8<T> x;
+            x.a = lds128(stage + static_cast<uint32_t>(rr) * 128u + ((static_cast<uint32_t>(g) ^ (static_cast<uint32_t>(rr) & 7u)) << 4));
+            uint32_t meta;
+            const uint32_t code = p.rha ? encode_unit_octet<true>(x, g, meta) : encode_unit_octet<false>(x, g, meta);
+            if (row0 + rr < p.M) {
+              dst[1 + g] = code;
+              if (g == 0) dst[0] = meta;
+            }
+            dst += 4 * (p.N >> 6) * kUnitWords;
+          }
+          __syncwarp();
+        }
+      };
+      // Asks for the slab after next (its first tile column) in the buffer that was stored, or read, a slab ago; steps on.
+      auto next_buffer = [&](bool request, int column) {
+        if (request && lane == 0) {
+          const uint32_t b = buf >= 1 ? buf - 1 : kStageBufs - 1;       // (buf + 2) mod 3
+          bulk_wait_read<1>();
+          mbar_expect_tx(my_side_full + 8 * b, kSlabBytes);
+          tma_load_2d(stage + b * kSlabBytes, &tmSide, w.n0 + column, static_cast<int>(row0), my_side_full + 8 * b);
+        }
+        if (++buf == kStageBufs) { buf = 0; buf_phase ^= 1u; }
+      };
+      // Whole, unshared tiles: the steps of a slab in one straight run of instructions per combination of bias and side
+      // matrix.  A warp alone on its scheduler's instruction stream pays for every jump over code that it does not run
+      // (8192 x 8192 x 256, SiLU: 190 us in the general loop below).
+      auto whole_tile = [&](auto has_bias, auto has_side, auto to_units) {
+        const T* b1 = bias + w.n0;
+        const T* b2 = bias2 + w.n0;
+#pragma unroll 1
+        for (int c0 = 0; c0 < kOutCols; c0 += kSlabCols) {
+          const uint32_t my = stage + buf * kSlabBytes + static_cast<uint32_t>(lane) * 64u;
+          uint32_t r[kSlabParts][16];
+          if (!kGated) {
+#pragma unroll
+            for (int h = 0; h < kSlabParts; ++h) tc_ld16(t_row + c0 + 16 * h, r[h]);
+          }
+          if constexpr (has_side.value) {
+            ok = __all_sync(0xFFFFFFFFu, mbar_wait(my_side_full + 8 * buf, buf_phase, abort_flag)) && ok;
+          } else if constexpr (!to_units.value && !kGrad) {
+            if (lane == 0) bulk_wait_read<kStageBufs - 1>();        // the store that used this buffer has read it
+            __syncwarp();
+          }
+#pragma unroll
+          for (int h = 0; h < kSlabParts; ++h) {
+            const int c = c0 + 16 * h;
+            float z[16], u[16];
+            Raw8<T> bz0, bz1, bu0, bu1;
+            if constexpr (has_bias.value) {
+              bz0 = load8(b1 + c); bz1 = load8(b1 + c + 8);
+              if constexpr (kGated) { bu0 = load8(b2 + c); bu1 = load8(b2 + c + 8); }
+            }
+            if constexpr (kGated) {
+              uint32_t r2[16];
+              tc_ld16(t_row + c, r[0]);
+              tc_ld16(t_row + kOutCols + c, r2);
+              tc_wait_ld16(r[0]);
+              tc_wait_ld16(r2);
+#pragma unroll
+              for (int e = 0; e < 16; ++e) { z[e] = __uint_as_float(r[0][e]); u[e] = __uint_as_float(r2[e]); }
+            } else {
+              tc_wait_ld16(r[h]);
+#pragma unroll
+              for (int e = 0; e < 16; ++e) z[e] = __uint_as_float(r[h][e]);
+            }
+            if constexpr (has_bias.value) {
+              add16<T>(z, bz0, bz1);
+              if constexpr (kGated) add16<T>(u, bu0, bu1);
+            }
+            float s[16];
+            if constexpr (has_side.value) read_staged16<T>(s, my, sw, h);
+            if constexpr (!kGrad) {
+              activate16<kAct>(z);
+              if constexpr (kGated) {
+#pragma unroll
+                for (int e = 0; e < 16; ++e) z[e] *= u[e];
+              }
+              if constexpr (has_side.value) {
+#pragma unroll
+                for (int e = 0; e < 16; ++e) z[e] = fmaf(p.res_scale, s[e], z[e]);
+              }
+              uint4 out[sizeof(T)];
+              pack16<T>(out, z);
+              if constexpr (to_units.value) {
+                const uint32_t mine = stage + static_cast<uint32_t>(lane) * 128u, k = (static_cast<uint32_t>(c) & 63u) >> 3, r7 = static_cast<uint32_t>(lane) & 7u;
+                sts128(mine + ((k ^ r7) << 4), out[0].x, out[0].y, out[0].z, out[0].w);
+                sts128(mine + (((k + 1u) ^ r7) << 4), out[1].x, out[1].y, out[1].z, out[1].w);
+              } else {
+#pragma unroll
+                for (int v = 0; v < static_cast<int>(sizeof(T)); ++v)
+                  sts128(my + (((static_cast<uint32_t>(sizeof(T)) * h + v) ^ sw) << 4), out[v].x, out[v].y, out[v].z, out[v].w);
+              }
+            } else {
+              float a[16];
+              activate_slope16<kAct>(z, a);
+#pragma unroll
+              for (int e = 0; e < 16; ++e) {
+                z[e] = row_ok ? s[e] * z[e] * (kGated ? u[e] : 1.0f) : 0.0f;
+                if (kGated) u[e] = row_ok ? s[e] * a[e] : 0.0f;
+              }
+              const int64_t col = static_cast<int64_t>(w.n0) + c;
+              constexpr int kParts = IsHalf<T>::value ? 2 : 1;
+              if (p.dz && row_ok) {
+                __nv_bfloat16* dst = p.dz + row * p.ld_dz + col;
+                store_parts<kParts>(z, dst, p.dz_plane, 16);
+                if (kGated) store_parts<kParts>(u, dst + kParts * p.dz_plane, p.dz_plane, 16);
+              }
+              if (p.colsum) {
+                float* sums = p.colsum + (row0 >> 5) * p.N + col + column_of_lane(lane);
+                const float sz = column_sum16(z, lane);
+                if ((lane & 1) == 0) *sums = sz;
+                if (kGated) {
+                  const float su = column_sum16(u, lane);
+                  if ((lane & 1) == 0) sums[p.colsum_plane] = su;
+                }
+              }
+            }
+          }
+          if constexpr (to_units.value) {
+            if (c0 & 32) convert_units(static_cast<int64_t>(w.n0) + c0);
+          } else {
+            fence_proxy_async_smem();                  // generic-proxy writes (reads) before the async proxy reads (writes) the buffer
+            __syncwarp();
+            if (!kGrad && lane == 0) {
+              tma_store_2d(&tmY, w.n0 + c0, static_cast<int>(row0), stage + buf * kSlabBytes);
+              bulk_commit();
+            }
+            next_buffer(has_side.value && c0 + 2 * kSlabCols < kOutCols, c0 + 2 * kSlabCols);
+          }
+        }
+      };
+      const bool whole = !shared_tile && parts == kOutCols / 16 && cols_left >= kOutCols && ((!bias && !bias2) || (bias_vec && bias && (!kGated || bias2))) &&
+                         (kGrad ? side_staged : p.units ? !side : p.tma_store && (!side || side_staged));
+      if (whole) {
+        if constexpr (kGrad) {
+          if (bias) whole_tile(Flag<true>{}, Flag<true>{}, Flag<false>{});
+          else whole_tile(Flag<false>{}, Flag<true>{}, Flag<false>{});
+        } else {
+          if (p.units) {
+            if constexpr (sizeof(T) == 2) {
+              if (bias) whole_tile(Flag<true>{}, Flag<false>{}, Flag<true>{});
+              else whole_tile(Flag<false>{}, Flag<false>{}, Flag<true>{});
+            }
+          } else if (side) {
+            if (bias) whole_tile(Flag<true>{}, Flag<true>{}, Flag<false>{});
+            else whole_tile(Flag<false>{}, Flag<true>{}, Flag<false>{});
+          } else {
+            if (bias) whole_tile(Flag<true>{}, Flag<false>{}, Flag<false>{});
+            else whole_tile(Flag<false>{}, Flag<false>{}, Flag<false>{});
+          }
+        }
+      } else {
       uint32_t r[16];
       if (!kGated && parts > 0) tc_ld16(t_row, r);
-      bool ok = true;
 #pragma unroll 1
       for (int part = 0; part < parts; ++part) {
         const int c = part * 16, h = part & (kSlabParts - 1);          // tile column, step within the slab
@@ -354,21 +556,7 @@ linear_tc2_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
         float s[16];
         if (side_staged) {
           if (h == 0) ok = __all_sync(0xFFFFFFFFu, mbar_wait(my_side_full + 8 * buf, buf_phase, abort_flag)) && ok;
-          Raw8<T> lo, hi;
-          if constexpr (sizeof(T) == 2) {
-            lo.a = lds128(my + (((2u * h) ^ sw) << 4));
-            hi.a = lds128(my + (((2u * h + 1u) ^ sw) << 4));
-          } else {
-            lo.a = lds128(my + ((0u ^ sw) << 4));
-            lo.b = lds128(my + ((1u ^ sw) << 4));
-            hi.a = lds128(my + ((2u ^ sw) << 4));
-            hi.b = lds128(my + ((3u ^ sw) << 4));
-          }
-          float a8[8], b8[8];
-          unpack8(lo, a8);
-          unpack8(hi, b8);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) { s[e] = a8[e]; s[8 + e] = b8[e]; }
+          read_staged16<T>(s, my, sw, h);
         } else if (side) {
           load16(side + (row_ok ? row : row0) * p.ld_side + col, p.side_vec && valid == 16, valid, s);
         }
@@ -383,41 +571,14 @@ linear_tc2_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
             for (int e = 0; e < 16; ++e) z[e] = fmaf(p.res_scale, s[e], z[e]);
           }
           uint4 out[kChunks];
-          {
-            Raw8<T> lo, hi;
-            const float a8[8] = {z[0], z[1], z[2], z[3], z[4], z[5], z[6], z[7]};
-            const float b8[8] = {z[8], z[9], z[10], z[11], z[12], z[13], z[14], z[15]};
-            lo = pack8<T>(a8);
-            hi = pack8<T>(b8);
-            if constexpr (sizeof(T) == 2) {
-              out[0] = lo.a; out[1] = hi.a;
-            } else {
-              out[0] = lo.a; out[1] = lo.b; out[2] = hi.a; out[3] = hi.b;
-            }
-          }
+          pack16<T>(out, z);
           if (p.units) {
             // 64 columns of 32 rows as 128-byte rows, 16-byte chunk c of row r at c ^ (r & 7); then eight lanes per unit
             if constexpr (sizeof(T) == 2) {
               const uint32_t mine = stage + static_cast<uint32_t>(lane) * 128u, c0 = static_cast<uint32_t>(part & 3) * 2u, r7 = static_cast<uint32_t>(lane) & 7u;
               sts128(mine + ((c0 ^ r7) << 4), out[0].x, out[0].y, out[0].z, out[0].w);
               sts128(mine + (((c0 + 1u) ^ r7) << 4), out[1].x, out[1].y, out[1].z, out[1].w);
-              if ((part & 3) == 3) {
-                __syncwarp();
-#pragma unroll 1
-                for (int pass = 0; pass < 8; ++pass) {
-                  const int rr = pass * 4 + (lane >> 3), g = lane & 7;
-                  Raw8<T> x;
-                  x.a = lds128(stage + static_cast<uint32_t>(rr) * 128u + ((static_cast<uint32_t>(g) ^ (static_cast<uint32_t>(rr) & 7u)) << 4));
-                  uint32_t meta;
-                  const uint32_t code = p.rha ? encode_unit_octet<true>(x, g, meta) : encode_unit_octet<false>(x, g, meta);
-                  if (row0 + rr < p.M) {
-                    uint32_t* dst = static_cast<uint32_t*>(p.y) + ((row0 + rr) * (p.N >> 6) + (col >> 6)) * kUnitWords;
-                    dst[1 + g] = code;
-                    if (g == 0) dst[0] = meta;
-                  }
-                }
-                __syncwarp();
-              }
+              if ((part & 3) == 3) convert_units(col);
             }
           } else if (p.tma_store) {
             if (!side_staged && h == 0) {
@@ -473,21 +634,13 @@ linear_tc2_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
           }
         }
         if (h == kSlabParts - 1 && (side_staged || (!kGrad && p.tma_store && !p.units))) {
-          // the slab is done: request the one after next into the buffer that was stored (read) a slab ago
-          if (side_staged && part + 2 * kSlabParts < parts) {
-            if (kGrad) {
-              fence_proxy_async_smem();
-              __syncwarp();                              // every lane has read the buffers that are asked for again
-            }
-            const uint32_t b = buf >= 1 ? buf - 1 : kStageBufs - 1;       // (buf + 2) mod 3
-            if (lane == 0) {
-              bulk_wait_read<1>();
-              mbar_expect_tx(my_side_full + 8 * b, kSlabBytes);
-              tma_load_2d(stage + b * kSlabBytes, &tmSide, static_cast<int>(col) - 16 * h + 2 * kSlabCols, static_cast<int>(row0), my_side_full + 8 * b);
-            }
+          if (kGrad) {
+            fence_proxy_async_smem();
+            __syncwarp();                                // every lane has read the buffer that is asked for again
           }
-          if (++buf == kStageBufs) { buf = 0; buf_phase ^= 1u; }
+          next_buffer(side_staged && part + 2 * kSlabParts < parts, c - 16 * h + 2 * kSlabCols);
         }
+      }
       }
       tc_fence_before();                             // accumulator fully read: hand it back
       __syncwarp();
