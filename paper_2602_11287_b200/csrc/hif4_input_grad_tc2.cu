@@ -9,9 +9,10 @@
 // where the forward kernel decodes 256, so the tensor pipe is the tighter bound here.
 //   warp 0      raw units: 64 rows x 80 bytes (the CTA's two units of a 144-byte chunk, and eight bytes beside) per step,
 //               eight stages ahead, by TMA or word by word as in the forward kernel
-//   warp 14     dZ: 128 rows x 64 columns per step into the operand stage that the MMA has released
-//   warps 6-13  decode, two teams of four warps on alternate steps: thread = one unit; a warp reports a step once its units
-//               are written and the step's dZ has landed
+//   warp 22     dZ: 128 rows x 64 columns per step into the operand stage that the MMA has released
+//   warps 6-21  decode, four teams of four warps on steps in turn: thread = one unit; a warp reports a step once its units
+//               are written and the step's dZ has landed.  (A unit is 200 dependent instructions of one warp: two teams
+//               took as long over a step as the tensor core.)
 //   warp 1      rank 0: MMA issue;   warps 2-5  epilogue, TMA stores of 64-byte rows
 // Phases: the BF16 parts of dZ (one for BF16 gradients, two for FP16), for both projections of a gated layer.
 // Tiles shared along the contraction pass FP32 partial sums as in the forward kernel.
@@ -29,7 +30,9 @@ constexpr int kOpHalfBytes = kRows * 128;              // dZ: 128 rows x 64 BF16
 constexpr int kOpStageBytes = 2 * kOpHalfBytes;
 constexpr int kOpRing = 5;
 constexpr int kTeamThreads = 128;
-constexpr int kGradThreads = 15 * 32;
+constexpr int kTeams = 4;
+constexpr int kGradDecodeWarp0 = 6, kGradZWarp = kGradDecodeWarp0 + kTeams * kTeamThreads / 32;
+constexpr int kGradThreads = (kGradZWarp + 1) * 32;
 constexpr int kGradSmemBytes = 1024 + kOpRing * kOpStageBytes + kRawRing * kRawStepBytes + kStageOutBytes + 512 /*barriers*/ + 1024 /*table*/;
 constexpr uint32_t kGradInstrDesc = kLinInstrDesc | (1u << 16);      // B is MN-major
 
@@ -165,7 +168,7 @@ input_grad_tc2_kernel(const __grid_constant__ CUtensorMap tmZ, const __grid_cons
       }
       if (!p.tma) asm volatile("cp.async.wait_all;" ::: "memory");
     }
-  } else if (warp == 14) {
+  } else if (warp == kGradZWarp) {
     // ---------------------------------------------------------------- dZ
     if (lane == 0) {
       Ring ring;
@@ -214,7 +217,7 @@ input_grad_tc2_kernel(const __grid_constant__ CUtensorMap tmZ, const __grid_cons
         tc2_commit_both(tmem_full + 8 * acc);
       }
     }
-  } else if (warp < 6) {
+  } else if (warp < kGradDecodeWarp0) {
     // ---------------------------------------------------------------- epilogue
     const int q = warp & 3;
     const uint32_t tmem_empty_leader = mapa(tmem_empty, 0);
@@ -308,7 +311,7 @@ input_grad_tc2_kernel(const __grid_constant__ CUtensorMap tmZ, const __grid_cons
     if (lane == 0) bulk_wait_all();
   } else {
     // ---------------------------------------------------------------- decode
-    const int d = threadIdx.x - 6 * 32;
+    const int d = threadIdx.x - kGradDecodeWarp0 * 32;
     const uint32_t team = static_cast<uint32_t>(d) / kTeamThreads;
     const int t = d & (kTeamThreads - 1), row = t & (kStepRows - 1), block = t >> 6;      // contraction row, 64-column block
     const uint32_t src0 = raw_base + static_cast<uint32_t>(row) * kWinBytes + rank * 8u + static_cast<uint32_t>(block) * kUnitBytes;
@@ -325,7 +328,7 @@ input_grad_tc2_kernel(const __grid_constant__ CUtensorMap tmZ, const __grid_cons
       for (int kc = w.kc0; kc < w.kc1 && ok; ++kc) {
         const StepRange c = chunk_steps(p, kc);
         for (int step = 0; step < c.steps; ++step, ++n, raw.next(kRawRing), op.next(kOpRing)) {
-          if ((n & 1u) != team) continue;
+          if (n % kTeams != team) continue;
           if (!(ok = __all_sync(0xFFFFFFFFu, mbar_wait(raw_full + 8 * raw.s, raw.ph, abort_flag)))) break;
           uint32_t W[9];
 #pragma unroll
