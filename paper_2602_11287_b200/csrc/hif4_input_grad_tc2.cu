@@ -314,7 +314,11 @@ input_grad_tc2_kernel(const __grid_constant__ CUtensorMap tmZ, const __grid_cons
     const int d = threadIdx.x - kGradDecodeWarp0 * 32;
     const uint32_t team = static_cast<uint32_t>(d) / kTeamThreads;
     const int t = d & (kTeamThreads - 1), row = t & (kStepRows - 1), block = t >> 6;      // contraction row, 64-column block
-    const uint32_t src0 = raw_base + static_cast<uint32_t>(row) * kWinBytes + rank * 8u + static_cast<uint32_t>(block) * kUnitBytes;
+    // The unit's nine words within the row's five 16-byte words: 2 rank + 9 block words from its start.  Three 16-byte
+    // loads (a row pitch of 80 bytes spreads eight of them over all banks; single words would meet four at a bank) from
+    // the 16-byte word it starts in, or the one before, then a shift by 0 to 3 words.
+    const uint32_t src0 = raw_base + static_cast<uint32_t>(row) * kWinBytes + static_cast<uint32_t>(block) * 32u;
+    const bool shift1 = block != 0, shift2 = rank != 0;
     const uint32_t op_row = op_base + kOpHalfBytes + static_cast<uint32_t>(block) * (kStepRows * 128) + static_cast<uint32_t>(row) * 128u;
     uint32_t chunk_addr[8];
 #pragma unroll
@@ -330,9 +334,16 @@ input_grad_tc2_kernel(const __grid_constant__ CUtensorMap tmZ, const __grid_cons
         for (int step = 0; step < c.steps; ++step, ++n, raw.next(kRawRing), op.next(kOpRing)) {
           if (n % kTeams != team) continue;
           if (!(ok = __all_sync(0xFFFFFFFFu, mbar_wait(raw_full + 8 * raw.s, raw.ph, abort_flag)))) break;
-          uint32_t W[9];
+          uint32_t L[12], W[9];
 #pragma unroll
-          for (int k = 0; k < 9; ++k) W[k] = lds32(src0 + raw.s * kRawStepBytes + 4 * k);
+          for (int k = 0; k < 3; ++k) {
+            const uint4 v = lds128(src0 + raw.s * kRawStepBytes + 16 * k);
+            L[4 * k] = v.x; L[4 * k + 1] = v.y; L[4 * k + 2] = v.z; L[4 * k + 3] = v.w;
+          }
+#pragma unroll
+          for (int k = 0; k < 11; ++k) L[k] = shift1 ? L[k + 1] : L[k];
+#pragma unroll
+          for (int k = 0; k < 9; ++k) W[k] = shift2 ? L[k + 2] : L[k];
           fence_proxy_async_smem();                  // these reads before the async proxy refills the stage
           mbar_arrive(raw_empty + 8 * raw.s);
           if (!(ok = __all_sync(0xFFFFFFFFu, mbar_wait(op_empty + 8 * op.s, op.ph ^ 1u, abort_flag)))) break;
