@@ -30,7 +30,7 @@ namespace {
 struct LinearParams {
   int64_t M, N;
   int num_kc, n_tiles, full_rounds, tail_tiles, slices, sk_tiles, sk_tile0;      // schedule (hif4_tc2_dense.cuh)
-  unsigned int* flags;              // [shared tiles][slices][8]: "this epilogue warp's rows of this slice's sums are there"
+  unsigned int* flags;              // [shared tiles][slices][8]: 16-column steps of this slice's sums that are there, per 32 rows
   float* partial;                   // [shared tiles][2 ranks][4 warps][16 x 16 columns][4][32 rows][4]
   unsigned int* error_word;
   DecodeMul mul;
@@ -45,7 +45,7 @@ struct LinearParams {
   float res_scale;
   void* y;
   int64_t ld_y;
-  int y_vec, tma_store, units, rha;
+  int tma_store, units, rha;
   __nv_bfloat16* dz;
   int64_t ld_dz, dz_plane;
   float* colsum;

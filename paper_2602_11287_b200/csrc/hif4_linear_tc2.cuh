@@ -13,6 +13,8 @@
 //     rows staged in shared memory and written with TMA stores, or 64-column rows converted to units there by eight
 //     lanes each.  The gradient form writes dZ (dG, dU) as BF16 parts for the product that follows, and FP32 column
 //     sums per 32 rows for the bias gradients.
+//   - The last tile of a CTA is finished by all of its warps: the decode warps, out of work, take four fifths of the
+//     columns (staged in the operand stages, which are free by then).  With few tiles this tail is most of the call.
 //   - Tiles shared along K pass FP32 partial sums through the workspace (the epilogue is not linear, so nothing can be
 //     added in place): slice s adds its part to what slice s - 1 left and the last slice finishes the tile, always in
 //     this order.
@@ -29,8 +31,10 @@ namespace {
 constexpr int kSlabBytes = 32 * 64;                   // 32 rows of one epilogue warp x 64 bytes
 constexpr int kStageBufs = 3;
 constexpr int kStageOutBytes = 4 * kStageBufs * kSlabBytes;    // 4 warps x 3 buffers (units: two of them as one of 32 x 128 bytes)
+constexpr int kEpiGroups = 5;                         // warps per TMEM quadrant that finish a CTA's last tile: its epilogue warp and four decode warps
+constexpr int kLinBarBytes = 640;                     // mbarriers: 144 bytes, then kStageBufs per warp that may take part in an epilogue (20)
 constexpr int kLinSmemBytes = 1024 /*alignment slack*/ + kDecStages * kDecStageBytes + kRawStages * kRawStageBytes + kStageOutBytes +
-                              256 /*barriers*/ + 1024 /*spread table*/;
+                              kLinBarBytes + 1024 /*spread table*/;
 constexpr uint32_t kLinInstrDesc = (1u << 4) | (1u << 7) | (1u << 10) | (static_cast<uint32_t>(kPairN >> 3) << 17) |
                                    (static_cast<uint32_t>(kPairM >> 4) << 24);
 
@@ -121,6 +125,38 @@ __device__ __forceinline__ void pack16(uint4 (&out)[sizeof(T)], const float (&z)
     out[0] = lo.a; out[1] = lo.b; out[2] = hi.a; out[3] = hi.b;
   }
 }
+// A slab (32 rows of 64 bytes) between a matrix of any alignment and the staging buffer, neighbouring lanes on neighbouring
+// elements; rows past `rows` and columns past `cols` are left out (read as zeros).
+template <typename T, bool kStore>
+__device__ __forceinline__ void copy_slab(T* matrix, int64_t ld, uint32_t buf, int lane, int64_t rows, int64_t cols) {
+  constexpr int kCols = 64 / sizeof(T), kRowsAtOnce = 32 / kCols;
+  const int c = lane & (kCols - 1), r0 = lane / kCols;
+  const uint32_t byte = static_cast<uint32_t>(c) * sizeof(T);
+#pragma unroll 8
+  for (int r = r0; r < 32; r += kRowsAtOnce) {
+    const uint32_t at = buf + static_cast<uint32_t>(r) * 64u + (((byte >> 4) ^ ((static_cast<uint32_t>(r) >> 1) & 3u)) << 4) + (byte & 15u);
+    const bool in = r < rows && c < cols;
+    if constexpr (sizeof(T) == 2) {
+      uint16_t v = 0;
+      if constexpr (kStore) {
+        asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(at));
+        if (in) reinterpret_cast<uint16_t*>(matrix)[r * ld + c] = v;
+      } else {
+        if (in) v = reinterpret_cast<const uint16_t*>(matrix)[r * ld + c];
+        asm volatile("st.shared.u16 [%0], %1;" ::"r"(at), "h"(v) : "memory");
+      }
+    } else {
+      uint32_t v = 0;
+      if constexpr (kStore) {
+        v = lds32(at);
+        if (in) reinterpret_cast<uint32_t*>(matrix)[r * ld + c] = v;
+      } else {
+        if (in) v = reinterpret_cast<const uint32_t*>(matrix)[r * ld + c];
+        asm volatile("st.shared.u32 [%0], %1;" ::"r"(at), "r"(v) : "memory");
+      }
+    }
+  }
+}
 // Waits for a tcgen05.ld into r; the registers pass through, so that nothing reads them before.
 __device__ __forceinline__ void tc_wait_ld16(uint32_t (&r)[16]) {
   asm volatile("tcgen05.wait::ld.sync.aligned;"
@@ -187,11 +223,11 @@ linear_tc2_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
   const uint32_t out_base = raw_base + kRawStages * kRawStageBytes;
   const uint32_t bar_base = out_base + kStageOutBytes;
   const uint32_t raw_full = bar_base, raw_empty = bar_base + 16, dec_full = bar_base + 32, dec_empty = bar_base + 64,
-                 tmem_full = bar_base + 96, tmem_empty = bar_base + 112, side_full = bar_base + 144;      // [4 warps][kStageBufs]
+                 tmem_full = bar_base + 96, tmem_empty = bar_base + 112, side_full = bar_base + 144;      // [20 warps][kStageBufs]
   uint8_t* gen_base = smem_raw + (smem_base - smem_u32(smem_raw));
   volatile uint32_t* tmem_ptr_smem = reinterpret_cast<volatile uint32_t*>(gen_base + (bar_base - smem_base) + 128);
   volatile uint32_t* abort_flag = tmem_ptr_smem + 1;
-  const uint32_t lut = bar_base + 256;
+  const uint32_t lut = bar_base + kLinBarBytes;
   if (threadIdx.x < 256)
     reinterpret_cast<uint32_t*>(gen_base + (lut - smem_base))[threadIdx.x] = spread_e8_entry(threadIdx.x);
 
@@ -213,7 +249,7 @@ linear_tc2_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
       mbar_init(tmem_full + 8 * s, 1);
       mbar_init(tmem_empty + 8 * s, 8);               // 4 epilogue warps of each CTA (used on rank 0)
     }
-    for (int s = 0; s < 4 * kStageBufs; ++s) mbar_init(side_full + 8 * s, 1);
+    for (int s = 0; s < 4 * kEpiGroups * kStageBufs; ++s) mbar_init(side_full + 8 * s, 1);
     *abort_flag = 0u;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -307,46 +343,105 @@ linear_tc2_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
         tc2_commit_both(tmem_full + 8 * acc);         // accumulator complete, in both CTAs
       }
     }
-  } else if (warp < kDecodeWarp0) {
+  } else {
+    // ---------------------------------------------------------------- decode, then its warps join the epilogue of the last tile
+    bool ok = true;
+    if (warp >= kDecodeWarp0) {
+      const int d = threadIdx.x - kDecodeWarp0 * 32;            // 0..511
+      const int h = d >> 8;                                     // which unit pair of the raw chunk
+      const int row = d & 255;                                  // 0..127 A rows, 128..255 B rows
+      const uint32_t r7 = static_cast<uint32_t>(row) & 7u;
+      const uint32_t raw_row = static_cast<uint32_t>(row) * kRawRowBytes + static_cast<uint32_t>(h) * 64u;
+      const uint32_t dec_row = dec_base + static_cast<uint32_t>(2 * h) * kDecStageBytes + static_cast<uint32_t>(row) * 128u;
+      uint32_t chunk_addr[8];
+  #pragma unroll
+      for (int j = 0; j < 8; ++j) chunk_addr[j] = dec_row + ((static_cast<uint32_t>(j) ^ r7) << 4);
+      const uint32_t dec_empty0 = dec_empty + 16 * h;
+      const uint32_t dec_full0_leader = mapa(dec_full, 0) + 16 * h;
+      uint32_t n = 0;
+      for (int i = 0; i < n_items && ok; ++i) {
+        const WorkItem w = work_item<kOutCols>(p, pair, num_pairs, i);
+        // the first of this warp's 32 rows exists (whole warps of rows past the edge are left out)
+        const int warp_row = row & ~31;
+        const bool live = warp_row < kRows ? static_cast<int64_t>(w.m0) + rank * kRows + warp_row < p.M
+                                           : static_cast<int64_t>(w.n0) + (kGated ? 0 : rank * kRows) + (warp_row - kRows) < p.N;
+        for (int kc = w.kc0; kc < w.kc1 && ok; ++kc, ++n) {
+          const uint32_t s = n & 1u, ph = (n >> 1) & 1u;
+          if (!(ok = __all_sync(0xFFFFFFFFu, mbar_wait(raw_full + 8 * s, ph, abort_flag)))) break;
+          uint32_t W[18];
+          if (live) {
+            uint32_t L[20];
+            const uint32_t src = raw_base + s * kRawStageBytes + raw_row;
+  #pragma unroll
+            for (int i = 0; i < 5; ++i) {
+              const uint4 v = lds128(src + 16 * i);
+              L[4 * i] = v.x; L[4 * i + 1] = v.y; L[4 * i + 2] = v.z; L[4 * i + 3] = v.w;
+            }
+            fence_proxy_async_smem();                  // these reads before the async proxy refills the stage
+  #pragma unroll
+            for (int i = 0; i < 18; ++i) W[i] = h ? L[i + 2] : L[i];
+          }
+          mbar_arrive(raw_empty + 8 * s);
+          ok = decode_two_units(W, chunk_addr, lut, p.mul, dec_empty0, dec_full0_leader, (n & 1u) ^ 1u, abort_flag, live);
+        }
+      }
+    }
+
     // ---------------------------------------------------------------- epilogue
+    // Warps 2-5 finish every tile; the CTA's last one, which no product hides, is shared with the decode warps, which have
+    // nothing left to decode: the slabs of a quadrant go round five warps.
+    const bool helper = warp >= kDecodeWarp0;
     const int q = warp & 3;                      // TMEM lane quadrant this warp may read
+    const int group = helper ? 1 + (warp - kDecodeWarp0) / 4 : 0;
     const uint32_t tmem_empty_leader = mapa(tmem_empty, 0);
-    const uint32_t stage = out_base + static_cast<uint32_t>(q) * (kStageBufs * kSlabBytes);
-    const uint32_t my_side_full = side_full + static_cast<uint32_t>(q) * (8 * kStageBufs);
+    // helpers stage in the operand stages, which the last tile's products no longer need once they are complete
+    const uint32_t stage = helper ? dec_base + static_cast<uint32_t>(warp - kDecodeWarp0) * (kStageBufs * kSlabBytes)
+                                  : out_base + static_cast<uint32_t>(q) * (kStageBufs * kSlabBytes);
+    const uint32_t my_side_full = side_full + static_cast<uint32_t>(group * 4 + q) * (8 * kStageBufs);
     const uint32_t sw = (static_cast<uint32_t>(lane) >> 1) & 3u;          // SWIZZLE_64B: 16-byte chunk c of row r at c ^ ((r >> 1) & 3)
     const T* bias = static_cast<const T*>(p.bias);
     const T* bias2 = static_cast<const T*>(p.bias_up);
     const T* side = static_cast<const T*>(p.side);        // residual, or dY in the gradient form
     const bool bias_vec = (reinterpret_cast<uintptr_t>(bias) & 15u) == 0 && (reinterpret_cast<uintptr_t>(bias2) & 15u) == 0;
     constexpr int kSlabParts = kSlabCols / 16;
-    uint32_t tcount = 0, buf = 0, buf_phase = 0;          // staging buffer in turn, parity of its side barrier
-    for (int it = 0; it < n_items; ++it, ++tcount) {
+    uint32_t buf = 0, buf_phase = 0;                      // staging buffer in turn, parity of its side barrier
+    const int first = helper && n_items > 0 ? n_items - 1 : 0;
+    uint32_t tcount = static_cast<uint32_t>(first);
+    for (int it = first; it < n_items && ok; ++it, ++tcount) {
       const WorkItem w = work_item<kOutCols>(p, pair, num_pairs, it);
       const uint32_t acc = tcount & 1u, aph = (tcount >> 1) & 1u;
       const int64_t row0 = static_cast<int64_t>(w.m0) + rank * kRows + q * 32, row = row0 + lane;
       const bool row_ok = row < p.M;
       const bool shared_tile = w.tail >= 0 && p.slices > 1;
       const bool adds = shared_tile && w.slice > 0, leaves = shared_tile && w.slice + 1 < p.slices;
-      // steps of 16 columns that hold outputs (a slab is done as a whole)
+      const int groups = it == n_items - 1 ? kEpiGroups : 1;
+      // columns that hold outputs, in whole slabs
       const int64_t cols_left = p.N - w.n0;
-      const int parts = row0 >= p.M ? 0 : cols_left >= kOutCols ? kOutCols / 16 : static_cast<int>((cols_left + kSlabCols - 1) / kSlabCols) * kSlabParts;
-      // Residual or dY through the staging buffers: two slabs are requested ahead, the first two while the product still runs.
+      const int cols = row0 >= p.M ? 0 : cols_left >= kOutCols ? kOutCols : static_cast<int>((cols_left + kSlabCols - 1) / kSlabCols) * kSlabCols;
+      // Residual or dY through the staging buffers: two slabs are requested ahead, the first two while the product still runs
+      // (by a helper once it is complete).
       const bool side_staged = p.side_tma && !leaves;
-      if (side_staged && lane == 0 && parts > 0) {
+      auto request_side = [&](int column, uint32_t b) {
+        mbar_expect_tx(my_side_full + 8 * b, kSlabBytes);
+        tma_load_2d(stage + b * kSlabBytes, &tmSide, w.n0 + column, static_cast<int>(row0), my_side_full + 8 * b);
+      };
+      auto request_first = [&]() {
+        if (!side_staged || lane != 0) return;
         bulk_wait_read<1>();                             // the two buffers' last stores have read them
-        for (int s = 0; s < 2 && s * kSlabParts < parts; ++s) {
-          const uint32_t b = (buf + s) % kStageBufs;
-          mbar_expect_tx(my_side_full + 8 * b, kSlabBytes);
-          tma_load_2d(stage + b * kSlabBytes, &tmSide, w.n0 + s * kSlabCols, static_cast<int>(row0), my_side_full + 8 * b);
+        for (int i = 0; i < 2; ++i) {
+          const int column = (group + i * groups) * kSlabCols;
+          if (column < cols) request_side(column, (buf + i) % kStageBufs);
         }
-      }
-      if (!__all_sync(0xFFFFFFFFu, mbar_wait(tmem_full + 8 * acc, aph, abort_flag, 256))) break;
+      };
+      if (!helper) request_first();
+      if (!__all_sync(0xFFFFFFFFu, mbar_wait(tmem_full + 8 * acc, aph, abort_flag, helper ? 32 : 256))) break;
       tc_fence_after();
+      if (helper) request_first();
+      // sixteen-column steps that the previous slice's warps have left in this quadrant: all of the tile's
       unsigned int* my_flag = shared_tile ? p.flags + (static_cast<size_t>(w.tail) * p.slices + w.slice) * 8 + rank * 4 + q : nullptr;
-      if (adds && !__all_sync(0xFFFFFFFFu, wait_count(my_flag - 8, 1u, abort_flag))) break;
+      if (adds && cols > 0 && !__all_sync(0xFFFFFFFFu, wait_count(my_flag - 8, static_cast<unsigned int>(cols / 16), abort_flag))) break;
       float4* part_sums = shared_tile ? partial_of(p.partial, w.tail, rank, q, lane) : nullptr;
       const uint32_t t_row = tmem_base + (static_cast<uint32_t>(q * 32) << 16) + acc * kPairN;
-      bool ok = true;
       // Eight lanes convert one unit of a staged 32 x 64 block (16-bit types), four rows at a time; `col`: a column of the block.
       auto convert_units = [&](int64_t col) {
         if constexpr (sizeof(T) == 2) {
@@ -368,13 +463,11 @@ linear_tc2_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
           __syncwarp();
         }
       };
-      // Asks for the slab after next (its first tile column) in the buffer that was stored, or read, a slab ago; steps on.
+      // Asks for this warp's slab after next in the buffer that was stored, or read, a slab ago; steps on.
       auto next_buffer = [&](bool request, int column) {
-        if (request && lane == 0) {
-          const uint32_t b = buf >= 1 ? buf - 1 : kStageBufs - 1;       // (buf + 2) mod 3
+        if (request && column < cols && lane == 0) {
           bulk_wait_read<1>();
-          mbar_expect_tx(my_side_full + 8 * b, kSlabBytes);
-          tma_load_2d(stage + b * kSlabBytes, &tmSide, w.n0 + column, static_cast<int>(row0), my_side_full + 8 * b);
+          request_side(column, buf >= 1 ? buf - 1 : kStageBufs - 1);       // (buf + 2) mod 3
         }
         if (++buf == kStageBufs) { buf = 0; buf_phase ^= 1u; }
       };
@@ -382,10 +475,13 @@ linear_tc2_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
       // matrix.  A warp alone on its scheduler's instruction stream pays for every jump over code that it does not run
       // (8192 x 8192 x 256, SiLU: 190 us in the general loop below).
       auto whole_tile = [&](auto has_bias, auto has_side, auto to_units) {
+        constexpr int kStep = to_units.value ? 64 : kSlabCols;          // columns taken at a time
         const T* b1 = bias + w.n0;
         const T* b2 = bias2 + w.n0;
 #pragma unroll 1
-        for (int c0 = 0; c0 < kOutCols; c0 += kSlabCols) {
+        for (int at = group * kStep; at < kOutCols; at += groups * kStep)
+#pragma unroll 1
+        for (int c0 = at; c0 < at + kStep; c0 += kSlabCols) {
           const uint32_t my = stage + buf * kSlabBytes + static_cast<uint32_t>(lane) * 64u;
           uint32_t r[kSlabParts][16];
           if (!kGated) {
@@ -482,11 +578,11 @@ linear_tc2_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
               tma_store_2d(&tmY, w.n0 + c0, static_cast<int>(row0), stage + buf * kSlabBytes);
               bulk_commit();
             }
-            next_buffer(has_side.value && c0 + 2 * kSlabCols < kOutCols, c0 + 2 * kSlabCols);
+            next_buffer(has_side.value, c0 + 2 * groups * kSlabCols);
           }
         }
       };
-      const bool whole = !shared_tile && parts == kOutCols / 16 && cols_left >= kOutCols && ((!bias && !bias2) || (bias_vec && bias && (!kGated || bias2))) &&
+      const bool whole = !shared_tile && cols == kOutCols && cols_left >= kOutCols && ((!bias && !bias2) || (bias_vec && bias && (!kGated || bias2))) &&
                          (kGrad ? side_staged : p.units ? !side : p.tma_store && (!side || side_staged));
       if (whole) {
         if constexpr (kGrad) {
@@ -506,195 +602,168 @@ linear_tc2_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
             else whole_tile(Flag<false>{}, Flag<false>{}, Flag<false>{});
           }
         }
-      } else {
-      uint32_t r[16];
-      if (!kGated && parts > 0) tc_ld16(t_row, r);
+      } else if (leaves) {
+        // a part of the contraction: FP32 sums for the next slice (16 columns are 128 words of 16 bytes)
+        unsigned int left = 0;
 #pragma unroll 1
-      for (int part = 0; part < parts; ++part) {
-        const int c = part * 16, h = part & (kSlabParts - 1);          // tile column, step within the slab
-        const int64_t col = static_cast<int64_t>(w.n0) + c;
-        float z[16], u[16];
-        if (kGated) {
-          uint32_t r2[16];
-          tc_ld16(t_row + c, r);
-          tc_ld16(t_row + kOutCols + c, r2);
-          tc_wait_ld16(r);
-          tc_wait_ld16(r2);
+        for (int c = group * 16; c < cols; c += groups * 16, ++left) {
+          uint32_t r[16];
+          float z[16];
 #pragma unroll
-          for (int e = 0; e < 16; ++e) { z[e] = __uint_as_float(r[e]); u[e] = __uint_as_float(r2[e]); }
-        } else {
-          tc_wait_ld16(r);
+          for (int half = 0; half < (kGated ? 2 : 1); ++half) {
+            const int cc = c + half * kOutCols;
+            tc_ld16(t_row + cc, r);
+            tc_wait_ld16(r);
 #pragma unroll
-          for (int e = 0; e < 16; ++e) z[e] = __uint_as_float(r[e]);
-          if (part + 1 < parts) tc_ld16(t_row + c + 16, r);             // the next step's while this one is finished
-        }
-        if (adds) {                                  // (16 columns are 128 words of 16 bytes)
-          add_partial16(z, part_sums + c * 8);
-          if (kGated) add_partial16(u, part_sums + (kOutCols + c) * 8);
-        }
-        if (leaves) {
-          leave_partial16(z, part_sums + c * 8);
-          if (kGated) leave_partial16(u, part_sums + (kOutCols + c) * 8);
-          continue;
-        }
-        const int valid = p.N - col < 16 ? static_cast<int>(p.N - col) : 16;      // may be <= 0 in the second half of a slab
-        if (bias) {
-          float b[16];
-          load16(bias + col, bias_vec && valid == 16, valid, b);
-#pragma unroll
-          for (int e = 0; e < 16; ++e) z[e] += b[e];
-        }
-        if (kGated && bias2) {
-          float b[16];
-          load16(bias2 + col, bias_vec && valid == 16, valid, b);
-#pragma unroll
-          for (int e = 0; e < 16; ++e) u[e] += b[e];
-        }
-        // this thread's row of the slab in the staging buffer in turn
-        const uint32_t my = stage + buf * kSlabBytes + static_cast<uint32_t>(lane) * 64u;
-        constexpr int kChunks = sizeof(T);               // 16-byte chunks of 16 elements: 2 or 4
-        float s[16];
-        if (side_staged) {
-          if (h == 0) ok = __all_sync(0xFFFFFFFFu, mbar_wait(my_side_full + 8 * buf, buf_phase, abort_flag)) && ok;
-          read_staged16<T>(s, my, sw, h);
-        } else if (side) {
-          load16(side + (row_ok ? row : row0) * p.ld_side + col, p.side_vec && valid == 16, valid, s);
-        }
-        if constexpr (!kGrad) {
-          activate16<kAct>(z);
-          if (kGated) {
-#pragma unroll
-            for (int e = 0; e < 16; ++e) z[e] *= u[e];
+            for (int e = 0; e < 16; ++e) z[e] = __uint_as_float(r[e]);
+            if (adds) add_partial16(z, part_sums + cc * 8);
+            leave_partial16(z, part_sums + cc * 8);
           }
-          if (side) {
-#pragma unroll
-            for (int e = 0; e < 16; ++e) z[e] = fmaf(p.res_scale, s[e], z[e]);
-          }
-          uint4 out[kChunks];
-          pack16<T>(out, z);
-          if (p.units) {
-            // 64 columns of 32 rows as 128-byte rows, 16-byte chunk c of row r at c ^ (r & 7); then eight lanes per unit
-            if constexpr (sizeof(T) == 2) {
-              const uint32_t mine = stage + static_cast<uint32_t>(lane) * 128u, c0 = static_cast<uint32_t>(part & 3) * 2u, r7 = static_cast<uint32_t>(lane) & 7u;
-              sts128(mine + ((c0 ^ r7) << 4), out[0].x, out[0].y, out[0].z, out[0].w);
-              sts128(mine + (((c0 + 1u) ^ r7) << 4), out[1].x, out[1].y, out[1].z, out[1].w);
-              if ((part & 3) == 3) convert_units(col);
-            }
-          } else if (p.tma_store) {
-            if (!side_staged && h == 0) {
-              if (lane == 0) bulk_wait_read<kStageBufs - 1>();        // the store that used this buffer has read it
+        }
+        __syncwarp();
+        if (lane == 0 && left > 0) {
+          __threadfence();
+          asm volatile("red.release.gpu.global.add.u32 [%0], %1;" ::"l"(my_flag), "r"(left) : "memory");
+        }
+      } else {
+        const int step = !kGrad && p.units ? 64 : kSlabCols;
+#pragma unroll 1
+        for (int at = group * step; at < cols; at += groups * step)
+#pragma unroll 1
+        for (int c0 = at; c0 < at + step; c0 += kSlabCols) {
+          const uint32_t slab = stage + buf * kSlabBytes, my = slab + static_cast<uint32_t>(lane) * 64u;
+          const int64_t col0 = static_cast<int64_t>(w.n0) + c0, rows_here = p.M - row0, cols_here = p.N - col0;
+          // (with units the staging buffers hold them: the residual comes straight from its matrix)
+          const bool side_copied = side && !side_staged && (kGrad || !p.units);
+          if (side_staged) {
+            ok = __all_sync(0xFFFFFFFFu, mbar_wait(my_side_full + 8 * buf, buf_phase, abort_flag)) && ok;
+          } else if (kGrad || !p.units) {
+            if (lane == 0) bulk_wait_read<kStageBufs - 1>();          // the store that used this buffer has read it
+            __syncwarp();
+            if (side_copied) {
+              copy_slab<T, false>(const_cast<T*>(side) + row0 * p.ld_side + col0, p.ld_side, slab, lane, rows_here, cols_here);
               __syncwarp();
             }
+          }
+#pragma unroll 1
+          for (int h = 0; h < kSlabParts; ++h) {
+            const int c = c0 + 16 * h;
+            const int64_t col = static_cast<int64_t>(w.n0) + c;
+            float z[16], u[16];
+            {
+              uint32_t r[16];
+              tc_ld16(t_row + c, r);
+              tc_wait_ld16(r);
 #pragma unroll
-            for (int v = 0; v < kChunks; ++v)
-              sts128(my + (((static_cast<uint32_t>(kChunks * h + v)) ^ sw) << 4), out[v].x, out[v].y, out[v].z, out[v].w);
-            if (h == kSlabParts - 1) {
-              fence_proxy_async_smem();                  // generic-proxy writes -> visible to the TMA store
-              __syncwarp();
-              if (lane == 0) {
-                tma_store_2d(&tmY, static_cast<int>(col) - 16 * h, static_cast<int>(row0), stage + buf * kSlabBytes);
-                bulk_commit();
+              for (int e = 0; e < 16; ++e) z[e] = __uint_as_float(r[e]);
+              if (kGated) {
+                tc_ld16(t_row + kOutCols + c, r);
+                tc_wait_ld16(r);
+#pragma unroll
+                for (int e = 0; e < 16; ++e) u[e] = __uint_as_float(r[e]);
               }
             }
-          } else if (row_ok) {
-            T* dst = static_cast<T*>(p.y) + row * p.ld_y + col;
-            if (p.y_vec && valid == 16) {
+            if (adds) {
+              add_partial16(z, part_sums + c * 8);
+              if (kGated) add_partial16(u, part_sums + (kOutCols + c) * 8);
+            }
+            const int valid = p.N - col < 16 ? static_cast<int>(p.N - col) : 16;      // may be <= 0 in the second half of a slab
+            if (bias) {
+              float b[16];
+              load16(bias + col, bias_vec && valid == 16, valid, b);
 #pragma unroll
-              for (int v = 0; v < kChunks; ++v) reinterpret_cast<uint4*>(dst)[v] = out[v];
+              for (int e = 0; e < 16; ++e) z[e] += b[e];
+            }
+            if (kGated && bias2) {
+              float b[16];
+              load16(bias2 + col, bias_vec && valid == 16, valid, b);
+#pragma unroll
+              for (int e = 0; e < 16; ++e) u[e] += b[e];
+            }
+            float s[16];
+            if (side_staged || side_copied) read_staged16<T>(s, my, sw, h);
+            else if (side) load16(side + (row_ok ? row : row0) * p.ld_side + col, p.side_vec && valid == 16, valid, s);
+            if constexpr (!kGrad) {
+              activate16<kAct>(z);
+              if (kGated) {
+#pragma unroll
+                for (int e = 0; e < 16; ++e) z[e] *= u[e];
+              }
+              if (side) {
+#pragma unroll
+                for (int e = 0; e < 16; ++e) z[e] = fmaf(p.res_scale, s[e], z[e]);
+              }
+              uint4 out[sizeof(T)];
+              pack16<T>(out, z);
+              if (p.units) {
+                // 64 columns of 32 rows as 128-byte rows, 16-byte chunk c of row r at c ^ (r & 7); then eight lanes per unit
+                if constexpr (sizeof(T) == 2) {
+                  const uint32_t mine = stage + static_cast<uint32_t>(lane) * 128u, k = (static_cast<uint32_t>(c) & 63u) >> 3, r7 = static_cast<uint32_t>(lane) & 7u;
+                  sts128(mine + ((k ^ r7) << 4), out[0].x, out[0].y, out[0].z, out[0].w);
+                  sts128(mine + (((k + 1u) ^ r7) << 4), out[1].x, out[1].y, out[1].z, out[1].w);
+                }
+              } else {
+#pragma unroll
+                for (int v = 0; v < static_cast<int>(sizeof(T)); ++v)
+                  sts128(my + (((static_cast<uint32_t>(sizeof(T)) * h + v) ^ sw) << 4), out[v].x, out[v].y, out[v].z, out[v].w);
+              }
             } else {
+              float a[16];
+              activate_slope16<kAct>(z, a);
 #pragma unroll
-              for (int e = 0; e < 16; ++e)
-                if (e < valid) dst[e] = from_f32<T>(z[e]);
+              for (int e = 0; e < 16; ++e) {
+                const bool in = row_ok && e < valid;
+                z[e] = in ? s[e] * z[e] * (kGated ? u[e] : 1.0f) : 0.0f;
+                if (kGated) u[e] = in ? s[e] * a[e] : 0.0f;
+              }
+              constexpr int kParts = IsHalf<T>::value ? 2 : 1;
+              if (p.dz && row_ok) {
+                __nv_bfloat16* dst = p.dz + row * p.ld_dz + col;
+                store_parts<kParts>(z, dst, p.dz_plane, p.ld_dz - col);
+                if (kGated) store_parts<kParts>(u, dst + kParts * p.dz_plane, p.dz_plane, p.ld_dz - col);
+              }
+              if (p.colsum) {
+                const float sz = column_sum16(z, lane);
+                const int cl = column_of_lane(lane);
+                float* sums = p.colsum + (row0 >> 5) * p.N + col;
+                if ((lane & 1) == 0 && cl < valid) sums[cl] = sz;
+                if (kGated) {
+                  const float su = column_sum16(u, lane);
+                  if ((lane & 1) == 0 && cl < valid) sums[p.colsum_plane + cl] = su;
+                }
+              }
             }
           }
-        } else {
-          float a[16];
-          activate_slope16<kAct>(z, a);
-#pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            const bool in = row_ok && e < valid;
-            z[e] = in ? s[e] * z[e] * (kGated ? u[e] : 1.0f) : 0.0f;
-            if (kGated) u[e] = in ? s[e] * a[e] : 0.0f;
+          if (!kGrad && p.units) {
+            if (c0 & 32) convert_units(col0);
+            continue;
           }
-          constexpr int kParts = IsHalf<T>::value ? 2 : 1;
-          if (p.dz && row_ok) {
-            __nv_bfloat16* dst = p.dz + row * p.ld_dz + col;
-            store_parts<kParts>(z, dst, p.dz_plane, p.ld_dz - col);
-            if (kGated) store_parts<kParts>(u, dst + kParts * p.dz_plane, p.dz_plane, p.ld_dz - col);
-          }
-          if (p.colsum) {
-            const float sz = column_sum16(z, lane);
-            const int cl = column_of_lane(lane);
-            float* sums = p.colsum + (row0 >> 5) * p.N + col;
-            if ((lane & 1) == 0 && cl < valid) sums[cl] = sz;
-            if (kGated) {
-              const float su = column_sum16(u, lane);
-              if ((lane & 1) == 0 && cl < valid) sums[p.colsum_plane + cl] = su;
+          fence_proxy_async_smem();                  // generic-proxy writes (reads) before the async proxy reads (writes) the buffer
+          __syncwarp();
+          if (!kGrad) {
+            if (p.tma_store) {
+              if (lane == 0) {
+                tma_store_2d(&tmY, static_cast<int>(col0), static_cast<int>(row0), slab);
+                bulk_commit();
+              }
+            } else {
+              copy_slab<T, true>(static_cast<T*>(p.y) + row0 * p.ld_y + col0, p.ld_y, slab, lane, rows_here, cols_here);
+              if (side_staged) {
+                fence_proxy_async_smem();
+                __syncwarp();
+              }
             }
           }
-        }
-        if (h == kSlabParts - 1 && (side_staged || (!kGrad && p.tma_store && !p.units))) {
-          if (kGrad) {
-            fence_proxy_async_smem();
-            __syncwarp();                                // every lane has read the buffer that is asked for again
-          }
-          next_buffer(side_staged && part + 2 * kSlabParts < parts, c - 16 * h + 2 * kSlabCols);
+          next_buffer(side_staged, c0 + 2 * groups * kSlabCols);
         }
       }
-      }
-      tc_fence_before();                             // accumulator fully read: hand it back
-      __syncwarp();
-      if (lane == 0) mbar_arrive_cluster(tmem_empty_leader + 8 * acc);
-      if (!ok) break;
-      if (leaves) {                                  // this warp's rows of the partial sums are there for the next slice
-        if (lane == 0) {
-          __threadfence();
-          asm volatile("st.release.gpu.global.u32 [%0], %1;" ::"l"(my_flag), "r"(1u) : "memory");
-        }
+      if (!helper) {
+        tc_fence_before();                           // accumulator fully read: hand it back
+        __syncwarp();
+        if (lane == 0) mbar_arrive_cluster(tmem_empty_leader + 8 * acc);
       }
     }
     if (lane == 0) bulk_wait_all();                  // shared memory stays valid until the last store has read it
-  } else {
-    // ---------------------------------------------------------------- decode
-    const int d = threadIdx.x - kDecodeWarp0 * 32;            // 0..511
-    const int h = d >> 8;                                     // which unit pair of the raw chunk
-    const int row = d & 255;                                  // 0..127 A rows, 128..255 B rows
-    const uint32_t r7 = static_cast<uint32_t>(row) & 7u;
-    const uint32_t raw_row = static_cast<uint32_t>(row) * kRawRowBytes + static_cast<uint32_t>(h) * 64u;
-    const uint32_t dec_row = dec_base + static_cast<uint32_t>(2 * h) * kDecStageBytes + static_cast<uint32_t>(row) * 128u;
-    uint32_t chunk_addr[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) chunk_addr[j] = dec_row + ((static_cast<uint32_t>(j) ^ r7) << 4);
-    const uint32_t dec_empty0 = dec_empty + 16 * h;
-    const uint32_t dec_full0_leader = mapa(dec_full, 0) + 16 * h;
-    uint32_t n = 0;
-    bool ok = true;
-    for (int i = 0; i < n_items && ok; ++i) {
-      const WorkItem w = work_item<kOutCols>(p, pair, num_pairs, i);
-      // the first of this warp's 32 rows exists (whole warps of rows past the edge are left out)
-      const int warp_row = row & ~31;
-      const bool live = warp_row < kRows ? static_cast<int64_t>(w.m0) + rank * kRows + warp_row < p.M
-                                         : static_cast<int64_t>(w.n0) + (kGated ? 0 : rank * kRows) + (warp_row - kRows) < p.N;
-      for (int kc = w.kc0; kc < w.kc1 && ok; ++kc, ++n) {
-        const uint32_t s = n & 1u, ph = (n >> 1) & 1u;
-        if (!(ok = __all_sync(0xFFFFFFFFu, mbar_wait(raw_full + 8 * s, ph, abort_flag)))) break;
-        uint32_t W[18];
-        if (live) {
-          uint32_t L[20];
-          const uint32_t src = raw_base + s * kRawStageBytes + raw_row;
-#pragma unroll
-          for (int i = 0; i < 5; ++i) {
-            const uint4 v = lds128(src + 16 * i);
-            L[4 * i] = v.x; L[4 * i + 1] = v.y; L[4 * i + 2] = v.z; L[4 * i + 3] = v.w;
-          }
-          fence_proxy_async_smem();                  // these reads before the async proxy refills the stage
-#pragma unroll
-          for (int i = 0; i < 18; ++i) W[i] = h ? L[i + 2] : L[i];
-        }
-        mbar_arrive(raw_empty + 8 * s);
-        ok = decode_two_units(W, chunk_addr, lut, p.mul, dec_empty0, dec_full0_leader, (n & 1u) ^ 1u, abort_flag, live);
-      }
-    }
   }
 
   // ------------------------------------------------------------------ teardown

@@ -61,9 +61,8 @@ hif4_status launch_linear_act(const LinearCall& c, void* workspace, cudaStream_t
   p.side_tma = c.side && p.side_vec && c.ld_side * sizeof(T) % 16 == 0 && !c.units && make_y_map<T>(&tmSide, const_cast<void*>(c.side), c.M, c.N, c.ld_side);
   p.y = c.y; p.ld_y = c.ld_y; p.units = c.units; p.rha = c.rha;
   if (!kGrad && !c.units) {
-    p.y_vec = at16(c.y) && (c.M == 1 || c.ld_y * sizeof(T) % 16 == 0);
-    // (a TMA store clips the innermost dimension in 16-byte pieces: other widths take the per-thread stores)
-    p.tma_store = p.y_vec && c.ld_y * sizeof(T) % 16 == 0 && c.N * sizeof(T) % 16 == 0 && make_y_map<T>(&tmY, c.y, c.M, c.N, c.ld_y);
+    // (a TMA store clips the innermost dimension in 16-byte pieces: other widths are copied from the staging buffers)
+    p.tma_store = at16(c.y) && c.ld_y * sizeof(T) % 16 == 0 && c.N * sizeof(T) % 16 == 0 && make_y_map<T>(&tmY, c.y, c.M, c.N, c.ld_y);
   }
   p.dz = c.dz; p.ld_dz = c.ld_dz; p.dz_plane = c.dz_plane;
   p.colsum = c.colsum; p.colsum_plane = ceil_div64(c.M, 32) * c.N;
