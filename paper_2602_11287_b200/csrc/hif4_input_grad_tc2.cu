@@ -13,7 +13,7 @@
 //   warps 6-21  decode, four teams of four warps on steps in turn: thread = one unit; a warp reports a step once its units
 //               are written and the step's dZ has landed.  (A unit is 200 dependent instructions of one warp: two teams
 //               took as long over a step as the tensor core.)
-//   warp 1      rank 0: MMA issue;   warps 2-5  epilogue, TMA stores of 64-byte rows
+//   warp 1      rank 0: MMA issue;   warps 2-5  epilogue, TMA stores of 64-byte rows (the last tile with the decode warps)
 // Phases: the BF16 parts of dZ (one for BF16 gradients, two for FP16), for both projections of a gated layer.
 // Tiles shared along the contraction pass FP32 partial sums as in the forward kernel.
 #include "hif4_linear_tc2_launch.cuh"
@@ -217,51 +217,95 @@ input_grad_tc2_kernel(const __grid_constant__ CUtensorMap tmZ, const __grid_cons
         tc2_commit_both(tmem_full + 8 * acc);
       }
     }
-  } else if (warp < kGradDecodeWarp0) {
-    // ---------------------------------------------------------------- epilogue
+  } else {
+    // ---------------------------------------------------------------- decode, then its warps join the epilogue of the last tile
+    bool ok = true;
+    if (warp >= kGradDecodeWarp0) {
+      const int d = threadIdx.x - kGradDecodeWarp0 * 32;
+      const uint32_t team = static_cast<uint32_t>(d) / kTeamThreads;
+      const int t = d & (kTeamThreads - 1), row = t & (kStepRows - 1), block = t >> 6;      // contraction row, 64-column block
+      // The unit's nine words within the row's five 16-byte words: 2 rank + 9 block words from its start.  Three 16-byte
+      // loads (a row pitch of 80 bytes spreads eight of them over all banks; single words would meet four at a bank) from
+      // the 16-byte word it starts in, or the one before, then a shift by 0 to 3 words.
+      const uint32_t src0 = raw_base + static_cast<uint32_t>(row) * kWinBytes + static_cast<uint32_t>(block) * 32u;
+      const bool shift1 = block != 0, shift2 = rank != 0;
+      const uint32_t op_row = op_base + kOpHalfBytes + static_cast<uint32_t>(block) * (kStepRows * 128) + static_cast<uint32_t>(row) * 128u;
+      uint32_t chunk_addr[8];
+  #pragma unroll
+      for (int j = 0; j < 8; ++j) chunk_addr[j] = op_row + ((static_cast<uint32_t>(j) ^ (static_cast<uint32_t>(row) & 7u)) << 4);
+      const uint32_t op_full_leader = mapa(op_full, 0);
+      Ring raw, op;
+      uint32_t n = 0;
+      for (int i = 0; i < n_items && ok; ++i) {
+        const WorkItem w = work_item<kPairN>(p, pair, num_pairs, i);
+        for (int kc = w.kc0; kc < w.kc1 && ok; ++kc) {
+          const StepRange c = chunk_steps(p, kc);
+          for (int step = 0; step < c.steps; ++step, ++n, raw.next(kRawRing), op.next(kOpRing)) {
+            if (n % kTeams != team) continue;
+            if (!(ok = __all_sync(0xFFFFFFFFu, mbar_wait(raw_full + 8 * raw.s, raw.ph, abort_flag)))) break;
+            uint32_t L[12], W[9];
+  #pragma unroll
+            for (int k = 0; k < 3; ++k) {
+              const uint4 v = lds128(src0 + raw.s * kRawStepBytes + 16 * k);
+              L[4 * k] = v.x; L[4 * k + 1] = v.y; L[4 * k + 2] = v.z; L[4 * k + 3] = v.w;
+            }
+  #pragma unroll
+            for (int k = 0; k < 11; ++k) L[k] = shift1 ? L[k + 1] : L[k];
+  #pragma unroll
+            for (int k = 0; k < 9; ++k) W[k] = shift2 ? L[k + 2] : L[k];
+            fence_proxy_async_smem();                  // these reads before the async proxy refills the stage
+            mbar_arrive(raw_empty + 8 * raw.s);
+            if (!(ok = __all_sync(0xFFFFFFFFu, mbar_wait(op_empty + 8 * op.s, op.ph ^ 1u, abort_flag)))) break;
+            decode_unit_balanced(W[0], &W[1], chunk_addr, op.s * kOpStageBytes, lut, p.mul);
+            fence_proxy_async_smem();                  // generic-proxy writes -> visible to the tensor core
+            if (!(ok = __all_sync(0xFFFFFFFFu, mbar_wait(z_full + 8 * op.s, op.ph, abort_flag)))) break;
+            __syncwarp();
+            if (lane == 0) mbar_arrive_cluster(op_full_leader + 8 * op.s);
+          }
+        }
+      }
+    }
+
+    // ---------------------------------------------------------------- epilogue (as in the forward kernel)
+    const bool helper = warp >= kGradDecodeWarp0;
     const int q = warp & 3;
+    const int group = helper ? 1 + (warp - kGradDecodeWarp0) / 4 : 0;
     const uint32_t tmem_empty_leader = mapa(tmem_empty, 0);
-    const uint32_t stage = out_base + static_cast<uint32_t>(q) * (kStageBufs * kSlabBytes);
-    uint32_t tcount = 0, slabs = 0;
-    for (int it = 0; it < n_items; ++it, ++tcount) {
+    const uint32_t stage = helper ? op_base + static_cast<uint32_t>(warp - kGradDecodeWarp0) * (2 * kSlabBytes)
+                                  : out_base + static_cast<uint32_t>(q) * (2 * kSlabBytes);
+    uint32_t slabs = 0;
+    const int first = helper && n_items > 0 ? n_items - 1 : 0;
+    uint32_t tcount = static_cast<uint32_t>(first);
+    for (int it = first; it < n_items && ok; ++it, ++tcount) {
       const WorkItem w = work_item<kPairN>(p, pair, num_pairs, it);
       const uint32_t acc = tcount & 1u, aph = (tcount >> 1) & 1u;
-      if (!__all_sync(0xFFFFFFFFu, mbar_wait(tmem_full + 8 * acc, aph, abort_flag, 256))) break;
+      if (!__all_sync(0xFFFFFFFFu, mbar_wait(tmem_full + 8 * acc, aph, abort_flag, helper ? 32 : 256))) break;
       tc_fence_after();
       const bool shared_tile = w.tail >= 0 && p.slices > 1;
       const bool adds = shared_tile && w.slice > 0, leaves = shared_tile && w.slice + 1 < p.slices;
-      unsigned int* my_flag = shared_tile ? p.flags + (static_cast<size_t>(w.tail) * p.slices + w.slice) * 8 + rank * 4 + q : nullptr;
-      if (adds && !__all_sync(0xFFFFFFFFu, wait_count(my_flag - 8, 1u, abort_flag))) break;
-      float4* part = shared_tile ? partial_of(p.partial, w.tail, rank, q, lane) : nullptr;
+      const int groups = it == n_items - 1 ? kEpiGroups : 1;
       const int64_t row0 = static_cast<int64_t>(w.m0) + rank * kRows + q * 32, row = row0 + lane;
+      const int64_t cols_left = p.K - w.n0;              // K is a multiple of 64: a slab is inside or outside as a whole
+      const int cols = row0 >= p.M ? 0 : cols_left < kPairN ? static_cast<int>(cols_left) : kPairN;
+      unsigned int* my_flag = shared_tile ? p.flags + (static_cast<size_t>(w.tail) * p.slices + w.slice) * 8 + rank * 4 + q : nullptr;
+      if (adds && cols > 0 && !__all_sync(0xFFFFFFFFu, wait_count(my_flag - 8, static_cast<unsigned int>(cols / 32), abort_flag))) break;
+      float4* part = shared_tile ? partial_of(p.partial, w.tail, rank, q, lane) : nullptr;
       const uint32_t t_row = tmem_base + (static_cast<uint32_t>(q * 32) << 16) + acc * kPairN;
+      unsigned int left = 0;
 #pragma unroll 1
-      for (int slab = 0; slab < kPairN / 32; ++slab) {
-        const int64_t col0 = static_cast<int64_t>(w.n0) + slab * 32;
-        const bool inside = row0 < p.M && col0 < p.K;
-        uint32_t words[16];
+      for (int c0 = group * 32; c0 < cols; c0 += groups * 32) {
+        const int64_t col0 = static_cast<int64_t>(w.n0) + c0;
+        uint32_t r[2][16], words[16];
+        tc_ld16(t_row + c0, r[0]);
+        tc_ld16(t_row + c0 + 16, r[1]);
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          const int c = slab * 32 + h * 16;
           float z[16];
-          if (inside) {
-            uint32_t r[16];
-            tc_ld16(t_row + c, r);
-            tc_wait_ld();
+          tc_wait_ld16(r[h]);
 #pragma unroll
-            for (int e = 0; e < 16; ++e) z[e] = __uint_as_float(r[e]);
-          }
-          if (slab == kPairN / 32 - 1 && h == 1) {
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive_cluster(tmem_empty_leader + 8 * acc);
-          }
-          if (!inside) continue;
-          if (adds) add_partial16(z, part + c * 8);
-          if (leaves) {
-            leave_partial16(z, part + c * 8);
-            continue;
-          }
+          for (int e = 0; e < 16; ++e) z[e] = __uint_as_float(r[h][e]);
+          if (adds) add_partial16(z, part + (c0 + 16 * h) * 8);
+          if (leaves) leave_partial16(z, part + (c0 + 16 * h) * 8);
 #pragma unroll
           for (int g = 0; g < 2; ++g) {                 // group of eight columns, held in the order 0 4 1 5 2 6 3 7
             const float* v = z + 8 * g;
@@ -272,7 +316,10 @@ input_grad_tc2_kernel(const __grid_constant__ CUtensorMap tmZ, const __grid_cons
             o[3] = pack2(v[5], v[7], T());
           }
         }
-        if (!inside || leaves) continue;
+        if (leaves) {
+          ++left;
+          continue;
+        }
         if (p.tma_store) {
           const uint32_t buf = stage + (slabs & 1u) * kSlabBytes;
           const uint32_t my = buf + static_cast<uint32_t>(lane) * 64u, sw = (static_cast<uint32_t>(lane) >> 1) & 3u;    // SWIZZLE_64B
@@ -288,7 +335,7 @@ input_grad_tc2_kernel(const __grid_constant__ CUtensorMap tmZ, const __grid_cons
             bulk_commit();
           }
           ++slabs;
-        } else if (row < p.M) {                          // K is a multiple of 64: a slab is inside as a whole
+        } else if (row < p.M) {
           T* dst = static_cast<T*>(p.dx) + row * p.ld_dx + col0;
           if (p.dx_vec) {
 #pragma unroll
@@ -302,59 +349,18 @@ input_grad_tc2_kernel(const __grid_constant__ CUtensorMap tmZ, const __grid_cons
       }
       if (leaves) {
         __syncwarp();
-        if (lane == 0) {
+        if (lane == 0 && left > 0) {
           __threadfence();
-          asm volatile("st.release.gpu.global.u32 [%0], %1;" ::"l"(my_flag), "r"(1u) : "memory");
+          asm volatile("red.release.gpu.global.add.u32 [%0], %1;" ::"l"(my_flag), "r"(left) : "memory");
         }
+      }
+      if (!helper) {
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive_cluster(tmem_empty_leader + 8 * acc);
       }
     }
     if (lane == 0) bulk_wait_all();
-  } else {
-    // ---------------------------------------------------------------- decode
-    const int d = threadIdx.x - kGradDecodeWarp0 * 32;
-    const uint32_t team = static_cast<uint32_t>(d) / kTeamThreads;
-    const int t = d & (kTeamThreads - 1), row = t & (kStepRows - 1), block = t >> 6;      // contraction row, 64-column block
-    // The unit's nine words within the row's five 16-byte words: 2 rank + 9 block words from its start.  Three 16-byte
-    // loads (a row pitch of 80 bytes spreads eight of them over all banks; single words would meet four at a bank) from
-    // the 16-byte word it starts in, or the one before, then a shift by 0 to 3 words.
-    const uint32_t src0 = raw_base + static_cast<uint32_t>(row) * kWinBytes + static_cast<uint32_t>(block) * 32u;
-    const bool shift1 = block != 0, shift2 = rank != 0;
-    const uint32_t op_row = op_base + kOpHalfBytes + static_cast<uint32_t>(block) * (kStepRows * 128) + static_cast<uint32_t>(row) * 128u;
-    uint32_t chunk_addr[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) chunk_addr[j] = op_row + ((static_cast<uint32_t>(j) ^ (static_cast<uint32_t>(row) & 7u)) << 4);
-    const uint32_t op_full_leader = mapa(op_full, 0);
-    Ring raw, op;
-    uint32_t n = 0;
-    bool ok = true;
-    for (int i = 0; i < n_items && ok; ++i) {
-      const WorkItem w = work_item<kPairN>(p, pair, num_pairs, i);
-      for (int kc = w.kc0; kc < w.kc1 && ok; ++kc) {
-        const StepRange c = chunk_steps(p, kc);
-        for (int step = 0; step < c.steps; ++step, ++n, raw.next(kRawRing), op.next(kOpRing)) {
-          if (n % kTeams != team) continue;
-          if (!(ok = __all_sync(0xFFFFFFFFu, mbar_wait(raw_full + 8 * raw.s, raw.ph, abort_flag)))) break;
-          uint32_t L[12], W[9];
-#pragma unroll
-          for (int k = 0; k < 3; ++k) {
-            const uint4 v = lds128(src0 + raw.s * kRawStepBytes + 16 * k);
-            L[4 * k] = v.x; L[4 * k + 1] = v.y; L[4 * k + 2] = v.z; L[4 * k + 3] = v.w;
-          }
-#pragma unroll
-          for (int k = 0; k < 11; ++k) L[k] = shift1 ? L[k + 1] : L[k];
-#pragma unroll
-          for (int k = 0; k < 9; ++k) W[k] = shift2 ? L[k + 2] : L[k];
-          fence_proxy_async_smem();                  // these reads before the async proxy refills the stage
-          mbar_arrive(raw_empty + 8 * raw.s);
-          if (!(ok = __all_sync(0xFFFFFFFFu, mbar_wait(op_empty + 8 * op.s, op.ph ^ 1u, abort_flag)))) break;
-          decode_unit_balanced(W[0], &W[1], chunk_addr, op.s * kOpStageBytes, lut, p.mul);
-          fence_proxy_async_smem();                  // generic-proxy writes -> visible to the tensor core
-          if (!(ok = __all_sync(0xFFFFFFFFu, mbar_wait(z_full + 8 * op.s, op.ph, abort_flag)))) break;
-          __syncwarp();
-          if (lane == 0) mbar_arrive_cluster(op_full_leader + 8 * op.s);
-        }
-      }
-    }
   }
 
   // ------------------------------------------------------------------ teardown
