@@ -1,4 +1,4 @@
-"""Thin ctypes binding of libhif4.so: argument marshalling only.
+"""Thin binding of libhif4.so: argument marshalling only (ctypes, and a native module for the calls of a transformer block).
 
 Every step of the path runs in the CUDA kernels behind the C ABI declared in ``include/hif4.h``;
 PyTorch supplies device memory and the current stream.  There is no CPU fallback: if the library has
@@ -8,7 +8,6 @@ from __future__ import annotations
 
 import ctypes
 import os
-import struct
 from typing import Optional
 
 import torch
@@ -77,18 +76,8 @@ def _load() -> ctypes.CDLL:
     L.hif4_mse_workspace.argtypes = [i64, ci, ctypes.POINTER(sz)]
     L.hif4_mse_roundtrip.restype = ci
     L.hif4_mse_roundtrip.argtypes = [vp, i64, ci, vp, vp, vp, sz, vp]
-    L.hif4_block_norm.restype = ci
-    L.hif4_block_norm.argtypes = [ctypes.c_char_p, vp]
     L.hif4_block_norm_backward_workspace.restype = ci
     L.hif4_block_norm_backward_workspace.argtypes = [i64, i64, ctypes.POINTER(sz)]
-    L.hif4_block_norm_backward.restype = ci
-    L.hif4_block_norm_backward.argtypes = [ctypes.c_char_p, vp, sz, vp]
-    for name in ("hif4_linear_act", "hif4_gated_linear"):
-        for suffix in ("", "_backward"):
-            call, query = getattr(L, name + suffix), getattr(L, name + suffix + "_workspace")
-            call.restype = query.restype = ci
-            call.argtypes = [ctypes.c_char_p, vp, sz, vp]
-            query.argtypes = [ctypes.c_char_p, ctypes.POINTER(sz)]
     L.hif4_last_device_status.restype = ci
     L.hif4_last_device_status.argtypes = [vp]
     L.hif4_status_string.restype = ctypes.c_char_p
@@ -103,6 +92,10 @@ def _load() -> ctypes.CDLL:
 
 
 lib = _load()
+try:
+    from . import _hif4_torch as _native  # noqa: E402  (tensor-level calls of csrc_torch/, linked against libhif4.so)
+except ImportError as e:
+    raise ImportError(f"the native calls are missing ({e}): build them with `python paper_2602_11287_b200/build.py`") from e
 
 
 def status_string(code: int) -> str:
@@ -338,13 +331,8 @@ def hif4_mse_roundtrip(src: torch.Tensor, fmt: int, want_image: bool = True, wor
 
 
 # ---------------------------------------------------------------------------------------- between two linears of a block
-def _dtype_any(dt: torch.dtype) -> int:
-    code = _TYPE_CODES.get(dt)
-    if code is None:
-        raise TypeError(f"bfloat16, float16 or float32 expected, not {dt}")
-    return code
-
-
+# These calls go through the native module: its functions check the tensors (ValueError, TypeError), allocate what is not
+# passed in, and call the library on the current stream.
 _TYPE_CODES = {torch.bfloat16: HIF4_BF16, torch.float32: HIF4_FP32, torch.float16: HIF4_FP16}
 
 
@@ -357,68 +345,19 @@ def _under(stream, call, params: dict):
         return call(**params)
 
 
-# Arguments go over as one packed structure (a ctypes.Structure costs three times as much to fill): the formats follow the
-# fields of the argument types in include/hif4.h.
-ARGUMENT_FORMATS = {
-    "hif4_block_norm_args": "qqiiPqPqfPqqiPiPPfPqPqii0q",
-    "hif4_block_norm_backward_args": "qqiiPqPqPqPqfPqqiPiPfPqPqPPPP0q",
-    "hif4_linear_act_args": "qqqPqiiiPPiPPiPqfPqi0q",
-    "hif4_linear_act_backward_args": "qqqPqiiiPPiPPiPqPqPP0q",
-}
-_pack_block_norm, _pack_block_norm_backward, _pack_linear_act, _pack_linear_act_backward = (
-    struct.Struct(f).pack for f in ARGUMENT_FORMATS.values())
-
-_current_raw_stream = torch._C._cuda_getCurrentRawStream      # what torch.cuda.current_stream(...).cuda_stream returns, without the object
+def _result(call: str, r):
+    if r.__class__ is int:
+        raise Hif4Error(call, r)
+    return r
 
 
-def _matrix(t: Optional[torch.Tensor], rows: int, cols: int, dtype: torch.dtype, what: str):
-    """(address, row stride) of a [rows, cols] operand with unit column stride; (0, 0) without one."""
-    if t is None:
-        return 0, 0
-    if t.dtype is dtype and t.is_cuda and t.shape == (rows, cols):
-        ld, step = t.stride()
-        if step == 1 or cols <= 1:
-            return t.data_ptr(), (ld if rows > 1 or ld >= cols else cols)
-    if not t.is_cuda:
-        raise ValueError("the HiF4 library takes device tensors only (no CPU path exists)")
-    raise ValueError(f"{what}: [{rows}, {cols}] of {dtype} with unit column stride expected, got "
-                     f"{tuple(t.shape)} of {t.dtype}, strides {t.stride()}")
-
-
-def _vector(t: Optional[torch.Tensor], n: int, dtype: Optional[torch.dtype], what: str) -> int:
-    """Address of a contiguous [n] operand of `dtype`; 0 without one."""
-    if t is None:
-        return 0
-    if t.dtype is dtype and t.is_cuda and t.shape == (n,) and (n <= 1 or t.stride(0) == 1):
-        return t.data_ptr()
-    if not t.is_cuda:
-        raise ValueError("the HiF4 library takes device tensors only (no CPU path exists)")
-    raise ValueError(f"{what}: contiguous [{n}] of {dtype} expected, got {tuple(t.shape)} of {t.dtype}, strides {t.stride()}")
-
-
-def _units(t: torch.Tensor, rows: int, units: int, what: str) -> int:
-    """Address of contiguous units [rows, units, 36]."""
-    if t.dtype is torch.uint8 and t.is_cuda and t.shape == (rows, units, UNIT_BYTES) and t.is_contiguous():
-        return t.data_ptr()
-    if not t.is_cuda:
-        raise ValueError("the HiF4 library takes device tensors only (no CPU path exists)")
-    raise ValueError(f"{what}: contiguous uint8 units [{rows}, {units}, {UNIT_BYTES}] expected, got {tuple(t.shape)} of {t.dtype}")
-
-
-def _rows_like(rows: int, cols: int, dtype: torch.dtype, device) -> torch.Tensor:
-    return torch.empty_strided((rows, cols), (cols, 1), dtype=dtype, device=device)
-
-
-def _new_units(rows: int, units: int, device) -> torch.Tensor:
-    return torch.empty_strided((rows, units, UNIT_BYTES), (units * UNIT_BYTES, UNIT_BYTES, 1), dtype=torch.uint8, device=device)
-
-
-def _gates(gate: Optional[torch.Tensor], rows: int, cols: int, rows_per_gate: int, dtype: torch.dtype):
-    if gate is None:
-        return 0, 0
-    if rows_per_gate < 1:
-        raise ValueError("a gate needs rows_per_gate >= 1")
-    return _matrix(gate, -(-rows // rows_per_gate), cols, dtype, "gate")
+def _type_code(dtype: Optional[torch.dtype]) -> int:
+    if dtype is None:
+        return -1
+    code = _TYPE_CODES.get(dtype)
+    if code is None:
+        raise TypeError(f"bfloat16, float16 or float32 expected, not {dtype}")
+    return code
 
 
 def hif4_block_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None, *,
@@ -431,33 +370,9 @@ def hif4_block_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias
     [rows, cols // 64, 36] with units=True.  h is x itself where nothing changes it and no out_h is given."""
     if stream is not None:
         return _under(stream, hif4_block_norm, locals())
-    if x.dim() != 2:
-        raise ValueError("x: a matrix expected")
-    rows, cols = x.shape
-    dtype, dev = x.dtype, x.device
-    code = _dtype_any(dtype)
-    px, ldx = _matrix(x, rows, cols, dtype, "x")
-    pr, ldr = _matrix(residual, rows, cols, dtype, "residual")
-    pg, ldg = _gates(gate, rows, cols, rows_per_gate, dtype)
-    wt = dtype if weight is None and bias is None and post_weight is None else next(
-        w.dtype for w in (weight, bias, post_weight) if w is not None)
-    h, y = out_h, out_y
-    if h is None and not (residual is None and gate is None and post == HIF4_NORM_NONE):
-        h = _rows_like(rows, cols, dtype, dev)
-    if y is None and pre != HIF4_NORM_NONE:
-        y = _new_units(rows, cols // UNIT_ELEMS, dev) if units else _rows_like(rows, cols, dtype, dev)
-    if h is None and y is None:
-        return x, None
-    ph, ldh = _matrix(h, rows, cols, dtype, "out_h")
-    if units and y is not None:
-        py, ldy = _units(y, rows, cols // UNIT_ELEMS, "out_y"), 0
-    else:
-        py, ldy = _matrix(y, rows, cols, dtype, "out_y")
-    a = _pack_block_norm(rows, cols, code, code if wt is dtype else _dtype_any(wt), px, ldx, pr, ldr, res_scale, pg, ldg, rows_per_gate,
-                         post, _vector(post_weight, cols, wt, "post_weight"), pre, _vector(weight, cols, wt, "weight"),
-                         _vector(bias, cols, wt, "bias"), eps, ph, ldh, py, ldy, 1 if units else 0, mode)
-    _check("hif4_block_norm", lib.hif4_block_norm(a, _current_raw_stream(dev.index)))
-    return (x if h is None else h), y
+    r = _native.block_norm(x, weight, bias, residual, res_scale, gate, rows_per_gate, post, post_weight, pre, eps, units, mode,
+                           out_h, out_y)
+    return r if r.__class__ is tuple else _result("hif4_block_norm", r)
 
 
 def hif4_block_norm_backward_workspace(rows: int, cols: int) -> int:
@@ -477,94 +392,9 @@ def hif4_block_norm_backward(dy: Optional[torch.Tensor], h: Optional[torch.Tenso
     forward call had no such input."""
     if stream is not None:
         return _under(stream, hif4_block_norm_backward, locals())
-    first = dy if dy is not None else dh
-    if first is None or first.dim() != 2:
-        raise ValueError("dy or dh: a matrix expected")
-    rows, cols = first.shape
-    dtype, dev = first.dtype, first.device
-    pdy, lddy = _matrix(dy, rows, cols, dtype, "dy")
-    pdh, lddh = _matrix(dh, rows, cols, dtype, "dh")
-    ph, ldh = _matrix(h, rows, cols, dtype, "h")
-    px, ldx = _matrix(x, rows, cols, dtype, "x")
-    pg, ldg = _gates(gate, rows, cols, rows_per_gate, dtype)
-    wt = next((w.dtype for w in (weight, post_weight) if w is not None), dtype)
-    pw, pwp = _vector(weight, cols, wt, "weight"), _vector(post_weight, cols, wt, "post_weight")
-    d = {"dx": _rows_like(rows, cols, dtype, dev),
-         "dresidual": _rows_like(rows, cols, dtype, dev) if want_dresidual else None,
-         "dgate": _rows_like(gate.shape[0], cols, dtype, dev) if gate is not None else None,
-         "dweight": torch.empty(cols, dtype=torch.float32, device=dev) if weight is not None and dy is not None else None,
-         "dbias": torch.empty(cols, dtype=torch.float32, device=dev) if bias and dy is not None else None,
-         "dpost_weight": torch.empty(cols, dtype=torch.float32, device=dev) if post_weight is not None else None}
-    need = hif4_block_norm_backward_workspace(rows, cols)
-    if workspace is None and need:
-        workspace = torch.empty(need, dtype=torch.uint8, device=dev)
-
-    def at(k):
-        return d[k].data_ptr() if d[k] is not None else 0
-
-    a = _pack_block_norm_backward(rows, cols, _dtype_any(dtype), _dtype_any(wt), pdy, lddy, pdh, lddh, ph, ldh, px, ldx, res_scale,
-                               pg, ldg, rows_per_gate, post, pwp, pre, pw, eps, at("dx"), cols, at("dresidual"), cols,
-                               at("dgate"), at("dweight"), at("dbias"), at("dpost_weight"))
-    _check("hif4_block_norm_backward", lib.hif4_block_norm_backward(
-        a, workspace.data_ptr() if workspace is not None else None, workspace.numel() if workspace is not None else 0,
-        _current_raw_stream(dev.index)))
-    return d
-
-
-def _activations(x: torch.Tensor):
-    """(rows, K, address, row stride, type code, 1 for units) of activations [rows, K] or units [rows, K / 64, 36]."""
-    if x.dtype is torch.uint8:
-        if x.dim() != 3:
-            raise ValueError(f"x: units [rows, K / {UNIT_ELEMS}, {UNIT_BYTES}] expected, got {tuple(x.shape)}")
-        rows, n, _ = x.shape
-        return rows, n * UNIT_ELEMS, _units(x, rows, n, "x"), 0, HIF4_BF16, 1
-    if x.dim() != 2:
-        raise ValueError(f"x: a matrix expected, got {tuple(x.shape)}")
-    rows, K = x.shape
-    p, ld = _matrix(x, rows, K, x.dtype, "x")
-    return rows, K, p, ld, _dtype_any(x.dtype), 0
-
-
-_workspace_bytes: dict = {}       # what the *_workspace queries answered, by everything that the answer depends on
-
-
-def _run_with_workspace(name: str, args: bytes, key: tuple, workspace: Optional[torch.Tensor], device) -> None:
-    key = (name, device.index, key)
-    need = _workspace_bytes.get(key)
-    if need is None:
-        n = ctypes.c_size_t(0)
-        _check(name + "_workspace", getattr(lib, name + "_workspace")(args, ctypes.byref(n)))
-        if len(_workspace_bytes) >= 4096:
-            _workspace_bytes.clear()
-        need = _workspace_bytes[key] = int(n.value)
-    if workspace is None and need:
-        workspace = torch.empty_strided((need,), (1,), dtype=torch.uint8, device=device)
-    if workspace is None:
-        code = getattr(lib, name)(args, None, 0, _current_raw_stream(device.index))
-    else:
-        code = getattr(lib, name)(args, workspace.data_ptr(), workspace.numel(), _current_raw_stream(device.index))
-    if code != HIF4_OK:
-        raise Hif4Error(name, code)
-
-
-def _linear_act(name, x, w_units, w_up, bias, bias_up, residual, res_scale, act, dtype, units, mode, out, workspace):
-    M, K, px, ldx, dt_x, x_units = _activations(x)
-    N, dev = w_units.shape[0], x.device
-    if dtype is None:
-        dtype = out.dtype if out is not None and not units else x.dtype if not x_units else torch.bfloat16
-    pr, ldr = _matrix(residual, M, N, dtype, "residual")
-    if out is None:
-        out = _new_units(M, N // UNIT_ELEMS, dev) if units else _rows_like(M, N, dtype, dev)
-    if units:
-        py, ldy = _units(out, M, N // UNIT_ELEMS, "out"), 0
-    else:
-        py, ldy = _matrix(out, M, N, dtype, "out")
-    dt, units = _dtype_any(dtype), 1 if units else 0
-    a = _pack_linear_act(M, N, K, px, ldx, dt_x, x_units, mode, _units(w_units, N, K // UNIT_ELEMS, "w_units"),
-                         0 if w_up is None else _units(w_up, N, K // UNIT_ELEMS, "w_up_units"), dt,
-                         _vector(bias, N, dtype, "bias"), _vector(bias_up, N, dtype, "bias_up"), act, pr, ldr, res_scale, py, ldy, units)
-    _run_with_workspace(name, a, (M, N, K, x_units, dt, units), workspace, dev)
-    return out
+    r = _result("hif4_block_norm_backward", _native.block_norm_backward(
+        dy, h, weight, dh, x, bias, res_scale, gate, rows_per_gate, post, post_weight, pre, eps, want_dresidual, workspace))
+    return dict(zip(("dx", "dresidual", "dgate", "dweight", "dbias", "dpost_weight"), r))
 
 
 def hif4_linear_act(x: torch.Tensor, w_units: torch.Tensor, bias: Optional[torch.Tensor] = None, *,
@@ -577,8 +407,9 @@ def hif4_linear_act(x: torch.Tensor, w_units: torch.Tensor, bias: Optional[torch
     `out` may be the residual itself."""
     if stream is not None:
         return _under(stream, hif4_linear_act, locals())
-    return _linear_act("hif4_linear_act", x, w_units, None, bias, None, residual, res_scale, act, dtype, units, mode, out,
-                       workspace)
+    r = _native.linear_act(x, w_units, None, bias, None, residual, res_scale, act, -1 if dtype is None else _type_code(dtype), units, mode,
+                           out, workspace)
+    return r if r.__class__ is not int else _result("hif4_linear_act", r)
 
 
 def hif4_gated_linear(x: torch.Tensor, w_units: torch.Tensor, w_up_units: torch.Tensor, bias: Optional[torch.Tensor] = None,
@@ -589,33 +420,11 @@ def hif4_gated_linear(x: torch.Tensor, w_units: torch.Tensor, w_up_units: torch.
     """act(HiF4(x) @ W^T + bias) * (HiF4(x) @ W_up^T + bias_up) + res_scale * residual; arguments as in hif4_linear_act."""
     if stream is not None:
         return _under(stream, hif4_gated_linear, locals())
-    return _linear_act("hif4_gated_linear", x, w_units, w_up_units, bias, bias_up, residual, res_scale, act, dtype, units, mode,
-                       out, workspace)
-
-
-def _linear_act_backward(name, dy, x, w_units, w_up, bias, bias_up, act, mode, want_dx, want_dbias, workspace):
-    if dy.dim() != 2:
-        raise ValueError("dy: a matrix expected")
-    M, N = dy.shape
-    dtype, dev = dy.dtype, dy.device
-    pdy, lddy = _matrix(dy, M, N, dtype, "dy")
-    K = w_units.shape[1] * UNIT_ELEMS
-    px, ldx, dt_x, x_units = 0, K, HIF4_BF16, 0
-    if x is not None:
-        rows, kx, px, ldx, dt_x, x_units = _activations(x)
-        if rows != M or kx != K:
-            raise ValueError(f"x: {M} rows of {K} activations expected, got {rows} of {kx}")
-    dx = _rows_like(M, K, dtype, dev) if want_dx else None
-    db = torch.empty(N, dtype=torch.float32, device=dev) if want_dbias else None
-    dbu = torch.empty(N, dtype=torch.float32, device=dev) if want_dbias and w_up is not None else None
-    dt = _dtype_any(dtype)
-    a = _pack_linear_act_backward(M, N, K, px, ldx, dt_x, x_units, mode, _units(w_units, N, K // UNIT_ELEMS, "w_units"),
-                                  0 if w_up is None else _units(w_up, N, K // UNIT_ELEMS, "w_up_units"), dt,
-                                  _vector(bias, N, dtype, "bias"), _vector(bias_up, N, dtype, "bias_up"), act, pdy, lddy,
-                                  0 if dx is None else dx.data_ptr(), K, 0 if db is None else db.data_ptr(),
-                                  0 if dbu is None else dbu.data_ptr())
-    _run_with_workspace(name, a, (M, N, K, x_units, dt, act == HIF4_ACT_NONE), workspace, dev)
-    return dx, db, dbu
+    if w_up_units is None:
+        raise TypeError("w_up_units: a tensor expected")
+    r = _native.linear_act(x, w_units, w_up_units, bias, bias_up, residual, res_scale, act, -1 if dtype is None else _type_code(dtype),
+                           units, mode, out, workspace)
+    return r if r.__class__ is not int else _result("hif4_gated_linear", r)
 
 
 def hif4_linear_act_backward(dy: torch.Tensor, x: Optional[torch.Tensor], w_units: torch.Tensor,
@@ -626,8 +435,8 @@ def hif4_linear_act_backward(dy: torch.Tensor, x: Optional[torch.Tensor], w_unit
     residual's gradient is res_scale * dy.  x may be None for act = HIF4_ACT_NONE."""
     if stream is not None:
         return _under(stream, hif4_linear_act_backward, locals())
-    dx, db, _ = _linear_act_backward("hif4_linear_act_backward", dy, x, w_units, None, bias, None, act, mode, want_dx, want_dbias,
-                                     workspace)
+    dx, db, _ = _result("hif4_linear_act_backward", _native.linear_act_backward(dy, x, w_units, None, bias, None, act, mode, want_dx,
+                                                                                want_dbias, workspace))
     return dx, db
 
 
@@ -638,8 +447,10 @@ def hif4_gated_linear_backward(dy: torch.Tensor, x: torch.Tensor, w_units: torch
     """(dx, dbias, dbias_up) of hif4_gated_linear from dy (BF16 or FP16); as hif4_linear_act_backward."""
     if stream is not None:
         return _under(stream, hif4_gated_linear_backward, locals())
-    return _linear_act_backward("hif4_gated_linear_backward", dy, x, w_units, w_up_units, bias, bias_up, act, mode, want_dx,
-                                want_dbias, workspace)
+    if w_up_units is None:
+        raise TypeError("w_up_units: a tensor expected")
+    return _result("hif4_gated_linear_backward", _native.linear_act_backward(dy, x, w_units, w_up_units, bias, bias_up, act, mode, want_dx,
+                                                                             want_dbias, workspace))
 
 
 def hif4_debug_wait_timeout(budget_ns: int, stream=None) -> None:

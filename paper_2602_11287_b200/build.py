@@ -11,6 +11,8 @@ ROOT = os.path.dirname(_HERE)
 CSRC = os.path.join(_HERE, "csrc")
 LIB = os.path.join(_HERE, "libhif4.so")
 OBJ_DIR = os.path.join(_HERE, "_build")
+TORCH_SRC = os.path.join(_HERE, "csrc_torch", "hif4_torch.cpp")
+TORCH_LIB = os.path.join(_HERE, "_hif4_torch.so")
 
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
@@ -26,7 +28,7 @@ def _stale(target: str, deps) -> bool:
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
-    """Compile every .cu under csrc/ and link them into libhif4.so; returns its path."""
+    """Compile every .cu under csrc/ and link them into libhif4.so, then the tensor-level calls; returns the library's path."""
     os.makedirs(OBJ_DIR, exist_ok=True)
     sources = sorted(glob.glob(os.path.join(CSRC, "*.cu")))
     headers = sorted(glob.glob(os.path.join(CSRC, "*.cuh"))) + [os.path.join(ROOT, "include", "hif4.h")]
@@ -49,10 +51,31 @@ def build(force: bool = False, verbose: bool = False) -> str:
     if failed:
         raise RuntimeError("nvcc failed")
     if force or procs or _stale(LIB, objs):
-        subprocess.run(["nvcc", "-shared", "-gencode", "arch=compute_100a,code=sm_100a", "-o", LIB + ".tmp", *objs],
-                       check=True)
+        subprocess.run(["nvcc", "-shared", "-gencode", "arch=compute_100a,code=sm_100a", "-Xlinker", "-soname=libhif4.so",
+                        "-o", LIB + ".tmp", *objs], check=True)
         os.replace(LIB + ".tmp", LIB)
+    build_torch_binding(force)
     return LIB
+
+
+def build_torch_binding(force: bool = False) -> str:
+    """Compile the tensor-level calls (csrc_torch/) against the installed PyTorch and libhif4.so; returns the module's path."""
+    if not (force or _stale(TORCH_LIB, [TORCH_SRC, LIB, os.path.join(ROOT, "include", "hif4.h"), __file__])):
+        return TORCH_LIB
+    import sysconfig
+
+    import torch
+    from torch.utils import cpp_extension
+    lib_dir = os.path.join(os.path.dirname(torch.__file__), "lib")
+    cmd = ["g++", "-O2", "-std=c++17", "-shared", "-fPIC", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+           "-I", os.path.join(ROOT, "include"), "-I", sysconfig.get_paths()["include"], "-I", "/usr/local/cuda/include"]
+    for inc in cpp_extension.include_paths():
+        cmd += ["-I", inc]
+    cmd += [TORCH_SRC, LIB, f"-L{lib_dir}", "-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10", "-lc10_cuda",
+            "-Wl,-rpath,$ORIGIN", f"-Wl,-rpath,{lib_dir}", "-o", TORCH_LIB + ".tmp"]
+    subprocess.run(cmd, check=True)
+    os.replace(TORCH_LIB + ".tmp", TORCH_LIB)
+    return TORCH_LIB
 
 
 if __name__ == "__main__":

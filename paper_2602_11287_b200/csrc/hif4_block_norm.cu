@@ -198,6 +198,8 @@ __global__ void __launch_bounds__(kVpt <= 2 ? 320 : 512)
 block_norm_kernel(const NormParams p) {
   __shared__ float red[2][4][32];
   uint32_t slot = 0;
+  grid_launch_next();
+  grid_wait();
   const int64_t row0 = static_cast<int64_t>(blockIdx.x) * p.rows / gridDim.x;
   const int64_t row1 = (static_cast<int64_t>(blockIdx.x) + 1) * p.rows / gridDim.x;
   const T* x = static_cast<const T*>(p.x);
@@ -300,6 +302,8 @@ __global__ void __launch_bounds__(kVpt == 4 ? 1024 : 512)
 block_norm_backward_kernel(const NormGradParams p) {
   __shared__ float red[2][4][32];
   uint32_t slot = 0;
+  grid_launch_next();
+  grid_wait();
   const int64_t row0 = static_cast<int64_t>(blockIdx.x) * p.rows / gridDim.x;
   const int64_t row1 = (static_cast<int64_t>(blockIdx.x) + 1) * p.rows / gridDim.x;
   const float inv_cols = 1.0f / static_cast<float>(p.cols);
@@ -565,9 +569,7 @@ template <typename T, typename W, int kVpt>
 hif4_status launch_norm_bulk(const NormParams& p, int grid, int threads, size_t smem, cudaStream_t st) {
   static uint64_t smem_opt_in = 0;
   if (!ensure_dynamic_smem(block_norm_bulk_kernel<T, W, kVpt>, kRingBytes + 128, smem_opt_in)) return HIF4_ERR_CUDA;
-  block_norm_bulk_kernel<T, W, kVpt><<<grid, threads, smem, st>>>(p);
-  note_launch();
-  return launch_status();
+  return launch_overlapped(block_norm_bulk_kernel<T, W, kVpt>, grid, threads, smem, st, p);
 }
 template <typename T, int kVpt>
 hif4_status launch_norm(NormParams p, bool vec, cudaStream_t st) {
@@ -593,10 +595,8 @@ hif4_status launch_norm(NormParams p, bool vec, cudaStream_t st) {
     }
   }
   const int grid = grid_for(p.rows, threads, kForwardThreadsPerSm);
-  if (vec) block_norm_kernel<T, kVpt, true><<<grid, threads, 0, st>>>(p);
-  else block_norm_kernel<T, kVpt, false><<<grid, threads, 0, st>>>(p);
-  note_launch();
-  return launch_status();
+  if (vec) return launch_overlapped(block_norm_kernel<T, kVpt, true>, grid, threads, 0, st, p);
+  return launch_overlapped(block_norm_kernel<T, kVpt, false>, grid, threads, 0, st, p);
 }
 template <typename T>
 hif4_status launch_norm_t(const NormParams& p, bool vec, cudaStream_t st) {
@@ -612,9 +612,7 @@ template <typename T, typename W, int kVpt, bool kPath>
 hif4_status launch_norm_grad_bulk(const NormGradParams& p, int threads, size_t smem, cudaStream_t st) {
   static uint64_t smem_opt_in = 0;
   if (!ensure_dynamic_smem(block_norm_backward_bulk_kernel<T, W, kVpt, kPath>, kRingBytes + 128, smem_opt_in)) return HIF4_ERR_CUDA;
-  block_norm_backward_bulk_kernel<T, W, kVpt, kPath><<<p.grid, threads, smem, st>>>(p);
-  note_launch();
-  return launch_status();
+  return launch_overlapped(block_norm_backward_bulk_kernel<T, W, kVpt, kPath>, p.grid, threads, smem, st, p);
 }
 template <typename T, int kVpt, bool kPath>
 hif4_status launch_norm_grad(NormGradParams p, bool vec, int threads, cudaStream_t st) {
@@ -629,10 +627,8 @@ hif4_status launch_norm_grad(NormGradParams p, bool vec, int threads, cudaStream
     const size_t smem = 128 + weights + p.stages * stage;
     return wide ? launch_norm_grad_bulk<T, float, kVpt, kPath>(p, threads, smem, st) : launch_norm_grad_bulk<T, T, kVpt, kPath>(p, threads, smem, st);
   }
-  if (vec) block_norm_backward_kernel<T, kVpt, true, kPath><<<p.grid, threads, 0, st>>>(p);
-  else block_norm_backward_kernel<T, kVpt, false, kPath><<<p.grid, threads, 0, st>>>(p);
-  note_launch();
-  return launch_status();
+  if (vec) return launch_overlapped(block_norm_backward_kernel<T, kVpt, true, kPath>, p.grid, threads, 0, st, p);
+  return launch_overlapped(block_norm_backward_kernel<T, kVpt, false, kPath>, p.grid, threads, 0, st, p);
 }
 template <typename T, int kVpt>
 hif4_status launch_norm_grad(const NormGradParams& p, bool vec, int threads, cudaStream_t st) {

@@ -133,6 +133,8 @@ block_norm_bulk_kernel(const NormParams p) {
   __shared__ uint32_t abort_word;
   extern __shared__ __align__(128) uint8_t ring_smem[];
   uint32_t slot = 0;
+  grid_launch_next();
+  grid_wait();
   const int64_t row0 = static_cast<int64_t>(blockIdx.x) * p.rows / gridDim.x;
   const int64_t row1 = (static_cast<int64_t>(blockIdx.x) + 1) * p.rows / gridDim.x;
   const float inv_cols = 1.0f / static_cast<float>(p.cols);
@@ -270,6 +272,8 @@ block_norm_backward_bulk_kernel(const NormGradParams p) {
   __shared__ uint32_t abort_word;
   extern __shared__ __align__(128) uint8_t ring_smem[];
   uint32_t slot = 0;
+  grid_launch_next();
+  grid_wait();
   const int64_t row0 = static_cast<int64_t>(blockIdx.x) * p.rows / gridDim.x;
   const int64_t row1 = (static_cast<int64_t>(blockIdx.x) + 1) * p.rows / gridDim.x;
   const float inv_cols = 1.0f / static_cast<float>(p.cols);

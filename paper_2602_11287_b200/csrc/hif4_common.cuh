@@ -36,6 +36,28 @@ inline bool ensure_dynamic_smem(Kernel kernel, int bytes, uint64_t& done_mask) {
   return true;
 }
 
+// Launch that may begin while the preceding kernel of the stream still runs (if that one says so, or as its last blocks leave):
+// the kernel has to pass griddepcontrol.wait before it touches global memory.
+template <typename... Params, typename... Args>
+inline hif4_status launch_overlapped(void (*kernel)(Params...), unsigned grid, unsigned block, size_t smem, cudaStream_t st, Args... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(grid);
+  cfg.blockDim = dim3(block);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  if (cudaLaunchKernelEx(&cfg, kernel, args...) != cudaSuccess) {
+    (void)cudaGetLastError();
+    return HIF4_ERR_CUDA;
+  }
+  note_launch();
+  return HIF4_OK;
+}
+
 __host__ __device__ inline int64_t ceil_div64(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 }  // namespace hif4

@@ -405,6 +405,7 @@ gemv_kernel(const __grid_constant__ CUtensorMap tm_full, const __grid_constant__
   const int ways = kGemvWarps / npairs;              // >= 1: npairs <= kMaxBlocks
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if constexpr (kEpi != kEpiNone) grid_launch_next();      // the block's next kernel may set itself up as these blocks leave
   if (threadIdx.x == 0) {
     for (int s = 0; s < p.stages; ++s) {
       mbar_init(full + 8 * s, 1);

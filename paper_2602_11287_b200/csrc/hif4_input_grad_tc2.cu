@@ -127,6 +127,8 @@ input_grad_tc2_kernel(const __grid_constant__ CUtensorMap tmZ, const __grid_cons
   cluster_sync_all();            // the peer's barriers are initialised before anyone arrives on them
   tc_fence_after();
   const uint32_t tmem_base = *tmem_ptr_smem;
+  grid_launch_next();
+  grid_wait();                   // (as in the forward kernel)
 
   if (warp == 0) {
     // ---------------------------------------------------------------- raw units
@@ -437,12 +439,9 @@ hif4_status launch_input_grad_t(const InputGradCall& c, void* workspace, cudaStr
   if (p.slices > 1) {
     p.flags = static_cast<unsigned int*>(workspace);
     p.partial = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + pl.flag_bytes);
-    if (cudaMemsetAsync(p.flags, 0, pl.flag_bytes, st) != cudaSuccess) return HIF4_ERR_CUDA;
   }
   const int pairs = p.full_rounds == 0 && p.sk_tiles == 0 ? p.tail_tiles * p.slices : pl.pairs;
-  input_grad_tc2_kernel<T><<<2 * pairs, kGradThreads, kGradSmemBytes, st>>>(tmZ, tmB, tmB2, tmX, p);
-  note_launch();
-  return launch_status();
+  return launch_overlapped(input_grad_tc2_kernel<T>, 2 * pairs, kGradThreads, kGradSmemBytes, st, tmZ, tmB, tmB2, tmX, p);
 }
 
 }  // namespace
@@ -451,6 +450,10 @@ size_t input_grad_tc2_workspace(int64_t M, int64_t N, int64_t K, int phases) {
   if (M <= 0 || N <= 0 || K <= 0) return 0;
   const Tc2Plan pl = grad_plan(M, N, K, phases);
   return pl.slices > 1 ? pl.flag_bytes + partial_tiles(pl) * kPartialTileBytes : 0;
+}
+hif4_status input_grad_tc2_clear(int64_t M, int64_t N, int64_t K, int phases, void* workspace, cudaStream_t st) {
+  const Tc2Plan pl = grad_plan(M, N, K, phases);
+  return pl.slices > 1 && cudaMemsetAsync(workspace, 0, pl.flag_bytes, st) != cudaSuccess ? HIF4_ERR_CUDA : HIF4_OK;
 }
 bool input_grad_tc2_supported(int64_t M, int64_t N, int64_t K, int phases) {
   return M * phases < (1ll << 31) - kPairM && N < (1ll << 29) && K < (1ll << 31) - kPairN &&

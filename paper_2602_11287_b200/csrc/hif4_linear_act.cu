@@ -153,6 +153,8 @@ hif4_status forward(const hif4_linear_act_args* a, bool gated, void* workspace, 
   if (s.stream) {
     pr = launch_linear_gemv(c, a->x_units ? nullptr : a->X, a->dt_x, a->ld_x, ws, st);
   } else {
+    pr = linear_tc2_clear(gated, a->M, a->N, a->K, ws + s.pair, st);
+    if (pr != HIF4_OK) return pr;
     if (!a->x_units) {
       const hif4_status q = hif4_quantize(a->X, a->dt_x, a->M, a->K, a->ld_x, ws + s.x, a->mode, stream);
       if (q != HIF4_OK) return q;
@@ -190,7 +192,13 @@ hif4_status backward(const hif4_linear_act_backward_args* a, bool gated, void* w
   if (!wants_dx && !wants_db) return HIF4_OK;
   float* colsum = wants_db ? reinterpret_cast<float*>(ws + s.colsum) : nullptr;
   __nv_bfloat16* dz = wants_dx && !s.direct ? reinterpret_cast<__nv_bfloat16*>(ws + s.dz) : nullptr;
+  if (wants_dx) {
+    const hif4_status z = input_grad_tc2_clear(a->M, a->N, a->K, s.phases, ws + s.last, st);
+    if (z != HIF4_OK) return z;
+  }
   if (s.recompute) {
+    const hif4_status z = linear_tc2_clear(gated, a->M, a->N, a->K, ws + s.pair, st);
+    if (z != HIF4_OK) return z;
     LinearCall c{};
     c.gated = gated; c.grad = true;
     c.M = a->M; c.N = a->N; c.K = a->K;
@@ -217,13 +225,7 @@ hif4_status backward(const hif4_linear_act_backward_args* a, bool gated, void* w
     note_launch();
     if (cudaGetLastError() != cudaSuccess) return HIF4_ERR_CUDA;
   }
-  if (wants_db) {
-    const dim3 grid(static_cast<unsigned>(ceil_div64(a->N, 32)), gated ? 2u : 1u);
-    column_finish_kernel<<<grid, 1024, 0, st>>>(colsum, ceil_div64(a->M, 32), a->N, a->dbias, gated ? a->dbias_up : nullptr);
-    note_launch();
-    if (cudaGetLastError() != cudaSuccess) return HIF4_ERR_CUDA;
-  }
-  if (!wants_dx) return HIF4_OK;
+  if (wants_dx) {
   InputGradCall g{};
   g.M = a->M; g.N = a->N; g.K = a->K;
   g.dz = s.direct ? a->dY : dz;
@@ -231,7 +233,16 @@ hif4_status backward(const hif4_linear_act_backward_args* a, bool gated, void* w
   g.parts = s.parts;
   g.B = a->W_units; g.B2 = gated ? a->W_up_units : nullptr;
   g.dt = a->dt; g.dx = a->dX; g.ld_dx = a->ld_dx;
-  return launch_input_grad_tc2(g, ws + s.last, st);
+  const hif4_status last = launch_input_grad_tc2(g, ws + s.last, st);
+  if (last != HIF4_OK) return last;
+  }
+  if (wants_db) {
+    const dim3 grid(static_cast<unsigned>(ceil_div64(a->N, 32)), gated ? 2u : 1u);
+    column_finish_kernel<<<grid, 1024, 0, st>>>(colsum, ceil_div64(a->M, 32), a->N, a->dbias, gated ? a->dbias_up : nullptr);
+    note_launch();
+    if (cudaGetLastError() != cudaSuccess) return HIF4_ERR_CUDA;
+  }
+  return HIF4_OK;
 }
 
 hif4_status forward_workspace(const hif4_linear_act_args* a, bool gated, size_t* bytes) {

@@ -58,6 +58,9 @@ struct LinearParams {
 hif4_status launch_linear_gemv(const LinearCall& c, const void* x, int dt_x, int64_t ld_x, void* workspace, cudaStream_t st);
 
 size_t linear_tc2_workspace(bool gated, int64_t M, int64_t N, int64_t K);
+// Zeroes the workspace's counts of finished steps; before the launch of the activations' conversion, so that the product's
+// kernel follows that one directly and can overlap it.
+hif4_status linear_tc2_clear(bool gated, int64_t M, int64_t N, int64_t K, void* workspace, cudaStream_t st);
 bool linear_tc2_supported(bool gated, int64_t M, int64_t N, int64_t K);
 hif4_status launch_linear_tc2(const LinearCall& c, void* workspace, cudaStream_t st);
 hif4_status launch_gated_tc2(const LinearCall& c, void* workspace, cudaStream_t st);
@@ -77,6 +80,7 @@ struct InputGradCall {
   int64_t ld_dx;
 };
 size_t input_grad_tc2_workspace(int64_t M, int64_t N, int64_t K, int phases);
+hif4_status input_grad_tc2_clear(int64_t M, int64_t N, int64_t K, int phases, void* workspace, cudaStream_t st);
 bool input_grad_tc2_supported(int64_t M, int64_t N, int64_t K, int phases);
 hif4_status launch_input_grad_tc2(const InputGradCall& c, void* workspace, cudaStream_t st);
 

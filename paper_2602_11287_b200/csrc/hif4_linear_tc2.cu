@@ -9,6 +9,11 @@ size_t linear_tc2_workspace(bool gated, int64_t M, int64_t N, int64_t K) {
   return pl.slices > 1 ? pl.flag_bytes + partial_tiles(pl) * kPartialTileBytes : 0;
 }
 
+hif4_status linear_tc2_clear(bool gated, int64_t M, int64_t N, int64_t K, void* workspace, cudaStream_t st) {
+  const Tc2Plan pl = tc2_plan(M, N, K, gated ? kPairN / 2 : kPairN);
+  return pl.slices > 1 && cudaMemsetAsync(workspace, 0, pl.flag_bytes, st) != cudaSuccess ? HIF4_ERR_CUDA : HIF4_OK;
+}
+
 bool linear_tc2_supported(bool gated, int64_t M, int64_t N, int64_t K) {
   return M < (1ll << 31) - kPairM && N < (1ll << 31) - kPairN && K < (1ll << 31) &&
          ceil_div64(M, kPairM) * ceil_div64(N, gated ? kPairN / 2 : kPairN) <= 0x7FFFFFFFll;

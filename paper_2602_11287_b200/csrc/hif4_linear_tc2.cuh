@@ -262,6 +262,8 @@ linear_tc2_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
   cluster_sync_all();            // the peer's barriers are initialised before anyone arrives on them
   tc_fence_after();
   const uint32_t tmem_base = *tmem_ptr_smem;
+  grid_launch_next();
+  grid_wait();                   // everything above overlaps the preceding kernel; nothing before this line reads or writes global memory
 
   if (warp == 0) {
     // ---------------------------------------------------------------- producer

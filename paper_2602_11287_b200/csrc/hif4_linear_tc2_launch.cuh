@@ -69,12 +69,9 @@ hif4_status launch_linear_act(const LinearCall& c, void* workspace, cudaStream_t
   if (p.slices > 1) {
     p.flags = static_cast<unsigned int*>(workspace);
     p.partial = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + pl.flag_bytes);
-    if (cudaMemsetAsync(p.flags, 0, pl.flag_bytes, st) != cudaSuccess) return HIF4_ERR_CUDA;
   }
   const int pairs = p.full_rounds == 0 && p.sk_tiles == 0 ? p.tail_tiles * p.slices : pl.pairs;      // a single round: one pair per slice
-  linear_tc2_kernel<kGated, kGrad, T, kAct><<<2 * pairs, kThreads, kLinSmemBytes, st>>>(tmA, tmB, tmB2, tmY, tmSide, p);
-  note_launch();
-  return launch_status();
+  return launch_overlapped(linear_tc2_kernel<kGated, kGrad, T, kAct>, 2 * pairs, kThreads, kLinSmemBytes, st, tmA, tmB, tmB2, tmY, tmSide, p);
 }
 
 template <bool kGated, bool kGrad, typename T>
