@@ -524,28 +524,41 @@ gemv_kernel(const __grid_constant__ CUtensorMap tm_full, const __grid_constant__
 #pragma unroll
       for (int i = 0; i < 4; ++i) mine[4 * t + i] = acc[t][i];
     asm volatile("bar.sync 1, %0;" ::"n"(kGemvWarps * 32) : "memory");     // consumer warps only
-    if (way == 0 && !*abort_flag) {
-      // acc[t]: {row g: tokens 2q, 2q+1; row g+8: tokens 2q, 2q+1} (+ 8 t)
-      const int64_t n0 = (blk_begin + (kEpi == kEpiGated ? 1 : 2) * pair) * kBlockRows + g;
-#pragma unroll
-      for (int t = 0; t < kTokTiles; ++t) {
-        float v[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          v[i] = acc[t][i];
-          for (int k = 1; k < ways; ++k)
-            v[i] += red[(static_cast<size_t>(k * npairs + pair) * 32 + lane) * (4 * kTokTiles) + 4 * t + i];
-        }
-#pragma unroll
-        for (int i = 0; i < (kEpi == kEpiGated ? 2 : 4); ++i) {
+    if constexpr (kEpi != kEpiNone) {
+      // the outputs of a pair go round its warps: an epilogue is some fifty instructions an output
+      constexpr int kOuts = (kEpi == kEpiGated ? 2 : 4) * kTokTiles;
+      if (active && !*abort_flag) {
+        const int64_t n0 = (blk_begin + (kEpi == kEpiGated ? 1 : 2) * pair) * kBlockRows + g;
+        const float* mine_red = red + (static_cast<size_t>(pair) * 32 + lane) * (4 * kTokTiles);
+        const size_t way_step = static_cast<size_t>(npairs) * 32 * (4 * kTokTiles);
+        for (int o = way; o < kOuts; o += ways) {
+          // {row g: tokens 2q, 2q+1; row g+8: tokens 2q, 2q+1} (+ 8 t); gated: row g+8 holds the products with W_up
+          const int t = kEpi == kEpiGated ? o >> 1 : o >> 2, i = kEpi == kEpiGated ? o & 1 : o & 3;
           const int tok = 8 * t + 2 * q + (i & 1);
           const int64_t n = n0 + (i >> 1) * 8;
-          if (tok < p.M && n < p.N && ((i >> 1) == 0 || has_hi)) {
-            if constexpr (kEpi == kEpiNone) p.C[static_cast<int64_t>(tok) * p.ldc + n] = v[i];
-            else finish_output<kEpi>(tail.e, tok, n, v[i], kEpi == kEpiGated ? v[i + 2] : 0.0f);
+          if (tok >= p.M || n >= p.N || ((i >> 1) != 0 && !has_hi)) continue;
+          float z = 0.0f, u = 0.0f;
+          for (int k = 0; k < ways; ++k) {
+            z += mine_red[k * way_step + 4 * t + i];
+            if (kEpi == kEpiGated) u += mine_red[k * way_step + 4 * t + i + 2];
           }
+          finish_output<kEpi>(tail.e, tok, n, z, u);
         }
       }
+    } else if (way == 0 && !*abort_flag) {
+      // acc[t]: {row g: tokens 2q, 2q+1; row g+8: tokens 2q, 2q+1} (+ 8 t)
+      const int64_t n0 = (blk_begin + 2 * pair) * kBlockRows + g;
+#pragma unroll
+      for (int t = 0; t < kTokTiles; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          float v = acc[t][i];
+          for (int k = 1; k < ways; ++k)
+            v += red[(static_cast<size_t>(k * npairs + pair) * 32 + lane) * (4 * kTokTiles) + 4 * t + i];
+          const int tok = 8 * t + 2 * q + (i & 1);
+          const int64_t n = n0 + (i >> 1) * 8;
+          if (tok < p.M && n < p.N && ((i >> 1) == 0 || has_hi)) p.C[static_cast<int64_t>(tok) * p.ldc + n] = v;
+        }
     }
   }
   __syncwarp();

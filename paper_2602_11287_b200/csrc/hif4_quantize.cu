@@ -56,6 +56,8 @@ template <bool kRHA, bool kContig>
 __global__ void __launch_bounds__(kThreads)
 quantize_bf16_kernel(const uint16_t* __restrict__ src, int64_t n_units, int64_t upr, int64_t ld_src,
                      uint32_t* __restrict__ dst) {
+  // a product's kernel may be set up meanwhile; it waits for this grid before it reads the units
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   const int lane = threadIdx.x & 31;
   const int l = lane & 1;
   const int64_t warp = (static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x) >> 5;
@@ -179,6 +181,8 @@ template <bool kRHA, bool kContig, typename Src>
 __global__ void __launch_bounds__(kThreads)
 quantize_fp32_kernel(const Src* __restrict__ src, int64_t n_units, int64_t upr, int64_t ld_src,
                      uint32_t* __restrict__ dst) {
+  // a product's kernel may be set up meanwhile; it waits for this grid before it reads the units
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   const int lane = threadIdx.x & 31;
   const int l = lane & 3;
   const int64_t warp = (static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x) >> 5;
