@@ -275,7 +275,7 @@ typedef struct {
   int64_t ld_dresidual;
   void* dgate;                   /* [ceil(rows / rows_per_gate), cols] of dt, contiguous, or NULL              */
   float* dpre_weight;            /* [cols] or NULL                                                             */
-  float* dpre_bias;
+  float* dpre_bias;              /* [cols] or NULL (LAYER only)                                                */
   float* dpost_weight;
 } hif4_block_norm_backward_args;
 hif4_status hif4_block_norm_backward_workspace(int64_t rows, int64_t cols, size_t* bytes);

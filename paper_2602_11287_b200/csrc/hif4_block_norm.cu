@@ -44,7 +44,7 @@ struct NormGradParams {
   int64_t ld_dx, ld_dresidual;
   float *dpre_weight, *dpre_bias, *dpost_weight;
   float* partial;           // [5][grid][cols]: dpre_weight, dpre_bias, dpost_weight, first and last group of gates of each block
-  int grid;
+  int grid, light;
   int strided;
   int stages;
   unsigned int* error_word;
@@ -511,7 +511,7 @@ norm_grad_finish_kernel(const NormGradParams p, int by_group) {
 // ------------------------------------------------------------------------------------------------------- host side
 // Groups of eight columns per thread.  Forward: two while 320 threads reach the row's end (8192 x 5120, two blocks an SM:
 // 63 us; one group 78 us, four 68 us), more beyond.  Backward: the column sums take 32 registers a group, so one while
-// 512 threads reach (4000 x 4096: 81 us, two groups 87 us).
+// 512 threads reach (4000 x 4096 with post norm and gates: 69 us, two groups 70 us and more spills beyond).
 int groups_forward(int64_t cols) { return cols <= 1024 ? 1 : cols <= 5120 ? 2 : cols <= 16384 ? 4 : 8; }
 int groups_backward(int64_t cols) { return cols <= 4096 ? 1 : cols <= 8192 ? 2 : 4; }
 int threads_for(int64_t cols, int vpt) {
@@ -608,24 +608,28 @@ hif4_status launch_norm_t(const NormParams& p, bool vec, cudaStream_t st) {
   }
 }
 
-template <typename T, typename W, int kVpt, bool kPath>
+template <typename T, typename W, int kVpt, bool kPath, bool kLayer>
 hif4_status launch_norm_grad_bulk(const NormGradParams& p, int threads, size_t smem, cudaStream_t st) {
   static uint64_t smem_opt_in = 0;
-  if (!ensure_dynamic_smem(block_norm_backward_bulk_kernel<T, W, kVpt, kPath>, kRingBytes + 128, smem_opt_in)) return HIF4_ERR_CUDA;
-  return launch_overlapped(block_norm_backward_bulk_kernel<T, W, kVpt, kPath>, p.grid, threads, smem, st, p);
+  if (!ensure_dynamic_smem(block_norm_backward_bulk_kernel<T, W, kVpt, kPath, kLayer>, kRingBytes + 128, smem_opt_in)) return HIF4_ERR_CUDA;
+  return launch_overlapped(block_norm_backward_bulk_kernel<T, W, kVpt, kPath, kLayer>, p.grid, threads, smem, st, p);
 }
 template <typename T, int kVpt, bool kPath>
 hif4_status launch_norm_grad(NormGradParams p, bool vec, int threads, cudaStream_t st) {
   const bool wide = p.dt_w == HIF4_FP32;
   const int mats = (p.dy ? 2 : 0) + (p.dh ? 1 : 0) + (kPath && p.x ? 1 : 0);
   const size_t stage = static_cast<size_t>(p.cols) * sizeof(T) * mats;
-  const size_t weights = static_cast<size_t>(p.cols) * type_size(p.dt_w) * ((p.dy ? 1 : 0) + (p.kind_post != HIF4_NORM_NONE ? 1 : 0));
-  p.stages = vec && (wide || p.dt_w == type_of<T>()) ? ring_stages(p.rows, p.grid, blocks_per_sm(threads, kBackwardThreadsPerSm), stage, weights) : 0;
+  const size_t weights = static_cast<size_t>(p.cols) * (type_size(p.dt_w) * ((p.dy ? 1 : 0) + (p.kind_post != HIF4_NORM_NONE ? 1 : 0)) +
+                                                        (p.gate && p.kind_post != HIF4_NORM_NONE ? 4 : 0));      // and the post weight's sums
+  p.stages = vec && (wide || p.dt_w == type_of<T>()) ? ring_stages(p.rows, p.grid, blocks_per_sm(threads, p.light && kVpt == 1 ? 2 * kBackwardThreadsPerSm : kBackwardThreadsPerSm), stage, weights) : 0;
   if (p.stages > 0) {
     p.error_word = device_error_word();
     if (!p.error_word) return HIF4_ERR_CUDA;
     const size_t smem = 128 + weights + p.stages * stage;
-    return wide ? launch_norm_grad_bulk<T, float, kVpt, kPath>(p, threads, smem, st) : launch_norm_grad_bulk<T, T, kVpt, kPath>(p, threads, smem, st);
+    // (dbias of an RMS norm is refused, so only a LAYER norm has one)
+    const bool layer = p.kind_pre == HIF4_NORM_LAYER || p.kind_post == HIF4_NORM_LAYER;
+    if (layer) return wide ? launch_norm_grad_bulk<T, float, kVpt, kPath, true>(p, threads, smem, st) : launch_norm_grad_bulk<T, T, kVpt, kPath, true>(p, threads, smem, st);
+    return wide ? launch_norm_grad_bulk<T, float, kVpt, kPath, false>(p, threads, smem, st) : launch_norm_grad_bulk<T, T, kVpt, kPath, false>(p, threads, smem, st);
   }
   if (vec) return launch_overlapped(block_norm_backward_kernel<T, kVpt, true, kPath>, p.grid, threads, 0, st, p);
   return launch_overlapped(block_norm_backward_kernel<T, kVpt, false, kPath>, p.grid, threads, 0, st, p);
@@ -654,8 +658,11 @@ hif4_status launch_norm_grad_t(const NormGradParams& p, bool vec, cudaStream_t s
   return launch_status();
 }
 
-int backward_grid(int64_t rows, int64_t cols) {
-  return grid_for(rows, threads_for(cols, groups_backward(cols)), kBackwardThreadsPerSm);
+// Blocks of the backward pass.  `light`: RMS norm alone, whose 61 registers a thread (one group) let twice the threads run
+// (8192 x 4096: 76 us with one block an SM).
+int backward_grid(int64_t rows, int64_t cols, bool light) {
+  const int vpt = groups_backward(cols);
+  return grid_for(rows, threads_for(cols, vpt), light && vpt == 1 ? 2 * kBackwardThreadsPerSm : kBackwardThreadsPerSm);
 }
 
 }  // namespace
@@ -703,7 +710,7 @@ extern "C" hif4_status hif4_block_norm(const hif4_block_norm_args* a, void* stre
 extern "C" hif4_status hif4_block_norm_backward_workspace(int64_t rows, int64_t cols, size_t* bytes) {
   if (!bytes) return HIF4_ERR_NULL;
   if (rows < 0 || cols < 0 || cols > kNormMaxCols) return HIF4_ERR_SHAPE;
-  *bytes = rows == 0 || cols == 0 ? 0 : static_cast<size_t>(5) * backward_grid(rows, cols) * cols * sizeof(float);
+  *bytes = rows == 0 || cols == 0 ? 0 : static_cast<size_t>(5) * backward_grid(rows, cols, true) * cols * sizeof(float);
   return HIF4_OK;
 }
 
@@ -715,7 +722,7 @@ extern "C" hif4_status hif4_block_norm_backward(const hif4_block_norm_backward_a
   const hif4_status ws = hif4_block_norm_backward_workspace(a->rows, a->cols, &need);
   if (ws != HIF4_OK) return ws;
   if ((a->gate && a->rows_per_gate < 1) || !(a->eps >= 0.0f) || (a->dy && a->pre == HIF4_NORM_NONE) ||
-      (a->dpost_weight && a->post == HIF4_NORM_NONE))
+      (a->dpost_weight && a->post == HIF4_NORM_NONE) || (a->dpre_bias && a->pre != HIF4_NORM_LAYER))
     return HIF4_ERR_SHAPE;
   const bool wants_x = a->post != HIF4_NORM_NONE || a->dgate;
   const size_t vec_bytes = static_cast<size_t>(a->cols) * sizeof(float);
@@ -751,7 +758,8 @@ extern "C" hif4_status hif4_block_norm_backward(const hif4_block_norm_backward_a
   p.dx = a->dx; p.dresidual = a->dresidual; p.dgate = a->dgate; p.ld_dx = a->ld_dx; p.ld_dresidual = a->ld_dresidual;
   p.dpre_weight = a->dpre_weight; p.dpre_bias = a->dpre_bias; p.dpost_weight = a->dpost_weight;
   p.partial = static_cast<float*>(workspace);
-  p.grid = backward_grid(a->rows, a->cols);
+  p.light = a->post == HIF4_NORM_NONE && !a->gate && a->pre != HIF4_NORM_LAYER;
+  p.grid = backward_grid(a->rows, a->cols, p.light);
   p.strided = a->cols % 8 != 0;
   if (a->dt == HIF4_BF16) return launch_norm_grad_t<__nv_bfloat16>(p, vec, st);
   if (a->dt == HIF4_FP16) return launch_norm_grad_t<__half>(p, vec, st);

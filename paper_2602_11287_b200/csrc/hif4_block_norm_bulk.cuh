@@ -265,7 +265,10 @@ block_norm_bulk_kernel(const NormParams p) {
   ring.finish(&abort_word, p.error_word);
 }
 
-template <typename T, typename W, int kVpt, bool kPath>
+// Gradients.  One sum over the rows, S = sum dt xhat(x) within a row of gates, gives both gradients that the path to x has:
+// dgate = S wp and dwp = sum over the rows of gates gate S; the latter is kept in shared memory, since it only changes where the
+// gates do.  kLayer: one of the norms is a LAYER norm (the RMS form has no means, no bias and fewer registers to carry).
+template <typename T, typename W, int kVpt, bool kPath, bool kLayer>
 __global__ void __launch_bounds__(kVpt == 4 ? 1024 : 512)
 block_norm_backward_bulk_kernel(const NormGradParams p) {
   __shared__ float red[2][4][32];
@@ -277,31 +280,35 @@ block_norm_backward_bulk_kernel(const NormGradParams p) {
   const int64_t row0 = static_cast<int64_t>(blockIdx.x) * p.rows / gridDim.x;
   const int64_t row1 = (static_cast<int64_t>(blockIdx.x) + 1) * p.rows / gridDim.x;
   const float inv_cols = 1.0f / static_cast<float>(p.cols);
-  const bool pre_layer = p.kind_pre == HIF4_NORM_LAYER, post_layer = p.kind_post == HIF4_NORM_LAYER;
+  const bool pre_layer = kLayer && p.kind_pre == HIF4_NORM_LAYER, post_layer = kLayer && p.kind_post == HIF4_NORM_LAYER;
   const bool post = kPath && p.kind_post != HIF4_NORM_NONE, has_dy = p.dy != nullptr, has_dh = p.dh != nullptr, has_x = kPath && p.x;
+  const bool has_gate = kPath && p.gate, sums_dwp = post && has_gate;
   const Groups<kVpt> g(p.cols);
-  constexpr int kPathVpt = kPath ? kVpt : 1;
-  Pairs dw[kVpt], db[kVpt], dwp[kPathVpt], dg[kPathVpt];
+  constexpr int kPathVpt = kPath ? kVpt : 1, kLayerVpt = kLayer ? kVpt : 1;
+  Pairs dw[kVpt], db[kLayerVpt], S[kPathVpt];
 #pragma unroll
   for (int i = 0; i < kVpt; ++i) {
-    dw[i] = db[i] = pairs_filled(0.0f);
-    if (kPath) dwp[i] = dg[i] = pairs_filled(0.0f);
+    dw[i] = pairs_filled(0.0f);
+    if (kLayer) db[i] = pairs_filled(0.0f);
+    if (kPath) S[i] = pairs_filled(0.0f);
   }
   const uint32_t wb = static_cast<uint32_t>(p.cols) * sizeof(W);
-  const uint32_t sm_pre = smem_u32(ring_smem), sm_post = sm_pre + (has_dy ? wb : 0u);
+  const uint32_t sm_pre = smem_u32(ring_smem), sm_post = sm_pre + (has_dy ? wb : 0u), sm_dwp = sm_post + (post ? wb : 0u);
   if (has_dy) stage_vector<W>(p.pre_weight, sm_pre, p.cols, 1.0f);
   if (post) stage_vector<W>(p.post_weight, sm_post, p.cols, 1.0f);
+  if (sums_dwp) stage_vector<float>(nullptr, sm_dwp, p.cols, 0.0f);
   if (threadIdx.x == 0) abort_word = 0u;
   RowRing<T, 4> ring{{has_dy ? static_cast<const T*>(p.h) : nullptr, static_cast<const T*>(p.dy), static_cast<const T*>(p.dh),
                       has_x ? static_cast<const T*>(p.x) : nullptr},
                      {p.ld_h, p.ld_dy, p.ld_dh, p.ld_x}};
-  ring.start(sm_post + (post ? wb : 0u), p.stages, p.cols, row0, row1);
+  ring.start(sm_dwp + (sums_dwp ? static_cast<uint32_t>(p.cols) * 4u : 0u), p.stages, p.cols, row0, row1);
   T* dx = p.dx ? static_cast<T*>(p.dx) + row0 * p.ld_dx : nullptr;
   T* dres = p.dresidual ? static_cast<T*>(p.dresidual) + row0 * p.ld_dresidual : nullptr;
   Raw8<T> gr[kPathVpt];
-  int64_t group = kPath && p.gate ? row0 / p.rows_per_gate : 0, gate_end = row0;
+  int64_t group = has_gate ? row0 / p.rows_per_gate : 0;
+  int64_t gate_end = has_gate ? group * p.rows_per_gate : row1 + 1;      // first row of the next gates; the first row loads its own
   for (int64_t row = row0; row < row1; ++row) {
-    if (kPath && p.gate && row == gate_end) {
+    if (kPath && has_gate && (row >= gate_end || row == row0)) {
       if (row != row0) ++group;
       gate_end = (group + 1) * p.rows_per_gate;
       if (gate_end > p.rows) gate_end = p.rows;
@@ -316,6 +323,9 @@ block_norm_backward_bulk_kernel(const NormGradParams p) {
       for (int i = 0; i < kVpt; ++i) {
         a[i] = pairs_of(lds_group<T>(ring.at(0) + g.col[i] * sizeof(T)));
         dy[i] = lds_group<T>(ring.at(1) + g.col[i] * sizeof(T));
+        const Pairs w = pairs_of(lds_group<W>(sm_pre + g.col[i] * sizeof(W))), d = pairs_of(dy[i]);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) dn[i].p[j] = mul2(d.p[j], w.p[j]);
       }
     } else {
 #pragma unroll
@@ -336,13 +346,11 @@ block_norm_backward_bulk_kernel(const NormGradParams p) {
       for (int i = 0; i < kVpt; ++i) x[i] = has_x ? pairs_of(lds_group<T>(ring.at(3) + g.col[i] * sizeof(T))) : pairs_filled(0.0f);
     }
     fence_proxy_async_smem();              // these reads before the async proxy writes the stage again
-    bool refilled = false;
-    if (pre_layer || post_layer) {
+    if constexpr (kLayer) {
       float s[2] = {g.sum([&](int i, int j, float2 c) { return add2(c, a[i].p[j]); }), 0.0f};
       if constexpr (kPath) s[1] = g.sum([&](int i, int j, float2 c) { return add2(c, x[i].p[j]); });
       block_sums_synced(s, red, slot);
       ring.refill(&abort_word);
-      refilled = true;
       const float2 m = both(pre_layer ? -s[0] * inv_cols : 0.0f), mx = both(post_layer ? -s[1] * inv_cols : 0.0f);
 #pragma unroll
       for (int i = 0; i < kVpt; ++i)
@@ -352,32 +360,26 @@ block_norm_backward_bulk_kernel(const NormGradParams p) {
           if constexpr (kPath) x[i].p[j] = add2(x[i].p[j], mx);
         }
     }
-    if (has_dy) {
-#pragma unroll
-      for (int i = 0; i < kVpt; ++i) {
-        const Pairs w = pairs_of(lds_group<W>(sm_pre + g.col[i] * sizeof(W))), d = pairs_of(dy[i]);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) dn[i].p[j] = mul2(d.p[j], w.p[j]);
-      }
-    }
     // sums over the row: (h - mean)^2, dn (h - mean), (x - mean_x)^2, dn
     float s2[4];
     s2[0] = g.sum([&](int i, int j, float2 c) { return fma2(a[i].p[j], a[i].p[j], c); });
     s2[1] = g.sum([&](int i, int j, float2 c) { return fma2(dn[i].p[j], a[i].p[j], c); });
-    s2[2] = 0.0f;
-    if constexpr (kPath) s2[2] = g.sum([&](int i, int j, float2 c) { return fma2(x[i].p[j], x[i].p[j], c); });
-    s2[3] = pre_layer ? g.sum([&](int i, int j, float2 c) { return add2(c, dn[i].p[j]); }) : 0.0f;
-    if (kPath || pre_layer) {
+    s2[2] = s2[3] = 0.0f;
+    if constexpr (kPath) {
+      if (post) s2[2] = g.sum([&](int i, int j, float2 c) { return fma2(x[i].p[j], x[i].p[j], c); });
+    }
+    if constexpr (kLayer) s2[3] = g.sum([&](int i, int j, float2 c) { return add2(c, dn[i].p[j]); });
+    if constexpr (kPath || kLayer) {
       block_sums_synced(s2, red, slot);
     } else {
       float s[2] = {s2[0], s2[1]};
       block_sums_synced(s, red, slot);
       s2[0] = s[0]; s2[1] = s[1];
     }
-    if (!refilled) ring.refill(&abort_word);
+    if constexpr (!kLayer) ring.refill(&abort_word);
     const float rstd = rsqrtf(fmaf(s2[0], inv_cols, p.eps));
     if (has_dy) {
-      const float2 r2 = both(rstd), m1 = both(-s2[1] * rstd * inv_cols), m0 = both(pre_layer ? -s2[3] * inv_cols : 0.0f);
+      const float2 r2 = both(rstd), m1 = both(-s2[1] * rstd * inv_cols);
 #pragma unroll
       for (int i = 0; i < kVpt; ++i) {
         const Pairs d = pairs_of(dy[i]);
@@ -387,8 +389,8 @@ block_norm_backward_bulk_kernel(const NormGradParams p) {
           dw[i].p[j] = fma2(d.p[j], n, dw[i].p[j]);
           t[i].p[j] = fma2(r2, fma2(n, m1, dn[i].p[j]), t[i].p[j]);
         }
-        if (pre_layer) {
-          const float2 shift = mul2(r2, m0);
+        if constexpr (kLayer) {
+          const float2 shift = both(pre_layer ? -rstd * s2[3] * inv_cols : 0.0f);
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
             db[i].p[j] = add2(db[i].p[j], d.p[j]);
@@ -409,31 +411,43 @@ block_norm_backward_bulk_kernel(const NormGradParams p) {
       dres += p.ld_dresidual;
     }
     if constexpr (kPath) {
-      const float rstd_x = post ? rsqrtf(fmaf(s2[2], inv_cols, p.eps)) : 1.0f;
-      const float2 rx = both(rstd_x);
       if (post) {
+        const float2 rx = both(rsqrtf(fmaf(s2[2], inv_cols, p.eps)));
 #pragma unroll
         for (int i = 0; i < kVpt; ++i) {
           const Pairs wp = pairs_of(lds_group<W>(sm_post + g.col[i] * sizeof(W)));
-          const Pairs gate = p.gate ? pairs_of(gr[i]) : pairs_filled(1.0f);
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
-            const float2 xn = mul2(x[i].p[j], rx), dp = mul2(t[i].p[j], gate.p[j]);
-            dg[i].p[j] = fma2(t[i].p[j], mul2(xn, wp.p[j]), dg[i].p[j]);
-            dwp[i].p[j] = fma2(dp, xn, dwp[i].p[j]);
+            const float2 xn = mul2(x[i].p[j], rx);
+            S[i].p[j] = fma2(t[i].p[j], xn, S[i].p[j]);
             x[i].p[j] = xn;
-            t[i].p[j] = mul2(dp, wp.p[j]);
+            t[i].p[j] = mul2(t[i].p[j], wp.p[j]);
+          }
+          if (has_gate) {
+            const Pairs gate = pairs_of(gr[i]);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) t[i].p[j] = mul2(t[i].p[j], gate.p[j]);
           }
         }
         if (dx) {
-          float s3[2] = {g.sum([&](int i, int j, float2 c) { return fma2(t[i].p[j], x[i].p[j], c); }),
-                         post_layer ? g.sum([&](int i, int j, float2 c) { return add2(c, t[i].p[j]); }) : 0.0f};
-          block_sums_synced(s3, red, slot);
-          const float2 q1 = both(-s3[0] * inv_cols), q0 = both(-s3[1] * inv_cols);
+          float s3[2] = {g.sum([&](int i, int j, float2 c) { return fma2(t[i].p[j], x[i].p[j], c); }), 0.0f};
+          if constexpr (kLayer) {
+            s3[1] = g.sum([&](int i, int j, float2 c) { return add2(c, t[i].p[j]); });
+            block_sums_synced(s3, red, slot);
+          } else {
+            float s1[1] = {s3[0]};
+            block_sums_synced(s1, red, slot);
+            s3[0] = s1[0];
+          }
+          const float2 q1 = both(-s3[0] * inv_cols), q0 = both(post_layer ? -s3[1] * inv_cols : 0.0f);
 #pragma unroll
           for (int i = 0; i < kVpt; ++i)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) t[i].p[j] = mul2(rx, add2(fma2(x[i].p[j], q1, t[i].p[j]), q0));
+            for (int j = 0; j < 4; ++j) {
+              float2 d = fma2(x[i].p[j], q1, t[i].p[j]);
+              if constexpr (kLayer) d = add2(d, q0);
+              t[i].p[j] = mul2(rx, d);
+            }
         }
       } else {                             // a gate without a norm
 #pragma unroll
@@ -441,7 +455,7 @@ block_norm_backward_bulk_kernel(const NormGradParams p) {
           const Pairs gate = pairs_of(gr[i]);
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
-            dg[i].p[j] = fma2(t[i].p[j], x[i].p[j], dg[i].p[j]);
+            S[i].p[j] = fma2(t[i].p[j], x[i].p[j], S[i].p[j]);
             t[i].p[j] = mul2(t[i].p[j], gate.p[j]);
           }
         }
@@ -453,16 +467,36 @@ block_norm_backward_bulk_kernel(const NormGradParams p) {
         if (g.in[i]) store8(dx + g.col[i], raw_of<T>(t[i]));
       dx += p.ld_dx;
     }
-    if (kPath && p.dgate && (row + 1 == gate_end || row + 1 == row1)) {
-      const bool starts_here = group * p.rows_per_gate >= row0, ends_here = row + 1 == gate_end;
-      float* part = p.partial + (static_cast<int64_t>(starts_here ? 4 : 3) * gridDim.x + blockIdx.x) * p.cols;
+    if constexpr (kPath) {
+      if (has_gate && (row + 1 == gate_end || row + 1 == row1)) {      // these gates' rows, or the block's, end here
+        const bool starts_here = group * p.rows_per_gate >= row0, ends_here = row + 1 == gate_end;
+        float* part = p.partial + (static_cast<int64_t>(starts_here ? 4 : 3) * gridDim.x + blockIdx.x) * p.cols;
 #pragma unroll
-      for (int i = 0; i < kVpt; ++i) {
-        if (g.in[i]) {
-          if (starts_here && ends_here) store8(static_cast<T*>(p.dgate) + group * p.cols + g.col[i], raw_of<T>(dg[i]));
-          else store8(part + g.col[i], raw_of<float>(dg[i]));
+        for (int i = 0; i < kVpt; ++i) {
+          if (g.in[i]) {
+            if (p.dgate) {
+              Pairs d = S[i];
+              if (post) {
+                const Pairs wp = pairs_of(lds_group<W>(sm_post + g.col[i] * sizeof(W)));
+#pragma unroll
+                for (int j = 0; j < 4; ++j) d.p[j] = mul2(d.p[j], wp.p[j]);
+              }
+              if (starts_here && ends_here) store8(static_cast<T*>(p.dgate) + group * p.cols + g.col[i], raw_of<T>(d));
+              else store8(part + g.col[i], raw_of<float>(d));
+            }
+            if (sums_dwp) {
+              const uint32_t at = sm_dwp + g.col[i] * 4u;
+              const Pairs gate = pairs_of(gr[i]), old = pairs_of(lds_group<float>(at));
+              Pairs now;
+#pragma unroll
+              for (int j = 0; j < 4; ++j) now.p[j] = fma2(gate.p[j], S[i].p[j], old.p[j]);
+              const Raw8<float> r = raw_of<float>(now);
+              sts128(at, r.a.x, r.a.y, r.a.z, r.a.w);
+              sts128(at + 16, r.b.x, r.b.y, r.b.z, r.b.w);
+            }
+          }
+          S[i] = pairs_filled(0.0f);
         }
-        dg[i] = pairs_filled(0.0f);
       }
     }
   }
@@ -472,8 +506,10 @@ block_norm_backward_bulk_kernel(const NormGradParams p) {
   for (int i = 0; i < kVpt; ++i) {
     if (!g.in[i]) continue;
     if (p.dpre_weight) store8(part + g.col[i], raw_of<float>(dw[i]));
-    if (p.dpre_bias) store8(part + plane + g.col[i], raw_of<float>(db[i]));
-    if (kPath && p.dpost_weight) store8(part + 2 * plane + g.col[i], raw_of<float>(dwp[i]));
+    if (p.dpre_bias) store8(part + plane + g.col[i], kLayer ? raw_of<float>(db[kLayer ? i : 0]) : raw_of<float>(pairs_filled(0.0f)));
+    if constexpr (kPath) {
+      if (p.dpost_weight) store8(part + 2 * plane + g.col[i], sums_dwp ? lds_group<float>(sm_dwp + g.col[i] * 4u) : raw_of<float>(S[i]));
+    }
   }
   ring.finish(&abort_word, p.error_word);
 }

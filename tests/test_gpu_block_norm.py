@@ -297,6 +297,7 @@ def test_refusals(hif4):
     assert code(lambda: hif4.hif4_block_norm_backward(x, None, w)) == 1
     assert code(lambda: hif4.hif4_block_norm_backward(x, x, w, post=1, post_weight=w)) == 1           # x is missing
     assert code(lambda: hif4.hif4_block_norm_backward(x, x, w, post_weight=w)) == 2                   # weight of no norm
+    assert code(lambda: hif4.hif4_block_norm_backward(x, x, w, bias=True)) == 2                       # bias of an RMS norm
     assert code(lambda: hif4.hif4_block_norm_backward(x, x, w, workspace=torch.empty(256, dtype=torch.uint8, device="cuda"))) == 5
     for bad in (lambda: hif4.hif4_block_norm(x, w[:100]), lambda: hif4.hif4_block_norm(x, w, residual=x[:2]),
                 lambda: hif4.hif4_block_norm(x, w, residual=x.float()), lambda: hif4.hif4_block_norm(x, w, gate=x[:1]),
