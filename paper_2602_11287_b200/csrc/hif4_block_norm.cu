@@ -4,7 +4,8 @@
 // 16-bit matrix being written.  Bound by HBM traffic (forward 6.6 - 8 bytes an element in 16 bits, backward 12).
 //
 // Instructions are the next bound after the loads, so the arithmetic runs in packed FP32 pairs.
-// A thread owns groups of eight columns (16-byte accesses when the matrices allow them).  Blocks take contiguous runs
+// A thread owns groups of eight columns (16-byte accesses when the matrices allow them; rows at odd addresses are read in
+// 16-byte words and shifted).  Blocks take contiguous runs
 // of rows and keep the next row's loads in flight while they reduce the current one; weights and gates are re-read
 // per row, from L1 after a block's first row.
 #include "hif4_common.cuh"
@@ -27,7 +28,6 @@ struct NormParams {
   void *h, *y;
   int64_t ld_h, ld_y;
   int units, rha;
-  int strided;              // element-wise access: element j of a group is column base + j * blockDim.x
   int stages;               // ring depth of the bulk form
   unsigned int* error_word;
 };
@@ -45,52 +45,85 @@ struct NormGradParams {
   float *dpre_weight, *dpre_bias, *dpost_weight;
   float* partial;           // [5][grid][cols]: dpre_weight, dpre_bias, dpost_weight, first and last group of gates of each block
   int grid, light;
-  int strided;
   int stages;
   unsigned int* error_word;
 };
 
-// Columns of a thread's group i: eight consecutive ones, or (element-wise access of rows that are not cut into groups
-// of eight) one in every blockDim.x, so that the lanes of a warp still touch neighbouring elements.
+// Columns of a thread's group i: base .. base + 7.
 struct Cols {
-  int base, step;
-  __device__ __forceinline__ Cols(int i, int strided) {
-    const int t = i * static_cast<int>(blockDim.x);
-    base = strided ? 8 * t + static_cast<int>(threadIdx.x) : 8 * (t + static_cast<int>(threadIdx.x));
-    step = strided ? static_cast<int>(blockDim.x) : 1;
-  }
+  int base;
+  __device__ __forceinline__ explicit Cols(int i) { base = 8 * (i * static_cast<int>(blockDim.x) + static_cast<int>(threadIdx.x)); }
 };
 
+// Eight 16-bit elements from two neighbouring 16-byte words of which they take bytes o .. o + 15 (o even, the same for all
+// threads of a row).
+__device__ __forceinline__ uint4 take16(const uint4& a, const uint4& b, uint32_t o) {
+  uint32_t w[5];
+  switch (o >> 2) {
+    case 0: w[0] = a.x; w[1] = a.y; w[2] = a.z; w[3] = a.w; w[4] = b.x; break;
+    case 1: w[0] = a.y; w[1] = a.z; w[2] = a.w; w[3] = b.x; w[4] = b.y; break;
+    case 2: w[0] = a.z; w[1] = a.w; w[2] = b.x; w[3] = b.y; w[4] = b.z; break;
+    default: w[0] = a.w; w[1] = b.x; w[2] = b.y; w[3] = b.z; w[4] = b.w; break;
+  }
+  const uint32_t s = (o & 2u) * 8u;
+  return make_uint4(__funnelshift_r(w[0], w[1], s), __funnelshift_r(w[1], w[2], s), __funnelshift_r(w[2], w[3], s), __funnelshift_r(w[3], w[4], s));
+}
+// A group of a row of any alignment: 16-byte loads, one or two of them, wherever those stay inside the row.
 template <bool kVec, typename T>
 __device__ __forceinline__ Raw8<T> load_group(const T* row, const Cols& c, int cols) {
   Raw8<T> r;
   zero8(r);
   if (kVec) {
     if (c.base < cols) r = load8(row + c.base);
-  } else {
-    float v[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const int e = c.base + j * c.step;
-      v[j] = e < cols ? to_f32(row[e]) : 0.0f;
-    }
-    r = pack8<T>(v);                                     // exact: the values come from T
+    return r;
   }
-  return r;
+  const uint32_t o = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(row)) & 15u;
+  if (o == 0u && c.base + 8 <= cols) return load8(row + c.base);
+  if constexpr (sizeof(T) == 2) {
+    if (c.base >= 8 && c.base + 16 <= cols) {
+      const uint4* p = reinterpret_cast<const uint4*>(reinterpret_cast<const uint8_t*>(row + c.base) - o);
+      r.a = take16(p[0], p[1], o);
+      return r;
+    }
+  }
+  float v[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) v[j] = c.base + j < cols ? to_f32(row[c.base + j]) : 0.0f;
+  return pack8<T>(v);                                      // exact: the values come from T
 }
+// The same for stores: 16-byte ones where the row allows them, else 4-byte ones with single elements at the odd ends.
 template <bool kVec, typename T>
 __device__ __forceinline__ void store_group(T* row, const Cols& c, int cols, const Raw8<T>& r) {
   if (kVec) {
     if (c.base < cols) store8(row + c.base, r);
-  } else {
-    float v[8];
-    unpack8(r, v);
+    return;
+  }
+  const uint32_t o = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(row)) & 15u;
+  if (c.base + 8 <= cols) {
+    if (o == 0u) {
+      store8(row + c.base, r);
+      return;
+    }
+    if constexpr (sizeof(T) == 2) {
+      const uint32_t w[4] = {r.a.x, r.a.y, r.a.z, r.a.w};
+      uint16_t* d = reinterpret_cast<uint16_t*>(row + c.base);
+      if ((o & 2u) == 0u) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const int e = c.base + j * c.step;
-      if (e < cols) row[e] = from_f32<T>(v[j]);
+        for (int k = 0; k < 4; ++k) reinterpret_cast<uint32_t*>(d)[k] = w[k];
+      } else {
+        d[0] = static_cast<uint16_t>(w[0]);
+#pragma unroll
+        for (int k = 0; k < 3; ++k) reinterpret_cast<uint32_t*>(d + 1)[k] = __funnelshift_r(w[k], w[k + 1], 16);
+        d[7] = static_cast<uint16_t>(w[3] >> 16);
+      }
+      return;
     }
   }
+  float v[8];
+  unpack8(r, v);
+#pragma unroll
+  for (int j = 0; j < 8; ++j)
+    if (c.base + j < cols) row[c.base + j] = from_f32<T>(v[j]);
 }
 // Column sums of a group to an FP32 row of the workspace (16-byte aligned where the columns come in groups).
 template <bool kVec>
@@ -148,11 +181,10 @@ __device__ __forceinline__ void block_sums_synced(float (&v)[kN], float (*red)[4
 // are zeros and have to stay that.
 template <bool kVec>
 __device__ __forceinline__ Pairs centre(float mean, const Cols& c, int cols) {
-  if (kVec) return pairs_filled(c.base < cols ? mean : 0.0f);
+  if (kVec || c.base + 8 <= cols || c.base >= cols) return pairs_filled(c.base < cols ? mean : 0.0f);
   Pairs m;
 #pragma unroll
-  for (int j = 0; j < 4; ++j)
-    m.p[j] = make_float2(c.base + 2 * j * c.step < cols ? mean : 0.0f, c.base + (2 * j + 1) * c.step < cols ? mean : 0.0f);
+  for (int j = 0; j < 4; ++j) m.p[j] = make_float2(c.base + 2 * j < cols ? mean : 0.0f, c.base + 2 * j + 1 < cols ? mean : 0.0f);
   return m;
 }
 template <bool kVec>
@@ -186,7 +218,7 @@ __device__ __forceinline__ float normalise(Pairs (&v)[kVpt], int kind, const Nor
     float s[1] = {sum_of(v)};
     block_sums(s, red, slot);
 #pragma unroll
-    for (int i = 0; i < kVpt; ++i) subtract_mean<kVec>(v[i], s[0] * inv_cols, Cols(i, p.strided), p.cols);
+    for (int i = 0; i < kVpt; ++i) subtract_mean<kVec>(v[i], s[0] * inv_cols, Cols(i), p.cols);
   }
   float s[1] = {dot_of(v, v)};
   block_sums(s, red, slot);
@@ -208,7 +240,7 @@ block_norm_kernel(const NormParams p) {
   auto fetch = [&](int64_t row) {
 #pragma unroll
     for (int i = 0; i < kVpt; ++i) {
-      const Cols c(i, p.strided);
+      const Cols c(i);
       xr[i] = load_group<kVec>(x + row * p.ld_x, c, p.cols);
       if (res) rr[i] = load_group<kVec>(res + row * p.ld_residual, c, p.cols);
       else zero8(rr[i]);
@@ -225,7 +257,7 @@ block_norm_kernel(const NormParams p) {
       gate_end = (gate_row + 1) * p.rows_per_gate;
 #pragma unroll
       for (int i = 0; i < kVpt; ++i)
-        gr[i] = load_group<kVec>(static_cast<const T*>(p.gate) + gate_row * p.ld_gate, Cols(i, p.strided), p.cols);
+        gr[i] = load_group<kVec>(static_cast<const T*>(p.gate) + gate_row * p.ld_gate, Cols(i), p.cols);
     }
     Pairs v[kVpt], r[kVpt];
 #pragma unroll
@@ -235,7 +267,7 @@ block_norm_kernel(const NormParams p) {
       const float2 rstd = both(normalise<kVec>(v, p.kind_post, p, inv_cols, red, slot));
 #pragma unroll
       for (int i = 0; i < kVpt; ++i) {
-        const Cols c(i, p.strided);
+        const Cols c(i);
         const Pairs w = load_weights<kVec>(p.post_weight, p.dt_w, c, p.cols, 1.0f);
 #pragma unroll
         for (int j = 0; j < 4; ++j) v[i].p[j] = mul2(mul2(v[i].p[j], rstd), w.p[j]);
@@ -258,13 +290,13 @@ block_norm_kernel(const NormParams p) {
     if (p.h) {
 #pragma unroll
       for (int i = 0; i < kVpt; ++i)
-        store_group<kVec>(static_cast<T*>(p.h) + row * p.ld_h, Cols(i, p.strided), p.cols, raw_of<T>(v[i]));
+        store_group<kVec>(static_cast<T*>(p.h) + row * p.ld_h, Cols(i), p.cols, raw_of<T>(v[i]));
     }
     if (!p.y) continue;
     const float2 rstd = both(normalise<kVec>(v, p.kind_pre, p, inv_cols, red, slot));
 #pragma unroll
     for (int i = 0; i < kVpt; ++i) {
-      const Cols c(i, p.strided);
+      const Cols c(i);
       Pairs w = load_weights<kVec>(p.pre_weight, p.dt_w, c, p.cols, 1.0f);
 #pragma unroll
       for (int j = 0; j < 4; ++j) v[i].p[j] = mul2(mul2(v[i].p[j], rstd), w.p[j]);
@@ -328,12 +360,12 @@ block_norm_backward_kernel(const NormGradParams p) {
       gate_end = (gate_row + 1) * p.rows_per_gate;
 #pragma unroll
       for (int i = 0; i < kVpt; ++i)
-        gr[i] = load_group<kVec>(static_cast<const T*>(p.gate) + gate_row * p.ld_gate, Cols(i, p.strided), p.cols);
+        gr[i] = load_group<kVec>(static_cast<const T*>(p.gate) + gate_row * p.ld_gate, Cols(i), p.cols);
     }
     Pairs a[kVpt], t[kVpt], x[kPath ? kVpt : 1], dy[kVpt];      // h, gradient of h, x, dy
 #pragma unroll
     for (int i = 0; i < kVpt; ++i) {
-      const Cols c(i, p.strided);
+      const Cols c(i);
       Raw8<T> z;
       zero8(z);
       a[i] = pairs_of(m_h ? load_group<kVec>(m_h + row * p.ld_h, c, p.cols) : z);
@@ -347,7 +379,7 @@ block_norm_backward_kernel(const NormGradParams p) {
       block_sums(s1, red, slot);
 #pragma unroll
       for (int i = 0; i < kVpt; ++i) {
-        const Cols c(i, p.strided);
+        const Cols c(i);
         if (pre_layer) subtract_mean<kVec>(a[i], s1[0] * inv_cols, c, p.cols);
         if (kPath && post_layer) subtract_mean<kVec>(x[i], s1[1] * inv_cols, c, p.cols);
       }
@@ -358,7 +390,7 @@ block_norm_backward_kernel(const NormGradParams p) {
     Pairs dn[kVpt];
 #pragma unroll
     for (int i = 0; i < kVpt; ++i) {
-      const Cols c(i, p.strided);
+      const Cols c(i);
       const Pairs w = load_weights<kVec>(p.pre_weight, p.dt_w, c, p.cols, 1.0f);
 #pragma unroll
       for (int j = 0; j < 4; ++j) dn[i].p[j] = mul2(dy[i].p[j], w.p[j]);
@@ -378,7 +410,7 @@ block_norm_backward_kernel(const NormGradParams p) {
     float2 s3a = both(0.0f), s3b = both(0.0f);
 #pragma unroll
     for (int i = 0; i < kVpt; ++i) {
-      const Cols c(i, p.strided);
+      const Cols c(i);
       if (p.dy) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
@@ -434,7 +466,7 @@ block_norm_backward_kernel(const NormGradParams p) {
     if (p.dx) {
 #pragma unroll
       for (int i = 0; i < kVpt; ++i)
-        store_group<kVec>(static_cast<T*>(p.dx) + row * p.ld_dx, Cols(i, p.strided), p.cols, raw_of<T>(t[i]));
+        store_group<kVec>(static_cast<T*>(p.dx) + row * p.ld_dx, Cols(i), p.cols, raw_of<T>(t[i]));
     }
     if (kPath && p.dgate) {
       const int64_t end = (group + 1) * p.rows_per_gate < p.rows ? (group + 1) * p.rows_per_gate : p.rows;
@@ -442,7 +474,7 @@ block_norm_backward_kernel(const NormGradParams p) {
         const bool starts_here = group * p.rows_per_gate >= row0, ends_here = row + 1 == end;
 #pragma unroll
         for (int i = 0; i < kVpt; ++i) {
-          const Cols c(i, p.strided);
+          const Cols c(i);
           if (starts_here && ends_here) {
             store_group<kVec>(static_cast<T*>(p.dgate) + group * p.cols, c, p.cols, raw_of<T>(dg[i]));
           } else {
@@ -457,7 +489,7 @@ block_norm_backward_kernel(const NormGradParams p) {
   }
 #pragma unroll
   for (int i = 0; i < kVpt; ++i) {
-    const Cols c(i, p.strided);
+    const Cols c(i);
     float* part = p.partial + static_cast<int64_t>(blockIdx.x) * p.cols;
     const int64_t plane = static_cast<int64_t>(gridDim.x) * p.cols;
     if (p.dpre_weight) store_sums<kVec>(part, c, p.cols, dw[i]);
@@ -700,7 +732,6 @@ extern "C" hif4_status hif4_block_norm(const hif4_block_norm_args* a, void* stre
   p.h = a->h; p.y = a->y; p.ld_h = a->ld_h; p.ld_y = a->ld_y;
   p.units = a->y_units ? 1 : 0; p.rha = a->mode == HIF4_RHA;
   vec = vec && vec_w;
-  p.strided = a->cols % 8 != 0;            // (a function of the width alone: rows and their units come from the same sums)
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   if (a->dt == HIF4_BF16) return launch_norm_t<__nv_bfloat16>(p, vec, st);
   if (a->dt == HIF4_FP16) return launch_norm_t<__half>(p, vec, st);
@@ -760,7 +791,6 @@ extern "C" hif4_status hif4_block_norm_backward(const hif4_block_norm_backward_a
   p.partial = static_cast<float*>(workspace);
   p.light = a->post == HIF4_NORM_NONE && !a->gate && a->pre != HIF4_NORM_LAYER;
   p.grid = backward_grid(a->rows, a->cols, p.light);
-  p.strided = a->cols % 8 != 0;
   if (a->dt == HIF4_BF16) return launch_norm_grad_t<__nv_bfloat16>(p, vec, st);
   if (a->dt == HIF4_FP16) return launch_norm_grad_t<__half>(p, vec, st);
   return launch_norm_grad_t<float>(p, vec, st);
