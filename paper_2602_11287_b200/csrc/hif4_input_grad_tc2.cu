@@ -284,14 +284,15 @@ input_grad_tc2_kernel(const __grid_constant__ CUtensorMap tmZ, const __grid_cons
       if (!__all_sync(0xFFFFFFFFu, mbar_wait(tmem_full + 8 * acc, aph, abort_flag, helper ? 32 : 256))) break;
       tc_fence_after();
       const bool shared_tile = w.tail >= 0 && p.slices > 1;
-      const bool adds = shared_tile && w.slice > 0, leaves = shared_tile && w.slice + 1 < p.slices;
+      const bool leaves = shared_tile && w.slice + 1 < p.slices, adds = shared_tile && !leaves;
+      const int others = p.slices - 1;
       const int groups = it == n_items - 1 ? kEpiGroups : 1;
       const int64_t row0 = static_cast<int64_t>(w.m0) + rank * kRows + q * 32, row = row0 + lane;
       const int64_t cols_left = p.K - w.n0;              // K is a multiple of 64: a slab is inside or outside as a whole
       const int cols = row0 >= p.M ? 0 : cols_left < kPairN ? static_cast<int>(cols_left) : kPairN;
-      unsigned int* my_flag = shared_tile ? p.flags + (static_cast<size_t>(w.tail) * p.slices + w.slice) * 8 + rank * 4 + q : nullptr;
-      if (adds && cols > 0 && !__all_sync(0xFFFFFFFFu, wait_count(my_flag - 8, static_cast<unsigned int>(cols / 32), abort_flag))) break;
-      float4* part = shared_tile ? partial_of(p.partial, w.tail, rank, q, lane) : nullptr;
+      unsigned int* flags = shared_tile ? p.flags + static_cast<size_t>(w.tail) * p.slices * 8 + rank * 4 + q : nullptr;
+      if (adds && cols > 0 && !wait_parts(flags, others, static_cast<unsigned int>(cols / 32), abort_flag)) break;
+      float4* part = shared_tile ? partial_of(p.partial, w.tail * others + (leaves ? w.slice : 0), rank, q, lane) : nullptr;
       const uint32_t t_row = tmem_base + (static_cast<uint32_t>(q * 32) << 16) + acc * kPairN;
       unsigned int left = 0;
 #pragma unroll 1
@@ -306,7 +307,7 @@ input_grad_tc2_kernel(const __grid_constant__ CUtensorMap tmZ, const __grid_cons
           tc_wait_ld16(r[h]);
 #pragma unroll
           for (int e = 0; e < 16; ++e) z[e] = __uint_as_float(r[h][e]);
-          if (adds) add_partial16(z, part + (c0 + 16 * h) * 8);
+          if (adds) add_partial16(z, part + (c0 + 16 * h) * 8, others);
           if (leaves) leave_partial16(z, part + (c0 + 16 * h) * 8);
 #pragma unroll
           for (int g = 0; g < 2; ++g) {                 // group of eight columns, held in the order 0 4 1 5 2 6 3 7
@@ -353,7 +354,7 @@ input_grad_tc2_kernel(const __grid_constant__ CUtensorMap tmZ, const __grid_cons
         __syncwarp();
         if (lane == 0 && left > 0) {
           __threadfence();
-          asm volatile("red.release.gpu.global.add.u32 [%0], %1;" ::"l"(my_flag), "r"(left) : "memory");
+          asm volatile("red.release.gpu.global.add.u32 [%0], %1;" ::"l"(flags + 8 * w.slice), "r"(left) : "memory");
         }
       }
       if (!helper) {
@@ -403,7 +404,7 @@ bool make_window_map(CUtensorMap* map, const void* base, int64_t rows, int64_t u
             CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-Tc2Plan grad_plan(int64_t M, int64_t N, int64_t K, int phases) { return tc2_plan(M, K, ceil_div64(N, 256) * 256 * phases); }
+Tc2Plan grad_plan(int64_t M, int64_t N, int64_t K, int phases) { return linear_plan(M, K, ceil_div64(N, 256) * 256 * phases, kPairN); }
 
 template <typename T>
 hif4_status launch_input_grad_t(const InputGradCall& c, void* workspace, cudaStream_t st) {

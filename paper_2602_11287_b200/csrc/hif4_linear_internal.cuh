@@ -31,7 +31,7 @@ struct LinearParams {
   int64_t M, N;
   int num_kc, n_tiles, full_rounds, tail_tiles, slices, sk_tiles, sk_tile0;      // schedule (hif4_tc2_dense.cuh)
   unsigned int* flags;              // [shared tiles][slices][8]: 16-column steps of this slice's sums that are there, per 32 rows
-  float* partial;                   // [shared tiles][2 ranks][4 warps][16 x 16 columns][4][32 rows][4]
+  float* partial;                   // [shared tiles][slices - 1][2 ranks][4 warps][16 x 16 columns][4][32 rows][4]
   unsigned int* error_word;
   DecodeMul mul;
   int tma;                          // 1: units come through TMA, 0: copied word by word

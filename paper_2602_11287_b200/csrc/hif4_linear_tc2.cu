@@ -5,12 +5,12 @@ namespace hif4 {
 
 size_t linear_tc2_workspace(bool gated, int64_t M, int64_t N, int64_t K) {
   if (M <= 0 || N <= 0) return 0;
-  const Tc2Plan pl = tc2_plan(M, N, K, gated ? kPairN / 2 : kPairN);
+  const Tc2Plan pl = linear_plan(M, N, K, gated ? kPairN / 2 : kPairN);
   return pl.slices > 1 ? pl.flag_bytes + partial_tiles(pl) * kPartialTileBytes : 0;
 }
 
 hif4_status linear_tc2_clear(bool gated, int64_t M, int64_t N, int64_t K, void* workspace, cudaStream_t st) {
-  const Tc2Plan pl = tc2_plan(M, N, K, gated ? kPairN / 2 : kPairN);
+  const Tc2Plan pl = linear_plan(M, N, K, gated ? kPairN / 2 : kPairN);
   return pl.slices > 1 && cudaMemsetAsync(workspace, 0, pl.flag_bytes, st) != cudaSuccess ? HIF4_ERR_CUDA : HIF4_OK;
 }
 

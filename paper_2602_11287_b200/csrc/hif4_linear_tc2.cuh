@@ -15,9 +15,13 @@
 //     sums per 32 rows for the bias gradients.
 //   - The last tile of a CTA is finished by all of its warps: the decode warps, out of work, take four fifths of the
 //     columns (staged in the operand stages, which are free by then).  With few tiles this tail is most of the call.
-//   - Tiles shared along K pass FP32 partial sums through the workspace (the epilogue is not linear, so nothing can be
-//     added in place): slice s adds its part to what slice s - 1 left and the last slice finishes the tile, always in
-//     this order.
+//   - Tiles shared along K pass FP32 partial sums through the workspace (the epilogue is not linear, so nothing can be added
+//     in place): every slice but the last leaves its part, the last adds them to its own in slice order and finishes the
+//     tile.  It waits for slices of lower index only, so a grid that is partly resident cannot wait for itself.
+// What bounds it: in long products the shared-memory port (operand reads of the tensor core, decoded stores and raw traffic
+// together fill its 128 bytes a clock, about 775 clocks per K = 64 step against 512 of the tensor core); in short ones the
+// set-up and the epilogue's latency.  4096 x 14336 x 4096 gated 795 us (1.21 PFLOP/s, 0.72 of the measured burst peak), 4096 x 4096 x
+// 14336 with residual 390 us; 64 x 4096 x 4096 27 us.
 #pragma once
 #include "hif4_activation.cuh"
 #include "hif4_gemm_internal.cuh"
@@ -52,21 +56,32 @@ __device__ __forceinline__ void load16(const T* p, bool vec, int valid, float (&
     for (int e = 0; e < 16; ++e) v[e] = e < valid ? to_f32(p[e]) : 0.0f;
   }
 }
-// Partial sums of 16 columns of a row: four 16-byte words, each beside those of the warp's other rows.
-__device__ __forceinline__ void add_partial16(float (&v)[16], const float4* part) {
+// Partial sums of 16 columns of a row: four 16-byte words, each beside those of the warp's other rows.  The `others` parts of
+// a tile lie one after another and are added in that order.
+constexpr size_t kPartialTileWords = static_cast<size_t>(kPairM) * kPairN / 4;
+__device__ __forceinline__ void add_partial16(float (&v)[16], const float4* part, int others) {
+#pragma unroll 2
+  for (int s = 0; s < others; ++s, part += kPartialTileWords) {
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    const float4 f = __ldcg(part + k * 32);
-    v[4 * k] += f.x; v[4 * k + 1] += f.y; v[4 * k + 2] += f.z; v[4 * k + 3] += f.w;
+    for (int k = 0; k < 4; ++k) {
+      const float4 f = __ldcg(part + k * 32);
+      v[4 * k] += f.x; v[4 * k + 1] += f.y; v[4 * k + 2] += f.z; v[4 * k + 3] += f.w;
+    }
   }
 }
 __device__ __forceinline__ void leave_partial16(const float (&v)[16], float4* part) {
 #pragma unroll
   for (int k = 0; k < 4; ++k) __stcg(part + k * 32, make_float4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]));
 }
-// A warp's corner of a shared tile's sums: 256 columns x 32 rows, 16 columns (2 KB) after 16 columns.
-__device__ __forceinline__ float4* partial_of(float* partial, int tail, uint32_t rank, int q, int lane) {
-  return reinterpret_cast<float4*>(partial) + ((static_cast<size_t>(tail) * 2 + rank) * 4 + q) * (32 * kPairN / 4) + lane;
+// A warp's corner of a part of a shared tile: 256 columns x 32 rows, 16 columns (2 KB) after 16 columns.
+__device__ __forceinline__ float4* partial_of(float* partial, int part, uint32_t rank, int q, int lane) {
+  return reinterpret_cast<float4*>(partial) + static_cast<size_t>(part) * kPartialTileWords + (rank * 4 + q) * (32 * kPairN / 4) + lane;
+}
+// Waits until the parts before the last have all `steps` counted in this quadrant.
+__device__ __forceinline__ bool wait_parts(const unsigned int* flags, int others, unsigned int steps, volatile uint32_t* abort_flag) {
+  for (int s = 0; s < others; ++s)
+    if (!__all_sync(0xFFFFFFFFu, wait_count(flags + 8 * s, steps, abort_flag))) return false;
+  return true;
 }
 template <int kAct>
 __device__ __forceinline__ void activate16(float (&v)[16]) {
@@ -415,7 +430,8 @@ linear_tc2_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
       const int64_t row0 = static_cast<int64_t>(w.m0) + rank * kRows + q * 32, row = row0 + lane;
       const bool row_ok = row < p.M;
       const bool shared_tile = w.tail >= 0 && p.slices > 1;
-      const bool adds = shared_tile && w.slice > 0, leaves = shared_tile && w.slice + 1 < p.slices;
+      const bool leaves = shared_tile && w.slice + 1 < p.slices, adds = shared_tile && !leaves;
+      const int others = p.slices - 1;                   // parts that the last slice adds to its own
       const int groups = it == n_items - 1 ? kEpiGroups : 1;
       // columns that hold outputs, in whole slabs
       const int64_t cols_left = p.N - w.n0;
@@ -439,10 +455,10 @@ linear_tc2_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
       if (!__all_sync(0xFFFFFFFFu, mbar_wait(tmem_full + 8 * acc, aph, abort_flag, helper ? 32 : 256))) break;
       tc_fence_after();
       if (helper) request_first();
-      // sixteen-column steps that the previous slice's warps have left in this quadrant: all of the tile's
-      unsigned int* my_flag = shared_tile ? p.flags + (static_cast<size_t>(w.tail) * p.slices + w.slice) * 8 + rank * 4 + q : nullptr;
-      if (adds && cols > 0 && !__all_sync(0xFFFFFFFFu, wait_count(my_flag - 8, static_cast<unsigned int>(cols / 16), abort_flag))) break;
-      float4* part_sums = shared_tile ? partial_of(p.partial, w.tail, rank, q, lane) : nullptr;
+      // sixteen-column steps that the other slices' warps have left in this quadrant: all of the tile's
+      unsigned int* flags = shared_tile ? p.flags + static_cast<size_t>(w.tail) * p.slices * 8 + rank * 4 + q : nullptr;
+      if (adds && cols > 0 && !wait_parts(flags, others, static_cast<unsigned int>(cols / 16), abort_flag)) break;
+      float4* part_sums = shared_tile ? partial_of(p.partial, w.tail * others + (leaves ? w.slice : 0), rank, q, lane) : nullptr;
       const uint32_t t_row = tmem_base + (static_cast<uint32_t>(q * 32) << 16) + acc * kPairN;
       // Eight lanes convert one unit of a staged 32 x 64 block (16-bit types), four rows at a time; `col`: a column of the block.
       auto convert_units = [&](int64_t col) {
@@ -618,14 +634,13 @@ linear_tc2_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
             tc_wait_ld16(r);
 #pragma unroll
             for (int e = 0; e < 16; ++e) z[e] = __uint_as_float(r[e]);
-            if (adds) add_partial16(z, part_sums + cc * 8);
             leave_partial16(z, part_sums + cc * 8);
           }
         }
         __syncwarp();
         if (lane == 0 && left > 0) {
           __threadfence();
-          asm volatile("red.release.gpu.global.add.u32 [%0], %1;" ::"l"(my_flag), "r"(left) : "memory");
+          asm volatile("red.release.gpu.global.add.u32 [%0], %1;" ::"l"(flags + 8 * w.slice), "r"(left) : "memory");
         }
       } else {
         const int step = !kGrad && p.units ? 64 : kSlabCols;
@@ -666,8 +681,8 @@ linear_tc2_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
               }
             }
             if (adds) {
-              add_partial16(z, part_sums + c * 8);
-              if (kGated) add_partial16(u, part_sums + (kOutCols + c) * 8);
+              add_partial16(z, part_sums + c * 8, others);
+              if (kGated) add_partial16(u, part_sums + (kOutCols + c) * 8, others);
             }
             const int valid = p.N - col < 16 ? static_cast<int>(p.N - col) : 16;      // may be <= 0 in the second half of a slab
             if (bias) {

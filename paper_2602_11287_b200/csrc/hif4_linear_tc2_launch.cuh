@@ -21,8 +21,30 @@ bool make_y_map(CUtensorMap* map, void* y, int64_t M, int64_t N, int64_t ld) {
             CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// The schedule of the FP32 product, but for a single round of tiles its own number of K slices: here the parts are left side
+// by side and one slice adds them all, where the FP32 product chains them.  A chunk (K = 256) is about 1.8 us; leaving and
+// meeting the parts costs about 2.5 us once, and adding one about 1.1 us for 256 columns (64 x 1024 x 14336: eight slices,
+// 35 us; the FP32 product with its chain of four 45 us).
+constexpr int kMaxLinearSlices = 32;
+inline Tc2Plan linear_plan(int64_t M, int64_t N, int64_t K, int tile_n) {
+  Tc2Plan pl = tc2_plan(M, N, K, tile_n);
+  if (pl.full_rounds > 0 || pl.sk_tiles > 0 || pl.tail_tiles <= 0) return pl;
+  const int64_t chunks = ceil_div64(K, 256), columns = N < tile_n ? N : tile_n;
+  int64_t s_max = sm_count() / 2 / pl.tail_tiles;
+  if (s_max > kMaxLinearSlices) s_max = kMaxLinearSlices;
+  if (s_max > chunks) s_max = chunks;
+  int64_t best = 1, best_cost = 18 * chunks;                                     // in tenths of a microsecond
+  for (int64_t s = 2; s <= s_max; ++s) {
+    const int64_t cost = 18 * ceil_div64(chunks, s) + 25 + 11 * (s - 1) * columns / tile_n;
+    if (cost < best_cost) { best = s; best_cost = cost; }
+  }
+  pl.slices = static_cast<int>(best);
+  pl.flag_bytes = best > 1 ? (static_cast<size_t>(pl.tail_tiles) * best * 8 * sizeof(unsigned int) + 255) / 256 * 256 : 0;
+  pl.bytes = pl.flag_bytes;
+  return pl;
+}
 inline size_t partial_tiles(const Tc2Plan& pl) {
-  return pl.sk_tiles > 0 ? static_cast<size_t>(pl.pairs) + 1 : pl.slices > 1 ? static_cast<size_t>(pl.tail_tiles) : 0;
+  return pl.sk_tiles > 0 ? static_cast<size_t>(pl.pairs) + 1 : pl.slices > 1 ? static_cast<size_t>(pl.tail_tiles) * (pl.slices - 1) : 0;
 }
 constexpr size_t kPartialTileBytes = static_cast<size_t>(kPairM) * kPairN * sizeof(float);
 
@@ -38,7 +60,7 @@ hif4_status launch_linear_act(const LinearCall& c, void* workspace, cudaStream_t
   const int64_t upr = c.K / kUnitElems;
   p.num_kc = c.K > 0 ? static_cast<int>(ceil_div64(upr, kRawUnits)) : 1;       // K = 0: one chunk of zeros
   p.n_tiles = static_cast<int>(ceil_div64(c.N, kTileN));
-  const Tc2Plan pl = tc2_plan(c.M, c.N, c.K, kTileN);
+  const Tc2Plan pl = linear_plan(c.M, c.N, c.K, kTileN);
   p.full_rounds = pl.full_rounds; p.tail_tiles = pl.tail_tiles; p.slices = pl.slices;
   p.sk_tiles = pl.sk_tiles; p.sk_tile0 = pl.sk_tile0;
   p.mul = make_decode_mul();
