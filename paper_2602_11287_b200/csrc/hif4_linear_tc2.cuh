@@ -18,10 +18,10 @@
 //   - Tiles shared along K pass FP32 partial sums through the workspace (the epilogue is not linear, so nothing can be added
 //     in place): every slice but the last leaves its part, the last adds them to its own in slice order and finishes the
 //     tile.  It waits for slices of lower index only, so a grid that is partly resident cannot wait for itself.
-// What bounds it: in long products the shared-memory port (operand reads of the tensor core, decoded stores and raw traffic
-// together fill its 128 bytes a clock, about 775 clocks per K = 64 step against 512 of the tensor core); in short ones the
-// set-up and the epilogue's latency.  4096 x 14336 x 4096 gated 795 us (1.21 PFLOP/s, 0.72 of the measured burst peak), 4096 x 4096 x
-// 14336 with residual 390 us; 64 x 4096 x 4096 27 us.
+// What bounds it: long products, what bounds the FP32 product (decode and tensor core take 3080 and 2350 clocks per K = 256
+// chunk by themselves and share issue slots and the shared-memory port); short ones, set-up, pipeline fill and the last
+// tile's epilogue.  4096 x 14336 x 4096 gated 795 us (1.21 PFLOP/s, 0.72 of the measured burst peak), 4096 x 4096 x 14336 with
+// residual 390 us, 64 x 4096 x 4096 27 us.
 #pragma once
 #include "hif4_activation.cuh"
 #include "hif4_gemm_internal.cuh"

@@ -5,6 +5,7 @@
 // A function returns its result, or the status code (a Python int) of a C call that refused its arguments; arguments that are
 // not what they should be raise ValueError or TypeError.
 #include <ATen/ATen.h>
+#include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -48,9 +49,20 @@ std::string about(const at::Tensor& t) {
   for (int64_t i = 0; i < t.dim(); ++i) s += (i ? ", " : "") + std::to_string(t.stride(i));
   return s + ")";
 }
+// The device of the call: that of its first tensor, current while it runs; every other tensor has to be there as well.
+thread_local int call_device = -1;
 void need_cuda(const at::Tensor& t) {
   if (!t.is_cuda()) throw std::invalid_argument("the HiF4 library takes device tensors only (no CPU path exists)");
+  if (t.get_device() != call_device) throw std::invalid_argument("tensors of one call must be on one device");
 }
+struct OnDeviceOf {
+  c10::cuda::OptionalCUDAGuard guard;
+  explicit OnDeviceOf(const at::Tensor& t) {
+    call_device = t.is_cuda() ? t.get_device() : -1;
+    need_cuda(t);
+    guard.set_index(static_cast<c10::DeviceIndex>(call_device));
+  }
+};
 int type_code(at::ScalarType t) {
   switch (t) {
     case at::kBFloat16: return HIF4_BF16;
@@ -145,6 +157,7 @@ struct Workspace {
 PyObject* block_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded(n, 15, [&]() -> PyObject* {
     const at::Tensor& x = tensor(a[0], "x");
+    const OnDeviceOf on(x);
     if (x.dim() != 2) throw std::invalid_argument("x: a matrix expected");
     const int64_t rows = x.size(0), cols = x.size(1);
     const at::ScalarType type = x.scalar_type();
@@ -210,6 +223,7 @@ PyObject* block_norm_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
                      *wp = tensor_or_null(a[10], "post_weight"), *ws = tensor_or_null(a[14], "workspace");
     const at::Tensor* first = dy ? dy : dh;
     if (!first || first->dim() != 2) throw std::invalid_argument("dy or dh: a matrix expected");
+    const OnDeviceOf on(*first);
     const int64_t rows = first->size(0), cols = first->size(1);
     const at::ScalarType type = first->scalar_type();
     const at::ScalarType wtype = w ? w->scalar_type() : wp ? wp->scalar_type() : type;
@@ -291,6 +305,7 @@ PyObject* linear_act(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const at::Tensor &x = tensor(a[0], "x"), &w = tensor(a[1], "w_units");
     const at::Tensor *wu = tensor_or_null(a[2], "w_up_units"), *b = tensor_or_null(a[3], "bias"), *bu = tensor_or_null(a[4], "bias_up"),
                      *res = tensor_or_null(a[5], "residual"), *out = tensor_or_null(a[11], "out"), *ws = tensor_or_null(a[12], "workspace");
+    const OnDeviceOf on(x);
     const Activations act = activations(x);
     if (w.dim() != 3) throw std::invalid_argument("w_units: units [N, K / 64, 36] expected, got " + about(w));
     const int64_t M = act.rows, N = w.size(0), K = act.K;
@@ -339,6 +354,7 @@ PyObject* linear_act_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const at::Tensor &dy = tensor(a[0], "dy"), &w = tensor(a[2], "w_units");
     const at::Tensor *x = tensor_or_null(a[1], "x"), *wu = tensor_or_null(a[3], "w_up_units"), *b = tensor_or_null(a[4], "bias"),
                      *bu = tensor_or_null(a[5], "bias_up"), *ws = tensor_or_null(a[10], "workspace");
+    const OnDeviceOf on(dy);
     if (dy.dim() != 2) throw std::invalid_argument("dy: a matrix expected");
     if (w.dim() != 3) throw std::invalid_argument("w_units: units [N, K / 64, 36] expected, got " + about(w));
     const int64_t M = dy.size(0), N = dy.size(1), K = w.size(1) * HIF4_UNIT_ELEMS;
