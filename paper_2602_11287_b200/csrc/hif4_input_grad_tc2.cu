@@ -91,7 +91,7 @@ input_grad_tc2_kernel(const __grid_constant__ CUtensorMap tmZ, const __grid_cons
   const uint32_t bar_base = raw_base + kRawRing * kRawStepBytes;
   const uint32_t raw_full = bar_base, raw_empty = raw_full + 8 * kRawRing, z_full = raw_empty + 8 * kRawRing, op_full = z_full + 8 * kOpRing,
                  op_empty = op_full + 8 * kOpRing, tmem_full = op_empty + 8 * kOpRing, tmem_empty = tmem_full + 16,
-                 tmem_slot = tmem_empty + 16;
+                 last_full = tmem_empty + 16, tmem_slot = last_full + 8;
   uint8_t* gen_base = smem_raw + (smem_base - smem_u32(smem_raw));
   volatile uint32_t* tmem_ptr_smem = reinterpret_cast<volatile uint32_t*>(gen_base + (tmem_slot - smem_base));
   volatile uint32_t* abort_flag = tmem_ptr_smem + 1;
@@ -118,6 +118,7 @@ input_grad_tc2_kernel(const __grid_constant__ CUtensorMap tmZ, const __grid_cons
       mbar_init(tmem_full + 8 * s, 1);
       mbar_init(tmem_empty + 8 * s, 8);               // 4 epilogue warps of each CTA (used on rank 0)
     }
+    mbar_init(last_full, 1);
     *abort_flag = 0u;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -220,6 +221,7 @@ input_grad_tc2_kernel(const __grid_constant__ CUtensorMap tmZ, const __grid_cons
         }
         if (!ok) break;
         tc2_commit_both(tmem_full + 8 * acc);
+        if (i == n_items - 1) tc2_commit_both(last_full);         // the same, for the helpers of the last epilogue
       }
     }
   } else {
@@ -284,7 +286,9 @@ input_grad_tc2_kernel(const __grid_constant__ CUtensorMap tmZ, const __grid_cons
     for (int it = first; it < n_items && ok; ++it, ++tcount) {
       const WorkItem w = work_item<kPairN>(p, pair, num_pairs, it);
       const uint32_t acc = tcount & 1u, aph = (tcount >> 1) & 1u;
-      if (!__all_sync(0xFFFFFFFFu, mbar_wait(tmem_full + 8 * acc, aph, abort_flag, helper ? 32 : 256))) break;
+      // A helper has not followed the phases of tmem_full, and with short items several may still be to come: the parity would
+      // not tell it which one it sees.  Its own barrier completes once.
+      if (!__all_sync(0xFFFFFFFFu, helper ? mbar_wait(last_full, 0u, abort_flag, 32) : mbar_wait(tmem_full + 8 * acc, aph, abort_flag, 256))) break;
       tc_fence_after();
       const bool shared_tile = w.tail >= 0 && p.slices > 1;
       const bool leaves = shared_tile && w.slice + 1 < p.slices, adds = shared_tile && !leaves;

@@ -238,7 +238,8 @@ linear_tc2_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
   const uint32_t out_base = raw_base + kRawStages * kRawStageBytes;
   const uint32_t bar_base = out_base + kStageOutBytes;
   const uint32_t raw_full = bar_base, raw_empty = bar_base + 16, dec_full = bar_base + 32, dec_empty = bar_base + 64,
-                 tmem_full = bar_base + 96, tmem_empty = bar_base + 112, side_full = bar_base + 144;      // [20 warps][kStageBufs]
+                 tmem_full = bar_base + 96, tmem_empty = bar_base + 112, last_full = bar_base + 136,
+                 side_full = bar_base + 144;      // [20 warps][kStageBufs]
   uint8_t* gen_base = smem_raw + (smem_base - smem_u32(smem_raw));
   volatile uint32_t* tmem_ptr_smem = reinterpret_cast<volatile uint32_t*>(gen_base + (bar_base - smem_base) + 128);
   volatile uint32_t* abort_flag = tmem_ptr_smem + 1;
@@ -265,6 +266,7 @@ linear_tc2_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
       mbar_init(tmem_empty + 8 * s, 8);               // 4 epilogue warps of each CTA (used on rank 0)
     }
     for (int s = 0; s < 4 * kEpiGroups * kStageBufs; ++s) mbar_init(side_full + 8 * s, 1);
+    mbar_init(last_full, 1);
     *abort_flag = 0u;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -358,6 +360,7 @@ linear_tc2_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
         }
         if (!ok) break;
         tc2_commit_both(tmem_full + 8 * acc);         // accumulator complete, in both CTAs
+        if (it == n_items - 1) tc2_commit_both(last_full);        // the same, for the helpers of the last epilogue
       }
     }
   } else {
@@ -452,7 +455,9 @@ linear_tc2_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
         }
       };
       if (!helper) request_first();
-      if (!__all_sync(0xFFFFFFFFu, mbar_wait(tmem_full + 8 * acc, aph, abort_flag, helper ? 32 : 256))) break;
+      // A helper has not followed the phases of tmem_full, and with short items several may still be to come: the parity would
+      // not tell it which one it sees.  Its own barrier completes once.
+      if (!__all_sync(0xFFFFFFFFu, helper ? mbar_wait(last_full, 0u, abort_flag, 32) : mbar_wait(tmem_full + 8 * acc, aph, abort_flag, 256))) break;
       tc_fence_after();
       if (helper) request_first();
       // sixteen-column steps that the other slices' warps have left in this quadrant: all of the tile's

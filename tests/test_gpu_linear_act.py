@@ -305,6 +305,26 @@ def test_gradient_large(hif4, M, N, K, gated):
     check_backward(hif4, M, N, K, torch.bfloat16, gated, act=2)
 
 
+@pytest.mark.parametrize("gated", [False, True])
+@pytest.mark.parametrize("M,N,K", [(2860, 15, 6144), (806, 36, 12032), (2507, 78, 7424), (936, 64, 12416), (1200, 130, 8192)])
+def test_gradient_of_many_tiles_with_a_short_contraction(hif4, M, N, K, gated):
+    """Each CTA pair works through several tiles of one to four contraction steps: the decode warps that join the epilogue
+    of the last tile must not take an earlier tile's completion for its own."""
+    for dtype in (torch.bfloat16, torch.float16):
+        check_backward(hif4, M, N, K, dtype, gated, act=2)
+
+
+@pytest.mark.parametrize("gated", [False, True])
+@pytest.mark.parametrize("M,N,K", [(3000, 4000, 64), (2000, 9000, 128), (5000, 2049, 256)])
+def test_forward_of_many_tiles_with_a_short_contraction(hif4, M, N, K, gated):
+    x, w, b = operands(hif4, M, N, K, torch.bfloat16, gated, M + N)
+    y = call(hif4, x, w, b, act=2)
+    ref, e = expect_forward(hif4, x, w, b, 2, None, 0.0)
+    close(y, ref, e, torch.bfloat16, f"{M}x{N}x{K}")
+    for _ in range(3):
+        assert torch.equal(y, call(hif4, x, w, b, act=2)), "two runs differ"
+
+
 @pytest.mark.parametrize("act", range(5))
 def test_gradient_activations(hif4, act):
     for gated in (False, True):
