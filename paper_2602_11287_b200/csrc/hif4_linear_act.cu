@@ -125,8 +125,18 @@ hif4_status check_operands(const Args* a, bool gated, bool reads_x) {
   return HIF4_OK;
 }
 
-hif4_status forward(const hif4_linear_act_args* a, bool gated, void* workspace, size_t workspace_bytes, void* stream) {
-  if (!a) return HIF4_ERR_NULL;
+// The arguments with the row stride of a single row of activations set to its length: no row follows it, so no kernel's or
+// conversion's rule on strides applies.
+template <typename Args>
+Args single_row_stride(const Args& a) {
+  Args c = a;
+  if (c.M == 1 && !c.x_units && c.ld_x > c.K) c.ld_x = c.K;
+  return c;
+}
+
+hif4_status forward(const hif4_linear_act_args* args, bool gated, void* workspace, size_t workspace_bytes, void* stream) {
+  if (!args) return HIF4_ERR_NULL;
+  const hif4_linear_act_args one = single_row_stride(*args), *a = &one;
   const hif4_status chk = check_operands(a, gated, true);
   if (chk != HIF4_OK) return chk;
   if ((a->y_units && a->N % kUnitElems != 0) || (!a->y_units && a->ld_y < a->N) || (a->residual && a->ld_residual < a->N)) return HIF4_ERR_SHAPE;
@@ -166,8 +176,9 @@ hif4_status forward(const hif4_linear_act_args* a, bool gated, void* workspace, 
   return pr != HIF4_OK ? pr : hif4_quantize(ws + s.y, a->dt, a->M, a->N, a->N, a->Y, a->mode, stream);
 }
 
-hif4_status backward(const hif4_linear_act_backward_args* a, bool gated, void* workspace, size_t workspace_bytes, void* stream) {
-  if (!a) return HIF4_ERR_NULL;
+hif4_status backward(const hif4_linear_act_backward_args* args, bool gated, void* workspace, size_t workspace_bytes, void* stream) {
+  if (!args) return HIF4_ERR_NULL;
+  const hif4_linear_act_backward_args one = single_row_stride(*args), *a = &one;
   if (a->dt == HIF4_FP32) return HIF4_ERR_DTYPE;
   const bool reads_x = gated || a->act != HIF4_ACT_NONE;
   const hif4_status chk = check_operands(a, gated, reads_x);
