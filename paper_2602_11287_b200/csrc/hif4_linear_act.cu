@@ -24,7 +24,7 @@ split_rows_kernel(const T* dy, int64_t ld_dy, int64_t M, int64_t N, __nv_bfloat1
     for (int part = 0; part < parts; ++part) {
       const __nv_bfloat16 b = __float2bfloat16_rn(v);
       dz[(part * M + r) * ld_dz + col] = b;
-      v -= __bfloat162float(b);
+      v = rest_of(v, __bfloat162float(b));
     }
   }
   if (colsum) colsum[static_cast<int64_t>(blockIdx.y) * N + col] = s;

@@ -199,7 +199,8 @@ __device__ __forceinline__ float column_sum16(const float (&v)[16], int lane) {
 // The column whose sum column_sum16 leaves in `lane`: bit w of the lane number chose the upper half at width w.
 __device__ __forceinline__ int column_of_lane(int lane) { return (lane & 16 ? 8 : 0) + (lane & 8 ? 4 : 0) + (lane & 4 ? 2 : 0) + (lane & 2 ? 1 : 0); }
 
-// BF16 parts of 16 values: part 0 holds the leading 8 bits, part 1 what is left of them.
+// BF16 parts of 16 values: part 0 holds the leading 8 bits, part 1 what is left of them (nothing of an infinity: the
+// difference would be NaN).
 template <int kParts>
 __device__ __forceinline__ void store_parts(const float (&v)[16], __nv_bfloat16* dst, int64_t plane, int64_t room) {
   float rest[16];
@@ -212,8 +213,8 @@ __device__ __forceinline__ void store_parts(const float (&v)[16], __nv_bfloat16*
     for (int e = 0; e < 8; ++e) {
       w[e] = pack2(rest[2 * e], rest[2 * e + 1], __nv_bfloat16());
       if (part + 1 < kParts) {
-        rest[2 * e] -= __uint_as_float(w[e] << 16);
-        rest[2 * e + 1] -= __uint_as_float(w[e] & 0xFFFF0000u);
+        rest[2 * e] = rest_of(rest[2 * e], __uint_as_float(w[e] << 16));
+        rest[2 * e + 1] = rest_of(rest[2 * e + 1], __uint_as_float(w[e] & 0xFFFF0000u));
       }
     }
     uint4* q = reinterpret_cast<uint4*>(dst + part * plane);

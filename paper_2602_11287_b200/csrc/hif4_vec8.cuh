@@ -29,6 +29,9 @@ template <> __device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(flo
 template <> __device__ __forceinline__ __half from_f32<__half>(float v) { return __float2half_rn(v); }
 template <> __device__ __forceinline__ float from_f32<float>(float v) { return v; }
 
+// What a rounded part leaves of v: zero where the part is infinite or NaN, which it then stands for by itself.
+__device__ __forceinline__ float rest_of(float v, float part) { return fabsf(part) < __int_as_float(0x7F800000) ? v - part : 0.0f; }
+
 __device__ __forceinline__ void unpack8(const Raw8<__nv_bfloat16>& r, float (&v)[8]) {
   const uint32_t w[4] = {r.a.x, r.a.y, r.a.z, r.a.w};
 #pragma unroll

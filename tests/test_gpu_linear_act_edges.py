@@ -40,3 +40,77 @@ def test_gradient_of_one_row_of_any_stride(hif4, gated, dtype, K):
     f = hif4.hif4_gated_linear_backward if gated else hif4.hif4_linear_act_backward
     got, want = (f(dy, t, *w, *b, act=2, want_dbias=True) for t in (row, x))
     assert all(torch.equal(g, v) for g, v in zip(got, want))
+
+
+# ------------------------------------------------------------------------------------------------------ NaN and infinity
+def nonzero_weights(hif4, N, K, seed):
+    """Codes without a zero: the product with an infinity is an infinity of the weight's sign."""
+    g = torch.Generator(device="cuda"); g.manual_seed(seed)
+    w = hif4.hif4_quantize(torch.where(torch.rand(N, K, generator=g, device="cuda") < 0.5, -1.0, 1.0).to(torch.bfloat16))
+    assert bool((decode(hif4, w) != 0).all())
+    return w
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("act", [0, 2])
+@pytest.mark.parametrize("M", [1, 40, 300])
+def test_an_infinite_gradient_stays_infinite(hif4, dtype, act, M):
+    """dX[m] = sum of dZ[m, n] W[n]: one infinite dZ and no zero among the codes give infinities, not NaN, in that row alone."""
+    N, K = 192, 512
+    x, _, b = operands(hif4, M, 1, K, dtype, False, 3)
+    w = nonzero_weights(hif4, N, K, 4)
+    bias = torch.full((N,), 3.0, dtype=dtype, device="cuda")
+    dy = torch.randn(M, N, device="cuda").to(dtype)
+    clean, dbc = hif4.hif4_linear_act_backward(dy, x, w, bias, act=act, want_dbias=True)
+    n, m = 77, M // 2
+    if act:            # an output whose slope is positive
+        z = decode(hif4, hif4.hif4_quantize(x)) @ decode(hif4, w).t() + 3.0
+        n = int(z[m].argmax())
+        assert float(z[m, n]) > 1.0
+    dy[m, n] = float("inf")
+    dx, db = hif4.hif4_linear_act_backward(dy, x, w, bias, act=act, want_dbias=True)
+    want = decode(hif4, w)[n].sign() * float("inf")
+    assert torch.equal(dx[m].double(), want)
+    keep = torch.arange(M, device="cuda") != m
+    assert torch.equal(dx[keep], clean[keep])
+    keep = torch.arange(N, device="cuda") != n
+    assert torch.equal(db[keep], dbc[keep]) and float(db[n]) == float("inf")
+
+
+@pytest.mark.parametrize("gated", [False, True])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("M", [3, 300])
+def test_a_nan_gradient_stays_in_its_row_and_column(hif4, gated, dtype, M):
+    x, w, b = operands(hif4, M, 256, 512, dtype, gated, 5)
+    dy = torch.randn(M, 256, device="cuda").to(dtype)
+    f = hif4.hif4_gated_linear_backward if gated else hif4.hif4_linear_act_backward
+    clean = f(dy, x, *w, *b, act=3, want_dbias=True)
+    dy[1, 9] = float("nan")
+    got = f(dy, x, *w, *b, act=3, want_dbias=True)
+    assert torch.isnan(got[0][1]).all()
+    rows = torch.arange(M, device="cuda") != 1
+    cols = torch.arange(256, device="cuda") != 9
+    assert torch.equal(got[0][rows], clean[0][rows])
+    for g, c in zip(got[1:], clean[1:]):
+        assert torch.isnan(g[9]) and torch.equal(g[cols], c[cols])
+
+
+@pytest.mark.parametrize("gated", [False, True])
+@pytest.mark.parametrize("M", [1, 12, 40, 300])
+def test_infinite_activations_residuals_and_results(hif4, M, gated):
+    """An infinite activation saturates in the conversion; an infinite residual and a result past FP16's range are infinities."""
+    x, w, b = operands(hif4, M, 256, 512, torch.float16, gated, 6)
+    x[0, 3], x[-1, 200] = float("inf"), float("-inf")
+    res = torch.randn(M, 256, device="cuda").to(torch.float16)
+    res[0, 5], res[-1, 6] = float("inf"), float("-inf")
+    res[-1, 7] = 60000.0
+    y = call(hif4, x, w, b, act=1, residual=res, res_scale=2.0)
+    ref, e = expect_forward(hif4, x, w, b, 1, res, 2.0)
+    e = torch.where(torch.isinf(ref), torch.zeros_like(e), e)
+    over = ref.abs() - e > 65520.0
+    under = ref.abs() + e < 65520.0
+    assert bool(over[0, 5]) and bool(over[-1, 6]) and bool(over[-1, 7])
+    assert torch.equal(y[over].double(), ref[over].sign() * float("inf"))
+    close(y[under], ref[under], e[under], torch.float16, "finite results")
+    u = call(hif4, x, w, b, act=1, residual=res, res_scale=2.0, units=True, dtype=torch.float16)
+    assert torch.equal(u, hif4.hif4_quantize(y))
