@@ -8,26 +8,29 @@ namespace hif4 {
 namespace {
 
 // A gradient that needs no activation: dZ = dY.  BF16 parts of dY (when the product cannot read dY itself) and the sums
-// of 32 rows at a time; one thread per column of a row block, so that the lanes of a warp read neighbouring elements.
+// of 32 rows at a time; one thread per column of a row block, so that the lanes of a warp read neighbouring elements.  The row
+// blocks go round the grid's second dimension, which ends at 65535.
 template <typename T>
 __global__ void __launch_bounds__(256)
 split_rows_kernel(const T* dy, int64_t ld_dy, int64_t M, int64_t N, __nv_bfloat16* dz, int64_t ld_dz, int parts, float* colsum) {
   const int64_t col = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
   if (col >= N) return;
-  const int64_t r0 = static_cast<int64_t>(blockIdx.y) * 32, r1 = r0 + 32 < M ? r0 + 32 : M;
-  float s = 0.0f;
+  for (int64_t block = blockIdx.y; block * 32 < M; block += gridDim.y) {
+    const int64_t r0 = block * 32, r1 = r0 + 32 < M ? r0 + 32 : M;
+    float s = 0.0f;
 #pragma unroll 8
-  for (int64_t r = r0; r < r1; ++r) {
-    float v = to_f32(dy[r * ld_dy + col]);
-    s += v;
-    if (!dz) continue;
-    for (int part = 0; part < parts; ++part) {
-      const __nv_bfloat16 b = __float2bfloat16_rn(v);
-      dz[(part * M + r) * ld_dz + col] = b;
-      v = rest_of(v, __bfloat162float(b));
+    for (int64_t r = r0; r < r1; ++r) {
+      float v = to_f32(dy[r * ld_dy + col]);
+      s += v;
+      if (!dz) continue;
+      for (int part = 0; part < parts; ++part) {
+        const __nv_bfloat16 b = __float2bfloat16_rn(v);
+        dz[(part * M + r) * ld_dz + col] = b;
+        v = rest_of(v, __bfloat162float(b));
+      }
     }
+    if (colsum) colsum[block * N + col] = s;
   }
-  if (colsum) colsum[static_cast<int64_t>(blockIdx.y) * N + col] = s;
 }
 
 // out[col] = sum of the row blocks' sums: 32 columns per block, 32 ways over the row blocks, joined in a fixed order.
@@ -227,8 +230,7 @@ hif4_status backward(const hif4_linear_act_backward_args* args, bool gated, void
     if (pr != HIF4_OK) return pr;
   } else if (dz || colsum) {
     const int64_t row_blocks = ceil_div64(a->M, 32);
-    if (row_blocks > 65535) return HIF4_ERR_SHAPE;
-    const dim3 grid(static_cast<unsigned>(ceil_div64(a->N, 256)), static_cast<unsigned>(row_blocks));
+    const dim3 grid(static_cast<unsigned>(ceil_div64(a->N, 256)), static_cast<unsigned>(row_blocks < 65535 ? row_blocks : 65535));
     if (a->dt == HIF4_BF16)
       split_rows_kernel<<<grid, 256, 0, st>>>(static_cast<const __nv_bfloat16*>(a->dY), a->ld_dy, a->M, a->N, dz, s.ld_dz, s.parts, colsum);
     else

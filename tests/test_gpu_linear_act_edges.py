@@ -114,3 +114,18 @@ def test_infinite_activations_residuals_and_results(hif4, M, gated):
     close(y[under], ref[under], e[under], torch.float16, "finite results")
     u = call(hif4, x, w, b, act=1, residual=res, res_scale=2.0, units=True, dtype=torch.float16)
     assert torch.equal(u, hif4.hif4_quantize(y))
+
+
+# -------------------------------------------------------------------------------------------------- rows past 65535 x 32
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_gradient_without_activation_of_two_million_rows(hif4, dtype):
+    M, N, K = 65535 * 32 + 33, 8, 64
+    _, w, _ = operands(hif4, 1, N, K, dtype, False, 3)
+    dy = torch.randn(M, N, device="cuda").to(dtype)
+    dx, db = hif4.hif4_linear_act_backward(dy, None, w[0], want_dbias=True)
+    wd = decode(hif4, w[0])
+    for r in range(0, M, 1 << 19):
+        d = dy[r:r + (1 << 19)].double()
+        close(dx[r:r + (1 << 19)], d @ wd, (TOL + 2.0 ** -16) * (d.abs() @ wd.abs()), dtype, f"dx from {r}")
+    # 32 rows in series, then 2049 row blocks for each of 32 ways, then the ways
+    close(db, dy.double().sum(0), 2.0 ** -24 * (32 + 2049 + 32) * dy.double().abs().sum(0), torch.float32, "dbias")
