@@ -208,7 +208,8 @@ typedef enum {
   HIF4_ACT_SILU = 2,       /* z / (1 + e^-z)                                         */
   HIF4_ACT_GELU = 3,       /* z Phi(z), Phi the normal distribution function         */
   HIF4_ACT_GELU_TANH = 4   /* z (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3))) / 2        */
-} hif4_activation;
+} hif4_activation;         /* within (8 + 2 |e|) 2^-22 of the value in FP32, e the formula's exponent: -z (SiLU), z^2 / 2 (GELU), twice
+                              the argument of tanh; a sigmoid below 2^-126 is zero */
 
 /* hif4_block_norm -- the norms around a block with its gate and residual, per row of `cols` elements:
  *     h = res_scale * residual + gate[row / rows_per_gate] * post(x)

@@ -129,3 +129,59 @@ def test_gradient_without_activation_of_two_million_rows(hif4, dtype):
         close(dx[r:r + (1 << 19)], d @ wd, (TOL + 2.0 ** -16) * (d.abs() @ wd.abs()), dtype, f"dx from {r}")
     # 32 rows in series, then 2049 row blocks for each of 32 ways, then the ways
     close(db, dy.double().sum(0), 2.0 ** -24 * (32 + 2049 + 32) * dy.double().abs().sum(0), torch.float32, "dbias")
+
+
+# ----------------------------------------------------------------------------------------------------- activations alone
+def exponent(z, act):
+    if act == 2:
+        return z.abs()
+    if act == 3:
+        return z * z / 2
+    if act == 4:
+        return (2 * (2 / torch.pi) ** 0.5 * (z + 0.044715 * z ** 3)).abs()
+    return torch.zeros_like(z)
+
+
+def value_and_slope64(z, act):
+    """The tanh form as z times a sigmoid of 2u: 1 + tanh(u) and 1 - tanh(u)^2 cancel in the left tail, in 64 bits too."""
+    if act != 4:
+        return act64(z, act)
+    c = 2 * (2 / torch.pi) ** 0.5
+    s = torch.sigmoid(c * (z + 0.044715 * z ** 3))
+    r = torch.sigmoid(-c * (z + 0.044715 * z ** 3))
+    return z * s, s + z * s * r * c * (1 + 3 * 0.044715 * z * z)
+
+
+@pytest.mark.parametrize("act", range(5))
+@pytest.mark.parametrize("gated", [False, True])
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("M,K", [(1, 256), (40, 256), (2, 0)])
+def test_activation_of_a_bias(hif4, act, gated, dtype, M, K):
+    """Zero activations leave act(bias) alone, from the streaming form, the tensor-core form and without a contraction."""
+    N = 1024
+    x, w, _ = operands(hif4, M, N, 256, dtype, gated, 2)
+    b = [torch.linspace(-12.0, 12.0, N, device="cuda").to(dtype), torch.full((N,), 3.0, dtype=dtype, device="cuda")][:len(w)]
+    y = call(hif4, torch.zeros_like(x)[:, :K].contiguous(), [t[:, :K // 64].contiguous() for t in w], b, act=act)
+    z = b[0].double()
+    a, _ = value_and_slope64(z, act)
+    up = 3.0 if gated else 1.0
+    err = up * ((8 + 2 * exponent(z, act)) * 2.0 ** -22 * a.abs() + z.abs() * 2.0 ** -126)
+    close(y, (up * a).expand(M, N), err.expand(M, N), dtype, f"act {act}")
+
+
+@pytest.mark.parametrize("act", range(1, 5))
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_slope_at_a_bias(hif4, act, dtype):
+    """One row of gradients of one: the bias gradient is act'(bias) in FP32.  Its two terms, the value's factor f and z f', carry the
+    activation's relative error each; for a sigmoid f of exponent e(z), z f' = z e' f (1 - f), so a sigmoid that is zero below 2^-126
+    leaves out up to (1 + |z e'|) 2^-126."""
+    N, K = 1024, 256
+    x, w, _ = operands(hif4, 1, N, K, dtype, False, 2)
+    b = torch.linspace(-12.0, 12.0, N, device="cuda").to(dtype)
+    _, db = hif4.hif4_linear_act_backward(torch.ones(1, N, dtype=dtype, device="cuda"), torch.zeros_like(x), w[0], b, act=act, want_dx=False, want_dbias=True)
+    z = b.double()
+    a, s = value_and_slope64(z, act)
+    rate = 2 * (2 / torch.pi) ** 0.5 * (1 + 3 * 0.044715 * z * z) if act == 4 else 1.0
+    first = torch.where(z == 0, torch.full_like(z, 0.5), a / torch.where(z == 0, torch.ones_like(z), z)).abs()
+    err = (8 + 2 * exponent(z, act)) * 2.0 ** -22 * (first + (s - first).abs()) + 2.0 ** -22 * first * z.abs() + (1 + z.abs() * rate) * 2.0 ** -126
+    close(db, s, err, torch.float32, f"slope {act}")
