@@ -321,8 +321,8 @@ hif4_status hif4_gated_linear(const hif4_linear_act_args* args, void* workspace,
  *     dZ = dY * act'(Z),  dX = dZ * W,  dbias = sum over the rows of dZ
  *     dG = dY * U * act'(G),  dU = dY * act(G),  dX = dG * W + dU * W_up,  dbias = sum dG,  dbias_up = sum dU
  * (the residual's gradient is res_scale * dY).  dZ, dG and dU enter the last product as sums of BF16 numbers: one for
- * BF16 gradients, two for FP16 (which hold its 11 bits); sums of biases run over the unrounded values, in an order
- * that depends only on the sizes.  FP32 gradients are refused (HIF4_ERR_DTYPE).  */
+ * BF16 gradients (two with `precise`), two for FP16 (which hold its 11 bits); sums of biases run over the unrounded values,
+ * in an order that depends only on the sizes.  FP32 gradients are refused (HIF4_ERR_DTYPE).  */
 typedef struct {
   int64_t M, N, K;
   const void* X;                 /* as in the forward pass; not read by hif4_linear_act_backward for act NONE   */
@@ -342,6 +342,7 @@ typedef struct {
   int64_t ld_dx;
   float* dbias;                  /* device, [N], or NULL; overwritten                                          */
   float* dbias_up;
+  int precise;                   /* 1: dZ, dG and dU as two BF16 numbers for BF16 gradients too                 */
 } hif4_linear_act_backward_args;
 hif4_status hif4_linear_act_backward_workspace(const hif4_linear_act_backward_args* args, size_t* bytes);
 hif4_status hif4_linear_act_backward(const hif4_linear_act_backward_args* args, void* workspace, size_t workspace_bytes,

@@ -429,28 +429,29 @@ def hif4_gated_linear(x: torch.Tensor, w_units: torch.Tensor, w_up_units: torch.
 
 def hif4_linear_act_backward(dy: torch.Tensor, x: Optional[torch.Tensor], w_units: torch.Tensor,
                              bias: Optional[torch.Tensor] = None, *, act: int = HIF4_ACT_NONE, mode: int = HIF4_RNE,
-                             want_dx: bool = True, want_dbias: bool = False, workspace: Optional[torch.Tensor] = None,
-                             stream=None):
+                             want_dx: bool = True, want_dbias: bool = False, precise: bool = False,
+                             workspace: Optional[torch.Tensor] = None, stream=None):
     """(dx, dbias) of hif4_linear_act from dy (BF16 or FP16): dx in the type of dy, dbias FP32; None where not wanted.  The
-    residual's gradient is res_scale * dy.  x may be None for act = HIF4_ACT_NONE."""
+    residual's gradient is res_scale * dy.  x may be None for act = HIF4_ACT_NONE.  For BF16, dy * act'(z) is rounded to BF16 before
+    its product with the weights; precise=True keeps 16 bits of it and multiplies twice (FP16 does so always)."""
     if stream is not None:
         return _under(stream, hif4_linear_act_backward, locals())
     dx, db, _ = _result("hif4_linear_act_backward", _native.linear_act_backward(dy, x, w_units, None, bias, None, act, mode, want_dx,
-                                                                                want_dbias, workspace))
+                                                                                want_dbias, precise, workspace))
     return dx, db
 
 
 def hif4_gated_linear_backward(dy: torch.Tensor, x: torch.Tensor, w_units: torch.Tensor, w_up_units: torch.Tensor,
                                bias: Optional[torch.Tensor] = None, bias_up: Optional[torch.Tensor] = None, *,
                                act: int = HIF4_ACT_SILU, mode: int = HIF4_RNE, want_dx: bool = True, want_dbias: bool = False,
-                               workspace: Optional[torch.Tensor] = None, stream=None):
+                               precise: bool = False, workspace: Optional[torch.Tensor] = None, stream=None):
     """(dx, dbias, dbias_up) of hif4_gated_linear from dy (BF16 or FP16); as hif4_linear_act_backward."""
     if stream is not None:
         return _under(stream, hif4_gated_linear_backward, locals())
     if w_up_units is None:
         raise TypeError("w_up_units: a tensor expected")
     return _result("hif4_gated_linear_backward", _native.linear_act_backward(dy, x, w_units, w_up_units, bias, bias_up, act, mode, want_dx,
-                                                                             want_dbias, workspace))
+                                                                             want_dbias, precise, workspace))
 
 
 def hif4_debug_wait_timeout(budget_ns: int, stream=None) -> None:

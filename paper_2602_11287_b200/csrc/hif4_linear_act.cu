@@ -99,7 +99,7 @@ hif4_status backward_plan(const hif4_linear_act_backward_args* a, bool gated, Ba
   if (a->M < 0 || a->N < 0 || a->K < 0 || a->K % kUnitElems != 0) return HIF4_ERR_SHAPE;
   if (a->M == 0 || a->N == 0) return HIF4_OK;
   s.recompute = gated || a->act != HIF4_ACT_NONE;
-  s.parts = a->dt == HIF4_FP16 ? 2 : 1;
+  s.parts = a->dt == HIF4_FP16 || (a->precise && s.recompute) ? 2 : 1;      // (dZ = dY of BF16 is one BF16 number)
   s.phases = s.parts * (gated ? 2 : 1);
   s.ld_dz = (a->N + 7) / 8 * 8;
   if (!linear_tc2_supported(gated, a->M, a->N, a->K) || !input_grad_tc2_supported(a->M, a->N, a->K, s.phases)) return HIF4_ERR_SHAPE;
@@ -224,7 +224,7 @@ hif4_status backward(const hif4_linear_act_backward_args* args, bool gated, void
     }
     c.dt = a->dt; c.bias = a->bias; c.bias_up = gated ? a->bias_up : nullptr; c.act = a->act;
     c.side = a->dY; c.ld_side = a->ld_dy;
-    c.dz = dz; c.ld_dz = s.ld_dz; c.dz_plane = a->M * s.ld_dz;
+    c.dz = dz; c.ld_dz = s.ld_dz; c.dz_plane = a->M * s.ld_dz; c.parts = s.parts;
     c.colsum = colsum;
     const hif4_status pr = launch_linear_tc2_grad(c, ws + s.pair, st);
     if (pr != HIF4_OK) return pr;

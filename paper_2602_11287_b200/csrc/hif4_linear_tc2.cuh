@@ -224,8 +224,9 @@ __device__ __forceinline__ void store_parts(const float (&v)[16], __nv_bfloat16*
 }
 
 // kGated: two projections.  kGrad: the gradient form.  T: type of bias, residual, Y and dY.  kAct: the activation (one kernel
-// each: five activations side by side cost the epilogue spills and instruction-cache misses).
-template <bool kGated, bool kGrad, typename T, int kAct>
+// each: five activations side by side cost the epilogue spills and instruction-cache misses).  kParts: BF16 numbers per element of
+// dZ (gradient form; see InputGradCall).
+template <bool kGated, bool kGrad, typename T, int kAct, int kParts>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 linear_tc2_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
                   const __grid_constant__ CUtensorMap tmB2, const __grid_constant__ CUtensorMap tmY,
@@ -576,7 +577,6 @@ linear_tc2_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
                 if (kGated) u[e] = row_ok ? s[e] * a[e] : 0.0f;
               }
               const int64_t col = static_cast<int64_t>(w.n0) + c;
-              constexpr int kParts = IsHalf<T>::value ? 2 : 1;
               if (p.dz && row_ok) {
                 __nv_bfloat16* dst = p.dz + row * p.ld_dz + col;
                 store_parts<kParts>(z, dst, p.dz_plane, 16);
@@ -739,7 +739,6 @@ linear_tc2_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
                 z[e] = in ? s[e] * z[e] * (kGated ? u[e] : 1.0f) : 0.0f;
                 if (kGated) u[e] = in ? s[e] * a[e] : 0.0f;
               }
-              constexpr int kParts = IsHalf<T>::value ? 2 : 1;
               if (p.dz && row_ok) {
                 __nv_bfloat16* dst = p.dz + row * p.ld_dz + col;
                 store_parts<kParts>(z, dst, p.dz_plane, p.ld_dz - col);

@@ -48,11 +48,11 @@ inline size_t partial_tiles(const Tc2Plan& pl) {
 }
 constexpr size_t kPartialTileBytes = static_cast<size_t>(kPairM) * kPairN * sizeof(float);
 
-template <bool kGated, bool kGrad, typename T, int kAct>
-hif4_status launch_linear_act(const LinearCall& c, void* workspace, cudaStream_t st) {
+template <bool kGated, bool kGrad, typename T, int kAct, int kParts>
+hif4_status launch_linear_parts(const LinearCall& c, void* workspace, cudaStream_t st) {
   constexpr int kTileN = kGated ? kPairN / 2 : kPairN;
   static uint64_t smem_opt_in = 0;
-  if (!ensure_dynamic_smem(linear_tc2_kernel<kGated, kGrad, T, kAct>, kLinSmemBytes, smem_opt_in)) return HIF4_ERR_CUDA;
+  if (!ensure_dynamic_smem(linear_tc2_kernel<kGated, kGrad, T, kAct, kParts>, kLinSmemBytes, smem_opt_in)) return HIF4_ERR_CUDA;
   LinearParams p{};
   p.M = c.M; p.N = c.N;
   p.error_word = device_error_word();
@@ -93,7 +93,16 @@ hif4_status launch_linear_act(const LinearCall& c, void* workspace, cudaStream_t
     p.partial = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + pl.flag_bytes);
   }
   const int pairs = p.full_rounds == 0 && p.sk_tiles == 0 ? p.tail_tiles * p.slices : pl.pairs;      // a single round: one pair per slice
-  return launch_overlapped(linear_tc2_kernel<kGated, kGrad, T, kAct>, 2 * pairs, kThreads, kLinSmemBytes, st, tmA, tmB, tmB2, tmY, tmSide, p);
+  return launch_overlapped(linear_tc2_kernel<kGated, kGrad, T, kAct, kParts>, 2 * pairs, kThreads, kLinSmemBytes, st, tmA, tmB, tmB2, tmY, tmSide, p);
+}
+
+template <bool kGated, bool kGrad, typename T, int kAct>
+hif4_status launch_linear_act(const LinearCall& c, void* workspace, cudaStream_t st) {
+  if constexpr (kGrad && IsHalf<T>::value) return launch_linear_parts<kGated, kGrad, T, kAct, 2>(c, workspace, st);
+  if constexpr (kGrad && !IsHalf<T>::value) {
+    if (c.parts == 2) return launch_linear_parts<kGated, kGrad, T, kAct, 2>(c, workspace, st);
+  }
+  return launch_linear_parts<kGated, kGrad, T, kAct, 1>(c, workspace, st);
 }
 
 template <bool kGated, bool kGrad, typename T>

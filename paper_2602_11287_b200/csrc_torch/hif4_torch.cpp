@@ -348,12 +348,12 @@ PyObject* linear_act(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
-// (dy, x, w_units, w_up_units, bias, bias_up, act, mode, want_dx, want_dbias, workspace) -> (dx, dbias, dbias_up)
+// (dy, x, w_units, w_up_units, bias, bias_up, act, mode, want_dx, want_dbias, precise, workspace) -> (dx, dbias, dbias_up)
 PyObject* linear_act_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  return guarded(n, 11, [&]() -> PyObject* {
+  return guarded(n, 12, [&]() -> PyObject* {
     const at::Tensor &dy = tensor(a[0], "dy"), &w = tensor(a[2], "w_units");
     const at::Tensor *x = tensor_or_null(a[1], "x"), *wu = tensor_or_null(a[3], "w_up_units"), *b = tensor_or_null(a[4], "bias"),
-                     *bu = tensor_or_null(a[5], "bias_up"), *ws = tensor_or_null(a[10], "workspace");
+                     *bu = tensor_or_null(a[5], "bias_up"), *ws = tensor_or_null(a[11], "workspace");
     const OnDeviceOf on(dy);
     if (dy.dim() != 2) throw std::invalid_argument("dy: a matrix expected");
     if (w.dim() != 3) throw std::invalid_argument("w_units: units [N, K / 64, 36] expected, got " + about(w));
@@ -388,8 +388,9 @@ PyObject* linear_act_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
     p.dX = at_of<void>(dx); p.ld_dx = K;
     p.dbias = at_of<float>(db);
     p.dbias_up = at_of<float>(dbu);
+    p.precise = truth(a[10]) ? 1 : 0;
     hif4_status s;
-    const size_t need = workspace_bytes(wu ? 3 : 2, dy.device().index(), {M, N, K, p.x_units, p.dt, p.act == HIF4_ACT_NONE}, s,
+    const size_t need = workspace_bytes(wu ? 3 : 2, dy.device().index(), {M, N, K, p.x_units, p.dt, (p.act == HIF4_ACT_NONE) + 2 * p.precise}, s,
                                         reinterpret_cast<hif4_status (*)(const void*, size_t*)>(wu ? hif4_gated_linear_backward_workspace : hif4_linear_act_backward_workspace), &p);
     if (s != HIF4_OK) return status(s);
     const Workspace space(ws, need, dy);

@@ -7,7 +7,7 @@ roundings around them, and e times the rounding of the exponent itself.  A sigmo
 import pytest
 import torch
 
-from tests.test_gpu_linear_act import FN, TINY, TOL, TYPES, U, act64, call, close, decode, expect_forward, hif4, operands  # noqa: F401
+from tests.test_gpu_linear_act import FN, TINY, TOL, TYPES, U, act64, call, close, decode, expect_forward, hif4, operands, products64  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -185,3 +185,32 @@ def test_slope_at_a_bias(hif4, act, dtype):
     first = torch.where(z == 0, torch.full_like(z, 0.5), a / torch.where(z == 0, torch.ones_like(z), z)).abs()
     err = (8 + 2 * exponent(z, act)) * 2.0 ** -22 * (first + (s - first).abs()) + 2.0 ** -22 * first * z.abs() + (1 + z.abs() * rate) * 2.0 ** -126
     close(db, s, err, torch.float32, f"slope {act}")
+
+
+# ---------------------------------------------------------------------------------------------- dZ as one or two numbers
+@pytest.mark.parametrize("gated", [False, True])
+@pytest.mark.parametrize("act", [0, 1, 2, 3, 4])
+@pytest.mark.parametrize("M,N,K", [(1, 64, 256), (40, 1000, 320), (300, 513, 512), (130, 4096, 256)])
+def test_precise_gradient(hif4, gated, act, M, N, K):
+    """BF16 with dZ in two parts: 2^-16 of it in the product's error where one part leaves 2^-8; bias gradients keep their bits."""
+    x, w, b = operands(hif4, M, N, K, torch.bfloat16, gated, M + N)
+    dy = torch.randn(M, N, device="cuda").to(torch.bfloat16)
+    f = hif4.hif4_gated_linear_backward if gated else hif4.hif4_linear_act_backward
+    one, two, again = (f(dy, x, *w, *b, act=act, want_dbias=True, precise=p) for p in (False, True, True))
+    assert all(torch.equal(a, v) for a, v in zip(two, again)) and all(torch.equal(a, v) for a, v in zip(one[1:], two[1:]))
+    p = products64(hif4, x, w, b)
+    z, ez, wg = p[0]
+    a, s = act64(z, act)
+    D = dy.double()
+    es = 2 * ez + FN * (s.abs() + z.abs()) if act else torch.zeros_like(z)
+    if act == 1:
+        es = es + (z.abs() <= ez).double()                    # the step at zero
+    if gated:
+        u, eu, wu = p[1]
+        grads = [(D * u * s, D.abs() * (es * (u.abs() + eu) + s.abs() * eu), wg), (D * a, D.abs() * (1.2 * ez + FN * a.abs()), wu)]
+    else:
+        grads = [(D * s, D.abs() * es, wg)]
+    ref = sum(dz @ wd for dz, _, wd in grads)
+    err = sum((e + (2.0 ** -16 + TOL) * dz.abs()) @ wd.abs() for dz, e, wd in grads)
+    close(two[0], ref, err, torch.bfloat16, "dx")
+    assert float((two[0].double() - ref).norm()) <= float((one[0].double() - ref).norm())
