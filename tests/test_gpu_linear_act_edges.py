@@ -213,4 +213,5 @@ def test_precise_gradient(hif4, gated, act, M, N, K):
     ref = sum(dz @ wd for dz, _, wd in grads)
     err = sum((e + (2.0 ** -16 + TOL) * dz.abs()) @ wd.abs() for dz, e, wd in grads)
     close(two[0], ref, err, torch.bfloat16, "dx")
-    assert float((two[0].double() - ref).norm()) <= float((one[0].double() - ref).norm())
+    if gated or act > 1:                                      # else dZ is dY or zero: one BF16 number holds it
+        assert float((two[0].double() - ref).norm()) <= float((one[0].double() - ref).norm())
