@@ -143,6 +143,7 @@ struct Workspace {
   Workspace(const at::Tensor* given, size_t need, const at::Tensor& like) {
     if (given) {
       need_cuda(*given);
+      if (!given->is_contiguous()) throw std::invalid_argument("workspace: contiguous memory expected, got " + about(*given));
       p = given->data_ptr();
       bytes = given->nbytes();
     } else if (need > 0) {

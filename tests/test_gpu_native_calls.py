@@ -1,0 +1,24 @@
+"""What the native calls do with arguments that are not what they should be, and with outputs that are not wanted."""
+import pytest
+import torch
+
+from tests.test_gpu_block_norm import hif4, make  # noqa: F401
+from tests.test_gpu_linear_act import operands
+
+pytestmark = pytest.mark.gpu
+
+
+def test_a_workspace_is_as_large_as_its_memory(hif4):
+    """An expanded tensor counts more elements than it holds: it is no workspace."""
+    x, w, b = operands(hif4, 64, 256, 512, torch.bfloat16, False, 3)
+    dy = torch.zeros(64, 256, dtype=torch.bfloat16, device="cuda")
+    n = torch.zeros(512, 512, dtype=torch.bfloat16, device="cuda")
+    expanded = torch.empty(1, dtype=torch.uint8, device="cuda").expand(1 << 28)
+    before = hif4.launch_count()
+    for f in (lambda: hif4.hif4_linear_act(x, w[0], workspace=expanded), lambda: hif4.hif4_linear_act_backward(dy, x, w[0], act=2, workspace=expanded),
+              lambda: hif4.hif4_block_norm_backward(n, n, None, workspace=expanded)):
+        with pytest.raises(ValueError):
+            f()
+    assert hif4.launch_count() == before
+    space = torch.empty(1 << 26, dtype=torch.float32, device="cuda")
+    assert torch.equal(hif4.hif4_linear_act(x, w[0], workspace=space), hif4.hif4_linear_act(x, w[0]))
