@@ -35,6 +35,11 @@ int64_t integer(PyObject* o) {
   if (v == -1 && PyErr_Occurred()) throw TypeProblem("an integer expected");
   return v;
 }
+// A code of an enumeration; one that no int holds is none of them.
+int code(PyObject* o) {
+  const int64_t v = integer(o);
+  return v < 0 || v > 0x7FFFFFFF ? -1 : static_cast<int>(v);
+}
 double real(PyObject* o) {
   const double v = PyFloat_AsDouble(o);
   if (v == -1.0 && PyErr_Occurred()) throw TypeProblem("a number expected");
@@ -177,14 +182,14 @@ PyObject* block_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
     p.rows_per_gate = integer(a[6]);
     const Mat mg = gates(gate, rows, cols, p.rows_per_gate, type);
     p.gate = mg.p; p.ld_gate = mg.ld;
-    p.post = static_cast<hif4_norm_kind>(integer(a[7]));
+    p.post = static_cast<hif4_norm_kind>(code(a[7]));
     p.post_weight = vector(wp, cols, wtype, "post_weight");
-    p.pre = static_cast<hif4_norm_kind>(integer(a[9]));
+    p.pre = static_cast<hif4_norm_kind>(code(a[9]));
     p.pre_weight = vector(w, cols, wtype, "weight");
     p.pre_bias = vector(b, cols, wtype, "bias");
     p.eps = static_cast<float>(real(a[10]));
     p.y_units = truth(a[11]) ? 1 : 0;
-    p.mode = static_cast<hif4_round>(integer(a[12]));
+    p.mode = static_cast<hif4_round>(code(a[12]));
     at::Tensor h, y;
     if (out_h) h = *out_h;
     else if (res || gate || p.post != HIF4_NORM_NONE) h = new_rows(rows, cols, type, x);
@@ -242,9 +247,9 @@ PyObject* block_norm_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
     p.rows_per_gate = integer(a[8]);
     const Mat mg = gates(gate, rows, cols, p.rows_per_gate, type);
     p.gate = mg.p; p.ld_gate = mg.ld;
-    p.post = static_cast<hif4_norm_kind>(integer(a[9]));
+    p.post = static_cast<hif4_norm_kind>(code(a[9]));
     p.post_weight = vector(wp, cols, wtype, "post_weight");
-    p.pre = static_cast<hif4_norm_kind>(integer(a[11]));
+    p.pre = static_cast<hif4_norm_kind>(code(a[11]));
     p.pre_weight = vector(w, cols, wtype, "weight");
     p.eps = static_cast<float>(real(a[12]));
     const auto sums = [&] { return at::empty({cols}, first->options().dtype(at::kFloat)); };
@@ -310,22 +315,22 @@ PyObject* linear_act(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const Activations act = activations(x);
     if (w.dim() != 3) throw std::invalid_argument("w_units: units [N, K / 64, 36] expected, got " + about(w));
     const int64_t M = act.rows, N = w.size(0), K = act.K;
-    const int code = static_cast<int>(integer(a[8]));
+    const int64_t out_type = integer(a[8]);
     const bool to_units = truth(a[9]);
-    const at::ScalarType type = code == HIF4_BF16 ? at::kBFloat16 : code == HIF4_FP32 ? at::kFloat : code == HIF4_FP16 ? at::kHalf
+    const at::ScalarType type = out_type == HIF4_BF16 ? at::kBFloat16 : out_type == HIF4_FP32 ? at::kFloat : out_type == HIF4_FP16 ? at::kHalf
                                 : out && !to_units ? out->scalar_type() : act.is_units ? at::kBFloat16 : x.scalar_type();
     hif4_linear_act_args p{};
     p.M = M; p.N = N; p.K = K;
     p.X = act.m.p; p.ld_x = act.m.ld;
     p.dt_x = static_cast<hif4_dtype>(act.dt);
     p.x_units = act.is_units;
-    p.mode = static_cast<hif4_round>(integer(a[10]));
+    p.mode = static_cast<hif4_round>(code(a[10]));
     p.W_units = units(&w, N, K / HIF4_UNIT_ELEMS, "w_units");
     p.W_up_units = units(wu, N, K / HIF4_UNIT_ELEMS, "w_up_units");
     p.dt = static_cast<hif4_dtype>(type_code(type));
     p.bias = vector(b, N, type, "bias");
     p.bias_up = vector(bu, N, type, "bias_up");
-    p.act = static_cast<hif4_activation>(integer(a[7]));
+    p.act = static_cast<hif4_activation>(code(a[7]));
     const Mat mr = matrix(res, M, N, type, "residual");
     p.residual = mr.p; p.ld_residual = mr.ld;
     p.res_scale = static_cast<float>(real(a[6]));
@@ -371,14 +376,14 @@ PyObject* linear_act_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
       p.dt_x = static_cast<hif4_dtype>(act.dt);
       p.x_units = act.is_units;
     }
-    p.mode = static_cast<hif4_round>(integer(a[7]));
+    p.mode = static_cast<hif4_round>(code(a[7]));
     p.W_units = units(&w, N, K / HIF4_UNIT_ELEMS, "w_units");
     p.W_up_units = units(wu, N, K / HIF4_UNIT_ELEMS, "w_up_units");
     const Mat mdy = matrix(&dy, M, N, type, "dy");
     p.dt = static_cast<hif4_dtype>(type_code(type));
     p.bias = vector(b, N, type, "bias");
     p.bias_up = vector(bu, N, type, "bias_up");
-    p.act = static_cast<hif4_activation>(integer(a[6]));
+    p.act = static_cast<hif4_activation>(code(a[6]));
     p.dY = mdy.p; p.ld_dy = mdy.ld;
     at::Tensor dx, db, dbu;
     if (truth(a[8])) dx = new_rows(M, K, type, dy);

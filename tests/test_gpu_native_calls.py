@@ -8,6 +8,23 @@ from tests.test_gpu_linear_act import operands
 pytestmark = pytest.mark.gpu
 
 
+def test_codes_past_32_bits_are_refused(hif4):
+    """2^32 + 1 is no code of a norm, an activation or a rounding, and not the code 1 either."""
+    x, r, gate, wp, w, b = make(4, 128, torch.bfloat16, torch.bfloat16, 1, 1, 0, True, 1)
+    far = 2 ** 32
+    xl, wl, bl = operands(hif4, 4, 64, 256, torch.bfloat16, True, 3)
+    dy = torch.zeros(4, 64, dtype=torch.bfloat16, device="cuda")
+    for f in (lambda: hif4.hif4_block_norm(x, w, pre=far + 1), lambda: hif4.hif4_block_norm(x, w, post=far + 1),
+              lambda: hif4.hif4_block_norm(x, w, mode=far), lambda: hif4.hif4_block_norm_backward(x, x, w, pre=far + 1),
+              lambda: hif4.hif4_block_norm_backward(x, x, w, x=x, post=far + 1),
+              lambda: hif4.hif4_linear_act(xl, wl[0], act=far + 2), lambda: hif4.hif4_linear_act(xl, wl[0], mode=far),
+              lambda: hif4.hif4_gated_linear(xl, *wl, act=far + 2), lambda: hif4.hif4_linear_act_backward(dy, xl, wl[0], act=far + 2),
+              lambda: hif4.hif4_gated_linear_backward(dy, xl, *wl, mode=far)):
+        with pytest.raises(hif4.Hif4Error) as e:
+            f()
+        assert e.value.code == 4
+
+
 def test_a_workspace_is_as_large_as_its_memory(hif4):
     """An expanded tensor counts more elements than it holds: it is no workspace."""
     x, w, b = operands(hif4, 64, 256, 512, torch.bfloat16, False, 3)
