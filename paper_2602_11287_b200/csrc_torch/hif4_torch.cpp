@@ -45,7 +45,11 @@ double real(PyObject* o) {
   if (v == -1.0 && PyErr_Occurred()) throw TypeProblem("a number expected");
   return v;
 }
-bool truth(PyObject* o) { return PyObject_IsTrue(o) == 1; }
+bool truth(PyObject* o) {
+  const int v = PyObject_IsTrue(o);
+  if (v < 0) throw TypeProblem("true or false expected");      // the object's own exception is set, and kept
+  return v == 1;
+}
 
 std::string about(const at::Tensor& t) {
   std::string s = "[";

@@ -25,6 +25,14 @@ def test_codes_past_32_bits_are_refused(hif4):
         assert e.value.code == 4
 
 
+def test_a_flag_that_is_neither_true_nor_false(hif4):
+    x = torch.zeros(4, 128, dtype=torch.bfloat16, device="cuda")
+    two = torch.ones(2)
+    for f in (lambda: hif4.hif4_block_norm(x, None, units=two), lambda: hif4.hif4_block_norm_backward(x, x, None, want_dresidual=two)):
+        with pytest.raises(RuntimeError, match="ambiguous"):
+            f()
+
+
 def test_a_workspace_is_as_large_as_its_memory(hif4):
     """An expanded tensor counts more elements than it holds: it is no workspace."""
     x, w, b = operands(hif4, 64, 256, 512, torch.bfloat16, False, 3)
