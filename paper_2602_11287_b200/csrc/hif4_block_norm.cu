@@ -727,7 +727,8 @@ extern "C" hif4_status hif4_block_norm(const hif4_block_norm_args* a, void* stre
   p.kind_pre = a->pre; p.kind_post = a->post; p.dt_w = a->dt_w;
   p.x = a->x; p.residual = a->residual; p.gate = a->gate;
   p.post_weight = a->post_weight; p.pre_weight = a->pre_weight; p.pre_bias = a->pre_bias;
-  p.ld_x = a->ld_x; p.ld_residual = a->ld_residual; p.ld_gate = a->ld_gate; p.rows_per_gate = a->rows_per_gate;
+  p.ld_x = a->ld_x; p.ld_residual = a->ld_residual; p.ld_gate = a->ld_gate;
+  p.rows_per_gate = a->rows_per_gate < a->rows ? a->rows_per_gate : a->rows;      // (no product with it overflows)
   p.res_scale = a->res_scale; p.eps = a->eps;
   p.h = a->h; p.y = a->y; p.ld_h = a->ld_h; p.ld_y = a->ld_y;
   p.units = a->y_units ? 1 : 0; p.rha = a->mode == HIF4_RHA;
@@ -784,7 +785,7 @@ extern "C" hif4_status hif4_block_norm_backward(const hif4_block_norm_backward_a
   p.dy = a->dy; p.dh = a->dh; p.h = a->h; p.x = wants_x ? a->x : nullptr; p.gate = a->gate;
   p.post_weight = a->post_weight; p.pre_weight = a->pre_weight;
   p.ld_dy = a->ld_dy; p.ld_dh = a->ld_dh; p.ld_h = a->ld_h; p.ld_x = a->ld_x; p.ld_gate = a->ld_gate;
-  p.rows_per_gate = a->gate ? a->rows_per_gate : 1;
+  p.rows_per_gate = !a->gate ? 1 : a->rows_per_gate < a->rows ? a->rows_per_gate : a->rows;      // (no product with it overflows)
   p.res_scale = a->res_scale; p.eps = a->eps;
   p.dx = a->dx; p.dresidual = a->dresidual; p.dgate = a->dgate; p.ld_dx = a->ld_dx; p.ld_dresidual = a->ld_dresidual;
   p.dpre_weight = a->dpre_weight; p.dpre_bias = a->dpre_bias; p.dpost_weight = a->dpost_weight;

@@ -109,7 +109,7 @@ void* units(const at::Tensor* t, int64_t rows, int64_t n, const char* what) {
 Mat gates(const at::Tensor* t, int64_t rows, int64_t cols, int64_t per, at::ScalarType type) {
   if (!t) return {nullptr, 0};
   if (per < 1) throw std::invalid_argument("a gate needs rows_per_gate >= 1");
-  return matrix(t, (rows + per - 1) / per, cols, type, "gate");
+  return matrix(t, rows / per + (rows % per != 0), cols, type, "gate");
 }
 at::Tensor new_rows(int64_t rows, int64_t cols, at::ScalarType type, const at::Tensor& like) {
   return at::empty({rows, cols}, like.options().dtype(type));

@@ -33,6 +33,18 @@ def test_a_flag_that_is_neither_true_nor_false(hif4):
             f()
 
 
+def test_one_row_of_gates_for_any_number_of_rows(hif4):
+    x, r, gate, wp, w, b = make(50, 320, torch.bfloat16, torch.bfloat16, 1, 1, 50, True, 1)
+    kw = dict(gate=gate, post=1, post_weight=wp)
+    want = hif4.hif4_block_norm(x, w, residual=r, rows_per_gate=50, **kw)
+    dwant = hif4.hif4_block_norm_backward(x, want[0], w, dh=r, x=x, rows_per_gate=50, **kw)
+    for per in (51, 2 ** 31, 2 ** 63 - 1):
+        got = hif4.hif4_block_norm(x, w, residual=r, rows_per_gate=per, **kw)
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+        d = hif4.hif4_block_norm_backward(x, want[0], w, dh=r, x=x, rows_per_gate=per, **kw)
+        assert all(torch.equal(d[k], v) for k, v in dwant.items() if v is not None)
+
+
 def test_a_workspace_is_as_large_as_its_memory(hif4):
     """An expanded tensor counts more elements than it holds: it is no workspace."""
     x, w, b = operands(hif4, 64, 256, 512, torch.bfloat16, False, 3)
