@@ -385,15 +385,17 @@ def hif4_block_norm_backward(dy: Optional[torch.Tensor], h: Optional[torch.Tenso
                              dh: Optional[torch.Tensor] = None, x: Optional[torch.Tensor] = None, bias: bool = False,
                              res_scale: float = 1.0, gate: Optional[torch.Tensor] = None, rows_per_gate: int = 0,
                              post: int = HIF4_NORM_NONE, post_weight: Optional[torch.Tensor] = None,
-                             pre: int = HIF4_NORM_RMS, eps: float = 1e-5, want_dresidual: bool = True,
+                             pre: int = HIF4_NORM_RMS, eps: float = 1e-5, want_dx: bool = True, want_dresidual: bool = True,
+                             want_dgate: bool = True, want_dweights: bool = True,
                              workspace: Optional[torch.Tensor] = None, stream=None) -> dict:
     """Gradients of hif4_block_norm from those of its outputs (dy, dh) and the stored h (and x, where there is a post norm
-    or a gate): a dict of dx, dresidual, dgate, dweight, dbias (with bias=True) and dpost_weight; None where the
-    forward call had no such input."""
+    or a gate): a dict of dx, dresidual, dgate, and with want_dweights dweight, dbias (with bias=True) and dpost_weight; None
+    where the forward call had no such input or the gradient is not wanted."""
     if stream is not None:
         return _under(stream, hif4_block_norm_backward, locals())
+    wanted = (1 if want_dx else 0) + (2 if want_dresidual else 0) + (4 if want_dgate else 0) + (8 if want_dweights else 0)
     r = _result("hif4_block_norm_backward", _native.block_norm_backward(
-        dy, h, weight, dh, x, bias, res_scale, gate, rows_per_gate, post, post_weight, pre, eps, want_dresidual, workspace))
+        dy, h, weight, dh, x, bias, res_scale, gate, rows_per_gate, post, post_weight, pre, eps, wanted, workspace))
     return dict(zip(("dx", "dresidual", "dgate", "dweight", "dbias", "dpost_weight"), r))
 
 

@@ -778,6 +778,7 @@ extern "C" hif4_status hif4_block_norm_backward(const hif4_block_norm_backward_a
   if (chk_w != HIF4_OK) return chk_w;
   if (!workspace || workspace_bytes < need) return HIF4_ERR_WORKSPACE;
   if (!aligned_to(workspace, 256)) return HIF4_ERR_ALIGN;
+  if (!a->dx && !a->dresidual && !a->dgate && !a->dpre_weight && !a->dpre_bias && !a->dpost_weight) return HIF4_OK;
   vec = vec && vec_w;
   NormGradParams p{};
   p.rows = a->rows; p.cols = static_cast<int>(a->cols);

@@ -224,7 +224,8 @@ PyObject* block_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
-// (dy, h, weight, dh, x, bias, res_scale, gate, rows_per_gate, post, post_weight, pre, eps, want_dresidual, workspace)
+// (dy, h, weight, dh, x, bias, res_scale, gate, rows_per_gate, post, post_weight, pre, eps, wanted, workspace), `wanted` the sum of
+// 1 (dx), 2 (dresidual), 4 (dgate) and 8 (weights and bias)
 //   -> (dx, dresidual, dgate, dweight, dbias, dpost_weight)
 PyObject* block_norm_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded(n, 15, [&]() -> PyObject* {
@@ -257,13 +258,15 @@ PyObject* block_norm_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
     p.pre_weight = vector(w, cols, wtype, "weight");
     p.eps = static_cast<float>(real(a[12]));
     const auto sums = [&] { return at::empty({cols}, first->options().dtype(at::kFloat)); };
+    const int64_t wanted = integer(a[13]);
+    const bool weights = (wanted & 8) != 0, has_bias = truth(a[5]);
     at::Tensor d[6];
-    d[0] = new_rows(rows, cols, type, *first);
-    if (truth(a[13])) d[1] = new_rows(rows, cols, type, *first);
-    if (gate) d[2] = new_rows(gate->size(0), cols, type, *first);
-    if (w && dy) d[3] = sums();
-    if (truth(a[5]) && dy) d[4] = sums();
-    if (wp) d[5] = sums();
+    if (wanted & 1) d[0] = new_rows(rows, cols, type, *first);
+    if (wanted & 2) d[1] = new_rows(rows, cols, type, *first);
+    if (gate && (wanted & 4)) d[2] = new_rows(gate->size(0), cols, type, *first);
+    if (w && dy && weights) d[3] = sums();
+    if (has_bias && dy && weights) d[4] = sums();
+    if (wp && weights) d[5] = sums();
     p.dx = at_of<void>(d[0]); p.ld_dx = cols;
     p.dresidual = at_of<void>(d[1]); p.ld_dresidual = cols;
     p.dgate = at_of<void>(d[2]);

@@ -59,3 +59,22 @@ def test_a_workspace_is_as_large_as_its_memory(hif4):
     assert hif4.launch_count() == before
     space = torch.empty(1 << 26, dtype=torch.float32, device="cuda")
     assert torch.equal(hif4.hif4_linear_act(x, w[0], workspace=space), hif4.hif4_linear_act(x, w[0]))
+
+
+@pytest.mark.parametrize("rows,cols", [(90, 320), (70, 1001), (700, 4096), (400, 10240)])
+@pytest.mark.parametrize("post,pre,rpg", [(0, 1, 0), (1, 1, 7), (2, 2, 0), (0, 2, 5)])
+def test_norm_gradients_that_are_not_wanted(hif4, rows, cols, post, pre, rpg):
+    """Each can be declined; the others keep their bits."""
+    x, r, gate, wp, w, b = make(rows, cols, torch.bfloat16, torch.bfloat16, post, pre, rpg, True, 3)
+    f = lambda **kw: hif4.hif4_block_norm_backward(x, r, w, dh=r, x=x, bias=b is not None, gate=gate, rows_per_gate=rpg, post=post,    # noqa: E731
+                                                   post_weight=wp, pre=pre, **kw)
+    full = f()
+    of = {"dx": "dx", "dresidual": "dresidual", "dgate": "dgate", "dweight": "dweights", "dbias": "dweights", "dpost_weight": "dweights"}
+    wants = ["dx", "dresidual", "dgate", "dweights"]
+    for off in [[k] for k in wants] + [[k for k in wants if k != keep] for keep in wants] + [wants]:
+        got = f(**{"want_" + k: False for k in off})
+        for k, v in full.items():
+            if v is None or of[k] in off:
+                assert got[k] is None, (off, k)
+            else:
+                assert torch.equal(got[k], v), (off, k)
