@@ -187,6 +187,36 @@ def test_slope_at_a_bias(hif4, act, dtype):
     close(db, s, err, torch.float32, f"slope {act}")
 
 
+# ------------------------------------------------------------------------------------------------------- captured graphs
+@pytest.mark.parametrize("gated", [False, True])
+@pytest.mark.parametrize("M,N,K", [(64, 512, 8192), (300, 4096, 1024), (2000, 2300, 512)])
+def test_pair_kernels_in_a_graph(hif4, M, N, K, gated):
+    """K slices, whole rounds and balanced rounds: the counts of finished parts are cleared by every replay."""
+    x, w, b = operands(hif4, M, N, K, torch.bfloat16, gated, 8)
+    dy = torch.randn(M, N, device="cuda").to(torch.bfloat16)
+    back = hif4.hif4_gated_linear_backward if gated else hif4.hif4_linear_act_backward
+    want, dwant = call(hif4, x, w, b, act=2), back(dy, x, *w, *b, act=2, want_dbias=True)
+    out = torch.empty_like(want)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        call(hif4, x, w, b, act=2, out=out)
+        back(dy, x, *w, *b, act=2, want_dbias=True)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call(hif4, x, w, b, act=2, out=out)
+        grads = back(dy, x, *w, *b, act=2, want_dbias=True)
+    for _ in range(3):
+        out.zero_()
+        for t in grads:
+            t.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want) and all(torch.equal(g, v) for g, v in zip(grads, dwant))
+    assert hif4.hif4_last_device_status() == 0
+
+
 # ---------------------------------------------------------------------------------------------- dZ as one or two numbers
 @pytest.mark.parametrize("gated", [False, True])
 @pytest.mark.parametrize("act", [0, 1, 2, 3, 4])
