@@ -627,7 +627,7 @@ linear_tc2_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
           }
         }
       } else if (leaves) {
-        // a part of the contraction: FP32 sums for the next slice (16 columns are 128 words of 16 bytes)
+        // a part of the contraction: FP32 sums for the last slice, which adds them all (16 columns are 128 words of 16 bytes)
         unsigned int left = 0;
 #pragma unroll 1
         for (int c = group * 16; c < cols; c += groups * 16, ++left) {

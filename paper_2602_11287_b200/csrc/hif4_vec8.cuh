@@ -14,10 +14,6 @@ namespace {
 template <typename T> struct Raw8 { uint4 a; };              // eight 16-bit elements as loaded
 template <> struct Raw8<float> { uint4 a, b; };
 
-// For code that a kernel of any type contains but only its 16-bit forms run: T where it has 16 bits, else BF16.
-template <typename T> struct SixteenBit { using type = T; };
-template <> struct SixteenBit<float> { using type = __nv_bfloat16; };
-template <typename T> using T16 = typename SixteenBit<T>::type;
 template <typename T> struct IsHalf { static constexpr bool value = false; };
 template <> struct IsHalf<__half> { static constexpr bool value = true; };
 
