@@ -332,7 +332,8 @@ def hif4_mse_roundtrip(src: torch.Tensor, fmt: int, want_image: bool = True, wor
 
 # ---------------------------------------------------------------------------------------- between two linears of a block
 # These calls go through the native module: its functions check the tensors (ValueError, TypeError), allocate what is not
-# passed in, and call the library on the current stream.
+# passed in, and call the library on the current stream.  They record nothing for autograd: the *_backward calls are there to be
+# called from a torch.autograd.Function (examples/ffn_block.py has one).
 _TYPE_CODES = {torch.bfloat16: HIF4_BF16, torch.float32: HIF4_FP32, torch.float16: HIF4_FP16}
 
 

@@ -3,7 +3,8 @@
 // loads to its stores, the row statistics are block-wide FP32 sums, and the result can leave as HiF4 units without the
 // 16-bit matrix being written.  Bound by HBM traffic (forward 6.6 - 8 bytes an element in 16 bits, backward 12).
 //
-// Instructions are the next bound after the loads, so the arithmetic runs in packed FP32 pairs.
+// Behind the loads comes the latency of a block's instruction stream, broken at every block-wide sum, so the arithmetic runs in packed
+// FP32 pairs.
 // A thread owns groups of eight columns (16-byte accesses when the matrices allow them; rows at odd addresses are read in
 // 16-byte words and shifted).  Blocks take contiguous runs
 // of rows and keep the next row's loads in flight while they reduce the current one; weights and gates are re-read

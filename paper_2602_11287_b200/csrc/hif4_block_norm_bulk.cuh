@@ -2,8 +2,9 @@
 // fills rows ahead with bulk copies, weights staged in shared memory once per block, and row loops without per-group
 // conditions.  (Included by hif4_block_norm.cu inside its namespace.)
 //
-// What bounds these kernels besides the traffic is a warp's instruction stream, about six cycles an instruction at the
-// 16 to 32 warps that registers allow.  So threads past the row's end compute on column 0 and are kept out of sums and
+// What bounds these kernels besides the traffic is the latency of a warp's instruction stream, about six cycles an instruction at the
+// 16 to 32 warps that registers allow, and of the block-wide sums in it (two or three a row one after another: the gradient with post
+// norm and gates issues in 41 % of the cycles, the forward pass in 57 %).  So threads past the row's end compute on column 0 and are kept out of sums and
 // stores only, absent weights are staged as ones, the stage is refilled behind the first sum's barrier, and pointers
 // advance by rows.  W: type of the weights, T or FP32.
 

@@ -16,9 +16,10 @@
 //   warp 1      rank 0: MMA issue;   warps 2-5  epilogue, TMA stores of 64-byte rows (the last tile with the decode warps)
 // Phases: the BF16 parts of dZ (one for BF16 gradients, two for FP16), for both projections of a gated layer.
 // Tiles shared along the contraction pass FP32 partial sums as in the forward kernel.
-// What bounds it: the tensor core with its MN-major operand, 816 clocks per K = 64 step as the issuing thread sees them (590
-// in the forward kernel; waits for operands are 105 on top).  2048 x 4096 x 4096 72 us (0.95 PFLOP/s), 4096 x 4096 x 14336
-// 421 us (1.14), 64 x 4096 x 4096 29 us.
+// What bounds it: a K = 64 step takes 816 clocks as the issuing thread sees them (590 in the forward kernel, 512 by its operations;
+// waits for operands are 105 on top).  The MN-major operand is read, dZ and the decoded units are written through the same
+// shared-memory port in that time; which of them costs the difference has not been measured apart.  2048 x 4096 x 4096 72 to 77 us
+// on different machines (0.89 to 0.95 PFLOP/s), 4096 x 4096 x 14336 421 to 428 us (1.13), 64 x 4096 x 4096 29 to 33 us.
 #include "hif4_linear_tc2_launch.cuh"
 
 namespace hif4 {

@@ -5,8 +5,8 @@
 //     gate products in columns 0..127 and the up products of the same outputs in columns 128..255 of one TMEM lane, and
 //     the thread that reads both finishes the output.
 //   - Loads.  TMA needs K % 256 == 0 and 16-byte aligned units; otherwise the producer warp copies the 144-byte row
-//     chunks word by word (cp.async, zeros past the last unit), which costs it 288 instructions per K = 256 chunk
-//     beside the decode warps' 6000.
+//     chunks word by word (cp.async, zeros past the last unit): 288 copies per K = 256 chunk, each with its address and bounds,
+//     by one warp that the other warps then wait for (2048 x 4096 x 4160 444 us, x 4096 through TMA 74 us).
 //   - Rows past M and columns past N are not decoded: their accumulators are garbage that no one reads (a row of the
 //     product depends on its own row of A only), and few rows leave the decode warps to the weights.
 //   - Epilogue.  Bias, activation, product, residual in FP32 on 16 columns of a row at a time; one rounding; 64-byte
@@ -20,8 +20,9 @@
 //     tile.  It waits for slices of lower index only, so a grid that is partly resident cannot wait for itself.
 // What bounds it: long products, what bounds the FP32 product (decode and tensor core take 3080 and 2350 clocks per K = 256
 // chunk by themselves and share issue slots and the shared-memory port); short ones, set-up, pipeline fill and the last
-// tile's epilogue.  4096 x 14336 x 4096 gated 795 us (1.21 PFLOP/s, 0.72 of the measured burst peak), 4096 x 4096 x 14336 with
-// residual 390 us, 64 x 4096 x 4096 27 us.
+// tile's epilogue.  From units, one call after another on the same inputs: 4096 x 14336 x 4096 gated 814 us (1.18 PFLOP/s, 0.71 of
+// the measured burst rate, 0.84 of the sustained one), 4096 x 4096 x 14336 with residual 418 us; from rows that change from call to
+// call 871 and 463 us, the conversion among them.  64 x 4096 x 4096 27 to 32 us on different machines.
 #pragma once
 #include "hif4_activation.cuh"
 #include "hif4_gemm_internal.cuh"
