@@ -167,7 +167,7 @@ def _row_of(ids, E):
 
 
 def _operand(rows, cols, fmt, g):
-    """Codes [rows, cols / 2] and scales [rows, padded] of a Gaussian matrix, in slabs (what a program loads)."""
+    """Codes [rows, cols / 2] and scales [words, rows, 16] of a Gaussian matrix, in slabs (what a program loads)."""
     codes = torch.empty(rows, cols // 2, dtype=torch.uint8, device="cuda")
     scales = torch.zeros(rows, -(-(cols // BLOCK[fmt]) // 16) * 16, dtype=torch.uint8, device="cuda")
     slab = max(1, (1 << 24) // cols)
@@ -176,7 +176,7 @@ def _operand(rows, cols, fmt, g):
         code, scale = _quantize(torch.randn(n, cols, generator=g, device="cuda") / 4.0, fmt)
         codes[r:r + n] = code[:, 0::2] | (code[:, 1::2] << 4)
         scales[r:r + n, : cols // BLOCK[fmt]] = scale
-    return codes, scales
+    return codes, scales.view(rows, -1, 16).transpose(0, 1).contiguous()
 
 
 def prepare(case, seed):
@@ -204,7 +204,7 @@ def prepare(case, seed):
                 s["out"] = torch.zeros(R, K // 64, 36, dtype=torch.uint8, device="cuda")
             else:
                 s["out"] = (torch.zeros(R, K // 2, dtype=torch.uint8, device="cuda"),
-                            torch.zeros(R, -(-(K // BLOCK[case["fmt"]]) // 16) * 16, dtype=torch.uint8, device="cuda"))
+                            torch.zeros(-(-(K // BLOCK[case["fmt"]]) // 16), R, 16, dtype=torch.uint8, device="cuda"))
             return s
         s["row_of"], s["offsets"] = _row_of(s["ids"], case["E"])
         s["w"] = torch.rand(s["ids"].shape, generator=g, device="cuda") / s["ids"].shape[1]
@@ -226,7 +226,7 @@ def prepare(case, seed):
     s["x"] = _activations(case["T"], case["K"], g, dt)
     s["logits"] = _logits(case["T"], case["E"], g, torch.float32)
     codes, scales = _operand(case["E"] * case["N"], case["K"], case["fmt"], g)
-    s["w"] = codes.view(case["E"], case["N"], -1), scales.view(case["E"], case["N"], -1)
+    s["w"] = codes.view(case["E"], case["N"], -1), scales.view(-1, case["E"], case["N"], 16).transpose(0, 1).contiguous()
     s["r"] = _activations(case["T"], case["N"], g, dt)
     return s
 
@@ -282,8 +282,10 @@ def _values(code, byte, fmt):
 
 
 def _operand_values(codes, scales, fmt):
-    code = torch.stack([codes & 15, codes >> 4], -1).view(codes.shape[0], -1)
-    return _values(code, scales[:, : code.shape[1] // BLOCK[fmt]], fmt)
+    """FP32 values [.., rows, cols] of codes [.., rows, cols / 2] and scales [.., words, rows, 16]."""
+    code = torch.stack([codes & 15, codes >> 4], -1).flatten(-2)
+    byte = scales.transpose(-3, -2).flatten(-2)[..., : code.shape[-1] // BLOCK[fmt]]
+    return _values(code.flatten(0, -2), byte.flatten(0, -2), fmt).view(code.shape)
 
 
 def _hif4(x):
@@ -402,13 +404,13 @@ def _plain(s):
     if op == "product":
         y = _operand_values(*s["a"], c["fmt"]) @ _operand_values(*s["b"], c["fmt"]).t()
         return {"y": (y if s["alpha"] is None else y * s["alpha"]).to(dt)}
-    T, E, N, K = c["T"], c["E"], c["N"], c["K"]
+    T, E = c["T"], c["E"]
     ids, w = _route(s["logits"], None, _router(c))
     # a token has an expert once at most, so T places per expert hold its rows
     x = _values(*_quantize(s["x"], c["fmt"]), c["fmt"])
     here = torch.zeros(E, T, dtype=torch.bool, device=x.device)
     here[ids.long(), torch.arange(T, device=x.device).unsqueeze(1)] = True
-    b = _operand_values(s["w"][0].view(E * N, -1), s["w"][1].view(E * N, -1), c["fmt"]).view(E, N, K)
+    b = _operand_values(*s["w"], c["fmt"])
     y = torch.bmm(torch.where(here.unsqueeze(-1), x, 0.0), b.transpose(1, 2))
     out = (y[ids.long(), torch.arange(T, device=x.device).unsqueeze(1)] * w.unsqueeze(-1)).sum(1)
     return {"y": (out + s["r"].float()).to(dt)}
@@ -493,11 +495,11 @@ def _packed_64(codes, scales, fmt):
     grid = torch.tensor(_E2M1 + tuple(-m for m in _E2M1), dtype=torch.float64, device=codes.device)
     i = torch.arange(2 * codes.shape[1], device=codes.device)
     v = grid[((codes[:, i // 2] >> (4 * (i % 2))) & 15).long()]
-    b = scales[:, i // BLOCK[fmt]].long()
-    two = torch.tensor(2.0, dtype=torch.float64, device=codes.device)
+    word = i // BLOCK[fmt] // 16
+    b = scales[word, :, i // BLOCK[fmt] % 16].t().long()
     if fmt == "mxfp4":
-        return v * two ** (b - 127)
-    return v * torch.where(b < 8, b.double() / 512.0, two ** (b // 8 - 7) * (1.0 + (b % 8).double() / 8.0))
+        return torch.ldexp(v, b - 127)
+    return v * torch.where(b < 8, b.double() / 512.0, torch.ldexp(1.0 + (b % 8).double() / 8.0, b // 8 - 7))
 
 
 def _hif4_64(v, digits):
