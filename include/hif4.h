@@ -368,6 +368,169 @@ hif4_status hif4_mse_workspace(int64_t n, hif4_bfp4_format fmt, size_t* bytes);
 hif4_status hif4_mse_roundtrip(const void* src_bf16, int64_t n, hif4_bfp4_format fmt, float* dst, double* sq_err_sum,
                                void* workspace, size_t workspace_bytes, void* stream);
 
+/* ---------------------------------------------------------------------------------------------
+ * What stands around the experts' products of a mixture-of-experts layer: which experts a token goes to, the experts' rows
+ * in the order that hif4_grouped_gemm and hif4_bfp4_grouped_gemm read, and the weighted sum of what comes back.
+ * Routing results stay on the device.  */
+#define HIF4_ROUTE_MAX_EXPERTS 1024
+#define HIF4_ROUTE_MAX_TOP_K 32
+#define HIF4_ROUTE_MAX_GROUPS 32
+typedef enum { HIF4_SCORE_SOFTMAX = 0, HIF4_SCORE_SIGMOID = 1 } hif4_score;
+
+/* hif4_route -- per token: scores s of the logits, choice c = s + bias, the `top_k` experts of the largest choice in
+ * descending order (equal ones: the lowest index first), and their weights w = scale * s, or scale * s / (sum of the chosen s).
+ *   groups    the experts are `groups` equal runs; a run's value is the sum of its `group_best` (1 or 2) largest choices, and
+ *             only experts of the `top_groups` runs of the largest value are chosen.
+ *   The order is that of the choices in 64 bits (of the logits themselves where there is no bias and no sum of two).
+ *   Experts whose choice is -inf are not chosen: where none is left, the id is -1 and the weight 0.  A NaN counts as -inf in
+ *   the choice, and every weight of its row is NaN (so too for an infinite logit under softmax).
+ * Limits: experts <= 1024, top_k <= 32, groups <= 32 (HIF4_ERR_UNSUPPORTED); top_k <= top_groups * experts / groups.  */
+typedef struct {
+  int64_t tokens, experts, top_k;
+  const void* logits;            /* device, [tokens, experts] of dt, row stride ld_logits elements              */
+  hif4_dtype dt;                 /* BF16, FP16 or FP32                                                         */
+  int64_t ld_logits;
+  const float* bias;             /* device, [experts], or NULL: 0                                              */
+  hif4_score score;
+  int64_t groups, top_groups, group_best;
+  int renormalize;               /* 1: weights of a token add up to scale                                      */
+  float scale;
+  int32_t* ids;                  /* device, [tokens, top_k]                                                    */
+  float* weights;                /* device, [tokens, top_k]                                                    */
+} hif4_route_args;
+hif4_status hif4_route(const hif4_route_args* args, void* stream);
+
+/* hif4_route_backward -- gradient of the weights with respect to the logits (the choice itself has none, nor has the
+ * bias): dlogits [tokens, experts] of dt, every element written.  Ids outside 0 .. experts - 1 take no part.  */
+typedef struct {
+  int64_t tokens, experts, top_k;
+  const void* logits;
+  hif4_dtype dt;
+  int64_t ld_logits;
+  const int32_t* ids;            /* device, [tokens, top_k], as hif4_route wrote them                          */
+  const float* dweights;         /* device, [tokens, top_k]                                                    */
+  hif4_score score;
+  int renormalize;
+  float scale;
+  void* dlogits;                 /* device, [tokens, experts] of dt                                            */
+  int64_t ld_dlogits;
+} hif4_route_backward_args;
+hif4_status hif4_route_backward(const hif4_route_backward_args* args, void* stream);
+
+/* hif4_expert_plan -- the order of the experts' rows: offsets[e] counts the assignments to experts below e
+ * (experts + 1 of them, what the grouped products take), row_of[t][j] is the row of assignment j of token t: rows are sorted by
+ * expert and within an expert by token and place.  Ids outside 0 .. experts - 1 (padding, experts held elsewhere) have no
+ * row: -1.  tokens * top_k < 2^31; experts <= 1024.
+ *   workspace  device scratch, 256-byte aligned, of hif4_expert_plan_workspace bytes (0 for few assignments).  */
+hif4_status hif4_expert_plan_workspace(int64_t tokens, int64_t top_k, int64_t experts, size_t* bytes);
+hif4_status hif4_expert_plan(const int32_t* ids, int64_t tokens, int64_t top_k, int64_t experts, int64_t* offsets, int32_t* row_of,
+                             void* workspace, size_t workspace_bytes, void* stream);
+
+/* What hif4_dispatch writes: rows of x as they are, or converted. */
+typedef enum { HIF4_ROWS_PLAIN = 0, HIF4_ROWS_HIF4 = 1, HIF4_ROWS_MXFP4 = 2, HIF4_ROWS_NVFP4 = 3 } hif4_rows_kind;
+
+/* hif4_dispatch -- the experts' rows: out[row_of[t][j]] = x[t] for every assignment that has a row; a token is read and
+ * converted once.  Converted rows are bit for bit those of hif4_quantize and hif4_bfp4_quantize.  Rows that no assignment
+ * has stay as they were; so does a row number outside 0 .. rows - 1.  (Its gradient is hif4_combine without weights.)  */
+typedef struct {
+  int64_t tokens, cols, top_k, rows;
+  const void* x;                 /* device, [tokens, cols] of dt, row stride ld_x elements; 16-byte aligned rows unless PLAIN */
+  hif4_dtype dt;
+  int64_t ld_x;
+  const int32_t* row_of;         /* device, [tokens, top_k]                                                    */
+  hif4_rows_kind kind;           /* all but PLAIN: cols % 64 == 0                                              */
+  hif4_round mode;               /* HIF4 only                                                                  */
+  const float* gain;             /* MXFP4, NVFP4: as in hif4_bfp4_quantize, or NULL                            */
+  void* out;                     /* device, [rows, cols] of dt; units [rows, cols / 64]; codes [rows, cols / 2] */
+  int64_t ld_out;                /* PLAIN only                                                                 */
+  void* out_scales;              /* MXFP4, NVFP4: scales of `rows` rows                                        */
+} hif4_dispatch_args;
+hif4_status hif4_dispatch(const hif4_dispatch_args* args, void* stream);
+
+/* hif4_combine -- y[t] = res_scale * residual[t] + sum over j of weights[t][j] * in[row_of[t][j]], added in the order of j in
+ * FP32; assignments without a row (outside 0 .. rows - 1) take no part.  */
+typedef struct {
+  int64_t tokens, cols, top_k, rows;
+  const void* in;                /* device, [rows, cols] of dt_in, row stride ld_in elements                   */
+  hif4_dtype dt_in;
+  int64_t ld_in;
+  const int32_t* row_of;         /* device, [tokens, top_k]                                                    */
+  const float* weights;          /* device, [tokens, top_k], or NULL: 1                                        */
+  hif4_dtype dt;                 /* type of residual and y                                                     */
+  const void* residual;          /* device, [tokens, cols], or NULL: 0                                         */
+  int64_t ld_residual;
+  float res_scale;
+  void* y;                       /* device, [tokens, cols]; may be residual itself                             */
+  int64_t ld_y;
+} hif4_combine_args;
+hif4_status hif4_combine(const hif4_combine_args* args, void* stream);
+
+/* hif4_combine_backward -- din[row_of[t][j]] = weights[t][j] * dy[t], dweights[t][j] = <dy[t], in[row_of[t][j]]> (0 without a
+ * row); the residual's gradient is res_scale * dy.  Rows of din that no assignment has stay as they were.  */
+typedef struct {
+  int64_t tokens, cols, top_k, rows;
+  const void* dy;                /* device, [tokens, cols] of dt                                               */
+  hif4_dtype dt;
+  int64_t ld_dy;
+  const int32_t* row_of;
+  const float* weights;          /* or NULL: 1                                                                 */
+  const void* in;                /* device, [rows, cols] of dt_in; needed for dweights                         */
+  hif4_dtype dt_in;              /* type of in and din                                                         */
+  int64_t ld_in;
+  void* din;                     /* device, [rows, cols], or NULL                                              */
+  int64_t ld_din;
+  float* dweights;               /* device, [tokens, top_k], or NULL                                           */
+} hif4_combine_backward_args;
+hif4_status hif4_combine_backward(const hif4_combine_backward_args* args, void* stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * The microscaled 4-bit formats that Section III-A compares HiF4 with, as packed operands and products on the tensor
+ * core's own block-scaled instructions.  `fmt` is HIF4_FMT_MXFP4 (blocks of 32, scale a power of two: E8M0) or HIF4_FMT_NVFP4
+ * (blocks of 16, scale E4M3); elements are E2M1.  The conversion is that of hif4_mse_roundtrip, step by step.
+ *
+ * A packed matrix [rows, cols], cols % 64 == 0, is two arrays:
+ *   codes    [rows, cols / 2] bytes; element i in byte i / 2, low nibble for even i; sign in the nibble's top bit.
+ *   scales   [ceil(cols / block / 16), rows, 16] bytes: the scales of sixteen consecutive blocks of a row are one 16-byte
+ *            word, and the words of all rows lie side by side (any run of rows is one contiguous copy for the product).
+ *            Bytes past the last block are written as 0 and never read.
+ * A gain (device, one FP32) is multiplied in before the conversion, which then works on FP32 products: out of range
+ * tensors are brought into range with it, and products undo it with alpha = 1 / (gain_a * gain_b).
+ * A block that holds a NaN has a NaN scale and zero codes; infinities saturate.  */
+size_t hif4_bfp4_scale_bytes(int64_t rows, int64_t cols, hif4_bfp4_format fmt);
+
+/* Conversion along the rows.  src: device, [rows, cols] of dt (BF16, FP16, FP32), rows 16-byte aligned.  codes and scales:
+ * 16-byte aligned, fully overwritten.  */
+hif4_status hif4_bfp4_quantize(const void* src, hif4_dtype dt, int64_t rows, int64_t cols, int64_t ld_src, hif4_bfp4_format fmt,
+                               const float* gain, void* codes, void* scales, void* stream);
+/* Conversion down the columns: codes and scales of the transposed matrix [cols, rows]; rows % 64 == 0, cols % 8 == 0.  With it the
+ * products of a backward pass, which contract along other dimensions, take their operands: dX = dY W from dY's rows and W's columns,
+ * dW = dY^T X from the columns of both.  */
+hif4_status hif4_bfp4_quantize_transposed(const void* src, hif4_dtype dt, int64_t rows, int64_t cols, int64_t ld_src,
+                                          hif4_bfp4_format fmt, const float* gain, void* codes, void* scales, void* stream);
+/* Values, divided by the gain if there is one; dst BF16 or FP32, rows 16-byte aligned (exact without a gain).  */
+hif4_status hif4_bfp4_dequantize(const void* codes, const void* scales, int64_t rows, int64_t cols, hif4_bfp4_format fmt,
+                                 const float* gain, void* dst, hif4_dtype dt, int64_t ld_dst, void* stream);
+
+/* hif4_bfp4_gemm -- Y = alpha * A * B^T; hif4_bfp4_grouped_gemm -- the same per group g of rows, Y[off[g]:off[g+1]] =
+ * alpha[g] * A[off[g]:off[g+1]] * B[g]^T.  FP32 accumulation, Y rounded once.  Rows of Y at and behind off[num_groups] stay as
+ * they were; offsets are clamped to 0 .. M.  */
+typedef struct {
+  int64_t M, N, K;               /* K > 0, K % 64 == 0                                                         */
+  hif4_bfp4_format fmt;          /* of both operands                                                           */
+  const void* A_codes;           /* device, [M, K / 2], 16-byte aligned                                        */
+  const void* A_scales;          /* device, scales of M rows                                                   */
+  const void* B_codes;           /* device, [N, K / 2], or [num_groups, N, K / 2]                              */
+  const void* B_scales;          /* device, scales of N rows, num_groups times                                 */
+  const float* alpha;            /* device, one FP32, or [num_groups], or NULL: 1                              */
+  hif4_dtype dt;                 /* of Y: BF16, FP16 or FP32                                                   */
+  void* Y;                       /* device, [M, N], row stride ld_y elements                                   */
+  int64_t ld_y;
+  int num_groups;                /* grouped only                                                               */
+  const int64_t* group_offsets;  /* grouped only: device, num_groups + 1                                       */
+} hif4_bfp4_gemm_args;
+hif4_status hif4_bfp4_gemm(const hif4_bfp4_gemm_args* args, void* stream);
+hif4_status hif4_bfp4_grouped_gemm(const hif4_bfp4_gemm_args* args, void* stream);
+
 /* Synchronises `stream` and returns HIF4_ERR_DEVICE_TIMEOUT if any kernel of this library gave up
  * a bounded wait since the last call (the flag is cleared), HIF4_ERR_CUDA if the stream reports
  * an error, else HIF4_OK.  For tests and debugging.  */

@@ -6,4 +6,7 @@ from .binding import (  # noqa: F401
     HIF4_ACT_GELU, HIF4_ACT_GELU_TANH, HIF4_ACT_NONE, HIF4_ACT_RELU, HIF4_ACT_SILU, HIF4_NORM_LAYER, HIF4_NORM_NONE, HIF4_NORM_RMS,
     hif4_block_norm, hif4_block_norm_backward, hif4_block_norm_backward_workspace, hif4_gated_linear, hif4_gated_linear_backward,
     hif4_linear_act, hif4_linear_act_backward,
+    HIF4_SCORE_SIGMOID, HIF4_SCORE_SOFTMAX, hif4_bfp4_dequantize, hif4_bfp4_gemm, hif4_bfp4_grouped_gemm, hif4_bfp4_quantize,
+    hif4_bfp4_quantize_transposed, hif4_combine, hif4_combine_backward, hif4_dispatch, hif4_expert_plan, hif4_expert_plan_workspace,
+    hif4_route, hif4_route_backward,
 )

@@ -21,6 +21,7 @@ HIF4_RNE, HIF4_RHA = 0, 1
 HIF4_FMT_HIF4, HIF4_FMT_MXFP4, HIF4_FMT_NVFP4, HIF4_FMT_NVFP4_PTS = 0, 1, 2, 3
 HIF4_NORM_NONE, HIF4_NORM_RMS, HIF4_NORM_LAYER = 0, 1, 2
 HIF4_ACT_NONE, HIF4_ACT_RELU, HIF4_ACT_SILU, HIF4_ACT_GELU, HIF4_ACT_GELU_TANH = 0, 1, 2, 3, 4
+HIF4_SCORE_SOFTMAX, HIF4_SCORE_SIGMOID = 0, 1
 HIF4_OK = 0
 
 EXPORTED_SYMBOLS = [
@@ -32,6 +33,9 @@ EXPORTED_SYMBOLS = [
     "hif4_block_norm", "hif4_block_norm_backward", "hif4_block_norm_backward_workspace",
     "hif4_linear_act", "hif4_linear_act_workspace", "hif4_linear_act_backward", "hif4_linear_act_backward_workspace",
     "hif4_gated_linear", "hif4_gated_linear_workspace", "hif4_gated_linear_backward", "hif4_gated_linear_backward_workspace",
+    "hif4_route", "hif4_route_backward", "hif4_expert_plan", "hif4_expert_plan_workspace", "hif4_dispatch", "hif4_combine",
+    "hif4_combine_backward", "hif4_bfp4_scale_bytes", "hif4_bfp4_quantize", "hif4_bfp4_quantize_transposed", "hif4_bfp4_dequantize",
+    "hif4_bfp4_gemm", "hif4_bfp4_grouped_gemm",
 ]
 
 
@@ -78,6 +82,10 @@ def _load() -> ctypes.CDLL:
     L.hif4_mse_roundtrip.argtypes = [vp, i64, ci, vp, vp, vp, sz, vp]
     L.hif4_block_norm_backward_workspace.restype = ci
     L.hif4_block_norm_backward_workspace.argtypes = [i64, i64, ctypes.POINTER(sz)]
+    L.hif4_expert_plan_workspace.restype = ci
+    L.hif4_expert_plan_workspace.argtypes = [i64, i64, i64, ctypes.POINTER(sz)]
+    L.hif4_bfp4_scale_bytes.restype = sz
+    L.hif4_bfp4_scale_bytes.argtypes = [i64, i64, ci]
     L.hif4_last_device_status.restype = ci
     L.hif4_last_device_status.argtypes = [vp]
     L.hif4_status_string.restype = ctypes.c_char_p
@@ -455,6 +463,126 @@ def hif4_gated_linear_backward(dy: torch.Tensor, x: torch.Tensor, w_units: torch
         raise TypeError("w_up_units: a tensor expected")
     return _result("hif4_gated_linear_backward", _native.linear_act_backward(dy, x, w_units, w_up_units, bias, bias_up, act, mode, want_dx,
                                                                              want_dbias, precise, workspace))
+
+
+# ------------------------------------------------------------------------------------------- around the experts' products
+def hif4_route(logits: torch.Tensor, top_k: int, bias: Optional[torch.Tensor] = None, *, score: int = HIF4_SCORE_SOFTMAX, groups: int = 1,
+               top_groups: Optional[int] = None, group_best: int = 1, renormalize: bool = True, scale: float = 1.0, stream=None):
+    """Experts of each token and their weights: (ids int32 [tokens, top_k], weights FP32 [tokens, top_k]).
+
+    logits are [tokens, experts] BF16 / FP16 / FP32, bias FP32 [experts].  Scores are a softmax over the experts or a sigmoid of
+    each logit; the top_k largest of score + bias are chosen, in descending order, equal ones by index (compared in 64 bits).
+    With groups > 1 the experts are that many equal runs, and only those of the top_groups (default: all) runs with the largest
+    sum of their group_best (1 or 2) best are chosen.  Weights are scores times scale, with renormalize divided by their sum.  An
+    expert whose logit or bias is -inf (or NaN) is not chosen; where none is left the id is -1 and the weight 0."""
+    if stream is not None:
+        return _under(stream, hif4_route, locals())
+    r = _native.route(logits, top_k, bias, score, groups, groups if top_groups is None else top_groups, group_best, renormalize, scale)
+    return r if r.__class__ is tuple else _result("hif4_route", r)
+
+
+def hif4_route_backward(dweights: torch.Tensor, logits: torch.Tensor, ids: torch.Tensor, *, score: int = HIF4_SCORE_SOFTMAX,
+                        renormalize: bool = True, scale: float = 1.0, stream=None) -> torch.Tensor:
+    """Gradient of hif4_route's weights with respect to the logits, in their type: [tokens, experts] from dweights FP32
+    [tokens, top_k], with the ids, score, renormalize and scale of the forward call."""
+    if stream is not None:
+        return _under(stream, hif4_route_backward, locals())
+    return _result("hif4_route_backward", _native.route_backward(dweights, logits, ids, score, renormalize, scale))
+
+
+def hif4_expert_plan_workspace(tokens: int, top_k: int, num_experts: int) -> int:
+    n = ctypes.c_size_t(0)
+    _check("hif4_expert_plan_workspace", lib.hif4_expert_plan_workspace(tokens, top_k, num_experts, ctypes.byref(n)))
+    return int(n.value)
+
+
+def hif4_expert_plan(ids: torch.Tensor, num_experts: int, *, workspace: Optional[torch.Tensor] = None, stream=None):
+    """Order of the experts' rows: (offsets int64 [num_experts + 1], row_of int32 [tokens, top_k]) from ids int32.
+
+    Rows are sorted by expert, within an expert by token and place; offsets are what the grouped products take.  Ids outside
+    0 .. num_experts - 1 have no row (-1)."""
+    if stream is not None:
+        return _under(stream, hif4_expert_plan, locals())
+    r = _native.expert_plan(ids, num_experts, workspace)
+    return r if r.__class__ is tuple else _result("hif4_expert_plan", r)
+
+
+def hif4_dispatch(x: torch.Tensor, row_of: torch.Tensor, *, fmt: Optional[int] = None, rows: Optional[int] = None, mode: int = HIF4_RNE,
+                  gain: Optional[torch.Tensor] = None, out=None, stream=None):
+    """The experts' rows: row row_of[t, j] is x[t], as it is (fmt None), as HiF4 units (HIF4_FMT_HIF4) or as (codes, scales) in
+    HIF4_FMT_MXFP4 / HIF4_FMT_NVFP4.  There are `rows` of them (default: those of out, else tokens * top_k); rows that no
+    assignment has are left as they are (undefined without out).  Its gradient is hif4_combine without weights."""
+    if stream is not None:
+        return _under(stream, hif4_dispatch, locals())
+    kind = 0 if fmt is None else fmt + 1 if fmt in (HIF4_FMT_HIF4, HIF4_FMT_MXFP4, HIF4_FMT_NVFP4) else -1
+    return _result("hif4_dispatch", _native.dispatch(x, row_of, kind, -1 if rows is None else rows, mode, gain, out))
+
+
+def hif4_combine(rows: torch.Tensor, row_of: torch.Tensor, weights: Optional[torch.Tensor] = None, *, residual: Optional[torch.Tensor] = None,
+                 res_scale: float = 1.0, dtype: Optional[torch.dtype] = None, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """res_scale * residual[t] + sum over j of weights[t, j] * rows[row_of[t, j]], added in FP32 in the order of j, in `dtype`
+    (default: that of out, residual or rows).  Assignments without a row take no part; out may be the residual itself."""
+    if stream is not None:
+        return _under(stream, hif4_combine, locals())
+    return _result("hif4_combine", _native.combine(rows, row_of, weights, residual, res_scale, -1 if dtype is None else _type_code(dtype), out))
+
+
+def hif4_combine_backward(dy: torch.Tensor, row_of: torch.Tensor, weights: Optional[torch.Tensor] = None, *, rows: Optional[torch.Tensor] = None,
+                          num_rows: Optional[int] = None, dtype: Optional[torch.dtype] = None, want_drows: bool = True,
+                          want_dweights: Optional[bool] = None, out: Optional[torch.Tensor] = None, stream=None):
+    """(drows, dweights) of hif4_combine from dy: drows[row_of[t, j]] = weights[t, j] * dy[t] in `dtype` (default: that of rows, out
+    or dy), dweights[t, j] = <dy[t], rows[row_of[t, j]]> (default: wanted where rows are given); None where not wanted.  Rows of
+    drows that no assignment has are left as they are (undefined without out).  The residual's gradient is res_scale * dy."""
+    if stream is not None:
+        return _under(stream, hif4_combine_backward, locals())
+    dw = rows is not None if want_dweights is None else want_dweights
+    return _result("hif4_combine_backward", _native.combine_backward(
+        dy, row_of, weights, rows, -1 if num_rows is None else num_rows, -1 if dtype is None else _type_code(dtype),
+        (1 if want_drows else 0) + (2 if dw else 0), out))
+
+
+# ------------------------------------------------------------------------------------------- microscaled 4-bit formats
+def hif4_bfp4_quantize(src: torch.Tensor, fmt: int, *, gain: Optional[torch.Tensor] = None, out=None, stream=None):
+    """[rows, cols] BF16 / FP16 / FP32 -> (codes uint8 [rows, cols // 2], scales uint8 [words, rows, 16]) in HIF4_FMT_MXFP4 or
+    HIF4_FMT_NVFP4; a word holds the scales of sixteen consecutive blocks of a row.  gain: FP32 [1], multiplied in first."""
+    if stream is not None:
+        return _under(stream, hif4_bfp4_quantize, locals())
+    return _result("hif4_bfp4_quantize", _native.bfp4_quantize(src, fmt, False, gain, out))
+
+
+def hif4_bfp4_quantize_transposed(src: torch.Tensor, fmt: int, *, gain: Optional[torch.Tensor] = None, out=None, stream=None):
+    """hif4_bfp4_quantize of src.T without the transpose being written (rows a multiple of 64, cols of 8): the operands of a
+    backward pass's products."""
+    if stream is not None:
+        return _under(stream, hif4_bfp4_quantize_transposed, locals())
+    return _result("hif4_bfp4_quantize_transposed", _native.bfp4_quantize(src, fmt, True, gain, out))
+
+
+def hif4_bfp4_dequantize(packed, fmt: int, dtype: torch.dtype = torch.bfloat16, *, gain: Optional[torch.Tensor] = None,
+                         out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Values of (codes, scales) in BF16 or FP32 (exact), divided by the gain if there is one."""
+    if stream is not None:
+        return _under(stream, hif4_bfp4_dequantize, locals())
+    return _result("hif4_bfp4_dequantize", _native.bfp4_dequantize(packed, fmt, _type_code(dtype), gain, out))
+
+
+def hif4_bfp4_gemm(a, b, fmt: int, *, alpha: Optional[torch.Tensor] = None, dtype: torch.dtype = torch.bfloat16,
+                   out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """alpha * A @ B^T in `dtype` (that of out, if given) for A [M, K] and B [N, K] given as (codes, scales) of `fmt`; alpha FP32 [1]."""
+    if stream is not None:
+        return _under(stream, hif4_bfp4_gemm, locals())
+    return _result("hif4_bfp4_gemm", _native.bfp4_gemm(a, b, None, fmt, alpha, _type_code(dtype), out))
+
+
+def hif4_bfp4_grouped_gemm(a, b, group_offsets: torch.Tensor, fmt: int, *, alpha: Optional[torch.Tensor] = None,
+                           dtype: torch.dtype = torch.bfloat16, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Per group g: Y[off[g]:off[g+1]] = alpha[g] * A[off[g]:off[g+1]] @ B[g]^T; b is (codes [G, N, K // 2], scales [G, words, N, 16]),
+    group_offsets int64 [G + 1] on the device, alpha FP32 [G].  Rows behind the last group are left as they are."""
+    if stream is not None:
+        return _under(stream, hif4_bfp4_grouped_gemm, locals())
+    if group_offsets is None:
+        raise TypeError("group_offsets: a tensor expected")
+    return _result("hif4_bfp4_grouped_gemm", _native.bfp4_gemm(a, b, group_offsets, fmt, alpha, _type_code(dtype), out))
 
 
 def hif4_debug_wait_timeout(budget_ns: int, stream=None) -> None:

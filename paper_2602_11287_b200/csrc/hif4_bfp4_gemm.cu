@@ -1,0 +1,399 @@
+// hif4_bfp4_gemm, hif4_bfp4_grouped_gemm -- Y = alpha A B^T for operands in MXFP4 or NVFP4, on the tensor core's block-scaled
+// instructions: codes go from HBM through shared memory into the MMA as they are, nothing is decoded.
+//
+// A CTA computes 128 rows of B (the MMA's M side: TMEM lanes) times T tokens (rows of A: accumulator columns), so that few
+// tokens cost few columns.  Per K = 256 a stage holds 128-byte code rows of both operands (TMA, SWIZZLE_128B) and their
+// scales (one 16-byte word per row, the words of consecutive rows consecutive: a single bulk copy).  The MMA wants
+// a scale word of row r in TMEM lane r % 32 (the same in all four lane quarters) and column r / 32, for each K = 64; four
+// warps read the rows' words, which are just the four K = 64 steps of a row, and store them to their lane quarter.
+// Few tiles: the K chunks of a tile are dealt to the CTAs of a cluster, whose FP32 sums are added through distributed
+// shared memory in rank order (no atomics, no workspace).
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "hif4_bfp4_device.cuh"
+#include "hif4_tc2_common.cuh"
+
+namespace hif4 {
+namespace {
+
+constexpr int kThreads = 256;               // warps: producer, MMA, tile lookup and TMEM, idle, 4 x scales and epilogue
+constexpr int BW = 128;                     // rows of B a tile
+constexpr int kChunk = 256;                 // elements of K a stage
+constexpr int kRowBytes = kChunk / 2;
+constexpr int kTmemCols = 256;
+
+template <int T> struct Shape {
+  static constexpr int kStages = T == 128 ? 3 : 4;
+  static constexpr int kCodeBytes = (BW + T) * kRowBytes;
+  static constexpr int kSfRows = T < 32 ? 32 : T;
+  static constexpr int kSfBytes = (BW + kSfRows) * 16;
+  static constexpr int kBars = kStages * (kCodeBytes + kSfBytes);
+  static constexpr int kSmem = 1024 + kBars + 256;
+  static constexpr int kAccCols = T < 32 ? 32 : T;
+  static_assert(kAccCols + kStages * 32 <= kTmemCols, "TMEM");
+  static_assert(T * BW * 4 <= kStages * kCodeBytes, "sums of a cluster");
+};
+
+struct Bfp4Params {
+  int64_t M, N;
+  int chunks, last_steps;                   // K chunks; K = 64 steps of the last one
+  int n_tiles;
+  const uint8_t *a_scales, *b_scales;
+  int64_t b_scale_group;                    // bytes of a group's scales of B
+  const float* alpha;
+  void* y;
+  int64_t ld_y;
+  int dt;
+  int num_groups;                           // 0: dense
+  const int64_t* offsets;
+  unsigned int* error_word;
+};
+
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar)
+               : "memory");
+}
+// kNv: four scales a K = 64 step (E4M3); else two (E8M0), of which the instruction descriptor names the half word.
+template <bool kNv>
+__device__ __forceinline__ void mma_scaled(uint32_t d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t sfa, uint32_t sfb, uint32_t accumulate) {
+  if (kNv)
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %6, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::mxf4nvf4.block_scale.scale_vec::4X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
+        ::"r"(d), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate) : "memory");
+  else
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %6, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
+        ::"r"(d), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate) : "memory");
+}
+// E2M1 operands, scale type, sizes; the scales' half word is added where it is used (bits 4 and 29).
+template <bool kNv, int kM, int kN>
+__host__ __device__ constexpr uint32_t instr_desc() {
+  return (1u << 7) | (1u << 10) | (static_cast<uint32_t>(kN >> 3) << 17) | (kNv ? 0u : 1u << 23) | (static_cast<uint32_t>(kM >> 4) << 24);
+}
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
+      ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
+      "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+      : "memory");
+}
+__device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ float ld_cluster_f32(uint32_t addr) {
+  float v;
+  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
+  return v;
+}
+
+// Scale words of up to 128 rows (`groups` runs of 32) -> sixteen columns: column 4 k + c holds step k of rows 32 c .. 32 c + 31.
+template <bool kNv, int kGroups>
+__device__ __forceinline__ void move_scales(uint32_t smem, uint32_t taddr, int lane, int half) {
+  uint32_t w[16];
+#pragma unroll
+  for (int c = 0; c < 4; ++c) {
+    uint4 v = make_uint4(0u, 0u, 0u, 0u);
+    if (c < kGroups) v = lds128(smem + (c * 32 + lane) * 16);
+    if (kNv) {
+      w[c] = v.x; w[4 + c] = v.y; w[8 + c] = v.z; w[12 + c] = v.w;
+    } else {
+      w[c] = half ? v.z : v.x; w[4 + c] = half ? v.w : v.y; w[8 + c] = 0u; w[12 + c] = 0u;
+    }
+  }
+  tmem_st16(taddr, w);
+}
+
+__device__ __forceinline__ void store_y(const Bfp4Params& p, int64_t m, int64_t n, float v) {
+  const int64_t at = m * p.ld_y + n;
+  if (p.dt == HIF4_FP32) static_cast<float*>(p.y)[at] = v;
+  else if (p.dt == HIF4_BF16) static_cast<__nv_bfloat16*>(p.y)[at] = __float2bfloat16_rn(v);
+  else static_cast<__half*>(p.y)[at] = __float2half_rn(v);
+}
+
+template <int T, bool kNv>
+__global__ void __launch_bounds__(kThreads, 2)
+bfp4_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const Bfp4Params p) {
+  using S = Shape<T>;
+  constexpr int kStages = S::kStages;
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t smem = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  const uint32_t codes = smem, sf = codes + kStages * S::kCodeBytes, bars = smem + S::kBars;
+  const uint32_t full = bars, ready = bars + 8 * kStages, empty = bars + 16 * kStages, done = bars + 24 * kStages;
+  uint8_t* gen = smem_raw + (smem - smem_u32(smem_raw));
+  volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(gen + S::kBars + 24 * kStages + 8);
+  volatile uint32_t* abort_flag = tmem_slot + 1;
+  volatile int* where = reinterpret_cast<volatile int*>(const_cast<uint32_t*>(tmem_slot) + 2);       // m0, m_end, group
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  uint32_t rank = 0u, ranks = 1u;
+  asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+  asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(ranks));
+  const int tile = static_cast<int>(blockIdx.x / ranks);
+  const int mt = tile / p.n_tiles, nt = tile - mt * p.n_tiles;
+  const int64_t n0 = static_cast<int64_t>(nt) * BW;
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < kStages; ++s) {
+      mbar_init(full + 8 * s, 1);
+      mbar_init(ready + 8 * s, 4);
+      mbar_init(empty + 8 * s, 1);
+    }
+    mbar_init(done, 1);
+    *abort_flag = 0u;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 2) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(bars + 24 * kStages + 8), "r"(kTmemCols) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  if (warp == 3) {
+    // the tile's rows: dense ones follow from the index, grouped ones from the offsets (tiles of a group, added up)
+    int64_t m0 = static_cast<int64_t>(mt) * T, m_end = p.M;
+    int group = 0;
+    if (p.num_groups) {
+      group = -1;
+      int64_t before = 0;
+      for (int g0 = 0; g0 < p.num_groups && group < 0; g0 += 32) {
+        const int g = g0 + lane;
+        int64_t lo = 0, hi = 0;
+        if (g < p.num_groups) {
+          lo = max(static_cast<int64_t>(0), min(p.M, p.offsets[g]));
+          hi = max(lo, min(p.M, p.offsets[g + 1]));
+        }
+        const int64_t tiles = (hi - lo + T - 1) / T;
+        int64_t incl = tiles;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+          const int64_t v = __shfl_up_sync(0xFFFFFFFFu, incl, o);
+          if (lane >= o) incl += v;
+        }
+        const bool hit = mt >= before + incl - tiles && mt < before + incl;
+        const uint32_t who = __ballot_sync(0xFFFFFFFFu, hit);
+        if (who) {
+          const int l = __ffs(who) - 1;
+          m0 = __shfl_sync(0xFFFFFFFFu, lo + (mt - before - incl + tiles) * T, l);
+          m_end = __shfl_sync(0xFFFFFFFFu, hi, l);
+          group = g0 + l;
+        }
+        before += __shfl_sync(0xFFFFFFFFu, incl, 31);
+      }
+    }
+    if (lane == 0) {
+      where[0] = static_cast<int>(m0);
+      where[1] = static_cast<int>(m_end);
+      where[2] = group;
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
+  const int m0 = where[0], m_end = where[1], group = where[2];
+  // this CTA's share of the chunks (none for a tile that no group has)
+  const int k_first = group < 0 ? 0 : static_cast<int>(static_cast<int64_t>(p.chunks) * rank / ranks);
+  const int k_last = group < 0 ? 0 : static_cast<int>(static_cast<int64_t>(p.chunks) * (rank + 1) / ranks);
+  const uint32_t sf_cols = tmem + S::kAccCols;
+
+  if (warp == 0) {
+    if (lane == 0) {
+      const int b_row = static_cast<int>(group * p.N + n0);
+      const uint32_t rows_b = static_cast<uint32_t>(min(static_cast<int64_t>(BW), p.N - n0)) * 16u;
+      const uint32_t rows_a = static_cast<uint32_t>(min(static_cast<int64_t>(T), p.M - m0)) * 16u;
+      const uint8_t* b_sf = p.b_scales + group * p.b_scale_group + n0 * 16;
+      const uint8_t* a_sf = p.a_scales + static_cast<int64_t>(m0) * 16;
+      for (int k = k_first, i = 0; k < k_last; ++k, ++i) {
+        const int s = i % kStages;
+        if (!mbar_wait(empty + 8 * s, ((i / kStages) & 1) ^ 1, abort_flag)) break;
+        const uint32_t bar = full + 8 * s, at = codes + s * S::kCodeBytes, sfs = sf + s * S::kSfBytes;
+        mbar_expect_tx(bar, S::kCodeBytes + rows_a + rows_b);
+        tma_load_2d(at, &tmB, k * kRowBytes, b_row, bar);
+        tma_load_2d(at + BW * kRowBytes, &tmA, k * kRowBytes, m0, bar);
+        const int64_t word = kNv ? k : k >> 1;
+        bulk_load(sfs, b_sf + word * p.N * 16, rows_b, bar);
+        bulk_load(sfs + BW * 16, a_sf + word * p.M * 16, rows_a, bar);
+      }
+    }
+  } else if (warp == 1) {
+    if (lane == 0) {
+      constexpr uint32_t kDesc = instr_desc<kNv, BW, T>();
+      bool ok = true;
+      for (int k = k_first, i = 0; k < k_last; ++k, ++i) {
+        const int s = i % kStages;
+        const uint32_t ph = (i / kStages) & 1;
+        if (!(ok = mbar_wait(full + 8 * s, ph, abort_flag) && mbar_wait(ready + 8 * s, ph, abort_flag))) break;
+        tc_fence_after();
+        const uint64_t bd = make_desc(codes + s * S::kCodeBytes), ad = make_desc(codes + s * S::kCodeBytes + BW * kRowBytes);
+        const uint32_t sfb = sf_cols + s * 32, sfa = sfb + 16;
+        const int steps = k == p.chunks - 1 ? p.last_steps : 4;
+        for (int j = 0; j < steps; ++j) {
+          const uint32_t at = kNv ? 4 * j : 4 * (j >> 1);
+          const uint32_t desc = kDesc | (kNv ? 0u : (static_cast<uint32_t>(j & 1) * 2u) * ((1u << 4) | (1u << 29)));
+          mma_scaled<kNv>(tmem, bd + 2 * j, ad + 2 * j, desc, sfb + at, sfa + at, (i | j) != 0);
+        }
+        tc_commit(empty + 8 * s);
+      }
+      if (ok && k_last > k_first) tc_commit(done);
+    }
+  } else if (warp >= 4) {
+    const int q = warp & 3;
+    bool ok = true;
+    for (int k = k_first, i = 0; k < k_last; ++k, ++i) {
+      const int s = i % kStages;
+      if (!(ok = mbar_wait(full + 8 * s, (i / kStages) & 1, abort_flag))) break;
+      tc_fence_after();
+      const uint32_t src = sf + s * S::kSfBytes, dst = sf_cols + s * 32 + (static_cast<uint32_t>(q * 32) << 16);
+      move_scales<kNv, 4>(src, dst, lane, k & 1);
+      move_scales<kNv, S::kSfRows / 32>(src + BW * 16, dst + 16, lane, k & 1);
+      tmem_wait_st();
+      fence_proxy_async_smem();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(ready + 8 * s);
+    }
+    if (ok && k_last > k_first) ok = mbar_wait(done, 0, abort_flag);
+    if (ok && k_last > k_first) {
+      tc_fence_after();
+      const uint32_t acc = tmem + (static_cast<uint32_t>(q * 32) << 16);
+      const float alpha = p.alpha ? p.alpha[p.num_groups ? group : 0] : 1.0f;
+      const int64_t n = n0 + q * 32 + lane;
+      for (int c = 0; c < T; c += 16) {
+        uint32_t r[16];
+        tc_ld16(acc + c, r);
+        tc_wait_ld();
+        if (ranks == 1) {
+#pragma unroll
+          for (int j = 0; j < 16; ++j)
+            if (n < p.N && m0 + c + j < m_end) store_y(p, m0 + c + j, n, alpha * __uint_as_float(r[j]));
+        } else {
+          float* sums = reinterpret_cast<float*>(gen) + q * 32 + lane;
+#pragma unroll
+          for (int j = 0; j < 16; ++j) sums[(c + j) * BW] = __uint_as_float(r[j]);
+        }
+      }
+    }
+    tc_fence_before();
+  }
+  __syncwarp();
+  if (ranks > 1) {
+    cluster_sync_all();
+    if (group >= 0) {
+      const float alpha = p.alpha ? p.alpha[p.num_groups ? group : 0] : 1.0f;
+      const int c0 = static_cast<int>(T * rank / ranks), c1 = static_cast<int>(T * (rank + 1) / ranks);
+      const int64_t n = n0 + (threadIdx.x & (BW - 1));
+      for (int c = c0 + static_cast<int>(threadIdx.x) / BW; c < c1 && m0 + c < m_end; c += kThreads / BW) {
+        float v = 0.0f;
+        for (uint32_t r = 0; r < ranks; ++r) v += ld_cluster_f32(mapa(smem + (c * BW + (threadIdx.x & (BW - 1))) * 4, r));
+        if (n < p.N) store_y(p, m0 + c, n, alpha * v);
+      }
+    }
+    cluster_sync_all();
+  }
+  if (*abort_flag) {
+    // a wait gave up: let copies and MMAs in flight land before their memory is released
+    const uint64_t t0 = global_ns();
+    while (global_ns() - t0 < 2000000ull) {}
+    if (threadIdx.x == 0) atomicExch(p.error_word, 1u);
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 2) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
+  }
+}
+
+// ------------------------------------------------------------------------------------ host side
+// Codes of a matrix: [rows, K / 2] bytes, box = 128 bytes x box_rows; what lies outside reads as zeros.
+bool make_code_map(CUtensorMap* map, const void* base, int64_t rows, int64_t K, int box_rows) {
+  EncodeTiledFn fn = encode_tiled_fn();
+  if (!fn) return false;
+  const cuuint64_t dims[2] = {static_cast<cuuint64_t>(K / 2), static_cast<cuuint64_t>(rows)};
+  const cuuint64_t strides[1] = {static_cast<cuuint64_t>(K / 2)};
+  const cuuint32_t box[2] = {kRowBytes, static_cast<cuuint32_t>(box_rows)};
+  const cuuint32_t estr[2] = {1, 1};
+  return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int T, bool kNv>
+hif4_status launch_tiles(const hif4_bfp4_gemm_args& a, Bfp4Params p, int64_t m_tiles, cudaStream_t st) {
+  const auto kernel = bfp4_gemm_kernel<T, kNv>;
+  static uint64_t ready = 0;
+  if (!ensure_dynamic_smem(kernel, Shape<T>::kSmem, ready)) return HIF4_ERR_CUDA;
+  CUtensorMap tmA, tmB;
+  const int64_t b_rows = a.N * (a.num_groups > 0 ? a.num_groups : 1);
+  if (!make_code_map(&tmA, a.A_codes, a.M, a.K, T) || !make_code_map(&tmB, a.B_codes, b_rows, a.K, BW)) return HIF4_ERR_CUDA;
+  const int64_t tiles = m_tiles * p.n_tiles;
+  if (tiles > 0x7FFFFFFFll / 8) return HIF4_ERR_SHAPE;
+  // two CTAs an SM; a cluster splits K while CTAs are missing and every one keeps two chunks
+  int ranks = 1;
+  while (ranks < 8 && tiles * ranks * 2 <= 2 * sm_count() && p.chunks >= 4 * ranks) ranks *= 2;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(static_cast<unsigned>(tiles * ranks));
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = Shape<T>::kSmem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim = {static_cast<unsigned>(ranks), 1, 1};
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  if (cudaLaunchKernelEx(&cfg, kernel, tmA, tmB, p) != cudaSuccess) {
+    (void)cudaGetLastError();
+    return HIF4_ERR_CUDA;
+  }
+  note_launch();
+  return HIF4_OK;
+}
+
+hif4_status product(const hif4_bfp4_gemm_args& a, bool grouped, void* stream) {
+  if (a.M < 0 || a.N < 0 || a.K < 1 || a.K % kUnitElems != 0 || a.ld_y < a.N || (grouped && a.num_groups < 0)) return HIF4_ERR_SHAPE;
+  if ((a.fmt != HIF4_FMT_MXFP4 && a.fmt != HIF4_FMT_NVFP4) || (a.dt != HIF4_BF16 && a.dt != HIF4_FP16 && a.dt != HIF4_FP32)) return HIF4_ERR_DTYPE;
+  if (a.M == 0 || a.N == 0 || (grouped && a.num_groups == 0)) return HIF4_OK;
+  constexpr int64_t kMost = (1ll << 31) - 512;                 // rows and bytes of a row are 32-bit TMA coordinates
+  if (a.M >= kMost || a.K >= kMost || a.N >= kMost / (grouped ? a.num_groups : 1)) return HIF4_ERR_SHAPE;
+  if (!a.Y || !a.A_codes || !a.A_scales || !a.B_codes || !a.B_scales || (grouped && !a.group_offsets)) return HIF4_ERR_NULL;
+  const int64_t size = a.dt == HIF4_FP32 ? 4 : 2;
+  const auto off = [](const void* p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) != 0; };
+  if (off(a.A_codes, 16) || off(a.A_scales, 16) || off(a.B_codes, 16) || off(a.B_scales, 16) || off(a.alpha, 4) ||
+      off(a.Y, static_cast<uintptr_t>(size)) || off(a.group_offsets, 8))
+    return HIF4_ERR_ALIGN;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  const bool nv = a.fmt == HIF4_FMT_NVFP4;
+  Bfp4Params p{};
+  p.M = a.M; p.N = a.N;
+  p.chunks = static_cast<int>(ceil_div64(a.K, kChunk));
+  p.last_steps = static_cast<int>(a.K / 64 - 4 * (static_cast<int64_t>(p.chunks) - 1));
+  p.n_tiles = static_cast<int>(ceil_div64(a.N, BW));
+  p.a_scales = static_cast<const uint8_t*>(a.A_scales);
+  p.b_scales = static_cast<const uint8_t*>(a.B_scales);
+  p.b_scale_group = grouped ? scale_words(a.K, nv) * a.N * 16 : 0;
+  p.alpha = a.alpha;
+  p.y = a.Y; p.ld_y = a.ld_y; p.dt = a.dt;
+  p.num_groups = grouped ? a.num_groups : 0;
+  p.offsets = a.group_offsets;
+  p.error_word = device_error_word();
+  if (!p.error_word) return HIF4_ERR_CUDA;
+  // tokens of a tile: the fewest that hold the rows of a (mean) group, at most 128
+  const int64_t mean = grouped ? ceil_div64(a.M, a.num_groups) : a.M;
+  const int T = mean <= 16 ? 16 : mean <= 32 ? 32 : mean <= 64 ? 64 : 128;
+  const int64_t m_tiles = ceil_div64(a.M, T) + (grouped ? a.num_groups : 0);
+  hif4_bfp4_gemm_args b = a;
+  b.num_groups = grouped ? a.num_groups : 0;
+  switch (T) {
+    case 16: return nv ? launch_tiles<16, true>(b, p, m_tiles, st) : launch_tiles<16, false>(b, p, m_tiles, st);
+    case 32: return nv ? launch_tiles<32, true>(b, p, m_tiles, st) : launch_tiles<32, false>(b, p, m_tiles, st);
+    case 64: return nv ? launch_tiles<64, true>(b, p, m_tiles, st) : launch_tiles<64, false>(b, p, m_tiles, st);
+    default: return nv ? launch_tiles<128, true>(b, p, m_tiles, st) : launch_tiles<128, false>(b, p, m_tiles, st);
+  }
+}
+
+}  // namespace
+}  // namespace hif4
+
+extern "C" hif4_status hif4_bfp4_gemm(const hif4_bfp4_gemm_args* args, void* stream) {
+  return args ? hif4::product(*args, false, stream) : HIF4_ERR_NULL;
+}
+extern "C" hif4_status hif4_bfp4_grouped_gemm(const hif4_bfp4_gemm_args* args, void* stream) {
+  return args ? hif4::product(*args, true, stream) : HIF4_ERR_NULL;
+}

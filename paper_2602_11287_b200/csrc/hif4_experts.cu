@@ -1,0 +1,490 @@
+// hif4_expert_plan, hif4_dispatch, hif4_combine, hif4_combine_backward -- the experts' rows of a mixture-of-experts
+// layer: their order, the rows themselves, the weighted sum of what comes back, and its gradient.  All but the plan are
+// bound by HBM traffic: a token's row is read (and converted) once, the experts' rows are read or written once.
+#include "hif4_bfp4_device.cuh"
+#include "hif4_vec8.cuh"
+
+namespace hif4 {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr uint32_t kAll = 0xFFFFFFFFu;
+
+// ----------------------------------------------------------------------------- order of the rows
+// A stable counting sort by expert.  A warp owns a run of consecutive assignments: it counts them per expert, the counts are
+// summed over warps (and blocks) in their order, and the warp then goes through its run again, 32 assignments a step, giving
+// each the next row of its expert: match_any finds the lanes with the same expert, their order is the lanes'.
+constexpr int kPlanWarps = 32;
+constexpr int kPlanItems = 8192;                        // assignments a block orders
+
+__global__ void __launch_bounds__(kPlanWarps * 32)
+plan_count_kernel(const int32_t* __restrict__ ids, int64_t n, int experts, int32_t* __restrict__ counts) {
+  extern __shared__ int32_t hist[];
+  for (int e = threadIdx.x; e < experts; e += blockDim.x) hist[e] = 0;
+  __syncthreads();
+  const int64_t first = static_cast<int64_t>(blockIdx.x) * kPlanItems, last = min(n, first + kPlanItems);
+  for (int64_t i = first + threadIdx.x; i < last; i += blockDim.x) {
+    const int e = ids[i];
+    if (e >= 0 && e < experts) atomicAdd(&hist[e], 1);
+  }
+  __syncthreads();
+  for (int e = threadIdx.x; e < experts; e += blockDim.x) counts[static_cast<int64_t>(blockIdx.x) * experts + e] = hist[e];
+}
+
+__global__ void __launch_bounds__(kPlanWarps * 32)
+plan_place_kernel(const int32_t* __restrict__ ids, int64_t n, int experts, const int32_t* __restrict__ counts, int blocks,
+                  int64_t* __restrict__ offsets, int32_t* __restrict__ row_of) {
+  extern __shared__ int32_t hist[];                     // [warps][experts]
+  __shared__ int32_t warp_total[kPlanWarps];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  for (int e = threadIdx.x; e < experts * kPlanWarps; e += blockDim.x) hist[e] = 0;
+  __syncthreads();
+  const int64_t block_first = static_cast<int64_t>(blockIdx.x) * kPlanItems, block_last = min(n, block_first + kPlanItems);
+  const int64_t run = ((block_last - block_first + kPlanWarps - 1) / kPlanWarps + 31) / 32 * 32;
+  const int64_t first = min(block_last, block_first + warp * run), last = min(block_last, first + run);
+  int32_t* mine = hist + warp * experts;
+  for (int64_t i = first + lane; i < last; i += 32) {
+    const int e = ids[i];
+    if (e >= 0 && e < experts) atomicAdd(&mine[e], 1);
+  }
+  __syncthreads();
+  // thread e: counts of expert e before this block and in all blocks, and its warps' first places
+  const int e = threadIdx.x;
+  int before = 0, total = 0;
+  if (e < experts) {
+    if (blocks > 1) {
+      for (int b = 0; b < blocks; ++b) {
+        const int c = counts[static_cast<int64_t>(b) * experts + e];
+        if (b < static_cast<int>(blockIdx.x)) before += c;
+        total += c;
+      }
+    }
+    int sum = 0;
+    for (int w = 0; w < kPlanWarps; ++w) {
+      const int c = hist[w * experts + e];
+      hist[w * experts + e] = sum;
+      sum += c;
+    }
+    if (blocks == 1) total = sum;
+  }
+  int incl = total;                                     // scan over the experts (experts <= threads)
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int v = __shfl_up_sync(kAll, incl, o);
+    if (lane >= o) incl += v;
+  }
+  if (lane == 31) warp_total[warp] = incl;
+  __syncthreads();
+  if (warp == 0) {
+    int v = warp_total[lane];
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int u = __shfl_up_sync(kAll, v, o);
+      if (lane >= o) v += u;
+    }
+    warp_total[lane] = v;
+  }
+  __syncthreads();
+  const int end = incl + (warp ? warp_total[warp - 1] : 0);
+  if (e < experts) {
+    const int base = end - total + before;
+    for (int w = 0; w < kPlanWarps; ++w) hist[w * experts + e] += base;
+    if (blockIdx.x == 0) {
+      if (e == 0) offsets[0] = 0;
+      offsets[e + 1] = end;
+    }
+  }
+  __syncthreads();
+  for (int64_t i = first + lane; i - lane < last; i += 32) {
+    const int id = i < last ? ids[i] : -1;
+    const bool fine = id >= 0 && id < experts;
+    const uint32_t same = __match_any_sync(kAll, fine ? id : -1);
+    const int rank = __popc(same & ((1u << lane) - 1u));
+    int row = -1;
+    if (fine) row = mine[id] + rank;
+    __syncwarp();
+    if (fine && rank == 0) mine[id] += __popc(same);
+    __syncwarp();
+    if (i < last) row_of[i] = row;
+  }
+}
+
+// ----------------------------------------------------------------------------- rows of the experts
+struct Gather {
+  int64_t rows, cols;
+  int top_k, segments;                                  // blocks of a token
+  const int32_t* row_of;
+};
+__device__ __forceinline__ bool has_row(int row, int64_t rows) { return row >= 0 && row < rows; }
+
+// Word: as many bytes as addresses, row strides and the row's length allow.
+template <typename Word>
+__global__ void __launch_bounds__(kThreads)
+dispatch_plain_kernel(Gather g, const Word* __restrict__ x, int64_t ld_x, Word* __restrict__ out, int64_t ld_out, int64_t words) {
+  const int64_t t = blockIdx.x / g.segments;
+  const int seg = static_cast<int>(blockIdx.x - t * g.segments);
+  const int32_t* row_of = g.row_of + t * g.top_k;
+  for (int64_t w = seg * kThreads + threadIdx.x; w < words; w += static_cast<int64_t>(g.segments) * kThreads) {
+    const Word v = x[t * ld_x + w];
+    for (int j = 0; j < g.top_k; ++j) {
+      const int row = row_of[j];
+      if (has_row(row, g.rows)) out[row * ld_out + w] = v;
+    }
+  }
+}
+
+// Eight lanes convert a unit.
+template <typename T, bool kRHA>
+__global__ void __launch_bounds__(kThreads)
+dispatch_hif4_kernel(Gather g, const T* __restrict__ x, int64_t ld_x, uint32_t* __restrict__ out) {
+  const int64_t t = blockIdx.x / g.segments;
+  const int seg = static_cast<int>(blockIdx.x - t * g.segments);
+  const int32_t* row_of = g.row_of + t * g.top_k;
+  const int part = threadIdx.x & 7;
+  const int64_t upr = g.cols / kUnitElems;
+  for (int64_t u0 = static_cast<int64_t>(seg) * (kThreads / 8); u0 < upr; u0 += static_cast<int64_t>(g.segments) * (kThreads / 8)) {
+    const int64_t mine = u0 + (threadIdx.x >> 3), u = min(mine, upr - 1);
+    uint32_t meta;
+    const uint32_t code = encode_unit_octet<kRHA>(load8(x + t * ld_x + u * kUnitElems + 8 * part), part, meta);
+    if (mine >= upr) continue;
+    for (int j = 0; j < g.top_k; ++j) {
+      const int row = row_of[j];
+      if (!has_row(row, g.rows)) continue;
+      uint32_t* unit = out + (row * upr + u) * kUnitWords;
+      unit[1 + part] = code;
+      if (part == 0) unit[0] = meta;
+    }
+  }
+}
+
+// A thread converts sixteen elements.
+template <typename T, bool kNv>
+__global__ void __launch_bounds__(kThreads)
+dispatch_bfp4_kernel(Gather g, const T* __restrict__ x, int64_t ld_x, const float* __restrict__ gain, uint2* __restrict__ codes,
+                     uint8_t* __restrict__ scales) {
+  const int64_t t = blockIdx.x / g.segments;
+  const int seg = static_cast<int>(blockIdx.x - t * g.segments);
+  const int32_t* row_of = g.row_of + t * g.top_k;
+  const int64_t n16 = g.cols / 16;
+  for (int64_t c0 = static_cast<int64_t>(seg) * kThreads; c0 < n16; c0 += static_cast<int64_t>(g.segments) * kThreads) {
+    const int64_t mine = c0 + threadIdx.x, c = mine < n16 ? mine : n16 - 2 + (threadIdx.x & 1);
+    float v[16], a[8];
+    unpack8(load8(x + t * ld_x + 16 * c), a);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = a[i];
+    unpack8(load8(x + t * ld_x + 16 * c + 8), a);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[8 + i] = a[i];
+    if (gain) {
+      const float f = *gain;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) v[i] = __fmul_rn(v[i], f);
+    }
+    uint32_t peak = peak16(v), byte;
+    if (!kNv) peak = max(peak, __shfl_xor_sync(kAll, peak, 1));
+    const uint2 code = encode16<kNv>(v, peak, byte);
+    if (mine >= n16) continue;
+    const int64_t block = kNv ? c : c >> 1;
+    for (int j = 0; j < g.top_k; ++j) {
+      const int row = row_of[j];
+      if (!has_row(row, g.rows)) continue;
+      codes[row * n16 + c] = code;
+      if (kNv || !(c & 1)) scales[scale_at(row, block, g.rows)] = static_cast<uint8_t>(byte);
+      if (c == n16 - 1)
+        for (int64_t b = block + 1; b & 15; ++b) scales[scale_at(row, b, g.rows)] = 0;
+    }
+  }
+}
+
+// ----------------------------------------------------------------------------- sums over a token's experts
+// kVec elements a thread: eight, or one where rows are not 16-byte aligned.
+template <typename T, int kVec>
+__device__ __forceinline__ void load_vec(const T* p, float (&v)[kVec]) {
+  if constexpr (kVec == 8) unpack8(load8(p), v);
+  else v[0] = to_f32(*p);
+}
+template <typename T, int kVec>
+__device__ __forceinline__ void store_vec(T* p, const float (&v)[kVec]) {
+  if constexpr (kVec == 8) store8(p, pack8<T>(v));
+  else *p = from_f32<T>(v[0]);
+}
+
+template <typename TI, typename TO, int kVec>
+__global__ void __launch_bounds__(kThreads)
+combine_kernel(Gather g, const TI* __restrict__ in, int64_t ld_in, const float* __restrict__ weights, const TO* residual, int64_t ld_r,
+               float res_scale, TO* y, int64_t ld_y) {
+  const int64_t t = blockIdx.x / g.segments;
+  const int seg = static_cast<int>(blockIdx.x - t * g.segments);
+  const int32_t* row_of = g.row_of + t * g.top_k;
+  const int64_t c = (static_cast<int64_t>(seg) * kThreads + threadIdx.x) * kVec;
+  if (c >= g.cols) return;
+  float acc[kVec], v[kVec];
+#pragma unroll
+  for (int i = 0; i < kVec; ++i) acc[i] = 0.0f;
+#pragma unroll 4
+  for (int j = 0; j < g.top_k; ++j) {
+    const int row = row_of[j];
+    const float w = weights ? weights[t * g.top_k + j] : 1.0f;
+    if (!has_row(row, g.rows)) continue;
+    load_vec(in + row * ld_in + c, v);
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) acc[i] = fmaf(w, v[i], acc[i]);
+  }
+  if (residual) {
+    load_vec(residual + t * ld_r + c, v);
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) acc[i] = fmaf(res_scale, v[i], acc[i]);
+  }
+  store_vec(y + t * ld_y + c, acc);
+}
+
+// A block goes over a token's row, eight assignments at a time.
+constexpr int kTogether = 8;
+template <typename TD, typename TI, int kVec>
+__global__ void __launch_bounds__(kThreads)
+combine_backward_kernel(Gather g, const TD* __restrict__ dy, int64_t ld_dy, const float* __restrict__ weights, const TI* __restrict__ in,
+                        int64_t ld_in, TI* __restrict__ din, int64_t ld_din, float* __restrict__ dweights) {
+  __shared__ float sums[kThreads / 32][kTogether];
+  const int64_t t = blockIdx.x;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  for (int j0 = 0; j0 < g.top_k; j0 += kTogether) {
+    int row[kTogether];
+    float w[kTogether], acc[kTogether];
+#pragma unroll
+    for (int j = 0; j < kTogether; ++j) {
+      const bool there = j0 + j < g.top_k;
+      row[j] = there ? g.row_of[t * g.top_k + j0 + j] : -1;
+      if (!has_row(row[j], g.rows)) row[j] = -1;
+      w[j] = there && weights ? weights[t * g.top_k + j0 + j] : 1.0f;
+      acc[j] = 0.0f;
+    }
+    for (int64_t c = static_cast<int64_t>(threadIdx.x) * kVec; c < g.cols; c += kThreads * kVec) {
+      float d[kVec], v[kVec];
+      load_vec(dy + t * ld_dy + c, d);
+#pragma unroll
+      for (int j = 0; j < kTogether; ++j) {
+        if (row[j] < 0) continue;
+        if (dweights) {
+          load_vec(in + row[j] * ld_in + c, v);
+#pragma unroll
+          for (int i = 0; i < kVec; ++i) acc[j] = fmaf(d[i], v[i], acc[j]);
+        }
+        if (din) {
+#pragma unroll
+          for (int i = 0; i < kVec; ++i) v[i] = __fmul_rn(w[j], d[i]);
+          store_vec(din + row[j] * ld_din + c, v);
+        }
+      }
+    }
+    if (dweights) {
+#pragma unroll
+      for (int j = 0; j < kTogether; ++j) {
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) acc[j] += __shfl_xor_sync(kAll, acc[j], o);
+        if (lane == 0) sums[warp][j] = acc[j];
+      }
+      __syncthreads();
+      if (threadIdx.x < kTogether && j0 + static_cast<int>(threadIdx.x) < g.top_k) {
+        float s = 0.0f;
+        for (int i = 0; i < kThreads / 32; ++i) s += sums[i][threadIdx.x];
+        dweights[t * g.top_k + j0 + threadIdx.x] = s;
+      }
+      __syncthreads();
+    }
+  }
+}
+
+// ----------------------------------------------------------------------------- arguments
+bool type_ok(int dt) { return dt == HIF4_BF16 || dt == HIF4_FP16 || dt == HIF4_FP32; }
+int64_t type_size(int dt) { return dt == HIF4_FP32 ? 4 : 2; }
+uintptr_t bits(const void* p) { return reinterpret_cast<uintptr_t>(p); }
+bool aligned(const void* p, int64_t to) { return bits(p) % static_cast<uintptr_t>(to) == 0; }
+// Row r of a matrix starts at a multiple of 16 bytes, for every r.
+bool rows_aligned(const void* p, int64_t ld, int dt) { return aligned(p, 16) && ld * type_size(dt) % 16 == 0; }
+
+hif4_status check_sizes(int64_t tokens, int64_t cols, int64_t top_k, int64_t rows) {
+  if (tokens < 0 || cols < 0 || top_k < 1 || rows < 0) return HIF4_ERR_SHAPE;
+  if (top_k > 0x7FFFFFFFll || rows > 0x7FFFFFFFll || cols > (1ll << 40) || tokens > 0x7FFFFFFFll / top_k) return HIF4_ERR_SHAPE;
+  return HIF4_OK;
+}
+// Blocks of a token: enough that few tokens fill the GPU, no more than there is work for `per_block` elements each.
+hif4_status make_gather(Gather& g, int64_t tokens, int64_t cols, int64_t top_k, int64_t rows, const int32_t* row_of, int64_t per_block,
+                        int64_t* blocks) {
+  g.rows = rows; g.cols = cols; g.top_k = static_cast<int>(top_k); g.row_of = row_of;
+  const int64_t segments = ceil_div64(cols, per_block);
+  if (segments > 0x7FFFFFFFll / (tokens > 0 ? tokens : 1)) return HIF4_ERR_SHAPE;
+  g.segments = static_cast<int>(segments);
+  *blocks = tokens * segments;
+  return HIF4_OK;
+}
+
+template <typename Word>
+void launch_plain(const Gather& g, int64_t blocks, const hif4_dispatch_args& a, cudaStream_t st) {
+  const int64_t n = static_cast<int64_t>(sizeof(Word)) / type_size(a.dt);
+  dispatch_plain_kernel<Word><<<static_cast<unsigned>(blocks), kThreads, 0, st>>>(
+      g, static_cast<const Word*>(a.x), a.ld_x / n, static_cast<Word*>(a.out), a.ld_out / n, a.cols / n);
+}
+template <typename T>
+void launch_converted(const Gather& g, int64_t blocks, const hif4_dispatch_args& a, cudaStream_t st) {
+  const unsigned grid = static_cast<unsigned>(blocks);
+  const T* x = static_cast<const T*>(a.x);
+  if (a.kind == HIF4_ROWS_HIF4) {
+    uint32_t* out = static_cast<uint32_t*>(a.out);
+    if (a.mode == HIF4_RHA) dispatch_hif4_kernel<T, true><<<grid, kThreads, 0, st>>>(g, x, a.ld_x, out);
+    else dispatch_hif4_kernel<T, false><<<grid, kThreads, 0, st>>>(g, x, a.ld_x, out);
+  } else {
+    uint2* codes = static_cast<uint2*>(a.out);
+    uint8_t* scales = static_cast<uint8_t*>(a.out_scales);
+    if (a.kind == HIF4_ROWS_NVFP4) dispatch_bfp4_kernel<T, true><<<grid, kThreads, 0, st>>>(g, x, a.ld_x, a.gain, codes, scales);
+    else dispatch_bfp4_kernel<T, false><<<grid, kThreads, 0, st>>>(g, x, a.ld_x, a.gain, codes, scales);
+  }
+}
+
+template <typename TI, typename TO>
+hif4_status launch_combine(const hif4_combine_args& a, cudaStream_t st) {
+  const bool vec = a.cols % 8 == 0 && rows_aligned(a.in, a.ld_in, a.dt_in) && rows_aligned(a.residual, a.residual ? a.ld_residual : 8, a.dt) &&
+                   rows_aligned(a.y, a.ld_y, a.dt);
+  Gather g;
+  int64_t blocks = 0;
+  const hif4_status s = make_gather(g, a.tokens, a.cols, a.top_k, a.rows, a.row_of, kThreads * (vec ? 8 : 1), &blocks);
+  if (s != HIF4_OK) return s;
+  const auto kernel = vec ? combine_kernel<TI, TO, 8> : combine_kernel<TI, TO, 1>;
+  kernel<<<static_cast<unsigned>(blocks), kThreads, 0, st>>>(g, static_cast<const TI*>(a.in), a.ld_in, a.weights, static_cast<const TO*>(a.residual),
+                                                             a.ld_residual, a.res_scale, static_cast<TO*>(a.y), a.ld_y);
+  note_launch();
+  return launch_status();
+}
+template <typename TI, typename TD>
+hif4_status launch_combine_backward(const hif4_combine_backward_args& a, cudaStream_t st) {
+  const bool vec = a.cols % 8 == 0 && rows_aligned(a.dy, a.ld_dy, a.dt) && (!a.dweights || rows_aligned(a.in, a.ld_in, a.dt_in)) &&
+                   (!a.din || rows_aligned(a.din, a.ld_din, a.dt_in));
+  Gather g;
+  int64_t blocks = 0;
+  const hif4_status s = make_gather(g, a.tokens, a.cols, a.top_k, a.rows, a.row_of, a.cols > 0 ? a.cols : 1, &blocks);
+  if (s != HIF4_OK) return s;
+  const auto kernel = vec ? combine_backward_kernel<TD, TI, 8> : combine_backward_kernel<TD, TI, 1>;
+  kernel<<<static_cast<unsigned>(a.tokens), kThreads, 0, st>>>(g, static_cast<const TD*>(a.dy), a.ld_dy, a.weights, static_cast<const TI*>(a.in),
+                                                               a.ld_in, static_cast<TI*>(a.din), a.ld_din, a.dweights);
+  note_launch();
+  return launch_status();
+}
+
+}  // namespace
+}  // namespace hif4
+
+using namespace hif4;
+
+// f<type of the experts' rows, type of the tokens' rows>(a, st)
+#define HIF4_BY_TYPES(f, dt_in, dt, a, st)                                                                                       \
+  (dt_in == HIF4_BF16 ? (dt == HIF4_BF16 ? f<__nv_bfloat16, __nv_bfloat16>(a, st) : dt == HIF4_FP16 ? f<__nv_bfloat16, __half>(a, st) \
+                                                                                                    : f<__nv_bfloat16, float>(a, st)) \
+   : dt_in == HIF4_FP16 ? (dt == HIF4_BF16 ? f<__half, __nv_bfloat16>(a, st) : dt == HIF4_FP16 ? f<__half, __half>(a, st)         \
+                                                                                               : f<__half, float>(a, st))         \
+                        : (dt == HIF4_BF16 ? f<float, __nv_bfloat16>(a, st) : dt == HIF4_FP16 ? f<float, __half>(a, st) : f<float, float>(a, st)))
+
+extern "C" hif4_status hif4_expert_plan_workspace(int64_t tokens, int64_t top_k, int64_t experts, size_t* bytes) {
+  if (!bytes) return HIF4_ERR_NULL;
+  const hif4_status s = check_sizes(tokens, 0, top_k, 0);
+  if (s != HIF4_OK) return s;
+  if (experts < 1) return HIF4_ERR_SHAPE;
+  if (experts > HIF4_ROUTE_MAX_EXPERTS) return HIF4_ERR_UNSUPPORTED;
+  const int64_t blocks = ceil_div64(tokens * top_k, kPlanItems);
+  *bytes = blocks > 1 ? (static_cast<size_t>(blocks) * experts * sizeof(int32_t) + 255) / 256 * 256 : 0;
+  return HIF4_OK;
+}
+
+extern "C" hif4_status hif4_expert_plan(const int32_t* ids, int64_t tokens, int64_t top_k, int64_t experts, int64_t* offsets, int32_t* row_of,
+                                        void* workspace, size_t workspace_bytes, void* stream) {
+  size_t need = 0;
+  const hif4_status s = hif4_expert_plan_workspace(tokens, top_k, experts, &need);
+  if (s != HIF4_OK) return s;
+  const int64_t n = tokens * top_k;
+  if (!offsets || (n > 0 && (!ids || !row_of)) || (need > 0 && !workspace)) return HIF4_ERR_NULL;
+  if (!aligned(ids, 4) || !aligned(row_of, 4) || !aligned(offsets, 8) || (need > 0 && !aligned(workspace, 256))) return HIF4_ERR_ALIGN;
+  if (workspace_bytes < need) return HIF4_ERR_WORKSPACE;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  const int64_t blocks = n > kPlanItems ? ceil_div64(n, kPlanItems) : 1;
+  const int smem = static_cast<int>(experts) * kPlanWarps * 4;
+  static uint64_t ready = 0;
+  if (smem > 48 * 1024 && !ensure_dynamic_smem(plan_place_kernel, HIF4_ROUTE_MAX_EXPERTS * kPlanWarps * 4, ready)) return HIF4_ERR_CUDA;
+  int32_t* counts = static_cast<int32_t*>(workspace);
+  if (blocks > 1) {
+    plan_count_kernel<<<static_cast<unsigned>(blocks), kPlanWarps * 32, experts * 4, st>>>(ids, n, static_cast<int>(experts), counts);
+    note_launch();
+  }
+  plan_place_kernel<<<static_cast<unsigned>(blocks), kPlanWarps * 32, smem, st>>>(ids, n, static_cast<int>(experts), counts,
+                                                                                  static_cast<int>(blocks), offsets, row_of);
+  note_launch();
+  return launch_status();
+}
+
+extern "C" hif4_status hif4_dispatch(const hif4_dispatch_args* args, void* stream) {
+  if (!args) return HIF4_ERR_NULL;
+  const hif4_dispatch_args& a = *args;
+  hif4_status s = check_sizes(a.tokens, a.cols, a.top_k, a.rows);
+  if (s != HIF4_OK) return s;
+  if (!type_ok(a.dt) || a.kind < HIF4_ROWS_PLAIN || a.kind > HIF4_ROWS_NVFP4 || (a.kind == HIF4_ROWS_HIF4 && a.mode != HIF4_RNE && a.mode != HIF4_RHA))
+    return HIF4_ERR_DTYPE;
+  const bool plain = a.kind == HIF4_ROWS_PLAIN, scaled = a.kind == HIF4_ROWS_MXFP4 || a.kind == HIF4_ROWS_NVFP4;
+  if (a.ld_x < a.cols || (plain && a.ld_out < a.cols) || (!plain && a.cols % kUnitElems != 0)) return HIF4_ERR_SHAPE;
+  if (a.tokens == 0 || a.cols == 0 || a.rows == 0) return HIF4_OK;
+  if (!a.x || !a.row_of || !a.out || (scaled && !a.out_scales)) return HIF4_ERR_NULL;
+  if (!aligned(a.row_of, 4) || !aligned(a.x, type_size(a.dt)) || (plain && !aligned(a.out, type_size(a.dt))) ||
+      (!plain && !rows_aligned(a.x, a.ld_x, a.dt)) || (a.kind == HIF4_ROWS_HIF4 && !aligned(a.out, 4)) ||
+      (scaled && (!aligned(a.out, 16) || !aligned(a.out_scales, 16) || !aligned(a.gain, 4))))
+    return HIF4_ERR_ALIGN;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  Gather g;
+  int64_t blocks = 0;
+  if (plain) {
+    const int64_t e = type_size(a.dt);
+    const uintptr_t all = bits(a.x) | bits(a.out) | static_cast<uintptr_t>(a.cols * e) | static_cast<uintptr_t>(a.tokens > 1 ? a.ld_x * e : 0) |
+                          static_cast<uintptr_t>(a.rows > 1 ? a.ld_out * e : 0);
+    const int64_t word = all % 16 == 0 ? 16 : all % 4 == 0 ? 4 : 2;
+    s = make_gather(g, a.tokens, a.cols, a.top_k, a.rows, a.row_of, kThreads * word / e, &blocks);
+    if (s != HIF4_OK) return s;
+    if (word == 16) launch_plain<uint4>(g, blocks, a, st);
+    else if (word == 4) launch_plain<uint32_t>(g, blocks, a, st);
+    else launch_plain<uint16_t>(g, blocks, a, st);
+  } else {
+    s = make_gather(g, a.tokens, a.cols, a.top_k, a.rows, a.row_of, a.kind == HIF4_ROWS_HIF4 ? kThreads * 8 : kThreads * 16, &blocks);
+    if (s != HIF4_OK) return s;
+    if (a.dt == HIF4_BF16) launch_converted<__nv_bfloat16>(g, blocks, a, st);
+    else if (a.dt == HIF4_FP16) launch_converted<__half>(g, blocks, a, st);
+    else launch_converted<float>(g, blocks, a, st);
+  }
+  note_launch();
+  return launch_status();
+}
+
+extern "C" hif4_status hif4_combine(const hif4_combine_args* args, void* stream) {
+  if (!args) return HIF4_ERR_NULL;
+  const hif4_combine_args& a = *args;
+  const hif4_status s = check_sizes(a.tokens, a.cols, a.top_k, a.rows);
+  if (s != HIF4_OK) return s;
+  if (!type_ok(a.dt) || !type_ok(a.dt_in)) return HIF4_ERR_DTYPE;
+  if (a.ld_in < a.cols || a.ld_y < a.cols || (a.residual && a.ld_residual < a.cols)) return HIF4_ERR_SHAPE;
+  if (a.tokens == 0 || a.cols == 0) return HIF4_OK;
+  if ((!a.in && a.rows > 0) || !a.row_of || !a.y) return HIF4_ERR_NULL;
+  if (!aligned(a.in, type_size(a.dt_in)) || !aligned(a.row_of, 4) || !aligned(a.weights, 4) || !aligned(a.residual, type_size(a.dt)) ||
+      !aligned(a.y, type_size(a.dt)))
+    return HIF4_ERR_ALIGN;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  return HIF4_BY_TYPES(launch_combine, a.dt_in, a.dt, a, st);
+}
+
+extern "C" hif4_status hif4_combine_backward(const hif4_combine_backward_args* args, void* stream) {
+  if (!args) return HIF4_ERR_NULL;
+  const hif4_combine_backward_args& a = *args;
+  const hif4_status s = check_sizes(a.tokens, a.cols, a.top_k, a.rows);
+  if (s != HIF4_OK) return s;
+  if (!type_ok(a.dt) || !type_ok(a.dt_in)) return HIF4_ERR_DTYPE;
+  if (a.ld_dy < a.cols || (a.din && a.ld_din < a.cols) || (a.dweights && a.ld_in < a.cols)) return HIF4_ERR_SHAPE;
+  if (a.tokens == 0 || (!a.din && !a.dweights)) return HIF4_OK;
+  if ((!a.dy && a.cols > 0) || !a.row_of || (a.dweights && !a.in && a.rows > 0 && a.cols > 0)) return HIF4_ERR_NULL;
+  if (!aligned(a.dy, type_size(a.dt)) || !aligned(a.row_of, 4) || !aligned(a.weights, 4) || !aligned(a.in, type_size(a.dt_in)) ||
+      !aligned(a.din, type_size(a.dt_in)) || !aligned(a.dweights, 4))
+    return HIF4_ERR_ALIGN;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  return HIF4_BY_TYPES(launch_combine_backward, a.dt_in, a.dt, a, st);
+}

@@ -1,4 +1,4 @@
-// The calls between two linears of a block for PyTorch tensors: checks, output and workspace allocation, current stream, and
+// The calls between two linears of a block, around the experts' products and in microscaled formats for PyTorch tensors: checks, output and workspace allocation, current stream, and
 // the C call, without the interpreter in between (a call of one token costs the host less than the GPU).  The Python names,
 // defaults and documentation are in binding.py, which passes every argument by position.
 //
@@ -418,7 +418,344 @@ PyObject* linear_act_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// ------------------------------------------------------------------------------------- around the experts' products
+at::ScalarType scalar_type(int64_t c, at::ScalarType otherwise) {
+  return c == HIF4_BF16 ? at::kBFloat16 : c == HIF4_FP32 ? at::kFloat : c == HIF4_FP16 ? at::kHalf : otherwise;
+}
+// A contiguous tensor of these sizes.
+void* array(const at::Tensor* t, at::IntArrayRef sizes, at::ScalarType type, const char* what) {
+  if (!t) return nullptr;
+  need_cuda(*t);
+  if (t->scalar_type() != type || t->sizes() != sizes || !t->is_contiguous()) {
+    std::string want;
+    for (int64_t n : sizes) want += (want.empty() ? "" : ", ") + std::to_string(n);
+    throw std::invalid_argument(std::string(what) + ": contiguous [" + want + "] of " + c10::toString(type) + " expected, got " + about(*t));
+  }
+  return t->data_ptr();
+}
+const at::Tensor& matrix_of(PyObject* o, const char* what) {
+  const at::Tensor& t = tensor(o, what);
+  if (t.dim() != 2) throw std::invalid_argument(std::string(what) + ": a matrix expected, got " + about(t));
+  return t;
+}
+PyObject* pair(const at::Tensor& a, const at::Tensor& b) {
+  PyObject* r = PyTuple_New(2);
+  if (!r) return nullptr;
+  PyTuple_SET_ITEM(r, 0, wrap(a));
+  PyTuple_SET_ITEM(r, 1, wrap(b));
+  return r;
+}
+// (codes, scales)
+void two(PyObject* o, const char* what, const at::Tensor*& codes, const at::Tensor*& scales) {
+  const bool tuple = PyTuple_Check(o);
+  if (!(tuple ? PyTuple_GET_SIZE(o) == 2 : PyList_Check(o) && PyList_GET_SIZE(o) == 2)) throw TypeProblem(std::string(what) + ": a pair (codes, scales) expected");
+  codes = &tensor(tuple ? PyTuple_GET_ITEM(o, 0) : PyList_GET_ITEM(o, 0), what);
+  scales = &tensor(tuple ? PyTuple_GET_ITEM(o, 1) : PyList_GET_ITEM(o, 1), what);
+}
+int64_t scale_words(int64_t cols, int fmt) { const int64_t span = fmt == HIF4_FMT_MXFP4 ? 512 : 256; return (cols + span - 1) / span; }
+struct Packed { int64_t rows, cols; void *codes, *scales; };
+// A packed matrix, or `groups` of them of equal size (groups < 0: no such dimension).
+Packed packed(PyObject* o, int fmt, int64_t groups, const char* what) {
+  const at::Tensor *c, *s;
+  two(o, what, c, s);
+  const bool many = groups >= 0;
+  if (c->dim() != (many ? 3 : 2)) throw std::invalid_argument(std::string(what) + ": codes " + (many ? "[groups, rows, cols / 2]" : "[rows, cols / 2]") + " expected, got " + about(*c));
+  Packed p;
+  p.rows = c->size(many ? 1 : 0);
+  p.cols = c->size(many ? 2 : 1) * 2;
+  const int64_t words = scale_words(p.cols, fmt);
+  p.codes = array(c, c->sizes(), at::kByte, what);
+  p.scales = many ? array(s, {c->size(0), words, p.rows, 16}, at::kByte, what) : array(s, {words, p.rows, 16}, at::kByte, what);
+  if (many && c->size(0) != groups) throw std::invalid_argument(std::string(what) + ": " + std::to_string(groups) + " groups expected, got " + about(*c));
+  return p;
+}
+// Memory for one, or the caller's.
+struct PackedOut { at::Tensor codes, scales; };
+PackedOut packed_out(PyObject* out, int64_t rows, int64_t cols, int fmt, const at::Tensor& like) {
+  PackedOut p;
+  const int64_t words = scale_words(cols, fmt);
+  if (out != Py_None) {
+    const at::Tensor *c, *s;
+    two(out, "out", c, s);
+    array(c, {rows, cols / 2}, at::kByte, "out");
+    array(s, {words, rows, 16}, at::kByte, "out");
+    p.codes = *c;
+    p.scales = *s;
+  } else {
+    p.codes = at::empty({rows, cols / 2}, like.options().dtype(at::kByte));
+    p.scales = at::empty({words, rows, 16}, like.options().dtype(at::kByte));
+  }
+  return p;
+}
+float* gain_of(PyObject* o, const char* what) {
+  const at::Tensor* g = tensor_or_null(o, what);
+  return static_cast<float*>(vector(g, 1, at::kFloat, what));
+}
+
+// (logits, top_k, bias, score, groups, top_groups, group_best, renormalize, scale) -> (ids, weights)
+PyObject* route(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 9, [&]() -> PyObject* {
+    const at::Tensor& logits = matrix_of(a[0], "logits");
+    const OnDeviceOf on(logits);
+    hif4_route_args p{};
+    p.tokens = logits.size(0); p.experts = logits.size(1); p.top_k = integer(a[1]);
+    const Mat m = matrix(&logits, p.tokens, p.experts, logits.scalar_type(), "logits");
+    p.logits = m.p; p.ld_logits = m.ld;
+    p.dt = static_cast<hif4_dtype>(type_code(logits.scalar_type()));
+    p.bias = static_cast<const float*>(vector(tensor_or_null(a[2], "bias"), p.experts, at::kFloat, "bias"));
+    p.score = static_cast<hif4_score>(code(a[3]));
+    p.groups = integer(a[4]); p.top_groups = integer(a[5]); p.group_best = integer(a[6]);
+    p.renormalize = truth(a[7]) ? 1 : 0;
+    p.scale = static_cast<float>(real(a[8]));
+    if (p.top_k < 1 || p.top_k > p.experts) return status(HIF4_ERR_SHAPE);
+    const at::Tensor ids = at::empty({p.tokens, p.top_k}, logits.options().dtype(at::kInt)), w = new_rows(p.tokens, p.top_k, at::kFloat, logits);
+    p.ids = at_of<int32_t>(ids);
+    p.weights = at_of<float>(w);
+    const hif4_status s = hif4_route(&p, stream_of(logits));
+    return s == HIF4_OK ? pair(ids, w) : status(s);
+  });
+}
+
+// (dweights, logits, ids, score, renormalize, scale) -> dlogits
+PyObject* route_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 6, [&]() -> PyObject* {
+    const at::Tensor &logits = matrix_of(a[1], "logits"), &ids = matrix_of(a[2], "ids"), &dw = matrix_of(a[0], "dweights");
+    const OnDeviceOf on(logits);
+    hif4_route_backward_args p{};
+    p.tokens = logits.size(0); p.experts = logits.size(1); p.top_k = ids.size(1);
+    const Mat m = matrix(&logits, p.tokens, p.experts, logits.scalar_type(), "logits");
+    p.logits = m.p; p.ld_logits = m.ld;
+    p.dt = static_cast<hif4_dtype>(type_code(logits.scalar_type()));
+    p.ids = static_cast<const int32_t*>(array(&ids, {p.tokens, p.top_k}, at::kInt, "ids"));
+    p.dweights = static_cast<const float*>(array(&dw, {p.tokens, p.top_k}, at::kFloat, "dweights"));
+    p.score = static_cast<hif4_score>(code(a[3]));
+    p.renormalize = truth(a[4]) ? 1 : 0;
+    p.scale = static_cast<float>(real(a[5]));
+    const at::Tensor d = new_rows(p.tokens, p.experts, logits.scalar_type(), logits);
+    p.dlogits = d.data_ptr(); p.ld_dlogits = p.experts;
+    const hif4_status s = hif4_route_backward(&p, stream_of(logits));
+    return s == HIF4_OK ? wrap(d) : status(s);
+  });
+}
+
+// (ids, experts, workspace) -> (offsets, row_of)
+PyObject* expert_plan(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 3, [&]() -> PyObject* {
+    const at::Tensor &ids = matrix_of(a[0], "ids"), *ws = tensor_or_null(a[2], "workspace");
+    const OnDeviceOf on(ids);
+    const int64_t tokens = ids.size(0), k = ids.size(1), experts = integer(a[1]);
+    const int32_t* p = static_cast<const int32_t*>(array(&ids, {tokens, k}, at::kInt, "ids"));
+    size_t need = 0;
+    hif4_status s = hif4_expert_plan_workspace(tokens, k, experts, &need);
+    if (s != HIF4_OK) return status(s);
+    const at::Tensor offsets = at::empty({experts + 1}, ids.options().dtype(at::kLong)), row_of = at::empty({tokens, k}, ids.options());
+    const Workspace space(ws, need, ids);
+    s = hif4_expert_plan(p, tokens, k, experts, at_of<int64_t>(offsets), at_of<int32_t>(row_of), space.p, space.bytes, stream_of(ids));
+    return s == HIF4_OK ? pair(offsets, row_of) : status(s);
+  });
+}
+
+// (x, row_of, kind, rows or -1, mode, gain, out) -> rows, units or (codes, scales)
+PyObject* dispatch(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 7, [&]() -> PyObject* {
+    const at::Tensor &x = matrix_of(a[0], "x"), &row_of = matrix_of(a[1], "row_of");
+    const OnDeviceOf on(x);
+    hif4_dispatch_args p{};
+    p.tokens = x.size(0); p.cols = x.size(1); p.top_k = row_of.size(1);
+    const Mat m = matrix(&x, p.tokens, p.cols, x.scalar_type(), "x");
+    p.x = m.p; p.ld_x = m.ld;
+    p.dt = static_cast<hif4_dtype>(type_code(x.scalar_type()));
+    p.row_of = static_cast<const int32_t*>(array(&row_of, {p.tokens, p.top_k}, at::kInt, "row_of"));
+    p.kind = static_cast<hif4_rows_kind>(code(a[2]));
+    p.mode = static_cast<hif4_round>(code(a[4]));
+    p.gain = gain_of(a[5], "gain");
+    p.rows = integer(a[3]);
+    const bool scaled = p.kind == HIF4_ROWS_MXFP4 || p.kind == HIF4_ROWS_NVFP4;
+    if (p.kind > HIF4_ROWS_NVFP4) return status(HIF4_ERR_DTYPE);
+    if (p.kind != HIF4_ROWS_PLAIN && p.cols % HIF4_UNIT_ELEMS != 0) return status(HIF4_ERR_SHAPE);
+    if (p.gain && !scaled) throw std::invalid_argument("gain: MXFP4 and NVFP4 only");
+    const at::Tensor* out = scaled ? nullptr : tensor_or_null(a[6], "out");
+    if (p.rows < 0) {
+      if (out && out->dim() > 0) p.rows = out->size(0);
+      else if (scaled && a[6] != Py_None) {
+        const at::Tensor *c, *sc;
+        two(a[6], "out", c, sc);
+        p.rows = c->dim() > 0 ? c->size(0) : 0;
+      } else p.rows = row_of.numel();
+    }
+    at::Tensor rows, scales;
+    if (scaled) {
+      const PackedOut q = packed_out(a[6], p.rows, p.cols, p.kind == HIF4_ROWS_MXFP4 ? HIF4_FMT_MXFP4 : HIF4_FMT_NVFP4, x);
+      rows = q.codes;
+      scales = q.scales;
+      p.out = rows.data_ptr();
+      p.out_scales = scales.data_ptr();
+    } else if (p.kind == HIF4_ROWS_HIF4) {
+      rows = out ? *out : new_units(p.rows, p.cols / HIF4_UNIT_ELEMS, x);
+      p.out = units(&rows, p.rows, p.cols / HIF4_UNIT_ELEMS, "out");
+    } else {
+      rows = out ? *out : new_rows(p.rows, p.cols, x.scalar_type(), x);
+      const Mat mo = matrix(&rows, p.rows, p.cols, x.scalar_type(), "out");
+      p.out = mo.p; p.ld_out = mo.ld;
+    }
+    const hif4_status s = hif4_dispatch(&p, stream_of(x));
+    if (s != HIF4_OK) return status(s);
+    if (a[6] != Py_None) { Py_INCREF(a[6]); return a[6]; }
+    return scaled ? pair(rows, scales) : wrap(rows);
+  });
+}
+
+// (rows, row_of, weights, residual, res_scale, dtype code or -1, out) -> y
+PyObject* combine(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 7, [&]() -> PyObject* {
+    const at::Tensor &rows = matrix_of(a[0], "rows"), &row_of = matrix_of(a[1], "row_of");
+    const at::Tensor *w = tensor_or_null(a[2], "weights"), *res = tensor_or_null(a[3], "residual"), *out = tensor_or_null(a[6], "out");
+    const OnDeviceOf on(rows);
+    hif4_combine_args p{};
+    p.tokens = row_of.size(0); p.cols = rows.size(1); p.top_k = row_of.size(1); p.rows = rows.size(0);
+    const Mat m = matrix(&rows, p.rows, p.cols, rows.scalar_type(), "rows");
+    p.in = m.p; p.ld_in = m.ld;
+    p.dt_in = static_cast<hif4_dtype>(type_code(rows.scalar_type()));
+    p.row_of = static_cast<const int32_t*>(array(&row_of, {p.tokens, p.top_k}, at::kInt, "row_of"));
+    p.weights = static_cast<const float*>(array(w, {p.tokens, p.top_k}, at::kFloat, "weights"));
+    const at::ScalarType type = scalar_type(integer(a[5]), out ? out->scalar_type() : res ? res->scalar_type() : rows.scalar_type());
+    p.dt = static_cast<hif4_dtype>(type_code(type));
+    const Mat mr = matrix(res, p.tokens, p.cols, type, "residual");
+    p.residual = mr.p; p.ld_residual = mr.ld;
+    p.res_scale = static_cast<float>(real(a[4]));
+    at::Tensor y = out ? *out : new_rows(p.tokens, p.cols, type, rows);
+    const Mat my = matrix(&y, p.tokens, p.cols, type, "out");
+    p.y = my.p; p.ld_y = my.ld;
+    const hif4_status s = hif4_combine(&p, stream_of(rows));
+    if (s != HIF4_OK) return status(s);
+    if (out) { Py_INCREF(a[6]); return a[6]; }
+    return wrap(y);
+  });
+}
+
+// (dy, row_of, weights, rows, number of rows or -1, dtype code of drows or -1, wanted, out) -> (drows, dweights), `wanted` the
+// sum of 1 (drows) and 2 (dweights)
+PyObject* combine_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 8, [&]() -> PyObject* {
+    const at::Tensor &dy = matrix_of(a[0], "dy"), &row_of = matrix_of(a[1], "row_of");
+    const at::Tensor *w = tensor_or_null(a[2], "weights"), *rows = tensor_or_null(a[3], "rows"), *out = tensor_or_null(a[7], "out");
+    const OnDeviceOf on(dy);
+    hif4_combine_backward_args p{};
+    p.tokens = dy.size(0); p.cols = dy.size(1); p.top_k = row_of.size(1);
+    const int64_t given = integer(a[4]), wanted = integer(a[6]);
+    if ((rows && rows->dim() != 2) || (out && out->dim() != 2)) throw std::invalid_argument("rows, out: matrices expected");
+    p.rows = given >= 0 ? given : rows ? rows->size(0) : out ? out->size(0) : row_of.numel();
+    const Mat m = matrix(&dy, p.tokens, p.cols, dy.scalar_type(), "dy");
+    p.dy = m.p; p.ld_dy = m.ld;
+    p.dt = static_cast<hif4_dtype>(type_code(dy.scalar_type()));
+    p.row_of = static_cast<const int32_t*>(array(&row_of, {p.tokens, p.top_k}, at::kInt, "row_of"));
+    p.weights = static_cast<const float*>(array(w, {p.tokens, p.top_k}, at::kFloat, "weights"));
+    const at::ScalarType type = scalar_type(integer(a[5]), rows ? rows->scalar_type() : out ? out->scalar_type() : dy.scalar_type());
+    p.dt_in = static_cast<hif4_dtype>(type_code(type));
+    const Mat mi = matrix(rows, p.rows, p.cols, type, "rows");
+    p.in = mi.p; p.ld_in = mi.ld;
+    at::Tensor drows, dw;
+    if (wanted & 1) {
+      drows = out ? *out : new_rows(p.rows, p.cols, type, dy);
+      const Mat mo = matrix(&drows, p.rows, p.cols, type, "out");
+      p.din = mo.p; p.ld_din = mo.ld;
+    }
+    if (wanted & 2) {
+      if (!rows) throw std::invalid_argument("rows: needed for the gradient of the weights");
+      dw = new_rows(p.tokens, p.top_k, at::kFloat, dy);
+      p.dweights = at_of<float>(dw);
+    }
+    const hif4_status s = hif4_combine_backward(&p, stream_of(dy));
+    return s == HIF4_OK ? pair(drows, dw) : status(s);
+  });
+}
+
+// ------------------------------------------------------------------------------------- microscaled 4-bit formats
+// (src, fmt, transposed, gain, out) -> (codes, scales)
+PyObject* bfp4_quantize(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 5, [&]() -> PyObject* {
+    const at::Tensor& src = matrix_of(a[0], "src");
+    const OnDeviceOf on(src);
+    const int fmt = code(a[1]);
+    const bool down = truth(a[2]);
+    const int64_t rows = src.size(0), cols = src.size(1);
+    const Mat m = matrix(&src, rows, cols, src.scalar_type(), "src");
+    const hif4_dtype dt = static_cast<hif4_dtype>(type_code(src.scalar_type()));
+    const float* gain = gain_of(a[3], "gain");
+    if ((down ? rows : cols) % HIF4_UNIT_ELEMS != 0) return status(HIF4_ERR_SHAPE);
+    const PackedOut q = packed_out(a[4], down ? cols : rows, down ? rows : cols, fmt, src);
+    const hif4_status s = (down ? hif4_bfp4_quantize_transposed : hif4_bfp4_quantize)(
+        m.p, dt, rows, cols, m.ld, static_cast<hif4_bfp4_format>(fmt), gain, q.codes.data_ptr(), q.scales.data_ptr(), stream_of(src));
+    if (s != HIF4_OK) return status(s);
+    if (a[4] != Py_None) { Py_INCREF(a[4]); return a[4]; }
+    return pair(q.codes, q.scales);
+  });
+}
+
+// ((codes, scales), fmt, dtype code, gain, out) -> values
+PyObject* bfp4_dequantize(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 5, [&]() -> PyObject* {
+    const at::Tensor *c, *sc;
+    two(a[0], "packed", c, sc);
+    const OnDeviceOf on(*c);
+    const int fmt = code(a[1]);
+    const Packed q = packed(a[0], fmt, -1, "packed");
+    const at::Tensor* out = tensor_or_null(a[4], "out");
+    const at::ScalarType type = out ? out->scalar_type() : scalar_type(integer(a[2]), at::kBFloat16);
+    at::Tensor y = out ? *out : new_rows(q.rows, q.cols, type, *c);
+    const Mat m = matrix(&y, q.rows, q.cols, type, "out");
+    const hif4_status s = hif4_bfp4_dequantize(q.codes, q.scales, q.rows, q.cols, static_cast<hif4_bfp4_format>(fmt), gain_of(a[3], "gain"), m.p,
+                                               static_cast<hif4_dtype>(type_code(type)), m.ld, stream_of(*c));
+    if (s != HIF4_OK) return status(s);
+    if (out) { Py_INCREF(a[4]); return a[4]; }
+    return wrap(y);
+  });
+}
+
+// ((codes, scales) of A, of B, offsets or None, fmt, alpha, dtype code, out) -> Y
+PyObject* bfp4_gemm(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 7, [&]() -> PyObject* {
+    const at::Tensor *ac, *as;
+    two(a[0], "a", ac, as);
+    const OnDeviceOf on(*ac);
+    const at::Tensor *offsets = tensor_or_null(a[2], "group_offsets"), *alpha = tensor_or_null(a[4], "alpha"), *out = tensor_or_null(a[6], "out");
+    const int fmt = code(a[3]);
+    int64_t groups = -1;
+    if (offsets) {
+      if (offsets->dim() != 1 || offsets->size(0) < 1 || offsets->size(0) > 0x7FFFFFFF) throw std::invalid_argument("group_offsets: [groups + 1] of int64 expected, got " + about(*offsets));
+      groups = offsets->size(0) - 1;
+    }
+    const Packed A = packed(a[0], fmt, -1, "a"), B = packed(a[1], fmt, groups, "b");
+    if (A.cols != B.cols) throw std::invalid_argument("a and b: rows of " + std::to_string(A.cols) + " and " + std::to_string(B.cols) + " elements");
+    hif4_bfp4_gemm_args p{};
+    p.M = A.rows; p.N = B.rows; p.K = A.cols;
+    p.fmt = static_cast<hif4_bfp4_format>(fmt);
+    p.A_codes = A.codes; p.A_scales = A.scales;
+    p.B_codes = B.codes; p.B_scales = B.scales;
+    p.alpha = static_cast<const float*>(vector(alpha, offsets ? groups : 1, at::kFloat, "alpha"));
+    const at::ScalarType type = out ? out->scalar_type() : scalar_type(integer(a[5]), at::kBFloat16);
+    p.dt = static_cast<hif4_dtype>(type_code(type));
+    at::Tensor y = out ? *out : new_rows(p.M, p.N, type, *ac);
+    const Mat m = matrix(&y, p.M, p.N, type, "out");
+    p.Y = m.p; p.ld_y = m.ld;
+    hif4_status s;
+    if (offsets) {
+      p.num_groups = static_cast<int>(groups);
+      p.group_offsets = static_cast<const int64_t*>(vector(offsets, groups + 1, at::kLong, "group_offsets"));
+      s = hif4_bfp4_grouped_gemm(&p, stream_of(*ac));
+    } else {
+      s = hif4_bfp4_gemm(&p, stream_of(*ac));
+    }
+    if (s != HIF4_OK) return status(s);
+    if (out) { Py_INCREF(a[6]); return a[6]; }
+    return wrap(y);
+  });
+}
+
+#define HIF4_METHOD(f) {#f, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {
+    HIF4_METHOD(route), HIF4_METHOD(route_backward), HIF4_METHOD(expert_plan), HIF4_METHOD(dispatch), HIF4_METHOD(combine),
+    HIF4_METHOD(combine_backward), HIF4_METHOD(bfp4_quantize), HIF4_METHOD(bfp4_dequantize), HIF4_METHOD(bfp4_gemm),
     {"block_norm", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(block_norm)), METH_FASTCALL, nullptr},
     {"block_norm_backward", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(block_norm_backward)), METH_FASTCALL, nullptr},
     {"linear_act", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(linear_act)), METH_FASTCALL, nullptr},
