@@ -1,48 +1,37 @@
 // hif4_bfp4_quantize, hif4_bfp4_quantize_transposed, hif4_bfp4_dequantize -- MXFP4 and NVFP4 operands from BF16, FP16
 // and FP32 matrices and back.  HBM bound: 2 (4) bytes read and 0.53 (MXFP4) or 0.5625 (NVFP4) written per element.
 #include "hif4_bfp4_device.cuh"
-#include "hif4_vec8.cuh"
+#include "hif4_tc_common.cuh"
 
 namespace hif4 {
 namespace {
 
 constexpr int kThreads = 256;
 
-template <typename T>
-__device__ __forceinline__ void load16(const T* p, float (&v)[16]) {
-  float a[8];
-  unpack8(load8(p), a);
-#pragma unroll
-  for (int i = 0; i < 8; ++i) v[i] = a[i];
-  unpack8(load8(p + 8), a);
-#pragma unroll
-  for (int i = 0; i < 8; ++i) v[8 + i] = a[i];
-}
-
 // A thread converts sixteen elements: a block of NVFP4, half a block of MXFP4 (its neighbour has the other half).
 template <typename T, bool kNv>
 __global__ void __launch_bounds__(kThreads)
-bfp4_quantize_kernel(const T* __restrict__ src, int64_t rows, int64_t n16, int64_t ld, const float* __restrict__ gain,
+bfp4_quantize_kernel(const T* __restrict__ src, int64_t rows, int64_t items, Divider n16, int64_t ld, int wide, const float* __restrict__ gain,
                      uint2* __restrict__ codes, uint8_t* __restrict__ scales) {
-  const int64_t i = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x;
-  const bool in = i < rows * n16;
-  const int64_t row = in ? i / n16 : 0, c = in ? i - row * n16 : 0;
-  float v[16];
-  load16(src + row * ld + 16 * c, v);
-  if (gain) {
-    const float g = *gain;
-#pragma unroll
-    for (int k = 0; k < 16; ++k) v[k] = __fmul_rn(v[k], g);
+  grid_launch_next();
+  for (int64_t first = static_cast<int64_t>(blockIdx.x) * kThreads; first < items; first += static_cast<int64_t>(gridDim.x) * kThreads) {
+    const int64_t i = first + threadIdx.x;
+    const bool in = i < items;
+    const int64_t at = in ? i : 0;
+    const int64_t row = items <= 0x7FFFFFFF ? n16.quotient(static_cast<uint32_t>(at)) : at / n16.d;
+    const uint32_t c = static_cast<uint32_t>(at - row * n16.d);
+    Sixteen v = sixteen_of(load_raw16(src + row * ld + 16 * static_cast<int64_t>(c), wide));
+    if (gain) scale16(v, *gain);
+    uint32_t peak = peak16(v), byte;
+    if (!kNv) peak = max(peak, __shfl_xor_sync(0xFFFFFFFFu, peak, 1));
+    const uint2 code = encode16<kNv>(v, peak, byte);
+    if (!in) continue;
+    codes[i] = code;
+    const uint32_t block = kNv ? c : c >> 1;
+    if (kNv || !(c & 1)) scales[scale_at(row, block, rows)] = static_cast<uint8_t>(byte);
+    if (c == n16.d - 1)
+      for (uint32_t b = block + 1; b & 15; ++b) scales[scale_at(row, b, rows)] = 0;
   }
-  uint32_t peak = peak16(v), byte;
-  if (!kNv) peak = max(peak, __shfl_xor_sync(0xFFFFFFFFu, peak, 1));
-  const uint2 code = encode16<kNv>(v, peak, byte);
-  if (!in) return;
-  codes[i] = code;
-  const int64_t block = kNv ? c : c >> 1;
-  if (kNv || !(c & 1)) scales[scale_at(row, block, rows)] = static_cast<uint8_t>(byte);
-  if (c == n16 - 1)
-    for (int64_t b = block + 1; b & 15; ++b) scales[scale_at(row, b, rows)] = 0;
 }
 
 // Tile of 256 rows x 32 columns in shared memory; a thread converts 32 rows of one column.
@@ -65,13 +54,15 @@ bfp4_quantize_transposed_kernel(const T* __restrict__ src, int64_t rows, int64_t
   const int64_t c = c0 + lane, r = r0 + (threadIdx.x >> 5) * 32;
   if (c >= cols || r >= rows) return;
   const T* mine = tile + (threadIdx.x >> 5) * 32 * kTileCols + lane;
-  const float g = gain ? *gain : 1.0f;
-  float a[16], b[16];
+  Sixteen a, b;
 #pragma unroll
-  for (int k = 0; k < 16; ++k) {
-    a[k] = to_f32(mine[k * kTileCols]);
-    b[k] = to_f32(mine[(16 + k) * kTileCols]);
-    if (gain) { a[k] = __fmul_rn(a[k], g); b[k] = __fmul_rn(b[k], g); }
+  for (int k = 0; k < 8; ++k) {
+    a.p[k] = make_float2(to_f32(mine[2 * k * kTileCols]), to_f32(mine[(2 * k + 1) * kTileCols]));
+    b.p[k] = make_float2(to_f32(mine[(16 + 2 * k) * kTileCols]), to_f32(mine[(17 + 2 * k) * kTileCols]));
+  }
+  if (gain) {
+    scale16(a, *gain);
+    scale16(b, *gain);
   }
   uint32_t pa = peak16(a), pb = peak16(b), sa, sb;
   if (!kNv) pa = pb = max(pa, pb);
@@ -84,29 +75,73 @@ bfp4_quantize_transposed_kernel(const T* __restrict__ src, int64_t rows, int64_t
     for (++block; block & 15; ++block) scales[scale_at(c, block, cols)] = 0;
 }
 
+// Sixteen values m s (m an E2M1 number), or m s / g.  Only 1 and 1.5 times a power of two occur among the m, so two divisions make
+// all quotients of a block, the rest are exact products with powers of two; where those might leave FP32's range each
+// element is divided.
 template <typename T, bool kNv>
-__global__ void __launch_bounds__(kThreads)
-bfp4_dequantize_kernel(const uint2* __restrict__ codes, const uint8_t* __restrict__ scales, int64_t rows, int64_t n16,
-                       const float* __restrict__ gain, T* __restrict__ dst, int64_t ld) {
-  const int64_t i = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x;
-  if (i >= rows * n16) return;
-  const int64_t row = i / n16, c = i - row * n16;
-  const uint2 code = codes[i];
-  const float s = scale_value<kNv>(scales[scale_at(row, kNv ? c : c >> 1, rows)]);
-  float v[16];
+__device__ __forceinline__ void decode16(uint2 code, uint32_t byte, const float* gain, float (&v)[16]) {
+  const float s = scale_value<kNv>(byte);
   e2m1_to8(code.x, v);
   e2m1_to8(code.y, v + 8);
-  const float g = gain ? *gain : 1.0f;
-  float lo[8], hi[8];
+  if (!gain) {
 #pragma unroll
-  for (int k = 0; k < 8; ++k) {
-    lo[k] = __fmul_rn(v[k], s);
-    hi[k] = __fmul_rn(v[8 + k], s);
-    if (gain) { lo[k] = __fdiv_rn(lo[k], g); hi[k] = __fdiv_rn(hi[k], g); }
+    for (int k = 0; k < 16; ++k) v[k] *= s;
+    return;
   }
-  T* p = dst + row * ld + 16 * c;
-  store8(p, pack8<T>(lo));
-  store8(p + 8, pack8<T>(hi));
+  const float g = *gain, d1 = __fdiv_rn(s, g), d3 = __fdiv_rn(1.5f * s, g), size = fabsf(d1);
+  if (size > 0x1p-100f && size < 0x1p100f && s > 0x1p-120f) {
+#pragma unroll
+    for (int k = 0; k < 16; ++k) {
+      const uint32_t m = __float_as_uint(v[k]);
+      v[k] = __uint_as_float(m & 0xFF800000u) * ((m & 0x00400000u) ? d3 : d1);
+    }
+  } else {
+#pragma unroll
+    for (int k = 0; k < 16; ++k) v[k] = __fdiv_rn(__fmul_rn(v[k], s), g);
+  }
+}
+
+__device__ __forceinline__ void store32(void* p, const uint32_t* w) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]),
+               "r"(w[6]), "r"(w[7]) : "memory");
+}
+__device__ __forceinline__ void store_row16(__nv_bfloat16* p, const float (&v)[16], bool wide) {
+  uint32_t w[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) w[i] = pack2(v[2 * i], v[2 * i + 1], __nv_bfloat16());
+  if (wide) {
+    store32(p, w);
+  } else {
+    reinterpret_cast<uint4*>(p)[0] = make_uint4(w[0], w[1], w[2], w[3]);
+    reinterpret_cast<uint4*>(p)[1] = make_uint4(w[4], w[5], w[6], w[7]);
+  }
+}
+__device__ __forceinline__ void store_row16(float* p, const float (&v)[16], bool wide) {
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    uint32_t w[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) w[i] = __float_as_uint(v[8 * h + i]);
+    if (wide) {
+      store32(p + 8 * h, w);
+    } else {
+      reinterpret_cast<uint4*>(p + 8 * h)[0] = make_uint4(w[0], w[1], w[2], w[3]);
+      reinterpret_cast<uint4*>(p + 8 * h)[1] = make_uint4(w[4], w[5], w[6], w[7]);
+    }
+  }
+}
+
+template <typename T, bool kNv>
+__global__ void __launch_bounds__(kThreads)
+bfp4_dequantize_kernel(const uint2* __restrict__ codes, const uint8_t* __restrict__ scales, int64_t rows, int64_t items, Divider n16,
+                       const float* __restrict__ gain, T* __restrict__ dst, int64_t ld, int wide) {
+  for (int64_t i = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x; i < items; i += static_cast<int64_t>(gridDim.x) * kThreads) {
+    const int64_t row = items <= 0x7FFFFFFF ? n16.quotient(static_cast<uint32_t>(i)) : i / n16.d;
+    const uint32_t c = static_cast<uint32_t>(i - row * n16.d);
+    float v[16];
+    decode16<T, kNv>(codes[i], scales[scale_at(row, kNv ? c : c >> 1, rows)], gain, v);
+    store_row16(dst + row * ld + 16 * static_cast<int64_t>(c), v, wide);
+  }
 }
 
 bool format_ok(int fmt) { return fmt == HIF4_FMT_MXFP4 || fmt == HIF4_FMT_NVFP4; }
@@ -132,11 +167,17 @@ extern "C" size_t hif4_bfp4_scale_bytes(int64_t rows, int64_t cols, hif4_bfp4_fo
   } while (0)
 
 namespace {
+unsigned blocks_for(int64_t items) {
+  const int64_t blocks = ceil_div64(items, kThreads);
+  return static_cast<unsigned>(blocks < 0x7FFFFFFFll ? blocks : 0x7FFFFFFFll);
+}
+int rows_wide(const void* p, int64_t ld, size_t size) { return (reinterpret_cast<uintptr_t>(p) | static_cast<uintptr_t>(ld) * size) % 32 == 0; }
 template <typename T, bool kNv>
 void quantize_rows(const void* src, int64_t rows, int64_t cols, int64_t ld, const float* gain, void* codes, void* scales, cudaStream_t st) {
-  const int64_t blocks = ceil_div64(rows * (cols / 16), kThreads);
-  bfp4_quantize_kernel<T, kNv><<<static_cast<unsigned>(blocks), kThreads, 0, st>>>(static_cast<const T*>(src), rows, cols / 16, ld, gain,
-                                                                                    static_cast<uint2*>(codes), static_cast<uint8_t*>(scales));
+  const int64_t items = rows * (cols / 16);
+  bfp4_quantize_kernel<T, kNv><<<blocks_for(items), kThreads, 0, st>>>(static_cast<const T*>(src), rows, items, make_divider(static_cast<uint32_t>(cols / 16)),
+                                                                       ld, rows_wide(src, ld, sizeof(T)), gain, static_cast<uint2*>(codes),
+                                                                       static_cast<uint8_t*>(scales));
 }
 template <typename T, bool kNv>
 void quantize_columns(const void* src, int64_t rows, int64_t cols, int64_t ld, const float* gain, void* codes, void* scales, cudaStream_t st) {
@@ -146,9 +187,10 @@ void quantize_columns(const void* src, int64_t rows, int64_t cols, int64_t ld, c
 }
 template <typename T, bool kNv>
 void dequantize_rows(const void* codes, const void* scales, int64_t rows, int64_t cols, const float* gain, void* dst, int64_t ld, cudaStream_t st) {
-  const int64_t blocks = ceil_div64(rows * (cols / 16), kThreads);
-  bfp4_dequantize_kernel<T, kNv><<<static_cast<unsigned>(blocks), kThreads, 0, st>>>(
-      static_cast<const uint2*>(codes), static_cast<const uint8_t*>(scales), rows, cols / 16, gain, static_cast<T*>(dst), ld);
+  const int64_t items = rows * (cols / 16);
+  bfp4_dequantize_kernel<T, kNv><<<blocks_for(items), kThreads, 0, st>>>(
+      static_cast<const uint2*>(codes), static_cast<const uint8_t*>(scales), rows, items, make_divider(static_cast<uint32_t>(cols / 16)), gain,
+      static_cast<T*>(dst), ld, rows_wide(dst, ld, sizeof(T)));
 }
 hif4_status check(const void* src, hif4_dtype dt, int64_t rows, int64_t cols, int64_t ld, hif4_bfp4_format fmt, const float* gain,
                   const void* codes, const void* scales) {

@@ -6,7 +6,7 @@
 #pragma once
 #include <cuda_fp16.h>
 
-#include "hif4_common.cuh"
+#include "hif4_vec8.cuh"
 
 namespace hif4 {
 namespace {
@@ -57,34 +57,133 @@ template <bool kNv> __device__ __forceinline__ float scale_value(uint32_t byte) 
   return kNv ? e4m3_value(byte) : e8m0_value(byte);
 }
 
-// Largest |v| of sixteen values as a bit pattern (a NaN sorts above infinity).
-__device__ __forceinline__ uint32_t peak16(const float (&v)[16]) {
-  uint32_t p = 0u;
-#pragma unroll
-  for (int i = 0; i < 16; ++i) p = max(p, __float_as_uint(v[i]) & 0x7FFFFFFFu);
-  return p;
+// Sixteen elements of a matrix row, as pairs.
+struct Sixteen { float2 p[8]; };
+template <typename T> struct Raw16 { uint32_t w[8 * sizeof(T) / 2]; };
+// One 32-byte instruction per lane (two for FP32): a warp's lanes lie side by side, so every sector is touched once.
+__device__ __forceinline__ void load32(const void* p, uint32_t* w) {
+  asm volatile("ld.global.nc.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7]) : "l"(p));
 }
+__device__ __forceinline__ void load16b(const void* p, uint32_t* w) {
+  const uint4 v = __ldg(static_cast<const uint4*>(p));
+  w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
+}
+// `wide`: the address is a multiple of 32 bytes.
+template <typename T>
+__device__ __forceinline__ Raw16<T> load_raw16(const T* p, bool wide) {
+  Raw16<T> r;
+  constexpr int kParts = static_cast<int>(sizeof(T)) / 2;
+#pragma unroll
+  for (int i = 0; i < kParts; ++i) {
+    if (wide) load32(reinterpret_cast<const char*>(p) + 32 * i, r.w + 8 * i);
+    else {
+      load16b(reinterpret_cast<const char*>(p) + 32 * i, r.w + 8 * i);
+      load16b(reinterpret_cast<const char*>(p) + 32 * i + 16, r.w + 8 * i + 4);
+    }
+  }
+  return r;
+}
+__device__ __forceinline__ Sixteen sixteen_of(const Raw16<__nv_bfloat16>& r) {
+  Sixteen v;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v.p[i] = make_float2(__uint_as_float(r.w[i] << 16), __uint_as_float(r.w[i] & 0xFFFF0000u));
+  return v;
+}
+__device__ __forceinline__ Sixteen sixteen_of(const Raw16<__half>& r) {
+  Sixteen v;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v.p[i] = __half22float2(*reinterpret_cast<const __half2*>(&r.w[i]));
+  return v;
+}
+__device__ __forceinline__ Sixteen sixteen_of(const Raw16<float>& r) {
+  Sixteen v;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v.p[i] = make_float2(__uint_as_float(r.w[2 * i]), __uint_as_float(r.w[2 * i + 1]));
+  return v;
+}
+__device__ __forceinline__ void scale16(Sixteen& v, float gain) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v.p[i] = mul2(v.p[i], both(gain));
+}
+
+// Largest of three magnitudes; a NaN stays one.
+__device__ __forceinline__ float max3_nan(float a, float b, float c) {
+  float d;
+  asm("{\n\t.reg .f32 x, y, z;\n\tabs.f32 x, %1;\n\tabs.f32 y, %2;\n\tabs.f32 z, %3;\n\tmax.NaN.f32 %0, x, y, z;\n\t}" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
+// Largest |v| of sixteen values as a bit pattern (a NaN sorts above infinity).
+__device__ __forceinline__ uint32_t peak16(const Sixteen& v) {
+  float p = 0.0f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) p = max3_nan(p, v.p[i].x, v.p[i].y);
+  return __float_as_uint(p);
+}
+
+constexpr uint32_t kInfBits = 0x7F800000u, kMostBits = 0x7F7FFFFFu;
+// a / b by the reciprocal y of b and one correction from the exact remainder: q0 = a y, q = q0 + (a - q0 b) y.  Before its
+// last rounding q is off by 2^-46 of its value at most.  For b of up to four significant bits (an E4M3 scale, 6) and a of 24 no
+// quotient lies that near to the middle between two FP32 numbers: a = m b with an odd 25-bit m would need 26 bits.  So q is a / b
+// rounded once, like __fdiv_rn, at a quarter of its instructions.
+__device__ __forceinline__ float2 divide2(float2 a, float2 minus_b, float2 y) {
+  const float2 q0 = mul2(a, y);
+  return fma2(fma2(q0, minus_b, a), y, q0);
+}
+
 // Sixteen values of a block whose peak is given -> codes (element i in nibble i) and the block's scale byte.
 template <bool kNv>
-__device__ __forceinline__ uint2 encode16(const float (&v)[16], uint32_t peak, uint32_t& byte) {
-  if (peak > 0x7F800000u) {
+__device__ __forceinline__ uint2 encode16(Sixteen v, uint32_t peak, uint32_t& byte) {
+  if (peak > kInfBits) {
     byte = kNv ? 0x7Fu : 0xFFu;
     return make_uint2(0u, 0u);
   }
   float q[16];
   if (kNv) {
-    byte = e4m3_of(__fdiv_rn(__uint_as_float(peak), 6.0f));
-    const float s = e4m3_value(byte);
+    if (peak == kInfBits) {                              // saturates as the largest number does
+      peak = kMostBits;
+      const float most = __uint_as_float(kMostBits);
 #pragma unroll
-    for (int i = 0; i < 16; ++i) q[i] = byte ? __fdiv_rn(v[i], s) : __uint_as_float(__float_as_uint(v[i]) & 0x80000000u);
+      for (int i = 0; i < 8; ++i) v.p[i] = make_float2(fminf(fmaxf(v.p[i].x, -most), most), fminf(fmaxf(v.p[i].y, -most), most));
+    }
+    const float p = __uint_as_float(peak);
+    byte = e4m3_of(divide2(both(p), both(-6.0f), both(1.0f / 6.0f)).x);
+    const float s = e4m3_value(byte);
+    const float2 y = both(byte ? __frcp_rn(s) : 0.0f), minus_s = both(-s);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float2 d = divide2(v.p[i], minus_s, y);
+      q[2 * i] = __uint_as_float(__float_as_uint(d.x) | (__float_as_uint(v.p[i].x) & 0x80000000u));        // -0 keeps its sign
+      q[2 * i + 1] = __uint_as_float(__float_as_uint(d.y) | (__float_as_uint(v.p[i].y) & 0x80000000u));
+    }
   } else {
     const int e = max(static_cast<int>(peak >> 23) - 127 - 2, -127);     // floor(log2 peak) - 2; infinity: 126
     byte = peak ? static_cast<uint32_t>(e + 127) : 0u;
-    const float inv = __uint_as_float(static_cast<uint32_t>(127 - e) << 23);      // the division by a power of two is exact
+    const float2 inv = both(__uint_as_float(static_cast<uint32_t>(127 - e) << 23));      // the division by a power of two is exact
 #pragma unroll
-    for (int i = 0; i < 16; ++i) q[i] = __fmul_rn(v[i], inv);
+    for (int i = 0; i < 8; ++i) {
+      const float2 d = mul2(v.p[i], inv);
+      q[2 * i] = d.x;
+      q[2 * i + 1] = d.y;
+    }
   }
   return make_uint2(e2m1_of8(q), e2m1_of8(q + 8));
+}
+
+// Item and block numbers as row and column: division by a number known at launch (Granlund and Montgomery's multiplication by a
+// rounded-up reciprocal; exact for dividends below 2^31).
+struct Divider {
+  uint32_t d, mul, shift;
+  __device__ __forceinline__ uint32_t quotient(uint32_t n) const { return d == 1u ? n : __umulhi(n, mul) >> shift; }
+};
+inline Divider make_divider(uint32_t d) {
+  Divider r{d, 0u, 0u};
+  if (d <= 1u) return r;
+  uint32_t log = 0;
+  while ((1ull << log) < d) ++log;
+  r.shift = log - 1;
+  r.mul = static_cast<uint32_t>(((1ull << (31 + log)) + d - 1) / d);
+  return r;
 }
 
 // Scales of a matrix: [words][rows][16 bytes].

@@ -168,18 +168,8 @@ dispatch_bfp4_kernel(Gather g, const T* __restrict__ x, int64_t ld_x, const floa
   const int64_t n16 = g.cols / 16;
   for (int64_t c0 = static_cast<int64_t>(seg) * kThreads; c0 < n16; c0 += static_cast<int64_t>(g.segments) * kThreads) {
     const int64_t mine = c0 + threadIdx.x, c = mine < n16 ? mine : n16 - 2 + (threadIdx.x & 1);
-    float v[16], a[8];
-    unpack8(load8(x + t * ld_x + 16 * c), a);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = a[i];
-    unpack8(load8(x + t * ld_x + 16 * c + 8), a);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[8 + i] = a[i];
-    if (gain) {
-      const float f = *gain;
-#pragma unroll
-      for (int i = 0; i < 16; ++i) v[i] = __fmul_rn(v[i], f);
-    }
+    Sixteen v = sixteen_of(load_raw16(x + t * ld_x + 16 * c, false));
+    if (gain) scale16(v, *gain);
     uint32_t peak = peak16(v), byte;
     if (!kNv) peak = max(peak, __shfl_xor_sync(kAll, peak, 1));
     const uint2 code = encode16<kNv>(v, peak, byte);

@@ -1,9 +1,15 @@
 // hif4_route / hif4_route_backward -- which experts a token goes to, with which weights, and the weights' gradient.
 //
-// A warp holds the scores of one token: lane l has the experts l, l + 32, ...  The choice is an order, so it is made in
-// 64 bits: two experts whose choices differ by less than FP32 holds would otherwise change places from one
-// implementation to the next.  Weights and gradients are FP32.
-#include "hif4_common.cuh"
+// A warp routes a token: lane l holds V consecutive experts, so that the lowest lane holds the lowest index and a group of
+// experts is a run of lanes.  The best of the warp is one redux over keys (the bits of a choice, made to order like whole
+// numbers) and one ballot; only the lane it came from looks through its experts again.
+//
+// The order is that of the choices in 64 bits: two experts whose choices differ by less than FP32 holds would change
+// places from one implementation to the next.  Choices are made in FP32 first, whose error is bounded (below); only where two
+// that are neighbours in the order, or the last group kept and the first left, are nearer than that, the warp starts again in
+// 64 bits.  16384 tokens x 256 experts in 8 groups: 74 us with every choice in 64 bits, 64-bit shuffles and a lane
+// per group.  Bound by instruction issue (16.8 MB of logits would take 2.6 us).
+#include "hif4_tc_common.cuh"
 #include "hif4_vec8.cuh"
 
 namespace hif4 {
@@ -27,15 +33,27 @@ __device__ __forceinline__ double warp_sum(double v) {
   for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(kAll, v, o);
   return v;
 }
-// Largest value of the warp and its place; of equal ones the lowest place.
-__device__ __forceinline__ void warp_best(double& v, int& at) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) {
-    const double w = __shfl_xor_sync(kAll, v, o);
-    const int b = __shfl_xor_sync(kAll, at, o);
-    if (w > v || (w == v && b < at)) { v = w; at = b; }
+
+// Numbers as whole numbers of the same order (no NaN; -0 below +0, which no choice is by itself).
+template <bool kWide> struct Keys;
+template <> struct Keys<false> {
+  using Real = float;
+  using Key = int;
+  static __device__ __forceinline__ Key of(float v) { const int b = __float_as_int(v + 0.0f); return b ^ ((b >> 31) & 0x7FFFFFFF); }
+  static __device__ __forceinline__ float value(Key k) { return __int_as_float(k ^ ((k >> 31) & 0x7FFFFFFF)); }
+  static __device__ __forceinline__ Key warp_max(Key k) { return __reduce_max_sync(kAll, k); }
+};
+template <> struct Keys<true> {
+  using Real = double;
+  using Key = long long;
+  static __device__ __forceinline__ Key of(double v) { const long long b = __double_as_longlong(v + 0.0); return b ^ ((b >> 63) & 0x7FFFFFFFFFFFFFFFll); }
+  static __device__ __forceinline__ double value(Key k) { return __longlong_as_double(k ^ ((k >> 63) & 0x7FFFFFFFFFFFFFFFll)); }
+  static __device__ __forceinline__ Key warp_max(Key k) {
+    const int high = __reduce_max_sync(kAll, static_cast<int>(k >> 32));
+    const unsigned low = __reduce_max_sync(kAll, static_cast<int>(k >> 32) == high ? static_cast<unsigned>(k) : 0u);
+    return (static_cast<long long>(high) << 32) | low;
   }
-}
+};
 
 // Sigmoid of x times e^-m, m = min(0, largest x of the sum): a common factor of all terms of a ratio, so that no ratio of very
 // small sigmoids loses its terms.
@@ -43,136 +61,230 @@ __device__ __forceinline__ float sigmoid_scaled(float x, float m) {
   return x > 0.0f ? 1.0f / (1.0f + expf(-x)) : expf(x - m) / (1.0f + expf(x));
 }
 
+struct RouteParams {
+  int64_t tokens, ld;
+  int experts, top_k, sigmoid, by_logit, groups, per, top_groups, group_best, renormalize, vec;
+  float scale;
+  const float* bias;
+};
+
+__device__ __forceinline__ float fast_rcp(float v) {
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+  return r;
+}
+
+// The choice of one token.  x: the lane's logits (-inf past the last expert), b: its biases, top: the largest logit that is a
+// number.  Lane j gets the j-th expert's index (or -1) and logit.  Returns whether neighbours were too near to tell apart.
+//
+// Errors in FP32: a sigmoid 1 / (1 + e) with e = exp2(-x log2 e): 2^-22.5 from exp2 and |x| 2^-24 from its argument reach the
+// result through e / (1 + e)^2 <= 1/4 (and |x| e / (1 + e)^2 < 0.23), 1 + e and the reciprocal add 2^-24 + 2^-23: together below
+// 2^-22; two of them 2^-21, taken as 2^-20.  A softmax the same, relative to the largest.  The bias's addition 2^-24 of the sum.
+template <bool kWide, int V>
+__device__ __forceinline__ bool choose(const float (&x)[V], const float (&b)[V], float top, const RouteParams& p, long long* scratch, int lane, int& id, float& xc) {
+  using K = Keys<kWide>;
+  using Real = typename K::Real;
+  using Key = typename K::Key;
+  const float kInf = __int_as_float(0x7F800000);
+  const Key none = K::of(static_cast<Real>(-kInf));
+  Key c[V];
+  Real near = 0;                                        // how near two choices may be and still be told apart
+  if (p.by_logit) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) c[i] = x[i] != x[i] ? none : K::of(static_cast<Real>(x[i]));
+  } else {
+    Real v[V];
+    if (p.sigmoid) {
+#pragma unroll
+      for (int i = 0; i < V; ++i)
+        v[i] = kWide ? static_cast<Real>(1.0 / (1.0 + exp(-static_cast<double>(x[i])))) : static_cast<Real>(fast_rcp(1.0f + __expf(-x[i])));
+      near = static_cast<Real>(0x1p-20);
+    } else {
+      Real total = 0;
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        v[i] = x[i] == top ? Real(1) : kWide ? static_cast<Real>(exp(static_cast<double>(x[i]) - static_cast<double>(top))) : static_cast<Real>(__expf(x[i] - top));
+        if (x[i] != x[i] || top == -kInf) v[i] = 0;
+        total += v[i];
+      }
+      total = warp_sum(total);
+      const Real inv = total > 0 ? Real(1) / total : Real(0);
+#pragma unroll
+      for (int i = 0; i < V; ++i) v[i] = kWide ? (total > 0 ? v[i] / total : v[i]) : v[i] * inv;
+      near = static_cast<Real>(0x1p-19) * inv;
+    }
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      v[i] += static_cast<Real>(b[i]);
+      c[i] = x[i] == -kInf || x[i] != x[i] || v[i] != v[i] ? none : K::of(v[i]);
+    }
+  }
+  const auto told_apart = [&](Key high, Key low, Real margin) {      // (a key of none is far from all others)
+    if (p.by_logit || kWide || low == none) return true;
+    const Real h = K::value(high);
+    return h - K::value(low) > margin + static_cast<Real>(0x1p-21) * fmaxf(fabsf(h), fabsf(K::value(low)));
+  };
+  bool contested = false;
+
+  if (p.top_groups < p.groups) {
+    const int span = p.per / V;                         // lanes of a group, where groups are whole lanes
+    const bool whole = p.per % V == 0 && (span & (span - 1)) == 0;
+    Key value = none;
+    if (whole) {
+      Key first = none, second = none;
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        second = max(second, min(first, c[i]));
+        first = max(first, c[i]);
+      }
+      for (int o = 1; o < span; o <<= 1) {
+        const Key f = __shfl_xor_sync(kAll, first, o), s = __shfl_xor_sync(kAll, second, o);
+        second = max(min(first, f), max(second, s));
+        first = max(first, f);
+      }
+      value = first;
+      if (p.group_best == 2) value = first == none || second == none ? none : K::of(K::value(first) + K::value(second));
+      if (lane >= p.groups * span) value = none;
+    } else {
+      Key* mine = reinterpret_cast<Key*>(scratch);
+#pragma unroll
+      for (int i = 0; i < V; ++i)
+        if (lane * V + i < p.experts) mine[lane * V + i] = c[i];
+      __syncwarp();
+      if (lane < p.groups) {
+        Key first = none, second = none;
+        for (int e = 0; e < p.per; ++e) {
+          const Key v = mine[lane * p.per + e];
+          second = max(second, min(first, v));
+          first = max(first, v);
+        }
+        value = first;
+        if (p.group_best == 2) value = first == none || second == none ? none : K::of(K::value(first) + K::value(second));
+      }
+      __syncwarp();
+    }
+    uint32_t open = 0u;
+    Key last = none;
+    bool free = whole ? lane < p.groups * span : lane < p.groups;
+    const int own = whole ? lane / span : lane;
+    for (int n = 0; n < p.top_groups; ++n) {
+      last = K::warp_max(free ? value : none);
+      const int g = __shfl_sync(kAll, own, __ffs(__ballot_sync(kAll, free && value == last)) - 1);
+      open |= 1u << g;
+      if (own == g) free = false;
+    }
+    contested = !told_apart(last, K::warp_max(free ? value : none), 2 * near);
+    int g = lane * V / p.per, left = p.per - (lane * V - g * p.per);
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      if (!((open >> (g & 31)) & 1u)) c[i] = none;
+      if (--left == 0) { ++g; left = p.per; }
+    }
+  }
+
+  id = -1;
+  xc = -kInf;
+  Key before = none;
+  int at = 0;
+  Key best = c[0];
+#pragma unroll
+  for (int i = 1; i < V; ++i)
+    if (c[i] > best) { best = c[i]; at = i; }
+  for (int j = 0; j <= p.top_k; ++j) {                  // the last round only looks at who would be next
+    const Key most = K::warp_max(best);
+    if (j > 0) contested |= !told_apart(before, most, near);
+    if (most == none || j == p.top_k) break;
+    before = most;
+    const int from = __ffs(__ballot_sync(kAll, best == most)) - 1;
+    float mine = 0.0f;
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+      if (i == at) mine = x[i];
+    const int e = __shfl_sync(kAll, lane * V + at, from);
+    mine = __shfl_sync(kAll, mine, from);
+    if (lane == j) { id = e; xc = mine; }
+    if (lane == from) {
+#pragma unroll
+      for (int i = 0; i < V; ++i)
+        if (i == at) c[i] = none;
+      best = c[0];
+      at = 0;
+#pragma unroll
+      for (int i = 1; i < V; ++i)
+        if (c[i] > best) { best = c[i]; at = i; }
+    }
+  }
+  return contested;
+}
+
 // V: experts a lane holds (experts <= 32 V).
 template <typename T, int V>
 __global__ void __launch_bounds__(kRouteWarps * 32)
-route_kernel(const T* __restrict__ logits, int64_t ld, int64_t tokens, int experts, int top_k, const float* __restrict__ bias,
-             int sigmoid, int groups, int top_groups, int group_best, int renormalize, float scale, int32_t* __restrict__ ids,
-             float* __restrict__ weights) {
-  extern __shared__ double choices[];                   // [warps][groups][experts / groups + 1], with more than one group
-  const double kNone = -__longlong_as_double(0x7FF0000000000000ll);
+route_kernel(const T* __restrict__ logits, const RouteParams p, int32_t* __restrict__ ids, float* __restrict__ weights) {
+  extern __shared__ long long scratch[];                // [warps][experts], where groups are not whole lanes
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int64_t t = static_cast<int64_t>(blockIdx.x) * kRouteWarps + warp;
-  if (t >= tokens) return;
-  const T* row = logits + t * ld;
   const float kInf = __int_as_float(0x7F800000);
-  float x[V];
-  float top = -kInf;
-  bool bad = false;
+  float b[V];
 #pragma unroll
-  for (int i = 0; i < V; ++i) {
-    const int e = i * 32 + lane;
-    x[i] = e < experts ? to_f32(row[e]) : -kInf;
-    bad |= x[i] != x[i];
-    top = fmaxf(top, x[i]);
-  }
-  top = warp_max(top);
-  bad = __any_sync(kAll, bad) || (!sigmoid && top == kInf);
-
-  // choices in 64 bits
-  const bool by_logit = !bias && (groups == 1 || group_best == 1);
-  double c[V];
-  if (by_logit) {
+  for (int i = 0; i < V; ++i) b[i] = p.bias && lane * V + i < p.experts ? p.bias[lane * V + i] : 0.0f;
+  for (int64_t t = static_cast<int64_t>(blockIdx.x) * kRouteWarps + warp; t < p.tokens; t += static_cast<int64_t>(gridDim.x) * kRouteWarps) {
+    const T* row = logits + t * p.ld + lane * V;
+    float x[V];
+    if (p.vec && (lane + 1) * V <= p.experts) {          // 16-byte loads
+      constexpr int kWords = static_cast<int>(V * sizeof(T) / 4);
+      if constexpr (kWords >= 4 && kWords % 4 == 0) {
+        uint32_t w[kWords];
 #pragma unroll
-    for (int i = 0; i < V; ++i) c[i] = x[i] != x[i] ? kNone : static_cast<double>(x[i]);
-  } else {
-    double total = 0.0;
+        for (int i = 0; i < kWords; i += 4) {
+          const uint4 q = __ldg(reinterpret_cast<const uint4*>(row) + i / 4);
+          w[i] = q.x; w[i + 1] = q.y; w[i + 2] = q.z; w[i + 3] = q.w;
+        }
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-      if (sigmoid) {
-        c[i] = 1.0 / (1.0 + exp(-static_cast<double>(x[i])));
-      } else {
-        c[i] = x[i] == top ? 1.0 : x[i] != x[i] ? 0.0 : exp(static_cast<double>(x[i]) - static_cast<double>(top));
-        if (top == -kInf) c[i] = 0.0;
-        total += c[i];
+        for (int i = 0; i < V; ++i) x[i] = to_f32(reinterpret_cast<const T*>(w)[i]);
       }
+    } else {
+#pragma unroll
+      for (int i = 0; i < V; ++i) x[i] = lane * V + i < p.experts ? to_f32(row[i]) : -kInf;
     }
-    if (!sigmoid) total = warp_sum(total);
+    float top = -kInf;
+    bool bad = false;
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-      const int e = i * 32 + lane;
-      if (!sigmoid && total > 0.0) c[i] /= total;
-      if (bias && e < experts) c[i] += static_cast<double>(bias[e]);
-      if (e >= experts || x[i] == -kInf || !(c[i] >= kNone) || x[i] != x[i]) c[i] = kNone;
+      bad |= x[i] != x[i];
+      top = fmaxf(top, x[i]);
     }
-  }
+    top = Keys<false>::value(Keys<false>::warp_max(Keys<false>::of(top)));
+    bad = __any_sync(kAll, bad) || (!p.sigmoid && top == kInf);
 
-  if (groups > 1) {
-    const int per = experts / groups;
-    double* mine = choices + static_cast<size_t>(warp) * groups * (per + 1);
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-      const int e = i * 32 + lane;
-      if (e < experts) mine[e + e / per] = c[i];
-    }
-    __syncwarp();
-    double value = kNone;
-    if (lane < groups) {
-      double first = kNone, second = kNone;
-      for (int e = 0; e < per; ++e) {
-        const double v = mine[lane * (per + 1) + e];
-        if (v > first) { second = first; first = v; }
-        else if (v > second) second = v;
+    int id;                                             // lane j: the j-th choice and its logit
+    float xc;
+    long long* mine = scratch + static_cast<size_t>(warp) * p.experts;
+    if (choose<false, V>(x, b, top, p, mine, lane, id, xc)) choose<true, V>(x, b, top, p, mine, lane, id, xc);
+
+    float w = 0.0f;
+    const float high = Keys<false>::value(Keys<false>::warp_max(Keys<false>::of(xc)));       // of the chosen
+    if (p.sigmoid) {
+      const float m = p.renormalize ? fminf(0.0f, high) : 0.0f;
+      w = id >= 0 ? sigmoid_scaled(xc, m) : 0.0f;
+      if (p.renormalize) {
+        const float sum = warp_sum(w);
+        w = sum > 0.0f ? w / sum : 0.0f;
       }
-      value = group_best == 2 ? first + second : first;
-      if (!(value >= kNone)) value = kNone;
-    }
-    uint32_t open = 0u;
-    for (int n = 0; n < top_groups; ++n) {
-      double v = value;
-      int at = lane < groups && !((open >> lane) & 1u) ? lane : 64;
-      if (at == 64) v = kNone;
-      warp_best(v, at);
-      open |= 1u << (at & 31);
-    }
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-      const int e = i * 32 + lane;
-      if (e < experts && !((open >> (e / per)) & 1u)) c[i] = kNone;
-    }
-  }
-
-  int id = -1;                                          // lane j: the j-th choice and its logit
-  float xc = -kInf;
-  for (int j = 0; j < top_k; ++j) {
-    double v = kNone;
-    int at = 1 << 30;
-#pragma unroll
-    for (int i = 0; i < V; ++i)
-      if (c[i] > v) { v = c[i]; at = i * 32 + lane; }
-    warp_best(v, at);
-    if (v == kNone) break;
-    float xv = 0.0f;
-#pragma unroll
-    for (int i = 0; i < V; ++i)
-      if (at == i * 32 + lane) { c[i] = kNone; xv = x[i]; }
-    xv = __shfl_sync(kAll, xv, at & 31);
-    if (lane == j) { id = at; xc = xv; }
-  }
-
-  float w = 0.0f;
-  const float high = warp_max(xc);                      // of the chosen
-  if (sigmoid) {
-    const float m = renormalize ? fminf(0.0f, high) : 0.0f;
-    w = id >= 0 ? sigmoid_scaled(xc, m) : 0.0f;
-    if (renormalize) {
+    } else if (p.renormalize) {
+      w = id >= 0 ? expf(xc - high) : 0.0f;
       const float sum = warp_sum(w);
       w = sum > 0.0f ? w / sum : 0.0f;
-    }
-  } else if (renormalize) {
-    w = id >= 0 ? expf(xc - high) : 0.0f;
-    const float sum = warp_sum(w);
-    w = sum > 0.0f ? w / sum : 0.0f;
-  } else {
-    float sum = 0.0f;
+    } else {
+      float sum = 0.0f;
 #pragma unroll
-    for (int i = 0; i < V; ++i) sum += expf(x[i] - top);
-    sum = warp_sum(sum);
-    w = id >= 0 ? expf(xc - top) / sum : 0.0f;
-  }
-  if (lane < top_k) {
-    ids[t * top_k + lane] = id;
-    weights[t * top_k + lane] = bad ? __int_as_float(0x7FC00000) : scale * w;
+      for (int i = 0; i < V; ++i) sum += expf(x[i] - top);
+      sum = warp_sum(sum);
+      w = id >= 0 ? expf(xc - top) / sum : 0.0f;
+    }
+    if (lane < p.top_k) {
+      ids[t * p.top_k + lane] = id;
+      weights[t * p.top_k + lane] = bad ? __int_as_float(0x7FC00000) : p.scale * w;
+    }
   }
 }
 
@@ -247,14 +359,30 @@ route_backward_kernel(const T* __restrict__ logits, int64_t ld, int64_t tokens, 
   }
 }
 
+bool type_ok(int dt) { return dt == HIF4_BF16 || dt == HIF4_FP16 || dt == HIF4_FP32; }
+size_t type_size(int dt) { return dt == HIF4_FP32 ? 4 : 2; }
+bool aligned(const void* p, size_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
+
 template <typename T, int V>
 hif4_status launch_route(const hif4_route_args& a, cudaStream_t st) {
-  const int64_t blocks = ceil_div64(a.tokens, kRouteWarps);
-  const int groups = static_cast<int>(a.groups), experts = static_cast<int>(a.experts);
-  const size_t smem = groups > 1 ? sizeof(double) * kRouteWarps * (experts + groups) : 0;
-  route_kernel<T, V><<<static_cast<unsigned>(blocks), kRouteWarps * 32, smem, st>>>(
-      static_cast<const T*>(a.logits), a.ld_logits, a.tokens, experts, static_cast<int>(a.top_k), a.bias, a.score == HIF4_SCORE_SIGMOID,
-      groups, static_cast<int>(a.top_groups), static_cast<int>(a.group_best), a.renormalize != 0, a.scale, a.ids, a.weights);
+  RouteParams p{};
+  p.tokens = a.tokens; p.ld = a.ld_logits;
+  p.experts = static_cast<int>(a.experts); p.top_k = static_cast<int>(a.top_k);
+  p.sigmoid = a.score == HIF4_SCORE_SIGMOID;
+  p.groups = static_cast<int>(a.groups); p.per = p.experts / p.groups;
+  p.top_groups = static_cast<int>(a.top_groups); p.group_best = static_cast<int>(a.group_best);
+  p.by_logit = !a.bias && (p.groups == 1 || p.group_best == 1);
+  p.renormalize = a.renormalize != 0;
+  p.vec = aligned(a.logits, 16) && a.ld_logits * type_size(a.dt) % 16 == 0 && V * sizeof(T) % 16 == 0;
+  p.scale = a.scale;
+  p.bias = a.bias;
+  const int span = p.per / V;
+  const bool scratch = p.top_groups < p.groups && (p.per % V != 0 || (span & (span - 1)) != 0);
+  const size_t smem = scratch ? sizeof(long long) * kRouteWarps * p.experts : 0;
+  // every warp keeps the biases of its experts over the tokens it routes
+  const int64_t most = static_cast<int64_t>(sm_count()) * 16, blocks = ceil_div64(a.tokens, kRouteWarps);
+  route_kernel<T, V><<<static_cast<unsigned>(blocks < most ? blocks : most), kRouteWarps * 32, smem, st>>>(static_cast<const T*>(a.logits), p, a.ids,
+                                                                                                           a.weights);
   note_launch();
   return launch_status();
 }
@@ -275,9 +403,6 @@ hif4_status launch_route_backward(const hif4_route_backward_args& a, cudaStream_
   (a.dt == HIF4_BF16 ? HIF4_ROUTE_BY_WIDTH(launch, __nv_bfloat16, a, st) : a.dt == HIF4_FP16 ? HIF4_ROUTE_BY_WIDTH(launch, __half, a, st) \
                                                                                : HIF4_ROUTE_BY_WIDTH(launch, float, a, st))
 
-bool type_ok(int dt) { return dt == HIF4_BF16 || dt == HIF4_FP16 || dt == HIF4_FP32; }
-size_t type_size(int dt) { return dt == HIF4_FP32 ? 4 : 2; }
-bool aligned(const void* p, size_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
 
 // What both directions ask of their sizes and types.
 hif4_status check_router(int64_t tokens, int64_t experts, int64_t top_k, int64_t ld, int dt, int score) {
