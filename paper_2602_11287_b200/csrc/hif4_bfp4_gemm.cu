@@ -8,19 +8,13 @@
 // warps read the rows' words, which are just the four K = 64 steps of a row, and store them to their lane quarter.
 // Few tiles: the K chunks of a tile are dealt to the CTAs of a cluster, whose FP32 sums are added through distributed
 // shared memory in rank order (no atomics, no workspace).
-#include <cuda_bf16.h>
-#include <cuda_fp16.h>
-
-#include "hif4_bfp4_device.cuh"
-#include "hif4_tc2_common.cuh"
+#include "hif4_bfp4_gemm.cuh"
 
 namespace hif4 {
 namespace {
 
 constexpr int kThreads = 256;               // warps: producer, MMA, tile lookup and TMEM, idle, 4 x scales and epilogue
 constexpr int BW = 128;                     // rows of B a tile
-constexpr int kChunk = 256;                 // elements of K a stage
-constexpr int kRowBytes = kChunk / 2;
 constexpr int kTmemCols = 256;
 
 template <int T> struct Shape {
@@ -35,80 +29,10 @@ template <int T> struct Shape {
   static_assert(T * BW * 4 <= kStages * kCodeBytes, "sums of a cluster");
 };
 
-struct Bfp4Params {
-  int64_t M, N;
-  int chunks, last_steps;                   // K chunks; K = 64 steps of the last one
-  int n_tiles;
-  const uint8_t *a_scales, *b_scales;
-  int64_t b_scale_group;                    // bytes of a group's scales of B
-  const float* alpha;
-  void* y;
-  int64_t ld_y;
-  int dt;
-  int num_groups;                           // 0: dense
-  const int64_t* offsets;
-  unsigned int* error_word;
-};
-
-__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
-  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar)
-               : "memory");
-}
-// kNv: four scales a K = 64 step (E4M3); else two (E8M0), of which the instruction descriptor names the half word.
-template <bool kNv>
-__device__ __forceinline__ void mma_scaled(uint32_t d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t sfa, uint32_t sfb, uint32_t accumulate) {
-  if (kNv)
-    asm volatile(
-        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %6, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::mxf4nvf4.block_scale.scale_vec::4X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
-        ::"r"(d), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate) : "memory");
-  else
-    asm volatile(
-        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %6, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
-        ::"r"(d), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate) : "memory");
-}
-// E2M1 operands, scale type, sizes; the scales' half word is added where it is used (bits 4 and 29).
-template <bool kNv, int kM, int kN>
-__host__ __device__ constexpr uint32_t instr_desc() {
-  return (1u << 7) | (1u << 10) | (static_cast<uint32_t>(kN >> 3) << 17) | (kNv ? 0u : 1u << 23) | (static_cast<uint32_t>(kM >> 4) << 24);
-}
-__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
-  asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
-      ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
-      "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
-      : "memory");
-}
-__device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ float ld_cluster_f32(uint32_t addr) {
   float v;
   asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
   return v;
-}
-
-// Scale words of up to 128 rows (`groups` runs of 32) -> sixteen columns: column 4 k + c holds step k of rows 32 c .. 32 c + 31.
-template <bool kNv, int kGroups>
-__device__ __forceinline__ void move_scales(uint32_t smem, uint32_t taddr, int lane, int half) {
-  uint32_t w[16];
-#pragma unroll
-  for (int c = 0; c < 4; ++c) {
-    uint4 v = make_uint4(0u, 0u, 0u, 0u);
-    if (c < kGroups) v = lds128(smem + (c * 32 + lane) * 16);
-    if (kNv) {
-      w[c] = v.x; w[4 + c] = v.y; w[8 + c] = v.z; w[12 + c] = v.w;
-    } else {
-      w[c] = half ? v.z : v.x; w[4 + c] = half ? v.w : v.y; w[8 + c] = 0u; w[12 + c] = 0u;
-    }
-  }
-  tmem_st16(taddr, w);
-}
-
-__device__ __forceinline__ void store_y(const Bfp4Params& p, int64_t m, int64_t n, float v) {
-  const int64_t at = m * p.ld_y + n;
-  if (p.dt == HIF4_FP32) static_cast<float*>(p.y)[at] = v;
-  else if (p.dt == HIF4_BF16) static_cast<__nv_bfloat16*>(p.y)[at] = __float2bfloat16_rn(v);
-  else static_cast<__half*>(p.y)[at] = __float2half_rn(v);
 }
 
 template <int T, bool kNv>
@@ -228,7 +152,7 @@ bfp4_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant_
         for (int j = 0; j < steps; ++j) {
           const uint32_t at = kNv ? 4 * j : 4 * (j >> 1);
           const uint32_t desc = kDesc | (kNv ? 0u : (static_cast<uint32_t>(j & 1) * 2u) * ((1u << 4) | (1u << 29)));
-          mma_scaled<kNv>(tmem, bd + 2 * j, ad + 2 * j, desc, sfb + at, sfa + at, (i | j) != 0);
+          mma_scaled<kNv, 1>(tmem, bd + 2 * j, ad + 2 * j, desc, sfb + at, sfa + at, (i | j) != 0);
         }
         tc_commit(empty + 8 * s);
       }
@@ -303,18 +227,6 @@ bfp4_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant_
 }
 
 // ------------------------------------------------------------------------------------ host side
-// Codes of a matrix: [rows, K / 2] bytes, box = 128 bytes x box_rows; what lies outside reads as zeros.
-bool make_code_map(CUtensorMap* map, const void* base, int64_t rows, int64_t K, int box_rows) {
-  EncodeTiledFn fn = encode_tiled_fn();
-  if (!fn) return false;
-  const cuuint64_t dims[2] = {static_cast<cuuint64_t>(K / 2), static_cast<cuuint64_t>(rows)};
-  const cuuint64_t strides[1] = {static_cast<cuuint64_t>(K / 2)};
-  const cuuint32_t box[2] = {kRowBytes, static_cast<cuuint32_t>(box_rows)};
-  const cuuint32_t estr[2] = {1, 1};
-  return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
 template <int T, bool kNv>
 hif4_status launch_tiles(const hif4_bfp4_gemm_args& a, Bfp4Params p, int64_t m_tiles, cudaStream_t st) {
   const auto kernel = bfp4_gemm_kernel<T, kNv>;
@@ -374,6 +286,9 @@ hif4_status product(const hif4_bfp4_gemm_args& a, bool grouped, void* stream) {
   p.offsets = a.group_offsets;
   p.error_word = device_error_word();
   if (!p.error_word) return HIF4_ERR_CUDA;
+  p.wide = ((reinterpret_cast<uintptr_t>(a.Y) | static_cast<uintptr_t>(a.ld_y * size)) & 31u) == 0;
+  // Prompts: 256 x 256 tiles on CTA pairs as soon as there are enough of them
+  if (!grouped && a.M > 128 && ceil_div64(a.M, 256) * ceil_div64(a.N, 256) * 4 >= sm_count()) return launch_bfp4_pairs(a, p, st);
   // tokens of a tile: the fewest that hold the rows of a (mean) group, at most 128
   const int64_t mean = grouped ? ceil_div64(a.M, a.num_groups) : a.M;
   const int T = mean <= 16 ? 16 : mean <= 32 ? 32 : mean <= 64 ? 64 : 128;

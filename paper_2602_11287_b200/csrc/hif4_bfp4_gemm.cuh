@@ -1,0 +1,104 @@
+// What the block-scaled products share: parameters, the MMA and its descriptor, the scales' way into tensor memory, the tensor map of
+// packed codes.
+//
+// The MMA wants a scale word of row r in TMEM lane r % 32 (the same in all four lane quarters) and column r / 32, for
+// each K = 64.  A row's scales of a K = 256 chunk are one 16-byte word in memory, which is just its four words; a warp of each
+// lane quarter reads the rows' words and stores them.
+#pragma once
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "hif4_bfp4_device.cuh"
+#include "hif4_tc2_common.cuh"
+
+namespace hif4 {
+
+struct Bfp4Params {
+  int64_t M, N;
+  int chunks, last_steps;                   // K chunks of 256; K = 64 steps of the last one
+  int n_tiles, m_tiles;
+  const uint8_t *a_scales, *b_scales;
+  int64_t b_scale_group;                    // bytes of a group's scales of B
+  const float* alpha;
+  void* y;
+  int64_t ld_y;
+  int dt, wide;                             // wide: 32-byte stores of Y's rows
+  int num_groups;                           // 0: dense
+  const int64_t* offsets;
+  unsigned int* error_word;
+};
+// The CTA-pair kernel (dense, 256 x 256 tiles).
+hif4_status launch_bfp4_pairs(const hif4_bfp4_gemm_args& a, Bfp4Params p, cudaStream_t st);
+
+namespace {
+
+constexpr int kChunk = 256;                 // elements of K a stage
+constexpr int kRowBytes = kChunk / 2;
+
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar)
+               : "memory");
+}
+// kNv: four scales a K = 64 step (E4M3); else two (E8M0), of which the instruction descriptor names the half word.
+template <bool kNv, int kCtas>
+__device__ __forceinline__ void mma_scaled(uint32_t d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t sfa, uint32_t sfb, uint32_t accumulate) {
+#define HIF4_MMA_SCALED(form)                                                                         \
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %6, 0;\n\ttcgen05.mma." form " [%0], %1, %2, %3, [%4], [%5], p;\n\t}" \
+               ::"r"(d), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate) : "memory")
+  if (kNv && kCtas == 1) HIF4_MMA_SCALED("cta_group::1.kind::mxf4nvf4.block_scale.scale_vec::4X");
+  else if (kNv) HIF4_MMA_SCALED("cta_group::2.kind::mxf4nvf4.block_scale.scale_vec::4X");
+  else if (kCtas == 1) HIF4_MMA_SCALED("cta_group::1.kind::mxf4.block_scale.scale_vec::2X");
+  else HIF4_MMA_SCALED("cta_group::2.kind::mxf4.block_scale.scale_vec::2X");
+#undef HIF4_MMA_SCALED
+}
+// E2M1 operands, scale type, sizes; the scales' half word is added where it is used (bits 4 and 29).
+template <bool kNv, int kM, int kN>
+__host__ __device__ constexpr uint32_t instr_desc() {
+  return (1u << 7) | (1u << 10) | (static_cast<uint32_t>(kN >> 3) << 17) | (kNv ? 0u : 1u << 23) | (static_cast<uint32_t>(kM >> 4) << 24);
+}
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
+      ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
+      "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+      : "memory");
+}
+__device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+// Scale words of up to 128 rows (`groups` runs of 32) -> sixteen columns: column 4 k + c holds step k of rows 32 c .. 32 c + 31.
+template <bool kNv, int kGroups>
+__device__ __forceinline__ void move_scales(uint32_t smem, uint32_t taddr, int lane, int half) {
+  uint32_t w[16];
+#pragma unroll
+  for (int c = 0; c < 4; ++c) {
+    uint4 v = make_uint4(0u, 0u, 0u, 0u);
+    if (c < kGroups) v = lds128(smem + (c * 32 + lane) * 16);
+    if (kNv) {
+      w[c] = v.x; w[4 + c] = v.y; w[8 + c] = v.z; w[12 + c] = v.w;
+    } else {
+      w[c] = half ? v.z : v.x; w[4 + c] = half ? v.w : v.y; w[8 + c] = 0u; w[12 + c] = 0u;
+    }
+  }
+  tmem_st16(taddr, w);
+}
+
+__device__ __forceinline__ void store_y(const Bfp4Params& p, int64_t m, int64_t n, float v) {
+  const int64_t at = m * p.ld_y + n;
+  if (p.dt == HIF4_FP32) static_cast<float*>(p.y)[at] = v;
+  else if (p.dt == HIF4_BF16) static_cast<__nv_bfloat16*>(p.y)[at] = __float2bfloat16_rn(v);
+  else static_cast<__half*>(p.y)[at] = __float2half_rn(v);
+}
+
+// Codes of a matrix: [rows, K / 2] bytes, box = 128 bytes x box_rows; what lies outside reads as zeros.
+bool make_code_map(CUtensorMap* map, const void* base, int64_t rows, int64_t K, int box_rows) {
+  EncodeTiledFn fn = encode_tiled_fn();
+  if (!fn) return false;
+  const cuuint64_t dims[2] = {static_cast<cuuint64_t>(K / 2), static_cast<cuuint64_t>(rows)};
+  const cuuint64_t strides[1] = {static_cast<cuuint64_t>(K / 2)};
+  const cuuint32_t box[2] = {kRowBytes, static_cast<cuuint32_t>(box_rows)};
+  const cuuint32_t estr[2] = {1, 1};
+  return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+}  // namespace
+}  // namespace hif4

@@ -74,14 +74,64 @@ __device__ __forceinline__ float fast_rcp(float v) {
   return r;
 }
 
-// The choice of one token.  x: the lane's logits (-inf past the last expert), b: its biases, top: the largest logit that is a
-// number.  Lane j gets the j-th expert's index (or -1) and logit.  Returns whether neighbours were too near to tell apart.
+// A lane's logits (-inf past the last expert) and biases (-inf for a NaN).
+template <typename T, int V>
+__device__ __forceinline__ void load_logits(const T* row, const RouteParams& p, int lane, float (&x)[V]) {
+  row += lane * V;
+  if (p.vec && (lane + 1) * V <= p.experts) {            // 16-byte loads
+    constexpr int kWords = static_cast<int>(V * sizeof(T) / 4);
+    if constexpr (kWords >= 4 && kWords % 4 == 0) {
+      uint32_t w[kWords];
+#pragma unroll
+      for (int i = 0; i < kWords; i += 4) {
+        const uint4 q = __ldg(reinterpret_cast<const uint4*>(row) + i / 4);
+        w[i] = q.x; w[i + 1] = q.y; w[i + 2] = q.z; w[i + 3] = q.w;
+      }
+#pragma unroll
+      for (int i = 0; i < V; ++i) x[i] = to_f32(reinterpret_cast<const T*>(w)[i]);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < V; ++i) x[i] = lane * V + i < p.experts ? to_f32(row[i]) : -__int_as_float(0x7F800000);
+  }
+}
+template <int V>
+__device__ __forceinline__ void load_bias(const RouteParams& p, int lane, float (&b)[V]) {
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    const float v = p.bias && lane * V + i < p.experts ? p.bias[lane * V + i] : 0.0f;
+    b[i] = v == v ? v : -__int_as_float(0x7F800000);
+  }
+}
+template <int V>
+__device__ __forceinline__ float largest(const float (&x)[V]) {
+  float top = -__int_as_float(0x7F800000);
+#pragma unroll
+  for (int i = 0; i < V; ++i) top = fmaxf(top, x[i]);
+  return Keys<false>::value(Keys<false>::warp_max(Keys<false>::of(top)));
+}
+
+// The two largest keys of a lane that `used` (a bit per expert) does not hold, and where they are.
+template <typename Key, int V>
+__device__ __forceinline__ void best_two(const Key (&c)[V], uint32_t used, Key none, Key& first, int& at, Key& second, int& at2) {
+  first = second = none;
+  at = at2 = 0;
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    const Key v = (used >> i) & 1u ? none : c[i];
+    if (v > first) { second = first; at2 = at; first = v; at = i; }
+    else if (v > second) { second = v; at2 = i; }
+  }
+}
+
+// The choice of one token from the lane's logits x and biases b; top is the largest logit that is a number.  Lane j gets the j-th
+// expert (or -1).  Sets `contested` where neighbours were too near to tell apart.
 //
 // Errors in FP32: a sigmoid 1 / (1 + e) with e = exp2(-x log2 e): 2^-22.5 from exp2 and |x| 2^-24 from its argument reach the
 // result through e / (1 + e)^2 <= 1/4 (and |x| e / (1 + e)^2 < 0.23), 1 + e and the reciprocal add 2^-24 + 2^-23: together below
 // 2^-22; two of them 2^-21, taken as 2^-20.  A softmax the same, relative to the largest.  The bias's addition 2^-24 of the sum.
 template <bool kWide, int V>
-__device__ __forceinline__ bool choose(const float (&x)[V], const float (&b)[V], float top, const RouteParams& p, long long* scratch, int lane, int& id, float& xc) {
+__device__ __forceinline__ int choose(const float (&x)[V], const float (&b)[V], float top, const RouteParams& p, long long* scratch, int lane, bool& contested) {
   using K = Keys<kWide>;
   using Real = typename K::Real;
   using Key = typename K::Key;
@@ -91,7 +141,7 @@ __device__ __forceinline__ bool choose(const float (&x)[V], const float (&b)[V],
   Real near = 0;                                        // how near two choices may be and still be told apart
   if (p.by_logit) {
 #pragma unroll
-    for (int i = 0; i < V; ++i) c[i] = x[i] != x[i] ? none : K::of(static_cast<Real>(x[i]));
+    for (int i = 0; i < V; ++i) c[i] = x[i] > -kInf ? K::of(static_cast<Real>(x[i])) : none;
   } else {
     Real v[V];
     if (p.sigmoid) {
@@ -104,7 +154,7 @@ __device__ __forceinline__ bool choose(const float (&x)[V], const float (&b)[V],
 #pragma unroll
       for (int i = 0; i < V; ++i) {
         v[i] = x[i] == top ? Real(1) : kWide ? static_cast<Real>(exp(static_cast<double>(x[i]) - static_cast<double>(top))) : static_cast<Real>(__expf(x[i] - top));
-        if (x[i] != x[i] || top == -kInf) v[i] = 0;
+        if (!(x[i] > -kInf)) v[i] = 0;
         total += v[i];
       }
       total = warp_sum(total);
@@ -114,37 +164,33 @@ __device__ __forceinline__ bool choose(const float (&x)[V], const float (&b)[V],
       near = static_cast<Real>(0x1p-19) * inv;
     }
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-      v[i] += static_cast<Real>(b[i]);
-      c[i] = x[i] == -kInf || x[i] != x[i] || v[i] != v[i] ? none : K::of(v[i]);
-    }
+    for (int i = 0; i < V; ++i) c[i] = x[i] > -kInf ? K::of(v[i] + static_cast<Real>(b[i])) : none;
   }
   const auto told_apart = [&](Key high, Key low, Real margin) {      // (a key of none is far from all others)
     if (p.by_logit || kWide || low == none) return true;
-    const Real h = K::value(high);
-    return h - K::value(low) > margin + static_cast<Real>(0x1p-21) * fmaxf(fabsf(h), fabsf(K::value(low)));
+    const Real h = K::value(high), l = K::value(low);
+    return h - l > margin + static_cast<Real>(0x1p-21) * fmaxf(fabsf(h), fabsf(l));
   };
-  bool contested = false;
+  const auto sum_of = [&](Key first, Key second) {
+    return p.group_best == 1 ? first : first == none || second == none ? none : K::of(K::value(first) + K::value(second));
+  };
+  contested = false;
 
-  if (p.top_groups < p.groups) {
-    const int span = p.per / V;                         // lanes of a group, where groups are whole lanes
-    const bool whole = p.per % V == 0 && (span & (span - 1)) == 0;
+  const int span = p.per / V;                           // lanes of a group, where groups are whole lanes
+  const bool grouped = p.top_groups < p.groups, whole = p.per % V == 0 && (span & (span - 1)) == 0;
+  Key first, second;
+  int at, at2;
+  if (!grouped || whole) best_two(c, 0u, none, first, at, second, at2);
+  if (grouped) {
     Key value = none;
     if (whole) {
-      Key first = none, second = none;
-#pragma unroll
-      for (int i = 0; i < V; ++i) {
-        second = max(second, min(first, c[i]));
-        first = max(first, c[i]);
-      }
+      Key f = first, s = second;
       for (int o = 1; o < span; o <<= 1) {
-        const Key f = __shfl_xor_sync(kAll, first, o), s = __shfl_xor_sync(kAll, second, o);
-        second = max(min(first, f), max(second, s));
-        first = max(first, f);
+        const Key f2 = __shfl_xor_sync(kAll, f, o), s2 = __shfl_xor_sync(kAll, s, o);
+        s = max(min(f, f2), max(s, s2));
+        f = max(f, f2);
       }
-      value = first;
-      if (p.group_best == 2) value = first == none || second == none ? none : K::of(K::value(first) + K::value(second));
-      if (lane >= p.groups * span) value = none;
+      value = sum_of(f, s);
     } else {
       Key* mine = reinterpret_cast<Key*>(scratch);
 #pragma unroll
@@ -152,21 +198,21 @@ __device__ __forceinline__ bool choose(const float (&x)[V], const float (&b)[V],
         if (lane * V + i < p.experts) mine[lane * V + i] = c[i];
       __syncwarp();
       if (lane < p.groups) {
-        Key first = none, second = none;
+        Key f = none, s = none;
         for (int e = 0; e < p.per; ++e) {
           const Key v = mine[lane * p.per + e];
-          second = max(second, min(first, v));
-          first = max(first, v);
+          s = max(s, min(f, v));
+          f = max(f, v);
         }
-        value = first;
-        if (p.group_best == 2) value = first == none || second == none ? none : K::of(K::value(first) + K::value(second));
+        value = sum_of(f, s);
       }
       __syncwarp();
     }
+    const int own = whole ? lane / span : lane;         // this lane's group
+    bool free = own < p.groups;
+    if (!free) value = none;
     uint32_t open = 0u;
     Key last = none;
-    bool free = whole ? lane < p.groups * span : lane < p.groups;
-    const int own = whole ? lane / span : lane;
     for (int n = 0; n < p.top_groups; ++n) {
       last = K::warp_max(free ? value : none);
       const int g = __shfl_sync(kAll, own, __ffs(__ballot_sync(kAll, free && value == last)) - 1);
@@ -174,92 +220,82 @@ __device__ __forceinline__ bool choose(const float (&x)[V], const float (&b)[V],
       if (own == g) free = false;
     }
     contested = !told_apart(last, K::warp_max(free ? value : none), 2 * near);
-    int g = lane * V / p.per, left = p.per - (lane * V - g * p.per);
+    if (whole) {
+      if (own >= p.groups || !((open >> own) & 1u)) first = second = none;
+    } else {
+      int g = lane * V / p.per, left = p.per - (lane * V - g * p.per);
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-      if (!((open >> (g & 31)) & 1u)) c[i] = none;
-      if (--left == 0) { ++g; left = p.per; }
+      for (int i = 0; i < V; ++i) {
+        if (!((open >> (g & 31)) & 1u)) c[i] = none;
+        if (--left == 0) { ++g; left = p.per; }
+      }
+      best_two(c, 0u, none, first, at, second, at2);
     }
   }
 
-  id = -1;
-  xc = -kInf;
-  Key before = none;
-  int at = 0;
-  Key best = c[0];
-#pragma unroll
-  for (int i = 1; i < V; ++i)
-    if (c[i] > best) { best = c[i]; at = i; }
-  for (int j = 0; j <= p.top_k; ++j) {                  // the last round only looks at who would be next
-    const Key most = K::warp_max(best);
-    if (j > 0) contested |= !told_apart(before, most, near);
+  int id = -1;
+  Key mine = none, most = none;                         // lane j: the j-th choice
+  uint32_t used = 0u;
+  bool known = true;                                    // whether `second` is the best that is left besides `first`
+  for (int j = 0;; ++j) {                               // the last round only looks at who would be next
+    most = K::warp_max(first);
     if (most == none || j == p.top_k) break;
-    before = most;
-    const int from = __ffs(__ballot_sync(kAll, best == most)) - 1;
-    float mine = 0.0f;
-#pragma unroll
-    for (int i = 0; i < V; ++i)
-      if (i == at) mine = x[i];
+    const int from = __ffs(__ballot_sync(kAll, first == most)) - 1;
     const int e = __shfl_sync(kAll, lane * V + at, from);
-    mine = __shfl_sync(kAll, mine, from);
-    if (lane == j) { id = e; xc = mine; }
+    if (lane == j) { id = e; mine = most; }
     if (lane == from) {
-#pragma unroll
-      for (int i = 0; i < V; ++i)
-        if (i == at) c[i] = none;
-      best = c[0];
-      at = 0;
-#pragma unroll
-      for (int i = 1; i < V; ++i)
-        if (c[i] > best) { best = c[i]; at = i; }
+      used |= 1u << at;
+      if (known) {
+        first = second;
+        at = at2;
+        known = false;
+      } else {
+        best_two(c, used, none, first, at, second, at2);
+        known = true;
+      }
     }
   }
-  return contested;
+  Key next = __shfl_down_sync(kAll, mine, 1);
+  if (lane == p.top_k - 1) next = most;
+  contested |= __any_sync(kAll, lane < p.top_k && mine != none && !told_apart(mine, next, near));
+  return id;
+}
+
+// The choice in 64 bits.  A call of its own: it is rare, and its registers are not the common path's.
+template <typename T, int V>
+__device__ __noinline__ int choose_wide(const T* row, const RouteParams* p, long long* scratch) {
+  const int lane = threadIdx.x & 31;
+  float x[V], b[V];
+  load_logits(row, *p, lane, x);
+  load_bias(*p, lane, b);
+  bool contested;
+  return choose<true, V>(x, b, largest(x), *p, scratch, lane, contested);
 }
 
 // V: experts a lane holds (experts <= 32 V).
 template <typename T, int V>
 __global__ void __launch_bounds__(kRouteWarps * 32)
-route_kernel(const T* __restrict__ logits, const RouteParams p, int32_t* __restrict__ ids, float* __restrict__ weights) {
+route_kernel(const T* __restrict__ logits, const __grid_constant__ RouteParams p, int32_t* __restrict__ ids, float* __restrict__ weights) {
   extern __shared__ long long scratch[];                // [warps][experts], where groups are not whole lanes
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const float kInf = __int_as_float(0x7F800000);
   float b[V];
-#pragma unroll
-  for (int i = 0; i < V; ++i) b[i] = p.bias && lane * V + i < p.experts ? p.bias[lane * V + i] : 0.0f;
+  load_bias(p, lane, b);
   for (int64_t t = static_cast<int64_t>(blockIdx.x) * kRouteWarps + warp; t < p.tokens; t += static_cast<int64_t>(gridDim.x) * kRouteWarps) {
-    const T* row = logits + t * p.ld + lane * V;
+    const T* row = logits + t * p.ld;
     float x[V];
-    if (p.vec && (lane + 1) * V <= p.experts) {          // 16-byte loads
-      constexpr int kWords = static_cast<int>(V * sizeof(T) / 4);
-      if constexpr (kWords >= 4 && kWords % 4 == 0) {
-        uint32_t w[kWords];
-#pragma unroll
-        for (int i = 0; i < kWords; i += 4) {
-          const uint4 q = __ldg(reinterpret_cast<const uint4*>(row) + i / 4);
-          w[i] = q.x; w[i + 1] = q.y; w[i + 2] = q.z; w[i + 3] = q.w;
-        }
-#pragma unroll
-        for (int i = 0; i < V; ++i) x[i] = to_f32(reinterpret_cast<const T*>(w)[i]);
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < V; ++i) x[i] = lane * V + i < p.experts ? to_f32(row[i]) : -kInf;
-    }
-    float top = -kInf;
+    load_logits(row, p, lane, x);
+    const float top = largest(x);
     bool bad = false;
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-      bad |= x[i] != x[i];
-      top = fmaxf(top, x[i]);
-    }
-    top = Keys<false>::value(Keys<false>::warp_max(Keys<false>::of(top)));
+    for (int i = 0; i < V; ++i) bad |= x[i] != x[i];
     bad = __any_sync(kAll, bad) || (!p.sigmoid && top == kInf);
 
-    int id;                                             // lane j: the j-th choice and its logit
-    float xc;
     long long* mine = scratch + static_cast<size_t>(warp) * p.experts;
-    if (choose<false, V>(x, b, top, p, mine, lane, id, xc)) choose<true, V>(x, b, top, p, mine, lane, id, xc);
+    bool contested;
+    int id = choose<false, V>(x, b, top, p, mine, lane, contested);      // lane j: the j-th choice
+    if (contested) id = choose_wide<T, V>(row, &p, mine);
+    const float xc = id >= 0 ? to_f32(row[id]) : -kInf;
 
     float w = 0.0f;
     const float high = Keys<false>::value(Keys<false>::warp_max(Keys<false>::of(xc)));       // of the chosen

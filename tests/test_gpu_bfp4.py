@@ -112,6 +112,8 @@ def check_product(y, a, b, scale=1.0):
     """FP32 sums in any order: the bound of the HiF4 product; then one rounding to the type of Y."""
     want, most = scale * (a @ b.t()), abs(scale) * 1e-5 * (a.abs() @ b.abs().t())
     most = most + torch.finfo(y.dtype).eps / 2 * want.abs() * (0 if y.dtype == torch.float32 else 1) + 2.0 ** -24 * want.abs()
+    if y.dtype == torch.float16:          # below 2^-14 FP16's step is 2^-24 whatever the value: half of it is 2^-25
+        most = most + 2.0 ** -25
     assert bool(((y.double() - want).abs() <= most).all()), float(((y.double() - want).abs() / most.clamp(min=1e-300)).max())
 
 
@@ -133,7 +135,14 @@ def test_product(hif4, fmt, M, N, K):
 
 
 @pytest.mark.parametrize("fmt", [MX, NV])
-@pytest.mark.parametrize("M", [1, 40, 200])
+@pytest.mark.parametrize("M,N,K", [(1500, 1777, 320), (2049, 2304, 1088), (257, 9600, 576), (8200, 512, 64), (1300, 2050, 2304), (2560, 2560, 512)])
+def test_product_of_prompts(hif4, fmt, M, N, K):
+    """The sizes of the CTA-pair kernel."""
+    test_product(hif4, fmt, M, N, K)
+
+
+@pytest.mark.parametrize("fmt", [MX, NV])
+@pytest.mark.parametrize("M", [1, 40, 200, 10000])
 def test_every_code_and_scale(hif4, fmt, M):
     """One row of A picks one element of each row of B: products are exact."""
     K = 512
@@ -166,7 +175,7 @@ def test_nan_blocks_and_row_padding(hif4, fmt):
     assert torch.equal(got.isnan(), nan) and torch.equal(got[~nan], clean[~nan])
 
 
-@pytest.mark.parametrize("M", [5, 100, 300])
+@pytest.mark.parametrize("M", [5, 100, 300, 10000])
 def test_product_into_a_view(hif4, M):
     g = gen(2)
     a, b = ref.random_operand(M, 1024, NV, g), ref.random_operand(203, 1024, NV, g)
@@ -229,7 +238,7 @@ def test_gradients_of_a_linear_layer(hif4):
 
 def test_same_bits_every_time_and_in_a_graph(hif4):
     g = gen(8)
-    for M in (1, 30, 100, 700):
+    for M in (1, 30, 100, 700, 3500):
         a, b = ref.random_operand(M, 4096, NV, g), ref.random_operand(520, 4096, NV, g)
         y = hif4.hif4_bfp4_gemm(a, b, NV, dtype=torch.float32)
         out = torch.empty_like(y)
