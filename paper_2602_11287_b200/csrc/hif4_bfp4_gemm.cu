@@ -138,26 +138,26 @@ bfp4_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant_
       }
     }
   } else if (warp == 1) {
-    if (lane == 0) {
-      constexpr uint32_t kDesc = instr_desc<kNv, BW, T>();
-      bool ok = true;
-      for (int k = k_first, i = 0; k < k_last; ++k, ++i) {
-        const int s = i % kStages;
-        const uint32_t ph = (i / kStages) & 1;
-        if (!(ok = mbar_wait(full + 8 * s, ph, abort_flag) && mbar_wait(ready + 8 * s, ph, abort_flag))) break;
-        tc_fence_after();
-        const uint64_t bd = make_desc(codes + s * S::kCodeBytes), ad = make_desc(codes + s * S::kCodeBytes + BW * kRowBytes);
-        const uint32_t sfb = sf_cols + s * 32, sfa = sfb + 16;
-        const int steps = k == p.chunks - 1 ? p.last_steps : 4;
-        for (int j = 0; j < steps; ++j) {
-          const uint32_t at = kNv ? 4 * j : 4 * (j >> 1);
-          const uint32_t desc = kDesc | (kNv ? 0u : (static_cast<uint32_t>(j & 1) * 2u) * ((1u << 4) | (1u << 29)));
-          mma_scaled<kNv, 1>(tmem, bd + 2 * j, ad + 2 * j, desc, sfb + at, sfa + at, (i | j) != 0);
-        }
+    constexpr uint32_t kDesc = instr_desc<kNv, BW, T>();
+    const uint64_t bd0 = make_desc(codes), ad0 = make_desc(codes + BW * kRowBytes);
+    const bool issuer = elect_one();
+    bool ok = true;
+    int s = 0;
+    uint32_t ph = 0u;
+    for (int k = k_first; k < k_last; ++k) {
+      if (!(ok = __all_sync(0xFFFFFFFFu, mbar_wait(full + 8 * s, ph, abort_flag) && mbar_wait(ready + 8 * s, ph, abort_flag)))) break;
+      tc_fence_after();
+      const uint64_t off = static_cast<uint64_t>(s * (S::kCodeBytes >> 4));
+      const uint32_t sfb = sf_cols + s * 32;
+      if (issuer) {
+        mma_stage<kNv, 1, 4, 4>(tmem, bd0 + off, ad0 + off, kDesc, sfb, sfb + 16, k == p.chunks - 1 ? p.last_steps : 4, k == k_first);
         tc_commit(empty + 8 * s);
       }
-      if (ok && k_last > k_first) tc_commit(done);
+      __syncwarp();
+      if (++s == kStages) { s = 0; ph ^= 1u; }
     }
+    if (ok && issuer && k_last > k_first) tc_commit(done);
+    __syncwarp();
   } else if (warp >= 4) {
     const int q = warp & 3;
     bool ok = true;
@@ -286,7 +286,6 @@ hif4_status product(const hif4_bfp4_gemm_args& a, bool grouped, void* stream) {
   p.offsets = a.group_offsets;
   p.error_word = device_error_word();
   if (!p.error_word) return HIF4_ERR_CUDA;
-  p.wide = ((reinterpret_cast<uintptr_t>(a.Y) | static_cast<uintptr_t>(a.ld_y * size)) & 31u) == 0;
   // Prompts: 256 x 256 tiles on CTA pairs as soon as there are enough of them
   if (!grouped && a.M > 128 && ceil_div64(a.M, 256) * ceil_div64(a.N, 256) * 4 >= sm_count()) return launch_bfp4_pairs(a, p, st);
   // tokens of a tile: the fewest that hold the rows of a (mean) group, at most 128

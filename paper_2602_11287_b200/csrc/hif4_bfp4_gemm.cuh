@@ -22,7 +22,7 @@ struct Bfp4Params {
   const float* alpha;
   void* y;
   int64_t ld_y;
-  int dt, wide;                             // wide: 32-byte stores of Y's rows
+  int dt, tma_store;
   int num_groups;                           // 0: dense
   const int64_t* offsets;
   unsigned int* error_word;
@@ -50,6 +50,26 @@ __device__ __forceinline__ void mma_scaled(uint32_t d, uint64_t adesc, uint64_t 
   else if (kCtas == 1) HIF4_MMA_SCALED("cta_group::1.kind::mxf4.block_scale.scale_vec::2X");
   else HIF4_MMA_SCALED("cta_group::2.kind::mxf4.block_scale.scale_vec::2X");
 #undef HIF4_MMA_SCALED
+}
+// One lane of the warp (all lanes call).  The loops around MMAs are run by whole warps with only the MMAs under this condition: their
+// descriptors are then uniform values for the compiler, where a loop run by one lane moves every operand to uniform registers
+// before each MMA (143 clocks an MMA that takes 128).
+__device__ __forceinline__ bool elect_one() {
+  uint32_t one;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(one));
+  return one != 0u;
+}
+// The MMAs of one stage (`steps` of K = 64) and their descriptors' half words; kA, kB: columns of a step's scales.
+template <bool kNv, int kCtas, int kA, int kB>
+__device__ __forceinline__ void mma_stage(uint32_t d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t sfa, uint32_t sfb, int steps, bool first) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    if (j < steps) {
+      const int word = kNv ? j : j >> 1;
+      const uint32_t half = kNv ? 0u : (static_cast<uint32_t>(j & 1) * 2u) * ((1u << 4) | (1u << 29));
+      mma_scaled<kNv, kCtas>(d, adesc + 2 * j, bdesc + 2 * j, idesc | half, sfa + kA * word, sfb + kB * word, !first || j > 0);
+    }
+  }
 }
 // E2M1 operands, scale type, sizes; the scales' half word is added where it is used (bits 4 and 29).
 template <bool kNv, int kM, int kN>

@@ -2,43 +2,46 @@
 // (tcgen05.mma.cta_group::2), persistent over its tiles.  Each CTA holds its 128 tokens and 128 of the rows of B, so an SM reads
 // 8 KB from L2 for a K = 64 step of 128 x 256 outputs; it needs the scales of all 256 rows of B, though.
 //
-// Per CTA: a TMA warp (5 stages of K = 256: 32 KB codes, 6 KB scales), four warps that move the scales of a stage to tensor memory
-// (48 columns a stage beside the 256 accumulator columns) and say so to the leader's MMA thread, eight epilogue warps.  The
-// accumulator is single: 16-bit outputs are read into registers as pairs and the accumulator handed back before any of them is
-// stored, so that the next tile's first MMAs wait for tensor-memory reads only.
+// Codes and scales have rings of their own (5 stages of 32 KB, 5 of 6 KB), so that the scales' way to tensor memory does not add to
+// the codes' latency: four warps read a chunk's scales ahead of time, store them (48 columns beside the 256 accumulator columns)
+// as soon as the MMAs that used these columns are done, and tell the leader's MMA thread; one more thread tells it that a CTA's codes
+// are there.  With both in one ring a stage took 1400 clocks (217 -> 151 us only).
+// Eight epilogue warps.  The accumulator is single: 16-bit outputs are read into registers as pairs and the accumulator handed back
+// before any of them is stored, so that the next tile's first MMAs wait for tensor-memory reads only.
 #include "hif4_bfp4_gemm.cuh"
 
 namespace hif4 {
 namespace {
 
-constexpr int kThreads = 512;                // warps: TMA, MMA, TMEM allocation, idle, 4 x scales, 8 x epilogue
+constexpr int kThreads = 512;                // warps: codes, MMA, TMEM allocation and arrival of codes, scales, 4 x scales to TMEM, 8 x epilogue
 constexpr int kTile = 256, kHalf = 128;
-constexpr int kStages = 5;
+constexpr int kStages = 5, kSfStages = 5;
 constexpr int kCodeBytes = 2 * kHalf * kRowBytes;
 constexpr int kSfBytes = (kHalf + kTile) * 16;
-constexpr int kBars = kStages * (kCodeBytes + kSfBytes);
-constexpr int kSmem = 1024 + kBars + 256;
+constexpr int kSlabBytes = 32 * 128;         // 32 rows x 128 bytes of Y, one per epilogue warp, in SWIZZLE_128B order
+constexpr int kSlabs = kStages * kCodeBytes;
+constexpr int kSf = kSlabs + 8 * kSlabBytes;
+constexpr int kBars = kSf + kSfStages * kSfBytes;
+constexpr int kSmem = 1024 + kBars + 512;
 constexpr int kSfCols = 48;                  // of a stage: 16 for the tokens, 32 for B
 constexpr int kTmemCols = 512;
 constexpr int kBand = 16;                    // token tiles that are walked together (their codes stay in L2)
 static_assert(kTile + kStages * kSfCols <= kTmemCols, "TMEM");
 static_assert(kSmem <= 227 * 1024, "shared memory");
 
-// Scale words of 256 rows -> 32 columns: column 8 k + c holds step k of rows 32 c .. 32 c + 31.
-template <bool kNv>
-__device__ __forceinline__ void move_scales_256(uint32_t smem, uint32_t taddr, int lane, int half) {
-  uint32_t lo[16], hi[16];
+// Scale words of the lane's rows, as the columns want them: of 128 rows column 4 k + c holds step k of rows 32 c .. 32 c + 31, of 256
+// rows column 8 k + c.
+template <bool kNv, int kRuns>
+__device__ __forceinline__ void read_scales(uint32_t smem, int lane, int half, uint32_t (&w)[kRuns * 4]) {
 #pragma unroll
-  for (int c = 0; c < 8; ++c) {
+  for (int c = 0; c < kRuns; ++c) {
     const uint4 v = lds128(smem + (c * 32 + lane) * 16);
     if (kNv) {
-      lo[c] = v.x; lo[8 + c] = v.y; hi[c] = v.z; hi[8 + c] = v.w;
+      w[c] = v.x; w[kRuns + c] = v.y; w[2 * kRuns + c] = v.z; w[3 * kRuns + c] = v.w;
     } else {
-      lo[c] = half ? v.z : v.x; lo[8 + c] = half ? v.w : v.y;
+      w[c] = half ? v.z : v.x; w[kRuns + c] = half ? v.w : v.y; w[2 * kRuns + c] = w[3 * kRuns + c] = 0u;
     }
   }
-  tmem_st16(taddr, lo);
-  if (kNv) tmem_st16(taddr + 16, hi);
 }
 
 struct PairTile { int m0, n0; };
@@ -49,19 +52,42 @@ __device__ __forceinline__ PairTile pair_tile(const Bfp4Params& p, int t) {
   return {mt * kTile, nt * kTile};
 }
 
-__device__ __forceinline__ void store32(void* p, const uint32_t* w) {
-  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]),
-               "r"(w[6]), "r"(w[7]) : "memory");
+// Y is written once and larger than what the codes leave of L2: its lines are the first to go.
+__device__ __forceinline__ uint64_t evict_first_policy() {
+  uint64_t policy;
+  asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(policy));
+  return policy;
+}
+__device__ __forceinline__ void tma_store_hinted(const CUtensorMap* map, int x, int y, uint32_t src, uint64_t policy) {
+  asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group.L2::cache_hint [%0, {%1, %2}], [%3], %4;" ::"l"(map), "r"(x), "r"(y), "r"(src),
+               "l"(policy) : "memory");
+}
+// A warp's 32 words per lane (128 bytes of its lane's row) -> its slab -> Y.  The slab is free once the copy before has read it.
+__device__ __forceinline__ void store_slab(const CUtensorMap* map, int x, int y, uint32_t slab, const uint32_t* w, int lane, uint64_t policy) {
+  if (lane == 0) bulk_wait_read<0>();
+  __syncwarp();
+  const uint32_t row = slab + lane * 128u, r7 = static_cast<uint32_t>(lane) & 7u;
+#pragma unroll
+  for (uint32_t i = 0; i < 8; ++i) sts128(row + ((i ^ r7) << 4), w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+  fence_proxy_async_smem();
+  __syncwarp();
+  if (lane == 0) {
+    tma_store_hinted(map, x, y, slab, policy);
+    bulk_commit();
+  }
 }
 
 template <bool kNv>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
-bfp4_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const __grid_constant__ Bfp4Params p) {
+bfp4_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const __grid_constant__ CUtensorMap tmY,
+                 const __grid_constant__ Bfp4Params p) {
   extern __shared__ uint8_t smem_raw[];
   const uint32_t smem = (smem_u32(smem_raw) + 1023u) & ~1023u;
-  const uint32_t sf = smem + kStages * kCodeBytes, bars = smem + kBars;
-  const uint32_t full = bars, ready = bars + 8 * kStages, empty = bars + 16 * kStages, acc_full = bars + 24 * kStages, acc_empty = acc_full + 8,
-                 slot = acc_full + 16;
+  const uint32_t sf = smem + kSf, bars = smem + kBars;
+  // full: this CTA's codes; empty: codes and scale columns are free; sf_full, sf_empty: ring of scales; ready (on rank 0): codes and
+  // scale columns of both CTAs
+  const uint32_t full = bars, empty = full + 8 * kStages, ready = empty + 8 * kStages, sf_full = ready + 8 * kStages,
+                 sf_empty = sf_full + 8 * kSfStages, acc_full = sf_empty + 8 * kSfStages, acc_empty = acc_full + 8, slot = acc_full + 16;
   uint8_t* gen = smem_raw + (smem - smem_u32(smem_raw));
   volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(gen + (slot - smem));
   volatile uint32_t* abort_flag = tmem_slot + 1;
@@ -72,8 +98,12 @@ bfp4_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant_
   if (threadIdx.x == 0) {
     for (int s = 0; s < kStages; ++s) {
       mbar_init(full + 8 * s, 1);
-      mbar_init(ready + 8 * s, 8);                       // four warps of each CTA (used on rank 0)
       mbar_init(empty + 8 * s, 1);
+      mbar_init(ready + 8 * s, 10);                      // of each CTA: four warps for the scales, one thread for the codes
+    }
+    for (int s = 0; s < kSfStages; ++s) {
+      mbar_init(sf_full + 8 * s, 1);
+      mbar_init(sf_empty + 8 * s, 4);
     }
     mbar_init(acc_full, 1);
     mbar_init(acc_empty, 16);                            // eight warps of each CTA (used on rank 0)
@@ -98,85 +128,124 @@ bfp4_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant_
       for (int t = pair; t < tiles && ok; t += pairs) {
         const PairTile w = pair_tile(p, t);
         const int m0 = w.m0 + static_cast<int>(rank) * kHalf, n0 = w.n0 + static_cast<int>(rank) * kHalf;
+        for (int k = 0; k < p.chunks; ++k) {
+          if (!(ok = mbar_wait(empty + 8 * s, ph, abort_flag))) break;
+          const uint32_t bar = full + 8 * s, at = smem + s * kCodeBytes;
+          mbar_expect_tx(bar, kCodeBytes);
+          tma_load_2d(at, &tmA, k * kRowBytes, m0, bar);
+          tma_load_2d(at + kHalf * kRowBytes, &tmB, k * kRowBytes, n0, bar);
+          if (++s == kStages) { s = 0; ph ^= 1u; }
+        }
+      }
+    }
+  } else if (warp == 3) {
+    if (lane == 0) {
+      int z = 0;
+      uint32_t ph = 1u;
+      bool ok = true;
+      for (int t = pair; t < tiles && ok; t += pairs) {
+        const PairTile w = pair_tile(p, t);
+        const int m0 = w.m0 + static_cast<int>(rank) * kHalf;
         const uint32_t sf_a = static_cast<uint32_t>(max(static_cast<int64_t>(0), min(static_cast<int64_t>(kHalf), p.M - m0))) * 16u;
         const uint32_t sf_b = static_cast<uint32_t>(min(static_cast<int64_t>(kTile), p.N - w.n0)) * 16u;
         const uint8_t *a_sf = p.a_scales + static_cast<int64_t>(m0) * 16, *b_sf = p.b_scales + static_cast<int64_t>(w.n0) * 16;
         for (int k = 0; k < p.chunks; ++k) {
-          if (!(ok = mbar_wait(empty + 8 * s, ph, abort_flag))) break;
-          const uint32_t bar = full + 8 * s, at = smem + s * kCodeBytes, sfs = sf + s * kSfBytes;
-          mbar_expect_tx(bar, kCodeBytes + sf_a + sf_b);
-          tma_load_2d(at, &tmA, k * kRowBytes, m0, bar);
-          tma_load_2d(at + kHalf * kRowBytes, &tmB, k * kRowBytes, n0, bar);
+          if (!(ok = mbar_wait(sf_empty + 8 * z, ph, abort_flag))) break;
+          const uint32_t bar = sf_full + 8 * z, sfs = sf + z * kSfBytes;
+          mbar_expect_tx(bar, sf_a + sf_b);
           const int64_t word = kNv ? k : k >> 1;
           if (sf_a) bulk_load(sfs, a_sf + word * p.M * 16, sf_a, bar);
           bulk_load(sfs + kHalf * 16, b_sf + word * p.N * 16, sf_b, bar);
+          if (++z == kSfStages) { z = 0; ph ^= 1u; }
+        }
+      }
+    }
+  } else if (warp == 2) {
+    if (lane == 0) {
+      const uint32_t ready_leader = mapa(ready, 0);
+      int s = 0;
+      uint32_t ph = 0u;
+      bool ok = true;
+      for (int t = pair; t < tiles && ok; t += pairs) {
+        for (int k = 0; k < p.chunks; ++k) {
+          if (!(ok = mbar_wait(full + 8 * s, ph, abort_flag))) break;
+          mbar_arrive_cluster(ready_leader + 8 * s);
           if (++s == kStages) { s = 0; ph ^= 1u; }
         }
       }
     }
   } else if (warp == 1) {
-    if (rank == 0 && lane == 0) {
+    if (rank == 0) {
       constexpr uint32_t kDesc = instr_desc<kNv, kTile, kTile>();
+      const uint64_t ad0 = make_desc(smem), bd0 = make_desc(smem + kHalf * kRowBytes);
+      const bool issuer = elect_one();
       int s = 0;
       uint32_t ph = 0u, aph = 1u;
       bool ok = true;
       for (int t = pair; t < tiles && ok; t += pairs) {
-        if (!(ok = mbar_wait_cluster(acc_empty, aph, abort_flag))) break;
+        if (!(ok = __all_sync(0xFFFFFFFFu, mbar_wait_cluster(acc_empty, aph, abort_flag)))) break;
         aph ^= 1u;
         tc_fence_after();
         for (int k = 0; k < p.chunks; ++k) {
-          if (!(ok = mbar_wait_cluster(ready + 8 * s, ph, abort_flag))) break;
+          if (!(ok = __all_sync(0xFFFFFFFFu, mbar_wait_cluster(ready + 8 * s, ph, abort_flag)))) break;
           tc_fence_after();
-          const uint64_t ad = make_desc(smem + s * kCodeBytes), bd = make_desc(smem + s * kCodeBytes + kHalf * kRowBytes);
-          const uint32_t sfa = sf_cols + s * kSfCols, sfb = sfa + 16;
-          const int steps = k == p.chunks - 1 ? p.last_steps : 4;
-          for (int j = 0; j < steps; ++j) {
-            const uint32_t word = kNv ? j : j >> 1;
-            const uint32_t desc = kDesc | (kNv ? 0u : (static_cast<uint32_t>(j & 1) * 2u) * ((1u << 4) | (1u << 29)));
-            mma_scaled<kNv, 2>(tmem, ad + 2 * j, bd + 2 * j, desc, sfa + 4 * word, sfb + 8 * word, (k | j) != 0);
+          const uint64_t off = static_cast<uint64_t>(s * (kCodeBytes >> 4));
+          const uint32_t sfa = sf_cols + s * kSfCols;
+          if (issuer) {
+            mma_stage<kNv, 2, 4, 8>(tmem, ad0 + off, bd0 + off, kDesc, sfa, sfa + 16, k == p.chunks - 1 ? p.last_steps : 4, k == 0);
+            tc2_commit_both(empty + 8 * s);
           }
-          tc2_commit_both(empty + 8 * s);
+          __syncwarp();
           if (++s == kStages) { s = 0; ph ^= 1u; }
         }
-        if (ok) tc2_commit_both(acc_full);
+        if (ok && issuer) tc2_commit_both(acc_full);
+        __syncwarp();
       }
     }
   } else if (warp >= 4 && warp < 8) {
     const int q = warp & 3;
     const uint32_t ready_leader = mapa(ready, 0);
-    int s = 0;
-    uint32_t ph = 0u;
+    int s = 0, z = 0;
+    uint32_t ph = 1u, sph = 0u;
     bool ok = true;
     for (int t = pair; t < tiles && ok; t += pairs) {
       for (int k = 0; k < p.chunks; ++k) {
-        if (!(ok = mbar_wait(full + 8 * s, ph, abort_flag))) break;
+        if (!(ok = mbar_wait(sf_full + 8 * z, sph, abort_flag))) break;
+        uint32_t wa[16], wb[32];
+        read_scales<kNv, 4>(sf + z * kSfBytes, lane, k & 1, wa);
+        read_scales<kNv, 8>(sf + z * kSfBytes + kHalf * 16, lane, k & 1, wb);
+        if (!(ok = mbar_wait(empty + 8 * s, ph, abort_flag))) break;
         tc_fence_after();
-        const uint32_t src = sf + s * kSfBytes, dst = sf_cols + s * kSfCols + (static_cast<uint32_t>(q * 32) << 16);
-        move_scales<kNv, 4>(src, dst, lane, k & 1);
-        move_scales_256<kNv>(src + kHalf * 16, dst + 16, lane, k & 1);
-        tmem_wait_st();
-        fence_proxy_async_smem();
+        const uint32_t dst = sf_cols + s * kSfCols + (static_cast<uint32_t>(q * 32) << 16);
+        tmem_st16(dst, wa);
+        tmem_st16(dst + 16, *reinterpret_cast<const uint32_t(*)[16]>(wb));
+        if (kNv) tmem_st16(dst + 32, *reinterpret_cast<const uint32_t(*)[16]>(wb + 16));
+        tmem_wait_st();                                  // the words have been read, so the ring's stage may be filled again
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive_cluster(ready_leader + 8 * s);
+        if (lane == 0) {
+          mbar_arrive_cluster(ready_leader + 8 * s);
+          mbar_arrive(sf_empty + 8 * z);
+        }
         if (++s == kStages) { s = 0; ph ^= 1u; }
+        if (++z == kSfStages) { z = 0; sph ^= 1u; }
       }
     }
   } else if (warp >= 8) {
     const int q = warp & 3, c0 = (warp >= 12 ? kHalf : 0);
     const uint32_t acc = tmem + (static_cast<uint32_t>(q * 32) << 16) + c0, empty_leader = mapa(acc_empty, 0);
     const float alpha = p.alpha ? *p.alpha : 1.0f;
-    const int size = p.dt == HIF4_FP32 ? 4 : 2;
+    const uint32_t slab = smem + kSlabs + (warp - 8) * kSlabBytes;
+    const uint64_t policy = evict_first_policy();
     uint32_t ph = 0u;
     for (int t = pair; t < tiles; t += pairs) {
       const PairTile w = pair_tile(p, t);
       if (!__all_sync(0xFFFFFFFFu, mbar_wait(acc_full, ph, abort_flag, 64))) break;
       ph ^= 1u;
       tc_fence_after();
-      const int64_t m = w.m0 + static_cast<int64_t>(rank) * kHalf + q * 32 + lane, n = w.n0 + c0;
-      const bool whole = p.wide && n + kHalf <= p.N;
-      uint8_t* row = static_cast<uint8_t*>(p.y) + (m * p.ld_y + n) * size;
-      if (whole && size == 2) {
+      const int m = w.m0 + static_cast<int>(rank) * kHalf + q * 32, n = w.n0 + c0;       // the warp's first row and column
+      const bool inside = m < p.M && n < p.N;
+      if (p.tma_store && p.dt != HIF4_FP32) {
         uint32_t packed[64];
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
@@ -192,10 +261,8 @@ bfp4_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant_
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive_cluster(empty_leader);
-        if (m < p.M) {
-#pragma unroll
-          for (int i = 0; i < 8; ++i) store32(row + 32 * i, packed + 8 * i);
-        }
+        if (inside) store_slab(&tmY, n, m, slab, packed, lane, policy);
+        if (inside && n + 64 < p.N) store_slab(&tmY, n + 64, m, slab, packed + 32, lane, policy);
       } else {
         for (int c = 0; c < 4; ++c) {
           uint32_t r[32];
@@ -203,15 +270,12 @@ bfp4_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant_
           tc_wait_ld();
 #pragma unroll
           for (int i = 0; i < 32; ++i) r[i] = __float_as_uint(alpha * __uint_as_float(r[i]));
-          if (m < p.M) {
-            if (whole) {
+          if (p.tma_store) {
+            if (inside && n + 32 * c < p.N) store_slab(&tmY, n + 32 * c, m, slab, r, lane, policy);
+          } else if (m + lane < p.M) {
 #pragma unroll
-              for (int i = 0; i < 4; ++i) store32(row + 128 * c + 32 * i, r + 8 * i);
-            } else {
-#pragma unroll
-              for (int i = 0; i < 32; ++i)
-                if (n + 32 * c + i < p.N) store_y(p, m, n + 32 * c + i, __uint_as_float(r[i]));
-            }
+            for (int i = 0; i < 32; ++i)
+              if (n + 32 * c + i < p.N) store_y(p, m + lane, n + 32 * c + i, __uint_as_float(r[i]));
           }
         }
         tc_fence_before();
@@ -219,6 +283,7 @@ bfp4_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant_
         if (lane == 0) mbar_arrive_cluster(empty_leader);
       }
     }
+    if (lane == 0) bulk_wait_all();
   }
 
   __syncwarp();
@@ -237,18 +302,36 @@ bfp4_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant_
   }
 }
 
+// Y for the epilogue's copies: box = 128 bytes x 32 rows.
+bool make_y_map(CUtensorMap* map, const hif4_bfp4_gemm_args& a) {
+  EncodeTiledFn fn = encode_tiled_fn();
+  if (!fn) return false;
+  const int size = a.dt == HIF4_FP32 ? 4 : 2;
+  const cuuint64_t dims[2] = {static_cast<cuuint64_t>(a.N), static_cast<cuuint64_t>(a.M)};
+  const cuuint64_t strides[1] = {static_cast<cuuint64_t>(a.ld_y) * size};
+  const cuuint32_t box[2] = {static_cast<cuuint32_t>(128 / size), 32};
+  const cuuint32_t estr[2] = {1, 1};
+  return fn(map, a.dt == HIF4_FP32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : a.dt == HIF4_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16,
+            2, a.Y, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_NONE,
+            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 template <bool kNv>
 hif4_status launch_pairs(const hif4_bfp4_gemm_args& a, Bfp4Params p, cudaStream_t st) {
   static uint64_t ready = 0;
   if (!ensure_dynamic_smem(bfp4_pair_kernel<kNv>, kSmem, ready)) return HIF4_ERR_CUDA;
-  CUtensorMap tmA, tmB;
+  CUtensorMap tmA, tmB, tmY;
   if (!make_code_map(&tmA, a.A_codes, a.M, a.K, kHalf) || !make_code_map(&tmB, a.B_codes, a.N, a.K, kHalf)) return HIF4_ERR_CUDA;
+  // (a TMA store clips the innermost dimension in 16-byte pieces, so a row's length has to be whole ones)
+  const int64_t size = a.dt == HIF4_FP32 ? 4 : 2;
+  p.tma_store = (reinterpret_cast<uintptr_t>(a.Y) & 15u) == 0 && a.ld_y * size % 16 == 0 && a.N * size % 16 == 0 && make_y_map(&tmY, a);
+  if (!p.tma_store) tmY = tmA;                           // not used
   const int64_t m_tiles = ceil_div64(a.M, kTile), n_tiles = ceil_div64(a.N, kTile);
   if (m_tiles * n_tiles > 0x7FFFFFFFll - 1024 || n_tiles > 0x7FFFFFFFll / kBand) return HIF4_ERR_SHAPE;
   p.m_tiles = static_cast<int>(m_tiles);
   p.n_tiles = static_cast<int>(n_tiles);
   const int most = sm_count() / 2, tiles = p.m_tiles * p.n_tiles;
-  bfp4_pair_kernel<kNv><<<2 * (tiles < most ? tiles : most), kThreads, kSmem, st>>>(tmA, tmB, p);
+  bfp4_pair_kernel<kNv><<<2 * (tiles < most ? tiles : most), kThreads, kSmem, st>>>(tmA, tmB, tmY, p);
   note_launch();
   return launch_status();
 }

@@ -274,7 +274,7 @@ __device__ __noinline__ int choose_wide(const T* row, const RouteParams* p, long
 
 // V: experts a lane holds (experts <= 32 V).
 template <typename T, int V>
-__global__ void __launch_bounds__(kRouteWarps * 32)
+__global__ void __launch_bounds__(kRouteWarps * 32, V <= 8 ? 8 : V == 16 ? 5 : 3)
 route_kernel(const T* __restrict__ logits, const __grid_constant__ RouteParams p, int32_t* __restrict__ ids, float* __restrict__ weights) {
   extern __shared__ long long scratch[];                // [warps][experts], where groups are not whole lanes
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
