@@ -185,9 +185,7 @@ bfp4_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant_
         tc_ld16(acc + c, r);
         tc_wait_ld();
         if (ranks == 1) {
-#pragma unroll
-          for (int j = 0; j < 16; ++j)
-            if (n < p.N && m0 + c + j < m_end) store_y(p, m0 + c + j, n, alpha * __uint_as_float(r[j]));
+          if (n < p.N) store_tokens(p, m0 + c, m_end - m0 - c, n, alpha, r);
         } else {
           float* sums = reinterpret_cast<float*>(gen) + q * 32 + lane;
 #pragma unroll
@@ -288,6 +286,7 @@ hif4_status product(const hif4_bfp4_gemm_args& a, bool grouped, void* stream) {
   if (!p.error_word) return HIF4_ERR_CUDA;
   // Prompts: 256 x 256 tiles on CTA pairs as soon as there are enough of them
   if (!grouped && a.M > 128 && ceil_div64(a.M, 256) * ceil_div64(a.N, 256) * 4 >= sm_count()) return launch_bfp4_pairs(a, p, st);
+  if (grouped && a.num_groups <= kMaxTableGroups) return launch_bfp4_grouped(a, p, st);
   // tokens of a tile: the fewest that hold the rows of a (mean) group, at most 128
   const int64_t mean = grouped ? ceil_div64(a.M, a.num_groups) : a.M;
   const int T = mean <= 16 ? 16 : mean <= 32 ? 32 : mean <= 64 ? 64 : 128;

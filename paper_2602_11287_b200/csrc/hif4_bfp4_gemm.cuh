@@ -22,13 +22,15 @@ struct Bfp4Params {
   const float* alpha;
   void* y;
   int64_t ld_y;
-  int dt, tma_store;
+  int dt, tma_store, row_copies;            // how Y leaves shared memory: boxes, whole rows
   int num_groups;                           // 0: dense
   const int64_t* offsets;
   unsigned int* error_word;
 };
-// The CTA-pair kernel (dense, 256 x 256 tiles).
+// The CTA-pair kernel (256 x 256 tiles) and the persistent kernel for groups of few rows; grouped: up to kMaxTableGroups groups.
+constexpr int kMaxTableGroups = 256;
 hif4_status launch_bfp4_pairs(const hif4_bfp4_gemm_args& a, Bfp4Params p, cudaStream_t st);
+hif4_status launch_bfp4_grouped(const hif4_bfp4_gemm_args& a, Bfp4Params p, cudaStream_t st);
 
 namespace {
 
@@ -106,6 +108,64 @@ __device__ __forceinline__ void store_y(const Bfp4Params& p, int64_t m, int64_t 
   if (p.dt == HIF4_FP32) static_cast<float*>(p.y)[at] = v;
   else if (p.dt == HIF4_BF16) static_cast<__nv_bfloat16*>(p.y)[at] = __float2bfloat16_rn(v);
   else static_cast<__half*>(p.y)[at] = __float2half_rn(v);
+}
+// A lane's column of Y: tokens m .. m + kCount - 1, of which `count` are there.
+template <typename TO, int kCount>
+__device__ __forceinline__ void store_tokens_as(TO* y, int64_t ld, int count, float alpha, const uint32_t (&r)[kCount]) {
+#pragma unroll
+  for (int j = 0; j < kCount; ++j, y += ld)
+    if (j < count) *y = from_f32<TO>(alpha * __uint_as_float(r[j]));
+}
+template <int kCount>
+__device__ __forceinline__ void store_tokens(const Bfp4Params& p, int64_t m, int count, int64_t n, float alpha, const uint32_t (&r)[kCount]) {
+  const int64_t at = m * p.ld_y + n;
+  if (p.dt == HIF4_FP32) store_tokens_as(static_cast<float*>(p.y) + at, p.ld_y, count, alpha, r);
+  else if (p.dt == HIF4_BF16) store_tokens_as(static_cast<__nv_bfloat16*>(p.y) + at, p.ld_y, count, alpha, r);
+  else store_tokens_as(static_cast<__half*>(p.y) + at, p.ld_y, count, alpha, r);
+}
+
+// ------------------------------------------------------------------------------------ tiles of a grouped product
+// First rows, ends and running number of row tiles of the groups, in shared memory.
+struct GroupTable { int tiles[kMaxTableGroups + 1], first[kMaxTableGroups], end[kMaxTableGroups]; };
+constexpr int kGroupTableBytes = (static_cast<int>(sizeof(GroupTable)) + 15) / 16 * 16;
+// One warp, from the offsets (clamped to 0 .. M; a group that ends before it begins is empty).
+__device__ __forceinline__ void build_group_table(GroupTable& table, const Bfp4Params& p, int tile_rows, int lane) {
+  int before = 0;
+  for (int g0 = 0; g0 < p.num_groups; g0 += 32) {
+    const int g = g0 + lane;
+    int64_t lo = 0, hi = 0;
+    if (g < p.num_groups) {
+      lo = max(static_cast<int64_t>(0), min(p.M, p.offsets[g]));
+      hi = max(lo, min(p.M, p.offsets[g + 1]));
+    }
+    int tiles = static_cast<int>((hi - lo + tile_rows - 1) / tile_rows);
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int v = __shfl_up_sync(0xFFFFFFFFu, tiles, o);
+      if (lane >= o) tiles += v;
+    }
+    if (g < p.num_groups) {
+      table.tiles[g + 1] = before + tiles;
+      table.first[g] = static_cast<int>(lo);
+      table.end[g] = static_cast<int>(hi);
+    }
+    before += __shfl_sync(0xFFFFFFFFu, tiles, 31);
+  }
+  if (lane == 0) table.tiles[0] = 0;
+}
+// Tile t: groups one after the other, within a group the row tiles of the same rows of B.
+struct GroupTile { int group, m0, m_end, nt; };
+__device__ __forceinline__ GroupTile group_tile(const GroupTable& table, const Bfp4Params& p, int t, int tile_rows) {
+  const int rows_before = t / p.n_tiles;                 // groups with table.tiles <= this end before the tile
+  int lo = 0, hi = p.num_groups - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi) >> 1;
+    if (table.tiles[mid + 1] <= rows_before) lo = mid + 1;
+    else hi = mid;
+  }
+  const int mt = table.tiles[lo + 1] - table.tiles[lo], in = t - table.tiles[lo] * p.n_tiles;
+  const int nt = in / mt;
+  return {lo, table.first[lo] + (in - nt * mt) * tile_rows, table.end[lo], nt};
 }
 
 // Codes of a matrix: [rows, K / 2] bytes, box = 128 bytes x box_rows; what lies outside reads as zeros.

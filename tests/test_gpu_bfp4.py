@@ -189,7 +189,8 @@ def test_product_into_a_view(hif4, M):
 
 @pytest.mark.parametrize("fmt", [MX, NV])
 @pytest.mark.parametrize("counts,N,K", [([3], 100, 64), ([0, 1, 0, 0, 17, 0], 130, 320), ([40, 0, 129, 1, 300], 257, 512), ([5] * 40, 128, 1024),
-                                        ([0, 0], 64, 128), ([600, 1, 1], 320, 2112)])
+                                        ([0, 0], 64, 128), ([600, 1, 1], 320, 2112),
+                                        ([20, 0, 70, 33, 64, 1], 520, 4096), ([1, 2, 0] * 100, 64, 320), ([7] * 256, 130, 576)])
 def test_grouped_product(hif4, fmt, counts, N, K):
     g = gen(sum(counts) + N)
     G, used = len(counts), sum(counts)
