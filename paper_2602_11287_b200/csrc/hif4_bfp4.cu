@@ -13,6 +13,7 @@ template <typename T, bool kNv>
 __global__ void __launch_bounds__(kThreads)
 bfp4_quantize_kernel(const T* __restrict__ src, int64_t rows, int64_t items, Divider n16, int64_t ld, int wide, const float* __restrict__ gain,
                      uint2* __restrict__ codes, uint8_t* __restrict__ scales) {
+  grid_wait();
   grid_launch_next();
   for (int64_t first = static_cast<int64_t>(blockIdx.x) * kThreads; first < items; first += static_cast<int64_t>(gridDim.x) * kThreads) {
     const int64_t i = first + threadIdx.x;
@@ -41,6 +42,8 @@ __global__ void __launch_bounds__(kThreads)
 bfp4_quantize_transposed_kernel(const T* __restrict__ src, int64_t rows, int64_t cols, int64_t ld, const float* __restrict__ gain,
                                 uint8_t* __restrict__ codes, uint8_t* __restrict__ scales, int64_t row_tiles) {
   __shared__ __align__(16) T tile[kTileRows * kTileCols];
+  grid_wait();
+  grid_launch_next();
   const int64_t ct = blockIdx.x / row_tiles, r0 = (blockIdx.x - ct * row_tiles) * kTileRows, c0 = ct * kTileCols;
   constexpr int kPer = 16 / sizeof(T), kChunks = kTileCols / kPer;      // elements of a 16-byte chunk, chunks of a tile row
   for (int n = threadIdx.x; n < kTileRows * kChunks; n += kThreads) {
@@ -135,6 +138,8 @@ template <typename T, bool kNv>
 __global__ void __launch_bounds__(kThreads)
 bfp4_dequantize_kernel(const uint2* __restrict__ codes, const uint8_t* __restrict__ scales, int64_t rows, int64_t items, Divider n16,
                        const float* __restrict__ gain, T* __restrict__ dst, int64_t ld, int wide) {
+  grid_wait();
+  grid_launch_next();
   for (int64_t i = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x; i < items; i += static_cast<int64_t>(gridDim.x) * kThreads) {
     const int64_t row = items <= 0x7FFFFFFF ? n16.quotient(static_cast<uint32_t>(i)) : i / n16.d;
     const uint32_t c = static_cast<uint32_t>(i - row * n16.d);
@@ -158,13 +163,10 @@ extern "C" size_t hif4_bfp4_scale_bytes(int64_t rows, int64_t cols, hif4_bfp4_fo
   return static_cast<size_t>(rows) * static_cast<size_t>(scale_words(cols, fmt == HIF4_FMT_NVFP4)) * 16;
 }
 
-#define HIF4_BFP4_LAUNCH(kernel, ...)                                                                       \
-  do {                                                                                                      \
-    const bool nv = fmt == HIF4_FMT_NVFP4;                                                                  \
-    if (dt == HIF4_BF16) nv ? kernel<__nv_bfloat16, true>(__VA_ARGS__) : kernel<__nv_bfloat16, false>(__VA_ARGS__); \
-    else if (dt == HIF4_FP16) nv ? kernel<__half, true>(__VA_ARGS__) : kernel<__half, false>(__VA_ARGS__);  \
-    else nv ? kernel<float, true>(__VA_ARGS__) : kernel<float, false>(__VA_ARGS__);                         \
-  } while (0)
+#define HIF4_BFP4_LAUNCH(f, nv, ...)                                                                                    \
+  (dt == HIF4_BF16 ? (nv ? f<__nv_bfloat16, true>(__VA_ARGS__) : f<__nv_bfloat16, false>(__VA_ARGS__))                   \
+   : dt == HIF4_FP16 ? (nv ? f<__half, true>(__VA_ARGS__) : f<__half, false>(__VA_ARGS__))                               \
+                     : (nv ? f<float, true>(__VA_ARGS__) : f<float, false>(__VA_ARGS__)))
 
 namespace {
 unsigned blocks_for(int64_t items) {
@@ -173,22 +175,22 @@ unsigned blocks_for(int64_t items) {
 }
 int rows_wide(const void* p, int64_t ld, size_t size) { return (reinterpret_cast<uintptr_t>(p) | static_cast<uintptr_t>(ld) * size) % 32 == 0; }
 template <typename T, bool kNv>
-void quantize_rows(const void* src, int64_t rows, int64_t cols, int64_t ld, const float* gain, void* codes, void* scales, cudaStream_t st) {
+hif4_status quantize_rows(const void* src, int64_t rows, int64_t cols, int64_t ld, const float* gain, void* codes, void* scales, cudaStream_t st) {
   const int64_t items = rows * (cols / 16);
-  bfp4_quantize_kernel<T, kNv><<<blocks_for(items), kThreads, 0, st>>>(static_cast<const T*>(src), rows, items, make_divider(static_cast<uint32_t>(cols / 16)),
-                                                                       ld, rows_wide(src, ld, sizeof(T)), gain, static_cast<uint2*>(codes),
-                                                                       static_cast<uint8_t*>(scales));
+  return launch_overlapped(bfp4_quantize_kernel<T, kNv>, blocks_for(items), kThreads, 0, st, static_cast<const T*>(src), rows, items,
+                           make_divider(static_cast<uint32_t>(cols / 16)), ld, rows_wide(src, ld, sizeof(T)), gain, static_cast<uint2*>(codes),
+                           static_cast<uint8_t*>(scales));
 }
 template <typename T, bool kNv>
-void quantize_columns(const void* src, int64_t rows, int64_t cols, int64_t ld, const float* gain, void* codes, void* scales, cudaStream_t st) {
+hif4_status quantize_columns(const void* src, int64_t rows, int64_t cols, int64_t ld, const float* gain, void* codes, void* scales, cudaStream_t st) {
   const int64_t row_tiles = ceil_div64(rows, kTileRows), blocks = row_tiles * ceil_div64(cols, kTileCols);
-  bfp4_quantize_transposed_kernel<T, kNv><<<static_cast<unsigned>(blocks), kThreads, 0, st>>>(
+  return launch_overlapped(bfp4_quantize_transposed_kernel<T, kNv>, static_cast<unsigned>(blocks), kThreads, 0, st,
       static_cast<const T*>(src), rows, cols, ld, gain, static_cast<uint8_t*>(codes), static_cast<uint8_t*>(scales), row_tiles);
 }
 template <typename T, bool kNv>
-void dequantize_rows(const void* codes, const void* scales, int64_t rows, int64_t cols, const float* gain, void* dst, int64_t ld, cudaStream_t st) {
+hif4_status dequantize_rows(const void* codes, const void* scales, int64_t rows, int64_t cols, const float* gain, void* dst, int64_t ld, cudaStream_t st) {
   const int64_t items = rows * (cols / 16);
-  bfp4_dequantize_kernel<T, kNv><<<blocks_for(items), kThreads, 0, st>>>(
+  return launch_overlapped(bfp4_dequantize_kernel<T, kNv>, blocks_for(items), kThreads, 0, st,
       static_cast<const uint2*>(codes), static_cast<const uint8_t*>(scales), rows, items, make_divider(static_cast<uint32_t>(cols / 16)), gain,
       static_cast<T*>(dst), ld, rows_wide(dst, ld, sizeof(T)));
 }
@@ -211,9 +213,7 @@ extern "C" hif4_status hif4_bfp4_quantize(const void* src, hif4_dtype dt, int64_
   if (cols % kUnitElems != 0) return HIF4_ERR_SHAPE;
   const hif4_status s = check(src, dt, rows, cols, ld_src, fmt, gain, codes, scales);
   if (s != HIF4_OK || rows == 0 || cols == 0) return s;
-  HIF4_BFP4_LAUNCH(quantize_rows, src, rows, cols, ld_src, gain, codes, scales, static_cast<cudaStream_t>(stream));
-  note_launch();
-  return launch_status();
+  return HIF4_BFP4_LAUNCH(quantize_rows, fmt == HIF4_FMT_NVFP4, src, rows, cols, ld_src, gain, codes, scales, static_cast<cudaStream_t>(stream));
 }
 
 extern "C" hif4_status hif4_bfp4_quantize_transposed(const void* src, hif4_dtype dt, int64_t rows, int64_t cols, int64_t ld_src,
@@ -221,9 +221,7 @@ extern "C" hif4_status hif4_bfp4_quantize_transposed(const void* src, hif4_dtype
   if (rows % kUnitElems != 0 || cols % 8 != 0) return HIF4_ERR_SHAPE;
   const hif4_status s = check(src, dt, rows, cols, ld_src, fmt, gain, codes, scales);
   if (s != HIF4_OK || rows == 0 || cols == 0) return s;
-  HIF4_BFP4_LAUNCH(quantize_columns, src, rows, cols, ld_src, gain, codes, scales, static_cast<cudaStream_t>(stream));
-  note_launch();
-  return launch_status();
+  return HIF4_BFP4_LAUNCH(quantize_columns, fmt == HIF4_FMT_NVFP4, src, rows, cols, ld_src, gain, codes, scales, static_cast<cudaStream_t>(stream));
 }
 
 extern "C" hif4_status hif4_bfp4_dequantize(const void* codes, const void* scales, int64_t rows, int64_t cols, hif4_bfp4_format fmt,
@@ -235,11 +233,8 @@ extern "C" hif4_status hif4_bfp4_dequantize(const void* codes, const void* scale
   const bool nv = fmt == HIF4_FMT_NVFP4;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   if (dt == HIF4_BF16)
-    nv ? dequantize_rows<__nv_bfloat16, true>(codes, scales, rows, cols, gain, dst, ld_dst, st)
-       : dequantize_rows<__nv_bfloat16, false>(codes, scales, rows, cols, gain, dst, ld_dst, st);
-  else
-    nv ? dequantize_rows<float, true>(codes, scales, rows, cols, gain, dst, ld_dst, st)
-       : dequantize_rows<float, false>(codes, scales, rows, cols, gain, dst, ld_dst, st);
-  note_launch();
-  return launch_status();
+    return nv ? dequantize_rows<__nv_bfloat16, true>(codes, scales, rows, cols, gain, dst, ld_dst, st)
+              : dequantize_rows<__nv_bfloat16, false>(codes, scales, rows, cols, gain, dst, ld_dst, st);
+  return nv ? dequantize_rows<float, true>(codes, scales, rows, cols, gain, dst, ld_dst, st)
+            : dequantize_rows<float, false>(codes, scales, rows, cols, gain, dst, ld_dst, st);
 }

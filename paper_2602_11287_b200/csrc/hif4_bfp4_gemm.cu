@@ -15,10 +15,13 @@ namespace {
 
 constexpr int kThreads = 256;               // warps: producer, MMA, tile lookup and TMEM, idle, 4 x scales and epilogue
 constexpr int BW = 128;                     // rows of B a tile
-constexpr int kTmemCols = 256;
 
 template <int T> struct Shape {
-  static constexpr int kStages = T == 128 ? 3 : 4;
+  // CTAs an SM: four of two stages for few tokens (a tile's chunks are dealt to many CTAs, all of whose loads start at once),
+  // two for more
+  static constexpr int kCtas = T <= 32 ? 4 : 2;
+  static constexpr int kStages = T <= 32 ? 2 : T == 128 ? 3 : 4;
+  static constexpr int kTmemCols = 512 / kCtas;
   static constexpr int kCodeBytes = (BW + T) * kRowBytes;
   static constexpr int kSfRows = T < 32 ? 32 : T;
   static constexpr int kSfBytes = (BW + kSfRows) * 16;
@@ -36,7 +39,7 @@ __device__ __forceinline__ float ld_cluster_f32(uint32_t addr) {
 }
 
 template <int T, bool kNv>
-__global__ void __launch_bounds__(kThreads, 2)
+__global__ void __launch_bounds__(kThreads, Shape<T>::kCtas)
 bfp4_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const Bfp4Params p) {
   using S = Shape<T>;
   constexpr int kStages = S::kStages;
@@ -67,9 +70,11 @@ bfp4_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant_
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == 2) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(bars + 24 * kStages + 8), "r"(kTmemCols) : "memory");
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(bars + 24 * kStages + 8), "r"(S::kTmemCols) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
+  grid_wait();
+  grid_launch_next();
   if (warp == 3) {
     // the tile's rows: dense ones follow from the index, grouped ones from the offsets (tiles of a group, added up)
     int64_t m0 = static_cast<int64_t>(mt) * T, m_end = p.M;
@@ -220,7 +225,7 @@ bfp4_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant_
   __syncthreads();
   if (warp == 2) {
     tc_fence_after();
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(S::kTmemCols) : "memory");
   }
 }
 
@@ -235,19 +240,21 @@ hif4_status launch_tiles(const hif4_bfp4_gemm_args& a, Bfp4Params p, int64_t m_t
   if (!make_code_map(&tmA, a.A_codes, a.M, a.K, T) || !make_code_map(&tmB, a.B_codes, b_rows, a.K, BW)) return HIF4_ERR_CUDA;
   const int64_t tiles = m_tiles * p.n_tiles;
   if (tiles > 0x7FFFFFFFll / 8) return HIF4_ERR_SHAPE;
-  // two CTAs an SM; a cluster splits K while CTAs are missing and every one keeps two chunks
+  // a cluster splits K while CTAs are missing and every one keeps two chunks
   int ranks = 1;
-  while (ranks < 8 && tiles * ranks * 2 <= 2 * sm_count() && p.chunks >= 4 * ranks) ranks *= 2;
+  while (ranks < 8 && tiles * ranks * 2 <= Shape<T>::kCtas * sm_count() && p.chunks >= 4 * ranks) ranks *= 2;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(static_cast<unsigned>(tiles * ranks));
   cfg.blockDim = dim3(kThreads);
   cfg.dynamicSmemBytes = Shape<T>::kSmem;
   cfg.stream = st;
-  cudaLaunchAttribute attr[1];
+  cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeClusterDimension;
   attr[0].val.clusterDim = {static_cast<unsigned>(ranks), 1, 1};
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = 1;
+  cfg.numAttrs = 2;
   if (cudaLaunchKernelEx(&cfg, kernel, tmA, tmB, p) != cudaSuccess) {
     (void)cudaGetLastError();
     return HIF4_ERR_CUDA;

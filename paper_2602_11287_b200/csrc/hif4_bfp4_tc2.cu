@@ -117,6 +117,8 @@ bfp4_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant_
   tc_fence_before();
   __syncthreads();
   cluster_sync_all();
+  grid_wait();
+  grid_launch_next();
   tc_fence_after();
   const uint32_t tmem = *tmem_slot, sf_cols = tmem + kTile;
 
@@ -331,9 +333,7 @@ hif4_status launch_pairs(const hif4_bfp4_gemm_args& a, Bfp4Params p, cudaStream_
   p.m_tiles = static_cast<int>(m_tiles);
   p.n_tiles = static_cast<int>(n_tiles);
   const int most = sm_count() / 2, tiles = p.m_tiles * p.n_tiles;
-  bfp4_pair_kernel<kNv><<<2 * (tiles < most ? tiles : most), kThreads, kSmem, st>>>(tmA, tmB, tmY, p);
-  note_launch();
-  return launch_status();
+  return launch_overlapped(bfp4_pair_kernel<kNv>, static_cast<unsigned>(2 * (tiles < most ? tiles : most)), kThreads, kSmem, st, tmA, tmB, tmY, p);
 }
 
 }  // namespace

@@ -2,7 +2,7 @@
 // layer: their order, the rows themselves, the weighted sum of what comes back, and its gradient.  All but the plan are
 // bound by HBM traffic: a token's row is read (and converted) once, the experts' rows are read or written once.
 #include "hif4_bfp4_device.cuh"
-#include "hif4_vec8.cuh"
+#include "hif4_tc_common.cuh"
 
 namespace hif4 {
 namespace {
@@ -13,99 +13,132 @@ constexpr uint32_t kAll = 0xFFFFFFFFu;
 // ----------------------------------------------------------------------------- order of the rows
 // A stable counting sort by expert.  A warp owns a run of consecutive assignments: it counts them per expert, the counts are
 // summed over warps (and blocks) in their order, and the warp then goes through its run again, 32 assignments a step, giving
-// each the next row of its expert: match_any finds the lanes with the same expert, their order is the lanes'.
-constexpr int kPlanWarps = 32;
-constexpr int kPlanItems = 8192;                        // assignments a block orders
+// each the next row of its expert: match_any finds the lanes with the same expert, their order is the lanes'.  A block's ids are
+// loaded at once; many assignments are counted by one launch and placed by a second, few take one launch.
+constexpr int kPlanWarps = 16, kPlanSteps = 4;
+constexpr int kPlanItems = kPlanWarps * kPlanSteps * 32;     // assignments that a block holds in registers
+constexpr int kPlanBlocks = 256;                             // at most; beyond, blocks go through several times kPlanItems
 
 __global__ void __launch_bounds__(kPlanWarps * 32)
-plan_count_kernel(const int32_t* __restrict__ ids, int64_t n, int experts, int32_t* __restrict__ counts) {
+plan_count_kernel(const int32_t* __restrict__ ids, int64_t n, int64_t per_block, int experts, int32_t* __restrict__ counts) {
   extern __shared__ int32_t hist[];
+  grid_wait();
+  grid_launch_next();
   for (int e = threadIdx.x; e < experts; e += blockDim.x) hist[e] = 0;
   __syncthreads();
-  const int64_t first = static_cast<int64_t>(blockIdx.x) * kPlanItems, last = min(n, first + kPlanItems);
-  for (int64_t i = first + threadIdx.x; i < last; i += blockDim.x) {
-    const int e = ids[i];
-    if (e >= 0 && e < experts) atomicAdd(&hist[e], 1);
+  const int64_t first = static_cast<int64_t>(blockIdx.x) * per_block, last = min(n, first + per_block);
+  for (int64_t i0 = first; i0 < last; i0 += kPlanItems) {
+    int id[kPlanSteps];
+#pragma unroll
+    for (int j = 0; j < kPlanSteps; ++j) {
+      const int64_t i = i0 + j * (kPlanWarps * 32) + threadIdx.x;
+      id[j] = i < last ? ids[i] : -1;
+    }
+#pragma unroll
+    for (int j = 0; j < kPlanSteps; ++j)
+      if (id[j] >= 0 && id[j] < experts) atomicAdd(&hist[id[j]], 1);
   }
   __syncthreads();
   for (int e = threadIdx.x; e < experts; e += blockDim.x) counts[static_cast<int64_t>(blockIdx.x) * experts + e] = hist[e];
 }
 
+// `runs` warps own assignments (the others only help with the sums).
 __global__ void __launch_bounds__(kPlanWarps * 32)
-plan_place_kernel(const int32_t* __restrict__ ids, int64_t n, int experts, const int32_t* __restrict__ counts, int blocks,
+plan_place_kernel(const int32_t* __restrict__ ids, int64_t n, int64_t per_block, int runs, int experts, const int32_t* __restrict__ counts, int blocks,
                   int64_t* __restrict__ offsets, int32_t* __restrict__ row_of) {
-  extern __shared__ int32_t hist[];                     // [warps][experts]
-  __shared__ int32_t warp_total[kPlanWarps];
+  extern __shared__ int32_t hist[];                     // [runs][experts]
+  __shared__ int32_t warp_total[kPlanWarps + 1];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  for (int e = threadIdx.x; e < experts * kPlanWarps; e += blockDim.x) hist[e] = 0;
+  grid_wait();
+  grid_launch_next();
+  const int64_t block_first = static_cast<int64_t>(blockIdx.x) * per_block, block_last = min(n, block_first + per_block);
+  const int passes = static_cast<int>((per_block + kPlanItems - 1) / kPlanItems);
+  const int64_t run = static_cast<int64_t>(passes) * kPlanSteps * 32;
+  const int64_t first = min(block_last, block_first + warp * run), last = warp < runs ? min(block_last, first + run) : first;
+  int id[kPlanSteps];
+  const auto load = [&](int pass) {
+#pragma unroll
+    for (int j = 0; j < kPlanSteps; ++j) {
+      const int64_t i = first + (static_cast<int64_t>(pass) * kPlanSteps + j) * 32 + lane;
+      id[j] = i < last ? ids[i] : -1;
+      if (id[j] >= experts) id[j] = -1;
+    }
+  };
+  load(0);
+  for (int e = threadIdx.x; e < experts * runs; e += blockDim.x) hist[e] = 0;
   __syncthreads();
-  const int64_t block_first = static_cast<int64_t>(blockIdx.x) * kPlanItems, block_last = min(n, block_first + kPlanItems);
-  const int64_t run = ((block_last - block_first + kPlanWarps - 1) / kPlanWarps + 31) / 32 * 32;
-  const int64_t first = min(block_last, block_first + warp * run), last = min(block_last, first + run);
   int32_t* mine = hist + warp * experts;
-  for (int64_t i = first + lane; i < last; i += 32) {
-    const int e = ids[i];
-    if (e >= 0 && e < experts) atomicAdd(&mine[e], 1);
+  for (int pass = 0; pass < passes; ++pass) {
+    if (passes > 1) load(pass);
+#pragma unroll
+    for (int j = 0; j < kPlanSteps; ++j)
+      if (id[j] >= 0) atomicAdd(&mine[id[j]], 1);
   }
   __syncthreads();
-  // thread e: counts of expert e before this block and in all blocks, and its warps' first places
-  const int e = threadIdx.x;
-  int before = 0, total = 0;
-  if (e < experts) {
-    if (blocks > 1) {
-      for (int b = 0; b < blocks; ++b) {
-        const int c = counts[static_cast<int64_t>(b) * experts + e];
-        if (b < static_cast<int>(blockIdx.x)) before += c;
-        total += c;
+  int past = 0;                                         // rows of the experts before those of this round
+  for (int e0 = 0; e0 < experts; e0 += blockDim.x) {
+    const int e = e0 + threadIdx.x;
+    int before = 0, total = 0;                          // of expert e: before this block, in all blocks
+    if (e < experts) {
+      int sum = 0;
+      for (int w = 0; w < runs; ++w) sum += hist[w * experts + e];
+      if (blocks == 1) {
+        total = sum;
+      } else {
+#pragma unroll 8
+        for (int b = 0; b < blocks; ++b) {
+          const int c = counts[static_cast<int64_t>(b) * experts + e];
+          before += b < static_cast<int>(blockIdx.x) ? c : 0;
+          total += c;
+        }
       }
     }
-    int sum = 0;
-    for (int w = 0; w < kPlanWarps; ++w) {
-      const int c = hist[w * experts + e];
-      hist[w * experts + e] = sum;
-      sum += c;
-    }
-    if (blocks == 1) total = sum;
-  }
-  int incl = total;                                     // scan over the experts (experts <= threads)
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const int v = __shfl_up_sync(kAll, incl, o);
-    if (lane >= o) incl += v;
-  }
-  if (lane == 31) warp_total[warp] = incl;
-  __syncthreads();
-  if (warp == 0) {
-    int v = warp_total[lane];
+    int incl = total;                                   // scan over the experts of this round
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-      const int u = __shfl_up_sync(kAll, v, o);
-      if (lane >= o) v += u;
+      const int v = __shfl_up_sync(kAll, incl, o);
+      if (lane >= o) incl += v;
     }
-    warp_total[lane] = v;
+    if (lane == 31) warp_total[warp] = incl;
+    __syncthreads();
+    int ahead = past, all = 0;
+    for (int w = 0; w < static_cast<int>(blockDim.x >> 5); ++w) {
+      ahead += w < warp ? warp_total[w] : 0;
+      all += warp_total[w];
+    }
+    __syncthreads();
+    past += all;
+    if (e < experts) {
+      const int end = ahead + incl;
+      int at = end - total + before;
+      for (int w = 0; w < runs; ++w) {                  // the warps' first places
+        const int c = hist[w * experts + e];
+        hist[w * experts + e] = at;
+        at += c;
+      }
+      if (blockIdx.x == 0) {
+        if (e == 0) offsets[0] = 0;
+        offsets[e + 1] = end;
+      }
+    }
   }
   __syncthreads();
-  const int end = incl + (warp ? warp_total[warp - 1] : 0);
-  if (e < experts) {
-    const int base = end - total + before;
-    for (int w = 0; w < kPlanWarps; ++w) hist[w * experts + e] += base;
-    if (blockIdx.x == 0) {
-      if (e == 0) offsets[0] = 0;
-      offsets[e + 1] = end;
+  if (warp >= runs) return;
+  for (int pass = 0; pass < passes; ++pass) {
+    if (passes > 1) load(pass);
+#pragma unroll
+    for (int j = 0; j < kPlanSteps; ++j) {
+      const int64_t i = first + (static_cast<int64_t>(pass) * kPlanSteps + j) * 32 + lane;
+      if (i - lane >= last) break;
+      const uint32_t same = __match_any_sync(kAll, id[j]);
+      const int rank = __popc(same & ((1u << lane) - 1u));
+      int row = -1;
+      if (id[j] >= 0) row = mine[id[j]] + rank;
+      __syncwarp();
+      if (id[j] >= 0 && rank == 0) mine[id[j]] += __popc(same);
+      __syncwarp();
+      if (i < last) row_of[i] = row;
     }
-  }
-  __syncthreads();
-  for (int64_t i = first + lane; i - lane < last; i += 32) {
-    const int id = i < last ? ids[i] : -1;
-    const bool fine = id >= 0 && id < experts;
-    const uint32_t same = __match_any_sync(kAll, fine ? id : -1);
-    const int rank = __popc(same & ((1u << lane) - 1u));
-    int row = -1;
-    if (fine) row = mine[id] + rank;
-    __syncwarp();
-    if (fine && rank == 0) mine[id] += __popc(same);
-    __syncwarp();
-    if (i < last) row_of[i] = row;
   }
 }
 
@@ -121,6 +154,8 @@ __device__ __forceinline__ bool has_row(int row, int64_t rows) { return row >= 0
 template <typename Word>
 __global__ void __launch_bounds__(kThreads)
 dispatch_plain_kernel(Gather g, const Word* __restrict__ x, int64_t ld_x, Word* __restrict__ out, int64_t ld_out, int64_t words) {
+  grid_wait();
+  grid_launch_next();
   const int64_t t = blockIdx.x / g.segments;
   const int seg = static_cast<int>(blockIdx.x - t * g.segments);
   const int32_t* row_of = g.row_of + t * g.top_k;
@@ -137,6 +172,8 @@ dispatch_plain_kernel(Gather g, const Word* __restrict__ x, int64_t ld_x, Word* 
 template <typename T, bool kRHA>
 __global__ void __launch_bounds__(kThreads)
 dispatch_hif4_kernel(Gather g, const T* __restrict__ x, int64_t ld_x, uint32_t* __restrict__ out) {
+  grid_wait();
+  grid_launch_next();
   const int64_t t = blockIdx.x / g.segments;
   const int seg = static_cast<int>(blockIdx.x - t * g.segments);
   const int32_t* row_of = g.row_of + t * g.top_k;
@@ -162,6 +199,8 @@ template <typename T, bool kNv>
 __global__ void __launch_bounds__(kThreads)
 dispatch_bfp4_kernel(Gather g, const T* __restrict__ x, int64_t ld_x, const float* __restrict__ gain, uint2* __restrict__ codes,
                      uint8_t* __restrict__ scales) {
+  grid_wait();
+  grid_launch_next();
   const int64_t t = blockIdx.x / g.segments;
   const int seg = static_cast<int>(blockIdx.x - t * g.segments);
   const int32_t* row_of = g.row_of + t * g.top_k;
@@ -203,6 +242,8 @@ template <typename TI, typename TO, int kVec>
 __global__ void __launch_bounds__(kThreads)
 combine_kernel(Gather g, const TI* __restrict__ in, int64_t ld_in, const float* __restrict__ weights, const TO* residual, int64_t ld_r,
                float res_scale, TO* y, int64_t ld_y) {
+  grid_wait();
+  grid_launch_next();
   const int64_t t = blockIdx.x / g.segments;
   const int seg = static_cast<int>(blockIdx.x - t * g.segments);
   const int32_t* row_of = g.row_of + t * g.top_k;
@@ -234,6 +275,8 @@ template <typename TD, typename TI, int kVec>
 __global__ void __launch_bounds__(kThreads)
 combine_backward_kernel(Gather g, const TD* __restrict__ dy, int64_t ld_dy, const float* __restrict__ weights, const TI* __restrict__ in,
                         int64_t ld_in, TI* __restrict__ din, int64_t ld_din, float* __restrict__ dweights) {
+  grid_wait();
+  grid_launch_next();
   __shared__ float sums[kThreads / 32][kTogether];
   const int64_t t = blockIdx.x;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -292,6 +335,9 @@ bool aligned(const void* p, int64_t to) { return bits(p) % static_cast<uintptr_t
 // Row r of a matrix starts at a multiple of 16 bytes, for every r.
 bool rows_aligned(const void* p, int64_t ld, int dt) { return aligned(p, 16) && ld * type_size(dt) % 16 == 0; }
 
+int64_t plan_per_block(int64_t n) { return kPlanItems * ceil_div64(n > 0 ? n : 1, static_cast<int64_t>(kPlanItems) * kPlanBlocks); }
+int64_t plan_blocks(int64_t n) { return n > 0 ? ceil_div64(n, plan_per_block(n)) : 1; }
+
 hif4_status check_sizes(int64_t tokens, int64_t cols, int64_t top_k, int64_t rows) {
   if (tokens < 0 || cols < 0 || top_k < 1 || rows < 0) return HIF4_ERR_SHAPE;
   if (top_k > 0x7FFFFFFFll || rows > 0x7FFFFFFFll || cols > (1ll << 40) || tokens > 0x7FFFFFFFll / top_k) return HIF4_ERR_SHAPE;
@@ -309,25 +355,20 @@ hif4_status make_gather(Gather& g, int64_t tokens, int64_t cols, int64_t top_k, 
 }
 
 template <typename Word>
-void launch_plain(const Gather& g, int64_t blocks, const hif4_dispatch_args& a, cudaStream_t st) {
+hif4_status launch_plain(const Gather& g, int64_t blocks, const hif4_dispatch_args& a, cudaStream_t st) {
   const int64_t n = static_cast<int64_t>(sizeof(Word)) / type_size(a.dt);
-  dispatch_plain_kernel<Word><<<static_cast<unsigned>(blocks), kThreads, 0, st>>>(
-      g, static_cast<const Word*>(a.x), a.ld_x / n, static_cast<Word*>(a.out), a.ld_out / n, a.cols / n);
+  return launch_overlapped(dispatch_plain_kernel<Word>, static_cast<unsigned>(blocks), kThreads, 0, st, g, static_cast<const Word*>(a.x), a.ld_x / n,
+                           static_cast<Word*>(a.out), a.ld_out / n, a.cols / n);
 }
 template <typename T>
-void launch_converted(const Gather& g, int64_t blocks, const hif4_dispatch_args& a, cudaStream_t st) {
+hif4_status launch_converted(const Gather& g, int64_t blocks, const hif4_dispatch_args& a, cudaStream_t st) {
   const unsigned grid = static_cast<unsigned>(blocks);
   const T* x = static_cast<const T*>(a.x);
-  if (a.kind == HIF4_ROWS_HIF4) {
-    uint32_t* out = static_cast<uint32_t*>(a.out);
-    if (a.mode == HIF4_RHA) dispatch_hif4_kernel<T, true><<<grid, kThreads, 0, st>>>(g, x, a.ld_x, out);
-    else dispatch_hif4_kernel<T, false><<<grid, kThreads, 0, st>>>(g, x, a.ld_x, out);
-  } else {
-    uint2* codes = static_cast<uint2*>(a.out);
-    uint8_t* scales = static_cast<uint8_t*>(a.out_scales);
-    if (a.kind == HIF4_ROWS_NVFP4) dispatch_bfp4_kernel<T, true><<<grid, kThreads, 0, st>>>(g, x, a.ld_x, a.gain, codes, scales);
-    else dispatch_bfp4_kernel<T, false><<<grid, kThreads, 0, st>>>(g, x, a.ld_x, a.gain, codes, scales);
-  }
+  if (a.kind == HIF4_ROWS_HIF4)
+    return launch_overlapped(a.mode == HIF4_RHA ? dispatch_hif4_kernel<T, true> : dispatch_hif4_kernel<T, false>, grid, kThreads, 0, st, g, x, a.ld_x,
+                             static_cast<uint32_t*>(a.out));
+  return launch_overlapped(a.kind == HIF4_ROWS_NVFP4 ? dispatch_bfp4_kernel<T, true> : dispatch_bfp4_kernel<T, false>, grid, kThreads, 0, st, g, x, a.ld_x,
+                           a.gain, static_cast<uint2*>(a.out), static_cast<uint8_t*>(a.out_scales));
 }
 
 template <typename TI, typename TO>
@@ -338,11 +379,9 @@ hif4_status launch_combine(const hif4_combine_args& a, cudaStream_t st) {
   int64_t blocks = 0;
   const hif4_status s = make_gather(g, a.tokens, a.cols, a.top_k, a.rows, a.row_of, kThreads * (vec ? 8 : 1), &blocks);
   if (s != HIF4_OK) return s;
-  const auto kernel = vec ? combine_kernel<TI, TO, 8> : combine_kernel<TI, TO, 1>;
-  kernel<<<static_cast<unsigned>(blocks), kThreads, 0, st>>>(g, static_cast<const TI*>(a.in), a.ld_in, a.weights, static_cast<const TO*>(a.residual),
-                                                             a.ld_residual, a.res_scale, static_cast<TO*>(a.y), a.ld_y);
-  note_launch();
-  return launch_status();
+  return launch_overlapped(vec ? combine_kernel<TI, TO, 8> : combine_kernel<TI, TO, 1>, static_cast<unsigned>(blocks), kThreads, 0, st, g,
+                           static_cast<const TI*>(a.in), a.ld_in, a.weights, static_cast<const TO*>(a.residual), a.ld_residual, a.res_scale,
+                           static_cast<TO*>(a.y), a.ld_y);
 }
 template <typename TI, typename TD>
 hif4_status launch_combine_backward(const hif4_combine_backward_args& a, cudaStream_t st) {
@@ -352,11 +391,9 @@ hif4_status launch_combine_backward(const hif4_combine_backward_args& a, cudaStr
   int64_t blocks = 0;
   const hif4_status s = make_gather(g, a.tokens, a.cols, a.top_k, a.rows, a.row_of, a.cols > 0 ? a.cols : 1, &blocks);
   if (s != HIF4_OK) return s;
-  const auto kernel = vec ? combine_backward_kernel<TD, TI, 8> : combine_backward_kernel<TD, TI, 1>;
-  kernel<<<static_cast<unsigned>(a.tokens), kThreads, 0, st>>>(g, static_cast<const TD*>(a.dy), a.ld_dy, a.weights, static_cast<const TI*>(a.in),
-                                                               a.ld_in, static_cast<TI*>(a.din), a.ld_din, a.dweights);
-  note_launch();
-  return launch_status();
+  return launch_overlapped(vec ? combine_backward_kernel<TD, TI, 8> : combine_backward_kernel<TD, TI, 1>, static_cast<unsigned>(a.tokens), kThreads, 0, st,
+                           g, static_cast<const TD*>(a.dy), a.ld_dy, a.weights, static_cast<const TI*>(a.in), a.ld_in, static_cast<TI*>(a.din), a.ld_din,
+                           a.dweights);
 }
 
 }  // namespace
@@ -378,7 +415,7 @@ extern "C" hif4_status hif4_expert_plan_workspace(int64_t tokens, int64_t top_k,
   if (s != HIF4_OK) return s;
   if (experts < 1) return HIF4_ERR_SHAPE;
   if (experts > HIF4_ROUTE_MAX_EXPERTS) return HIF4_ERR_UNSUPPORTED;
-  const int64_t blocks = ceil_div64(tokens * top_k, kPlanItems);
+  const int64_t blocks = plan_blocks(tokens * top_k);
   *bytes = blocks > 1 ? (static_cast<size_t>(blocks) * experts * sizeof(int32_t) + 255) / 256 * 256 : 0;
   return HIF4_OK;
 }
@@ -393,19 +430,21 @@ extern "C" hif4_status hif4_expert_plan(const int32_t* ids, int64_t tokens, int6
   if (!aligned(ids, 4) || !aligned(row_of, 4) || !aligned(offsets, 8) || (need > 0 && !aligned(workspace, 256))) return HIF4_ERR_ALIGN;
   if (workspace_bytes < need) return HIF4_ERR_WORKSPACE;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  const int64_t blocks = n > kPlanItems ? ceil_div64(n, kPlanItems) : 1;
-  const int smem = static_cast<int>(experts) * kPlanWarps * 4;
+  const int64_t blocks = plan_blocks(n), per_block = plan_per_block(n);
+  const int64_t block_items = blocks > 1 ? kPlanItems : n;
+  const int runs = n == 0 ? 1 : static_cast<int>(ceil_div64(block_items, kPlanSteps * 32)), of_experts = static_cast<int>(ceil_div64(experts, 32));
+  const int warps = runs > of_experts ? runs : of_experts < kPlanWarps ? of_experts : kPlanWarps;
+  const int smem = static_cast<int>(experts) * runs * 4;
   static uint64_t ready = 0;
   if (smem > 48 * 1024 && !ensure_dynamic_smem(plan_place_kernel, HIF4_ROUTE_MAX_EXPERTS * kPlanWarps * 4, ready)) return HIF4_ERR_CUDA;
   int32_t* counts = static_cast<int32_t*>(workspace);
   if (blocks > 1) {
-    plan_count_kernel<<<static_cast<unsigned>(blocks), kPlanWarps * 32, experts * 4, st>>>(ids, n, static_cast<int>(experts), counts);
-    note_launch();
+    const hif4_status c = launch_overlapped(plan_count_kernel, static_cast<unsigned>(blocks), kPlanWarps * 32, static_cast<size_t>(experts) * 4, st, ids, n,
+                                            per_block, static_cast<int>(experts), counts);
+    if (c != HIF4_OK) return c;
   }
-  plan_place_kernel<<<static_cast<unsigned>(blocks), kPlanWarps * 32, smem, st>>>(ids, n, static_cast<int>(experts), counts,
-                                                                                  static_cast<int>(blocks), offsets, row_of);
-  note_launch();
-  return launch_status();
+  return launch_overlapped(plan_place_kernel, static_cast<unsigned>(blocks), static_cast<unsigned>(warps) * 32, static_cast<size_t>(smem), st, ids, n,
+                           per_block, runs, static_cast<int>(experts), static_cast<const int32_t*>(counts), static_cast<int>(blocks), offsets, row_of);
 }
 
 extern "C" hif4_status hif4_dispatch(const hif4_dispatch_args* args, void* stream) {
@@ -433,18 +472,14 @@ extern "C" hif4_status hif4_dispatch(const hif4_dispatch_args* args, void* strea
     const int64_t word = all % 16 == 0 ? 16 : all % 4 == 0 ? 4 : 2;
     s = make_gather(g, a.tokens, a.cols, a.top_k, a.rows, a.row_of, kThreads * word / e, &blocks);
     if (s != HIF4_OK) return s;
-    if (word == 16) launch_plain<uint4>(g, blocks, a, st);
-    else if (word == 4) launch_plain<uint32_t>(g, blocks, a, st);
-    else launch_plain<uint16_t>(g, blocks, a, st);
+    return word == 16 ? launch_plain<uint4>(g, blocks, a, st) : word == 4 ? launch_plain<uint32_t>(g, blocks, a, st) : launch_plain<uint16_t>(g, blocks, a, st);
   } else {
     s = make_gather(g, a.tokens, a.cols, a.top_k, a.rows, a.row_of, a.kind == HIF4_ROWS_HIF4 ? kThreads * 8 : kThreads * 16, &blocks);
     if (s != HIF4_OK) return s;
-    if (a.dt == HIF4_BF16) launch_converted<__nv_bfloat16>(g, blocks, a, st);
-    else if (a.dt == HIF4_FP16) launch_converted<__half>(g, blocks, a, st);
-    else launch_converted<float>(g, blocks, a, st);
+    return a.dt == HIF4_BF16   ? launch_converted<__nv_bfloat16>(g, blocks, a, st)
+           : a.dt == HIF4_FP16 ? launch_converted<__half>(g, blocks, a, st)
+                               : launch_converted<float>(g, blocks, a, st);
   }
-  note_launch();
-  return launch_status();
 }
 
 extern "C" hif4_status hif4_combine(const hif4_combine_args* args, void* stream) {

@@ -279,6 +279,8 @@ route_kernel(const T* __restrict__ logits, const __grid_constant__ RouteParams p
   extern __shared__ long long scratch[];                // [warps][experts], where groups are not whole lanes
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const float kInf = __int_as_float(0x7F800000);
+  grid_wait();
+  grid_launch_next();
   float b[V];
   load_bias(p, lane, b);
   for (int64_t t = static_cast<int64_t>(blockIdx.x) * kRouteWarps + warp; t < p.tokens; t += static_cast<int64_t>(gridDim.x) * kRouteWarps) {
@@ -330,6 +332,8 @@ route_backward_kernel(const T* __restrict__ logits, int64_t ld, int64_t tokens, 
                       const float* __restrict__ dweights, int sigmoid, int renormalize, float scale, T* __restrict__ dlogits, int64_t ld_d) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int64_t t = static_cast<int64_t>(blockIdx.x) * kRouteWarps + warp;
+  grid_wait();
+  grid_launch_next();
   if (t >= tokens) return;
   const float kInf = __int_as_float(0x7F800000);
   const T* row = logits + t * ld;
@@ -417,19 +421,16 @@ hif4_status launch_route(const hif4_route_args& a, cudaStream_t st) {
   const size_t smem = scratch ? sizeof(long long) * kRouteWarps * p.experts : 0;
   // every warp keeps the biases of its experts over the tokens it routes
   const int64_t most = static_cast<int64_t>(sm_count()) * 16, blocks = ceil_div64(a.tokens, kRouteWarps);
-  route_kernel<T, V><<<static_cast<unsigned>(blocks < most ? blocks : most), kRouteWarps * 32, smem, st>>>(static_cast<const T*>(a.logits), p, a.ids,
-                                                                                                           a.weights);
-  note_launch();
-  return launch_status();
+  return launch_overlapped(route_kernel<T, V>, static_cast<unsigned>(blocks < most ? blocks : most), kRouteWarps * 32, smem, st,
+                           static_cast<const T*>(a.logits), p, a.ids, a.weights);
 }
 template <typename T, int V>
 hif4_status launch_route_backward(const hif4_route_backward_args& a, cudaStream_t st) {
   const int64_t blocks = ceil_div64(a.tokens, kRouteWarps);
-  route_backward_kernel<T, V><<<static_cast<unsigned>(blocks), kRouteWarps * 32, 0, st>>>(
-      static_cast<const T*>(a.logits), a.ld_logits, a.tokens, static_cast<int>(a.experts), static_cast<int>(a.top_k), a.ids, a.dweights,
-      a.score == HIF4_SCORE_SIGMOID, a.renormalize != 0, a.scale, static_cast<T*>(a.dlogits), a.ld_dlogits);
-  note_launch();
-  return launch_status();
+  return launch_overlapped(route_backward_kernel<T, V>, static_cast<unsigned>(blocks), kRouteWarps * 32, 0, st, static_cast<const T*>(a.logits),
+                           a.ld_logits, a.tokens, static_cast<int>(a.experts), static_cast<int>(a.top_k), a.ids, a.dweights,
+                           static_cast<int>(a.score == HIF4_SCORE_SIGMOID), static_cast<int>(a.renormalize != 0), a.scale,
+                           static_cast<T*>(a.dlogits), a.ld_dlogits);
 }
 
 #define HIF4_ROUTE_BY_WIDTH(launch, T, a, st)                                                                            \
