@@ -171,10 +171,12 @@ bfp4_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant_
       if (!(ok = mbar_wait(full + 8 * s, (i / kStages) & 1, abort_flag))) break;
       tc_fence_after();
       const uint32_t src = sf + s * S::kSfBytes, dst = sf_cols + s * 32 + (static_cast<uint32_t>(q * 32) << 16);
-      move_scales<kNv, 4>(src, dst, lane, k & 1);
-      move_scales<kNv, S::kSfRows / 32>(src + BW * 16, dst + 16, lane, k & 1);
+      uint32_t wb[16], wa[16];
+      read_scales<kNv, 4>(src, lane, k & 1, wb);
+      read_scales_128<kNv, S::kSfRows / 32>(src + BW * 16, lane, k & 1, wa);
+      tmem_st16(dst, wb);
+      tmem_st16(dst + 16, wa);
       tmem_wait_st();
-      fence_proxy_async_smem();
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(ready + 8 * s);

@@ -86,21 +86,28 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16
       : "memory");
 }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-// Scale words of up to 128 rows (`groups` runs of 32) -> sixteen columns: column 4 k + c holds step k of rows 32 c .. 32 c + 31.
-template <bool kNv, int kGroups>
-__device__ __forceinline__ void move_scales(uint32_t smem, uint32_t taddr, int lane, int half) {
-  uint32_t w[16];
+// Scale words of the lane's rows, as the columns want them: of 128 rows column 4 k + c holds step k of rows 32 c .. 32 c + 31, of 256
+// rows column 8 k + c.
+template <bool kNv, int kRuns>
+__device__ __forceinline__ void read_scales(uint32_t smem, int lane, int half, uint32_t (&w)[kRuns * 4]) {
 #pragma unroll
-  for (int c = 0; c < 4; ++c) {
-    uint4 v = make_uint4(0u, 0u, 0u, 0u);
-    if (c < kGroups) v = lds128(smem + (c * 32 + lane) * 16);
+  for (int c = 0; c < kRuns; ++c) {
+    const uint4 v = lds128(smem + (c * 32 + lane) * 16);
     if (kNv) {
-      w[c] = v.x; w[4 + c] = v.y; w[8 + c] = v.z; w[12 + c] = v.w;
+      w[c] = v.x; w[kRuns + c] = v.y; w[2 * kRuns + c] = v.z; w[3 * kRuns + c] = v.w;
     } else {
-      w[c] = half ? v.z : v.x; w[4 + c] = half ? v.w : v.y; w[8 + c] = 0u; w[12 + c] = 0u;
+      w[c] = half ? v.z : v.x; w[kRuns + c] = half ? v.w : v.y; w[2 * kRuns + c] = w[3 * kRuns + c] = 0u;
     }
   }
-  tmem_st16(taddr, w);
+}
+
+// The same of 32 kRuns <= 128 rows in the columns of 128 (zeros for rows that are not there).
+template <bool kNv, int kRuns>
+__device__ __forceinline__ void read_scales_128(uint32_t smem, int lane, int half, uint32_t (&w)[16]) {
+  uint32_t v[kRuns * 4];
+  read_scales<kNv, kRuns>(smem, lane, half, v);
+#pragma unroll
+  for (int i = 0; i < 16; ++i) w[i] = (i & 3) < kRuns ? v[(i >> 2) * kRuns + (i & 3)] : 0u;
 }
 
 __device__ __forceinline__ void store_y(const Bfp4Params& p, int64_t m, int64_t n, float v) {
@@ -178,6 +185,20 @@ bool make_code_map(CUtensorMap* map, const void* base, int64_t rows, int64_t K, 
   const cuuint32_t estr[2] = {1, 1};
   return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// Y for an epilogue's copies.
+bool make_y_map(CUtensorMap* map, const hif4_bfp4_gemm_args& a, int box_cols, int box_rows, CUtensorMapSwizzle swizzle) {
+  EncodeTiledFn fn = encode_tiled_fn();
+  if (!fn) return false;
+  const int size = a.dt == HIF4_FP32 ? 4 : 2;
+  const cuuint64_t dims[2] = {static_cast<cuuint64_t>(a.N), static_cast<cuuint64_t>(a.M)};
+  const cuuint64_t strides[1] = {static_cast<cuuint64_t>(a.ld_y) * size};
+  const cuuint32_t box[2] = {static_cast<cuuint32_t>(box_cols), static_cast<cuuint32_t>(box_rows)};
+  const cuuint32_t estr[2] = {1, 1};
+  return fn(map, a.dt == HIF4_FP32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : a.dt == HIF4_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16,
+            2, a.Y, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle, CU_TENSOR_MAP_L2_PROMOTION_NONE,
+            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 }  // namespace

@@ -29,21 +29,6 @@ constexpr int kBand = 16;                    // token tiles that are walked toge
 static_assert(kTile + kStages * kSfCols <= kTmemCols, "TMEM");
 static_assert(kSmem <= 227 * 1024, "shared memory");
 
-// Scale words of the lane's rows, as the columns want them: of 128 rows column 4 k + c holds step k of rows 32 c .. 32 c + 31, of 256
-// rows column 8 k + c.
-template <bool kNv, int kRuns>
-__device__ __forceinline__ void read_scales(uint32_t smem, int lane, int half, uint32_t (&w)[kRuns * 4]) {
-#pragma unroll
-  for (int c = 0; c < kRuns; ++c) {
-    const uint4 v = lds128(smem + (c * 32 + lane) * 16);
-    if (kNv) {
-      w[c] = v.x; w[kRuns + c] = v.y; w[2 * kRuns + c] = v.z; w[3 * kRuns + c] = v.w;
-    } else {
-      w[c] = half ? v.z : v.x; w[kRuns + c] = half ? v.w : v.y; w[2 * kRuns + c] = w[3 * kRuns + c] = 0u;
-    }
-  }
-}
-
 struct PairTile { int m0, n0; };
 __device__ __forceinline__ PairTile pair_tile(const Bfp4Params& p, int t) {
   const int band_tiles = kBand * p.n_tiles, band = t / band_tiles, in = t - band * band_tiles;
@@ -304,20 +289,6 @@ bfp4_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant_
   }
 }
 
-// Y for the epilogue's copies: box = 128 bytes x 32 rows.
-bool make_y_map(CUtensorMap* map, const hif4_bfp4_gemm_args& a) {
-  EncodeTiledFn fn = encode_tiled_fn();
-  if (!fn) return false;
-  const int size = a.dt == HIF4_FP32 ? 4 : 2;
-  const cuuint64_t dims[2] = {static_cast<cuuint64_t>(a.N), static_cast<cuuint64_t>(a.M)};
-  const cuuint64_t strides[1] = {static_cast<cuuint64_t>(a.ld_y) * size};
-  const cuuint32_t box[2] = {static_cast<cuuint32_t>(128 / size), 32};
-  const cuuint32_t estr[2] = {1, 1};
-  return fn(map, a.dt == HIF4_FP32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : a.dt == HIF4_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16,
-            2, a.Y, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_NONE,
-            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
 template <bool kNv>
 hif4_status launch_pairs(const hif4_bfp4_gemm_args& a, Bfp4Params p, cudaStream_t st) {
   static uint64_t ready = 0;
@@ -326,7 +297,7 @@ hif4_status launch_pairs(const hif4_bfp4_gemm_args& a, Bfp4Params p, cudaStream_
   if (!make_code_map(&tmA, a.A_codes, a.M, a.K, kHalf) || !make_code_map(&tmB, a.B_codes, a.N, a.K, kHalf)) return HIF4_ERR_CUDA;
   // (a TMA store clips the innermost dimension in 16-byte pieces, so a row's length has to be whole ones)
   const int64_t size = a.dt == HIF4_FP32 ? 4 : 2;
-  p.tma_store = (reinterpret_cast<uintptr_t>(a.Y) & 15u) == 0 && a.ld_y * size % 16 == 0 && a.N * size % 16 == 0 && make_y_map(&tmY, a);
+  p.tma_store = (reinterpret_cast<uintptr_t>(a.Y) & 15u) == 0 && a.ld_y * size % 16 == 0 && a.N * size % 16 == 0 && make_y_map(&tmY, a, static_cast<int>(128 / size), 32, CU_TENSOR_MAP_SWIZZLE_128B);
   if (!p.tma_store) tmY = tmA;                           // not used
   const int64_t m_tiles = ceil_div64(a.M, kTile), n_tiles = ceil_div64(a.N, kTile);
   if (m_tiles * n_tiles > 0x7FFFFFFFll - 1024 || n_tiles > 0x7FFFFFFFll / kBand) return HIF4_ERR_SHAPE;
