@@ -55,10 +55,28 @@ template <> struct Keys<true> {
   }
 };
 
+__device__ __forceinline__ float fast_rcp(float v) {
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+  return r;
+}
+__device__ __forceinline__ float fast_exp2(float v) {
+  float r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+  return r;
+}
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
+constexpr float kLog2e = 1.4426950408889634f;
+
 // Sigmoid of x times e^-m, m = min(0, largest x of the sum): a common factor of all terms of a ratio, so that no ratio of very
 // small sigmoids loses its terms.
 __device__ __forceinline__ float sigmoid_scaled(float x, float m) {
-  return x > 0.0f ? 1.0f / (1.0f + expf(-x)) : expf(x - m) / (1.0f + expf(x));
+  const float t = expf(-fabsf(x));
+  return (x > 0.0f ? 1.0f : m == 0.0f ? t : expf(x - m)) * fast_rcp(1.0f + t);
 }
 
 struct RouteParams {
@@ -67,12 +85,6 @@ struct RouteParams {
   float scale;
   const float* bias;
 };
-
-__device__ __forceinline__ float fast_rcp(float v) {
-  float r;
-  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
-  return r;
-}
 
 // A lane's logits (-inf past the last expert) and biases (-inf for a NaN).
 template <typename T, int V>
@@ -127,11 +139,12 @@ __device__ __forceinline__ void best_two(const Key (&c)[V], uint32_t used, Key n
 // The choice of one token from the lane's logits x and biases b; top is the largest logit that is a number.  Lane j gets the j-th
 // expert (or -1).  Sets `contested` where neighbours were too near to tell apart.
 //
-// Errors in FP32: a sigmoid 1 / (1 + e) with e = exp2(-x log2 e): 2^-22.5 from exp2 and |x| 2^-24 from its argument reach the
+// Errors in FP32: a sigmoid 1 / (1 + e) with e = exp2(-x log2 e): 2^-22 from exp2 and 1.5 |x| 2^-24 from its argument reach the
 // result through e / (1 + e)^2 <= 1/4 (and |x| e / (1 + e)^2 < 0.23), 1 + e and the reciprocal add 2^-24 + 2^-23: together below
-// 2^-22; two of them 2^-21, taken as 2^-20.  A softmax the same, relative to the largest.  The bias's addition 2^-24 of the sum.
+// 1.1 2^-22, two of them below 2^-20.  A softmax the same relative to the largest, whose sum adds as much again: 2^-19.  The bias's
+// addition: 2^-24 of the sum, two of them 2^-23, a group's sum of two as much again.
 template <bool kWide, int V>
-__device__ __forceinline__ int choose(const float (&x)[V], const float (&b)[V], float top, const RouteParams& p, long long* scratch, int lane, bool& contested) {
+__device__ __forceinline__ int choose(const float (&x)[V], const float (&b)[V], float top, const RouteParams& p, long long* scratch, long long* notes, int lane, bool& contested) {
   using K = Keys<kWide>;
   using Real = typename K::Real;
   using Key = typename K::Key;
@@ -147,13 +160,13 @@ __device__ __forceinline__ int choose(const float (&x)[V], const float (&b)[V], 
     if (p.sigmoid) {
 #pragma unroll
       for (int i = 0; i < V; ++i)
-        v[i] = kWide ? static_cast<Real>(1.0 / (1.0 + exp(-static_cast<double>(x[i])))) : static_cast<Real>(fast_rcp(1.0f + __expf(-x[i])));
+        v[i] = kWide ? static_cast<Real>(1.0 / (1.0 + exp(-static_cast<double>(x[i])))) : static_cast<Real>(fast_rcp(1.0f + fast_exp2(-kLog2e * x[i])));
       near = static_cast<Real>(0x1p-20);
     } else {
       Real total = 0;
 #pragma unroll
       for (int i = 0; i < V; ++i) {
-        v[i] = x[i] == top ? Real(1) : kWide ? static_cast<Real>(exp(static_cast<double>(x[i]) - static_cast<double>(top))) : static_cast<Real>(__expf(x[i] - top));
+        v[i] = x[i] == top ? Real(1) : kWide ? static_cast<Real>(exp(static_cast<double>(x[i]) - static_cast<double>(top))) : static_cast<Real>(fast_exp2(kLog2e * (x[i] - top)));
         if (!(x[i] > -kInf)) v[i] = 0;
         total += v[i];
       }
@@ -233,17 +246,20 @@ __device__ __forceinline__ int choose(const float (&x)[V], const float (&b)[V], 
     }
   }
 
-  int id = -1;
-  Key mine = none, most = none;                         // lane j: the j-th choice
+  // the lane that holds the best notes it as the j-th choice (the lowest lane of equal ones, the lowest index of a lane)
+  struct Chosen { Key key; int id; };
+  Chosen* chosen = reinterpret_cast<Chosen*>(notes);
+  const uint32_t lower = (1u << lane) - 1u;
+  Key most = none;
   uint32_t used = 0u;
   bool known = true;                                    // whether `second` is the best that is left besides `first`
-  for (int j = 0;; ++j) {                               // the last round only looks at who would be next
+  int found = 0;
+  for (;; ++found) {                                    // the last round only looks at who would be next
     most = K::warp_max(first);
-    if (most == none || j == p.top_k) break;
-    const int from = __ffs(__ballot_sync(kAll, first == most)) - 1;
-    const int e = __shfl_sync(kAll, lane * V + at, from);
-    if (lane == j) { id = e; mine = most; }
-    if (lane == from) {
+    if (most == none || found == p.top_k) break;
+    const uint32_t holders = __ballot_sync(kAll, first == most);
+    if (first == most && !(holders & lower)) {
+      chosen[found] = {most, lane * V + at};
       used |= 1u << at;
       if (known) {
         first = second;
@@ -254,22 +270,30 @@ __device__ __forceinline__ int choose(const float (&x)[V], const float (&b)[V], 
         known = true;
       }
     }
+    __syncwarp();
   }
-  Key next = __shfl_down_sync(kAll, mine, 1);
-  if (lane == p.top_k - 1) next = most;
-  contested |= __any_sync(kAll, lane < p.top_k && mine != none && !told_apart(mine, next, near));
+  const bool here = lane < found;
+  Key mine = none, next = most;
+  int id = -1;
+  if (here) {
+    mine = chosen[lane].key;
+    id = chosen[lane].id;
+    if (lane + 1 < found) next = chosen[lane + 1].key;
+  }
+  __syncwarp();
+  contested |= __any_sync(kAll, here && !told_apart(mine, next, near));
   return id;
 }
 
 // The choice in 64 bits.  A call of its own: it is rare, and its registers are not the common path's.
 template <typename T, int V>
-__device__ __noinline__ int choose_wide(const T* row, const RouteParams* p, long long* scratch) {
+__device__ __noinline__ int choose_wide(const T* row, const RouteParams* p, long long* scratch, long long* notes) {
   const int lane = threadIdx.x & 31;
   float x[V], b[V];
   load_logits(row, *p, lane, x);
   load_bias(*p, lane, b);
   bool contested;
-  return choose<true, V>(x, b, largest(x), *p, scratch, lane, contested);
+  return choose<true, V>(x, b, largest(x), *p, scratch, notes, lane, contested);
 }
 
 // V: experts a lane holds (experts <= 32 V).
@@ -277,6 +301,7 @@ template <typename T, int V>
 __global__ void __launch_bounds__(kRouteWarps * 32, V <= 8 ? 8 : V == 16 ? 5 : 3)
 route_kernel(const T* __restrict__ logits, const __grid_constant__ RouteParams p, int32_t* __restrict__ ids, float* __restrict__ weights) {
   extern __shared__ long long scratch[];                // [warps][experts], where groups are not whole lanes
+  __shared__ long long notes[kRouteWarps][2 * HIF4_ROUTE_MAX_TOP_K];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const float kInf = __int_as_float(0x7F800000);
   grid_wait();
@@ -287,16 +312,16 @@ route_kernel(const T* __restrict__ logits, const __grid_constant__ RouteParams p
     const T* row = logits + t * p.ld;
     float x[V];
     load_logits(row, p, lane, x);
-    const float top = largest(x);
-    bool bad = false;
+    const float top = p.sigmoid ? 0.0f : largest(x);
+    float probe = 0.0f;                                 // NaN where one of the logits is
 #pragma unroll
-    for (int i = 0; i < V; ++i) bad |= x[i] != x[i];
-    bad = __any_sync(kAll, bad) || (!p.sigmoid && top == kInf);
+    for (int i = 0; i < V; ++i) probe = max_nan(probe, x[i]);
+    const bool bad = __any_sync(kAll, probe != probe) || (!p.sigmoid && top == kInf);
 
     long long* mine = scratch + static_cast<size_t>(warp) * p.experts;
     bool contested;
-    int id = choose<false, V>(x, b, top, p, mine, lane, contested);      // lane j: the j-th choice
-    if (contested) id = choose_wide<T, V>(row, &p, mine);
+    int id = choose<false, V>(x, b, top, p, mine, notes[warp], lane, contested);      // lane j: the j-th choice
+    if (contested) id = choose_wide<T, V>(row, &p, mine, notes[warp]);
     const float xc = id >= 0 ? to_f32(row[id]) : -kInf;
 
     float w = 0.0f;
