@@ -8,31 +8,42 @@ namespace {
 
 constexpr int kThreads = 256;
 
-// A thread converts sixteen elements: a block of NVFP4, half a block of MXFP4 (its neighbour has the other half).
+// A warp takes the elements of 32 scale bytes or fewer: two rows' words of NVFP4 (16 lanes of 16 elements each; the words of neighbouring
+// rows are neighbours in memory) or one row's word of MXFP4 (two lanes a block).  Warps go along the rows first.
+struct WordTask { int64_t row; int word; uint32_t c; };       // c: the lane's sixteen elements within the row
+template <bool kNv>
+__device__ __forceinline__ WordTask word_task(uint32_t warp, const Divider& words, int lane) {
+  const uint32_t line = words.quotient(warp), word = warp - line * words.d;
+  if (kNv) return {static_cast<int64_t>(line) * 2 + (lane >> 4), static_cast<int>(word), word * 16 + (lane & 15)};
+  return {line, static_cast<int>(word), word * 32 + lane};
+}
+
 template <typename T, bool kNv>
 __global__ void __launch_bounds__(kThreads)
-bfp4_quantize_kernel(const T* __restrict__ src, int64_t rows, int64_t items, Divider n16, int64_t ld, int wide, const float* __restrict__ gain,
-                     uint2* __restrict__ codes, uint8_t* __restrict__ scales) {
+bfp4_quantize_kernel(const T* __restrict__ src, int64_t rows, uint32_t n16, uint32_t tasks, Divider words, int64_t ld, int wide,
+                     const float* __restrict__ gain, uint2* __restrict__ codes, uint8_t* __restrict__ scales) {
+  const int lane = threadIdx.x & 31;
+  const uint32_t warp = blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5);
   grid_wait();
   grid_launch_next();
-  for (int64_t first = static_cast<int64_t>(blockIdx.x) * kThreads; first < items; first += static_cast<int64_t>(gridDim.x) * kThreads) {
-    const int64_t i = first + threadIdx.x;
-    const bool in = i < items;
-    const int64_t at = in ? i : 0;
-    const int64_t row = items <= 0x7FFFFFFF ? n16.quotient(static_cast<uint32_t>(at)) : at / n16.d;
-    const uint32_t c = static_cast<uint32_t>(at - row * n16.d);
-    Sixteen v = sixteen_of(load_raw16(src + row * ld + 16 * static_cast<int64_t>(c), wide));
-    if (gain) scale16(v, *gain);
-    uint32_t peak = peak16(v), byte;
-    if (!kNv) peak = max(peak, __shfl_xor_sync(0xFFFFFFFFu, peak, 1));
-    const uint2 code = encode16<kNv>(v, peak, byte);
-    if (!in) continue;
-    codes[i] = code;
-    const uint32_t block = kNv ? c : c >> 1;
-    if (kNv || !(c & 1)) scales[scale_at(row, block, rows)] = static_cast<uint8_t>(byte);
-    if (c == n16.d - 1)
-      for (uint32_t b = block + 1; b & 15; ++b) scales[scale_at(row, b, rows)] = 0;
+  if (warp >= tasks) return;
+  const WordTask t = word_task<kNv>(warp, words, lane);
+  const bool in = t.row < rows && t.c < n16;
+  const int64_t row = min(t.row, rows - 1);
+  const uint32_t c = min(t.c, n16 - 1);
+  const Raw16<T> raw = load_raw16(src + row * ld + 16 * static_cast<int64_t>(c), wide);
+  Sixteen v = sixteen_of(raw);
+  uint32_t peak = peak16(raw), byte;
+  if (gain) {
+    const float g = *gain;
+    scale16(v, g);
+    peak = scaled_peak(peak, g);
   }
+  if (!kNv) peak = max(peak, __shfl_xor_sync(0xFFFFFFFFu, peak, 1));
+  const uint2 code = encode16<kNv>(v, peak, byte);
+  if (in) codes[row * n16 + c] = code;
+  if (t.row < rows && (kNv || !(lane & 1)))                              // (0 past the last block)
+    scales[(static_cast<int64_t>(t.word) * rows + t.row) * 16 + (kNv ? lane & 15 : lane >> 1)] = static_cast<uint8_t>(in ? byte : 0u);
 }
 
 // Tile of 256 rows x 32 columns in shared memory; a thread converts 32 rows of one column.
@@ -58,6 +69,7 @@ bfp4_quantize_transposed_kernel(const T* __restrict__ src, int64_t rows, int64_t
   if (c >= cols || r >= rows) return;
   const T* mine = tile + (threadIdx.x >> 5) * 32 * kTileCols + lane;
   Sixteen a, b;
+  uint32_t pa = 0u, pb = 0u, sa, sb;
 #pragma unroll
   for (int k = 0; k < 8; ++k) {
     a.p[k] = make_float2(to_f32(mine[2 * k * kTileCols]), to_f32(mine[(2 * k + 1) * kTileCols]));
@@ -67,7 +79,11 @@ bfp4_quantize_transposed_kernel(const T* __restrict__ src, int64_t rows, int64_t
     scale16(a, *gain);
     scale16(b, *gain);
   }
-  uint32_t pa = peak16(a), pb = peak16(b), sa, sb;
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    pa = max(pa, max(__float_as_uint(a.p[k].x) & 0x7FFFFFFFu, __float_as_uint(a.p[k].y) & 0x7FFFFFFFu));
+    pb = max(pb, max(__float_as_uint(b.p[k].x) & 0x7FFFFFFFu, __float_as_uint(b.p[k].y) & 0x7FFFFFFFu));
+  }
   if (!kNv) pa = pb = max(pa, pb);
   const uint2 ca = encode16<kNv>(a, pa, sa), cb = encode16<kNv>(b, pb, sb);
   *reinterpret_cast<uint4*>(codes + c * (rows / 2) + r / 2) = make_uint4(ca.x, ca.y, cb.x, cb.y);
@@ -78,29 +94,55 @@ bfp4_quantize_transposed_kernel(const T* __restrict__ src, int64_t rows, int64_t
     for (++block; block & 15; ++block) scales[scale_at(c, block, cols)] = 0;
 }
 
-// Sixteen values m s (m an E2M1 number), or m s / g.  Only 1 and 1.5 times a power of two occur among the m, so two divisions make
-// all quotients of a block, the rest are exact products with powers of two; where those might leave FP32's range each
-// element is divided.
-template <typename T, bool kNv>
-__device__ __forceinline__ void decode16(uint2 code, uint32_t byte, const float* gain, float (&v)[16]) {
-  const float s = scale_value<kNv>(byte);
+// Values m s of E2M1 numbers m, or m s / g, FP32.
+template <bool kNv>
+__device__ __forceinline__ void decode16(uint2 code, float s, const float* gain, float (&v)[16]) {
   e2m1_to8(code.x, v);
   e2m1_to8(code.y, v + 8);
-  if (!gain) {
+  const float g = gain ? *gain : 1.0f;
 #pragma unroll
-    for (int k = 0; k < 16; ++k) v[k] *= s;
-    return;
+  for (int k = 0; k < 16; ++k) {
+    v[k] = __fmul_rn(v[k], s);
+    if (gain) v[k] = __fdiv_rn(v[k], g);
   }
-  const float g = *gain, d1 = __fdiv_rn(s, g), d3 = __fdiv_rn(1.5f * s, g), size = fabsf(d1);
-  if (size > 0x1p-100f && size < 0x1p100f && s > 0x1p-120f) {
-#pragma unroll
-    for (int k = 0; k < 16; ++k) {
-      const uint32_t m = __float_as_uint(v[k]);
-      v[k] = __uint_as_float(m & 0xFF800000u) * ((m & 0x00400000u) ? d3 : d1);
-    }
+}
+
+// The eight BF16 magnitudes of a block, as tables of low and high bytes.  Only 1 and 1.5 times a power of two occur among the E2M1
+// numbers, so the quotients s / g and 1.5 s / g and steps of their exponents make all of them.
+struct Bf16Table { uint32_t low0, low1, high0, high1; };
+__device__ __forceinline__ bool make_table(float s, const float* gain, Bf16Table& t) {
+  float d1 = s, d3 = 1.5f * s;
+  if (gain) {
+    const float g = *gain;
+    d1 = __fdiv_rn(d1, g);
+    d3 = __fdiv_rn(d3, g);
+  }
+  const uint32_t pair = pack2(d1, d3, __nv_bfloat16());                   // 1 and 1.5
+  const uint32_t exponent = (pair >> 7) & 0xFFu, sign = pair & 0x8000u;
+  uint32_t w0, w1 = pair, w2, w3;                                        // (0, 0.5), (1, 1.5), (2, 3), (4, 6)
+  if (s == 0.0f && d1 == 0.0f) {
+    w0 = w1 = w2 = w3 = sign * 0x10001u;
+  } else if (d1 != d1) {
+    w0 = w1 = w2 = w3 = 0x7FC07FC0u;
   } else {
+    if (exponent < 2u || exponent > 250u) return false;                 // steps of the exponent might leave BF16's normal numbers
+    w0 = ((pair - 0x80u) << 16) | sign;
+    w2 = pair + 0x00800080u;
+    w3 = pair + 0x01000100u;
+  }
+  t.low0 = prmt(w0, w1, 0x6420u); t.low1 = prmt(w2, w3, 0x6420u);
+  t.high0 = prmt(w0, w1, 0x7531u); t.high1 = prmt(w2, w3, 0x7531u);
+  return true;
+}
+// Eight codes -> four pairs.
+__device__ __forceinline__ void look_up8(uint32_t codes, const Bf16Table& t, uint32_t* out) {
+  const uint32_t magnitude = codes & 0x77777777u, sign = (codes >> 3) & 0x11111111u;
 #pragma unroll
-    for (int k = 0; k < 16; ++k) v[k] = __fdiv_rn(__fmul_rn(v[k], s), g);
+  for (int h = 0; h < 2; ++h) {
+    const uint32_t low = prmt(t.low0, t.low1, magnitude >> (16 * h));
+    const uint32_t high = prmt(t.high0, t.high1, magnitude >> (16 * h)) ^ prmt(0x00008000u, 0u, sign >> (16 * h));
+    out[2 * h] = prmt(low, high, 0x5140u);
+    out[2 * h + 1] = prmt(low, high, 0x7362u);
   }
 }
 
@@ -108,44 +150,49 @@ __device__ __forceinline__ void store32(void* p, const uint32_t* w) {
   asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]),
                "r"(w[6]), "r"(w[7]) : "memory");
 }
-__device__ __forceinline__ void store_row16(__nv_bfloat16* p, const float (&v)[16], bool wide) {
-  uint32_t w[8];
-#pragma unroll
-  for (int i = 0; i < 8; ++i) w[i] = pack2(v[2 * i], v[2 * i + 1], __nv_bfloat16());
+__device__ __forceinline__ void store_words8(void* p, const uint32_t* w, bool wide) {
   if (wide) {
     store32(p, w);
   } else {
-    reinterpret_cast<uint4*>(p)[0] = make_uint4(w[0], w[1], w[2], w[3]);
-    reinterpret_cast<uint4*>(p)[1] = make_uint4(w[4], w[5], w[6], w[7]);
-  }
-}
-__device__ __forceinline__ void store_row16(float* p, const float (&v)[16], bool wide) {
-#pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    uint32_t w[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) w[i] = __float_as_uint(v[8 * h + i]);
-    if (wide) {
-      store32(p + 8 * h, w);
-    } else {
-      reinterpret_cast<uint4*>(p + 8 * h)[0] = make_uint4(w[0], w[1], w[2], w[3]);
-      reinterpret_cast<uint4*>(p + 8 * h)[1] = make_uint4(w[4], w[5], w[6], w[7]);
-    }
+    static_cast<uint4*>(p)[0] = make_uint4(w[0], w[1], w[2], w[3]);
+    static_cast<uint4*>(p)[1] = make_uint4(w[4], w[5], w[6], w[7]);
   }
 }
 
 template <typename T, bool kNv>
 __global__ void __launch_bounds__(kThreads)
-bfp4_dequantize_kernel(const uint2* __restrict__ codes, const uint8_t* __restrict__ scales, int64_t rows, int64_t items, Divider n16,
+bfp4_dequantize_kernel(const uint2* __restrict__ codes, const uint8_t* __restrict__ scales, int64_t rows, uint32_t n16, uint32_t tasks, Divider words,
                        const float* __restrict__ gain, T* __restrict__ dst, int64_t ld, int wide) {
+  const int lane = threadIdx.x & 31;
+  const uint32_t warp = blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5);
   grid_wait();
   grid_launch_next();
-  for (int64_t i = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x; i < items; i += static_cast<int64_t>(gridDim.x) * kThreads) {
-    const int64_t row = items <= 0x7FFFFFFF ? n16.quotient(static_cast<uint32_t>(i)) : i / n16.d;
-    const uint32_t c = static_cast<uint32_t>(i - row * n16.d);
+  if (warp >= tasks) return;
+  const WordTask t = word_task<kNv>(warp, words, lane);
+  if (t.row >= rows || t.c >= n16) return;
+  const uint2 code = codes[t.row * n16 + t.c];
+  const float s = scale_value<kNv>(scales[(static_cast<int64_t>(t.word) * rows + t.row) * 16 + (kNv ? lane & 15 : lane >> 1)]);
+  T* p = dst + t.row * ld + 16 * static_cast<int64_t>(t.c);
+  uint32_t w[16];
+  if (sizeof(T) == 2) {
+    Bf16Table table;
+    if (make_table(s, gain, table)) {
+      look_up8(code.x, table, w);
+      look_up8(code.y, table, w + 4);
+    } else {
+      float v[16];
+      decode16<kNv>(code, s, gain, v);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) w[i] = pack2(v[2 * i], v[2 * i + 1], __nv_bfloat16());
+    }
+    store_words8(p, w, wide);
+  } else {
     float v[16];
-    decode16<T, kNv>(codes[i], scales[scale_at(row, kNv ? c : c >> 1, rows)], gain, v);
-    store_row16(dst + row * ld + 16 * static_cast<int64_t>(c), v, wide);
+    decode16<kNv>(code, s, gain, v);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) w[i] = __float_as_uint(v[i]);
+    store_words8(p, w, wide);
+    store_words8(p + 8, w + 8, wide);
   }
 }
 
@@ -169,16 +216,21 @@ extern "C" size_t hif4_bfp4_scale_bytes(int64_t rows, int64_t cols, hif4_bfp4_fo
                      : (nv ? f<float, true>(__VA_ARGS__) : f<float, false>(__VA_ARGS__)))
 
 namespace {
-unsigned blocks_for(int64_t items) {
-  const int64_t blocks = ceil_div64(items, kThreads);
-  return static_cast<unsigned>(blocks < 0x7FFFFFFFll ? blocks : 0x7FFFFFFFll);
+// Warps' tasks of a matrix (HIF4_ERR_SHAPE where they are more than 2^31).
+struct Tasks { bool ok; uint32_t n16, count, blocks; Divider words; };
+Tasks word_tasks(int64_t rows, int64_t cols, bool nv) {
+  const int64_t words = scale_words(cols, nv), lines = nv ? ceil_div64(rows, 2) : rows;
+  if (words > 0x7FFFFFFFll / lines) return {false, 0, 0, 0, {}};
+  const int64_t count = words * lines;
+  return {true, static_cast<uint32_t>(cols / 16), static_cast<uint32_t>(count), static_cast<uint32_t>(ceil_div64(count, kThreads / 32)),
+          make_divider(static_cast<uint32_t>(words))};
 }
 int rows_wide(const void* p, int64_t ld, size_t size) { return (reinterpret_cast<uintptr_t>(p) | static_cast<uintptr_t>(ld) * size) % 32 == 0; }
 template <typename T, bool kNv>
 hif4_status quantize_rows(const void* src, int64_t rows, int64_t cols, int64_t ld, const float* gain, void* codes, void* scales, cudaStream_t st) {
-  const int64_t items = rows * (cols / 16);
-  return launch_overlapped(bfp4_quantize_kernel<T, kNv>, blocks_for(items), kThreads, 0, st, static_cast<const T*>(src), rows, items,
-                           make_divider(static_cast<uint32_t>(cols / 16)), ld, rows_wide(src, ld, sizeof(T)), gain, static_cast<uint2*>(codes),
+  const Tasks t = word_tasks(rows, cols, kNv);
+  if (!t.ok) return HIF4_ERR_SHAPE;
+  return launch_overlapped(bfp4_quantize_kernel<T, kNv>, t.blocks, kThreads, 0, st, static_cast<const T*>(src), rows, t.n16, t.count, t.words, ld, rows_wide(src, ld, sizeof(T)), gain, static_cast<uint2*>(codes),
                            static_cast<uint8_t*>(scales));
 }
 template <typename T, bool kNv>
@@ -189,10 +241,10 @@ hif4_status quantize_columns(const void* src, int64_t rows, int64_t cols, int64_
 }
 template <typename T, bool kNv>
 hif4_status dequantize_rows(const void* codes, const void* scales, int64_t rows, int64_t cols, const float* gain, void* dst, int64_t ld, cudaStream_t st) {
-  const int64_t items = rows * (cols / 16);
-  return launch_overlapped(bfp4_dequantize_kernel<T, kNv>, blocks_for(items), kThreads, 0, st,
-      static_cast<const uint2*>(codes), static_cast<const uint8_t*>(scales), rows, items, make_divider(static_cast<uint32_t>(cols / 16)), gain,
-      static_cast<T*>(dst), ld, rows_wide(dst, ld, sizeof(T)));
+  const Tasks t = word_tasks(rows, cols, kNv);
+  if (!t.ok) return HIF4_ERR_SHAPE;
+  return launch_overlapped(bfp4_dequantize_kernel<T, kNv>, t.blocks, kThreads, 0, st, static_cast<const uint2*>(codes),
+                           static_cast<const uint8_t*>(scales), rows, t.n16, t.count, t.words, gain, static_cast<T*>(dst), ld, rows_wide(dst, ld, sizeof(T)));
 }
 hif4_status check(const void* src, hif4_dtype dt, int64_t rows, int64_t cols, int64_t ld, hif4_bfp4_format fmt, const float* gain,
                   const void* codes, const void* scales) {

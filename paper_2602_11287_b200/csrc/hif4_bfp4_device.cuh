@@ -107,23 +107,30 @@ __device__ __forceinline__ void scale16(Sixteen& v, float gain) {
   for (int i = 0; i < 8; ++i) v.p[i] = mul2(v.p[i], both(gain));
 }
 
-// Largest of three magnitudes; a NaN stays one.
-__device__ __forceinline__ float max3_nan(float a, float b, float c) {
-  float d;
-  asm("{\n\t.reg .f32 x, y, z;\n\tabs.f32 x, %1;\n\tabs.f32 y, %2;\n\tabs.f32 z, %3;\n\tmax.NaN.f32 %0, x, y, z;\n\t}" : "=f"(d) : "f"(a), "f"(b), "f"(c));
-  return d;
-}
-// Largest |v| of sixteen values as a bit pattern (a NaN sorts above infinity).
-__device__ __forceinline__ uint32_t peak16(const Sixteen& v) {
-  float p = 0.0f;
+// Largest magnitude of sixteen elements as FP32 bits (a NaN sorts above infinity): the largest pattern without its sign, and
+// patterns order like values.
+__device__ __forceinline__ uint32_t peak_of_words(const uint32_t (&w)[8]) {
+  uint32_t m = 0u;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) p = max3_nan(p, v.p[i].x, v.p[i].y);
-  return __float_as_uint(p);
+  for (int i = 0; i < 8; ++i) m = __vmaxu2(m, w[i] & 0x7FFF7FFFu);
+  return max(m & 0xFFFFu, m >> 16);
 }
+__device__ __forceinline__ uint32_t peak16(const Raw16<__nv_bfloat16>& r) { return peak_of_words(r.w) << 16; }
+__device__ __forceinline__ uint32_t peak16(const Raw16<__half>& r) {
+  return __float_as_uint(__half2float(__ushort_as_half(static_cast<unsigned short>(peak_of_words(r.w)))));
+}
+__device__ __forceinline__ uint32_t peak16(const Raw16<float>& r) {
+  uint32_t m = 0u;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) m = max(m, r.w[i] & 0x7FFFFFFFu);
+  return m;
+}
+// The peak of the products with a gain is the product with the peak: rounding keeps the order.
+__device__ __forceinline__ uint32_t scaled_peak(uint32_t peak, float gain) { return __float_as_uint(fabsf(__fmul_rn(__uint_as_float(peak), gain))); }
 
 constexpr uint32_t kInfBits = 0x7F800000u, kMostBits = 0x7F7FFFFFu;
-// a / b by the reciprocal y of b and one correction from the exact remainder: q0 = a y, q = q0 + (a - q0 b) y.  Before its
-// last rounding q is off by 2^-46 of its value at most.  For b of up to four significant bits (an E4M3 scale, 6) and a of 24 no
+// a / b by the reciprocal y of b (within 2^-23 of its value) and one correction from the exact remainder: q0 = a y, q = q0 + (a - q0 b) y.
+// Before its last rounding q is off by 2^-45 of its value at most.  For b of up to four significant bits (an E4M3 scale, 6) and a of 24 no
 // quotient lies that near to the middle between two FP32 numbers: a = m b with an odd 25-bit m would need 26 bits.  So q is a / b
 // rounded once, like __fdiv_rn, at a quarter of its instructions.
 __device__ __forceinline__ float2 divide2(float2 a, float2 minus_b, float2 y) {
@@ -146,10 +153,12 @@ __device__ __forceinline__ uint2 encode16(Sixteen v, uint32_t peak, uint32_t& by
 #pragma unroll
       for (int i = 0; i < 8; ++i) v.p[i] = make_float2(fminf(fmaxf(v.p[i].x, -most), most), fminf(fmaxf(v.p[i].y, -most), most));
     }
-    const float p = __uint_as_float(peak);
-    byte = e4m3_of(divide2(both(p), both(-6.0f), both(1.0f / 6.0f)).x);
+    const float p = __uint_as_float(peak), p6 = p * (1.0f / 6.0f);
+    byte = e4m3_of(fmaf(fmaf(p6, -6.0f, p), 1.0f / 6.0f, p6));
     const float s = e4m3_value(byte);
-    const float2 y = both(byte ? __frcp_rn(s) : 0.0f), minus_s = both(-s);
+    float rcp;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(rcp) : "f"(s));
+    const float2 y = both(byte ? rcp : 0.0f), minus_s = both(-s);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const float2 d = divide2(v.p[i], minus_s, y);

@@ -207,9 +207,14 @@ dispatch_bfp4_kernel(Gather g, const T* __restrict__ x, int64_t ld_x, const floa
   const int64_t n16 = g.cols / 16;
   for (int64_t c0 = static_cast<int64_t>(seg) * kThreads; c0 < n16; c0 += static_cast<int64_t>(g.segments) * kThreads) {
     const int64_t mine = c0 + threadIdx.x, c = mine < n16 ? mine : n16 - 2 + (threadIdx.x & 1);
-    Sixteen v = sixteen_of(load_raw16(x + t * ld_x + 16 * c, false));
-    if (gain) scale16(v, *gain);
-    uint32_t peak = peak16(v), byte;
+    const Raw16<T> raw = load_raw16(x + t * ld_x + 16 * c, false);
+    Sixteen v = sixteen_of(raw);
+    uint32_t peak = peak16(raw), byte;
+    if (gain) {
+      const float f = *gain;
+      scale16(v, f);
+      peak = scaled_peak(peak, f);
+    }
     if (!kNv) peak = max(peak, __shfl_xor_sync(kAll, peak, 1));
     const uint2 code = encode16<kNv>(v, peak, byte);
     if (mine >= n16) continue;
@@ -269,17 +274,17 @@ combine_kernel(Gather g, const TI* __restrict__ in, int64_t ld_in, const float* 
   store_vec(y + t * ld_y + c, acc);
 }
 
-// A block goes over a token's row, eight assignments at a time.
-constexpr int kTogether = 8;
+// A block goes over a token's row, four assignments at a time, whose rows are loaded together.
+constexpr int kTogether = 4;
 template <typename TD, typename TI, int kVec>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, 4)
 combine_backward_kernel(Gather g, const TD* __restrict__ dy, int64_t ld_dy, const float* __restrict__ weights, const TI* __restrict__ in,
                         int64_t ld_in, TI* __restrict__ din, int64_t ld_din, float* __restrict__ dweights) {
-  grid_wait();
-  grid_launch_next();
   __shared__ float sums[kThreads / 32][kTogether];
   const int64_t t = blockIdx.x;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  grid_wait();
+  grid_launch_next();
   for (int j0 = 0; j0 < g.top_k; j0 += kTogether) {
     int row[kTogether];
     float w[kTogether], acc[kTogether];
@@ -291,18 +296,38 @@ combine_backward_kernel(Gather g, const TD* __restrict__ dy, int64_t ld_dy, cons
       w[j] = there && weights ? weights[t * g.top_k + j0 + j] : 1.0f;
       acc[j] = 0.0f;
     }
-    for (int64_t c = static_cast<int64_t>(threadIdx.x) * kVec; c < g.cols; c += kThreads * kVec) {
+    for (int64_t c = static_cast<int64_t>(threadIdx.x) * kVec; c < g.cols; c += blockDim.x * kVec) {
       float d[kVec], v[kVec];
-      load_vec(dy + t * ld_dy + c, d);
-#pragma unroll
-      for (int j = 0; j < kTogether; ++j) {
-        if (row[j] < 0) continue;
+      if constexpr (kVec == 8) {
+        const Raw8<TD> raw_d = load8(dy + t * ld_dy + c);
+        Raw8<TI> raw[kTogether];
         if (dweights) {
-          load_vec(in + row[j] * ld_in + c, v);
 #pragma unroll
-          for (int i = 0; i < kVec; ++i) acc[j] = fmaf(d[i], v[i], acc[j]);
+          for (int j = 0; j < kTogether; ++j)
+            if (row[j] >= 0) raw[j] = load8(in + row[j] * ld_in + c);
         }
-        if (din) {
+        unpack8(raw_d, d);
+        if (dweights) {
+#pragma unroll
+          for (int j = 0; j < kTogether; ++j) {
+            if (row[j] < 0) continue;
+            unpack8(raw[j], v);
+#pragma unroll
+            for (int i = 0; i < kVec; ++i) acc[j] = fmaf(d[i], v[i], acc[j]);
+          }
+        }
+      } else {
+        d[0] = to_f32(dy[t * ld_dy + c]);
+        if (dweights) {
+#pragma unroll
+          for (int j = 0; j < kTogether; ++j)
+            if (row[j] >= 0) acc[j] = fmaf(d[0], to_f32(in[row[j] * ld_in + c]), acc[j]);
+        }
+      }
+      if (din) {
+#pragma unroll
+        for (int j = 0; j < kTogether; ++j) {
+          if (row[j] < 0) continue;
 #pragma unroll
           for (int i = 0; i < kVec; ++i) v[i] = __fmul_rn(w[j], d[i]);
           store_vec(din + row[j] * ld_din + c, v);
@@ -319,7 +344,7 @@ combine_backward_kernel(Gather g, const TD* __restrict__ dy, int64_t ld_dy, cons
       __syncthreads();
       if (threadIdx.x < kTogether && j0 + static_cast<int>(threadIdx.x) < g.top_k) {
         float s = 0.0f;
-        for (int i = 0; i < kThreads / 32; ++i) s += sums[i][threadIdx.x];
+        for (int i = 0; i < static_cast<int>(blockDim.x >> 5); ++i) s += sums[i][threadIdx.x];
         dweights[t * g.top_k + j0 + threadIdx.x] = s;
       }
       __syncthreads();
@@ -391,7 +416,10 @@ hif4_status launch_combine_backward(const hif4_combine_backward_args& a, cudaStr
   int64_t blocks = 0;
   const hif4_status s = make_gather(g, a.tokens, a.cols, a.top_k, a.rows, a.row_of, a.cols > 0 ? a.cols : 1, &blocks);
   if (s != HIF4_OK) return s;
-  return launch_overlapped(vec ? combine_backward_kernel<TD, TI, 8> : combine_backward_kernel<TD, TI, 1>, static_cast<unsigned>(a.tokens), kThreads, 0, st,
+  // as many threads as go over the row in equal rounds
+  const int64_t words = ceil_div64(a.cols > 0 ? a.cols : 1, vec ? 8 : 1), rounds = ceil_div64(words, kThreads);
+  const unsigned threads = static_cast<unsigned>(ceil_div64(ceil_div64(words, rounds), 32) * 32);
+  return launch_overlapped(vec ? combine_backward_kernel<TD, TI, 8> : combine_backward_kernel<TD, TI, 1>, static_cast<unsigned>(a.tokens), threads, 0, st,
                            g, static_cast<const TD*>(a.dy), a.ld_dy, a.weights, static_cast<const TI*>(a.in), a.ld_in, static_cast<TI*>(a.din), a.ld_din,
                            a.dweights);
 }
