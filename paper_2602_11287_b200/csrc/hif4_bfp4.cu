@@ -8,42 +8,53 @@ namespace {
 
 constexpr int kThreads = 256;
 
-// A warp takes the elements of 32 scale bytes or fewer: two rows' words of NVFP4 (16 lanes of 16 elements each; the words of neighbouring
-// rows are neighbours in memory) or one row's word of MXFP4 (two lanes a block).  Warps go along the rows first.
-struct WordTask { int64_t row; int word; uint32_t c; };       // c: the lane's sixteen elements within the row
+// A thread takes 32 elements: two blocks of NVFP4, one of MXFP4.  A warp takes the scale words of one place in four rows (NVFP4, eight lanes a
+// word) or two (MXFP4, sixteen lanes): the words of neighbouring rows are neighbours in memory.  Warps go along the rows first.
+// (Sixteen elements a thread: half as long again, addresses and scales cost as much as the elements.)
+struct WordTask { int64_t row; uint32_t word, c; };           // c: the lane's 32 elements within the row
 template <bool kNv>
 __device__ __forceinline__ WordTask word_task(uint32_t warp, const Divider& words, int lane) {
   const uint32_t line = words.quotient(warp), word = warp - line * words.d;
-  if (kNv) return {static_cast<int64_t>(line) * 2 + (lane >> 4), static_cast<int>(word), word * 16 + (lane & 15)};
-  return {line, static_cast<int>(word), word * 32 + lane};
+  if (kNv) return {static_cast<int64_t>(line) * 4 + (lane >> 3), word, word * 8 + (lane & 7)};
+  return {static_cast<int64_t>(line) * 2 + (lane >> 4), word, word * 16 + (lane & 15)};
+}
+// Where the lane's scale bytes are.
+template <bool kNv>
+__device__ __forceinline__ int64_t scale_offset(const WordTask& t, int64_t rows, int lane) {
+  return (t.word * rows + t.row) * 16 + (kNv ? 2 * (lane & 7) : lane & 15);
 }
 
 template <typename T, bool kNv>
 __global__ void __launch_bounds__(kThreads)
-bfp4_quantize_kernel(const T* __restrict__ src, int64_t rows, uint32_t n16, uint32_t tasks, Divider words, int64_t ld, int wide,
-                     const float* __restrict__ gain, uint2* __restrict__ codes, uint8_t* __restrict__ scales) {
+bfp4_quantize_kernel(const T* __restrict__ src, int64_t rows, uint32_t n32, uint32_t tasks, Divider words, int64_t ld, int wide,
+                     const float* __restrict__ gain, uint4* __restrict__ codes, uint8_t* __restrict__ scales) {
   const int lane = threadIdx.x & 31;
   const uint32_t warp = blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5);
   grid_wait();
   grid_launch_next();
   if (warp >= tasks) return;
   const WordTask t = word_task<kNv>(warp, words, lane);
-  const bool in = t.row < rows && t.c < n16;
-  const int64_t row = min(t.row, rows - 1);
-  const uint32_t c = min(t.c, n16 - 1);
-  const Raw16<T> raw = load_raw16(src + row * ld + 16 * static_cast<int64_t>(c), wide);
-  Sixteen v = sixteen_of(raw);
-  uint32_t peak = peak16(raw), byte;
-  if (gain) {
-    const float g = *gain;
-    scale16(v, g);
-    peak = scaled_peak(peak, g);
+  if (t.row >= rows) return;
+  uint8_t* scale = scales + scale_offset<kNv>(t, rows, lane);
+  uint32_t sa = 0u, sb = 0u;                                              // (0 past the last block)
+  if (t.c < n32) {
+    const T* p = src + t.row * ld + 32 * static_cast<int64_t>(t.c);
+    const Raw16<T> ra = load_raw16(p, wide), rb = load_raw16(p + 16, wide);
+    Sixteen a = sixteen_of(ra), b = sixteen_of(rb);
+    uint32_t pa = peak16(ra), pb = peak16(rb);
+    if (!kNv) pa = pb = max(pa, pb);
+    if (gain) {
+      const float g = *gain;
+      scale16(a, g);
+      scale16(b, g);
+      pa = scaled_peak(pa, g);
+      pb = kNv ? scaled_peak(pb, g) : pa;
+    }
+    const uint2 ca = encode16<kNv>(a, pa, sa), cb = encode16<kNv>(b, pb, sb);
+    codes[t.row * n32 + t.c] = make_uint4(ca.x, ca.y, cb.x, cb.y);
   }
-  if (!kNv) peak = max(peak, __shfl_xor_sync(0xFFFFFFFFu, peak, 1));
-  const uint2 code = encode16<kNv>(v, peak, byte);
-  if (in) codes[row * n16 + c] = code;
-  if (t.row < rows && (kNv || !(lane & 1)))                              // (0 past the last block)
-    scales[(static_cast<int64_t>(t.word) * rows + t.row) * 16 + (kNv ? lane & 15 : lane >> 1)] = static_cast<uint8_t>(in ? byte : 0u);
+  if (kNv) *reinterpret_cast<uint16_t*>(scale) = static_cast<uint16_t>(sa | (sb << 8));
+  else *scale = static_cast<uint8_t>(sa);
 }
 
 // Tile of 256 rows x 32 columns in shared memory; a thread converts 32 rows of one column.
@@ -159,20 +170,10 @@ __device__ __forceinline__ void store_words8(void* p, const uint32_t* w, bool wi
   }
 }
 
+// Sixteen codes of a block -> the row.
 template <typename T, bool kNv>
-__global__ void __launch_bounds__(kThreads)
-bfp4_dequantize_kernel(const uint2* __restrict__ codes, const uint8_t* __restrict__ scales, int64_t rows, uint32_t n16, uint32_t tasks, Divider words,
-                       const float* __restrict__ gain, T* __restrict__ dst, int64_t ld, int wide) {
-  const int lane = threadIdx.x & 31;
-  const uint32_t warp = blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5);
-  grid_wait();
-  grid_launch_next();
-  if (warp >= tasks) return;
-  const WordTask t = word_task<kNv>(warp, words, lane);
-  if (t.row >= rows || t.c >= n16) return;
-  const uint2 code = codes[t.row * n16 + t.c];
-  const float s = scale_value<kNv>(scales[(static_cast<int64_t>(t.word) * rows + t.row) * 16 + (kNv ? lane & 15 : lane >> 1)]);
-  T* p = dst + t.row * ld + 16 * static_cast<int64_t>(t.c);
+__device__ __forceinline__ void store_decoded(T* p, uint2 code, uint32_t byte, const float* gain, bool wide) {
+  const float s = scale_value<kNv>(byte);
   uint32_t w[16];
   if (sizeof(T) == 2) {
     Bf16Table table;
@@ -196,6 +197,25 @@ bfp4_dequantize_kernel(const uint2* __restrict__ codes, const uint8_t* __restric
   }
 }
 
+template <typename T, bool kNv>
+__global__ void __launch_bounds__(kThreads)
+bfp4_dequantize_kernel(const uint4* __restrict__ codes, const uint8_t* __restrict__ scales, int64_t rows, uint32_t n32, uint32_t tasks, Divider words,
+                       const float* __restrict__ gain, T* __restrict__ dst, int64_t ld, int wide) {
+  const int lane = threadIdx.x & 31;
+  const uint32_t warp = blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5);
+  grid_wait();
+  grid_launch_next();
+  if (warp >= tasks) return;
+  const WordTask t = word_task<kNv>(warp, words, lane);
+  if (t.row >= rows || t.c >= n32) return;
+  const uint4 code = codes[t.row * n32 + t.c];
+  const uint8_t* scale = scales + scale_offset<kNv>(t, rows, lane);
+  const uint32_t bytes = kNv ? *reinterpret_cast<const uint16_t*>(scale) : *scale * 0x101u;
+  T* p = dst + t.row * ld + 32 * static_cast<int64_t>(t.c);
+  store_decoded<T, kNv>(p, make_uint2(code.x, code.y), bytes & 0xFFu, gain, wide);
+  store_decoded<T, kNv>(p + 16, make_uint2(code.z, code.w), bytes >> 8, gain, wide);
+}
+
 bool format_ok(int fmt) { return fmt == HIF4_FMT_MXFP4 || fmt == HIF4_FMT_NVFP4; }
 size_t type_size(int dt) { return dt == HIF4_FP32 ? 4 : 2; }
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
@@ -217,12 +237,12 @@ extern "C" size_t hif4_bfp4_scale_bytes(int64_t rows, int64_t cols, hif4_bfp4_fo
 
 namespace {
 // Warps' tasks of a matrix (HIF4_ERR_SHAPE where they are more than 2^31).
-struct Tasks { bool ok; uint32_t n16, count, blocks; Divider words; };
+struct Tasks { bool ok; uint32_t n32, count, blocks; Divider words; };
 Tasks word_tasks(int64_t rows, int64_t cols, bool nv) {
-  const int64_t words = scale_words(cols, nv), lines = nv ? ceil_div64(rows, 2) : rows;
+  const int64_t words = scale_words(cols, nv), lines = ceil_div64(rows, nv ? 4 : 2);
   if (words > 0x7FFFFFFFll / lines) return {false, 0, 0, 0, {}};
   const int64_t count = words * lines;
-  return {true, static_cast<uint32_t>(cols / 16), static_cast<uint32_t>(count), static_cast<uint32_t>(ceil_div64(count, kThreads / 32)),
+  return {true, static_cast<uint32_t>(cols / 32), static_cast<uint32_t>(count), static_cast<uint32_t>(ceil_div64(count, kThreads / 32)),
           make_divider(static_cast<uint32_t>(words))};
 }
 int rows_wide(const void* p, int64_t ld, size_t size) { return (reinterpret_cast<uintptr_t>(p) | static_cast<uintptr_t>(ld) * size) % 32 == 0; }
@@ -230,7 +250,7 @@ template <typename T, bool kNv>
 hif4_status quantize_rows(const void* src, int64_t rows, int64_t cols, int64_t ld, const float* gain, void* codes, void* scales, cudaStream_t st) {
   const Tasks t = word_tasks(rows, cols, kNv);
   if (!t.ok) return HIF4_ERR_SHAPE;
-  return launch_overlapped(bfp4_quantize_kernel<T, kNv>, t.blocks, kThreads, 0, st, static_cast<const T*>(src), rows, t.n16, t.count, t.words, ld, rows_wide(src, ld, sizeof(T)), gain, static_cast<uint2*>(codes),
+  return launch_overlapped(bfp4_quantize_kernel<T, kNv>, t.blocks, kThreads, 0, st, static_cast<const T*>(src), rows, t.n32, t.count, t.words, ld, rows_wide(src, ld, sizeof(T)), gain, static_cast<uint4*>(codes),
                            static_cast<uint8_t*>(scales));
 }
 template <typename T, bool kNv>
@@ -243,8 +263,8 @@ template <typename T, bool kNv>
 hif4_status dequantize_rows(const void* codes, const void* scales, int64_t rows, int64_t cols, const float* gain, void* dst, int64_t ld, cudaStream_t st) {
   const Tasks t = word_tasks(rows, cols, kNv);
   if (!t.ok) return HIF4_ERR_SHAPE;
-  return launch_overlapped(bfp4_dequantize_kernel<T, kNv>, t.blocks, kThreads, 0, st, static_cast<const uint2*>(codes),
-                           static_cast<const uint8_t*>(scales), rows, t.n16, t.count, t.words, gain, static_cast<T*>(dst), ld, rows_wide(dst, ld, sizeof(T)));
+  return launch_overlapped(bfp4_dequantize_kernel<T, kNv>, t.blocks, kThreads, 0, st, static_cast<const uint4*>(codes),
+                           static_cast<const uint8_t*>(scales), rows, t.n32, t.count, t.words, gain, static_cast<T*>(dst), ld, rows_wide(dst, ld, sizeof(T)));
 }
 hif4_status check(const void* src, hif4_dtype dt, int64_t rows, int64_t cols, int64_t ld, hif4_bfp4_format fmt, const float* gain,
                   const void* codes, const void* scales) {
