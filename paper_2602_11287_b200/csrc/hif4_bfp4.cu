@@ -35,7 +35,6 @@ bfp4_quantize_kernel(const T* __restrict__ src, int64_t rows, uint32_t n32, uint
   if (warp >= tasks) return;
   const WordTask t = word_task<kNv>(warp, words, lane);
   if (t.row >= rows) return;
-  uint8_t* scale = scales + scale_offset<kNv>(t, rows, lane);
   uint32_t sa = 0u, sb = 0u;                                              // (0 past the last block)
   if (t.c < n32) {
     const T* p = src + t.row * ld + 32 * static_cast<int64_t>(t.c);
@@ -53,6 +52,7 @@ bfp4_quantize_kernel(const T* __restrict__ src, int64_t rows, uint32_t n32, uint
     const uint2 ca = encode16<kNv>(a, pa, sa), cb = encode16<kNv>(b, pb, sb);
     codes[t.row * n32 + t.c] = make_uint4(ca.x, ca.y, cb.x, cb.y);
   }
+  uint8_t* scale = scales + scale_offset<kNv>(t, rows, lane);
   if (kNv) *reinterpret_cast<uint16_t*>(scale) = static_cast<uint16_t>(sa | (sb << 8));
   else *scale = static_cast<uint8_t>(sa);
 }
@@ -107,26 +107,43 @@ bfp4_quantize_transposed_kernel(const T* __restrict__ src, int64_t rows, int64_t
 
 // Values m s of E2M1 numbers m, or m s / g, FP32.
 template <bool kNv>
-__device__ __forceinline__ void decode16(uint2 code, float s, const float* gain, float (&v)[16]) {
+__device__ __forceinline__ void decode16(uint2 code, float s, bool scaled, float gain, float (&v)[16]) {
   e2m1_to8(code.x, v);
   e2m1_to8(code.y, v + 8);
-  const float g = gain ? *gain : 1.0f;
 #pragma unroll
   for (int k = 0; k < 16; ++k) {
     v[k] = __fmul_rn(v[k], s);
-    if (gain) v[k] = __fdiv_rn(v[k], g);
+    if (scaled) v[k] = __fdiv_rn(v[k], gain);
   }
 }
 
 // The eight BF16 magnitudes of a block, as tables of low and high bytes.  Only 1 and 1.5 times a power of two occur among the E2M1
 // numbers, so the quotients s / g and 1.5 s / g and steps of their exponents make all of them.
 struct Bf16Table { uint32_t low0, low1, high0, high1; };
-__device__ __forceinline__ bool make_table(float s, const float* gain, Bf16Table& t) {
+// The gain with its reciprocal, rounded once: then a quotient within an ulp and one correction from the exact remainder is the
+// quotient rounded once (Markstein 1990, theorem on division with a correctly rounded reciprocal).  The first correction here
+// makes it that near; `fine`: far enough from both ends of FP32's range that nothing on the way leaves it.
+struct Gain { float g, y; bool given, fine; };
+__device__ __forceinline__ Gain load_gain(const float* p) {
+  Gain k{1.0f, 1.0f, p != nullptr, true};
+  if (p) {
+    k.g = *p;
+    k.y = __frcp_rn(k.g);
+    k.fine = fabsf(k.g) > 0x1p-60f && fabsf(k.g) < 0x1p60f;
+  }
+  return k;
+}
+__device__ __forceinline__ float quotient(float a, const Gain& k) {
+  if (!k.fine || a > 0x1p60f || a < 0x1p-60f) return __fdiv_rn(a, k.g);
+  float q = a * k.y;
+  q = fmaf(fmaf(-q, k.g, a), k.y, q);
+  return fmaf(fmaf(-q, k.g, a), k.y, q);
+}
+__device__ __forceinline__ bool make_table(float s, const Gain& gain, Bf16Table& t) {
   float d1 = s, d3 = 1.5f * s;
-  if (gain) {
-    const float g = *gain;
-    d1 = __fdiv_rn(d1, g);
-    d3 = __fdiv_rn(d3, g);
+  if (gain.given) {
+    d1 = quotient(d1, gain);
+    d3 = quotient(d3, gain);
   }
   const uint32_t pair = pack2(d1, d3, __nv_bfloat16());                   // 1 and 1.5
   const uint32_t exponent = (pair >> 7) & 0xFFu, sign = pair & 0x8000u;
@@ -172,7 +189,7 @@ __device__ __forceinline__ void store_words8(void* p, const uint32_t* w, bool wi
 
 // Sixteen codes of a block -> the row.
 template <typename T, bool kNv>
-__device__ __forceinline__ void store_decoded(T* p, uint2 code, uint32_t byte, const float* gain, bool wide) {
+__device__ __forceinline__ void store_decoded(T* p, uint2 code, uint32_t byte, const Gain& gain, bool wide) {
   const float s = scale_value<kNv>(byte);
   uint32_t w[16];
   if (sizeof(T) == 2) {
@@ -182,14 +199,14 @@ __device__ __forceinline__ void store_decoded(T* p, uint2 code, uint32_t byte, c
       look_up8(code.y, table, w + 4);
     } else {
       float v[16];
-      decode16<kNv>(code, s, gain, v);
+      decode16<kNv>(code, s, gain.given, gain.g, v);
 #pragma unroll
       for (int i = 0; i < 8; ++i) w[i] = pack2(v[2 * i], v[2 * i + 1], __nv_bfloat16());
     }
     store_words8(p, w, wide);
   } else {
     float v[16];
-    decode16<kNv>(code, s, gain, v);
+    decode16<kNv>(code, s, gain.given, gain.g, v);
 #pragma unroll
     for (int i = 0; i < 16; ++i) w[i] = __float_as_uint(v[i]);
     store_words8(p, w, wide);
@@ -211,9 +228,10 @@ bfp4_dequantize_kernel(const uint4* __restrict__ codes, const uint8_t* __restric
   const uint4 code = codes[t.row * n32 + t.c];
   const uint8_t* scale = scales + scale_offset<kNv>(t, rows, lane);
   const uint32_t bytes = kNv ? *reinterpret_cast<const uint16_t*>(scale) : *scale * 0x101u;
+  const Gain k = load_gain(gain);
   T* p = dst + t.row * ld + 32 * static_cast<int64_t>(t.c);
-  store_decoded<T, kNv>(p, make_uint2(code.x, code.y), bytes & 0xFFu, gain, wide);
-  store_decoded<T, kNv>(p + 16, make_uint2(code.z, code.w), bytes >> 8, gain, wide);
+  store_decoded<T, kNv>(p, make_uint2(code.x, code.y), bytes & 0xFFu, k, wide);
+  store_decoded<T, kNv>(p + 16, make_uint2(code.z, code.w), bytes >> 8, k, wide);
 }
 
 bool format_ok(int fmt) { return fmt == HIF4_FMT_MXFP4 || fmt == HIF4_FMT_NVFP4; }

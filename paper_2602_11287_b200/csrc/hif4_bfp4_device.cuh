@@ -133,9 +133,14 @@ constexpr uint32_t kInfBits = 0x7F800000u, kMostBits = 0x7F7FFFFFu;
 // Before its last rounding q is off by 2^-45 of its value at most.  For b of up to four significant bits (an E4M3 scale, 6) and a of 24 no
 // quotient lies that near to the middle between two FP32 numbers: a = m b with an odd 25-bit m would need 26 bits.  So q is a / b
 // rounded once, like __fdiv_rn, at a quarter of its instructions.
+// The remainder is exact in every rounding; rounded down, a remainder of zero is -0, which leaves the sign of q0 = -0 alone.
 __device__ __forceinline__ float2 divide2(float2 a, float2 minus_b, float2 y) {
   const float2 q0 = mul2(a, y);
-  return fma2(fma2(q0, minus_b, a), y, q0);
+  float2 r;
+  asm("{\n\t.reg .b64 a, b, c, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmov.b64 c, {%6, %7};\n\t"
+      "fma.rm.f32x2 d, a, b, c;\n\tmov.b64 {%0, %1}, d;\n\t}"
+      : "=f"(r.x), "=f"(r.y) : "f"(q0.x), "f"(q0.y), "f"(minus_b.x), "f"(minus_b.y), "f"(a.x), "f"(a.y));
+  return fma2(r, y, q0);
 }
 
 // Sixteen values of a block whose peak is given -> codes (element i in nibble i) and the block's scale byte.
@@ -162,8 +167,8 @@ __device__ __forceinline__ uint2 encode16(Sixteen v, uint32_t peak, uint32_t& by
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const float2 d = divide2(v.p[i], minus_s, y);
-      q[2 * i] = __uint_as_float(__float_as_uint(d.x) | (__float_as_uint(v.p[i].x) & 0x80000000u));        // -0 keeps its sign
-      q[2 * i + 1] = __uint_as_float(__float_as_uint(d.y) | (__float_as_uint(v.p[i].y) & 0x80000000u));
+      q[2 * i] = d.x;
+      q[2 * i + 1] = d.y;
     }
   } else {
     const int e = max(static_cast<int>(peak >> 23) - 127 - 2, -127);     // floor(log2 peak) - 2; infinity: 126

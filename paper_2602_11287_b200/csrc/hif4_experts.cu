@@ -274,10 +274,10 @@ combine_kernel(Gather g, const TI* __restrict__ in, int64_t ld_in, const float* 
   store_vec(y + t * ld_y + c, acc);
 }
 
-// A block goes over a token's row, four assignments at a time, whose rows are loaded together.
-constexpr int kTogether = 4;
+// A block goes over a token's row, eight assignments at a time, whose rows are loaded together.
+constexpr int kTogether = 8;
 template <typename TD, typename TI, int kVec>
-__global__ void __launch_bounds__(kThreads, 4)
+__global__ void __launch_bounds__(kThreads, 3)
 combine_backward_kernel(Gather g, const TD* __restrict__ dy, int64_t ld_dy, const float* __restrict__ weights, const TI* __restrict__ in,
                         int64_t ld_in, TI* __restrict__ din, int64_t ld_din, float* __restrict__ dweights) {
   __shared__ float sums[kThreads / 32][kTogether];
@@ -297,7 +297,6 @@ combine_backward_kernel(Gather g, const TD* __restrict__ dy, int64_t ld_dy, cons
       acc[j] = 0.0f;
     }
     for (int64_t c = static_cast<int64_t>(threadIdx.x) * kVec; c < g.cols; c += blockDim.x * kVec) {
-      float d[kVec], v[kVec];
       if constexpr (kVec == 8) {
         const Raw8<TD> raw_d = load8(dy + t * ld_dy + c);
         Raw8<TI> raw[kTogether];
@@ -306,31 +305,35 @@ combine_backward_kernel(Gather g, const TD* __restrict__ dy, int64_t ld_dy, cons
           for (int j = 0; j < kTogether; ++j)
             if (row[j] >= 0) raw[j] = load8(in + row[j] * ld_in + c);
         }
-        unpack8(raw_d, d);
+        const Pairs d = pairs_of(raw_d);
         if (dweights) {
 #pragma unroll
           for (int j = 0; j < kTogether; ++j) {
             if (row[j] < 0) continue;
-            unpack8(raw[j], v);
+            const Pairs v = pairs_of(raw[j]);
+            float2 part = mul2(d.p[0], v.p[0]);
 #pragma unroll
-            for (int i = 0; i < kVec; ++i) acc[j] = fmaf(d[i], v[i], acc[j]);
+            for (int i = 1; i < 4; ++i) part = fma2(d.p[i], v.p[i], part);
+            acc[j] += part.x + part.y;
+          }
+        }
+        if (din) {
+#pragma unroll
+          for (int j = 0; j < kTogether; ++j) {
+            if (row[j] < 0) continue;
+            Pairs v;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v.p[i] = mul2(both(w[j]), d.p[i]);
+            store8(din + row[j] * ld_din + c, raw_of<TI>(v));
           }
         }
       } else {
-        d[0] = to_f32(dy[t * ld_dy + c]);
-        if (dweights) {
-#pragma unroll
-          for (int j = 0; j < kTogether; ++j)
-            if (row[j] >= 0) acc[j] = fmaf(d[0], to_f32(in[row[j] * ld_in + c]), acc[j]);
-        }
-      }
-      if (din) {
+        const float d = to_f32(dy[t * ld_dy + c]);
 #pragma unroll
         for (int j = 0; j < kTogether; ++j) {
           if (row[j] < 0) continue;
-#pragma unroll
-          for (int i = 0; i < kVec; ++i) v[i] = __fmul_rn(w[j], d[i]);
-          store_vec(din + row[j] * ld_din + c, v);
+          if (dweights) acc[j] = fmaf(d, to_f32(in[row[j] * ld_in + c]), acc[j]);
+          if (din) din[row[j] * ld_din + c] = from_f32<TI>(__fmul_rn(w[j], d));
         }
       }
     }
@@ -349,6 +352,75 @@ combine_backward_kernel(Gather g, const TD* __restrict__ dy, int64_t ld_dy, cons
       }
       __syncthreads();
     }
+  }
+}
+
+// A warp goes over the row of one assignment, `kAtOnce` loads of both operands at a time: no barrier, and the warps of a token read
+// its gradient from L1 after the first.
+constexpr int kAtOnce = 4;
+template <typename TD, typename TI, int kVec>
+__global__ void __launch_bounds__(kThreads)
+combine_backward_rows_kernel(Gather g, int64_t assignments, const TD* __restrict__ dy, int64_t ld_dy, const float* __restrict__ weights,
+                             const TI* __restrict__ in, int64_t ld_in, TI* __restrict__ din, int64_t ld_din, float* __restrict__ dweights) {
+  const int lane = threadIdx.x & 31;
+  const int64_t a = static_cast<int64_t>(blockIdx.x) * (kThreads / 32) + (threadIdx.x >> 5);
+  grid_wait();
+  grid_launch_next();
+  if (a >= assignments) return;
+  const int row = g.row_of[a];
+  float acc = 0.0f;
+  if (has_row(row, g.rows)) {
+    const float w = weights ? weights[a] : 1.0f;
+    const TD* d_row = dy + (a / g.top_k) * ld_dy;
+    const TI* in_row = in + row * ld_in;
+    TI* out = din + row * ld_din;
+    for (int64_t c0 = lane * kVec; c0 < g.cols; c0 += kAtOnce * 32 * kVec) {
+      if constexpr (kVec == 8) {
+        Raw8<TD> rd[kAtOnce];
+        Raw8<TI> rv[kAtOnce];
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) {
+          const int64_t c = c0 + u * 32 * kVec;
+          if (c < g.cols) {
+            rd[u] = load8(d_row + c);
+            if (dweights) rv[u] = load8(in_row + c);
+          }
+        }
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) {
+          const int64_t c = c0 + u * 32 * kVec;
+          if (c >= g.cols) continue;
+          const Pairs d = pairs_of(rd[u]);
+          if (dweights) {
+            const Pairs v = pairs_of(rv[u]);
+            float2 part = mul2(d.p[0], v.p[0]);
+#pragma unroll
+            for (int i = 1; i < 4; ++i) part = fma2(d.p[i], v.p[i], part);
+            acc += part.x + part.y;
+          }
+          if (din) {
+            Pairs v;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v.p[i] = mul2(both(w), d.p[i]);
+            store8(out + c, raw_of<TI>(v));
+          }
+        }
+      } else {
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) {
+          const int64_t c = c0 + u * 32;
+          if (c >= g.cols) continue;
+          const float d = to_f32(d_row[c]);
+          if (dweights) acc = fmaf(d, to_f32(in_row[c]), acc);
+          if (din) out[c] = from_f32<TI>(__fmul_rn(w, d));
+        }
+      }
+    }
+  }
+  if (dweights) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) acc += __shfl_xor_sync(kAll, acc, o);
+    if (lane == 0) dweights[a] = acc;
   }
 }
 
@@ -416,6 +488,12 @@ hif4_status launch_combine_backward(const hif4_combine_backward_args& a, cudaStr
   int64_t blocks = 0;
   const hif4_status s = make_gather(g, a.tokens, a.cols, a.top_k, a.rows, a.row_of, a.cols > 0 ? a.cols : 1, &blocks);
   if (s != HIF4_OK) return s;
+  // a warp a row where there are enough of them for all SMs, else a block a token
+  const int64_t assignments = a.tokens * a.top_k;
+  if (assignments >= 8ll * sm_count())
+    return launch_overlapped(vec ? combine_backward_rows_kernel<TD, TI, 8> : combine_backward_rows_kernel<TD, TI, 1>,
+                             static_cast<unsigned>(ceil_div64(assignments, kThreads / 32)), kThreads, 0, st, g, assignments, static_cast<const TD*>(a.dy),
+                             a.ld_dy, a.weights, static_cast<const TI*>(a.in), a.ld_in, static_cast<TI*>(a.din), a.ld_din, a.dweights);
   // as many threads as go over the row in equal rounds
   const int64_t words = ceil_div64(a.cols > 0 ? a.cols : 1, vec ? 8 : 1), rounds = ceil_div64(words, kThreads);
   const unsigned threads = static_cast<unsigned>(ceil_div64(ceil_div64(words, rounds), 32) * 32);

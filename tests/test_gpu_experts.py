@@ -288,7 +288,7 @@ def test_rows_outside_the_output_are_left_out(hif4):
 TYPES = [torch.bfloat16, torch.float16, torch.float32]
 
 
-@pytest.mark.parametrize("T,k,K,pad", [(1, 8, 7168, 0), (1, 1, 1, 0), (40, 6, 2056, 0), (33, 9, 1001, 0), (200, 4, 64, 8), (50, 32, 320, 3)])
+@pytest.mark.parametrize("T,k,K,pad", [(1, 8, 7168, 0), (1, 1, 1, 0), (40, 6, 2056, 0), (33, 9, 1001, 0), (200, 4, 64, 8), (50, 32, 320, 3), (700, 3, 2056, 0), (300, 5, 777, 0)])
 @pytest.mark.parametrize("dt_in", TYPES)
 @pytest.mark.parametrize("dt", TYPES)
 def test_combine_and_its_gradient(hif4, T, k, K, pad, dt_in, dt):
