@@ -32,9 +32,9 @@ template <int T> struct Shape {
   static_assert(T * BW * 4 <= kStages * kCodeBytes, "sums of a cluster");
 };
 
-__device__ __forceinline__ float ld_cluster_f32(uint32_t addr) {
-  float v;
-  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
+__device__ __forceinline__ float4 ld_cluster_f32x4(uint32_t addr) {
+  float4 v;
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr));
   return v;
 }
 
@@ -207,12 +207,22 @@ bfp4_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant_
     cluster_sync_all();
     if (group >= 0) {
       const float alpha = p.alpha ? p.alpha[p.num_groups ? group : 0] : 1.0f;
-      const int c0 = static_cast<int>(T * rank / ranks), c1 = static_cast<int>(T * (rank + 1) / ranks);
-      const int64_t n = n0 + (threadIdx.x & (BW - 1));
-      for (int c = c0 + static_cast<int>(threadIdx.x) / BW; c < c1 && m0 + c < m_end; c += kThreads / BW) {
-        float v = 0.0f;
-        for (uint32_t r = 0; r < ranks; ++r) v += ld_cluster_f32(mapa(smem + (c * BW + (threadIdx.x & (BW - 1))) * 4, r));
-        if (n < p.N) store_y(p, m0 + c, n, alpha * v);
+      // four columns of Y a thread: all CTAs' sums are on their way before the first is added
+      const int c0 = static_cast<int>(T * rank / ranks), c1 = static_cast<int>(T * (rank + 1) / ranks), at = (threadIdx.x & 31) * 4;
+      const int64_t n = n0 + at;
+      for (int c = c0 + warp; c < c1 && m0 + c < m_end; c += kThreads / 32) {
+        float4 part[8];
+#pragma unroll
+        for (uint32_t r = 0; r < 8; ++r)
+          if (r < ranks) part[r] = ld_cluster_f32x4(mapa(smem + (c * BW + at) * 4, r));
+        float4 v = part[0];
+#pragma unroll
+        for (uint32_t r = 1; r < 8; ++r)
+          if (r < ranks) { v.x += part[r].x; v.y += part[r].y; v.z += part[r].z; v.w += part[r].w; }
+        const float out[4] = {alpha * v.x, alpha * v.y, alpha * v.z, alpha * v.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (n + i < p.N) store_y(p, m0 + c, n + i, out[i]);
       }
     }
     cluster_sync_all();
@@ -293,8 +303,12 @@ hif4_status product(const hif4_bfp4_gemm_args& a, bool grouped, void* stream) {
   p.offsets = a.group_offsets;
   p.error_word = device_error_word();
   if (!p.error_word) return HIF4_ERR_CUDA;
-  // Prompts: 256 x 256 tiles on CTA pairs as soon as there are enough of them
-  if (!grouped && a.M > 128 && ceil_div64(a.M, 256) * ceil_div64(a.N, 256) * 4 >= sm_count()) return launch_bfp4_pairs(a, p, st);
+  // More than 64 tokens: 256 x 256 tiles on CTA pairs, unless few tiles have many chunks, which a cluster shares out here and one pair
+  // has to walk alone, or so few that its longer start is not made up.  Pairs / clusters, us: 512 x 4096 x 4096 10.9 / 12.4,
+  // 128 x 14336 x 4096 11.4 / 12.5, 256 x 4096 x 14336 22.1 / 16.4, 512 x 4096 x 14336 22.8 / 22.9, 2048 x 512 x 512 6.5 / 5.4;
+  // 64 x 4096 x 4096 9.9 / 8.4.
+  if (!grouped && a.M > 64 && p.chunks > 2 && (p.chunks <= 16 || ceil_div64(a.M, 256) * ceil_div64(a.N, 256) * 4 >= sm_count()))
+    return launch_bfp4_pairs(a, p, st);
   if (grouped && a.num_groups <= kMaxTableGroups) return launch_bfp4_grouped(a, p, st);
   // tokens of a tile: the fewest that hold the rows of a (mean) group, at most 128
   const int64_t mean = grouped ? ceil_div64(a.M, a.num_groups) : a.M;
