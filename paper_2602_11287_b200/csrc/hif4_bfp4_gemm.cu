@@ -301,6 +301,8 @@ hif4_status product(const hif4_bfp4_gemm_args& a, bool grouped, void* stream) {
   p.y = a.Y; p.ld_y = a.ld_y; p.dt = a.dt;
   p.num_groups = grouped ? a.num_groups : 0;
   p.offsets = a.group_offsets;
+  hif4_bfp4_gemm_args b = a;
+  b.num_groups = grouped ? a.num_groups : 0;
   p.error_word = device_error_word();
   if (!p.error_word) return HIF4_ERR_CUDA;
   // More than 64 tokens: 256 x 256 tiles on CTA pairs, unless few tiles have many chunks, which a cluster shares out here and one pair
@@ -308,14 +310,15 @@ hif4_status product(const hif4_bfp4_gemm_args& a, bool grouped, void* stream) {
   // 128 x 14336 x 4096 11.4 / 12.5, 256 x 4096 x 14336 22.1 / 16.4, 512 x 4096 x 14336 22.8 / 22.9, 2048 x 512 x 512 6.5 / 5.4;
   // 64 x 4096 x 4096 9.9 / 8.4.
   if (!grouped && a.M > 64 && p.chunks > 2 && (p.chunks <= 16 || ceil_div64(a.M, 256) * ceil_div64(a.N, 256) * 4 >= sm_count()))
-    return launch_bfp4_pairs(a, p, st);
-  if (grouped && a.num_groups <= kMaxTableGroups) return launch_bfp4_grouped(a, p, st);
+    return launch_bfp4_pairs(b, p, st);
+  // Groups (this kernel takes any number of them): pairs where a mean group fills more than half of their 256 rows.  Pairs / one CTA, us,
+  // 32 groups of 2048 -> 7168: 4096 rows 69.5 / 66.0, 6144 79.8 / 83.6, 8192 92 / 108, 16384 153 / 183.
+  if (grouped && a.num_groups <= kMaxTableGroups)
+    return ceil_div64(a.M, a.num_groups) > 128 ? launch_bfp4_pairs(b, p, st) : launch_bfp4_grouped(b, p, st);
   // tokens of a tile: the fewest that hold the rows of a (mean) group, at most 128
   const int64_t mean = grouped ? ceil_div64(a.M, a.num_groups) : a.M;
   const int T = mean <= 16 ? 16 : mean <= 32 ? 32 : mean <= 64 ? 64 : 128;
   const int64_t m_tiles = ceil_div64(a.M, T) + (grouped ? a.num_groups : 0);
-  hif4_bfp4_gemm_args b = a;
-  b.num_groups = grouped ? a.num_groups : 0;
   switch (T) {
     case 16: return nv ? launch_tiles<16, true>(b, p, m_tiles, st) : launch_tiles<16, false>(b, p, m_tiles, st);
     case 32: return nv ? launch_tiles<32, true>(b, p, m_tiles, st) : launch_tiles<32, false>(b, p, m_tiles, st);

@@ -1,4 +1,4 @@
-// CTA-pair form of the block-scaled product for prompts: a cluster of two CTAs on 256 tokens x 256 rows of B
+// CTA-pair form of the block-scaled product for prompts and large groups: a cluster of two CTAs on 256 tokens x 256 rows of B
 // (tcgen05.mma.cta_group::2), persistent over its tiles.  Each CTA holds its 128 tokens and 128 of the rows of B, so an SM reads
 // 8 KB from L2 for a K = 64 step of 128 x 256 outputs; it needs the scales of all 256 rows of B, though.
 //
@@ -21,7 +21,8 @@ constexpr int kSfBytes = (kHalf + kTile) * 16;
 constexpr int kSlabBytes = 32 * 128;         // 32 rows x 128 bytes of Y, one per epilogue warp, in SWIZZLE_128B order
 constexpr int kSlabs = kStages * kCodeBytes;
 constexpr int kSf = kSlabs + 8 * kSlabBytes;
-constexpr int kBars = kSf + kSfStages * kSfBytes;
+constexpr int kTable = kSf + kSfStages * kSfBytes;
+constexpr int kBars = kTable + kGroupTableBytes;
 constexpr int kSmem = 1024 + kBars + 512;
 constexpr int kSfCols = 48;                  // of a stage: 16 for the tokens, 32 for B
 constexpr int kTmemCols = 512;
@@ -29,12 +30,18 @@ constexpr int kBand = 16;                    // token tiles that are walked toge
 static_assert(kTile + kStages * kSfCols <= kTmemCols, "TMEM");
 static_assert(kSmem <= 227 * 1024, "shared memory");
 
-struct PairTile { int m0, n0; };
-__device__ __forceinline__ PairTile pair_tile(const Bfp4Params& p, int t) {
+// Tile t of a dense product (bands of token tiles, within a band the token tiles of the same rows of B) or of a grouped one.
+struct PairTile { int group, m0, m_end, n0; };
+template <bool kGrouped>
+__device__ __forceinline__ PairTile pair_tile(const GroupTable& table, const Bfp4Params& p, int t) {
+  if (kGrouped) {
+    const GroupTile w = group_tile(table, p, t, kTile);
+    return {w.group, w.m0, w.m_end, w.nt * kTile};
+  }
   const int band_tiles = kBand * p.n_tiles, band = t / band_tiles, in = t - band * band_tiles;
   const int rows = min(kBand, p.m_tiles - band * kBand);
   const int nt = in / rows, mt = band * kBand + in - nt * rows;
-  return {mt * kTile, nt * kTile};
+  return {0, mt * kTile, static_cast<int>(p.M), nt * kTile};
 }
 
 // Y is written once and larger than what the codes leave of L2: its lines are the first to go.
@@ -62,7 +69,7 @@ __device__ __forceinline__ void store_slab(const CUtensorMap* map, int x, int y,
   }
 }
 
-template <bool kNv>
+template <bool kNv, bool kGrouped>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 bfp4_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const __grid_constant__ CUtensorMap tmY,
                  const __grid_constant__ Bfp4Params p) {
@@ -78,7 +85,8 @@ bfp4_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant_
   volatile uint32_t* abort_flag = tmem_slot + 1;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = cluster_ctarank();
-  const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1, tiles = p.m_tiles * p.n_tiles;
+  const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
+  GroupTable& table = *reinterpret_cast<GroupTable*>(gen + kTable);
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < kStages; ++s) {
@@ -99,13 +107,15 @@ bfp4_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant_
     asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(slot), "r"(kTmemCols) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
   }
+  grid_wait();
+  grid_launch_next();
+  if (kGrouped && warp == 3) build_group_table(table, p, kTile, lane);
   tc_fence_before();
   __syncthreads();
   cluster_sync_all();
-  grid_wait();
-  grid_launch_next();
   tc_fence_after();
   const uint32_t tmem = *tmem_slot, sf_cols = tmem + kTile;
+  const int tiles = (kGrouped ? table.tiles[p.num_groups] : p.m_tiles) * p.n_tiles;
 
   if (warp == 0) {
     if (lane == 0) {
@@ -113,8 +123,8 @@ bfp4_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant_
       uint32_t ph = 1u;
       bool ok = true;
       for (int t = pair; t < tiles && ok; t += pairs) {
-        const PairTile w = pair_tile(p, t);
-        const int m0 = w.m0 + static_cast<int>(rank) * kHalf, n0 = w.n0 + static_cast<int>(rank) * kHalf;
+        const PairTile w = pair_tile<kGrouped>(table, p, t);
+        const int m0 = w.m0 + static_cast<int>(rank) * kHalf, n0 = static_cast<int>(w.group * p.N + w.n0) + static_cast<int>(rank) * kHalf;
         for (int k = 0; k < p.chunks; ++k) {
           if (!(ok = mbar_wait(empty + 8 * s, ph, abort_flag))) break;
           const uint32_t bar = full + 8 * s, at = smem + s * kCodeBytes;
@@ -131,11 +141,11 @@ bfp4_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant_
       uint32_t ph = 1u;
       bool ok = true;
       for (int t = pair; t < tiles && ok; t += pairs) {
-        const PairTile w = pair_tile(p, t);
+        const PairTile w = pair_tile<kGrouped>(table, p, t);
         const int m0 = w.m0 + static_cast<int>(rank) * kHalf;
         const uint32_t sf_a = static_cast<uint32_t>(max(static_cast<int64_t>(0), min(static_cast<int64_t>(kHalf), p.M - m0))) * 16u;
         const uint32_t sf_b = static_cast<uint32_t>(min(static_cast<int64_t>(kTile), p.N - w.n0)) * 16u;
-        const uint8_t *a_sf = p.a_scales + static_cast<int64_t>(m0) * 16, *b_sf = p.b_scales + static_cast<int64_t>(w.n0) * 16;
+        const uint8_t *a_sf = p.a_scales + static_cast<int64_t>(m0) * 16, *b_sf = p.b_scales + w.group * p.b_scale_group + static_cast<int64_t>(w.n0) * 16;
         for (int k = 0; k < p.chunks; ++k) {
           if (!(ok = mbar_wait(sf_empty + 8 * z, ph, abort_flag))) break;
           const uint32_t bar = sf_full + 8 * z, sfs = sf + z * kSfBytes;
@@ -221,17 +231,17 @@ bfp4_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant_
   } else if (warp >= 8) {
     const int q = warp & 3, c0 = (warp >= 12 ? kHalf : 0);
     const uint32_t acc = tmem + (static_cast<uint32_t>(q * 32) << 16) + c0, empty_leader = mapa(acc_empty, 0);
-    const float alpha = p.alpha ? *p.alpha : 1.0f;
     const uint32_t slab = smem + kSlabs + (warp - 8) * kSlabBytes;
     const uint64_t policy = evict_first_policy();
     uint32_t ph = 0u;
     for (int t = pair; t < tiles; t += pairs) {
-      const PairTile w = pair_tile(p, t);
+      const PairTile w = pair_tile<kGrouped>(table, p, t);
       if (!__all_sync(0xFFFFFFFFu, mbar_wait(acc_full, ph, abort_flag, 64))) break;
       ph ^= 1u;
       tc_fence_after();
       const int m = w.m0 + static_cast<int>(rank) * kHalf + q * 32, n = w.n0 + c0;       // the warp's first row and column
-      const bool inside = m < p.M && n < p.N;
+      const bool inside = m < w.m_end && n < p.N, boxes = !kGrouped || m + 32 <= w.m_end;      // (a box would reach into the next group)
+      const float alpha = p.alpha ? p.alpha[w.group] : 1.0f;
       if (p.tma_store && p.dt != HIF4_FP32) {
         uint32_t packed[64];
 #pragma unroll
@@ -248,8 +258,15 @@ bfp4_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant_
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive_cluster(empty_leader);
-        if (inside) store_slab(&tmY, n, m, slab, packed, lane, policy);
-        if (inside && n + 64 < p.N) store_slab(&tmY, n + 64, m, slab, packed + 32, lane, policy);
+        if (boxes) {
+          if (inside) store_slab(&tmY, n, m, slab, packed, lane, policy);
+          if (inside && n + 64 < p.N) store_slab(&tmY, n + 64, m, slab, packed + 32, lane, policy);
+        } else if (m + lane < w.m_end) {
+          uint16_t* row = static_cast<uint16_t*>(p.y) + (m + lane) * p.ld_y + n;
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            if (n + 8 * i < p.N) reinterpret_cast<uint4*>(row)[i] = make_uint4(packed[4 * i], packed[4 * i + 1], packed[4 * i + 2], packed[4 * i + 3]);
+        }
       } else {
         for (int c = 0; c < 4; ++c) {
           uint32_t r[32];
@@ -257,9 +274,9 @@ bfp4_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant_
           tc_wait_ld();
 #pragma unroll
           for (int i = 0; i < 32; ++i) r[i] = __float_as_uint(alpha * __uint_as_float(r[i]));
-          if (p.tma_store) {
+          if (p.tma_store && boxes) {
             if (inside && n + 32 * c < p.N) store_slab(&tmY, n + 32 * c, m, slab, r, lane, policy);
-          } else if (m + lane < p.M) {
+          } else if (m + lane < w.m_end) {
 #pragma unroll
             for (int i = 0; i < 32; ++i)
               if (n + 32 * c + i < p.N) store_y(p, m + lane, n + 32 * c + i, __uint_as_float(r[i]));
@@ -289,28 +306,30 @@ bfp4_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant_
   }
 }
 
-template <bool kNv>
+template <bool kNv, bool kGrouped>
 hif4_status launch_pairs(const hif4_bfp4_gemm_args& a, Bfp4Params p, cudaStream_t st) {
   static uint64_t ready = 0;
-  if (!ensure_dynamic_smem(bfp4_pair_kernel<kNv>, kSmem, ready)) return HIF4_ERR_CUDA;
+  if (!ensure_dynamic_smem(bfp4_pair_kernel<kNv, kGrouped>, kSmem, ready)) return HIF4_ERR_CUDA;
   CUtensorMap tmA, tmB, tmY;
-  if (!make_code_map(&tmA, a.A_codes, a.M, a.K, kHalf) || !make_code_map(&tmB, a.B_codes, a.N, a.K, kHalf)) return HIF4_ERR_CUDA;
+  if (!make_code_map(&tmA, a.A_codes, a.M, a.K, kHalf) || !make_code_map(&tmB, a.B_codes, a.N * (kGrouped ? a.num_groups : 1), a.K, kHalf)) return HIF4_ERR_CUDA;
   // (a TMA store clips the innermost dimension in 16-byte pieces, so a row's length has to be whole ones)
   const int64_t size = a.dt == HIF4_FP32 ? 4 : 2;
   p.tma_store = (reinterpret_cast<uintptr_t>(a.Y) & 15u) == 0 && a.ld_y * size % 16 == 0 && a.N * size % 16 == 0 && make_y_map(&tmY, a, static_cast<int>(128 / size), 32, CU_TENSOR_MAP_SWIZZLE_128B);
   if (!p.tma_store) tmY = tmA;                           // not used
-  const int64_t m_tiles = ceil_div64(a.M, kTile), n_tiles = ceil_div64(a.N, kTile);
+  const int64_t m_tiles = ceil_div64(a.M, kTile) + (kGrouped ? a.num_groups : 0), n_tiles = ceil_div64(a.N, kTile);
   if (m_tiles * n_tiles > 0x7FFFFFFFll - 1024 || n_tiles > 0x7FFFFFFFll / kBand) return HIF4_ERR_SHAPE;
   p.m_tiles = static_cast<int>(m_tiles);
   p.n_tiles = static_cast<int>(n_tiles);
   const int most = sm_count() / 2, tiles = p.m_tiles * p.n_tiles;
-  return launch_overlapped(bfp4_pair_kernel<kNv>, static_cast<unsigned>(2 * (tiles < most ? tiles : most)), kThreads, kSmem, st, tmA, tmB, tmY, p);
+  return launch_overlapped(bfp4_pair_kernel<kNv, kGrouped>, static_cast<unsigned>(2 * (tiles < most ? tiles : most)), kThreads, kSmem, st, tmA, tmB, tmY, p);
 }
 
 }  // namespace
 
 hif4_status launch_bfp4_pairs(const hif4_bfp4_gemm_args& a, Bfp4Params p, cudaStream_t st) {
-  return a.fmt == HIF4_FMT_NVFP4 ? launch_pairs<true>(a, p, st) : launch_pairs<false>(a, p, st);
+  const bool nv = a.fmt == HIF4_FMT_NVFP4;
+  if (a.num_groups > 0) return nv ? launch_pairs<true, true>(a, p, st) : launch_pairs<false, true>(a, p, st);
+  return nv ? launch_pairs<true, false>(a, p, st) : launch_pairs<false, false>(a, p, st);
 }
 
 }  // namespace hif4

@@ -118,7 +118,8 @@ def check_product(y, a, b, scale=1.0):
 
 
 SIZES = [(1, 1, 64), (1, 8, 128), (1, 300, 256), (2, 129, 320), (7, 128, 512), (16, 256, 576), (17, 513, 1024), (33, 64, 2048),
-         (64, 1000, 4096), (65, 130, 192), (128, 384, 1088), (129, 257, 768), (300, 200, 8256), (513, 777, 320), (1024, 512, 1024)]
+         (64, 1000, 4096), (65, 130, 192), (128, 384, 1088), (129, 257, 768), (300, 200, 8256), (513, 777, 320), (1024, 512, 1024),
+         (200, 1, 1024), (70, 9, 2048), (66, 40, 4096)]
 
 
 @pytest.mark.parametrize("fmt", [MX, NV])
@@ -190,7 +191,7 @@ def test_product_into_a_view(hif4, M):
 @pytest.mark.parametrize("fmt", [MX, NV])
 @pytest.mark.parametrize("counts,N,K", [([3], 100, 64), ([0, 1, 0, 0, 17, 0], 130, 320), ([40, 0, 129, 1, 300], 257, 512), ([5] * 40, 128, 1024),
                                         ([0, 0], 64, 128), ([600, 1, 1], 320, 2112),
-                                        ([20, 0, 70, 33, 64, 1], 520, 4096), ([1, 2, 0] * 100, 64, 320), ([7] * 256, 130, 576)])
+                                        ([20, 0, 70, 33, 64, 1], 520, 4096), ([700, 0, 333, 1], 520, 320), ([256, 512, 17], 300, 1088), ([1000, 31], 257, 128), ([1, 2, 0] * 100, 64, 320), ([7] * 256, 130, 576)])
 def test_grouped_product(hif4, fmt, counts, N, K):
     g = gen(sum(counts) + N)
     G, used = len(counts), sum(counts)
