@@ -449,3 +449,83 @@ def test_a_layer_in_a_graph_on_another_stream(hif4):
         logits.copy_(torch.randn(100, E, generator=gen(seed + 9), device="cuda"))
         graph.replay()
         assert torch.equal(y, layer(x, logits))
+
+
+@pytest.mark.parametrize("T", [1, 150])
+@pytest.mark.parametrize("fmt", [1, 2])
+def test_training_step_of_a_layer(hif4, T, fmt):
+    """Forward and backward of routing, rows, grouped product and combination, every gradient call fed by the one before: against the
+    formulas in 64 bits on the operands as converted.  (Conversions are passed straight through.)"""
+    g = gen(T + fmt)
+    E, k, K, N = 10, 2, 192, 256
+    rnd = lambda *s: torch.randn(*s, generator=g, device="cuda").to(torch.bfloat16)      # noqa: E731
+    x, w, dout, logits = rnd(T, K), rnd(E * N, K) / 8, rnd(T, N), torch.randn(T, E, generator=g, device="cuda")
+    V = lambda q: ref.values(*q, fmt)      # noqa: E731
+
+    def grouped(v, rows):
+        c, s = hif4.hif4_bfp4_quantize(v.contiguous(), fmt)
+        return c.view(E, rows, -1), s.view(s.shape[0], E, rows, 16).transpose(0, 1).contiguous()
+    weights = grouped(w, N)                                              # laid out once: rows for the product, columns for its gradient
+    turned = [hif4.hif4_bfp4_quantize_transposed(e, fmt) for e in w.view(E, N, K)]
+    columns = torch.stack([c for c, _ in turned]), torch.stack([s for _, s in turned])
+    ids, p = hif4.hif4_route(logits, k)
+    off, row_of = hif4.hif4_expert_plan(ids, E)
+    rows = hif4.hif4_dispatch(x, row_of, fmt=fmt)
+    y = hif4.hif4_bfp4_grouped_gemm(rows, weights, off, fmt, dtype=torch.float32)
+    out = hif4.hif4_combine(y, row_of, p, dtype=torch.bfloat16)
+    dy, dp = hif4.hif4_combine_backward(dout, row_of, p, rows=y)
+    drows = hif4.hif4_bfp4_grouped_gemm(hif4.hif4_bfp4_quantize(dy, fmt), columns, off, fmt, dtype=torch.float32)
+    dx = hif4.hif4_combine(drows, row_of, dtype=torch.bfloat16)
+    dlogits = hif4.hif4_route_backward(dp, logits, ids)
+    # the same with the converted operands
+    X, W, WT = V(hif4.hif4_bfp4_quantize(x, fmt)), V(weights), V(columns).transpose(1, 2)
+    at = ids.long()
+    l64 = logits.double().requires_grad_()
+    P = torch.softmax(l64.gather(1, at), 1)
+    Y = torch.einsum("tkno,to->tkn", W[at], X)
+    dY = V(hif4.hif4_bfp4_quantize(dy, fmt))[row_of.long()]
+    want = {"out": (P.unsqueeze(-1) * Y).sum(1), "dp": (dout.double().unsqueeze(1) * Y).sum(-1),
+            "dx": torch.einsum("tkn,tkno->to", dY, WT[at])}
+    want["dlogits"], = torch.autograd.grad(P, l64, want["dp"].detach())
+    size = {"out": (Y.abs()).sum(1), "dp": (dout.double().abs().unsqueeze(1) * Y.abs()).sum(-1), "dx": torch.einsum("tkn,tkno->to", dY.abs(), WT[at].abs())}
+    size["dlogits"] = size["dp"].amax(1, keepdim=True)
+    for name, got, roundings in (("out", out, 2.0 ** -8), ("dp", dp, 0.0), ("dx", dx, 2.0 ** -8), ("dlogits", dlogits, 0.0)):
+        ref64 = want[name].detach()
+        # a product's FP32 sums: 1e-5 of the terms; the combinations after it add fewer; one rounding to BF16
+        assert bool(((got.double() - ref64).abs() <= roundings * ref64.abs() + 3e-5 * size[name].detach()).all()), name
+    # rounded to the type of the experts' rows (FP32): the weight times the token's gradient
+    assert torch.equal(dy[row_of.long()], p.unsqueeze(-1) * dout.float().unsqueeze(1))
+
+
+def test_plan_workspaces(hif4):
+    ids = torch.randint(0, 64, (3000, 2), device="cuda", dtype=torch.int32)
+    need = hif4.hif4_expert_plan_workspace(3000, 2, 64)
+    want = hif4.hif4_expert_plan(ids, 64)
+    got = hif4.hif4_expert_plan(ids, 64, workspace=torch.empty(need, dtype=torch.uint8, device="cuda"))
+    assert need > 0 and torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    for space, code in ((torch.empty(need - 1, dtype=torch.uint8, device="cuda"), 5), (torch.empty(need + 64, dtype=torch.uint8, device="cuda")[64:], 3)):
+        with pytest.raises(hif4.Hif4Error) as e:
+            hif4.hif4_expert_plan(ids, 64, workspace=space)
+        assert e.value.code == code
+    with pytest.raises(ValueError):
+        hif4.hif4_expert_plan(ids, 64, workspace=torch.empty(1, dtype=torch.uint8, device="cuda").expand(need))
+
+
+def test_calls_on_a_stream_of_their_own(hif4):
+    """stream=: the call and its allocations belong to that stream; two streams at once keep out of each other's way."""
+    x, logits = torch.randn(500, 256, device="cuda").to(torch.bfloat16), torch.randn(500, 40, device="cuda")
+    c, s = hif4.hif4_bfp4_quantize(torch.randn(40 * 128, 256, device="cuda").to(torch.bfloat16), 2)
+    b = c.view(40, 128, -1), s.view(-1, 40, 128, 16).transpose(0, 1).contiguous()
+
+    def layer(st):
+        ids, w = hif4.hif4_route(logits, 6, stream=st)
+        off, row_of = hif4.hif4_expert_plan(ids, 40, stream=st)
+        rows = hif4.hif4_dispatch(x, row_of, fmt=2, stream=st)
+        y = hif4.hif4_bfp4_grouped_gemm(rows, b, off, 2, stream=st)
+        return hif4.hif4_combine(y, row_of, w, stream=st)
+    want = layer(None)
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    got = [layer(st) for _ in range(4) for st in streams]
+    torch.cuda.synchronize()
+    assert all(torch.equal(v, want) for v in got)
