@@ -202,9 +202,5 @@ inline Divider make_divider(uint32_t d) {
 
 // Scales of a matrix: [words][rows][16 bytes].
 __host__ __device__ inline int64_t scale_words(int64_t cols, bool nv) { return ceil_div64(cols, nv ? 256 : 512); }
-__device__ __forceinline__ int64_t scale_at(int64_t row, int64_t block, int64_t rows) {
-  return ((block >> 4) * rows + row) * 16 + (block & 15);
-}
-
 }  // namespace
 }  // namespace hif4

@@ -168,78 +168,106 @@ dispatch_plain_kernel(Gather g, const Word* __restrict__ x, int64_t ld_x, Word* 
   }
 }
 
-// Eight lanes convert a unit.
+// Eight lanes convert a unit.  A block's units are collected in shared memory and copied to every row in 16-byte words (4-byte ones
+// where rows of units are not multiples of 16 bytes): stored by the lanes that made them, 4 bytes a lane, 4096 x 7168 tokens for
+// eight experts each took 51 us.
+constexpr int kBlockUnits = 128;
 template <typename T, bool kRHA>
 __global__ void __launch_bounds__(kThreads)
-dispatch_hif4_kernel(Gather g, const T* __restrict__ x, int64_t ld_x, uint32_t* __restrict__ out) {
+dispatch_hif4_kernel(Gather g, const T* __restrict__ x, int64_t ld_x, uint32_t* __restrict__ out, int block_units, int wide) {
+  __shared__ __align__(16) uint32_t units[kBlockUnits * kUnitWords];
   grid_wait();
   grid_launch_next();
   const int64_t t = blockIdx.x / g.segments;
   const int seg = static_cast<int>(blockIdx.x - t * g.segments);
   const int32_t* row_of = g.row_of + t * g.top_k;
   const int part = threadIdx.x & 7;
-  const int64_t upr = g.cols / kUnitElems;
-  for (int64_t u0 = static_cast<int64_t>(seg) * (kThreads / 8); u0 < upr; u0 += static_cast<int64_t>(g.segments) * (kThreads / 8)) {
-    const int64_t mine = u0 + (threadIdx.x >> 3), u = min(mine, upr - 1);
+  const int64_t upr = g.cols / kUnitElems, first = static_cast<int64_t>(seg) * block_units;
+  const int count = static_cast<int>(min(static_cast<int64_t>(block_units), upr - first));
+  for (int u0 = 0; u0 < count; u0 += kThreads / 8) {
+    const int mine = u0 + (threadIdx.x >> 3), u = min(mine, count - 1);
     uint32_t meta;
-    const uint32_t code = encode_unit_octet<kRHA>(load8(x + t * ld_x + u * kUnitElems + 8 * part), part, meta);
-    if (mine >= upr) continue;
-    for (int j = 0; j < g.top_k; ++j) {
-      const int row = row_of[j];
-      if (!has_row(row, g.rows)) continue;
-      uint32_t* unit = out + (row * upr + u) * kUnitWords;
-      unit[1 + part] = code;
-      if (part == 0) unit[0] = meta;
+    const uint32_t code = encode_unit_octet<kRHA>(load8(x + t * ld_x + (first + u) * kUnitElems + 8 * part), part, meta);
+    if (mine < count) {
+      units[mine * kUnitWords + 1 + part] = code;
+      if (part == 0) units[mine * kUnitWords] = meta;
+    }
+  }
+  __syncthreads();
+  for (int j = 0; j < g.top_k; ++j) {
+    const int row = row_of[j];
+    if (!has_row(row, g.rows)) continue;
+    uint32_t* dst = out + (row * upr + first) * kUnitWords;
+    if (wide) {
+      for (int i = threadIdx.x; i < count * kUnitWords / 4; i += kThreads) reinterpret_cast<uint4*>(dst)[i] = reinterpret_cast<const uint4*>(units)[i];
+    } else {
+      for (int i = threadIdx.x; i < count * kUnitWords; i += kThreads) dst[i] = units[i];
     }
   }
 }
 
-// A thread converts sixteen elements.
+// A thread converts 32 elements.
 template <typename T, bool kNv>
 __global__ void __launch_bounds__(kThreads)
-dispatch_bfp4_kernel(Gather g, const T* __restrict__ x, int64_t ld_x, const float* __restrict__ gain, uint2* __restrict__ codes,
+dispatch_bfp4_kernel(Gather g, const T* __restrict__ x, int64_t ld_x, const float* __restrict__ gain, uint4* __restrict__ codes,
                      uint8_t* __restrict__ scales) {
   grid_wait();
   grid_launch_next();
   const int64_t t = blockIdx.x / g.segments;
   const int seg = static_cast<int>(blockIdx.x - t * g.segments);
   const int32_t* row_of = g.row_of + t * g.top_k;
-  const int64_t n16 = g.cols / 16;
-  for (int64_t c0 = static_cast<int64_t>(seg) * kThreads; c0 < n16; c0 += static_cast<int64_t>(g.segments) * kThreads) {
-    const int64_t mine = c0 + threadIdx.x, c = mine < n16 ? mine : n16 - 2 + (threadIdx.x & 1);
-    const Raw16<T> raw = load_raw16(x + t * ld_x + 16 * c, false);
-    Sixteen v = sixteen_of(raw);
-    uint32_t peak = peak16(raw), byte;
+  const int64_t n32 = g.cols / 32, c = static_cast<int64_t>(seg) * blockDim.x + threadIdx.x;
+  constexpr int kOfWord = kNv ? 8 : 16;                  // threads of a scale word
+  const int64_t padded = scale_words(g.cols, kNv) * kOfWord;
+  if (c >= padded) return;
+  uint4 code = make_uint4(0u, 0u, 0u, 0u);
+  uint32_t sa = 0u, sb = 0u;                             // (0 past the last block)
+  if (c < n32) {
+    const Raw16<T> ra = load_raw16(x + t * ld_x + 32 * c, false), rb = load_raw16(x + t * ld_x + 32 * c + 16, false);
+    Sixteen a = sixteen_of(ra), b = sixteen_of(rb);
+    uint32_t pa = peak16(ra), pb = peak16(rb);
+    if (!kNv) pa = pb = max(pa, pb);
     if (gain) {
       const float f = *gain;
-      scale16(v, f);
-      peak = scaled_peak(peak, f);
+      scale16(a, f);
+      scale16(b, f);
+      pa = scaled_peak(pa, f);
+      pb = kNv ? scaled_peak(pb, f) : pa;
     }
-    if (!kNv) peak = max(peak, __shfl_xor_sync(kAll, peak, 1));
-    const uint2 code = encode16<kNv>(v, peak, byte);
-    if (mine >= n16) continue;
-    const int64_t block = kNv ? c : c >> 1;
-    for (int j = 0; j < g.top_k; ++j) {
-      const int row = row_of[j];
-      if (!has_row(row, g.rows)) continue;
-      codes[row * n16 + c] = code;
-      if (kNv || !(c & 1)) scales[scale_at(row, block, g.rows)] = static_cast<uint8_t>(byte);
-      if (c == n16 - 1)
-        for (int64_t b = block + 1; b & 15; ++b) scales[scale_at(row, b, g.rows)] = 0;
-    }
+    const uint2 ca = encode16<kNv>(a, pa, sa), cb = encode16<kNv>(b, pb, sb);
+    code = make_uint4(ca.x, ca.y, cb.x, cb.y);
+  }
+  const int64_t word = c / kOfWord;
+  const int at = static_cast<int>(c - word * kOfWord);
+#pragma unroll 4
+  for (int j = 0; j < g.top_k; ++j) {
+    const int row = row_of[j];
+    if (!has_row(row, g.rows)) continue;
+    if (c < n32) codes[row * n32 + c] = code;
+    uint8_t* scale = scales + (word * g.rows + row) * 16;
+    if (kNv) reinterpret_cast<uint16_t*>(scale)[at] = static_cast<uint16_t>(sa | (sb << 8));
+    else scale[at] = static_cast<uint8_t>(sa);
   }
 }
 
 // ----------------------------------------------------------------------------- sums over a token's experts
-// kVec elements a thread: eight, or one where rows are not 16-byte aligned.
+// kVec elements a thread: eight, or where rows are not 16-byte aligned two of 16 bits each, or one.
 template <typename T, int kVec>
 __device__ __forceinline__ void load_vec(const T* p, float (&v)[kVec]) {
-  if constexpr (kVec == 8) unpack8(load8(p), v);
-  else v[0] = to_f32(*p);
+  if constexpr (kVec == 8) {
+    unpack8(load8(p), v);
+  } else if constexpr (kVec == 2) {
+    const uint32_t w = *reinterpret_cast<const uint32_t*>(p);              // 16-bit elements only
+    v[0] = to_f32(reinterpret_cast<const T*>(&w)[0]);
+    v[1] = to_f32(reinterpret_cast<const T*>(&w)[1]);
+  } else {
+    v[0] = to_f32(*p);
+  }
 }
 template <typename T, int kVec>
 __device__ __forceinline__ void store_vec(T* p, const float (&v)[kVec]) {
   if constexpr (kVec == 8) store8(p, pack8<T>(v));
+  else if constexpr (kVec == 2) *reinterpret_cast<uint32_t*>(p) = pack2(v[0], v[1], T());
   else *p = from_f32<T>(v[0]);
 }
 
@@ -458,25 +486,45 @@ hif4_status launch_plain(const Gather& g, int64_t blocks, const hif4_dispatch_ar
                            static_cast<Word*>(a.out), a.ld_out / n, a.cols / n);
 }
 template <typename T>
-hif4_status launch_converted(const Gather& g, int64_t blocks, const hif4_dispatch_args& a, cudaStream_t st) {
-  const unsigned grid = static_cast<unsigned>(blocks);
+hif4_status launch_converted(const hif4_dispatch_args& a, cudaStream_t st) {
   const T* x = static_cast<const T*>(a.x);
-  if (a.kind == HIF4_ROWS_HIF4)
-    return launch_overlapped(a.mode == HIF4_RHA ? dispatch_hif4_kernel<T, true> : dispatch_hif4_kernel<T, false>, grid, kThreads, 0, st, g, x, a.ld_x,
-                             static_cast<uint32_t*>(a.out));
-  return launch_overlapped(a.kind == HIF4_ROWS_NVFP4 ? dispatch_bfp4_kernel<T, true> : dispatch_bfp4_kernel<T, false>, grid, kThreads, 0, st, g, x, a.ld_x,
-                           a.gain, static_cast<uint2*>(a.out), static_cast<uint8_t*>(a.out_scales));
+  Gather g;
+  int64_t blocks = 0;
+  if (a.kind == HIF4_ROWS_HIF4) {
+    // a whole row a block where tokens fill the GPU, else as many blocks as there are rounds of 32 units
+    const int64_t upr = a.cols / kUnitElems, per_round = kThreads / 8;
+    const int block_units = a.tokens * ceil_div64(upr, kBlockUnits) >= 4ll * sm_count() ? kBlockUnits : static_cast<int>(per_round);
+    const hif4_status s = make_gather(g, a.tokens, a.cols, a.top_k, a.rows, a.row_of, static_cast<int64_t>(block_units) * kUnitElems, &blocks);
+    if (s != HIF4_OK) return s;
+    const int wide = upr % 4 == 0 && aligned(a.out, 16);
+    return launch_overlapped(a.mode == HIF4_RHA ? dispatch_hif4_kernel<T, true> : dispatch_hif4_kernel<T, false>, static_cast<unsigned>(blocks), kThreads, 0,
+                             st, g, x, a.ld_x, static_cast<uint32_t*>(a.out), block_units, wide);
+  }
+  // a thread per 32 elements of the scale words' span, in blocks that share a row's evenly
+  const bool nv = a.kind == HIF4_ROWS_NVFP4;
+  const int64_t span = scale_words(a.cols, nv) * (nv ? 8 : 16), rounds = ceil_div64(span, kThreads);
+  const unsigned threads = static_cast<unsigned>(ceil_div64(ceil_div64(span, rounds), 32) * 32);
+  const hif4_status s = make_gather(g, a.tokens, span, a.top_k, a.rows, a.row_of, threads, &blocks);
+  if (s != HIF4_OK) return s;
+  g.cols = a.cols;
+  return launch_overlapped(nv ? dispatch_bfp4_kernel<T, true> : dispatch_bfp4_kernel<T, false>, static_cast<unsigned>(blocks), threads, 0, st, g, x, a.ld_x,
+                           a.gain, static_cast<uint4*>(a.out), static_cast<uint8_t*>(a.out_scales));
 }
 
 template <typename TI, typename TO>
 hif4_status launch_combine(const hif4_combine_args& a, cudaStream_t st) {
   const bool vec = a.cols % 8 == 0 && rows_aligned(a.in, a.ld_in, a.dt_in) && rows_aligned(a.residual, a.residual ? a.ld_residual : 8, a.dt) &&
                    rows_aligned(a.y, a.ld_y, a.dt);
+  const bool pairs = !vec && sizeof(TI) == 2 && sizeof(TO) == 2 &&
+                     ((bits(a.in) | bits(a.residual) | bits(a.y) | static_cast<uintptr_t>(2 * (a.cols | a.ld_in | a.ld_y | (a.residual ? a.ld_residual : 0)))) & 3u) == 0;
   Gather g;
   int64_t blocks = 0;
-  const hif4_status s = make_gather(g, a.tokens, a.cols, a.top_k, a.rows, a.row_of, kThreads * (vec ? 8 : 1), &blocks);
+  const hif4_status s = make_gather(g, a.tokens, a.cols, a.top_k, a.rows, a.row_of, kThreads * (vec ? 8 : pairs ? 2 : 1), &blocks);
   if (s != HIF4_OK) return s;
-  return launch_overlapped(vec ? combine_kernel<TI, TO, 8> : combine_kernel<TI, TO, 1>, static_cast<unsigned>(blocks), kThreads, 0, st, g,
+  auto kernel = vec ? combine_kernel<TI, TO, 8> : combine_kernel<TI, TO, 1>;
+  if constexpr (sizeof(TI) == 2 && sizeof(TO) == 2)
+    if (pairs) kernel = combine_kernel<TI, TO, 2>;
+  return launch_overlapped(kernel, static_cast<unsigned>(blocks), kThreads, 0, st, g,
                            static_cast<const TI*>(a.in), a.ld_in, a.weights, static_cast<const TO*>(a.residual), a.ld_residual, a.res_scale,
                            static_cast<TO*>(a.y), a.ld_y);
 }
@@ -569,23 +617,19 @@ extern "C" hif4_status hif4_dispatch(const hif4_dispatch_args* args, void* strea
       (scaled && (!aligned(a.out, 16) || !aligned(a.out_scales, 16) || !aligned(a.gain, 4))))
     return HIF4_ERR_ALIGN;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
+  if (!plain)
+    return a.dt == HIF4_BF16   ? launch_converted<__nv_bfloat16>(a, st)
+           : a.dt == HIF4_FP16 ? launch_converted<__half>(a, st)
+                               : launch_converted<float>(a, st);
   Gather g;
   int64_t blocks = 0;
-  if (plain) {
-    const int64_t e = type_size(a.dt);
-    const uintptr_t all = bits(a.x) | bits(a.out) | static_cast<uintptr_t>(a.cols * e) | static_cast<uintptr_t>(a.tokens > 1 ? a.ld_x * e : 0) |
-                          static_cast<uintptr_t>(a.rows > 1 ? a.ld_out * e : 0);
-    const int64_t word = all % 16 == 0 ? 16 : all % 4 == 0 ? 4 : 2;
-    s = make_gather(g, a.tokens, a.cols, a.top_k, a.rows, a.row_of, kThreads * word / e, &blocks);
-    if (s != HIF4_OK) return s;
-    return word == 16 ? launch_plain<uint4>(g, blocks, a, st) : word == 4 ? launch_plain<uint32_t>(g, blocks, a, st) : launch_plain<uint16_t>(g, blocks, a, st);
-  } else {
-    s = make_gather(g, a.tokens, a.cols, a.top_k, a.rows, a.row_of, a.kind == HIF4_ROWS_HIF4 ? kThreads * 8 : kThreads * 16, &blocks);
-    if (s != HIF4_OK) return s;
-    return a.dt == HIF4_BF16   ? launch_converted<__nv_bfloat16>(g, blocks, a, st)
-           : a.dt == HIF4_FP16 ? launch_converted<__half>(g, blocks, a, st)
-                               : launch_converted<float>(g, blocks, a, st);
-  }
+  const int64_t e = type_size(a.dt);
+  const uintptr_t all = bits(a.x) | bits(a.out) | static_cast<uintptr_t>(a.cols * e) | static_cast<uintptr_t>(a.tokens > 1 ? a.ld_x * e : 0) |
+                        static_cast<uintptr_t>(a.rows > 1 ? a.ld_out * e : 0);
+  const int64_t word = all % 16 == 0 ? 16 : all % 4 == 0 ? 4 : 2;
+  s = make_gather(g, a.tokens, a.cols, a.top_k, a.rows, a.row_of, kThreads * word / e, &blocks);
+  if (s != HIF4_OK) return s;
+  return word == 16 ? launch_plain<uint4>(g, blocks, a, st) : word == 4 ? launch_plain<uint32_t>(g, blocks, a, st) : launch_plain<uint16_t>(g, blocks, a, st);
 }
 
 extern "C" hif4_status hif4_combine(const hif4_combine_args* args, void* stream) {

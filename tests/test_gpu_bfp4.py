@@ -87,7 +87,7 @@ def test_special_values(hif4, fmt, dtype):
 
 @pytest.mark.parametrize("fmt", [MX, NV])
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16, torch.float32])
-@pytest.mark.parametrize("rows,cols", [(64, 8), (64, 136), (320, 1000), (1024, 40)])
+@pytest.mark.parametrize("rows,cols", [(64, 8), (64, 136), (320, 1000), (1024, 40), (256, 72), (768, 264), (1088, 128)])
 def test_conversion_down_the_columns(hif4, fmt, dtype, rows, cols):
     x = matrix(rows, max(cols, 64), dtype, rows + cols)[:, :cols]
     g = torch.full((1,), 0.3, device="cuda") if cols == 136 else None

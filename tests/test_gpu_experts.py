@@ -234,7 +234,7 @@ def assignment(T, k, E, seed, drop=0.1):
     return ids
 
 
-@pytest.mark.parametrize("T,k,K", [(1, 1, 64), (1, 8, 7168), (5, 3, 192), (130, 6, 1088), (600, 2, 64)])
+@pytest.mark.parametrize("T,k,K", [(1, 1, 64), (1, 8, 7168), (5, 3, 192), (130, 6, 1088), (600, 2, 64), (1500, 2, 9280)])
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16, torch.float32])
 def test_dispatch(hif4, T, k, K, dtype):
     x = (torch.randn(T, K, generator=gen(T + K), device="cuda") * 3).to(dtype)
@@ -288,7 +288,7 @@ def test_rows_outside_the_output_are_left_out(hif4):
 TYPES = [torch.bfloat16, torch.float16, torch.float32]
 
 
-@pytest.mark.parametrize("T,k,K,pad", [(1, 8, 7168, 0), (1, 1, 1, 0), (40, 6, 2056, 0), (33, 9, 1001, 0), (200, 4, 64, 8), (50, 32, 320, 3), (700, 3, 2056, 0), (300, 5, 777, 0)])
+@pytest.mark.parametrize("T,k,K,pad", [(1, 8, 7168, 0), (1, 1, 1, 0), (40, 6, 2056, 0), (33, 9, 1001, 0), (200, 4, 64, 8), (50, 32, 320, 3), (700, 3, 2056, 0), (300, 5, 777, 0), (90, 4, 1002, 2)])
 @pytest.mark.parametrize("dt_in", TYPES)
 @pytest.mark.parametrize("dt", TYPES)
 def test_combine_and_its_gradient(hif4, T, k, K, pad, dt_in, dt):
