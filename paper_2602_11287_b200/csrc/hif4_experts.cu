@@ -79,11 +79,13 @@ plan_place_kernel(const int32_t* __restrict__ ids, int64_t n, int64_t per_block,
   for (int e0 = 0; e0 < experts; e0 += blockDim.x) {
     const int e = e0 + threadIdx.x;
     int before = 0, total = 0;                          // of expert e: before this block, in all blocks
+    int of_run[kPlanWarps];                             // (registers, so that the loads do not wait for the stores below)
     if (e < experts) {
-      int sum = 0;
-      for (int w = 0; w < runs; ++w) sum += hist[w * experts + e];
+#pragma unroll
+      for (int w = 0; w < kPlanWarps; ++w) of_run[w] = w < runs ? hist[w * experts + e] : 0;
       if (blocks == 1) {
-        total = sum;
+#pragma unroll
+        for (int w = 0; w < kPlanWarps; ++w) total += of_run[w];
       } else {
 #pragma unroll 8
         for (int b = 0; b < blocks; ++b) {
@@ -111,10 +113,10 @@ plan_place_kernel(const int32_t* __restrict__ ids, int64_t n, int64_t per_block,
     if (e < experts) {
       const int end = ahead + incl;
       int at = end - total + before;
-      for (int w = 0; w < runs; ++w) {                  // the warps' first places
-        const int c = hist[w * experts + e];
-        hist[w * experts + e] = at;
-        at += c;
+#pragma unroll
+      for (int w = 0; w < kPlanWarps; ++w) {            // the warps' first places
+        if (w < runs) hist[w * experts + e] = at;
+        at += of_run[w];
       }
       if (blockIdx.x == 0) {
         if (e == 0) offsets[0] = 0;

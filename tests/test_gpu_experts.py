@@ -204,7 +204,7 @@ def plan(ids, E):
     return off, torch.where(key < E, row, -1).view(ids.shape).int()
 
 
-@pytest.mark.parametrize("T,k,E", [(1, 1, 1), (1, 8, 256), (3, 5, 7), (1000, 8, 256), (1024, 8, 1024), (1025, 8, 64), (5000, 6, 100), (70000, 2, 33),
+@pytest.mark.parametrize("T,k,E", [(1, 1, 1), (1, 8, 256), (3, 5, 7), (1000, 8, 256), (1024, 8, 1024), (1025, 8, 64), (5000, 6, 100), (70000, 2, 33), (512, 8, 1024), (513, 8, 300), (300000, 8, 64),
                                    (4096, 8, 1)])
 @pytest.mark.parametrize("drop", [0.0, 0.3])
 def test_plan(hif4, T, k, E, drop):
