@@ -8,6 +8,9 @@
 // warps read the rows' words, which are just the four K = 64 steps of a row, and store them to their lane quarter.
 // Few tiles: the K chunks of a tile are dealt to the CTAs of a cluster, whose FP32 sums are added through distributed
 // shared memory in rank order (no atomics, no workspace).
+//
+// One token, 14336 x 4096 NVFP4: 8.3 us in a graph, 9.3 us over weights that come from HBM (33 MB: 5.1 us); 4096 x 4096 5.8 us.  What is
+// left is start-up (barriers, tensor memory, tensor maps: 2 us), the cluster's two barriers and the launch.
 #include "hif4_bfp4_gemm.cuh"
 
 namespace hif4 {

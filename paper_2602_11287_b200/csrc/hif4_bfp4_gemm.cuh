@@ -55,7 +55,7 @@ __device__ __forceinline__ void mma_scaled(uint32_t d, uint64_t adesc, uint64_t 
 }
 // One lane of the warp (all lanes call).  The loops around MMAs are run by whole warps with only the MMAs under this condition: their
 // descriptors are then uniform values for the compiler, where a loop run by one lane moves every operand to uniform registers
-// before each MMA (143 clocks an MMA that takes 128).
+// before each MMA (218 clocks an MMA, waits included, that takes 128: 4096 x 14336 x 4096 152 -> 128 us).
 __device__ __forceinline__ bool elect_one() {
   uint32_t one;
   asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(one));

@@ -1,6 +1,10 @@
 // hif4_expert_plan, hif4_dispatch, hif4_combine, hif4_combine_backward -- the experts' rows of a mixture-of-experts
 // layer: their order, the rows themselves, the weighted sum of what comes back, and its gradient.  All but the plan are
 // bound by HBM traffic: a token's row is read (and converted) once, the experts' rows are read or written once.
+//
+// 4096 tokens, 8 of 256 experts, 7168 columns, BF16: rows as they are 86 us (6.1 TB/s), HiF4 units 44 us (4.3), MXFP4 33 us (5.5),
+// NVFP4 37 us (5.2); FP32 rows back to tokens with a residual 155 us (6.8 TB/s).  Its gradient, 2047 x 6 x 2056 BF16: 21 us (5.2 TB/s).
+// The plan of 32768 assignments: 8 us in two launches, of 64: 2.3 us in one.
 #include "hif4_bfp4_device.cuh"
 #include "hif4_tc_common.cuh"
 
