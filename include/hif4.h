@@ -371,7 +371,8 @@ hif4_status hif4_mse_roundtrip(const void* src_bf16, int64_t n, hif4_bfp4_format
 /* ---------------------------------------------------------------------------------------------
  * What stands around the experts' products of a mixture-of-experts layer: which experts a token goes to, the experts' rows
  * in the order that hif4_grouped_gemm and hif4_bfp4_grouped_gemm read, and the weighted sum of what comes back.
- * Routing results stay on the device.  */
+ * Routing results stay on the device.  Matrices that a call writes must not overlap what it reads, except where a parameter
+ * says so.  */
 #define HIF4_ROUTE_MAX_EXPERTS 1024
 #define HIF4_ROUTE_MAX_TOP_K 32
 #define HIF4_ROUTE_MAX_GROUPS 32
@@ -431,7 +432,8 @@ typedef enum { HIF4_ROWS_PLAIN = 0, HIF4_ROWS_HIF4 = 1, HIF4_ROWS_MXFP4 = 2, HIF
 
 /* hif4_dispatch -- the experts' rows: out[row_of[t][j]] = x[t] for every assignment that has a row; a token is read and
  * converted once.  Converted rows are bit for bit those of hif4_quantize and hif4_bfp4_quantize.  Rows that no assignment
- * has stay as they were; so does a row number outside 0 .. rows - 1.  (Its gradient is hif4_combine without weights.)  */
+ * has stay as they were; a row number outside 0 .. rows - 1 is no row.  Row numbers differ (hif4_expert_plan's do): of two assignments with
+ * the same one, either's token may be found there.  (Its gradient is hif4_combine without weights.)  */
 typedef struct {
   int64_t tokens, cols, top_k, rows;
   const void* x;                 /* device, [tokens, cols] of dt, row stride ld_x elements; 16-byte aligned rows unless PLAIN */
@@ -507,7 +509,8 @@ hif4_status hif4_bfp4_quantize(const void* src, hif4_dtype dt, int64_t rows, int
  * dW = dY^T X from the columns of both.  */
 hif4_status hif4_bfp4_quantize_transposed(const void* src, hif4_dtype dt, int64_t rows, int64_t cols, int64_t ld_src,
                                           hif4_bfp4_format fmt, const float* gain, void* codes, void* scales, void* stream);
-/* Values, divided by the gain if there is one; dst BF16 or FP32, rows 16-byte aligned (exact without a gain).  */
+/* Values in FP32 (6 * 2^126, which an infinity becomes in MXFP4, is one again), divided by the gain if there is one, rounded to dst:
+ * BF16 or FP32, rows 16-byte aligned (exact without a gain; FP16 is refused as in hif4_dequantize).  */
 hif4_status hif4_bfp4_dequantize(const void* codes, const void* scales, int64_t rows, int64_t cols, hif4_bfp4_format fmt,
                                  const float* gain, void* dst, hif4_dtype dt, int64_t ld_dst, void* stream);
 

@@ -170,6 +170,7 @@ __device__ __forceinline__ float quotient(float a, const Gain& k) {
 __device__ __forceinline__ bool make_table(float s, const Gain& gain, Bf16Table& t) {
   float d1 = s, d3 = 1.5f * s;
   if (gain.given) {
+    if (s > 0x1p125f) return false;                                      // the values leave FP32's range before the division
     d1 = quotient(d1, gain);
     d3 = quotient(d3, gain);
   }

@@ -48,6 +48,21 @@ def test_conversion(hif4, fmt, dtype, rows, cols, gain):
 
 
 @pytest.mark.parametrize("fmt", [MX, NV])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("gain", [-0.7, 1e-30, 1e30, 3e38, 2.0 ** -140, 0.0, float("nan")])
+def test_gains_of_any_size(hif4, fmt, dtype, gain):
+    x = matrix(20, 320, dtype, 11)
+    g = torch.full((1,), gain, device="cuda")
+    codes, scales = hif4.hif4_bfp4_quantize(x, fmt, gain=g)
+    want = ref.pack(*ref.convert(x, fmt, g))
+    assert torch.equal(codes, want[0]) and torch.equal(scales, want[1])
+    for dt in (torch.bfloat16, torch.float32):
+        got, v = hif4.hif4_bfp4_dequantize((codes, scales), fmt, dt, gain=g), (ref.values(*want, fmt).float() / g).to(dt)
+        assert torch.equal(got.isnan(), v.isnan()) and torch.equal(got.nan_to_num(0.0, 1e38, -1e38), v.nan_to_num(0.0, 1e38, -1e38))
+        assert torch.equal(torch.signbit(got[~got.isnan()]), torch.signbit(v[~v.isnan()]))
+
+
+@pytest.mark.parametrize("fmt", [MX, NV])
 def test_image_is_the_quantization_study_s(hif4, fmt):
     x = matrix(64, 1024, torch.bfloat16, 5)
     image, _ = hif4.hif4_mse_roundtrip(x, fmt)
