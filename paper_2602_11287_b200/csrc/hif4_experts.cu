@@ -79,7 +79,7 @@ plan_place_kernel(const int32_t* __restrict__ ids, int64_t n, int64_t per_block,
       if (id[j] >= 0) atomicAdd(&mine[id[j]], 1);
   }
   __syncthreads();
-  int past = 0;                                         // rows of the experts before those of this round
+  int past = 0;                                         // rows of the experts before these
   for (int e0 = 0; e0 < experts; e0 += blockDim.x) {
     const int e = e0 + threadIdx.x;
     int before = 0, total = 0;                          // of expert e: before this block, in all blocks
@@ -99,7 +99,7 @@ plan_place_kernel(const int32_t* __restrict__ ids, int64_t n, int64_t per_block,
         }
       }
     }
-    int incl = total;                                   // scan over the experts of this round
+    int incl = total;                                   // scan over these experts
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
       const int v = __shfl_up_sync(kAll, incl, o);
