@@ -22,7 +22,7 @@ struct Bfp4Params {
   const float* alpha;
   void* y;
   int64_t ld_y;
-  int dt, tma_store, row_copies;            // how Y leaves shared memory: boxes, whole rows
+  int dt, tma_store, row_copies, pair_words;  // how Y leaves shared memory: boxes, whole rows, two 16-bit elements at a time
   int num_groups;                           // 0: dense
   const int64_t* offsets;
   unsigned int* error_word;

@@ -58,19 +58,54 @@ __device__ __forceinline__ void tma_store_hinted(const CUtensorMap* map, int x, 
   asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group.L2::cache_hint [%0, {%1, %2}], [%3], %4;" ::"l"(map), "r"(x), "r"(y), "r"(src),
                "l"(policy) : "memory");
 }
-// A warp's 32 words per lane (128 bytes of its lane's row) -> its slab -> Y.  The slab is free once the copy before has read it.
-__device__ __forceinline__ void store_slab(const CUtensorMap* map, int x, int y, uint32_t slab, const uint32_t* w, int lane, uint64_t policy) {
+// A warp's 32 words per lane (128 bytes of its lane's row) -> its slab, once the copy before has read it.
+__device__ __forceinline__ void fill_slab(uint32_t slab, const uint32_t* w, int lane) {
   if (lane == 0) bulk_wait_read<0>();
   __syncwarp();
   const uint32_t row = slab + lane * 128u, r7 = static_cast<uint32_t>(lane) & 7u;
 #pragma unroll
   for (uint32_t i = 0; i < 8; ++i) sts128(row + ((i ^ r7) << 4), w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+}
+__device__ __forceinline__ void store_slab(const CUtensorMap* map, int x, int y, uint32_t slab, const uint32_t* w, int lane, uint64_t policy) {
+  fill_slab(slab, w, lane);
   fence_proxy_async_smem();
   __syncwarp();
   if (lane == 0) {
     tma_store_hinted(map, x, y, slab, policy);
     bulk_commit();
   }
+}
+// The same without a box, for rows at any address and the last rows of a group: a row after the other, the lanes along it (four bytes
+// a lane where Y allows, so that a row's 128 bytes are one store).  From the registers, a row a lane, 3798 x 2836 x 1024 took 125 us.
+template <typename Word>
+__device__ __forceinline__ void copy_slab(Word* y, int64_t ld, int rows, int cols, uint32_t slab, int lane) {
+  constexpr int kOfRow = 128 / static_cast<int>(sizeof(Word));
+  for (int r = 0; r < rows; ++r) {
+#pragma unroll
+    for (int e0 = 0; e0 < kOfRow; e0 += 32) {
+      const uint32_t e = static_cast<uint32_t>(e0 + lane), at = e * sizeof(Word), src = slab + r * 128u + (((at >> 4) ^ (r & 7u)) << 4) + (at & 15u);
+      if (static_cast<int>(e) < cols) {
+        if constexpr (sizeof(Word) == 4) {
+          y[r * ld + e] = lds32(src);
+        } else {
+          uint16_t v;
+          asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(src));
+          y[r * ld + e] = v;
+        }
+      }
+    }
+  }
+}
+__device__ __forceinline__ void store_rows(const Bfp4Params& p, int n, int m, int m_end, uint32_t slab, const uint32_t* w, int lane) {
+  fill_slab(slab, w, lane);
+  __syncwarp();
+  const int rows = min(32, m_end - m);
+  const int64_t at = static_cast<int64_t>(m) * p.ld_y + n;
+  const int64_t cols = p.N - n;
+  if (p.dt == HIF4_FP32) copy_slab(static_cast<uint32_t*>(p.y) + at, p.ld_y, rows, static_cast<int>(min(cols, static_cast<int64_t>(32))), slab, lane);
+  else if (p.pair_words) copy_slab(static_cast<uint32_t*>(p.y) + at / 2, p.ld_y / 2, rows, static_cast<int>(min(cols, static_cast<int64_t>(64)) / 2), slab, lane);
+  else copy_slab(static_cast<uint16_t*>(p.y) + at, p.ld_y, rows, static_cast<int>(min(cols, static_cast<int64_t>(64))), slab, lane);
+  __syncwarp();
 }
 
 template <bool kNv, bool kGrouped>
@@ -244,9 +279,9 @@ bfp4_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant_
       ph ^= 1u;
       tc_fence_after();
       const int m = w.m0 + static_cast<int>(rank) * kHalf + q * 32, n = w.n0 + c0;       // the warp's first row and column
-      const bool inside = m < w.m_end && n < p.N, boxes = !kGrouped || m + 32 <= w.m_end;      // (a box would reach into the next group)
+      const bool inside = m < w.m_end && n < p.N, boxes = p.tma_store && (!kGrouped || m + 32 <= w.m_end);      // (a box would reach into the next group)
       const float alpha = p.alpha ? p.alpha[w.group] : 1.0f;
-      if (p.tma_store && p.dt != HIF4_FP32) {
+      if (p.dt != HIF4_FP32) {
         uint32_t packed[64];
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
@@ -262,14 +297,11 @@ bfp4_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant_
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive_cluster(empty_leader);
-        if (boxes) {
-          if (inside) store_slab(&tmY, n, m, slab, packed, lane, policy);
-          if (inside && n + 64 < p.N) store_slab(&tmY, n + 64, m, slab, packed + 32, lane, policy);
-        } else if (m + lane < w.m_end) {
-          uint16_t* row = static_cast<uint16_t*>(p.y) + (m + lane) * p.ld_y + n;
 #pragma unroll
-          for (int i = 0; i < 16; ++i)
-            if (n + 8 * i < p.N) reinterpret_cast<uint4*>(row)[i] = make_uint4(packed[4 * i], packed[4 * i + 1], packed[4 * i + 2], packed[4 * i + 3]);
+        for (int c = 0; c < 2; ++c) {
+          if (!inside || n + 64 * c >= p.N) continue;
+          if (boxes) store_slab(&tmY, n + 64 * c, m, slab, packed + 32 * c, lane, policy);
+          else store_rows(p, n + 64 * c, m, w.m_end, slab, packed + 32 * c, lane);
         }
       } else {
         for (int c = 0; c < 4; ++c) {
@@ -278,13 +310,9 @@ bfp4_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant_
           tc_wait_ld();
 #pragma unroll
           for (int i = 0; i < 32; ++i) r[i] = __float_as_uint(alpha * __uint_as_float(r[i]));
-          if (p.tma_store && boxes) {
-            if (inside && n + 32 * c < p.N) store_slab(&tmY, n + 32 * c, m, slab, r, lane, policy);
-          } else if (m + lane < w.m_end) {
-#pragma unroll
-            for (int i = 0; i < 32; ++i)
-              if (n + 32 * c + i < p.N) store_y(p, m + lane, n + 32 * c + i, __uint_as_float(r[i]));
-          }
+          if (!inside || n + 32 * c >= p.N) continue;
+          if (boxes) store_slab(&tmY, n + 32 * c, m, slab, r, lane, policy);
+          else store_rows(p, n + 32 * c, m, w.m_end, slab, r, lane);
         }
         tc_fence_before();
         __syncwarp();
@@ -320,6 +348,7 @@ hif4_status launch_pairs(const hif4_bfp4_gemm_args& a, Bfp4Params p, cudaStream_
   const int64_t size = a.dt == HIF4_FP32 ? 4 : 2;
   p.tma_store = (reinterpret_cast<uintptr_t>(a.Y) & 15u) == 0 && a.ld_y * size % 16 == 0 && a.N * size % 16 == 0 && make_y_map(&tmY, a, static_cast<int>(128 / size), 32, CU_TENSOR_MAP_SWIZZLE_128B);
   if (!p.tma_store) tmY = tmA;                           // not used
+  p.pair_words = size == 2 && ((reinterpret_cast<uintptr_t>(a.Y) | static_cast<uintptr_t>(2 * (a.ld_y | a.N))) & 3u) == 0;
   const int64_t m_tiles = ceil_div64(a.M, kTile) + (kGrouped ? a.num_groups : 0), n_tiles = ceil_div64(a.N, kTile);
   if (m_tiles * n_tiles > 0x7FFFFFFFll - 1024 || n_tiles > 0x7FFFFFFFll / kBand) return HIF4_ERR_SHAPE;
   p.m_tiles = static_cast<int>(m_tiles);

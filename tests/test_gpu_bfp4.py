@@ -151,7 +151,8 @@ def test_product(hif4, fmt, M, N, K):
 
 
 @pytest.mark.parametrize("fmt", [MX, NV])
-@pytest.mark.parametrize("M,N,K", [(1500, 1777, 320), (2049, 2304, 1088), (257, 9600, 576), (8200, 512, 64), (1300, 2050, 2304), (2560, 2560, 512)])
+@pytest.mark.parametrize("M,N,K", [(1500, 1777, 320), (2049, 2304, 1088), (257, 9600, 576), (8200, 512, 64), (1300, 2050, 2304), (2560, 2560, 512),
+                                   (700, 2836, 1024), (333, 1001, 320), (70, 131, 832)])
 def test_product_of_prompts(hif4, fmt, M, N, K):
     """The sizes of the CTA-pair kernel."""
     test_product(hif4, fmt, M, N, K)
@@ -206,7 +207,7 @@ def test_product_into_a_view(hif4, M):
 @pytest.mark.parametrize("fmt", [MX, NV])
 @pytest.mark.parametrize("counts,N,K", [([3], 100, 64), ([0, 1, 0, 0, 17, 0], 130, 320), ([40, 0, 129, 1, 300], 257, 512), ([5] * 40, 128, 1024),
                                         ([0, 0], 64, 128), ([600, 1, 1], 320, 2112),
-                                        ([20, 0, 70, 33, 64, 1], 520, 4096), ([700, 0, 333, 1], 520, 320), ([256, 512, 17], 300, 1088), ([1000, 31], 257, 128), ([1, 2, 0] * 100, 64, 320), ([7] * 256, 130, 576)])
+                                        ([20, 0, 70, 33, 64, 1], 520, 4096), ([700, 0, 333, 1], 520, 320), ([256, 512, 17], 300, 1088), ([1000, 31], 257, 128), ([500, 140, 0, 141], 1002, 192), ([1, 2, 0] * 100, 64, 320), ([7] * 256, 130, 576)])
 def test_grouped_product(hif4, fmt, counts, N, K):
     g = gen(sum(counts) + N)
     G, used = len(counts), sum(counts)
