@@ -5,6 +5,8 @@
 // 4096 tokens, 8 of 256 experts, 7168 columns, BF16: rows as they are 86 us (6.1 TB/s), HiF4 units 44 us (4.3), MXFP4 33 us (5.5),
 // NVFP4 37 us (5.2); FP32 rows back to tokens with a residual 155 us (6.8 TB/s).  Its gradient, 2047 x 6 x 2056 BF16: 21 us (5.2 TB/s).
 // The plan of 32768 assignments: 8 us in two launches, of 64: 2.3 us in one.
+#include <type_traits>
+
 #include "hif4_bfp4_device.cuh"
 #include "hif4_tc_common.cuh"
 
@@ -156,8 +158,12 @@ struct Gather {
 };
 __device__ __forceinline__ bool has_row(int row, int64_t rows) { return row >= 0 && row < rows; }
 
+// Rows that are no multiples of 16 bytes move in words of 4 or 2 bytes, kNarrow of them a thread, so that as many bytes are under way
+// (2048 tokens x 6 of 4097 BF16 elements, with one word a thread -> with four: rows 59 -> 33 us, their sum 90 -> 49, its gradient
+// 74 -> 68; of 4098 35 -> 29, 55 -> 43, 74 -> 54).
+constexpr int kNarrow = 4;
 // Word: as many bytes as addresses, row strides and the row's length allow.
-template <typename Word>
+template <typename Word, int kAcross>
 __global__ void __launch_bounds__(kThreads)
 dispatch_plain_kernel(Gather g, const Word* __restrict__ x, int64_t ld_x, Word* __restrict__ out, int64_t ld_out, int64_t words) {
   grid_wait();
@@ -165,12 +171,17 @@ dispatch_plain_kernel(Gather g, const Word* __restrict__ x, int64_t ld_x, Word* 
   const int64_t t = blockIdx.x / g.segments;
   const int seg = static_cast<int>(blockIdx.x - t * g.segments);
   const int32_t* row_of = g.row_of + t * g.top_k;
-  for (int64_t w = seg * kThreads + threadIdx.x; w < words; w += static_cast<int64_t>(g.segments) * kThreads) {
-    const Word v = x[t * ld_x + w];
-    for (int j = 0; j < g.top_k; ++j) {
-      const int row = row_of[j];
-      if (has_row(row, g.rows)) out[row * ld_out + w] = v;
-    }
+  const int64_t w0 = static_cast<int64_t>(seg) * kThreads * kAcross + threadIdx.x;
+  Word v[kAcross];
+#pragma unroll
+  for (int i = 0; i < kAcross; ++i)
+    if (w0 + i * kThreads < words) v[i] = x[t * ld_x + w0 + i * kThreads];
+  for (int j = 0; j < g.top_k; ++j) {
+    const int row = row_of[j];
+    if (!has_row(row, g.rows)) continue;
+#pragma unroll
+    for (int i = 0; i < kAcross; ++i)
+      if (w0 + i * kThreads < words) out[row * ld_out + w0 + i * kThreads] = v[i];
   }
 }
 
@@ -277,7 +288,7 @@ __device__ __forceinline__ void store_vec(T* p, const float (&v)[kVec]) {
   else *p = from_f32<T>(v[0]);
 }
 
-template <typename TI, typename TO, int kVec>
+template <typename TI, typename TO, int kVec, int kAcross>
 __global__ void __launch_bounds__(kThreads)
 combine_kernel(Gather g, const TI* __restrict__ in, int64_t ld_in, const float* __restrict__ weights, const TO* residual, int64_t ld_r,
                float res_scale, TO* y, int64_t ld_y) {
@@ -286,26 +297,35 @@ combine_kernel(Gather g, const TI* __restrict__ in, int64_t ld_in, const float* 
   const int64_t t = blockIdx.x / g.segments;
   const int seg = static_cast<int>(blockIdx.x - t * g.segments);
   const int32_t* row_of = g.row_of + t * g.top_k;
-  const int64_t c = (static_cast<int64_t>(seg) * kThreads + threadIdx.x) * kVec;
-  if (c >= g.cols) return;
-  float acc[kVec], v[kVec];
+  const int64_t c0 = (static_cast<int64_t>(seg) * kThreads * kAcross + threadIdx.x) * kVec;
+  constexpr int kStep = kThreads * kVec;
+  if (c0 >= g.cols) return;
+  float acc[kAcross][kVec], v[kAcross][kVec];
 #pragma unroll
-  for (int i = 0; i < kVec; ++i) acc[i] = 0.0f;
+  for (int u = 0; u < kAcross; ++u)
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) acc[u][i] = 0.0f;
+  const auto add = [&](const auto* from, float w) {
+#pragma unroll
+    for (int u = 0; u < kAcross; ++u)
+      if (c0 + u * kStep < g.cols) load_vec(from + c0 + u * kStep, v[u]);
+#pragma unroll
+    for (int u = 0; u < kAcross; ++u)
+      if (c0 + u * kStep < g.cols) {
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) acc[u][i] = fmaf(w, v[u][i], acc[u][i]);
+      }
+  };
 #pragma unroll 4
   for (int j = 0; j < g.top_k; ++j) {
     const int row = row_of[j];
     const float w = weights ? weights[t * g.top_k + j] : 1.0f;
-    if (!has_row(row, g.rows)) continue;
-    load_vec(in + row * ld_in + c, v);
-#pragma unroll
-    for (int i = 0; i < kVec; ++i) acc[i] = fmaf(w, v[i], acc[i]);
+    if (has_row(row, g.rows)) add(in + row * ld_in, w);
   }
-  if (residual) {
-    load_vec(residual + t * ld_r + c, v);
+  if (residual) add(residual + t * ld_r, res_scale);
 #pragma unroll
-    for (int i = 0; i < kVec; ++i) acc[i] = fmaf(res_scale, v[i], acc[i]);
-  }
-  store_vec(y + t * ld_y + c, acc);
+  for (int u = 0; u < kAcross; ++u)
+    if (c0 + u * kStep < g.cols) store_vec(y + t * ld_y + c0 + u * kStep, acc[u]);
 }
 
 // A block goes over a token's row, eight assignments at a time, whose rows are loaded together.
@@ -330,7 +350,8 @@ combine_backward_kernel(Gather g, const TD* __restrict__ dy, int64_t ld_dy, cons
       w[j] = there && weights ? weights[t * g.top_k + j0 + j] : 1.0f;
       acc[j] = 0.0f;
     }
-    for (int64_t c = static_cast<int64_t>(threadIdx.x) * kVec; c < g.cols; c += blockDim.x * kVec) {
+    constexpr int kAcross = kVec == 8 ? 1 : kNarrow;
+    for (int64_t c = static_cast<int64_t>(threadIdx.x) * kVec; c < g.cols; c += blockDim.x * kVec * kAcross) {
       if constexpr (kVec == 8) {
         const Raw8<TD> raw_d = load8(dy + t * ld_dy + c);
         Raw8<TI> raw[kTogether];
@@ -362,12 +383,30 @@ combine_backward_kernel(Gather g, const TD* __restrict__ dy, int64_t ld_dy, cons
           }
         }
       } else {
-        const float d = to_f32(dy[t * ld_dy + c]);
+        TD d[kAcross];
+        TI v[kTogether][kAcross];
+        int64_t at[kAcross];                            // past the row: its last element, loaded and not used
+#pragma unroll
+        for (int u = 0; u < kAcross; ++u) at[u] = min(c + u * static_cast<int>(blockDim.x), g.cols - 1);
+#pragma unroll
+        for (int u = 0; u < kAcross; ++u) d[u] = dy[t * ld_dy + at[u]];
+        if (dweights) {
+#pragma unroll
+          for (int j = 0; j < kTogether; ++j)
+            if (row[j] >= 0) {
+#pragma unroll
+              for (int u = 0; u < kAcross; ++u) v[j][u] = in[row[j] * ld_in + at[u]];
+            }
+        }
 #pragma unroll
         for (int j = 0; j < kTogether; ++j) {
           if (row[j] < 0) continue;
-          if (dweights) acc[j] = fmaf(d, to_f32(in[row[j] * ld_in + c]), acc[j]);
-          if (din) din[row[j] * ld_din + c] = from_f32<TI>(__fmul_rn(w[j], d));
+#pragma unroll
+          for (int u = 0; u < kAcross; ++u) {
+            if (c + u * static_cast<int>(blockDim.x) >= g.cols) continue;
+            if (dweights) acc[j] = fmaf(to_f32(d[u]), to_f32(v[j][u]), acc[j]);
+            if (din) din[row[j] * ld_din + at[u]] = from_f32<TI>(__fmul_rn(w[j], to_f32(d[u])));
+          }
         }
       }
     }
@@ -408,13 +447,14 @@ combine_backward_rows_kernel(Gather g, int64_t assignments, const TD* __restrict
     const TD* d_row = dy + (a / g.top_k) * ld_dy;
     const TI* in_row = in + row * ld_in;
     TI* out = din + row * ld_din;
-    for (int64_t c0 = lane * kVec; c0 < g.cols; c0 += kAtOnce * 32 * kVec) {
+    constexpr int kStep = 32 * kVec;
+    for (int64_t c0 = lane * kVec; c0 < g.cols; c0 += (kVec == 8 ? kAtOnce : 2 * kAtOnce) * kStep) {
       if constexpr (kVec == 8) {
         Raw8<TD> rd[kAtOnce];
         Raw8<TI> rv[kAtOnce];
 #pragma unroll
         for (int u = 0; u < kAtOnce; ++u) {
-          const int64_t c = c0 + u * 32 * kVec;
+          const int64_t c = c0 + u * kStep;
           if (c < g.cols) {
             rd[u] = load8(d_row + c);
             if (dweights) rv[u] = load8(in_row + c);
@@ -422,7 +462,7 @@ combine_backward_rows_kernel(Gather g, int64_t assignments, const TD* __restrict
         }
 #pragma unroll
         for (int u = 0; u < kAtOnce; ++u) {
-          const int64_t c = c0 + u * 32 * kVec;
+          const int64_t c = c0 + u * kStep;
           if (c >= g.cols) continue;
           const Pairs d = pairs_of(rd[u]);
           if (dweights) {
@@ -440,14 +480,29 @@ combine_backward_rows_kernel(Gather g, int64_t assignments, const TD* __restrict
           }
         }
       } else {
+        constexpr int kMany = 2 * kAtOnce;
+        const auto some = [&](auto whole) {
+          constexpr bool kWhole = decltype(whole)::value;
+          float d[kMany][kVec], v[kMany][kVec];
 #pragma unroll
-        for (int u = 0; u < kAtOnce; ++u) {
-          const int64_t c = c0 + u * 32;
-          if (c >= g.cols) continue;
-          const float d = to_f32(d_row[c]);
-          if (dweights) acc = fmaf(d, to_f32(in_row[c]), acc);
-          if (din) out[c] = from_f32<TI>(__fmul_rn(w, d));
-        }
+          for (int u = 0; u < kMany; ++u) {
+            if (!kWhole && c0 + u * kStep >= g.cols) break;
+            load_vec(d_row + c0 + u * kStep, d[u]);
+            if (dweights) load_vec(in_row + c0 + u * kStep, v[u]);
+          }
+#pragma unroll
+          for (int u = 0; u < kMany; ++u) {
+            if (!kWhole && c0 + u * kStep >= g.cols) break;
+#pragma unroll
+            for (int i = 0; i < kVec; ++i) {
+              if (dweights) acc = fmaf(d[u][i], v[u][i], acc);
+              d[u][i] = __fmul_rn(w, d[u][i]);
+            }
+            if (din) store_vec(out + c0 + u * kStep, d[u]);
+          }
+        };
+        if (c0 + (kMany - 1) * kStep < g.cols) some(std::true_type());
+        else some(std::false_type());
       }
     }
   }
@@ -465,6 +520,8 @@ uintptr_t bits(const void* p) { return reinterpret_cast<uintptr_t>(p); }
 bool aligned(const void* p, int64_t to) { return bits(p) % static_cast<uintptr_t>(to) == 0; }
 // Row r of a matrix starts at a multiple of 16 bytes, for every r.
 bool rows_aligned(const void* p, int64_t ld, int dt) { return aligned(p, 16) && ld * type_size(dt) % 16 == 0; }
+// Rows of 16-bit elements go in whole 4-byte words.
+bool words_aligned(const void* p, int64_t ld, int64_t cols) { return aligned(p, 4) && (ld | cols) % 2 == 0; }
 
 int64_t plan_per_block(int64_t n) { return kPlanItems * ceil_div64(n > 0 ? n : 1, static_cast<int64_t>(kPlanItems) * kPlanBlocks); }
 int64_t plan_blocks(int64_t n) { return n > 0 ? ceil_div64(n, plan_per_block(n)) : 1; }
@@ -485,10 +542,14 @@ hif4_status make_gather(Gather& g, int64_t tokens, int64_t cols, int64_t top_k, 
   return HIF4_OK;
 }
 
-template <typename Word>
-hif4_status launch_plain(const Gather& g, int64_t blocks, const hif4_dispatch_args& a, cudaStream_t st) {
+template <typename Word, int kAcross>
+hif4_status launch_plain(const hif4_dispatch_args& a, cudaStream_t st) {
   const int64_t n = static_cast<int64_t>(sizeof(Word)) / type_size(a.dt);
-  return launch_overlapped(dispatch_plain_kernel<Word>, static_cast<unsigned>(blocks), kThreads, 0, st, g, static_cast<const Word*>(a.x), a.ld_x / n,
+  Gather g;
+  int64_t blocks = 0;
+  const hif4_status s = make_gather(g, a.tokens, a.cols, a.top_k, a.rows, a.row_of, kThreads * kAcross * n, &blocks);
+  if (s != HIF4_OK) return s;
+  return launch_overlapped(dispatch_plain_kernel<Word, kAcross>, static_cast<unsigned>(blocks), kThreads, 0, st, g, static_cast<const Word*>(a.x), a.ld_x / n,
                            static_cast<Word*>(a.out), a.ld_out / n, a.cols / n);
 }
 template <typename T>
@@ -521,15 +582,15 @@ template <typename TI, typename TO>
 hif4_status launch_combine(const hif4_combine_args& a, cudaStream_t st) {
   const bool vec = a.cols % 8 == 0 && rows_aligned(a.in, a.ld_in, a.dt_in) && rows_aligned(a.residual, a.residual ? a.ld_residual : 8, a.dt) &&
                    rows_aligned(a.y, a.ld_y, a.dt);
-  const bool pairs = !vec && sizeof(TI) == 2 && sizeof(TO) == 2 &&
-                     ((bits(a.in) | bits(a.residual) | bits(a.y) | static_cast<uintptr_t>(2 * (a.cols | a.ld_in | a.ld_y | (a.residual ? a.ld_residual : 0)))) & 3u) == 0;
+  const bool pairs = !vec && sizeof(TI) == 2 && sizeof(TO) == 2 && words_aligned(a.in, a.ld_in, a.cols) && words_aligned(a.y, a.ld_y, a.cols) &&
+                     (!a.residual || words_aligned(a.residual, a.ld_residual, a.cols));
   Gather g;
   int64_t blocks = 0;
-  const hif4_status s = make_gather(g, a.tokens, a.cols, a.top_k, a.rows, a.row_of, kThreads * (vec ? 8 : pairs ? 2 : 1), &blocks);
+  const hif4_status s = make_gather(g, a.tokens, a.cols, a.top_k, a.rows, a.row_of, kThreads * (vec ? 8 : kNarrow * (pairs ? 2 : 1)), &blocks);
   if (s != HIF4_OK) return s;
-  auto kernel = vec ? combine_kernel<TI, TO, 8> : combine_kernel<TI, TO, 1>;
+  auto kernel = vec ? combine_kernel<TI, TO, 8, 1> : combine_kernel<TI, TO, 1, kNarrow>;
   if constexpr (sizeof(TI) == 2 && sizeof(TO) == 2)
-    if (pairs) kernel = combine_kernel<TI, TO, 2>;
+    if (pairs) kernel = combine_kernel<TI, TO, 2, kNarrow>;
   return launch_overlapped(kernel, static_cast<unsigned>(blocks), kThreads, 0, st, g,
                            static_cast<const TI*>(a.in), a.ld_in, a.weights, static_cast<const TO*>(a.residual), a.ld_residual, a.res_scale,
                            static_cast<TO*>(a.y), a.ld_y);
@@ -544,10 +605,14 @@ hif4_status launch_combine_backward(const hif4_combine_backward_args& a, cudaStr
   if (s != HIF4_OK) return s;
   // a warp a row where there are enough of them for all SMs, else a block a token
   const int64_t assignments = a.tokens * a.top_k;
-  if (assignments >= 8ll * sm_count())
-    return launch_overlapped(vec ? combine_backward_rows_kernel<TD, TI, 8> : combine_backward_rows_kernel<TD, TI, 1>,
-                             static_cast<unsigned>(ceil_div64(assignments, kThreads / 32)), kThreads, 0, st, g, assignments, static_cast<const TD*>(a.dy),
+  if (assignments >= 8ll * sm_count()) {
+    auto kernel = vec ? combine_backward_rows_kernel<TD, TI, 8> : combine_backward_rows_kernel<TD, TI, 1>;
+    if constexpr (sizeof(TI) == 2 && sizeof(TD) == 2)
+      if (!vec && words_aligned(a.dy, a.ld_dy, a.cols) && (!a.dweights || words_aligned(a.in, a.ld_in, a.cols)) && (!a.din || words_aligned(a.din, a.ld_din, a.cols)))
+        kernel = combine_backward_rows_kernel<TD, TI, 2>;
+    return launch_overlapped(kernel, static_cast<unsigned>(ceil_div64(assignments, kThreads / 32)), kThreads, 0, st, g, assignments, static_cast<const TD*>(a.dy),
                              a.ld_dy, a.weights, static_cast<const TI*>(a.in), a.ld_in, static_cast<TI*>(a.din), a.ld_din, a.dweights);
+  }
   // as many threads as go over the row in equal rounds
   const int64_t words = ceil_div64(a.cols > 0 ? a.cols : 1, vec ? 8 : 1), rounds = ceil_div64(words, kThreads);
   const unsigned threads = static_cast<unsigned>(ceil_div64(ceil_div64(words, rounds), 32) * 32);
@@ -610,7 +675,7 @@ extern "C" hif4_status hif4_expert_plan(const int32_t* ids, int64_t tokens, int6
 extern "C" hif4_status hif4_dispatch(const hif4_dispatch_args* args, void* stream) {
   if (!args) return HIF4_ERR_NULL;
   const hif4_dispatch_args& a = *args;
-  hif4_status s = check_sizes(a.tokens, a.cols, a.top_k, a.rows);
+  const hif4_status s = check_sizes(a.tokens, a.cols, a.top_k, a.rows);
   if (s != HIF4_OK) return s;
   if (!type_ok(a.dt) || a.kind < HIF4_ROWS_PLAIN || a.kind > HIF4_ROWS_NVFP4 || (a.kind == HIF4_ROWS_HIF4 && a.mode != HIF4_RNE && a.mode != HIF4_RHA))
     return HIF4_ERR_DTYPE;
@@ -627,15 +692,11 @@ extern "C" hif4_status hif4_dispatch(const hif4_dispatch_args* args, void* strea
     return a.dt == HIF4_BF16   ? launch_converted<__nv_bfloat16>(a, st)
            : a.dt == HIF4_FP16 ? launch_converted<__half>(a, st)
                                : launch_converted<float>(a, st);
-  Gather g;
-  int64_t blocks = 0;
   const int64_t e = type_size(a.dt);
   const uintptr_t all = bits(a.x) | bits(a.out) | static_cast<uintptr_t>(a.cols * e) | static_cast<uintptr_t>(a.tokens > 1 ? a.ld_x * e : 0) |
                         static_cast<uintptr_t>(a.rows > 1 ? a.ld_out * e : 0);
   const int64_t word = all % 16 == 0 ? 16 : all % 4 == 0 ? 4 : 2;
-  s = make_gather(g, a.tokens, a.cols, a.top_k, a.rows, a.row_of, kThreads * word / e, &blocks);
-  if (s != HIF4_OK) return s;
-  return word == 16 ? launch_plain<uint4>(g, blocks, a, st) : word == 4 ? launch_plain<uint32_t>(g, blocks, a, st) : launch_plain<uint16_t>(g, blocks, a, st);
+  return word == 16 ? launch_plain<uint4, 1>(a, st) : word == 4 ? launch_plain<uint32_t, kNarrow>(a, st) : launch_plain<uint16_t, kNarrow>(a, st);
 }
 
 extern "C" hif4_status hif4_combine(const hif4_combine_args* args, void* stream) {
