@@ -116,6 +116,18 @@ def test_route_equal_scores_and_close_ones(hif4):
     check_route(hif4, close, 8, torch.randn(64, generator=g, device="cuda") * 2.0 ** -30, score=SOFTMAX)
 
 
+@pytest.mark.parametrize("E,groups,kept,k", [(256, 1, 1, 8), (256, 8, 4, 8), (40, 1, 1, 32), (32, 1, 1, 32), (168, 8, 7, 15), (66, 2, 1, 9), (775, 31, 5, 32), (96, 32, 3, 6)])
+@pytest.mark.parametrize("score", [SOFTMAX, SIGMOID])
+def test_route_few_values(hif4, E, groups, kept, k, score):
+    """Logits and biases of few values: most neighbours are equal, and some equal sums are of different terms."""
+    g = gen(E + k)
+    logits = torch.randint(-6, 7, (200, E), generator=g, device="cuda").bfloat16() / 4
+    bias = torch.randint(0, 3, (E,), generator=g, device="cuda") / 64.0
+    for b in (None, bias, torch.zeros_like(bias)):
+        for best in (1, 2):
+            check_route(hif4, logits, k, b, score=score, groups=groups, top_groups=kept, group_best=best)
+
+
 @pytest.mark.parametrize("score", [SOFTMAX, SIGMOID])
 def test_route_masked_and_special_logits(hif4, score):
     g = gen(9)
