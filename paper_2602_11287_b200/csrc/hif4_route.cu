@@ -294,9 +294,11 @@ __device__ __forceinline__ int choose(const T* row, const float (&x)[V], const f
     const Key end = __shfl_sync(kAll, mine, found - 1);
     doubt = doubt && lane + 1 < found && !(xs == xn && bs == bn);
     if (first != none) {                                // of those left, all that are as near to the last have to be its equals
+      float again[V];                                   // (held until here, the logits' registers would cost the common path)
+      load_logits(row, p, lane, again);
 #pragma unroll
       for (int i = 0; i < V; ++i)
-        doubt |= !((used >> i) & 1u) && c[i] != none && !(x[i] == xl && b[i] == bl) && !told_apart(end, c[i], near);
+        doubt |= !((used >> i) & 1u) && c[i] != none && !(again[i] == xl && b[i] == bl) && !told_apart(end, c[i], near);
     }
     contested = __any_sync(kAll, doubt);
   }
