@@ -7,7 +7,7 @@
 // The order is that of the choices in 64 bits: two experts whose choices differ by less than FP32 holds would change
 // places from one implementation to the next.  Choices are made in FP32 first, whose error is bounded (below); only where two
 // that are neighbours in the order, or the last group kept and the first left, are nearer than that, the warp starts again in
-// 64 bits.  16384 tokens x 256 experts in 8 groups, top 8, FP32: 24 us (74 us with every choice in 64 bits, 64-bit shuffles and a lane
+// 64 bits.  16384 tokens x 256 experts in 8 groups, top 8, FP32: 25 us (74 us with every choice in 64 bits, 64-bit shuffles and a lane
 // per group); 15 us without groups and bias.  Bound by instruction issue, 71 % busy with 1050 warp instructions a token, of which
 // 430 stay with one expert chosen; the 16.8 MB of logits would take 2.6 us.  More or fewer tokens a warp change nothing.
 #include "hif4_tc_common.cuh"
