@@ -143,7 +143,9 @@ __device__ __forceinline__ void best_two(const Key (&c)[V], uint32_t used, Key n
 // Errors in FP32: a sigmoid 1 / (1 + e) with e = exp2(-x log2 e): 2^-22 from exp2 and 1.5 |x| 2^-24 from its argument reach the
 // result through e / (1 + e)^2 <= 1/4 (and |x| e / (1 + e)^2 < 0.23), 1 + e and the reciprocal add 2^-24 + 2^-23: together below
 // 1.1 2^-22, two of them below 2^-20.  A softmax the same relative to the largest, whose sum adds as much again: 2^-19.  The bias's
-// addition: 2^-24 of the sum, two of them 2^-23, a group's sum of two as much again.
+// addition: 2^-24 of the choice, two of them 2^-23.  A group's value is off by its terms' errors, however small a sum they leave (one
+// large and positive, one large and negative), and by 2^-24 of itself: together 2^-23 of the terms' magnitudes and, next to it, the two
+// scores' `near`.  Groups are therefore told apart by bounds of their own: the lowest of those kept against the highest of those left.
 //
 // Neighbours with the same logit and bias are equal in any arithmetic, and in their places by index: BF16 logits have such in
 // most rows (16384 tokens x 256 experts in 8 groups without bias: 47 us where they are chosen again, 28 us as here; 264 tokens 10.6, 5.1).
@@ -183,10 +185,10 @@ __device__ __forceinline__ int choose(const T* row, const float (&x)[V], const f
 #pragma unroll
     for (int i = 0; i < V; ++i) c[i] = x[i] > -kInf ? K::of(v[i] + static_cast<Real>(b[i])) : none;
   }
-  const auto told_apart = [&](Key high, Key low, Real margin) {      // (a key of none is far from all others)
+  const auto told_apart = [&](Key high, Key low) {      // (a key of none is far from all others)
     if (p.by_logit || kWide || low == none) return true;
     const Real h = K::value(high), l = K::value(low);
-    return h - l > margin + static_cast<Real>(0x1p-21) * fmaxf(fabsf(h), fabsf(l));
+    return h - l > near + static_cast<Real>(0x1p-21) * fmaxf(fabsf(h), fabsf(l));
   };
   const auto sum_of = [&](Key first, Key second) {
     return p.group_best == 1 ? first : first == none || second == none ? none : K::of(K::value(first) + K::value(second));
@@ -229,14 +231,22 @@ __device__ __forceinline__ int choose(const T* row, const float (&x)[V], const f
     bool free = own < p.groups;
     if (!free) value = none;
     uint32_t open = 0u;
-    Key last = none;
     for (int n = 0; n < p.top_groups; ++n) {
-      last = K::warp_max(free ? value : none);
-      const int g = __shfl_sync(kAll, own, __ffs(__ballot_sync(kAll, free && value == last)) - 1);
+      const Key best = K::warp_max(free ? value : none);
+      const int g = __shfl_sync(kAll, own, __ffs(__ballot_sync(kAll, free && value == best)) - 1);
       open |= 1u << g;
       if (own == g) free = false;
     }
-    contested = !told_apart(last, K::warp_max(free ? value : none), 2 * near);
+    if constexpr (!kWide) {
+      if (!p.by_logit) {                                // (an infinite value is exact, and so is that of a group that has none)
+        const bool there = value != none, kept = own < p.groups && !free;
+        const float v = K::value(value), terms = fabsf(K::value(f)) + (p.group_best == 2 ? fabsf(K::value(s)) : 0.0f);
+        const float off = v == kInf ? 0.0f : near + 0x1p-22f * terms;
+        const Key highest = K::warp_max(free && there ? K::of(v + off) : none);
+        const Key lowest = ~K::warp_max(~K::of(kept && there ? v - off : kInf));
+        contested = highest != none && !(lowest > highest);
+      }
+    }
     if (whole) {
       if (own >= p.groups || !((open >> own) & 1u)) first = second = none;
     } else {
@@ -286,7 +296,7 @@ __device__ __forceinline__ int choose(const T* row, const float (&x)[V], const f
   }
   __syncwarp();
   if (kWide || contested) return id;
-  bool doubt = here && !told_apart(mine, next, near);
+  bool doubt = here && !told_apart(mine, next);
   if (__any_sync(kAll, doubt)) {
     const float xs = here ? to_f32(row[id]) : 0.0f, bs = here && p.bias ? p.bias[id] : 0.0f;
     const float xn = __shfl_down_sync(kAll, xs, 1), bn = __shfl_down_sync(kAll, bs, 1);
@@ -298,7 +308,7 @@ __device__ __forceinline__ int choose(const T* row, const float (&x)[V], const f
       load_logits(row, p, lane, again);
 #pragma unroll
       for (int i = 0; i < V; ++i)
-        doubt |= !((used >> i) & 1u) && c[i] != none && !(again[i] == xl && b[i] == bl) && !told_apart(end, c[i], near);
+        doubt |= !((used >> i) & 1u) && c[i] != none && !(again[i] == xl && b[i] == bl) && !told_apart(end, c[i]);
     }
     contested = __any_sync(kAll, doubt);
   }

@@ -1,0 +1,45 @@
+"""Routing where FP32 cannot tell groups apart: sums of two choices that cancel."""
+import pytest
+import torch
+
+from tests.test_gpu_experts import SIGMOID, SOFTMAX, check_route, gen, hif4  # noqa: F401  (hif4: fixture)
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("bias,logits,kept", [
+    ([65536.0, -65536.0, 65536.0, -65536.0], [1.441, -1.237, -0.774, 0.967], 1),
+    ([1000.0, -1000.0, 1000.0, -1000.0], [-6.648e-5, -5.265e-5, -1.2645e-4, 5.188e-5], 1)])
+def test_a_cancelling_sum_of_two(hif4, bias, logits, kept):  # noqa: F811
+    """The sums of the groups differ by less than FP32 keeps of their terms: the second group's is larger in 64 bits."""
+    x, b = torch.tensor([logits], device="cuda"), torch.tensor(bias, device="cuda")
+    ids, _ = check_route(hif4, x, 2, b, score=SIGMOID, groups=2, top_groups=kept, group_best=2)
+    assert ids.tolist() == [[2, 3]]
+
+
+# (E, groups): groups of whole lanes, of several lanes, of parts of lanes, many experts a lane
+@pytest.mark.parametrize("E,groups,kept,k", [(4, 2, 1, 2), (256, 8, 4, 8), (512, 8, 4, 6), (160, 8, 3, 6), (96, 32, 5, 4), (775, 31, 9, 12), (1024, 4, 2, 32)])
+@pytest.mark.parametrize("size", [1.0, 16.0, 256.0, 4096.0, 65536.0])
+@pytest.mark.parametrize("score", [SOFTMAX, SIGMOID])
+def test_groups_with_biases_of_both_signs(hif4, E, groups, kept, k, size, score):  # noqa: F811
+    """One expert of a group with a bias of +size, the others with -size."""
+    g = gen(E + int(size))
+    per = E // groups
+    bias = torch.full((groups, per), -size, device="cuda")
+    bias.scatter_(1, torch.randint(0, per, (groups, 1), generator=g, device="cuda"), size)
+    for spread in (1.0, size * 2.0 ** -18):                # and logits whose scores differ by about the rounding of such a bias
+        logits = spread * torch.randn(4000, E, generator=g, device="cuda")
+        for best in (1, 2):
+            check_route(hif4, logits, k, bias.view(-1), score=score, groups=groups, top_groups=kept, group_best=best)
+
+
+@pytest.mark.parametrize("score", [SOFTMAX, SIGMOID])
+def test_a_kept_group_of_large_terms(hif4, score):  # noqa: F811
+    """Not the last kept group but the first one has the terms that FP32 cannot hold."""
+    g = gen(7)
+    E, groups, per = 64, 8, 8
+    bias = torch.zeros(groups, per, device="cuda")
+    bias[2, 1], bias[2, 2:] = 2.0 ** 17, -(2.0 ** 17)
+    bias[2, 0] = -(2.0 ** 17)
+    logits = 2.0 ** -6 * torch.randn(4000, E, generator=g, device="cuda")
+    check_route(hif4, logits, 8, bias.view(-1), score=score, groups=groups, top_groups=3, group_best=2)
