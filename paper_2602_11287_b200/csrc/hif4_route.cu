@@ -144,8 +144,9 @@ __device__ __forceinline__ void best_two(const Key (&c)[V], uint32_t used, Key n
 // result through e / (1 + e)^2 <= 1/4 (and |x| e / (1 + e)^2 < 0.23), 1 + e and the reciprocal add 2^-24 + 2^-23: together below
 // 1.1 2^-22, two of them below 2^-20.  A softmax the same relative to the largest, whose sum adds as much again: 2^-19.  The bias's
 // addition: 2^-24 of the choice, two of them 2^-23.  A group's value is off by its terms' errors, however small a sum they leave (one
-// large and positive, one large and negative), and by 2^-24 of itself: together 2^-23 of the terms' magnitudes and, next to it, the two
-// scores' `near`.  Groups are therefore told apart by bounds of their own: the lowest of those kept against the highest of those left.
+// large and positive, one large and negative), and by 2^-24 of itself: half the sum of two by 2^-24 of the terms' magnitudes (twice that
+// with the rounding of its bounds) and half of `near`, which is two scores' error.  So groups are told apart by bounds of their own,
+// the lowest of those kept against the highest of those left.
 //
 // Neighbours with the same logit and bias are equal in any arithmetic, and in their places by index: BF16 logits have such in
 // most rows (16384 tokens x 256 experts in 8 groups without bias: 47 us where they are chosen again, 28 us as here; 264 tokens 10.6, 5.1).
@@ -190,8 +191,9 @@ __device__ __forceinline__ int choose(const T* row, const float (&x)[V], const f
     const Real h = K::value(high), l = K::value(low);
     return h - l > near + static_cast<Real>(0x1p-21) * fmaxf(fabsf(h), fabsf(l));
   };
-  const auto sum_of = [&](Key first, Key second) {
-    return p.group_best == 1 ? first : first == none || second == none ? none : K::of(K::value(first) + K::value(second));
+  // half of the sum of two, whose order is the same: a sum of two finite choices may be none that FP32 holds
+  const auto half_sum = [&](Key first, Key second) {
+    return p.group_best == 1 ? first : first == none || second == none ? none : K::of(Real(0.5) * K::value(first) + Real(0.5) * K::value(second));
   };
   contested = false;
 
@@ -227,7 +229,7 @@ __device__ __forceinline__ int choose(const T* row, const float (&x)[V], const f
       s = max(min(f, f2), max(s, s2));
       f = max(f, f2);
     }
-    Key value = sum_of(f, s);
+    Key value = half_sum(f, s);
     bool free = own < p.groups;
     if (!free) value = none;
     uint32_t open = 0u;
@@ -240,8 +242,8 @@ __device__ __forceinline__ int choose(const T* row, const float (&x)[V], const f
     if constexpr (!kWide) {
       if (!p.by_logit) {                                // (an infinite value is exact, and so is that of a group that has none)
         const bool there = value != none, kept = own < p.groups && !free;
-        const float v = K::value(value), terms = fabsf(K::value(f)) + (p.group_best == 2 ? fabsf(K::value(s)) : 0.0f);
-        const float off = v == kInf ? 0.0f : near + 0x1p-22f * terms;
+        const float v = K::value(value), terms = 0x1p-23f * fabsf(K::value(f)) + 0x1p-23f * fabsf(K::value(p.group_best == 2 ? s : f));
+        const float off = v == kInf ? 0.0f : 0.5f * near + terms;
         const Key highest = K::warp_max(free && there ? K::of(v + off) : none);
         const Key lowest = ~K::warp_max(~K::of(kept && there ? v - off : kInf));
         contested = highest != none && !(lowest > highest);

@@ -1,4 +1,6 @@
-"""Routing where FP32 cannot tell groups apart: sums of two choices that cancel."""
+"""Routing where FP32 cannot tell groups apart: sums of two choices that cancel or overflow."""
+import math
+
 import pytest
 import torch
 
@@ -43,3 +45,40 @@ def test_a_kept_group_of_large_terms(hif4, score):  # noqa: F811
     bias[2, 0] = -(2.0 ** 17)
     logits = 2.0 ** -6 * torch.randn(4000, E, generator=g, device="cuda")
     check_route(hif4, logits, 8, bias.view(-1), score=score, groups=groups, top_groups=3, group_best=2)
+
+
+@pytest.mark.parametrize("score", [SOFTMAX, SIGMOID])
+@pytest.mark.parametrize("E,groups", [(6, 3), (256, 8), (160, 8), (96, 32)])
+def test_groups_masked_by_the_lowest_value(hif4, score, E, groups):  # noqa: F811
+    """Experts masked by FP32's lowest value can be chosen, those masked by -inf cannot: a group's sum of two lowest values is no -inf.
+    Sums of two largest values are no +inf either."""
+    g = gen(E)
+    per = E // groups
+    low = torch.finfo(torch.float32).min
+    logits = torch.randn(50, E, generator=g, device="cuda")
+    for fills in ((-math.inf, low, 0.0), (low, -math.inf, 0.0), (low, low, -math.inf), (-low, -low, 0.0), (0.0, -low, -low)):
+        bias = torch.zeros(groups, per, device="cuda")
+        for at, fill in enumerate(fills):
+            bias[at] = fill
+        bias[3:] = -math.inf
+        for kept in (1, 2, 3):
+            ids, _ = check_route(hif4, logits, min(2 * kept, 8), bias.view(-1), score=score, groups=groups, top_groups=kept, group_best=2)
+    bias = torch.full((groups, per), -math.inf, device="cuda")
+    bias[1], bias[2] = low, 0.0
+    ids, _ = check_route(hif4, logits, 4, bias.view(-1), score=score, groups=groups, top_groups=2, group_best=2)
+    if per == 2:                                           # the third group's two, then the second's
+        assert bool((ids[:, :2] >= 4).all()) and bool(((ids[:, 2:] == 2) | (ids[:, 2:] == 3)).all())
+
+
+@pytest.mark.parametrize("score", [SOFTMAX, SIGMOID])
+def test_groups_with_infinite_biases(hif4, score):  # noqa: F811
+    """An expert with a bias of +inf is chosen first, and so is its group; several such go by index."""
+    g = gen(11)
+    logits = torch.randn(300, 256, generator=g, device="cuda")
+    bias = 0.1 * torch.randn(256, generator=g, device="cuda")
+    for places in ([5], [5, 6], [5, 100], [5, 100, 200, 250]):
+        b = bias.clone()
+        b[places] = math.inf
+        for best in (1, 2):
+            for kept in (1, 3):
+                check_route(hif4, logits, 8, b, score=score, groups=8, top_groups=kept, group_best=best)
