@@ -142,11 +142,14 @@ __device__ __forceinline__ void best_two(const Key (&c)[V], uint32_t used, Key n
 //
 // Errors in FP32: a sigmoid 1 / (1 + e) with e = exp2(-x log2 e): 2^-22 from exp2 and 1.5 |x| 2^-24 from its argument reach the
 // result through e / (1 + e)^2 <= 1/4 (and |x| e / (1 + e)^2 < 0.23), 1 + e and the reciprocal add 2^-24 + 2^-23: together below
-// 1.1 2^-22, two of them below 2^-20.  A softmax the same relative to the largest, whose sum adds as much again: 2^-19.  The bias's
-// addition: 2^-24 of the choice, two of them 2^-23.  A group's value is off by its terms' errors, however small a sum they leave (one
-// large and positive, one large and negative), and by 2^-24 of itself: half the sum of two by 2^-24 of the terms' magnitudes (twice that
-// with the rounding of its bounds) and half of `near`, which is two scores' error.  So groups are told apart by bounds of their own,
-// the lowest of those kept against the highest of those left.
+// 1.1 2^-22, two of them below 2^-20.  A softmax: terms, relative to the largest, 1.21 2^-22, two of them 2.4 2^-22.  Their sum over
+// at most 1024 experts: 3.5 2^-22 from the terms (their mean distance from the largest, weighted by them, is below 4.5), (V + 4) 2^-24 from the additions; it
+// and quotient and products (0.8 2^-22) move the distance of two scores by that part of it: together below (32 + V) 2^-24 of the
+// largest.  The bias's addition: 2^-24 of the choice, two of them 2^-23.
+// A group's value is off by its terms' errors, however small a sum they leave (one large and positive, one large and negative), and by
+// 2^-24 of itself: half the sum of two by 2^-24 of the terms' magnitudes (twice that with the rounding of its bounds) and half of
+// `near`, which is two scores' error.  So groups are told apart by bounds of their own, the lowest of those kept against the highest of
+// those left.
 //
 // Neighbours with the same logit and bias are equal in any arithmetic, and in their places by index: BF16 logits have such in
 // most rows (16384 tokens x 256 experts in 8 groups without bias: 47 us where they are chosen again, 28 us as here; 264 tokens 10.6, 5.1).
@@ -181,7 +184,7 @@ __device__ __forceinline__ int choose(const T* row, const float (&x)[V], const f
       const Real inv = total > 0 ? Real(1) / total : Real(0);
 #pragma unroll
       for (int i = 0; i < V; ++i) v[i] = kWide ? (total > 0 ? v[i] / total : v[i]) : v[i] * inv;
-      near = static_cast<Real>(0x1p-19) * inv;
+      near = static_cast<Real>((32 + V) * 0x1p-24) * inv;
     }
 #pragma unroll
     for (int i = 0; i < V; ++i) c[i] = x[i] > -kInf ? K::of(v[i] + static_cast<Real>(b[i])) : none;

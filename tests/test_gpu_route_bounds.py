@@ -1,4 +1,4 @@
-"""Routing where FP32 cannot tell groups apart: sums of two choices that cancel or overflow."""
+"""Routing where FP32 cannot tell groups apart: sums of two choices that cancel or overflow, scores next to the error bound."""
 import math
 
 import pytest
@@ -82,3 +82,18 @@ def test_groups_with_infinite_biases(hif4, score):  # noqa: F811
         for best in (1, 2):
             for kept in (1, 3):
                 check_route(hif4, logits, 8, b, score=score, groups=8, top_groups=kept, group_best=best)
+
+
+@pytest.mark.parametrize("E,k", [(256, 8), (512, 8), (1024, 32)])
+def test_softmax_choices_next_to_the_error_bound(hif4, E, k):  # noqa: F811
+    """Biases that bring experts of different scores within a few 2^-22 of the largest score of one another, among many terms whose
+    rounded sum is off."""
+    g = gen(E)
+    depth = -7.0 - torch.rand(3000, 1, generator=g, device="cuda")
+    logits = depth.expand(-1, E).clone()
+    logits[:, 0] = 0.0
+    total = 1.0 + (E - 1) * depth[0, 0].double().exp()
+    bias = torch.zeros(E, device="cuda")
+    for n in range(1, k):                                  # expert n against the first: its bias makes up for the difference, nearly
+        bias[n] = ((1.0 - depth[0, 0].double().exp()) / total * (1.0 + (n - k // 2) * 2.0 ** -22)).float()
+    check_route(hif4, torch.cat([logits[:1].expand(3000, -1) + 2.0 ** -24 * torch.randn(3000, E, generator=g, device="cuda"), logits]), k, bias, score=SOFTMAX)
