@@ -38,19 +38,14 @@ bfp4_quantize_kernel(const T* __restrict__ src, int64_t rows, uint32_t n32, uint
   const WordTask t = word_task<kNv>(warp, words, lane);
   if (t.row >= rows) return;
   uint32_t sa = 0u, sb = 0u;                                              // (0 past the last block)
+  const float g = gain ? *gain : 1.0f;
   if (t.c < n32) {
     const T* p = src + t.row * ld + 32 * static_cast<int64_t>(t.c);
     const Raw16<T> ra = load_raw16(p, wide), rb = load_raw16(p + 16, wide);
     Sixteen a = sixteen_of(ra), b = sixteen_of(rb);
     uint32_t pa = peak16(ra), pb = peak16(rb);
     if (!kNv) pa = pb = max(pa, pb);
-    if (gain) {
-      const float g = *gain;
-      scale16(a, g);
-      scale16(b, g);
-      pa = scaled_peak(pa, g);
-      pb = kNv ? scaled_peak(pb, g) : pa;
-    }
+    if (gain) apply_gain<kNv>(a, b, pa, pb, g);
     const uint2 ca = encode16<kNv>(a, pa, sa), cb = encode16<kNv>(b, pb, sb);
     codes[t.row * n32 + t.c] = make_uint4(ca.x, ca.y, cb.x, cb.y);
   }
@@ -95,7 +90,7 @@ bfp4_quantize_transposed_kernel(const T* __restrict__ src, int64_t rows, int64_t
     for (int col = lane; col < kCols; col += 32) {
       const T* mine = tile + part * 32 * kCols + col;
       Sixteen a, b;
-      uint32_t pa = 0u, pb = 0u, sa, sb;
+      uint32_t pa, pb, sa, sb;
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
         a.p[k] = make_float2(to_f32(mine[2 * k * kCols]), to_f32(mine[(2 * k + 1) * kCols]));
@@ -105,11 +100,8 @@ bfp4_quantize_transposed_kernel(const T* __restrict__ src, int64_t rows, int64_t
         scale16(a, g);
         scale16(b, g);
       }
-#pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        pa = max(pa, max(__float_as_uint(a.p[k].x) & 0x7FFFFFFFu, __float_as_uint(a.p[k].y) & 0x7FFFFFFFu));
-        pb = max(pb, max(__float_as_uint(b.p[k].x) & 0x7FFFFFFFu, __float_as_uint(b.p[k].y) & 0x7FFFFFFFu));
-      }
+      pa = peak_of(a);
+      pb = peak_of(b);
       if (!kNv) pa = pb = max(pa, pb);
       const uint2 ca = encode16<kNv>(a, pa, sa), cb = encode16<kNv>(b, pb, sb);
       *reinterpret_cast<uint4*>(code_tile + col * kCodePitch + part * 16) = make_uint4(ca.x, ca.y, cb.x, cb.y);

@@ -125,10 +125,30 @@ __device__ __forceinline__ uint32_t peak16(const Raw16<float>& r) {
   for (int i = 0; i < 16; ++i) m = max(m, r.w[i] & 0x7FFFFFFFu);
   return m;
 }
-// The peak of the products with a gain is the product with the peak: rounding keeps the order.
-__device__ __forceinline__ uint32_t scaled_peak(uint32_t peak, float gain) { return __float_as_uint(fabsf(__fmul_rn(__uint_as_float(peak), gain))); }
+__device__ __forceinline__ uint32_t peak_of(const Sixteen& v) {
+  uint32_t m = 0u;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) m = max(m, max(__float_as_uint(v.p[i].x) & 0x7FFFFFFFu, __float_as_uint(v.p[i].y) & 0x7FFFFFFFu));
+  return m;
+}
 
 constexpr uint32_t kInfBits = 0x7F800000u, kMostBits = 0x7F7FFFFFu;
+// A gain multiplied into two runs of sixteen elements with these peaks.  The peak of the products with a finite gain is the product with the
+// peak: rounding keeps the order.  An infinite gain makes zeros NaN, which only the products show.
+template <bool kNv>
+__device__ __forceinline__ void apply_gain(Sixteen& a, Sixteen& b, uint32_t& pa, uint32_t& pb, float gain) {
+  scale16(a, gain);
+  scale16(b, gain);
+  const auto scaled = [gain](uint32_t peak) { return __float_as_uint(fabsf(__fmul_rn(__uint_as_float(peak), gain))); };
+  if ((__float_as_uint(gain) & 0x7FFFFFFFu) == kInfBits) {
+    pa = peak_of(a);
+    pb = peak_of(b);
+    if (!kNv) pa = pb = max(pa, pb);
+  } else {
+    pa = scaled(pa);
+    pb = kNv ? scaled(pb) : pa;
+  }
+}
 // a / b by the reciprocal y of b (within 2^-23 of its value) and one correction from the exact remainder: q0 = a y, q = q0 + (a - q0 b) y.
 // Before its last rounding q is off by 2^-45 of its value at most.  For b of up to four significant bits (an E4M3 scale, 6) and a of 24 no
 // quotient lies that near to the middle between two FP32 numbers: a = m b with an odd 25-bit m would need 26 bits.  So q is a / b

@@ -239,18 +239,13 @@ dispatch_bfp4_kernel(Gather g, const T* __restrict__ x, int64_t ld_x, const floa
   if (c >= padded) return;
   uint4 code = make_uint4(0u, 0u, 0u, 0u);
   uint32_t sa = 0u, sb = 0u;                             // (0 past the last block)
+  const float f = gain ? *gain : 1.0f;
   if (c < n32) {
     const Raw16<T> ra = load_raw16(x + t * ld_x + 32 * c, false), rb = load_raw16(x + t * ld_x + 32 * c + 16, false);
     Sixteen a = sixteen_of(ra), b = sixteen_of(rb);
     uint32_t pa = peak16(ra), pb = peak16(rb);
     if (!kNv) pa = pb = max(pa, pb);
-    if (gain) {
-      const float f = *gain;
-      scale16(a, f);
-      scale16(b, f);
-      pa = scaled_peak(pa, f);
-      pb = kNv ? scaled_peak(pb, f) : pa;
-    }
+    if (gain) apply_gain<kNv>(a, b, pa, pb, f);
     const uint2 ca = encode16<kNv>(a, pa, sa), cb = encode16<kNv>(b, pb, sb);
     code = make_uint4(ca.x, ca.y, cb.x, cb.y);
   }
