@@ -655,8 +655,8 @@ extern "C" hif4_status hif4_expert_plan(const int32_t* ids, int64_t tokens, int6
   const int runs = n == 0 ? 1 : static_cast<int>(ceil_div64(block_items, kPlanSteps * 32)), of_experts = static_cast<int>(ceil_div64(experts, 32));
   const int warps = runs > of_experts ? runs : of_experts < kPlanWarps ? of_experts : kPlanWarps;
   const int smem = static_cast<int>(experts) * runs * 4;
-  static uint64_t ready = 0;
-  if (smem > 48 * 1024 && !ensure_dynamic_smem(plan_place_kernel, HIF4_ROUTE_MAX_EXPERTS * kPlanWarps * 4, ready)) return HIF4_ERR_CUDA;
+  static uint64_t ready = 0;                             // (a launch that has not asked gets 48 KB, the kernel's own arrays included)
+  if (!ensure_dynamic_smem(plan_place_kernel, HIF4_ROUTE_MAX_EXPERTS * kPlanWarps * 4, ready)) return HIF4_ERR_CUDA;
   int32_t* counts = static_cast<int32_t*>(workspace);
   if (blocks > 1) {
     const hif4_status c = launch_overlapped(plan_count_kernel, static_cast<unsigned>(blocks), kPlanWarps * 32, static_cast<size_t>(experts) * 4, st, ids, n,
