@@ -312,7 +312,7 @@ hif4_status check(const void* src, hif4_dtype dt, int64_t rows, int64_t cols, in
   if (rows == 0 || cols == 0) return HIF4_OK;
   if (cols / 16 + 1 > 0x7FFFFFFFll / (rows / 16 + 1)) return HIF4_ERR_SHAPE;      // more blocks than a grid has
   if (!src || !codes || !scales) return HIF4_ERR_NULL;
-  if (!aligned16(src) || (static_cast<size_t>(ld) * type_size(dt)) % 16 != 0 || !aligned16(codes) || !aligned16(scales) ||
+  if (!aligned16(src) || (rows > 1 && (static_cast<size_t>(ld) * type_size(dt)) % 16 != 0) || !aligned16(codes) || !aligned16(scales) ||
       (reinterpret_cast<uintptr_t>(gain) & 3u))
     return HIF4_ERR_ALIGN;
   return HIF4_OK;

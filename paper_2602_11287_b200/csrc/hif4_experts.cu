@@ -679,7 +679,7 @@ extern "C" hif4_status hif4_dispatch(const hif4_dispatch_args* args, void* strea
   if (a.tokens == 0 || a.cols == 0 || a.rows == 0) return HIF4_OK;
   if (!a.x || !a.row_of || !a.out || (scaled && !a.out_scales)) return HIF4_ERR_NULL;
   if (!aligned(a.row_of, 4) || !aligned(a.x, type_size(a.dt)) || (plain && !aligned(a.out, type_size(a.dt))) ||
-      (!plain && !rows_aligned(a.x, a.ld_x, a.dt)) || (a.kind == HIF4_ROWS_HIF4 && !aligned(a.out, 4)) ||
+      (!plain && !rows_aligned(a.x, a.tokens > 1 ? a.ld_x : 0, a.dt)) || (a.kind == HIF4_ROWS_HIF4 && !aligned(a.out, 4)) ||
       (scaled && (!aligned(a.out, 16) || !aligned(a.out_scales, 16) || !aligned(a.gain, 4))))
     return HIF4_ERR_ALIGN;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
