@@ -151,9 +151,11 @@ hif4_status hif4_grouped_gemm_workspace(int num_groups, int64_t total_rows, int6
  *   A_units            device, [total_rows, K/64] units, rows sorted by group.
  *   B_units            device, [num_groups, N, K/64] units.
  *   C                  device, [total_rows, N] FP32, row stride ldc.
- *   group_offsets_dev  device, num_groups+1 int64 prefix sums, off[0] = 0, off[num_groups] =
+ *   group_offsets_dev  device, num_groups+1 int64 prefix sums, off[0] = 0, off[num_groups] <=
  *                      total_rows, non-decreasing.  Read by the kernel only: routing results never
- *                      return to the host.  Empty groups are allowed.  */
+ *                      return to the host.  Empty groups are allowed.  Rows of C at and behind
+ *                      off[num_groups] (assignments without a row here: padding, experts held elsewhere)
+ *                      stay as they were.  */
 hif4_status hif4_grouped_gemm(const void* A_units, const void* B_units, float* C,
                               const int64_t* group_offsets_dev, int num_groups, int64_t total_rows,
                               int64_t N, int64_t K, int64_t ldc, void* workspace,

@@ -73,12 +73,8 @@ extern "C" hif4_status hif4_grouped_gemm_noalloc(const void* A_units, const void
   if (!aligned(A_units, 4) || !aligned(B_units, 4) || !aligned(C, 4) || !aligned(group_offsets_dev, 8))
     return HIF4_ERR_ALIGN;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  if (K == 0) {
-    if (cudaMemset2DAsync(C, static_cast<size_t>(ldc) * 4, 0, static_cast<size_t>(N) * 4,
-                          static_cast<size_t>(total_rows), st) != cudaSuccess)
-      return HIF4_ERR_CUDA;
-    return HIF4_OK;
-  }
+  if (K == 0)                            // zeros in the rows of the groups
+    return launch_grouped_gemm_simt(A_units, B_units, C, group_offsets_dev, num_groups, total_rows, N, K, ldc, st);
   if (!gemm_tc_supported(A_units, B_units, total_rows, static_cast<int64_t>(num_groups) * N, N, K)) {
     // K not a multiple of 256 or operands not 16-byte aligned: the CUDA-core kernel walks the
     // offsets itself and needs no scratch at all.
