@@ -382,8 +382,8 @@ typedef enum { HIF4_SCORE_SOFTMAX = 0, HIF4_SCORE_SIGMOID = 1 } hif4_score;
 
 /* hif4_route -- per token: scores s of the logits, choice c = s + bias, the `top_k` experts of the largest choice in
  * descending order (equal ones: the lowest index first), and their weights w = scale * s, or scale * s / (sum of the chosen s).
- *   groups    the experts are `groups` equal runs; a run's value is the sum of its `group_best` (1 or 2) largest choices, and
- *             only experts of the `top_groups` runs of the largest value are chosen.
+ *   groups    the experts are `groups` equal runs; a run's value is the sum of its `group_best` (1 or 2) largest choices (-inf where
+ *             fewer can be chosen), and only experts of the `top_groups` runs of the largest value are chosen.
  *   The order is that of the choices in 64 bits (of the logits themselves where there is no bias and no sum of two).
  *   Experts whose choice is -inf are not chosen: where none is left, the id is -1 and the weight 0.  A NaN counts as -inf in
  *   the choice, and every weight of its row is NaN (so too for an infinite logit under softmax).
@@ -434,8 +434,8 @@ typedef enum { HIF4_ROWS_PLAIN = 0, HIF4_ROWS_HIF4 = 1, HIF4_ROWS_MXFP4 = 2, HIF
 
 /* hif4_dispatch -- the experts' rows: out[row_of[t][j]] = x[t] for every assignment that has a row; a token is read and
  * converted once.  Converted rows are bit for bit those of hif4_quantize and hif4_bfp4_quantize.  Rows that no assignment
- * has stay as they were; a row number outside 0 .. rows - 1 is no row.  Row numbers differ (hif4_expert_plan's do): of two assignments with
- * the same one, either's token may be found there.  (Its gradient is hif4_combine without weights.)  */
+ * has stay as they were; a row number outside 0 .. rows - 1 is no row.  Row numbers differ (hif4_expert_plan's do): where two assignments have
+ * the same one, its row may be made of parts of both tokens.  (Its gradient is hif4_combine without weights.)  */
 typedef struct {
   int64_t tokens, cols, top_k, rows;
   const void* x;                 /* device, [tokens, cols] of dt, row stride ld_x elements; 16-byte aligned rows unless PLAIN */
@@ -470,7 +470,8 @@ typedef struct {
 hif4_status hif4_combine(const hif4_combine_args* args, void* stream);
 
 /* hif4_combine_backward -- din[row_of[t][j]] = weights[t][j] * dy[t], dweights[t][j] = <dy[t], in[row_of[t][j]]> (0 without a
- * row); the residual's gradient is res_scale * dy.  Rows of din that no assignment has stay as they were.  */
+ * row); the residual's gradient is res_scale * dy.  Rows of din that no assignment has stay as they were; row numbers differ,
+ * as for hif4_dispatch.  */
 typedef struct {
   int64_t tokens, cols, top_k, rows;
   const void* dy;                /* device, [tokens, cols] of dt                                               */

@@ -311,7 +311,9 @@ hif4_status product(const hif4_bfp4_gemm_args& a, bool grouped, void* stream) {
   // More than 64 tokens: 256 x 256 tiles on CTA pairs, unless few tiles have many chunks, which a cluster shares out here and one pair
   // has to walk alone, or so few that its longer start is not made up.  Pairs / clusters, us: 512 x 4096 x 4096 10.9 / 12.4,
   // 128 x 14336 x 4096 11.4 / 12.5, 256 x 4096 x 14336 22.1 / 16.4, 512 x 4096 x 14336 22.8 / 22.9, 2048 x 512 x 512 6.5 / 5.4;
-  // 64 x 4096 x 4096 9.9 / 8.4.
+  // 64 x 4096 x 4096 9.9 / 8.4.  The rule for K <= 512 looks at none but small Ys, where it is right (BF16 Y: 2048 x 512 x 512 6.5 / 5.2,
+  // 512 x 4096 x 512 6.5 / 5.2); of larger ones it takes the slower side (512 x 14336 x 512 8.3 / 12.0, 8192 x 4096 x 256 15.9 / 37.5,
+  // 4096 x 14336 x 512 28 / 69, 4096 x 32768 x 512 56 / 148).
   if (!grouped && a.M > 64 && p.chunks > 2 && (p.chunks <= 16 || ceil_div64(a.M, 256) * ceil_div64(a.N, 256) * 4 >= sm_count()))
     return launch_bfp4_pairs(b, p, st);
   // Groups (this kernel takes any number of them): pairs where a mean group fills more than half of their 256 rows.  Pairs / one CTA, us,

@@ -6,8 +6,8 @@
 //
 // The order is that of the choices in 64 bits: two experts whose choices differ by less than FP32 holds would change
 // places from one implementation to the next.  Choices are made in FP32 first, whose error is bounded (below); only where two
-// that are neighbours in the order, or the last group kept and the first left, are nearer than that, the warp starts again in
-// 64 bits.  16384 tokens x 256 experts in 8 groups, top 8, FP32: 25 us (74 us with every choice in 64 bits, 64-bit shuffles and a lane
+// that are neighbours in the order, or a group kept and one left, are nearer than that, the warp starts again in
+// 64 bits.  16384 tokens x 256 experts in 8 groups, top 8, FP32: 25 to 27 us (74 us with every choice in 64 bits, 64-bit shuffles and a lane
 // per group); 15 us without groups and bias.  Bound by instruction issue, 71 % busy with 1050 warp instructions a token, of which
 // 430 stay with one expert chosen; the 16.8 MB of logits would take 2.6 us.  More or fewer tokens a warp change nothing.
 #include "hif4_tc_common.cuh"
@@ -74,7 +74,8 @@ __device__ __forceinline__ float max_nan(float a, float b) {
 constexpr float kLog2e = 1.4426950408889634f;
 
 // Sigmoid of x times e^-m, m = min(0, largest x of the sum): a common factor of all terms of a ratio, so that no ratio of very
-// small sigmoids loses its terms.
+// small sigmoids loses its terms.  The reciprocal is off by an ulp at most, half an ulp more than a division, and less than the
+// exponential.
 __device__ __forceinline__ float sigmoid_scaled(float x, float m) {
   const float t = expf(-fabsf(x));
   return (x > 0.0f ? 1.0f : m == 0.0f ? t : expf(x - m)) * fast_rcp(1.0f + t);
@@ -143,9 +144,9 @@ __device__ __forceinline__ void best_two(const Key (&c)[V], uint32_t used, Key n
 // Errors in FP32: a sigmoid 1 / (1 + e) with e = exp2(-x log2 e): 2^-22 from exp2 and 1.5 |x| 2^-24 from its argument reach the
 // result through e / (1 + e)^2 <= 1/4 (and |x| e / (1 + e)^2 < 0.23), 1 + e and the reciprocal add 2^-24 + 2^-23: together below
 // 1.1 2^-22, two of them below 2^-20.  A softmax: terms, relative to the largest, 1.21 2^-22, two of them 2.4 2^-22.  Their sum over
-// at most 1024 experts: 3.5 2^-22 from the terms (their mean distance from the largest, weighted by them, is below 4.5), (V + 4) 2^-24 from the additions; it
-// and quotient and products (0.8 2^-22) move the distance of two scores by that part of it: together below (32 + V) 2^-24 of the
-// largest.  The bias's addition: 2^-24 of the choice, two of them 2^-23.
+// at most 1024 experts: 3.5 2^-22 from the terms (their mean distance from the largest logit, weighted by them, is below 4.5),
+// (V + 4) 2^-24 from the additions; it and quotient and products (0.8 2^-22) move the distance of two scores by that part of it: together
+// below (32 + V) 2^-24 of the largest.  The bias's addition: 2^-24 of the choice, two of them 2^-23.
 // A group's value is off by its terms' errors, however small a sum they leave (one large and positive, one large and negative), and by
 // 2^-24 of itself: half the sum of two by 2^-24 of the terms' magnitudes (twice that with the rounding of its bounds) and half of
 // `near`, which is two scores' error.  So groups are told apart by bounds of their own, the lowest of those kept against the highest of

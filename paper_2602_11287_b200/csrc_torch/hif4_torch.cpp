@@ -1,6 +1,6 @@
-// The calls between two linears of a block, around the experts' products and in microscaled formats for PyTorch tensors: checks, output and workspace allocation, current stream, and
-// the C call, without the interpreter in between (a call of one token costs the host less than the GPU).  The Python names,
-// defaults and documentation are in binding.py, which passes every argument by position.
+// The calls between two linears of a block, around the experts' products and in microscaled formats for PyTorch tensors: checks,
+// output and workspace allocation, current stream, and the C call, without the interpreter in between (a call of one token costs the
+// host less than the GPU).  The Python names, defaults and documentation are in binding.py, which passes every argument by position.
 //
 // A function returns its result, or the status code (a Python int) of a C call that refused its arguments; arguments that are
 // not what they should be raise ValueError or TypeError.
