@@ -155,7 +155,7 @@ hif4_status hif4_grouped_gemm_workspace(int num_groups, int64_t total_rows, int6
  *                      total_rows, non-decreasing.  Read by the kernel only: routing results never
  *                      return to the host.  Empty groups are allowed.  Rows of C at and behind
  *                      off[num_groups] (assignments without a row here: padding, experts held elsewhere)
- *                      stay as they were.  */
+ *                      stay as they were.  Offsets are clamped to 0 .. total_rows.  */
 hif4_status hif4_grouped_gemm(const void* A_units, const void* B_units, float* C,
                               const int64_t* group_offsets_dev, int num_groups, int64_t total_rows,
                               int64_t N, int64_t K, int64_t ldc, void* workspace,

@@ -261,8 +261,8 @@ def hif4_grouped_gemm(a_units: torch.Tensor, b_units: torch.Tensor, group_offset
                       out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
                       stream=None) -> torch.Tensor:
     """Per group g: C[off[g]:off[g+1]] = A[off[g]:off[g+1]] @ B[g]^T; B is [G, N, K/64, 36] and
-    `group_offsets` a device int64 tensor of G+1 prefix sums.  Rows behind the last group (where assignments have been
-    dropped) are left as they are (undefined without out)."""
+    `group_offsets` a device int64 tensor of G+1 prefix sums, clamped to the rows.  Rows behind the last group (where
+    assignments have been dropped) are left as they are (undefined without out)."""
     _need_cuda(a_units, b_units, group_offsets, out, workspace)
     assert a_units.dtype == torch.uint8 and b_units.dtype == torch.uint8 and group_offsets.dtype == torch.int64
     assert a_units.dim() == 3 and b_units.dim() == 4 and a_units.shape[1] == b_units.shape[2]

@@ -4,6 +4,9 @@
 
 namespace hif4 {
 
+// A group's offset as a row number: the rows may be fewer than the assignments that the offsets count.
+__device__ __forceinline__ int64_t clamp_row(int64_t offset, int64_t total_rows) { return max(static_cast<int64_t>(0), min(total_rows, offset)); }
+
 // CUDA-core path: any M, N, K % 64 == 0, 4-byte aligned operands.
 hif4_status launch_gemm_simt(const void* A, const void* B, float* C, int64_t M, int64_t N, int64_t K,
                              int64_t ldc, cudaStream_t st);

@@ -62,8 +62,8 @@ gemm_simt_kernel(const uint32_t* __restrict__ A, const uint32_t* __restrict__ B,
     int g = 0;
     int64_t lo = 0, hi = 0;
     for (; g < num_groups; ++g) {
-      lo = offsets[g]; hi = offsets[g + 1];
-      const int64_t tiles = (hi - lo + kTile - 1) / kTile;
+      lo = clamp_row(offsets[g], M); hi = clamp_row(offsets[g + 1], M);
+      const int64_t tiles = hi > lo ? (hi - lo + kTile - 1) / kTile : 0;
       if (tile < tiles) break;
       tile -= tiles;
     }

@@ -271,13 +271,13 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
 
 // Builds the m-tile table of a grouped problem from the device-side offsets: one entry per 128-row
 // tile of every non-empty group, then invalid entries up to `max_tiles`.
-__global__ void build_mtile_table_kernel(const int64_t* __restrict__ offsets, int num_groups, MTile* table,
+__global__ void build_mtile_table_kernel(const int64_t* __restrict__ offsets, int num_groups, int64_t total_rows, MTile* table,
                                          int max_tiles) {
   __shared__ int s_total;
   if (threadIdx.x == 0) {
     int n = 0;
     for (int g = 0; g < num_groups; ++g) {
-      const int64_t lo = offsets[g], hi = offsets[g + 1];
+      const int64_t lo = clamp_row(offsets[g], total_rows), hi = clamp_row(offsets[g + 1], total_rows);
       for (int64_t r = lo; r < hi && n < max_tiles; r += BM) {
         table[n].row0 = static_cast<int>(r);
         table[n].row_end = static_cast<int>(hi);
@@ -342,7 +342,7 @@ hif4_status launch_grouped_gemm_tc(const void* A, const void* B, float* C, const
                                    cudaStream_t st) {
   const int max_tiles = static_cast<int>(ceil_div64(total_rows, BM) + num_groups);
   MTile* table = static_cast<MTile*>(workspace);
-  build_mtile_table_kernel<<<1, 256, 0, st>>>(offsets, num_groups, table, max_tiles);
+  build_mtile_table_kernel<<<1, 256, 0, st>>>(offsets, num_groups, total_rows, table, max_tiles);
   note_launch();
   if (cudaGetLastError() != cudaSuccess) return HIF4_ERR_CUDA;
   GemmParams p{};

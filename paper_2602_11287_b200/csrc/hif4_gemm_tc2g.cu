@@ -91,7 +91,7 @@ struct GroupedParams {
 // of the list; block 0 writes the record count.  Groups are taken 256 at a time.
 constexpr int kTableBlocks = 16;
 __global__ void __launch_bounds__(256)
-build_work_table_kernel(const int64_t* __restrict__ offsets, int num_groups, int64_t N, int n_wtiles, uint8_t* table_mem,
+build_work_table_kernel(const int64_t* __restrict__ offsets, int num_groups, int64_t total_rows, int64_t N, int n_wtiles, uint8_t* table_mem,
                         int max_records) {
   __shared__ int warp_sums[8];
   __shared__ int s_first[257];                 // first record of each group of the batch (relative), and their total
@@ -104,7 +104,7 @@ build_work_table_kernel(const int64_t* __restrict__ offsets, int num_groups, int
   for (int g0 = 0; g0 < num_groups; g0 += 256) {
     const int g = g0 + threadIdx.x;
     int64_t lo = 0, hi = 0;
-    if (g < num_groups) { lo = offsets[g]; hi = offsets[g + 1]; }
+    if (g < num_groups) { lo = clamp_row(offsets[g], total_rows); hi = clamp_row(offsets[g + 1], total_rows); }
     if (hi < lo) hi = lo;
     const int64_t rows = hi - lo;
     const int64_t full = rows / kMaxTok;
@@ -633,7 +633,7 @@ hif4_status launch_grouped_gemm_tc2(const void* A, const void* B, float* C, cons
   const int64_t max_records = (ceil_div64(total_rows, kMaxTok) + num_groups) * n_wtiles;
   if (max_records > 0x7FFFFFFFll) return HIF4_ERR_SHAPE;
   uint8_t* table_mem = static_cast<uint8_t*>(workspace);
-  build_work_table_kernel<<<kTableBlocks, 256, 0, st>>>(offsets, num_groups, N, n_wtiles, table_mem, static_cast<int>(max_records));
+  build_work_table_kernel<<<kTableBlocks, 256, 0, st>>>(offsets, num_groups, total_rows, N, n_wtiles, table_mem, static_cast<int>(max_records));
   note_launch();
   if (cudaGetLastError() != cudaSuccess) return HIF4_ERR_CUDA;
   GroupedParams p{};

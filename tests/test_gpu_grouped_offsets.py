@@ -50,6 +50,30 @@ def test_products_of_no_terms(hif4, product):  # noqa: F811
     assert bool((c[:8] == 0.0).all()) and bool((c[8:] == 9.0).all())
 
 
+@pytest.mark.parametrize("N,K", [(130, 256), (512, 2816), (100, 192)])
+@pytest.mark.parametrize("cap", [1, 100, 257, 599])
+def test_fewer_rows_than_assignments(hif4, product, N, K, cap):  # noqa: F811
+    """Rows up to a capacity: assignments past it have no row, and the offsets that count them reach no memory behind the rows."""
+    g = gen(N + cap)
+    G, T, k = 7, 300, 2
+    x = torch.randn(T, K, generator=g, device="cuda").to(torch.bfloat16)
+    b = hif4.hif4_quantize(torch.randn(G * N, K, generator=g, device="cuda")).view(G, N, K // 64, 36)
+    off, row_of = hif4.hif4_expert_plan(torch.randint(0, G, (T, k), generator=g, device="cuda", dtype=torch.int32), G)
+    pool = torch.full((cap + 300, K // 64, 36), 255, dtype=torch.uint8, device="cuda")          # NaN units behind the rows
+    a = hif4.hif4_dispatch(x, row_of, fmt=hif4.HIF4_FMT_HIF4, out=pool[:cap])
+    A, B = hif4.hif4_dequantize(a, torch.float32).double(), hif4.hif4_dequantize(b.view(G * N, K // 64, 36), torch.float32).double().view(G, N, K)
+    c = torch.full((cap + 300, N), 9.0, device="cuda")
+    for offsets in (off, torch.cat([torch.tensor([-5], device="cuda"), off[1:-1], torch.tensor([2 ** 40], device="cuda")])):
+        c.fill_(9.0)
+        product(a, b, offsets, c[:cap])
+        for n in range(G):
+            rows = slice(min(cap, int(off[n])), min(cap, int(off[n + 1])))
+            want, size = A[rows] @ B[n].t(), A[rows].abs() @ B[n].abs().t()
+            assert bool(((c[rows].double() - want).abs() <= 1e-5 * size + 1e-300).all())
+        assert bool((c[cap:] == 9.0).all())
+    assert hif4.hif4_last_device_status() == 0
+
+
 def layer(hif4, x, logits, up, down, k, E, N):  # noqa: F811
     """Routing, HiF4 rows, two grouped products around an activation, their sum: nothing is read back."""
     ids, w = hif4.hif4_route(logits, k)
