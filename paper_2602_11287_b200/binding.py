@@ -148,6 +148,8 @@ def hif4_packed_bytes(rows: int, cols: int) -> int:
 def hif4_quantize(src: torch.Tensor, mode: int = HIF4_RNE, out: Optional[torch.Tensor] = None,
                   stream=None) -> torch.Tensor:
     """[rows, cols] BF16/FP32 (row stride = src.stride(0)) -> uint8 units [rows, cols // 64, 36]."""
+    if stream is not None:
+        return _under(stream, hif4_quantize, locals())
     _need_cuda(src, out)
     assert src.dim() == 2 and src.stride(1) == 1
     rows, cols = src.shape
@@ -163,6 +165,8 @@ def hif4_quantize(src: torch.Tensor, mode: int = HIF4_RNE, out: Optional[torch.T
 def hif4_quantize_transposed(src: torch.Tensor, mode: int = HIF4_RNE, out: Optional[torch.Tensor] = None,
                              stream=None) -> torch.Tensor:
     """[rows, cols] BF16 / FP32 / FP16 -> uint8 units [cols, rows // 64, 36]: the units of src.T without transposing."""
+    if stream is not None:
+        return _under(stream, hif4_quantize_transposed, locals())
     _need_cuda(src, out)
     assert src.dim() == 2 and src.stride(1) == 1
     rows, cols = src.shape
@@ -178,6 +182,8 @@ def hif4_quantize_transposed(src: torch.Tensor, mode: int = HIF4_RNE, out: Optio
 def hif4_dequantize(units: torch.Tensor, dtype: torch.dtype = torch.bfloat16, out: Optional[torch.Tensor] = None,
                     stream=None) -> torch.Tensor:
     """uint8 units [rows, upr, 36] -> [rows, upr * 64] of `dtype` (Eq. 2)."""
+    if stream is not None:
+        return _under(stream, hif4_dequantize, locals())
     _need_cuda(units, out)
     assert units.dtype == torch.uint8 and units.dim() == 3 and units.shape[2] == UNIT_BYTES and units.is_contiguous()
     rows, upr, _ = units.shape
@@ -200,6 +206,8 @@ def hif4_gemm_workspace(M: int, N: int, K: int) -> int:
 def hif4_gemm(a_units: torch.Tensor, b_units: torch.Tensor, out: Optional[torch.Tensor] = None,
               workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """C[M, N] (FP32) = A[M, K] @ B[N, K]^T on HiF4 units ([M, K/64, 36] and [N, K/64, 36])."""
+    if stream is not None:
+        return _under(stream, hif4_gemm, locals())
     _need_cuda(a_units, b_units, out, workspace)
     assert a_units.dtype == torch.uint8 and b_units.dtype == torch.uint8
     assert a_units.dim() == 3 and b_units.dim() == 3 and a_units.shape[1] == b_units.shape[1]
@@ -230,6 +238,8 @@ def hif4_linear(x: torch.Tensor, w_units: torch.Tensor, out: Optional[torch.Tens
                 workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """Y[M, N] (FP32) = HiF4(X[M, K]) @ W[N, K]^T: activations quantized on the fly (Algorithm 1), weights
     given as HiF4 units [N, K/64, 36]."""
+    if stream is not None:
+        return _under(stream, hif4_linear, locals())
     _need_cuda(x, w_units, out, workspace)
     assert x.dim() == 2 and x.stride(1) == 1 and w_units.dtype == torch.uint8 and w_units.dim() == 3
     assert w_units.is_contiguous() and w_units.shape[2] == UNIT_BYTES
@@ -263,6 +273,8 @@ def hif4_grouped_gemm(a_units: torch.Tensor, b_units: torch.Tensor, group_offset
     """Per group g: C[off[g]:off[g+1]] = A[off[g]:off[g+1]] @ B[g]^T; B is [G, N, K/64, 36] and
     `group_offsets` a device int64 tensor of G+1 prefix sums, clamped to the rows.  Rows behind the last group (where
     assignments have been dropped) are left as they are (undefined without out)."""
+    if stream is not None:
+        return _under(stream, hif4_grouped_gemm, locals())
     _need_cuda(a_units, b_units, group_offsets, out, workspace)
     assert a_units.dtype == torch.uint8 and b_units.dtype == torch.uint8 and group_offsets.dtype == torch.int64
     assert a_units.dim() == 3 and b_units.dim() == 4 and a_units.shape[1] == b_units.shape[2]
@@ -326,6 +338,8 @@ def hif4_mse_roundtrip(src: torch.Tensor, fmt: int, want_image: bool = True, wor
                        stream=None):
     """BF16 tensor -> (FP32 image after a round trip through the 4-bit format `fmt` or None, one-element FP64 device
     tensor holding the summed squared error): the quantization-error experiment of Section III-A."""
+    if stream is not None:
+        return _under(stream, hif4_mse_roundtrip, locals())
     _need_cuda(src, workspace)
     assert src.dtype == torch.bfloat16 and src.is_contiguous()
     n = src.numel()
